@@ -509,6 +509,120 @@ const char* hccl_last_cuda_error(void); /* text of the last CUDA failure seen by
 int hccl_version(void);
 
 /* ------------------------------------------------------------------------
+ * Expert layers: the operators on either side of the AllToAllv that carries tokens to their experts. Device-
+ * triggered inference fuses exactly this pair (a routing kernel that produces the counts, and the exchange they
+ * size; Sec. IV-B.2, IV-B.3); here the counts that hccl_route writes can be a row of the count matrix of
+ * hccl_plan_alltoallv_dynamic.
+ *
+ * All calls below are asynchronous on `stream`, keep no state between calls, allocate nothing and may be captured in
+ * a CUDA graph. Matrices are row-major with the stated distance between rows (ld*, in elements); any distance
+ * and any element-aligned base address is legal unless said otherwise. Types: hccl_dtype_t. Sums, statistics and
+ * scores are FP32 or 32-bit integers. No call uses atomics on floating-point data: results repeat bit for bit.
+ * Zero tokens or rows are legal and launch what little is left to do.
+ * ------------------------------------------------------------------------ */
+#define HCCL_MAX_EXPERTS 1024
+#define HCCL_MAX_TOP_K 32
+
+typedef enum { HCCL_SCORE_SOFTMAX = 0, HCCL_SCORE_SIGMOID = 1 } hccl_score_t;
+
+/* How tokens choose experts. score s = softmax(l) over the experts, or sigmoid(l) for each. The choice goes by key
+ * = s + bias (softmax without bias: by l itself, whose order is the same and which no rounding ties). With
+ * groups > 1 the experts form equal consecutive groups; a group's score is the sum of its group_best (1 or 2) largest
+ * keys, and only experts of the top_groups best groups stay eligible. The top_k largest keys win; ties go to the
+ * lowest index, of groups and of experts. Weights: w = s of the chosen, divided by their sum if renormalise, times scale. */
+typedef struct {
+    int32_t experts;     /* 1 .. HCCL_MAX_EXPERTS */
+    int32_t top_k;       /* 1 .. min(experts, HCCL_MAX_TOP_K) */
+    int32_t score;       /* hccl_score_t */
+    int32_t groups;      /* 0 or 1: none; must divide experts */
+    int32_t top_groups;  /* 1 .. groups */
+    int32_t group_best;  /* 1 or 2 */
+    int32_t renormalise;
+    float scale;
+} hccl_router_t;
+
+/* The outcome, in caller-owned device memory; dispatch, combine and the grouped product read it.
+ * "Row" means a row in expert order: rows of expert e are [offsets[e], offsets[e+1]), tokens ascending in each. */
+typedef struct {
+    int64_t tokens;
+    int32_t top_k, experts;
+    int32_t* ids;      /* [tokens, top_k] expert, best first; -1: none */
+    float* weights;    /* [tokens, top_k]; 0 where ids is -1 */
+    int64_t* counts;   /* [experts] rows of each expert */
+    int32_t* offsets;  /* [experts + 1] */
+    int32_t* slots;    /* [tokens, top_k] row of this choice, -1: none */
+    int32_t* source;   /* [tokens * top_k] t * top_k + k of the choice a row belongs to, -1 from offsets[experts] on */
+} hccl_routing_t;
+
+/* Route tokens. logits [tokens, experts]; bias (FP32 [experts]) and token_mask (uint8 [tokens], 0 = padding) may be
+ * NULL. Who is left out: a token whose mask is 0 (its logits are not read); an expert whose bias is -inf (its logits
+ * are not looked at, and are in no softmax sum); an expert whose logit is -inf, for that token. A token with fewer
+ * eligible experts than top_k gets ids -1 and weights 0 in the places left over; one with none gets them everywhere.
+ * A token that cannot be scored (an eligible logit or bias is NaN, a bias is +inf, or a logit is +inf under softmax) gets ids -1 and weights NaN.
+ * Chosen scores that are all 0 keep weight 0 when renormalised. tokens * top_k < 2^31.
+ * Workspace: hccl_route_workspace_bytes, 16-byte aligned, contents arbitrary; not shared by calls in flight at once. */
+hccl_status_t hccl_route_workspace_bytes(const hccl_router_t*, int64_t tokens, size_t* bytes);
+hccl_status_t hccl_route(const hccl_router_t*, const void* logits, int64_t ld, hccl_dtype_t dt, const float* bias,
+                         const uint8_t* token_mask, const hccl_routing_t* out, void* workspace, size_t bytes, void* stream);
+
+/* Gradient of the logits for a gradient dweights (FP32 [tokens, top_k]) of the weights. The choice itself has no gradient.
+ * Reads routing->ids only; scores are formed again from the logits. Every element of dlogits is written, zeros for
+ * what was left out and for tokens that chose nothing; NaN for tokens that could not be scored. */
+hccl_status_t hccl_route_backward(const hccl_router_t*, const void* logits, int64_t ld, hccl_dtype_t dt, const float* bias,
+                                  const uint8_t* token_mask, const hccl_routing_t* routing, const float* dweights,
+                                  void* dlogits, int64_t ldd, void* stream);
+
+/* Dispatch: rows[slots[t,k]] = x[t] for every choice. n_rows is the capacity of `rows`; a choice whose slot does
+ * not fit is dropped, rows that no choice fills, from offsets[experts] to n_rows, are set to zero.
+ * Backward: dx[t] = sum over k of drows[slots[t,k]], summed in FP32 in the order of k and rounded once. x [tokens, H]. */
+hccl_status_t hccl_dispatch(const void* x, int64_t ldx, int64_t H, hccl_dtype_t dt, const hccl_routing_t* routing, void* rows,
+                            int64_t ldr, int64_t n_rows, void* stream);
+hccl_status_t hccl_dispatch_backward(const void* drows, int64_t ldr, int64_t n_rows, int64_t H, hccl_dtype_t dt,
+                                     const hccl_routing_t* routing, void* dx, int64_t ldx, void* stream);
+
+/* Combine: y[t] = sum over k of weights[t,k] * rows[slots[t,k]], in FP32 in the order of k, rounded once. A choice
+ * without a row (slot -1, or not below n_rows) adds nothing, whatever its weight; a token without rows gets 0.
+ * Backward: drows[slots[t,k]] = weights[t,k] * dy[t] and dweights[t,k] = <dy[t], rows[slots[t,k]]> (0 without a row);
+ * rows that no choice fills get 0. weights: FP32 [tokens, top_k] (routing->weights or any other). */
+hccl_status_t hccl_combine(const void* rows, int64_t ldr, int64_t n_rows, int64_t H, hccl_dtype_t dt, const hccl_routing_t* routing,
+                           const float* weights, void* y, int64_t ldy, void* stream);
+hccl_status_t hccl_combine_backward(const void* dy, int64_t ldy, const void* rows, int64_t ldr, int64_t n_rows, int64_t H,
+                                    hccl_dtype_t dt, const hccl_routing_t* routing, const float* weights, void* drows,
+                                    int64_t ldd, float* dweights, void* stream);
+
+/* 8-bit rows: scale[m] = max|x[m]| / 127, q[m] = round-half-even(x[m] * (127 / max|x[m]|)) in FP32. Rows below 1e-30 in every
+ * element become zeros with scale 0; a row with an infinity or a NaN gets scale NaN. K <= HCCL_MAX_I8_K; columns K .. ldq-1 of q are
+ * left alone. routing NULL: M rows of x to M rows of q. Otherwise M must be routing->tokens and row t is written to
+ * every slots[t,k] below n_q (the 8-bit form of hccl_dispatch, for half the bytes in the exchange). */
+#define HCCL_MAX_I8_K 131071 /* 128 * 128 * K stays below 2^31 */
+hccl_status_t hccl_quantize_rows_i8(const void* x, int64_t ldx, int64_t M, int64_t K, hccl_dtype_t dt, const hccl_routing_t* routing,
+                                    int8_t* q, int64_t ldq, int64_t n_q, float* scale, void* stream);
+
+/* Products in 8-bit integers: y[m,n] = round(float(sum_k a[m,k] * w[g,n,k]) * a_scale[m] * w_scale[g,n] (+ bias[g,n])), the sum
+ * exact in 32-bit integers. groups 0: one matrix for all M rows. groups > 0: row m belongs to group g when
+ * offsets[g] <= m < offsets[g+1] (device memory, ascending, at most M; rows outside all groups are left alone), and a group without rows costs nothing.
+ * a and w must start on 16-byte boundaries with lda and ldw multiples of 16; row n of group g starts at
+ * w + (g * N + n) * ldw. y: any stride, type dt. dev_status: one device int32 or NULL; a failure on the device
+ * (a bounded wait that ran out, HCCL_ERR_TIMEOUT) is stored there and y is then undefined; nothing is stored otherwise. */
+typedef struct {
+    int64_t M, N, K;
+    int32_t groups;
+    int32_t dtype; /* of y */
+    const int8_t* a; int64_t lda; const float* a_scale;
+    const int8_t* w; int64_t ldw; const float* w_scale;
+    const float* bias;        /* NULL: none */
+    const int32_t* offsets;   /* [groups + 1], NULL when groups is 0 */
+    void* y; int64_t ldy;
+    int32_t* dev_status;
+} hccl_matmul_i8_t;
+hccl_status_t hccl_matmul_i8(const hccl_matmul_i8_t*, void* stream);
+
+/* The same on rows of 16- or 32-bit data, which are quantised within the call (hccl_quantize_rows_i8 into a and a_scale, here
+ * scratch of the caller's; then the product): y[m] = x[m] W^T, or, with a routing, y[row] = x[source[row] / top_k] W[e]^T for the rows of each
+ * expert e (groups = routing->experts, offsets = routing->offsets, M the rows of y and of the scratch). */
+hccl_status_t hccl_linear_i8(const hccl_matmul_i8_t*, const void* x, int64_t ldx, hccl_dtype_t x_dt, const hccl_routing_t* routing, void* stream);
+
+/* ------------------------------------------------------------------------
  * Plan verification on the host (debugging aids for schedules; never part of hccl_execute).
  * ------------------------------------------------------------------------ */
 

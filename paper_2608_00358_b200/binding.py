@@ -27,6 +27,8 @@ HINT_READ_ONCE, HINT_LAST_READ_A = 1, 2
 MAX_RANKS = 256
 NOALLOC_WORKSPACE_BYTES = 8 << 20
 ELEM_BYTES = {FP32: 4, BF16: 2, FP16: 2}
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+MAX_EXPERTS, MAX_TOP_K, MAX_I8_K = 1024, 32, 131071
 
 
 class Opts(C.Structure):
@@ -56,6 +58,25 @@ class PlanInfo(C.Structure):
                 ("epoch", C.c_int64), ("crossrack_bytes", C.c_int64), ("static_chains", C.c_int64)]
 
 
+class RouterConfig(C.Structure):
+    """hccl_router_t"""
+    _fields_ = [("experts", C.c_int32), ("top_k", C.c_int32), ("score", C.c_int32), ("groups", C.c_int32), ("top_groups", C.c_int32),
+                ("group_best", C.c_int32), ("renormalise", C.c_int32), ("scale", C.c_float)]
+
+
+class RoutingRecord(C.Structure):
+    """hccl_routing_t"""
+    _fields_ = [("tokens", C.c_int64), ("top_k", C.c_int32), ("experts", C.c_int32), ("ids", C.c_void_p), ("weights", C.c_void_p),
+                ("counts", C.c_void_p), ("offsets", C.c_void_p), ("slots", C.c_void_p), ("source", C.c_void_p)]
+
+
+class MatmulI8(C.Structure):
+    """hccl_matmul_i8_t"""
+    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("groups", C.c_int32), ("dtype", C.c_int32), ("a", C.c_void_p),
+                ("lda", C.c_int64), ("a_scale", C.c_void_p), ("w", C.c_void_p), ("ldw", C.c_int64), ("w_scale", C.c_void_p),
+                ("bias", C.c_void_p), ("offsets", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("dev_status", C.c_void_p)]
+
+
 class HcclError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -69,6 +90,7 @@ def _load() -> C.CDLL:
     path = _build.build()
     lib = C.CDLL(path)
     P, I64P = C.c_void_p, C.POINTER(C.c_int64)
+    RT, RG = C.POINTER(RouterConfig), C.POINTER(RoutingRecord)
     sigs = {
         "hccl_plan_allreduce": [C.c_int, C.c_int64, C.c_int, C.c_int, C.POINTER(Opts), C.POINTER(P)],
         "hccl_plan_reducescatter": [C.c_int, I64P, C.c_int64, C.c_int, C.c_int, C.POINTER(Opts), C.POINTER(P)],
@@ -104,6 +126,16 @@ def _load() -> C.CDLL:
         "hccl_hostpipe_bind": [P, P, C.c_size_t, P],
         "hccl_hostpipe_execute": [P, C.POINTER(P), C.POINTER(P), C.POINTER(P), C.POINTER(P), P, P, P],
         "hccl_hostpipe_status": [P, C.POINTER(C.c_int), I64P],
+        "hccl_route_workspace_bytes": [RT, C.c_int64, C.POINTER(C.c_size_t)],
+        "hccl_route": [RT, P, C.c_int64, C.c_int, P, P, RG, P, C.c_size_t, P],
+        "hccl_route_backward": [RT, P, C.c_int64, C.c_int, P, P, RG, P, P, C.c_int64, P],
+        "hccl_dispatch": [P, C.c_int64, C.c_int64, C.c_int, RG, P, C.c_int64, C.c_int64, P],
+        "hccl_dispatch_backward": [P, C.c_int64, C.c_int64, C.c_int64, C.c_int, RG, P, C.c_int64, P],
+        "hccl_combine": [P, C.c_int64, C.c_int64, C.c_int64, C.c_int, RG, P, P, C.c_int64, P],
+        "hccl_combine_backward": [P, C.c_int64, P, C.c_int64, C.c_int64, C.c_int64, C.c_int, RG, P, P, C.c_int64, P, P],
+        "hccl_quantize_rows_i8": [P, C.c_int64, C.c_int64, C.c_int64, C.c_int, RG, P, C.c_int64, C.c_int64, P, P],
+        "hccl_matmul_i8": [C.POINTER(MatmulI8), P],
+        "hccl_linear_i8": [C.POINTER(MatmulI8), P, C.c_int64, C.c_int, RG, P],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -137,7 +169,9 @@ EXPORTS = ["hccl_plan_allreduce", "hccl_plan_reducescatter", "hccl_plan_allgathe
            "hccl_plan_extents", "hccl_plan_layout", "hccl_plan_destroy", "hccl_status_string", "hccl_last_cuda_error", "hccl_version",
            "hccl_plan_check_hazards", "hccl_plan_interpret_host",
            "hccl_hostpipe_alltoallv_create", "hccl_hostpipe_windows", "hccl_hostpipe_workspace_bytes", "hccl_hostpipe_bind",
-           "hccl_hostpipe_execute", "hccl_hostpipe_status", "hccl_hostpipe_destroy", "hccl_opts_for_overlap"]
+           "hccl_hostpipe_execute", "hccl_hostpipe_status", "hccl_hostpipe_destroy", "hccl_opts_for_overlap",
+           "hccl_route_workspace_bytes", "hccl_route", "hccl_route_backward", "hccl_dispatch", "hccl_dispatch_backward", "hccl_combine",
+           "hccl_combine_backward", "hccl_quantize_rows_i8", "hccl_matmul_i8", "hccl_linear_i8"]
 
 
 def status_string(status: int) -> str:
@@ -313,6 +347,35 @@ def hccl_plan_alltoallv_dynamic(R: int, max_send_rows, max_recv_rows, dt: int = 
     h = C.c_void_p()
     return _new_plan(_lib.hccl_plan_alltoallv_dynamic(R, _i64(max_send_rows), _i64(max_recv_rows), dt, row_elems,
                                                       C.byref(make_opts(opts)), C.byref(h)), h, "hccl_plan_alltoallv_dynamic")
+
+
+# Expert layers: the C calls as they are, pointers as integers (0: NULL); each raises HcclError on a refusal.
+def _call(name):
+    fn = getattr(_lib, name)
+
+    def call(*args):
+        rc = fn(*args)
+        if rc != OK:
+            raise HcclError(rc, name)
+    call.__name__ = name
+    return call
+
+
+hccl_route = _call("hccl_route")
+hccl_route_backward = _call("hccl_route_backward")
+hccl_dispatch = _call("hccl_dispatch")
+hccl_dispatch_backward = _call("hccl_dispatch_backward")
+hccl_combine = _call("hccl_combine")
+hccl_combine_backward = _call("hccl_combine_backward")
+hccl_quantize_rows_i8 = _call("hccl_quantize_rows_i8")
+hccl_matmul_i8 = _call("hccl_matmul_i8")
+hccl_linear_i8 = _call("hccl_linear_i8")
+
+
+def hccl_route_workspace_bytes(router: RouterConfig, tokens: int) -> int:
+    n = C.c_size_t()
+    _chk(_lib.hccl_route_workspace_bytes(C.byref(router), tokens, C.byref(n)), "hccl_route_workspace_bytes")
+    return n.value
 
 
 class HostPipe:

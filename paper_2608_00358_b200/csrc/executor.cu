@@ -20,6 +20,9 @@ hccl_status_t cuda_fail(cudaError_t e, const char* what) {
     } while (0)
 }  // namespace
 
+// For the library's other C entry points (experts.cu): one text per thread, whichever call failed.
+hccl_status_t hccl::note_cuda_error(cudaError_t e, const char* what) { return cuda_fail(e, what); }
+
 extern "C" {
 
 const char* hccl_last_cuda_error(void) { return g_cuda_err; }

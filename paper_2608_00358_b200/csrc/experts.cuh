@@ -1,0 +1,108 @@
+// Kernels of the expert-layer operators (routing, exchange of rows, products in 8-bit integers): parameter records,
+// launchers, and the few device helpers that they share. experts.cu holds the C entry points and their checks.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/hccl.h"
+
+namespace hccl {
+namespace experts {
+
+constexpr int SMS = 148;
+
+// ---------------------------------------------------------------- element access
+template <typename T> __device__ __forceinline__ float to_f32(T v);
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);  // one rounding to nearest even
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+// A piece of a row: BYTES at once (16, 8, 4, or one element).
+template <int BYTES> struct Piece;
+template <> struct Piece<16> { using type = uint4; };
+template <> struct Piece<8> { using type = uint2; };
+template <> struct Piece<4> { using type = unsigned int; };
+template <> struct Piece<2> { using type = unsigned short; };
+
+template <typename T, int N> union Pack {
+    typename Piece<N * sizeof(T)>::type raw;
+    T v[N];
+    __device__ __forceinline__ Pack() {}
+};
+
+// ---------------------------------------------------------------- routing
+struct RouteParams {
+    const void* logits;
+    const float* bias;
+    const uint8_t* mask;
+    long long ld, tokens;
+    int E, K, groups, per_group, top_groups, group_best, sigmoid, renorm;
+    float scale;
+    int chunk;   // tokens per block
+    int blocks;
+    int* ids;
+    float* weights;
+    long long* counts;
+    int *offsets, *slots, *source;
+    int* hist;   // [blocks][E]
+};
+
+struct RouteGradParams {
+    RouteParams r;  // logits, bias, mask, sizes, ids
+    const float* dweights;
+    void* dlogits;
+    long long ldd;
+};
+
+size_t route_workspace(int E, long long tokens);
+cudaError_t launch_route(int dt, const RouteParams& p, cudaStream_t s);
+cudaError_t launch_route_grad(int dt, const RouteGradParams& p, cudaStream_t s);
+
+// ---------------------------------------------------------------- exchange of rows
+struct RowsParams {
+    const void* x;        // [tokens, H]: dispatch's input, combine_backward's dy
+    void* y;              // [tokens, H]: combine's output
+    const void* rows;     // [n_rows, H]
+    void* rows_out;       // [n_rows, H]
+    long long ldx, ldy, ldr, ldro, tokens, n_rows, H;
+    int K, E;
+    const int* slots;
+    const int* offsets;
+    const float* weights; // null: 1
+    float* dweights;
+};
+
+cudaError_t launch_dispatch(int dt, const RowsParams& p, cudaStream_t s);
+cudaError_t launch_combine(int dt, const RowsParams& p, cudaStream_t s);
+cudaError_t launch_combine_grad(int dt, const RowsParams& p, cudaStream_t s);
+
+// ---------------------------------------------------------------- products in 8-bit integers
+struct QuantParams {
+    const void* x;
+    long long ldx, M, K, ldq, n_q;
+    int8_t* q;
+    float* scale;
+    const int* slots;  // null: row m of x to row m of q
+    int top_k;
+};
+cudaError_t launch_quantise(int dt, const QuantParams& p, cudaStream_t s);
+
+struct MatmulParams {
+    long long M, N, K, lda, ldw, ldy;
+    int groups;  // 0: one matrix
+    const int8_t *a, *w;
+    const float *a_scale, *w_scale, *bias;
+    const int* offsets;
+    void* y;
+    int* status;
+};
+cudaError_t launch_matmul_i8(int dt, const MatmulParams& p, cudaStream_t s);
+
+}  // namespace experts
+}  // namespace hccl

@@ -6,6 +6,8 @@
 
 namespace hccl {
 
+hccl_status_t note_cuda_error(cudaError_t e, const char* what);  // records the text behind hccl_last_cuda_error
+
 struct Doorbell {                       // layout shared with hccl_doorbell_t in hccl.h
     unsigned long long request;         // host -> device: number of executions asked for so far
     unsigned long long completed;       // device -> host: executions finished

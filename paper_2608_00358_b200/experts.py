@@ -1,0 +1,443 @@
+"""Expert layers on torch tensors: routing, dispatch and combine of rows, linear layers in 8-bit integers.
+
+The operators are the C calls of include/hccl.h (``hccl_route`` and the ones after it); this module checks tensors,
+supplies outputs and workspaces, and joins the gradients to torch's autograd. Everything runs on the current stream of
+the tensors' device; nothing here computes, and there is no CPU form.
+
+    router = Router(experts=64, top_k=8, score="sigmoid", renormalise=True)
+    r = router.route(logits, bias=balance)            # who goes where, with which weight
+    y = up(x, routing=r)                              # Int8Linear over experts: rows gathered, quantised, multiplied
+    out = combine(down(act(y), offsets=r.offsets), r) # back to tokens
+
+With real exchanges between ranks, ``dispatch`` (or ``quantize_rows(x, routing=r)`` for half the bytes) lays out the send
+buffer of an AllToAllv, and ``r.counts`` is the rank's row of its count matrix when each rank holds one expert.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional
+
+import torch
+
+from . import binding as hb
+
+_DT = {torch.float32: hb.FP32, torch.bfloat16: hb.BF16, torch.float16: hb.FP16}
+_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _refuse(status: int, what: str):
+    raise hb.HcclError(status, what)
+
+
+def _matrix(t: torch.Tensor, what: str, cols: Optional[int] = None, rows: Optional[int] = None) -> int:
+    """Checks a 2-d CUDA matrix with adjacent columns; returns the distance between its rows."""
+    if not t.is_cuda:
+        _refuse(hb.ERR_INVALID_ARG, "%s must be on a CUDA device" % what)
+    if t.dim() != 2:
+        _refuse(hb.ERR_INVALID_ARG, "%s must have two dimensions, not %d" % (what, t.dim()))
+    n, m = t.shape
+    if (cols is not None and m != cols) or (rows is not None and n != rows):
+        _refuse(hb.ERR_COUNT_MISMATCH, "%s is [%d, %d], expected [%s, %s]" % (what, n, m, "any" if rows is None else rows, "any" if cols is None else cols))
+    ld, step = t.stride()
+    if step != 1 and m > 1:
+        _refuse(hb.ERR_ALIGNMENT, "%s must have adjacent columns" % what)
+    return ld if n > 1 else max(ld, m)
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    d = _DT.get(t.dtype)
+    if d is None:
+        _refuse(hb.ERR_DTYPE, "%s is %s" % (what, t.dtype))
+    return d
+
+
+def _vector(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int, device: torch.device):
+    if t.dtype != dtype:
+        _refuse(hb.ERR_DTYPE, "%s is %s, expected %s" % (what, t.dtype, dtype))
+    if t.numel() != numel:
+        _refuse(hb.ERR_COUNT_MISMATCH, "%s has %d elements, expected %d" % (what, t.numel(), numel))
+    if t.device != device or not t.is_contiguous():
+        _refuse(hb.ERR_INVALID_ARG, "%s must be contiguous and on %s" % (what, device))
+
+
+def _same(a: torch.Tensor, b: torch.Tensor, what: str):
+    if a.dtype != b.dtype:
+        _refuse(hb.ERR_DTYPE, "%s: %s and %s" % (what, a.dtype, b.dtype))
+    if a.device != b.device:
+        _refuse(hb.ERR_INVALID_ARG, "%s: %s and %s" % (what, a.device, b.device))
+
+
+def _on(device: torch.device, call, *args):
+    """call(*args, stream) with `device` current."""
+    i = device.index
+    if i == torch.cuda.current_device():
+        call(*args, _stream(i))
+    else:
+        with torch.cuda.device(i):
+            call(*args, _stream(i))
+
+
+class _Scratch:
+    """Device memory of one object, one piece for each stream it is used on: calls on different streams do not share it."""
+
+    def __init__(self):
+        self._of = {}
+
+    def get(self, device: torch.device, nbytes: int) -> torch.Tensor:
+        key = (device.index, _stream(device.index))
+        t = self._of.get(key)
+        if t is None or t.numel() < nbytes:
+            t = self._of[key] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return t
+
+
+class Routing:
+    """Which token goes to which expert (hccl_routing_t), as tensors: ids, weights, slots [tokens, top_k]; counts [experts];
+    offsets [experts + 1]; source [tokens * top_k]. Rows of expert e, in expert order, are offsets[e]:offsets[e + 1]."""
+
+    __slots__ = ("ids", "weights", "counts", "offsets", "slots", "source", "tokens", "top_k", "experts", "device", "record", "ref")
+
+    def __init__(self, ids, weights, counts, offsets, slots, source):
+        if ids.dim() != 2 or not ids.is_cuda:
+            _refuse(hb.ERR_INVALID_ARG, "Routing: ids must be a CUDA tensor [tokens, top_k]")
+        self.tokens, self.top_k = ids.shape
+        self.experts, self.device = counts.numel(), ids.device
+        n = self.tokens * self.top_k
+        for t, what, dt, numel in ((ids, "ids", torch.int32, n), (weights, "weights", torch.float32, n), (counts, "counts", torch.int64, self.experts),
+                                   (offsets, "offsets", torch.int32, self.experts + 1), (slots, "slots", torch.int32, n),
+                                   (source, "source", torch.int32, n)):
+            _vector(t, what, dt, numel, self.device)
+        self.ids, self.weights, self.counts, self.offsets, self.slots, self.source = ids, weights, counts, offsets, slots, source
+        self.record = hb.RoutingRecord(self.tokens, self.top_k, self.experts, ids.data_ptr(), weights.data_ptr(), counts.data_ptr(),
+                                       offsets.data_ptr(), slots.data_ptr(), source.data_ptr())
+        self.ref = C.byref(self.record)
+
+
+class Router:
+    """How tokens choose experts (hccl_router_t). score "softmax" or "sigmoid"; groups > 1: only the experts of the top_groups best
+    groups are eligible, a group's score being the sum of its group_best (1 or 2) largest keys."""
+
+    def __init__(self, experts: int, top_k: int, score: str = "softmax", groups: int = 1, top_groups: int = 1, group_best: int = 1,
+                 renormalise: bool = True, scale: float = 1.0):
+        if score not in ("softmax", "sigmoid"):
+            _refuse(hb.ERR_INVALID_ARG, "Router: score %r" % (score,))
+        self.config = hb.RouterConfig(experts, top_k, hb.SCORE_SIGMOID if score == "sigmoid" else hb.SCORE_SOFTMAX, groups, top_groups, group_best,
+                                      1 if renormalise else 0, scale)
+        hb.hccl_route_workspace_bytes(self.config, 0)  # refuses a configuration that does not hold together
+        self.experts, self.top_k = experts, top_k
+        self._ref = C.byref(self.config)
+        self._scratch = _Scratch()
+        self._need = {}  # workspace bytes by number of tokens
+
+    def outputs(self, tokens: int, device="cuda") -> Routing:
+        """Memory for one routing of `tokens` tokens, to be given as out=."""
+        n, i32 = (tokens, self.top_k), dict(dtype=torch.int32, device=device)
+        return Routing(torch.empty(n, **i32), torch.empty(n, dtype=torch.float32, device=device),
+                       torch.empty(self.experts, dtype=torch.int64, device=device), torch.empty(self.experts + 1, **i32),
+                       torch.empty(n, **i32), torch.empty(tokens * self.top_k, **i32))
+
+    def _inputs(self, logits, bias, token_mask):
+        ld = _matrix(logits, "logits", cols=self.experts)
+        dt = _dtype(logits, "logits")
+        if bias is not None:
+            _vector(bias, "bias", torch.float32, self.experts, logits.device)
+        if token_mask is not None:
+            if token_mask.dtype == torch.bool:
+                token_mask = token_mask.view(torch.uint8)
+            _vector(token_mask, "token_mask", torch.uint8, logits.shape[0], logits.device)
+        return ld, dt, (bias.data_ptr() if bias is not None else None), (token_mask.data_ptr() if token_mask is not None else None)
+
+    def _run(self, logits, bias, token_mask, out):
+        ld, dt, b, m = self._inputs(logits, bias, token_mask)
+        if out.tokens != logits.shape[0] or out.experts != self.experts or out.top_k != self.top_k:
+            _refuse(hb.ERR_COUNT_MISMATCH, "route: out is for %d tokens, %d experts, top %d" % (out.tokens, out.experts, out.top_k))
+        if out.device != logits.device:
+            _refuse(hb.ERR_INVALID_ARG, "route: out is on %s" % out.device)
+        need = self._need.get(out.tokens)
+        if need is None:
+            need = self._need[out.tokens] = max(hb.hccl_route_workspace_bytes(self.config, out.tokens), 16)
+        ws = self._scratch.get(logits.device, need)
+        _on(logits.device, hb.hccl_route, self._ref, logits.data_ptr(), ld, dt, b, m, out.ref, ws.data_ptr(), need)
+
+    def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, token_mask: Optional[torch.Tensor] = None,
+              out: Optional[Routing] = None) -> Routing:
+        """logits [tokens, experts]; bias fp32 [experts], added to the scores for the choice only; token_mask [tokens], 0 or False for padding.
+        With gradients enabled and logits that require them, the result's weights carry the graph."""
+        if logits.requires_grad and torch.is_grad_enabled():
+            if out is not None:
+                _refuse(hb.ERR_INVALID_ARG, "route: out= cannot carry a gradient")
+            out = self.outputs(logits.shape[0], logits.device)
+            w = _Route.apply(logits, self, bias, token_mask, out)
+            return Routing(out.ids, w, out.counts, out.offsets, out.slots, out.source)
+        if out is None:
+            out = self.outputs(logits.shape[0], logits.device)
+        self._run(logits, bias, token_mask, out)
+        return out
+
+    def backward(self, logits: torch.Tensor, routing: Routing, dweights: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                 token_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Gradient of the logits for a gradient of the weights (fp32 [tokens, top_k])."""
+        ld, dt, b, m = self._inputs(logits, bias, token_mask)
+        if routing.tokens != logits.shape[0] or routing.device != logits.device:
+            _refuse(hb.ERR_COUNT_MISMATCH, "route backward: routing of %d tokens on %s" % (routing.tokens, routing.device))
+        _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, logits.device)
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        _same(out, logits, "route backward")
+        ldd = _matrix(out, "dlogits", cols=self.experts, rows=routing.tokens)
+        _on(logits.device, hb.hccl_route_backward, self._ref, logits.data_ptr(), ld, dt, b, m, routing.ref, dweights.data_ptr(), out.data_ptr(), ldd)
+        return out
+
+
+class _Route(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, router, bias, token_mask, out):
+        router._run(logits, bias, token_mask, out)
+        ctx.save_for_backward(logits, bias, token_mask, out.ids)
+        ctx.router, ctx.routing = router, out
+        return out.weights
+
+    @staticmethod
+    def backward(ctx, dweights):
+        logits, bias, token_mask, _ = ctx.saved_tensors
+        return ctx.router.backward(logits, ctx.routing, dweights.contiguous(), bias, token_mask), None, None, None, None
+
+
+def _rows_in(rows: torch.Tensor, routing: Routing, what: str):
+    ld = _matrix(rows, what)
+    if rows.device != routing.device:
+        _refuse(hb.ERR_INVALID_ARG, "%s is on %s, the routing on %s" % (what, rows.device, routing.device))
+    return ld, _dtype(rows, what)
+
+
+def _new(out, shape, like, what):
+    if out is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device)
+    _same(out, like, what)
+    return out
+
+
+def _dispatch(x, routing, out, n_rows):
+    ldx, dt = _rows_in(x, routing, "x")
+    if x.shape[0] != routing.tokens:
+        _refuse(hb.ERR_COUNT_MISMATCH, "dispatch: %d tokens, the routing has %d" % (x.shape[0], routing.tokens))
+    H = x.shape[1]
+    out = _new(out, (routing.tokens * routing.top_k if n_rows is None else n_rows, H), x, "dispatch")
+    ldr = _matrix(out, "rows", cols=H)
+    _on(x.device, hb.hccl_dispatch, x.data_ptr(), ldx, H, dt, routing.ref, out.data_ptr(), ldr, out.shape[0])
+    return out
+
+
+def dispatch(x: torch.Tensor, routing: Routing, out: Optional[torch.Tensor] = None, n_rows: Optional[int] = None) -> torch.Tensor:
+    """Rows in expert order: out[slots[t, k]] = x[t]. n_rows (default tokens * top_k): the capacity; choices beyond it are dropped."""
+    if x.requires_grad and torch.is_grad_enabled():
+        if out is not None:
+            _refuse(hb.ERR_INVALID_ARG, "dispatch: out= cannot carry a gradient")
+        return _Dispatch.apply(x, routing, n_rows)
+    return _dispatch(x, routing, out, n_rows)
+
+
+def dispatch_backward(drows: torch.Tensor, routing: Routing, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dx[t] = sum over k of drows[slots[t, k]]."""
+    ldr, dt = _rows_in(drows, routing, "drows")
+    n, H = drows.shape
+    out = _new(out, (routing.tokens, H), drows, "dispatch backward")
+    ldx = _matrix(out, "dx", cols=H, rows=routing.tokens)
+    _on(drows.device, hb.hccl_dispatch_backward, drows.data_ptr(), ldr, n, H, dt, routing.ref, out.data_ptr(), ldx)
+    return out
+
+
+def _combine(rows, routing, weights, out):
+    ldr, dt = _rows_in(rows, routing, "rows")
+    if weights is None:
+        weights = routing.weights
+    else:
+        _vector(weights, "weights", torch.float32, routing.tokens * routing.top_k, routing.device)
+    n, H = rows.shape
+    out = _new(out, (routing.tokens, H), rows, "combine")
+    ldy = _matrix(out, "y", cols=H, rows=routing.tokens)
+    _on(rows.device, hb.hccl_combine, rows.data_ptr(), ldr, n, H, dt, routing.ref, weights.data_ptr(), out.data_ptr(), ldy)
+    return out
+
+
+def combine(rows: torch.Tensor, routing: Routing, weights: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y[t] = sum over k of weights[t, k] * rows[slots[t, k]]; weights default to the routing's."""
+    if torch.is_grad_enabled() and (rows.requires_grad or (routing.weights if weights is None else weights).requires_grad):
+        if out is not None:
+            _refuse(hb.ERR_INVALID_ARG, "combine: out= cannot carry a gradient")
+        return _Combine.apply(rows, routing.weights if weights is None else weights, routing)
+    return _combine(rows, routing, weights, out)
+
+
+def combine_backward(dy: torch.Tensor, rows: torch.Tensor, routing: Routing, weights: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None):
+    """(drows, dweights) for a gradient dy of combine's result."""
+    ldr, dt = _rows_in(rows, routing, "rows")
+    n, H = rows.shape
+    ldy = _matrix(dy, "dy", cols=H, rows=routing.tokens)
+    _same(dy, rows, "combine backward")
+    if weights is None:
+        weights = routing.weights
+    else:
+        _vector(weights, "weights", torch.float32, routing.tokens * routing.top_k, routing.device)
+    out = _new(out, (n, H), rows, "combine backward")
+    ldd = _matrix(out, "drows", cols=H, rows=n)
+    dw = torch.empty((routing.tokens, routing.top_k), dtype=torch.float32, device=rows.device)
+    _on(rows.device, hb.hccl_combine_backward, dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.ref, weights.data_ptr(), out.data_ptr(), ldd,
+        dw.data_ptr())
+    return out, dw
+
+
+def _cols(t: torch.Tensor) -> torch.Tensor:
+    """Adjacent columns for a gradient that autograd hands over in any layout (an expanded one, say)."""
+    return t if t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
+
+
+class _Dispatch(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, routing, n_rows):
+        ctx.routing = routing
+        return _dispatch(x, routing, None, n_rows)
+
+    @staticmethod
+    def backward(ctx, drows):
+        return dispatch_backward(_cols(drows), ctx.routing), None, None
+
+
+class _Combine(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, rows, weights, routing):
+        ctx.save_for_backward(rows, weights)
+        ctx.routing = routing
+        return _combine(rows, routing, weights, None)
+
+    @staticmethod
+    def backward(ctx, dy):
+        rows, weights = ctx.saved_tensors
+        drows, dw = combine_backward(_cols(dy), rows, ctx.routing, weights)
+        return drows, dw.view_as(weights), None
+
+
+def _pad16(n: int) -> int:
+    return (n + 15) // 16 * 16
+
+
+def quantize_rows(x: torch.Tensor, routing: Optional[Routing] = None, n_rows: Optional[int] = None):
+    """(q, scale): 8-bit rows and a scale for each, x[m] ~ q[m] * scale[m]. With a routing the rows come in expert order (n_rows: the
+    capacity, default tokens * top_k; rows that no choice fills are left alone). q's rows start 16 bytes apart or a multiple of it."""
+    ldx = _matrix(x, "x")
+    dt = _dtype(x, "x")
+    M, K = x.shape
+    n = M if routing is None else (routing.tokens * routing.top_k if n_rows is None else n_rows)
+    if routing is not None and routing.device != x.device:
+        _refuse(hb.ERR_INVALID_ARG, "quantize_rows: the routing is on %s" % routing.device)
+    q = torch.empty((n, _pad16(K)), dtype=torch.int8, device=x.device)
+    scale = torch.empty(n, dtype=torch.float32, device=x.device)
+    _on(x.device, hb.hccl_quantize_rows_i8, x.data_ptr(), ldx, M, K, dt, routing.ref if routing is not None else None, q.data_ptr(), q.shape[1], n,
+        scale.data_ptr())
+    return q[:, :K], scale
+
+
+class Int8Linear:
+    """y = x W^T (+ bias) with W in 8-bit integers and a scale for each output channel: weight [N, K], or [experts, N, K]; scale and bias
+    (fp32) [N] or [experts, N]. The rows of x are quantised within the call, each with a scale of its own. Weights whose rows do not start
+    on 16-byte boundaries are laid out anew once, here. A result's rows beyond the last expert's are left alone. For serving: no gradient."""
+
+    def __init__(self, weight: torch.Tensor, scale: torch.Tensor, bias: Optional[torch.Tensor] = None):
+        if weight.dtype != torch.int8:
+            _refuse(hb.ERR_DTYPE, "Int8Linear: weight is %s" % weight.dtype)
+        if weight.dim() not in (2, 3) or not weight.is_cuda:
+            _refuse(hb.ERR_INVALID_ARG, "Int8Linear: weight must be a CUDA tensor [N, K] or [experts, N, K]")
+        self.experts = weight.shape[0] if weight.dim() == 3 else 0
+        self.N, self.K = weight.shape[-2:]
+        self.device = weight.device
+        rows = max(self.experts, 1) * self.N
+        _vector(scale, "scale", torch.float32, rows, self.device)
+        if bias is not None:
+            _vector(bias, "bias", torch.float32, rows, self.device)
+        if not weight.is_contiguous() or self.K % 16 or weight.data_ptr() % 16:
+            padded = torch.zeros(weight.shape[:-1] + (_pad16(self.K),), dtype=torch.int8, device=self.device)
+            padded[..., : self.K] = weight
+            weight = padded
+        self.weight, self.scale, self.bias = weight, scale, bias
+        self.ldw = weight.shape[-1]
+        self._scratch = _Scratch()
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+
+    @classmethod
+    def from_float(cls, weight: torch.Tensor, bias: Optional[torch.Tensor] = None) -> "Int8Linear":
+        """Quantises a weight matrix (or one for each expert), a scale for each output channel."""
+        q, scale = quantize_rows(weight.reshape(-1, weight.shape[-1]))
+        return cls(q.reshape(weight.shape), scale.view(weight.shape[:-1]), bias)
+
+    def _args(self, M, y, ldy, offsets):
+        if offsets is not None:
+            _vector(offsets, "offsets", torch.int32, self.experts + 1, self.device)
+        return hb.MatmulI8(M, self.N, self.K, self.experts, _DT[y.dtype], None, 0, None, self.weight.data_ptr(), self.ldw, self.scale.data_ptr(),
+                           self.bias.data_ptr() if self.bias is not None else None, offsets.data_ptr() if offsets is not None else None,
+                           y.data_ptr(), ldy, self._status.data_ptr())
+
+    def _out(self, out, M, dtype):
+        if out is None:
+            return torch.empty((M, self.N), dtype=dtype, device=self.device), self.N
+        if out.device != self.device:
+            _refuse(hb.ERR_INVALID_ARG, "Int8Linear: out is on %s" % out.device)
+        _dtype(out, "out")
+        return out, _matrix(out, "out", cols=self.N, rows=M)
+
+    def _which(self, routing, offsets):
+        if self.experts and (routing is None) == (offsets is None):
+            _refuse(hb.ERR_INVALID_ARG, "Int8Linear over experts takes a routing or offsets")
+        if not self.experts and (routing is not None or offsets is not None):
+            _refuse(hb.ERR_INVALID_ARG, "Int8Linear with one matrix takes neither a routing nor offsets")
+        if routing is not None and (routing.experts != self.experts or routing.device != self.device):
+            _refuse(hb.ERR_COUNT_MISMATCH, "Int8Linear: routing over %d experts on %s" % (routing.experts, routing.device))
+
+    def __call__(self, x: torch.Tensor, routing: Optional[Routing] = None, offsets: Optional[torch.Tensor] = None,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x [M, K]. Over experts: with a routing, x holds tokens and row r of the result belongs to choice source[r]; with offsets (int32
+        [experts + 1], on the device) x is in expert order already."""
+        ldx = _matrix(x, "x", cols=self.K)
+        dt = _dtype(x, "x")
+        if x.device != self.device:
+            _refuse(hb.ERR_INVALID_ARG, "Int8Linear: x is on %s" % x.device)
+        self._which(routing, offsets)
+        M, ref = x.shape[0], None
+        if routing is not None:
+            if M != routing.tokens:
+                _refuse(hb.ERR_COUNT_MISMATCH, "Int8Linear: %d tokens, the routing has %d" % (M, routing.tokens))
+            M, ref, offsets = M * routing.top_k, routing.ref, routing.offsets
+        y, ldy = self._out(out, M, x.dtype)
+        a = self._args(M, y, ldy, offsets)
+        lda = _pad16(self.K)
+        room = M * lda
+        t = self._scratch.get(self.device, room + 4 * M)
+        a.a, a.lda = t.data_ptr(), lda
+        a.a_scale = a.a + room
+        _on(self.device, hb.hccl_linear_i8, C.byref(a), x.data_ptr(), ldx, dt, ref)
+        return y
+
+    def matmul(self, q: torch.Tensor, q_scale: torch.Tensor, offsets: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        """The product alone, of rows that are in 8 bits already (quantize_rows; received from an exchange)."""
+        if q.dtype != torch.int8:
+            _refuse(hb.ERR_DTYPE, "Int8Linear: q is %s" % q.dtype)
+        lda = _matrix(q, "q", cols=self.K)
+        if q.device != self.device:
+            _refuse(hb.ERR_INVALID_ARG, "Int8Linear: q is on %s" % q.device)
+        _vector(q_scale, "q_scale", torch.float32, q.shape[0], self.device)
+        self._which(None, offsets)
+        y, ldy = self._out(out, q.shape[0], dtype)
+        a = self._args(q.shape[0], y, ldy, offsets)
+        a.a, a.lda, a.a_scale = q.data_ptr(), lda if q.shape[0] > 1 else _pad16(lda), q_scale.data_ptr()
+        _on(self.device, hb.hccl_matmul_i8, C.byref(a))
+        return y
+
+    def check(self):
+        """Synchronises and raises if a product failed on the device since the last check (its result is then undefined)."""
+        torch.cuda.synchronize(self.device)
+        st = int(self._status.item())
+        if st != hb.OK:
+            self._status.zero_()
+            raise hb.HcclError(st, "Int8Linear")

@@ -590,7 +590,7 @@ hccl_status_t hccl_combine_backward(const void* dy, int64_t ldy, const void* row
                                     hccl_dtype_t dt, const hccl_routing_t* routing, const float* weights, void* drows,
                                     int64_t ldd, float* dweights, void* stream);
 
-/* 8-bit rows: scale[m] = max|x[m]| / 127, q[m] = round-half-even(x[m] * (127 / max|x[m]|)) in FP32. Rows below 1e-30 in every
+/* 8-bit rows: scale[m] = max|x[m]| / 127, q[m] = round-half-even(x[m] * (1 / max|x[m]| * 127)), each step rounded to FP32. Rows below 1e-30 in every
  * element become zeros with scale 0; a row with an infinity or a NaN gets scale NaN. K <= HCCL_MAX_I8_K; columns K .. ldq-1 of q are
  * left alone. routing NULL: M rows of x to M rows of q. Otherwise M must be routing->tokens and row t is written to
  * every slots[t,k] below n_q (the 8-bit form of hccl_dispatch, for half the bytes in the exchange). */

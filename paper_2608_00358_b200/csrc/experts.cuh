@@ -101,6 +101,7 @@ struct MatmulParams {
     const int* offsets;
     void* y;
     int* status;
+    int dependent;  // launched behind the quantiser, which lets it start early
 };
 cudaError_t launch_matmul_i8(int dt, const MatmulParams& p, cudaStream_t s);
 

@@ -1,64 +1,427 @@
-// Product of 8-bit integers with scales for each row of both operands, sums exact in 32-bit integers.
+// Products in 8-bit integers with scales for each row of both operands, on the fifth-generation tensor cores.
+//
+// y[m, n] = (sum_k a[m, k] w[n, k]) * a_scale[m] * w_scale[n] (+ bias[n]). The weights are the instruction's 128-row operand and the
+// tokens its columns, so that one kernel serves a single token (N = 16 columns, the weights stream past them) and a
+// long prompt (N = 256); the sum is exact in 32-bit integers, in any order.
+//
+// Roles of a block (8 warps): warp 0 issues the TMA loads, warp 1 the matrix instructions, warp 2 owns the tensor memory, warps 4-7 turn
+// accumulators into results. Stages of 128 bytes of K pass from the loads to the instructions through mbarriers; two
+// accumulators let the results of one tile leave while the next is formed. Blocks stay and walk tiles; where there are
+// too few tiles for the SMs, a cluster of blocks shares a tile's K and adds its partial sums through distributed shared memory.
+#include <cuda.h>
+
 #include "experts.cuh"
 
 namespace hccl {
 namespace experts {
 namespace {
 
-constexpr int TM = 64, TN = 64, TK = 64, MM_THREADS = 256;
+constexpr int MM_THREADS = 256, CH = 128 /* channels of a tile */, KB = 128 /* bytes of K in a stage */;
+constexpr unsigned long long WAIT_NS = 2000000000ull;  // bound of every wait
 
-// One block forms 64 rows x 64 columns; each thread 4 x 4 of them, four products at a time.
-template <typename T> __global__ void __launch_bounds__(MM_THREADS) hccl_matmul_i8_simple(const __grid_constant__ MatmulParams p) {
-    __shared__ int as[TM][TK / 4 + 1], ws[TN][TK / 4 + 1];
-    // which rows: tiles are counted group by group
-    long long m0 = 0, m1 = p.M;
-    int g = 0;
-    long long tile = blockIdx.y;
+template <int TN> struct Shape {
+    static constexpr int BOX = TN < 64 ? TN : 64;  // token rows of one TMA load
+    static constexpr int STAGE = (CH + TN) * KB;
+    static constexpr int STAGES = (200 * 1024) / STAGE;
+    static constexpr int COLS = 2 * TN < 32 ? 32 : 2 * TN;  // tensor memory columns: two accumulators
+    static constexpr int SMEM = STAGES * STAGE + 1024;
+};
+
+struct TileParams {
+    CUtensorMap a, w;
+    long long ldy;
+    const float *a_scale, *w_scale, *bias;
+    const int* offsets;
+    void* y;
+    int* status;
+    int M, N, groups, k_blocks, n_tiles, splits, dependent;
+};
+
+// ---------------------------------------------------------------- instructions
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// Waits for a phase to complete. After WAIT_NS, or once another wait of this block has given up, it returns false.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
+    if (mbar_try(bar, parity)) return true;
+    const unsigned long long t0 = now_ns();
+    for (;;) {
+        for (int i = 0; i < 64; i++)
+            if (mbar_try(bar, parity)) return true;
+        if (*gave_up) return false;
+        if (now_ns() - t0 > WAIT_NS) {
+            *gave_up = 1;
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// Shared-memory operand with 128-byte rows of K in the 128-byte swizzle: groups of 8 rows lie 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <int N> __device__ __forceinline__ void tmem_load(uint32_t addr, int (&v)[N]);
+template <> __device__ __forceinline__ void tmem_load<16>(uint32_t addr, int (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
+                   "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// ---------------------------------------------------------------- tiles
+struct Tile {
+    int group, row, rows, chan;  // rows [row, row + rows) of the tokens, channels from chan on
+};
+
+// Tile t. before[g] = token tiles of the groups below g. Within a group 8 token tiles pass under one tile of channels
+// before the next, so that the blocks of a wave share both operands in the L2.
+template <int TN> __device__ __forceinline__ Tile tile_of(const TileParams& p, const int* before, int t, int* hint) {
+    Tile r;
+    int g = 0, lo = 0, hi = p.M;
     if (p.groups) {
-        for (g = 0; g < p.groups; g++) {
-            m0 = max(0ll, (long long)p.offsets[g]);
-            m1 = min(p.M, (long long)p.offsets[g + 1]);
-            const long long n = m1 > m0 ? (m1 - m0 + TM - 1) / TM : 0;
-            if (tile < n) break;
-            tile -= n;
-        }
-        if (g == p.groups) return;
+        g = *hint;
+        while (t >= before[g + 1] * p.n_tiles) g++;
+        *hint = g;
+        lo = max(0, p.offsets[g]);
+        hi = min(p.M, p.offsets[g + 1]);
     }
-    m0 += tile * TM;
-    const long long n0 = (long long)blockIdx.x * TN;
-    const int8_t* w = p.w + ((long long)g * p.N) * p.ldw;
-    int acc[4][4] = {};
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    for (long long k0 = 0; k0 < p.K; k0 += TK) {
-        for (int i = threadIdx.x; i < TM * TK; i += MM_THREADS) {
-            const int r = i / TK, c = i % TK;
-            const bool k_in = k0 + c < p.K;
-            ((int8_t*)as[r])[c] = (k_in && m0 + r < m1) ? p.a[(m0 + r) * p.lda + k0 + c] : 0;
-            ((int8_t*)ws[r])[c] = (k_in && n0 + r < p.N) ? w[(n0 + r) * p.ldw + k0 + c] : 0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int c = 0; c < TK / 4; c++)
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[i][j] = __dp4a(as[ty + 16 * i][c], ws[tx + 16 * j][c], acc[i][j]);
-        __syncthreads();
+    const int mt = p.groups ? before[g + 1] - before[g] : (p.M + TN - 1) / TN;
+    const int i = t - (p.groups ? before[g] * p.n_tiles : 0);
+    const int band = i / (8 * p.n_tiles), first = band * 8, deep = min(8, mt - first), j = i - band * 8 * p.n_tiles;
+    r.group = g;
+    r.row = lo + (first + j % deep) * TN;
+    r.rows = min(TN, hi - r.row);
+    r.chan = (j / deep) * CH;
+    return r;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int cluster_load(uint32_t addr, uint32_t rank) {
+    int v;
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.s32 %0, [a];\n}" : "=r"(v) : "r"(addr), "r"(rank) : "memory");
+    return v;
+}
+
+template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) hccl_matmul_i8_tiles(const __grid_constant__ TileParams p) {
+    using S = Shape<TN>;
+    extern __shared__ char dynamic[];
+    __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 4];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    __shared__ int before[HCCL_MAX_EXPERTS + 1];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t base = (smem_addr(dynamic) + 1023) & ~1023u;
+    const uint32_t bar0 = smem_addr(bars);
+    const auto full = [&](int s) { return bar0 + 8 * s; };
+    const auto empty = [&](int s) { return bar0 + 8 * (S::STAGES + s); };
+    const auto acc_full = [&](int b) { return bar0 + 8 * (2 * S::STAGES + b); };
+    const auto acc_empty = [&](int b) { return bar0 + 8 * (2 * S::STAGES + 2 + b); };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::STAGES; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
+        for (int b = 0; b < 2; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 4);
+        gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&p.a));
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&p.w));
     }
-    for (int i = 0; i < 4; i++)
-        for (int j = 0; j < 4; j++) {
-            const long long m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (m >= m1 || n >= p.N) continue;
-            float v = (float)acc[i][j] * p.a_scale[m] * p.w_scale[(long long)g * p.N + n];
-            if (p.bias) v += p.bias[(long long)g * p.N + n];
-            ((T*)p.y)[m * p.ldy + n] = from_f32<T>(v);
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::COLS));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (warp == 3 && p.groups) {
+        int run = 0;
+        for (int b = 0; b < p.groups; b += 32) {
+            const int g = b + lane;
+            int n = 0;
+            if (g < p.groups) n = max(0, (min(p.M, p.offsets[g + 1]) - max(0, p.offsets[g]) + TN - 1) / TN);
+            int inc = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += v;
+            }
+            if (g < p.groups) before[g] = run + inc - n;
+            run += __shfl_sync(0xffffffffu, inc, 31);
         }
+        if (lane == 0) before[p.groups] = run;
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_at;
+    const int tiles = p.n_tiles * (p.groups ? before[p.groups] : (p.M + TN - 1) / TN);
+    const int splits = p.splits, rank = (int)blockIdx.x % splits, first = (int)blockIdx.x / splits, step = (int)gridDim.x / splits;
+    const int k0 = (int)((long long)p.k_blocks * rank / splits), k1 = (int)((long long)p.k_blocks * (rank + 1) / splits);
+
+    // A step's state, kept by each role for itself
+    int it = 0, acc = 0, hint = 0;  // stages passed, tiles passed, group
+    bool waited = !p.dependent;
+    const auto rely = [&] {  // from here on reads what the kernel before this one wrote
+        if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+        waited = true;
+    };
+    const auto load_w = [&](const Tile& t, int s, int kb) { tma_load(base + s * S::STAGE, &p.w, kb * KB, t.group * p.N + t.chan, full(s)); };
+    const auto load_a = [&](const Tile& t, int s, int kb) {
+        const int boxes = (t.rows + S::BOX - 1) / S::BOX;
+        for (int i = 0; i < boxes; i++) tma_load(base + s * S::STAGE + CH * KB + i * S::BOX * KB, &p.a, kb * KB, t.row + i * S::BOX, full(s));
+    };
+    const auto stage_bytes = [&](const Tile& t) { return (uint32_t)(CH * KB + (t.rows + S::BOX - 1) / S::BOX * S::BOX * KB); };
+
+    const auto produce = [&](const Tile& t) {
+        int kb = k0;
+        if (!waited) {  // the weights do not hang on the kernel before: the first stages' share of them is under way while it runs
+            const int pre = min(k1 - k0, S::STAGES);
+            for (int i = 0; i < pre; i++) {
+                mbar_expect(full(i), stage_bytes(t));
+                load_w(t, i, k0 + i);
+            }
+            rely();
+            for (int i = 0; i < pre; i++) load_a(t, i, k0 + i);
+            kb += pre;
+            it += pre;
+        }
+        for (; kb < k1; kb++, it++) {
+            const int s = it % S::STAGES;
+            if (!mbar_wait(empty(s), ((it / S::STAGES) & 1) ^ 1, &gave_up)) return;
+            mbar_expect(full(s), stage_bytes(t));
+            load_w(t, s, kb);
+            load_a(t, s, kb);
+        }
+    };
+    const auto multiply = [&](const Tile& t) {
+        const int b = acc & 1;
+        const uint32_t cols = (uint32_t)((t.rows + 15) & ~15);
+        // 32-bit accumulators, signed 8-bit operands, both with K innermost
+        const uint32_t desc = (2u << 4) | (1u << 7) | (1u << 10) | ((cols >> 3) << 17) | ((uint32_t)(CH >> 4) << 24);
+        if (!mbar_wait(acc_empty(b), ((acc >> 1) & 1) ^ 1, &gave_up)) return;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (int kb = k0; kb < k1; kb++, it++) {
+            const int s = it % S::STAGES;
+            if (!mbar_wait(full(s), (it / S::STAGES) & 1, &gave_up)) return;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint64_t w = operand(base + s * S::STAGE), a = operand(base + s * S::STAGE + CH * KB);
+#pragma unroll
+            for (int k = 0; k < KB / 32; k++) mma_i8(tmem + b * TN, w + 2 * k, a + 2 * k, desc, (kb > k0 || k > 0) ? 1u : 0u);
+            mma_commit(empty(s));
+        }
+        mma_commit(acc_full(b));
+    };
+    const auto store = [&](const Tile& t, int chan, int row, int sum, float sa, float sw, float bias) {
+        // the sum's conversion is the one rounding that an exact product of the scales would not have: sums pass 2^24 from K = 1024 on
+        float v = __fmul_rn(__fmul_rn((float)sum, sa), sw);
+        if (p.bias) v = __fadd_rn(v, bias);
+        ((T*)p.y)[(long long)row * p.ldy + chan] = from_f32<T>(v);
+    };
+    const auto results = [&](const Tile& t) {
+        const int b = acc & 1, quarter = warp & 3, chan = t.chan + quarter * 32 + lane;
+        const bool in = chan < p.N;
+        const long long gc = (long long)t.group * p.N + chan;
+        const float sw = in ? p.w_scale[gc] : 0.f, bias = (in && p.bias) ? p.bias[gc] : 0.f;
+        const bool ok = !p.k_blocks || mbar_wait(acc_full(b), (acc >> 1) & 1, &gave_up);
+        if (!__all_sync(0xffffffffu, ok)) return;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (int c0 = 0; c0 < t.rows; c0 += 16) {
+            int v[16];
+            __syncwarp();
+            if (p.k_blocks) tmem_load<16>(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + c0, v);
+            else
+#pragma unroll
+                for (int i = 0; i < 16; i++) v[i] = 0;
+            const float mine = (lane < 16 && c0 + lane < t.rows) ? p.a_scale[t.row + c0 + lane] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const float sa = __shfl_sync(0xffffffffu, mine, i);
+                if (in && c0 + i < t.rows) store(t, chan, t.row + c0 + i, v[i], sa, sw, bias);
+            }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acc_empty(b));
+    };
+
+    if (splits == 1) {
+        if (warp == 0 && lane == 0) {
+            if (p.k_blocks)
+                for (int t = first; t < tiles && !*(volatile int*)&gave_up; t += step) produce(tile_of<TN>(p, before, t, &hint));
+        } else if (warp == 1 && lane == 0) {
+            if (p.k_blocks)
+                for (int t = first; t < tiles && !*(volatile int*)&gave_up; t += step, acc++) multiply(tile_of<TN>(p, before, t, &hint));
+        } else if (warp >= 4) {
+            rely();
+            for (int t = first; t < tiles && !*(volatile int*)&gave_up; t += step, acc++) results(tile_of<TN>(p, before, t, &hint));
+        }
+    } else {
+        // One tile at a time for the whole cluster. The partial sums go to shared memory (the stages are idle by then), column by
+        // column; then each block adds a share of the outputs over all blocks of the cluster. Every block passes every barrier, also
+        // after a wait that gave up.
+        int* part = (int*)(dynamic + (base - smem_addr(dynamic)));
+        for (int t = first; t < tiles; t += step, acc++) {
+            const Tile tile = tile_of<TN>(p, before, t, &hint);
+            if (warp == 0 && lane == 0) produce(tile);
+            if (warp == 1 && lane == 0) multiply(tile);
+            if (warp >= 4) {
+                const int b = acc & 1, quarter = warp & 3;
+                const bool ok = mbar_wait(acc_full(b), (acc >> 1) & 1, &gave_up);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (__all_sync(0xffffffffu, ok))
+                    for (int c0 = 0; c0 < tile.rows; c0 += 16) {
+                        int v[16];
+                        tmem_load<16>(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + c0, v);
+#pragma unroll
+                        for (int i = 0; i < 16; i++) part[(c0 + i) * CH + quarter * 32 + lane] = v[i];
+                    }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty(b));
+            }
+            rely();
+            __syncwarp();
+            cluster_sync();
+            const int total = tile.rows * CH, lo = (int)((long long)total * rank / splits), hi = (int)((long long)total * (rank + 1) / splits);
+            for (int i = lo + (int)threadIdx.x; i < hi; i += MM_THREADS) {
+                int sum = 0;
+                for (int r = 0; r < splits; r++) sum += cluster_load(base + 4 * i, r);
+                const int chan = tile.chan + i % CH, row = tile.row + i / CH;
+                const long long gc = (long long)tile.group * p.N + chan;
+                if (chan < p.N) store(tile, chan, row, sum, p.a_scale[row], p.w_scale[gc], p.bias ? p.bias[gc] : 0.f);
+            }
+            // what the generic proxy read and wrote here, the next tile's loads will overwrite
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            cluster_sync();
+        }
+    }
+    rely();
+    // After a wait that gave up, loads may still be in flight: wait (with a limit) for the stages that were issued.
+    if (warp == 0 && lane == 0 && *(volatile int*)&gave_up) {
+        const unsigned long long t0 = now_ns();
+        for (int i = max(0, it - S::STAGES); i < it; i++)
+            while (!mbar_try(full(i % S::STAGES), (i / S::STAGES) & 1) && now_ns() - t0 < WAIT_NS) {}
+        __nanosleep(1000000);  // and the instructions issued last, which end by themselves
+        if (p.status) *p.status = HCCL_ERR_TIMEOUT;
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::COLS));
+}
+
+// ---------------------------------------------------------------- host
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder() {
+    static const EncodeFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) f = nullptr;
+        return (EncodeFn)f;
+    }();
+    return fn;
+}
+
+// Rows of `ld` bytes of which K count; a box is 128 bytes wide. What lies beyond K or beyond the rows reads as zero.
+cudaError_t make_map(CUtensorMap* m, const void* at, long long rows, long long K, long long ld, int box_rows) {
+    const EncodeFn fn = encoder();
+    if (!fn) return cudaErrorNotSupported;
+    const long long least = (K + 15) / 16 * 16;
+    const cuuint64_t dim[2] = {(cuuint64_t)K, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)(ld > least ? ld : least)};
+    const cuuint32_t box[2] = {KB, (cuuint32_t)box_rows}, one[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(at), dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
+template <typename T, int TN> cudaError_t tiles_launch(const MatmulParams& q, int splits, cudaStream_t s) {
+    using S = Shape<TN>;
+    TileParams p = {};
+    p.ldy = q.ldy;
+    p.a_scale = q.a_scale;
+    p.w_scale = q.w_scale;
+    p.bias = q.bias;
+    p.offsets = q.offsets;
+    p.y = q.y;
+    p.status = q.status;
+    p.M = (int)q.M;
+    p.N = (int)q.N;
+    p.groups = q.groups;
+    p.k_blocks = (int)((q.K + KB - 1) / KB);
+    p.n_tiles = (int)((q.N + CH - 1) / CH);
+    p.splits = splits;
+    p.dependent = q.dependent;
+    cudaError_t e;
+    if (q.K) {
+        if ((e = make_map(&p.a, q.a, q.M, q.K, q.lda, S::BOX)) != cudaSuccess) return e;
+        if ((e = make_map(&p.w, q.w, q.N * (q.groups ? q.groups : 1), q.K, q.ldw, CH)) != cudaSuccess) return e;
+    }
+    static bool ready[64];  // by device; setting it twice does no harm
+    int dev = 0;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    if (dev >= 64 || !ready[dev]) {
+        e = cudaFuncSetAttribute(hccl_matmul_i8_tiles<T, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) ready[dev] = true;
+    }
+    const long long tiles = (long long)p.n_tiles * ((q.M + TN - 1) / TN + q.groups);  // at most, with groups
+    const long long clusters = SMS / splits;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((tiles < clusters ? tiles : clusters) * splits));
+    cfg.blockDim = dim3(MM_THREADS);
+    cfg.dynamicSmemBytes = S::SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (splits > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)splits;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        n++;
+    }
+    if (q.dependent) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        n++;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, hccl_matmul_i8_tiles<T, TN>, p);
 }
 
 template <typename T> cudaError_t matmul_launch(const MatmulParams& p, cudaStream_t s) {
-    const long long tiles = (p.M + TM - 1) / TM + p.groups;
-    hccl_matmul_i8_simple<T><<<dim3((unsigned)((p.N + TN - 1) / TN), (unsigned)tiles), MM_THREADS, 0, s>>>(p);
-    return cudaGetLastError();
+    const long long rows = p.groups ? (p.M + p.groups - 1) / p.groups : p.M;  // of a group, if they were even
+    const int k_blocks = (int)((p.K + KB - 1) / KB), n_tiles = (int)((p.N + CH - 1) / CH);
+    int splits = 1;
+    if (rows <= 64)  // few rows: the weights' bytes are the time, and all SMs are to fetch them
+        while (splits < 8 && (long long)n_tiles * splits * 2 * (p.groups ? p.groups : 1) <= SMS && splits * 2 * 4 <= k_blocks) splits *= 2;
+    if (rows <= 16) return tiles_launch<T, 16>(p, splits, s);
+    if (rows <= 32) return tiles_launch<T, 32>(p, splits, s);
+    if (rows <= 64) return tiles_launch<T, 64>(p, splits, s);
+    if (rows <= 128) return tiles_launch<T, 128>(p, 1, s);
+    return tiles_launch<T, 256>(p, 1, s);
 }
 
 }  // namespace

@@ -1,4 +1,4 @@
-// Rows to 8-bit integers with a scale for each row: scale = max|x| / 127, q = round(x * (127 / max|x|)). One block holds a row;
+// Rows to 8-bit integers with a scale for each row: scale = max|x| / 127, q = round(x * (1 / max|x| * 127)). One block holds a row;
 // with a routing the row is written to every place that the token was sent to, so it is read and quantised once.
 #include "experts.cuh"
 
@@ -11,6 +11,7 @@ constexpr float TINY = 1e-30f;  // below it 127 / max could overflow
 
 template <typename T> __global__ void __launch_bounds__(QUANT_THREADS) hccl_quantise_rows(const __grid_constant__ QuantParams p) {
     __shared__ float part[QUANT_THREADS / 32];
+    asm volatile("griddepcontrol.launch_dependents;");  // the product may start to fetch its weights
     for (long long m = blockIdx.x; m < p.M; m += gridDim.x) {
         const T* x = (const T*)p.x + m * p.ldx;
         float top = 0.f;
@@ -29,7 +30,7 @@ template <typename T> __global__ void __launch_bounds__(QUANT_THREADS) hccl_quan
         for (int i = 1; i < QUANT_THREADS / 32; i++) top = part[i] > top || isnan(part[i]) ? part[i] : top;
         __syncthreads();
         const bool finite = top < INFINITY;
-        const float inv = finite && top >= TINY ? 127.f / top : 0.f;
+        const float inv = finite && top >= TINY ? __fmul_rn(1.f / top, 127.f) : 0.f;
         const float scale = !finite ? __int_as_float(0x7fc00000) : top >= TINY ? top / 127.f : 0.f;
         const int copies = p.slots ? p.top_k : 1;
         for (int c = 0; c < copies; c++) {

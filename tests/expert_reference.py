@@ -92,7 +92,7 @@ def quantise(x):
         amax = np.abs(x).max(axis=1) if x.shape[1] else np.zeros(x.shape[0], dtype=np.float32)
         bad = ~(amax < np.inf)
         use = ~bad & (amax >= np.float32(1e-30))
-        inv = np.where(use, np.float32(127) / np.where(use, amax, np.float32(1)), np.float32(0)).astype(np.float32)
+        inv = np.where(use, np.float32(1) / np.where(use, amax, np.float32(1)) * np.float32(127), np.float32(0)).astype(np.float32)
         q = np.rint(np.where(bad[:, None], np.float32(0), x) * inv[:, None])
         scale = np.where(bad, np.float32(np.nan), np.where(use, amax / np.float32(127), np.float32(0))).astype(np.float32)
     return q.astype(np.int8), scale

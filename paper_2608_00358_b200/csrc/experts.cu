@@ -175,7 +175,7 @@ hccl_status_t hccl_route(const hccl_router_t* c, const void* logits, int64_t ld,
     if (!workspace) return HCCL_ERR_INVALID_ARG;
     if (!aligned(workspace, 16)) return HCCL_ERR_ALIGNMENT;
     RouteParams p = route_params(c, logits, ld, bias, mask, out);
-    p.hist = (int*)workspace;
+    p.hist = (uint8_t*)workspace;
     return done(launch_route(dt, p, (cudaStream_t)stream), "hccl_route");
 }
 

@@ -44,13 +44,15 @@ struct RouteParams {
     long long ld, tokens;
     int E, K, groups, per_group, top_groups, group_best, sigmoid, renorm;
     float scale;
-    int chunk;   // tokens per block
-    int blocks;
+    int per4, magic;     // quads of experts lie in one group each; e * magic >> 20 = e / per_group
+    int vec;             // rows of logits can be read four elements at once
+    int warps;           // per block
+    int chunk, chunks;   // tokens counted together; chunks of them (1: a single block does everything)
     int* ids;
     float* weights;
     long long* counts;
     int *offsets, *slots, *source;
-    int* hist;   // [blocks][E]
+    uint8_t* hist;       // [chunks][E rounded up to 16] rows of each expert in each chunk
 };
 
 struct RouteGradParams {
@@ -58,6 +60,7 @@ struct RouteGradParams {
     const float* dweights;
     void* dlogits;
     long long ldd;
+    int vec;
 };
 
 size_t route_workspace(int E, long long tokens);
@@ -88,6 +91,7 @@ struct QuantParams {
     long long ldx, M, K, ldq, n_q;
     int8_t* q;
     float* scale;
+    int vec, vec_q;    // 16 bytes at a time
     const int* slots;  // null: row m of x to row m of q
     int top_k;
 };

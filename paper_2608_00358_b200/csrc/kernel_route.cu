@@ -1,9 +1,15 @@
 // Routing of tokens to experts: scores, the choice of the top k, their weights, the layout of the rows in expert
 // order, and the gradient of the scores.
 //
-// One warp holds one token's scores in registers, expert e in register e / 32 of lane e % 32. The keys that the choice
-// goes by are mapped to unsigned integers in the same order (sign bit flipped, negative numbers complemented), so
-// that a maximum over the warp is one redux instruction; 0 stands for "not eligible" and is below every key.
+// The choice. L lanes share a token (8: four tokens to a warp; 32: one). Experts go to lanes in quads: quad q = experts 4q .. 4q + 3 belongs to
+// lane q % L, as its quad q / L. Keys lie in shared memory and the largest key of each quad in a register, so a round of
+// the top k costs a maximum over the lane's quads, one over the lanes, and a second look at one quad. Not eligible: -inf. What bounds it is
+// the number of instructions: a token of 256 experts is 512 bytes of input and some 270 instructions of a warp.
+//
+// Keys are good to a few 2^-24 (__expf and an approximate reciprocal); the weights of the chosen are formed anew with
+// expf and a rounded division.
+#include <algorithm>
+
 #include "experts.cuh"
 
 namespace hccl {
@@ -11,139 +17,246 @@ namespace experts {
 namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
-constexpr int ROUTE_THREADS = 256, ROUTE_WARPS = ROUTE_THREADS / 32;
+constexpr int LAYOUT_THREADS = 512;
+constexpr int ONE_BLOCK_WARPS = 16, MANY_WARPS = 8;
+constexpr int NOT_A_NUMBER = 0x7fc00000;
 
-__device__ __forceinline__ unsigned ordered(float f) {
-    const unsigned u = __float_as_uint(f + 0.0f);  // -0 becomes +0: they compare equal
-    return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
-}
-__device__ __forceinline__ float unordered(unsigned k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
+__host__ __device__ constexpr int round_up(int n, int m) { return (n + m - 1) / m * m; }
+// floats from one token's keys to the next: 8 banks on, so that lanes of four tokens that walk their groups do not collide
+__host__ __device__ __forceinline__ int key_stride(int E) { return round_up(E, 32) + 8; }
+__host__ __device__ __forceinline__ int token_floats(const RouteParams& p) { return key_stride(p.E) + (p.groups > 1 ? 2 * round_up(p.groups, 4) : 0) + round_up(p.K, 4); }
 
-__device__ __forceinline__ float warp_sum(float v) {
+template <int L> __device__ __forceinline__ float lanes_max(float v) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    for (int o = L / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
     return v;
 }
-
-// Scores of one token. On return s[] is the score's numerator (sigmoid: the score itself; softmax: exp(l - max)), key[] the ordered
-// key or 0. Returns false for a token that cannot be scored. *total: the softmax's sum (1 for the sigmoid).
-template <typename T, int V>
-__device__ __forceinline__ bool score_token(const RouteParams& p, long long t, int lane, float (&s)[V], unsigned (&key)[V], float* total) {
-    const T* row = (const T*)p.logits + t * p.ld;
-    float l[V], b[V];
+template <int L> __device__ __forceinline__ int lanes_min(int v) {
+    if constexpr (L == 32) {
+        return __reduce_min_sync(FULL, v);
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-        const int e = i * 32 + lane;
-        l[i] = e < p.E ? to_f32<T>(row[e]) : -INFINITY;
-        b[i] = (p.bias && e < p.E) ? p.bias[e] : 0.f;
+        for (int o = L / 2; o; o >>= 1) v = min(v, __shfl_xor_sync(FULL, v, o));
+        return v;
     }
-    bool bad = false, off[V];
+}
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    return v;
+}
+template <int L> __device__ __forceinline__ bool lanes_any(bool v) {
+    const unsigned b = __ballot_sync(FULL, v);
+    return (b >> (threadIdx.x % 32 / L * L)) & (L == 32 ? FULL : (1u << (L % 32)) - 1);
+}
+
+// Experts 4q .. 4q + 3 of a row; -inf from E on.
+template <typename T> __device__ __forceinline__ void load_quad(const T* row, int q, int E, bool vec, float (&x)[4]) {
+    if (vec && 4 * q + 4 <= E) {
+        Pack<T, 4> v;
+        v.raw = *(const typename Piece<4 * sizeof(T)>::type*)(row + 4 * q);
+#pragma unroll
+        for (int j = 0; j < 4; j++) x[j] = to_f32<T>(v.v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; j++) x[j] = 4 * q + j < E ? to_f32<T>(row[4 * q + j]) : -INFINITY;
+    }
+}
+
+__device__ __forceinline__ float quick_sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+
+// One token for each L lanes. keys: this token's shared memory (token_floats). sbias: the bias in shared memory, up to a multiple of 4 experts.
+// Writes ids and weights, counts the chosen in hist.
+template <typename T, int Q, int L>
+__device__ __forceinline__ void choose_token(const RouteParams& p, long long t, bool in, float* keys, const float* sbias, int* hist) {
+    const int lane = threadIdx.x % 32, l = lane % L;
+    const int stride = key_stride(p.E), gpad = p.groups > 1 ? round_up(p.groups, 4) : 0;
+    float* gscore = keys + stride;
+    int* gkeep = (int*)(gscore + gpad);
+    int* chosen = (int*)(keys + stride + 2 * gpad);
+    const bool live = in && (!p.mask || p.mask[t]);
+    const T* row = (const T*)p.logits + (in ? t : 0) * p.ld;
+
+    float x[Q][4];
+#pragma unroll
+    for (int i = 0; i < Q; i++) {
+        if (live) load_quad<T>(row, i * L + l, p.E, p.vec, x[i]);
+        else x[i][0] = x[i][1] = x[i][2] = x[i][3] = -INFINITY;
+    }
+    bool bad = false;
     float m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-        off[i] = l[i] == -INFINITY || b[i] == -INFINITY;
-        if (!off[i]) {
-            bad |= isnan(l[i]) || !(b[i] < INFINITY) || (!p.sigmoid && l[i] == INFINITY);
-            m = fmaxf(m, l[i]);
-        }
-    }
-    if (__any_sync(FULL, bad)) return false;
-    if (p.sigmoid) {
+    for (int i = 0; i < Q; i++) {
+        if (p.bias && (i * L + l) * 4 < p.E) {
+            const float4 b4 = *(const float4*)(sbias + (i * L + l) * 4);
+            const float b[4] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            s[i] = off[i] ? 0.f : 1.f / (1.f + expf(-l[i]));
-            key[i] = off[i] ? 0u : ordered(s[i] + b[i]);
-        }
-        *total = 1.f;
-        return true;
-    }
-    m = unordered(__reduce_max_sync(FULL, ordered(m)));
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < V; i++) {
-        s[i] = off[i] ? 0.f : expf(l[i] - m);  // l is finite and so is m, if any expert is eligible
-        sum += s[i];
-    }
-    sum = warp_sum(sum);
-    *total = sum;
-#pragma unroll
-    for (int i = 0; i < V; i++) key[i] = off[i] ? 0u : ordered(p.bias ? s[i] / sum + b[i] : l[i]);
-    return true;
-}
-
-// Clears the keys of experts whose group is not among the best. Lane g keeps group g's score.
-template <int V> __device__ __forceinline__ void keep_best_groups(const RouteParams& p, int lane, unsigned (&key)[V]) {
-    // groups beyond 32 are walked in rounds of 32: lane j of round r holds group r * 32 + j
-    unsigned mine[V];  // group score (ordered) of group r * 32 + lane
-#pragma unroll
-    for (int r = 0; r < V; r++) mine[r] = 0;
-    for (int g = 0; g < p.groups; g++) {
-        const int lo = g * p.per_group, hi = lo + p.per_group;
-        unsigned k1 = 0, k2 = 0;
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-            if (i * 32 + 31 >= lo && i * 32 < hi) {
-                const int e = i * 32 + lane;
-                const unsigned k = (e >= lo && e < hi) ? key[i] : 0u;
-                k2 = max(k2, min(k1, k));
-                k1 = max(k1, k);
+            for (int j = 0; j < 4; j++) {
+                if (b[j] == -INFINITY) x[i][j] = -INFINITY;  // the expert is off, whatever its logit
+                bad |= x[i][j] != -INFINITY && !(b[j] < INFINITY);
             }
         }
-        const unsigned m1 = __reduce_max_sync(FULL, k1);
-        unsigned score = m1;
-        if (p.group_best == 2) {
-            const int owner = __ffs(__ballot_sync(FULL, k1 == m1)) - 1;
-            const unsigned m2 = __reduce_max_sync(FULL, lane == owner ? k2 : k1);
-            if (m1 && m2) score = ordered(unordered(m1) + unordered(m2));
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            bad |= isnan(x[i][j]);
+            m = fmaxf(m, x[i][j]);
         }
-#pragma unroll
-        for (int r = 0; r < V; r++)
-            if (g == r * 32 + lane) mine[r] = score;
     }
-    unsigned chosen[V];  // bit g % 32 of word g / 32, the same in all lanes
+    m = lanes_max<L>(m);
+    bad |= !p.sigmoid && m == INFINITY;
+    bad = lanes_any<L>(bad);
+    float total = 1.f;
+    if (p.sigmoid || p.bias || !p.renorm) {
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
 #pragma unroll
-    for (int r = 0; r < V; r++) chosen[r] = 0;
-    for (int n = 0; n < p.top_groups; n++) {
-        unsigned best = 0;
+        for (int i = 0; i < Q; i++) {
+            float b[4] = {0.f, 0.f, 0.f, 0.f};
+            if (p.sigmoid) {
+                if (p.bias && (i * L + l) * 4 < p.E) {
+                    const float4 b4 = *(const float4*)(sbias + (i * L + l) * 4);
+                    b[0] = b4.x, b[1] = b4.y, b[2] = b4.z, b[3] = b4.w;
+                }
 #pragma unroll
-        for (int r = 0; r < V; r++) best = max(best, mine[r]);
-        best = __reduce_max_sync(FULL, best);
-        if (!best) break;
-        bool done = false;
+                for (int j = 0; j < 4; j++)
+                    if (x[i][j] != -INFINITY) x[i][j] = quick_sigmoid(x[i][j]) + b[j];
+            } else {
 #pragma unroll
-        for (int r = 0; r < V; r++) {
-            const unsigned who = __ballot_sync(FULL, mine[r] == best);
-            if (!done && who) {
-                const int owner = __ffs(who) - 1;
-                chosen[r] |= 1u << owner;
-                if (lane == owner) mine[r] = 0;
-                done = true;
+                for (int j = 0; j < 4; j++) sum += __expf(x[i][j] - base);
+            }
+        }
+        if (!p.sigmoid) {
+            total = lanes_sum<L>(sum);
+            if (p.bias) {
+                const float r = __fdividef(1.f, total);
+#pragma unroll
+                for (int i = 0; i < Q; i++)
+                    if ((i * L + l) * 4 < p.E) {
+                        const float4 b4 = *(const float4*)(sbias + (i * L + l) * 4);
+                        const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                        for (int j = 0; j < 4; j++)
+                            if (x[i][j] != -INFINITY) x[i][j] = __expf(x[i][j] - base) * r + b[j];
+                    }
             }
         }
     }
+    // x is the key now
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-        const int g = (i * 32 + lane) / p.per_group;
-        unsigned word = 0;
+    for (int i = 0; i < Q; i++)
+        if ((i * L + l) * 4 < p.E) *(float4*)(keys + (i * L + l) * 4) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+    if (p.groups > 1) {
+        __syncwarp();
+        for (int g = l; g < p.groups; g += L) {
+            float k1 = -INFINITY, k2 = -INFINITY;
+            int at = g % p.per_group;  // lanes start at different places of their groups: different banks
+            const float* k = keys + g * p.per_group;
+            for (int i = 0; i < p.per_group; i++) {
+                const float v = k[at];
+                k2 = fmaxf(k2, fminf(k1, v));
+                k1 = fmaxf(k1, v);
+                at = at + 1 == p.per_group ? 0 : at + 1;
+            }
+            gscore[g] = (p.group_best == 2 && k2 != -INFINITY) ? k1 + k2 : k1;
+        }
+        __syncwarp();
+        for (int g = l; g < p.groups; g += L) {
+            const float mine = gscore[g];
+            int above = 0;
+            for (int o = 0; o < p.groups; o++) above += gscore[o] > mine || (gscore[o] == mine && o < g);
+            gkeep[g] = above < p.top_groups;
+        }
+        __syncwarp();
 #pragma unroll
-        for (int r = 0; r < V; r++)
-            if (g / 32 == r) word = chosen[r];
-        if (!((word >> (g & 31)) & 1u)) key[i] = 0;
+        for (int i = 0; i < Q; i++) {
+            const int e = (i * L + l) * 4;
+            if (e >= p.E) continue;
+            if (p.per4) {
+                if (!gkeep[(e * p.magic) >> 20]) x[i][0] = x[i][1] = x[i][2] = x[i][3] = -INFINITY;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (e + j < p.E && !gkeep[((e + j) * p.magic) >> 20]) x[i][j] = -INFINITY;
+                *(float4*)(keys + e) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+            }
+        }
     }
+    float top[Q];
+#pragma unroll
+    for (int i = 0; i < Q; i++) top[i] = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
+    __syncwarp();
+    for (int k = 0; k < p.K; k++) {
+        float best = top[0];
+        int at = 0;
+#pragma unroll
+        for (int i = 1; i < Q; i++)
+            if (top[i] > best) best = top[i], at = i;
+        const float win = lanes_max<L>(best);
+        const int quad = lanes_min<L>(best == win ? at * L + l : 0x7fffffff);
+        if (win == -INFINITY || bad) {
+            if (l == 0) chosen[k] = -1;
+        } else if (quad == at * L + l && best == win) {
+            float* c = keys + quad * 4;
+            float4 v = *(float4*)c;
+            const int j = v.x == win ? 0 : v.y == win ? 1 : v.z == win ? 2 : 3;
+            chosen[k] = quad * 4 + j;
+            c[j] = -INFINITY;
+            if (j == 0) v.x = -INFINITY;
+            if (j == 1) v.y = -INFINITY;
+            if (j == 2) v.z = -INFINITY;
+            if (j == 3) v.w = -INFINITY;
+            const float next = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
+#pragma unroll
+            for (int i = 0; i < Q; i++)
+                if (at == i) top[i] = next;
+        }
+    }
+    __syncwarp();
+    constexpr int R = 32 / L;  // at most 32 choices over L lanes
+    float s[R], sum = 0.f;
+    int id[R];
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        const int k = r * L + l;
+        id[r] = k < p.K ? chosen[k] : -1;
+        s[r] = 0.f;
+        if (id[r] >= 0) {
+            const float v = to_f32<T>(row[id[r]]);
+            s[r] = p.sigmoid ? 1.f / (1.f + expf(-v)) : expf(v - m);  // softmax: the common divisor drops out of renormalised weights
+        }
+        sum += s[r];
+        if (r * L + L >= p.K) {
+#pragma unroll
+            for (int q = 0; q < R; q++)
+                if (q > r) id[q] = -1, s[q] = 0.f;
+            break;
+        }
+    }
+    const float div = p.renorm ? lanes_sum<L>(sum) : total;
+    if (in) {
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            const int k = r * L + l;
+            if (k >= p.K) break;
+            p.ids[t * p.K + k] = id[r];
+            p.weights[t * p.K + k] = (live && bad) ? __int_as_float(NOT_A_NUMBER) : (id[r] >= 0 && div > 0.f) ? s[r] / div * p.scale : 0.f;
+            if (id[r] >= 0) atomicAdd(&hist[id[r]], 1);
+        }
+    }
+    __syncwarp();
 }
 
-// Layout of this block's tokens: base[e] (shared) = first row of expert e for this block; the rows of a block's
-// tokens follow in token order. Each warp takes a run of the block's choices; a first walk counts them by expert, a second hands
-// out the rows with match_any, so that the order does not depend on which warp is faster.
-__device__ __forceinline__ void layout_block(const RouteParams& p, long long t0, long long t1, int* base, int* cnt, int threads) {
+// Rows of the choices [first, first + n). base[e] (shared) = first row of expert e for them; rows follow in the order of the choices.
+// Each warp takes a run of them; a first walk counts by expert, a second hands out the rows with match_any, so that the
+// order does not depend on which warp is faster. cnt: shared, [warps][E].
+__device__ __forceinline__ void layout_choices(const RouteParams& p, long long first, int n, const int* base, int* cnt, int threads) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = threads / 32;
-    const long long first = t0 * p.K, n = (t1 - t0) * p.K;
-    const long long per = ((n + warps - 1) / warps + 31) / 32 * 32;
-    const long long lo = min((long long)warp * per, n), hi = min(lo + per, n);
-    int* mine = cnt + (size_t)warp * p.E;
+    const int per = round_up((n + warps - 1) / warps, 32);
+    const int lo = min(warp * per, n), hi = min(lo + per, n);
+    int* mine = cnt + warp * p.E;
     for (int e = lane; e < p.E; e += 32) mine[e] = 0;
     __syncwarp();
-    for (long long i = lo + lane; i < hi; i += 32) {
+    for (int i = lo + lane; i < hi; i += 32) {
         const int e = p.ids[first + i];
         if (e >= 0) atomicAdd(&mine[e], 1);
     }
@@ -151,14 +264,14 @@ __device__ __forceinline__ void layout_block(const RouteParams& p, long long t0,
     for (int e = threadIdx.x; e < p.E; e += threads) {  // counts become first rows
         int at = base[e];
         for (int w = 0; w < warps; w++) {
-            const int c = cnt[(size_t)w * p.E + e];
-            cnt[(size_t)w * p.E + e] = at;
+            const int c = cnt[w * p.E + e];
+            cnt[w * p.E + e] = at;
             at += c;
         }
     }
     __syncthreads();
-    for (long long b = lo; b < hi; b += 32) {
-        const long long i = b + lane;
+    for (int b = lo; b < hi; b += 32) {
+        const int i = b + lane;
         const int e = i < hi ? p.ids[first + i] : -1;
         const unsigned same = __match_any_sync(FULL, e);
         int row = -1;
@@ -173,9 +286,8 @@ __device__ __forceinline__ void layout_block(const RouteParams& p, long long t0,
     }
 }
 
-// Offsets of all experts from their totals, and this block's first rows. tot and base: shared, E ints each.
-__device__ __forceinline__ void offsets_block(const RouteParams& p, int* tot, int* base, bool write, int threads) {
-    // one warp scans the totals
+// Offsets of all experts from their totals tot[E] (shared); each expert's first row is added to base[e]. Returns the number of rows.
+__device__ __forceinline__ int offsets_of(const RouteParams& p, const int* tot, int* base, int* rows, bool write) {
     if (threadIdx.x < 32) {
         int run = 0;
         for (int b = 0; b < p.E; b += 32) {
@@ -198,195 +310,337 @@ __device__ __forceinline__ void offsets_block(const RouteParams& p, int* tot, in
             run += __shfl_sync(FULL, inc, 31);
         }
         if (threadIdx.x == 0) {
-            tot[p.E] = run;
+            *rows = run;
             if (write) p.offsets[p.E] = run;
         }
     }
     __syncthreads();
+    return *rows;
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(ROUTE_THREADS) hccl_route_choose(const __grid_constant__ RouteParams p) {
-    extern __shared__ int sm[];  // hist[E]
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    for (int e = threadIdx.x; e < p.E; e += ROUTE_THREADS) sm[e] = 0;
+// A block chooses for one chunk of tokens and leaves its counts for the layout; a single block goes on to the layout itself.
+template <typename T, int Q, int L>
+__global__ void __launch_bounds__(32 * ONE_BLOCK_WARPS) hccl_route_choose(const __grid_constant__ RouteParams p) {
+    extern __shared__ __align__(16) int sm[];  // hist[E16] bias[E16], then the tokens' keys; a single block: its layout's base and counts in their place
+    __shared__ int rows;
+    const int E16 = round_up(p.E, 16), threads = 32 * p.warps, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    int* hist = sm;
+    float* sbias = (float*)(sm + E16);
+    float* keys = sbias + E16;
+    asm volatile("griddepcontrol.launch_dependents;");
+    for (int e = threadIdx.x; e < E16; e += threads) {
+        hist[e] = 0;
+        if (p.bias) sbias[e] = e < p.E ? p.bias[e] : 0.f;
+    }
     __syncthreads();
     const long long t0 = (long long)blockIdx.x * p.chunk, t1 = min(t0 + p.chunk, p.tokens);
-    for (long long t = t0 + warp; t < t1; t += ROUTE_WARPS) {
-        int id = -1;       // of choice `lane`
-        float w = 0.f;
-        float s[V], total = 1.f;
-        unsigned key[V];
-        const bool live = !p.mask || p.mask[t];
-        if (live) {
-            if (!score_token<T, V>(p, t, lane, s, key, &total)) {
-                w = __int_as_float(0x7fc00000);
-            } else {
-                if (p.groups > 1) keep_best_groups<V>(p, lane, key);
-                for (int k = 0; k < p.K; k++) {
-                    unsigned best = 0;
-                    int at = 0;
-                    float sv = 0.f;
+    const int sub = lane / L, per = 32 / L;
+    float* mine = keys + (warp * per + sub) * token_floats(p);
+    for (long long t = t0 + warp * per; t < t1; t += p.warps * per) choose_token<T, Q, L>(p, t + sub, t + sub < t1, mine, sbias, hist);
+    __syncthreads();
+    if (p.chunks > 1) {
+        for (int e = threadIdx.x; e < E16; e += threads) p.hist[(size_t)blockIdx.x * E16 + e] = (uint8_t)hist[e];
+        return;
+    }
+    int *base = (int*)sbias, *cnt = base + E16;
+    for (int e = threadIdx.x; e < p.E; e += threads) base[e] = 0;
+    __syncthreads();
+    const int used = offsets_of(p, hist, base, &rows, true);
+    const int n = (int)(p.tokens * p.K);
+    layout_choices(p, 0, n, base, cnt, threads);
+    for (int i = used + (int)threadIdx.x; i < n; i += threads) p.source[i] = -1;
+}
+
+// Adds 16 counters of 8 bits to 16 sums of 16 bits: bytes 0 and 2 of word w to sum[2w], bytes 1 and 3 to sum[2w + 1].
+__device__ __forceinline__ void add_bytes(uint4 v, unsigned (&sum)[8]) {
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int i = 0; i < V; i++)
-                        if (key[i] > best) best = key[i], at = i, sv = s[i];
-                    const unsigned m = __reduce_max_sync(FULL, best);
-                    if (!m) break;
-                    const int e = __reduce_min_sync(FULL, best == m ? at * 32 + lane : 0x7fffffff);
-                    const float se = __shfl_sync(FULL, sv, e & 31);
+    for (int i = 0; i < 4; i++) {
+        sum[2 * i] += w[i] & 0x00ff00ffu;
+        sum[2 * i + 1] += (w[i] >> 8) & 0x00ff00ffu;
+    }
+}
+__device__ __forceinline__ void flush_bytes(int* to, int e0, int E, unsigned (&sum)[8]) {
 #pragma unroll
-                    for (int i = 0; i < V; i++)
-                        if (e == i * 32 + lane) key[i] = 0;
-                    if (lane == k) id = e, w = se;
+    for (int i = 0; i < 8; i++) {
+        const int e = e0 + i / 2 * 4 + (i & 1);
+        if (e < E && (sum[i] & 0xffffu)) atomicAdd(&to[e], (int)(sum[i] & 0xffffu));
+        if (e + 2 < E && (sum[i] >> 16)) atomicAdd(&to[e + 2], (int)(sum[i] >> 16));
+        sum[i] = 0;
+    }
+}
+
+// Each block lays out the choices of a run of chunks. How many rows of each expert lie before them, and in all, it adds up itself from the
+// chunks' counts: 8 bits each (a chunk has at most 255 tokens, a token chooses an expert once), read 16 at a time.
+__global__ void __launch_bounds__(LAYOUT_THREADS) hccl_route_layout(const __grid_constant__ RouteParams p) {
+    extern __shared__ __align__(16) int sm[];  // tot[E16], base[E16], cnt[warps][E]
+    __shared__ int rows;
+    const int E16 = round_up(p.E, 16);
+    int *tot = sm, *base = sm + E16, *cnt = base + E16;
+    for (int e = threadIdx.x; e < E16; e += LAYOUT_THREADS) tot[e] = base[e] = 0;
+    __syncthreads();
+    const int c0 = (int)((long long)p.chunks * blockIdx.x / gridDim.x), c1 = (int)((long long)p.chunks * (blockIdx.x + 1) / gridDim.x);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int columns = E16 / 16, lines = LAYOUT_THREADS / columns, col = (int)threadIdx.x % columns, line = (int)threadIdx.x / columns;
+    if (line < lines) {
+        unsigned sum[8] = {};
+        const uint4* h = (const uint4*)p.hist + col;
+        const auto add_up = [&](int from, int to, int* where) {
+            int n = 0;
+            for (int c = from + line; c < to; c += 8 * lines) {
+                uint4 v[8];
+#pragma unroll
+                for (int u = 0; u < 8; u++) v[u] = c + u * lines < to ? h[(size_t)(c + u * lines) * columns] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int u = 0; u < 8; u++) add_bytes(v[u], sum);
+                n += 8;
+                if (n + 8 > 256) {  // 257 bytes of 255 fill 16 bits
+                    flush_bytes(where, col * 16, p.E, sum);
+                    n = 0;
                 }
-                // softmax: s is exp(l - max); the common divisor drops out of a renormalised weight
-                const float div = p.renorm ? warp_sum(w) : total;
-                w = div > 0.f ? w / div * p.scale : 0.f;
             }
-        }
-        if (lane < p.K) {
-            p.ids[t * p.K + lane] = id;
-            p.weights[t * p.K + lane] = w;
-            if (id >= 0) atomicAdd(&sm[id], 1);
-        }
+            flush_bytes(where, col * 16, p.E, sum);
+        };
+        add_up(0, c0, base);
+        add_up(c0, p.chunks, tot);
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < p.E; e += ROUTE_THREADS) p.hist[(size_t)blockIdx.x * p.E + e] = sm[e];
-}
-
-__global__ void __launch_bounds__(ROUTE_THREADS) hccl_route_layout(const __grid_constant__ RouteParams p) {
-    extern __shared__ int sm[];  // tot[E + 1], base[E], cnt[ROUTE_WARPS][E]
-    int *tot = sm, *base = sm + p.E + 1, *cnt = base + p.E;
-    for (int e = threadIdx.x; e < p.E; e += ROUTE_THREADS) {
-        int before = 0, all = 0;
-        for (int b = 0; b < p.blocks; b++) {
-            const int c = p.hist[(size_t)b * p.E + e];
-            if (b < (int)blockIdx.x) before += c;
-            all += c;
-        }
-        tot[e] = all;
-        base[e] = before;
-    }
+    for (int e = threadIdx.x; e < p.E; e += LAYOUT_THREADS) tot[e] += base[e];
     __syncthreads();
-    offsets_block(p, tot, base, blockIdx.x == 0, ROUTE_THREADS);
-    const long long t0 = (long long)blockIdx.x * p.chunk, t1 = min(t0 + p.chunk, p.tokens);
-    if (t0 < t1) layout_block(p, t0, t1, base, cnt, ROUTE_THREADS);
-    // rows that belong to no choice
-    const long long n = p.tokens * p.K;
-    for (long long i = tot[p.E] + (long long)blockIdx.x * ROUTE_THREADS + threadIdx.x; i < n; i += (long long)gridDim.x * ROUTE_THREADS) p.source[i] = -1;
+    const int used = offsets_of(p, tot, base, &rows, blockIdx.x == 0);
+    const long long t0 = (long long)c0 * p.chunk, t1 = min((long long)c1 * p.chunk, p.tokens);
+    if (t0 < t1) layout_choices(p, t0 * p.K, (int)((t1 - t0) * p.K), base, cnt, LAYOUT_THREADS);
+    const long long n = p.tokens * p.K;  // rows that belong to no choice
+    for (long long i = used + (long long)blockIdx.x * LAYOUT_THREADS + threadIdx.x; i < n; i += (long long)gridDim.x * LAYOUT_THREADS) p.source[i] = -1;
 }
 
 // d of the logits. Weight j of the chosen has w_j = scale * s_j / S (S = sum of the chosen scores if renormalised, else 1), so
 // ds_j = scale / S * (dw_j - sum_i dw_i s_i / S) or scale * dw_j; then the score's own derivative:
-// sigmoid dl = ds s (1 - s), softmax dl_e = s_e (ds_e - sum_j ds_j s_j) over all experts.
-template <typename T, int V>
-__global__ void __launch_bounds__(ROUTE_THREADS) hccl_route_grad(const __grid_constant__ RouteGradParams q) {
+// sigmoid dl = ds s (1 - s), softmax dl_e = s_e (ds_e - sum_j ds_j s_j) over all experts. Where the weights are renormalised (the softmax's
+// divisor drops out, and with it sum_j ds_j s_j = 0) or the scores are sigmoids, only the chosen have a gradient: their logits alone
+// are read, and the row is zeros with k places filled, put together in shared memory. Memory is the bound.
+template <typename T, int L>
+__global__ void __launch_bounds__(256) hccl_route_grad(const __grid_constant__ RouteGradParams q) {
     const RouteParams& p = q.r;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    for (long long t = (long long)blockIdx.x * ROUTE_WARPS + warp; t < p.tokens; t += (long long)gridDim.x * ROUTE_WARPS) {
-        T* out = (T*)q.dlogits + t * q.ldd;
-        float s[V], total = 1.f, d[V];
-        unsigned key[V];
-        const bool live = !p.mask || p.mask[t];
-        bool ok = live;
-        if (live) ok = score_token<T, V>(p, t, lane, s, key, &total);
-        if (!ok) {
-            const T v = from_f32<T>(live ? __int_as_float(0x7fc00000) : 0.f);
-            for (int e = lane; e < p.E; e += 32) out[e] = v;
-            continue;
-        }
-        const float inv = total > 0.f ? 1.f / total : 0.f;  // 0: no expert was eligible
-        int id = -1;
-        float dw = 0.f, c = 0.f;
-        if (lane < p.K) {
-            id = p.ids[t * p.K + lane];
-            if (id >= p.E) id = -1;
-            if (id >= 0) dw = q.dweights[t * p.K + lane] * p.scale;
-        }
-        // score of this lane's choice
-        for (int k = 0; k < p.K; k++) {
-            const int e = __shfl_sync(FULL, id, k);
-            float v = 0.f;
+    extern __shared__ __align__(16) char smem[];  // a row of T for each token of the block, rounded up to 16 bytes
+    constexpr int R = 32 / L, V = 16 / sizeof(T);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % L, per = 32 / L;
+    const int row_elems = round_up(p.E, V);
+    T* buf = (T*)smem + (size_t)(warp * per + lane / L) * row_elems;
+    const bool whole_row = !p.sigmoid && !p.renorm;
+    for (long long t0 = (long long)blockIdx.x * 8 * per; t0 < p.tokens; t0 += (long long)gridDim.x * 8 * per) {
+        const long long t = t0 + warp * per + lane / L;
+        const bool in = t < p.tokens, live = in && (!p.mask || p.mask[t]);
+        const T* row = (const T*)p.logits + (in ? t : 0) * p.ld;
+        int id[R];
+        float dw[R], x[R], c[R];
+        bool some = false;
 #pragma unroll
-            for (int i = 0; i < V; i++)
-                if (e == i * 32 + lane) v = s[i];
-            v = __shfl_sync(FULL, v, e & 31);
-            if (lane == k && e >= 0) c = v;
+        for (int r = 0; r < R; r++) {
+            const int k = r * L + l;
+            id[r] = -1, dw[r] = 0.f, x[r] = -INFINITY;
+            if (live && k < p.K) {
+                id[r] = p.ids[t * p.K + k];
+                if (id[r] >= p.E) id[r] = -1;
+                if (id[r] >= 0) {
+                    dw[r] = q.dweights[t * p.K + k] * p.scale;
+                    x[r] = to_f32<T>(row[id[r]]);
+                    some = true;
+                }
+            }
+        }
+        some = lanes_any<L>(some);
+        // what the row is filled with, where it is not one of the chosen
+        float m = -INFINITY, total = 1.f, dot = 0.f, fill = 0.f;
+        const bool walk = whole_row || !__all_sync(FULL, some || !live);  // a live token that chose nothing: were its scores numbers?
+        bool bad = false;
+        if (walk) {
+            for (int e = l; e < p.E && live; e += L) {
+                float v = to_f32<T>(row[e]);
+                const float b = p.bias ? p.bias[e] : 0.f;
+                if (b == -INFINITY) v = -INFINITY;
+                bad |= isnan(v) || (v != -INFINITY && !(b < INFINITY));
+                m = fmaxf(m, v);
+            }
+            m = lanes_max<L>(m);
+            bad |= live && !p.sigmoid && m == INFINITY;
+            bad = lanes_any<L>(bad);
+            if (bad) fill = __int_as_float(NOT_A_NUMBER);
+            if (whole_row) {
+                float sum = 0.f;
+                for (int e = l; e < p.E && live; e += L)
+                    if (m != -INFINITY && !(p.bias && p.bias[e] == -INFINITY)) sum += expf(to_f32<T>(row[e]) - m);
+                total = lanes_sum<L>(sum);
+            }
+        }
+        if (!whole_row && !p.sigmoid) {
+            m = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < R; r++) m = fmaxf(m, x[r]);
+            m = lanes_max<L>(m);
+        }
+        float sc = 0.f, sdc = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            c[r] = id[r] < 0 ? 0.f : p.sigmoid ? 1.f / (1.f + expf(-x[r])) : expf(x[r] - m);
+            sc += c[r];
+            sdc += dw[r] * c[r];
         }
         if (p.renorm) {
-            const float S = warp_sum(c);
-            const float r = S > 0.f ? 1.f / S : 0.f;
-            dw = (dw - warp_sum(dw * c) * r) * r;  // the softmax's divisor has dropped out: d of exp(l - max)
-            if (id < 0) dw = 0.f;
-            // in terms of exp(l - max) the chain through the sum is already in: dl_e = exp_e * dw_e
-        }
-        const float dot = (!p.sigmoid && !p.renorm) ? warp_sum(dw * c) * inv : 0.f;
+            const float S = lanes_sum<L>(sc), D = lanes_sum<L>(sdc), r1 = S > 0.f ? 1.f / S : 0.f;
 #pragma unroll
-        for (int i = 0; i < V; i++) d[i] = 0.f;
-        for (int k = 0; k < p.K; k++) {
-            const int e = __shfl_sync(FULL, id, k);
-            const float g = __shfl_sync(FULL, dw, k);
-#pragma unroll
-            for (int i = 0; i < V; i++)
-                if (e == i * 32 + lane) d[i] = g;
+            for (int r = 0; r < R; r++) dw[r] = (dw[r] - D * r1) * r1;
+        } else if (whole_row) {
+            const float r1 = total > 0.f ? 1.f / total : 0.f;
+            dot = lanes_sum<L>(sdc) * r1;
+            total = r1;
         }
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-            const int e = i * 32 + lane;
-            if (e >= p.E) continue;
-            float v;
-            if (p.sigmoid) v = d[i] * s[i] * (1.f - s[i]);
-            else if (p.renorm) v = d[i] * s[i];
-            else v = s[i] * inv * (d[i] - dot);
-            out[e] = from_f32<T>(v);
+        // the row
+        if (!whole_row || bad) {
+            for (int e = l; e < row_elems; e += L) buf[e] = from_f32<T>(fill);
+        } else {
+            for (int e = l; e < p.E && live; e += L) {
+                const bool off = m == -INFINITY || (p.bias && p.bias[e] == -INFINITY);
+                buf[e] = from_f32<T>(off ? 0.f : -expf(to_f32<T>(row[e]) - m) * total * dot);
+            }
+            if (!live)
+                for (int e = l; e < row_elems; e += L) buf[e] = from_f32<T>(0.f);
         }
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < R; r++)
+            if (id[r] >= 0 && !bad) buf[id[r]] = from_f32<T>(p.sigmoid ? dw[r] * c[r] * (1.f - c[r]) : p.renorm ? dw[r] * c[r] : c[r] * total * (dw[r] - dot));
+        __syncwarp();
+        if (in) {
+            T* out = (T*)q.dlogits + t * q.ldd;
+            if (q.vec) {
+                for (int v = l; v < p.E / V; v += L) ((uint4*)out)[v] = ((const uint4*)buf)[v];
+            } else {
+                for (int e = l; e < p.E; e += L) out[e] = buf[e];
+            }
+        }
+        __syncwarp();
     }
 }
 
-int route_blocks(long long tokens) {
-    const long long b = (tokens + ROUTE_WARPS - 1) / ROUTE_WARPS;
-    return (int)(b < 1 ? 1 : (b > SMS ? SMS : b));
+// ---------------------------------------------------------------- host
+// Lanes for a token: 32 while each can have a warp of the one block, or where 8 lanes would hold more than 8 quads each.
+int lanes_for(long long tokens, int E) { return (tokens <= ONE_BLOCK_WARPS || E > 256) ? 32 : 8; }
+bool one_block(long long tokens, int lanes) { return tokens <= ONE_BLOCK_WARPS * (32 / lanes) * 2; }
+
+struct Cut {
+    int lanes, warps, chunk, chunks;
+};
+Cut cut(long long tokens, int E) {
+    Cut c;
+    c.lanes = lanes_for(tokens, E);
+    const int per = 32 / c.lanes;
+    if (one_block(tokens, c.lanes)) {
+        c.warps = (int)std::min<long long>(ONE_BLOCK_WARPS, std::max<long long>(4, (tokens + per - 1) / per));
+        c.chunk = (int)tokens;
+        c.chunks = 1;
+        return c;
+    }
+    c.warps = MANY_WARPS;
+    const int round = MANY_WARPS * per;  // tokens a block chooses for at once: 32 or 8
+    long long want = (tokens + 16 * SMS - 1) / (16 * SMS);
+    want = (want + round - 1) / round * round;
+    c.chunk = (int)std::min<long long>(std::max<long long>(want, round), 255 / round * round);
+    c.chunks = (int)((tokens + c.chunk - 1) / c.chunk);
+    return c;
 }
 
-template <typename T, int V> cudaError_t route_launch(const RouteParams& p, cudaStream_t s) {
-    hccl_route_choose<T, V><<<p.blocks, ROUTE_THREADS, p.E * 4, s>>>(p);
-    hccl_route_layout<<<p.blocks, ROUTE_THREADS, (2 * p.E + 1 + ROUTE_WARPS * p.E) * 4, s>>>(p);
-    return cudaGetLastError();
-}
-template <typename T, int V> cudaError_t grad_launch(const RouteGradParams& p, cudaStream_t s) {
-    const long long b = (p.r.tokens + ROUTE_WARPS - 1) / ROUTE_WARPS;
-    hccl_route_grad<T, V><<<(int)(b > SMS * 8 ? SMS * 8 : b), ROUTE_THREADS, 0, s>>>(p);
-    return cudaGetLastError();
+// Opt-in to large shared memory, once for each kernel and device.
+template <typename K> cudaError_t allow(K* kernel, size_t bytes, bool (&ready)[64]) {
+    if (bytes <= 48 * 1024) return cudaSuccess;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < 64 && ready[dev])) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    if (e == cudaSuccess && dev < 64) ready[dev] = true;
+    return e;
 }
 
-#define ROUTE_PICK_V(FN, T, E, ...)                       \
-    do {                                                  \
-        const int v_ = ((E) + 31) / 32;                   \
-        if (v_ <= 2) return FN<T, 2>(__VA_ARGS__);        \
-        if (v_ <= 4) return FN<T, 4>(__VA_ARGS__);        \
-        if (v_ <= 8) return FN<T, 8>(__VA_ARGS__);        \
-        if (v_ <= 16) return FN<T, 16>(__VA_ARGS__);      \
-        return FN<T, 32>(__VA_ARGS__);                    \
-    } while (0)
+template <typename T, int Q, int L> cudaError_t route_launch(const RouteParams& p, cudaStream_t s) {
+    const int E16 = round_up(p.E, 16);
+    size_t smem = (size_t)(2 * E16) * 4 + (size_t)p.warps * (32 / L) * token_floats(p) * 4;
+    if (p.chunks == 1) smem = std::max(smem, (size_t)(2 * E16 + p.warps * p.E) * 4);
+    static bool ready[64];
+    cudaError_t e = allow(hccl_route_choose<T, Q, L>, smem, ready);
+    if (e != cudaSuccess) return e;
+    hccl_route_choose<T, Q, L><<<p.chunks, 32 * p.warps, smem, s>>>(p);
+    if (p.chunks == 1) return cudaGetLastError();
+    static bool ready2[64];
+    cudaLaunchConfig_t cfg = {};
+    cfg.dynamicSmemBytes = (size_t)(2 * E16 + LAYOUT_THREADS / 32 * p.E) * 4;
+    if ((e = allow(hccl_route_layout, cfg.dynamicSmemBytes, ready2)) != cudaSuccess) return e;
+    cfg.gridDim = dim3((unsigned)std::min(p.chunks, SMS));
+    cfg.blockDim = dim3(LAYOUT_THREADS);
+    cfg.stream = s;
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, hccl_route_layout, p);
+}
+
+template <typename T> cudaError_t route_sizes(const RouteParams& p, int lanes, cudaStream_t s) {
+    if (lanes == 8) {
+        if (p.E <= 32) return route_launch<T, 1, 8>(p, s);
+        if (p.E <= 64) return route_launch<T, 2, 8>(p, s);
+        if (p.E <= 128) return route_launch<T, 4, 8>(p, s);
+        return route_launch<T, 8, 8>(p, s);
+    }
+    if (p.E <= 128) return route_launch<T, 1, 32>(p, s);
+    if (p.E <= 256) return route_launch<T, 2, 32>(p, s);
+    if (p.E <= 512) return route_launch<T, 4, 32>(p, s);
+    return route_launch<T, 8, 32>(p, s);
+}
+
+template <typename T, int L> cudaError_t grad_launch(const RouteGradParams& p, cudaStream_t s) {
+    const int per_block = 8 * (32 / L);
+    const size_t smem = (size_t)per_block * round_up(p.r.E, 16 / sizeof(T)) * sizeof(T);
+    const long long blocks = (p.r.tokens + per_block - 1) / per_block;
+    hccl_route_grad<T, L><<<(int)std::min<long long>(blocks, SMS * 8), 256, smem, s>>>(p);
+    return cudaGetLastError();
+}
+template <typename T> cudaError_t grad_sizes(const RouteGradParams& p, cudaStream_t s) {
+    return p.r.E <= 256 ? grad_launch<T, 8>(p, s) : grad_launch<T, 32>(p, s);
+}
+
+bool aligned_rows(const void* at, long long ld, int es, int bytes) { return (uintptr_t)at % bytes == 0 && (ld * es) % bytes == 0; }
 
 }  // namespace
 
-size_t route_workspace(int E, long long tokens) { return (size_t)route_blocks(tokens) * E * 4; }
+size_t route_workspace(int E, long long tokens) {
+    const Cut c = cut(tokens, E);
+    return c.chunks > 1 ? (size_t)c.chunks * round_up(E, 16) : 16;  // never nothing: one rule for callers
+}
 
 cudaError_t launch_route(int dt, const RouteParams& in, cudaStream_t s) {
     RouteParams p = in;
-    p.blocks = route_blocks(p.tokens);
-    p.chunk = (int)((p.tokens + p.blocks - 1) / p.blocks);
-    if (dt == HCCL_FP32) ROUTE_PICK_V(route_launch, float, p.E, p, s);
-    if (dt == HCCL_BF16) ROUTE_PICK_V(route_launch, __nv_bfloat16, p.E, p, s);
-    ROUTE_PICK_V(route_launch, __half, p.E, p, s);
+    const Cut c = cut(p.tokens, p.E);
+    p.warps = c.warps;
+    p.chunk = c.chunk;
+    p.chunks = c.chunks;
+    p.per4 = p.per_group % 4 == 0;
+    p.magic = ((1 << 20) + p.per_group - 1) / p.per_group;
+    const int es = dt == HCCL_FP32 ? 4 : 2;
+    p.vec = aligned_rows(p.logits, p.ld, es, 4 * es);
+    if (dt == HCCL_FP32) return route_sizes<float>(p, c.lanes, s);
+    if (dt == HCCL_BF16) return route_sizes<__nv_bfloat16>(p, c.lanes, s);
+    return route_sizes<__half>(p, c.lanes, s);
 }
 
-cudaError_t launch_route_grad(int dt, const RouteGradParams& p, cudaStream_t s) {
+cudaError_t launch_route_grad(int dt, const RouteGradParams& in, cudaStream_t s) {
+    RouteGradParams p = in;
     if (p.r.tokens == 0) return cudaSuccess;
-    if (dt == HCCL_FP32) ROUTE_PICK_V(grad_launch, float, p.r.E, p, s);
-    if (dt == HCCL_BF16) ROUTE_PICK_V(grad_launch, __nv_bfloat16, p.r.E, p, s);
-    ROUTE_PICK_V(grad_launch, __half, p.r.E, p, s);
+    const int es = dt == HCCL_FP32 ? 4 : 2;
+    p.vec = aligned_rows(p.dlogits, p.ldd, es, 16) && (p.r.E * es) % 16 == 0;
+    if (dt == HCCL_FP32) return grad_sizes<float>(p, s);
+    if (dt == HCCL_BF16) return grad_sizes<__nv_bfloat16>(p, s);
+    return grad_sizes<__half>(p, s);
 }
 
 }  // namespace experts

@@ -45,7 +45,7 @@ def test_route_workspace():
         hb.hccl_route_workspace_bytes(router(), -1)
     with pytest.raises(hb.HcclError):
         hb.hccl_route_workspace_bytes(router(), 1 << 30)  # tokens * top_k reaches 2^31
-    assert hb.hccl_route_workspace_bytes(router(), (1 << 30) - 1) < 1 << 24
+    assert hb.hccl_route_workspace_bytes(router(), (1 << 30) - 1) < 1 << 30  # a byte for each expert and some 200 tokens
 
 
 def test_route_refusals():

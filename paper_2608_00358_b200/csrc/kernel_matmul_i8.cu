@@ -4,6 +4,10 @@
 // tokens its columns, so that one kernel serves a single token (N = 16 columns, the weights stream past them) and a
 // long prompt (N = 256); the sum is exact in 32-bit integers, in any order.
 //
+// With CG = 2 two blocks on neighbouring SMs form one tile of 256 channels x 256 tokens: each holds its own 128 channels and half the
+// tokens, and the first one's instructions read both. A stage then is 32 KB for each SM instead of 48 KB, which matters because
+// shared memory is the bound: a block alone writes and reads 2 x 48 KB for 512 cycles of products, at 128 bytes a cycle.
+//
 // Roles of a block (8 warps): warp 0 issues the TMA loads, warp 1 the matrix instructions, warp 2 owns the tensor memory, warps 4-7 turn
 // accumulators into results. Stages of 128 bytes of K pass from the loads to the instructions through mbarriers; two
 // accumulators let the results of one tile leave while the next is formed. Blocks stay and walk tiles; where there are
@@ -19,9 +23,10 @@ namespace {
 constexpr int MM_THREADS = 256, CH = 128 /* channels of a tile */, KB = 128 /* bytes of K in a stage */;
 constexpr unsigned long long WAIT_NS = 2000000000ull;  // bound of every wait
 
-template <int TN> struct Shape {
-    static constexpr int BOX = TN < 64 ? TN : 64;  // token rows of one TMA load
-    static constexpr int STAGE = (CH + TN) * KB;
+template <int TN, int CG> struct Shape {
+    static constexpr int ROWS = TN / CG;               // token rows that a block holds
+    static constexpr int BOX = ROWS < 64 ? ROWS : 64;  // of them, in one TMA load
+    static constexpr int STAGE = (CH + ROWS) * KB;
     static constexpr int STAGES = (200 * 1024) / STAGE;
     static constexpr int COLS = 2 * TN < 32 ? 32 : 2 * TN;  // tensor memory columns: two accumulators
     static constexpr int SMEM = STAGES * STAGE + 1024;
@@ -68,36 +73,62 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
         }
     }
 }
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+__device__ __forceinline__ uint32_t of_rank(uint32_t addr, uint32_t rank) {  // the same place in another block of the cluster
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory"); }
+// bar: an address in the cluster's shared memory; with CG = 2 it may lie in the pair's other block.
+template <int CG> __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if constexpr (CG == 2) {
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+        return;
+    }
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 // Shared-memory operand with 128-byte rows of K in the 128-byte swizzle: groups of 8 rows lie 1024 bytes apart.
 __device__ __forceinline__ uint64_t operand(uint32_t addr) {
     return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
-__device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t accumulate) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(accumulate) : "memory");
+template <int CG> __device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t accumulate) {
+    if constexpr (CG == 2)
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// Arrives at the barrier, in both blocks of a pair, when the instructions issued so far are done.
+template <int CG> __device__ __forceinline__ void mma_commit(uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-template <int N> __device__ __forceinline__ void tmem_load(uint32_t addr, int (&v)[N]);
-template <> __device__ __forceinline__ void tmem_load<16>(uint32_t addr, int (&v)[16]) {
+__device__ __forceinline__ void tmem_load(uint32_t addr, int (&v)[16]) {  // 16 columns of a warp's 32 lanes; tmem_arrived before use
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
                    "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
                  : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_arrived() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int cluster_load(uint32_t addr, uint32_t rank) {
+    int v;
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.s32 %0, [a];\n}" : "=r"(v) : "r"(addr), "r"(rank) : "memory");
+    return v;
 }
 
 // ---------------------------------------------------------------- tiles
 struct Tile {
-    int group, row, rows, chan;  // rows [row, row + rows) of the tokens, channels from chan on
+    int group, row, rows, chan;  // rows [row, row + rows) of the tokens, this block's channels from chan on
 };
 
 // Tile t. before[g] = token tiles of the groups below g. Within a group 8 token tiles pass under one tile of channels
 // before the next, so that the blocks of a wave share both operands in the L2.
-template <int TN> __device__ __forceinline__ Tile tile_of(const TileParams& p, const int* before, int t, int* hint) {
+template <int TN, int CG> __device__ __forceinline__ Tile tile_of(const TileParams& p, const int* before, int t, int rank, int* hint) {
     Tile r;
     int g = 0, lo = 0, hi = p.M;
     if (p.groups) {
@@ -113,21 +144,12 @@ template <int TN> __device__ __forceinline__ Tile tile_of(const TileParams& p, c
     r.group = g;
     r.row = lo + (first + j % deep) * TN;
     r.rows = min(TN, hi - r.row);
-    r.chan = (j / deep) * CH;
+    r.chan = (j / deep) * CH * CG + rank * CH;
     return r;
 }
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ int cluster_load(uint32_t addr, uint32_t rank) {
-    int v;
-    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.s32 %0, [a];\n}" : "=r"(v) : "r"(addr), "r"(rank) : "memory");
-    return v;
-}
-
-template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) hccl_matmul_i8_tiles(const __grid_constant__ TileParams p) {
-    using S = Shape<TN>;
+template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREADS, 1) hccl_matmul_i8_tiles(const __grid_constant__ TileParams p) {
+    using S = Shape<TN, CG>;
     extern __shared__ char dynamic[];
     __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 4];
     __shared__ uint32_t tmem_at;
@@ -141,17 +163,56 @@ template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) h
     const auto acc_full = [&](int b) { return bar0 + 8 * (2 * S::STAGES + b); };
     const auto acc_empty = [&](int b) { return bar0 + 8 * (2 * S::STAGES + 2 + b); };
 
+    // Which blocks work together: a pair (CG = 2, on one tile), or p.splits blocks that share a tile's K, or each alone.
+    const int splits = CG == 2 ? 1 : p.splits, team = CG == 2 ? 2 : p.splits;
+    const int rank = (int)blockIdx.x % team, first = (int)blockIdx.x / team, step = (int)gridDim.x / team;
+    const int pair_rank = CG == 2 ? rank : 0;
+    const int k0 = CG == 2 ? 0 : (int)((long long)p.k_blocks * rank / splits), k1 = CG == 2 ? p.k_blocks : (int)((long long)p.k_blocks * (rank + 1) / splits);
+
+    // A role's own state
+    int it = 0, acc = 0, hint = 0;  // stages passed, tiles passed, group
+    bool waited = !p.dependent;
+    const auto rely = [&] {  // from here on reads what the kernel before this one wrote
+        if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+        waited = true;
+    };
+    // Token rows that this block loads: all of the tile's, or, of a pair, a half of them, rounded up to 16.
+    const auto half_of = [&](const Tile& t) { return CG == 2 ? ((t.rows + 31) / 32) * 16 : t.rows; };
+    const auto full_at = [&](int s) { return CG == 2 ? of_rank(full(s), 0) : full(s); };
+    const auto load_w = [&](const Tile& t, int s, int kb) { tma_load<CG>(base + s * S::STAGE, &p.w, kb * KB, t.group * p.N + t.chan, full_at(s)); };
+    const auto load_a = [&](const Tile& t, int s, int kb) {
+        const int half = half_of(t), boxes = (half + S::BOX - 1) / S::BOX;
+        for (int i = 0; i < boxes; i++) tma_load<CG>(base + s * S::STAGE + CH * KB + i * S::BOX * KB, &p.a, kb * KB, t.row + pair_rank * half + i * S::BOX, full_at(s));
+    };
+    // The first block's barrier counts the bytes of both.
+    const auto expect = [&](const Tile& t, int s) {
+        if (pair_rank == 0) mbar_expect(full(s), (uint32_t)(CG * (CH * KB + (half_of(t) + S::BOX - 1) / S::BOX * S::BOX * KB)));
+    };
+
+    int pre = 0;  // stages of the first tile whose weights are under way
+    const auto prefetch = [&](const Tile& t) {
+        pre = min(k1 - k0, S::STAGES);
+        for (int i = 0; i < pre; i++) {
+            expect(t, i);
+            load_w(t, i, k0 + i);
+        }
+    };
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
-        for (int b = 0; b < 2; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 4);
+        for (int b = 0; b < 2; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 4 * CG);
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&p.a));
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&p.w));
+        // The weights do not hang on the kernel before, nor on the other warps: they are asked for at once.
+        if (!p.groups && CG == 1) prefetch(tile_of<TN, CG>(p, before, first, pair_rank, &hint));
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::COLS));
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if constexpr (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::COLS));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::COLS));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        }
     }
     if (warp == 3 && p.groups) {
         int run = 0;
@@ -170,54 +231,33 @@ template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) h
         }
         if (lane == 0) before[p.groups] = run;
     }
+    __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (CG == 2) cluster_sync();  // both blocks' barriers exist before either uses the other's
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_at;
     const int tiles = p.n_tiles * (p.groups ? before[p.groups] : (p.M + TN - 1) / TN);
-    const int splits = p.splits, rank = (int)blockIdx.x % splits, first = (int)blockIdx.x / splits, step = (int)gridDim.x / splits;
-    const int k0 = (int)((long long)p.k_blocks * rank / splits), k1 = (int)((long long)p.k_blocks * (rank + 1) / splits);
-
-    // A step's state, kept by each role for itself
-    int it = 0, acc = 0, hint = 0;  // stages passed, tiles passed, group
-    bool waited = !p.dependent;
-    const auto rely = [&] {  // from here on reads what the kernel before this one wrote
-        if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
-        waited = true;
-    };
-    const auto load_w = [&](const Tile& t, int s, int kb) { tma_load(base + s * S::STAGE, &p.w, kb * KB, t.group * p.N + t.chan, full(s)); };
-    const auto load_a = [&](const Tile& t, int s, int kb) {
-        const int boxes = (t.rows + S::BOX - 1) / S::BOX;
-        for (int i = 0; i < boxes; i++) tma_load(base + s * S::STAGE + CH * KB + i * S::BOX * KB, &p.a, kb * KB, t.row + i * S::BOX, full(s));
-    };
-    const auto stage_bytes = [&](const Tile& t) { return (uint32_t)(CH * KB + (t.rows + S::BOX - 1) / S::BOX * S::BOX * KB); };
 
     const auto produce = [&](const Tile& t) {
-        int kb = k0;
-        if (!waited) {  // the weights do not hang on the kernel before: the first stages' share of them is under way while it runs
-            const int pre = min(k1 - k0, S::STAGES);
-            for (int i = 0; i < pre; i++) {
-                mbar_expect(full(i), stage_bytes(t));
-                load_w(t, i, k0 + i);
-            }
-            rely();
-            for (int i = 0; i < pre; i++) load_a(t, i, k0 + i);
-            kb += pre;
-            it += pre;
-        }
-        for (; kb < k1; kb++, it++) {
+        if (!pre && !waited) prefetch(t);
+        rely();
+        for (int i = 0; i < pre; i++) load_a(t, i, k0 + i);
+        it += pre;
+        for (int kb = k0 + pre; kb < k1; kb++, it++) {
             const int s = it % S::STAGES;
             if (!mbar_wait(empty(s), ((it / S::STAGES) & 1) ^ 1, &gave_up)) return;
-            mbar_expect(full(s), stage_bytes(t));
+            expect(t, s);
             load_w(t, s, kb);
             load_a(t, s, kb);
         }
+        pre = 0;
     };
     const auto multiply = [&](const Tile& t) {
         const int b = acc & 1;
-        const uint32_t cols = (uint32_t)((t.rows + 15) & ~15);
+        const uint32_t cols = CG == 2 ? (uint32_t)((t.rows + 31) & ~31) : (uint32_t)((t.rows + 15) & ~15);
         // 32-bit accumulators, signed 8-bit operands, both with K innermost
-        const uint32_t desc = (2u << 4) | (1u << 7) | (1u << 10) | ((cols >> 3) << 17) | ((uint32_t)(CH >> 4) << 24);
+        const uint32_t desc = (2u << 4) | (1u << 7) | (1u << 10) | ((cols >> 3) << 17) | ((uint32_t)(CH * CG >> 4) << 24);
         if (!mbar_wait(acc_empty(b), ((acc >> 1) & 1) ^ 1, &gave_up)) return;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         for (int kb = k0; kb < k1; kb++, it++) {
@@ -226,54 +266,74 @@ template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) h
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint64_t w = operand(base + s * S::STAGE), a = operand(base + s * S::STAGE + CH * KB);
 #pragma unroll
-            for (int k = 0; k < KB / 32; k++) mma_i8(tmem + b * TN, w + 2 * k, a + 2 * k, desc, (kb > k0 || k > 0) ? 1u : 0u);
-            mma_commit(empty(s));
+            for (int k = 0; k < KB / 32; k++) mma_i8<CG>(tmem + b * TN, w + 2 * k, a + 2 * k, desc, (kb > k0 || k > 0) ? 1u : 0u);
+            mma_commit<CG>(empty(s));
         }
-        mma_commit(acc_full(b));
+        mma_commit<CG>(acc_full(b));
     };
-    const auto store = [&](const Tile& t, int chan, int row, int sum, float sa, float sw, float bias) {
-        // the sum's conversion is the one rounding that an exact product of the scales would not have: sums pass 2^24 from K = 1024 on
-        float v = __fmul_rn(__fmul_rn((float)sum, sa), sw);
-        if (p.bias) v = __fadd_rn(v, bias);
-        ((T*)p.y)[(long long)row * p.ldy + chan] = from_f32<T>(v);
+    const auto scaled = [&](int sum, float sa, float sw, float bias) {
+        // a sum passes 2^24 from K = 1024 on: its conversion to 32-bit floating point is a rounding, like each scale's product
+        const float v = __fmul_rn(__fmul_rn((float)sum, sa), sw);
+        return from_f32<T>(p.bias ? __fadd_rn(v, bias) : v);
     };
     const auto results = [&](const Tile& t) {
         const int b = acc & 1, quarter = warp & 3, chan = t.chan + quarter * 32 + lane;
         const bool in = chan < p.N;
         const long long gc = (long long)t.group * p.N + chan;
         const float sw = in ? p.w_scale[gc] : 0.f, bias = (in && p.bias) ? p.bias[gc] : 0.f;
+        float sa[(TN + 31) / 32];  // scales of the tile's rows, row 32 i + lane in sa[i]: loaded while the products are formed
+#pragma unroll
+        for (int i = 0; i < (TN + 31) / 32; i++) sa[i] = i * 32 + lane < t.rows ? p.a_scale[t.row + i * 32 + lane] : 0.f;
         const bool ok = !p.k_blocks || mbar_wait(acc_full(b), (acc >> 1) & 1, &gave_up);
         if (!__all_sync(0xffffffffu, ok)) return;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        for (int c0 = 0; c0 < t.rows; c0 += 16) {
-            int v[16];
+        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + b * TN;
+#pragma unroll
+        for (int i = 0; i < (TN + 31) / 32; i++) {
+            if (i * 32 >= t.rows) break;
+            int v[32];
             __syncwarp();
-            if (p.k_blocks) tmem_load<16>(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + c0, v);
-            else
+            if (p.k_blocks) {
+                tmem_load(at + i * 32, *(int(*)[16])v);
+                if (TN > 16) tmem_load(at + i * 32 + 16, *(int(*)[16])(v + 16));
+                tmem_arrived();
+            } else {
 #pragma unroll
-                for (int i = 0; i < 16; i++) v[i] = 0;
-            const float mine = (lane < 16 && c0 + lane < t.rows) ? p.a_scale[t.row + c0 + lane] : 0.f;
+                for (int j = 0; j < 32; j++) v[j] = 0;
+            }
+            constexpr int C = TN < 32 ? TN : 32;
+            T o[C];  // all of them before the first store: a branch for each would leave its chain of latencies bare
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const float sa = __shfl_sync(0xffffffffu, mine, i);
-                if (in && c0 + i < t.rows) store(t, chan, t.row + c0 + i, v[i], sa, sw, bias);
+            for (int j = 0; j < C; j++) o[j] = scaled(v[j], __shfl_sync(0xffffffffu, sa[i], j), sw, bias);
+            T* y = (T*)p.y + (long long)(t.row + i * 32) * p.ldy + chan;
+            if (in && i * 32 + C <= t.rows) {
+#pragma unroll
+                for (int j = 0; j < C; j++, y += p.ldy) *y = o[j];
+            } else if (in) {
+#pragma unroll
+                for (int j = 0; j < C; j++, y += p.ldy)
+                    if (i * 32 + j < t.rows) *y = o[j];
             }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(acc_empty(b));
+        if (lane == 0) {
+            if (CG == 2) mbar_arrive_at(of_rank(acc_empty(b), 0));
+            else mbar_arrive(acc_empty(b));
+        }
     };
+    const auto stopped = [&] { return *(volatile int*)&gave_up != 0; };
 
     if (splits == 1) {
         if (warp == 0 && lane == 0) {
             if (p.k_blocks)
-                for (int t = first; t < tiles && !*(volatile int*)&gave_up; t += step) produce(tile_of<TN>(p, before, t, &hint));
-        } else if (warp == 1 && lane == 0) {
+                for (int t = first; t < tiles && !stopped(); t += step) produce(tile_of<TN, CG>(p, before, t, pair_rank, &hint));
+        } else if (warp == 1 && lane == 0 && pair_rank == 0) {
             if (p.k_blocks)
-                for (int t = first; t < tiles && !*(volatile int*)&gave_up; t += step, acc++) multiply(tile_of<TN>(p, before, t, &hint));
+                for (int t = first; t < tiles && !stopped(); t += step, acc++) multiply(tile_of<TN, CG>(p, before, t, pair_rank, &hint));
         } else if (warp >= 4) {
             rely();
-            for (int t = first; t < tiles && !*(volatile int*)&gave_up; t += step, acc++) results(tile_of<TN>(p, before, t, &hint));
+            for (int t = first; t < tiles && !stopped(); t += step, acc++) results(tile_of<TN, CG>(p, before, t, pair_rank, &hint));
         }
     } else {
         // One tile at a time for the whole cluster. The partial sums go to shared memory (the stages are idle by then), column by
@@ -281,7 +341,7 @@ template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) h
         // after a wait that gave up.
         int* part = (int*)(dynamic + (base - smem_addr(dynamic)));
         for (int t = first; t < tiles; t += step, acc++) {
-            const Tile tile = tile_of<TN>(p, before, t, &hint);
+            const Tile tile = tile_of<TN, CG>(p, before, t, 0, &hint);
             if (warp == 0 && lane == 0) produce(tile);
             if (warp == 1 && lane == 0) multiply(tile);
             if (warp >= 4) {
@@ -291,7 +351,8 @@ template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) h
                 if (__all_sync(0xffffffffu, ok))
                     for (int c0 = 0; c0 < tile.rows; c0 += 16) {
                         int v[16];
-                        tmem_load<16>(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + c0, v);
+                        tmem_load(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + c0, v);
+                        tmem_arrived();
 #pragma unroll
                         for (int i = 0; i < 16; i++) part[(c0 + i) * CH + quarter * 32 + lane] = v[i];
                     }
@@ -308,7 +369,7 @@ template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) h
                 for (int r = 0; r < splits; r++) sum += cluster_load(base + 4 * i, r);
                 const int chan = tile.chan + i % CH, row = tile.row + i / CH;
                 const long long gc = (long long)tile.group * p.N + chan;
-                if (chan < p.N) store(tile, chan, row, sum, p.a_scale[row], p.w_scale[gc], p.bias ? p.bias[gc] : 0.f);
+                if (chan < p.N) ((T*)p.y)[(long long)row * p.ldy + chan] = scaled(sum, p.a_scale[row], p.w_scale[gc], p.bias ? p.bias[gc] : 0.f);
             }
             // what the generic proxy read and wrote here, the next tile's loads will overwrite
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -317,16 +378,22 @@ template <typename T, int TN> __global__ void __launch_bounds__(MM_THREADS, 1) h
     }
     rely();
     // After a wait that gave up, loads may still be in flight: wait (with a limit) for the stages that were issued.
-    if (warp == 0 && lane == 0 && *(volatile int*)&gave_up) {
+    if (warp == 0 && lane == 0 && stopped()) {
         const unsigned long long t0 = now_ns();
-        for (int i = max(0, it - S::STAGES); i < it; i++)
-            while (!mbar_try(full(i % S::STAGES), (i / S::STAGES) & 1) && now_ns() - t0 < WAIT_NS) {}
+        if (pair_rank == 0)
+            for (int i = max(0, it - S::STAGES); i < it; i++)
+                while (!mbar_try(full(i % S::STAGES), (i / S::STAGES) & 1) && now_ns() - t0 < WAIT_NS) {}
         __nanosleep(1000000);  // and the instructions issued last, which end by themselves
         if (p.status) *p.status = HCCL_ERR_TIMEOUT;
     }
+    __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::COLS));
+    if (CG == 2) cluster_sync();  // neither block leaves while the other's instructions or arrivals may still reach it
+    if (warp == 2) {
+        if constexpr (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::COLS));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::COLS));
+    }
 }
 
 // ---------------------------------------------------------------- host
@@ -356,8 +423,8 @@ cudaError_t make_map(CUtensorMap* m, const void* at, long long rows, long long K
                : cudaErrorInvalidValue;
 }
 
-template <typename T, int TN> cudaError_t tiles_launch(const MatmulParams& q, int splits, cudaStream_t s) {
-    using S = Shape<TN>;
+template <typename T, int TN, int CG> cudaError_t tiles_launch(const MatmulParams& q, int splits, cudaStream_t s) {
+    using S = Shape<TN, CG>;
     TileParams p = {};
     p.ldy = q.ldy;
     p.a_scale = q.a_scale;
@@ -370,7 +437,7 @@ template <typename T, int TN> cudaError_t tiles_launch(const MatmulParams& q, in
     p.N = (int)q.N;
     p.groups = q.groups;
     p.k_blocks = (int)((q.K + KB - 1) / KB);
-    p.n_tiles = (int)((q.N + CH - 1) / CH);
+    p.n_tiles = (int)((q.N + CH * CG - 1) / (CH * CG));
     p.splits = splits;
     p.dependent = q.dependent;
     cudaError_t e;
@@ -382,22 +449,23 @@ template <typename T, int TN> cudaError_t tiles_launch(const MatmulParams& q, in
     int dev = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     if (dev >= 64 || !ready[dev]) {
-        e = cudaFuncSetAttribute(hccl_matmul_i8_tiles<T, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+        e = cudaFuncSetAttribute(hccl_matmul_i8_tiles<T, TN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
         if (e != cudaSuccess) return e;
         if (dev < 64) ready[dev] = true;
     }
     const long long tiles = (long long)p.n_tiles * ((q.M + TN - 1) / TN + q.groups);  // at most, with groups
-    const long long clusters = SMS / splits;
+    const int team = CG == 2 ? 2 : splits;
+    const long long teams = SMS / team;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((tiles < clusters ? tiles : clusters) * splits));
+    cfg.gridDim = dim3((unsigned)((tiles < teams ? tiles : teams) * team));
     cfg.blockDim = dim3(MM_THREADS);
     cfg.dynamicSmemBytes = S::SMEM;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     int n = 0;
-    if (splits > 1) {
+    if (team > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = (unsigned)splits;
+        attr[n].val.clusterDim.x = (unsigned)team;
         attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
         n++;
     }
@@ -408,7 +476,7 @@ template <typename T, int TN> cudaError_t tiles_launch(const MatmulParams& q, in
     }
     cfg.attrs = attr;
     cfg.numAttrs = n;
-    return cudaLaunchKernelEx(&cfg, hccl_matmul_i8_tiles<T, TN>, p);
+    return cudaLaunchKernelEx(&cfg, hccl_matmul_i8_tiles<T, TN, CG>, p);
 }
 
 template <typename T> cudaError_t matmul_launch(const MatmulParams& p, cudaStream_t s) {
@@ -417,11 +485,11 @@ template <typename T> cudaError_t matmul_launch(const MatmulParams& p, cudaStrea
     int splits = 1;
     if (rows <= 64)  // few rows: the weights' bytes are the time, and all SMs are to fetch them
         while (splits < 8 && (long long)n_tiles * splits * 2 * (p.groups ? p.groups : 1) <= SMS && splits * 2 * 4 <= k_blocks) splits *= 2;
-    if (rows <= 16) return tiles_launch<T, 16>(p, splits, s);
-    if (rows <= 32) return tiles_launch<T, 32>(p, splits, s);
-    if (rows <= 64) return tiles_launch<T, 64>(p, splits, s);
-    if (rows <= 128) return tiles_launch<T, 128>(p, 1, s);
-    return tiles_launch<T, 256>(p, 1, s);
+    if (rows <= 16) return tiles_launch<T, 16, 1>(p, splits, s);
+    if (rows <= 32) return tiles_launch<T, 32, 1>(p, splits, s);
+    if (rows <= 64) return tiles_launch<T, 64, 1>(p, splits, s);
+    if (rows <= 128) return tiles_launch<T, 128, 1>(p, 1, s);
+    return tiles_launch<T, 256, 2>(p, 1, s);
 }
 
 }  // namespace

@@ -290,9 +290,10 @@ hccl_status_t hccl_linear_i8(const hccl_matmul_i8_t* in, const void* x, int64_t 
     TRY(check_matmul(&m));
     QuantParams p;
     TRY(quant_params(&p, x, ldx, r ? r->tokens : m.M, m.K, dt, r, (int8_t*)m.a, m.lda, m.M, (float*)m.a_scale));
+    MatmulParams mm = matmul_params(&m);
+    if (mm.M && mm.N && few_rows(mm) && few_rows_quantise(mm)) return done(launch_linear_i8_few(m.dtype, mm, p, dt, (cudaStream_t)stream), "hccl_linear_i8");
     const cudaError_t e = launch_quantise(dt, p, (cudaStream_t)stream);
     if (e != cudaSuccess) return hccl::note_cuda_error(e, "hccl_linear_i8");
-    MatmulParams mm = matmul_params(&m);
     mm.dependent = p.M > 0;
     return done(launch_matmul_i8(m.dtype, mm, (cudaStream_t)stream), "hccl_linear_i8");
 }

@@ -109,5 +109,11 @@ struct MatmulParams {
 };
 cudaError_t launch_matmul_i8(int dt, const MatmulParams& p, cudaStream_t s);
 
+// At most 8 rows (kernel_rows_i8.cu): whether the kernel takes them, and whether it quantises them itself.
+bool few_rows(const MatmulParams& p);
+bool few_rows_quantise(const MatmulParams& p);
+cudaError_t launch_matmul_i8_few(int dt, const MatmulParams& p, cudaStream_t s);
+cudaError_t launch_linear_i8_few(int dt, const MatmulParams& p, const QuantParams& x, int x_dt, cudaStream_t s);
+
 }  // namespace experts
 }  // namespace hccl

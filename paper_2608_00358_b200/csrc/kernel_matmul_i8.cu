@@ -8,8 +8,8 @@
 // tokens, and the first one's instructions read both. A stage then is 32 KB for each SM instead of 48 KB, which matters because
 // shared memory is the bound: a block alone writes and reads 2 x 48 KB for 512 cycles of products, at 128 bytes a cycle.
 //
-// Roles of a block (8 warps): warp 0 issues the TMA loads, warp 1 the matrix instructions, warp 2 owns the tensor memory, warps 4-7 turn
-// accumulators into results. Stages of 128 bytes of K pass from the loads to the instructions through mbarriers; two
+// Roles of a block (12 warps): warp 0 issues the TMA loads, warp 1 the matrix instructions, warp 2 owns the tensor memory, warps 4-11 turn
+// accumulators into results (two to each quarter of the tensor memory's lanes). Stages of 128 bytes of K pass from the loads to the instructions through mbarriers; two
 // accumulators let the results of one tile leave while the next is formed. Blocks stay and walk tiles; where there are
 // too few tiles for the SMs, a cluster of blocks shares a tile's K and adds its partial sums through distributed shared memory.
 #include <cuda.h>
@@ -20,7 +20,7 @@ namespace hccl {
 namespace experts {
 namespace {
 
-constexpr int MM_THREADS = 256, CH = 128 /* channels of a tile */, KB = 128 /* bytes of K in a stage */;
+constexpr int MM_THREADS = 384, CH = 128 /* channels of a tile */, KB = 128 /* bytes of K in a stage */;
 constexpr unsigned long long WAIT_NS = 2000000000ull;  // bound of every wait
 
 template <int TN, int CG> struct Shape {
@@ -59,18 +59,23 @@ __device__ __forceinline__ unsigned long long now_ns() {
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-// Waits for a phase to complete. After WAIT_NS, or once another wait of this block has given up, it returns false.
+// One lane of a warp that is whole here. The matrix and copy instructions want their operands in uniform registers: issued behind
+// `lane == 0` the compiler cannot tell that one lane is left and wraps each in a loop over lanes (169 cycles an instruction, measured, against
+// 128 of products at 256 columns); behind this it can, if the operands come from values that are the same in all lanes.
+__device__ __forceinline__ bool elected() {
+    uint32_t e;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+    return e;
+}
+// Waits for a phase to complete, by a whole warp. After WAIT_NS, or once another wait of this block has given up, it returns false.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-    if (mbar_try(bar, parity)) return true;
+    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
     const unsigned long long t0 = now_ns();
     for (;;) {
         for (int i = 0; i < 64; i++)
-            if (mbar_try(bar, parity)) return true;
-        if (*gave_up) return false;
-        if (now_ns() - t0 > WAIT_NS) {
-            *gave_up = 1;
-            return false;
-        }
+            if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+        if (now_ns() - t0 > WAIT_NS) *gave_up = 1;
+        if (__any_sync(0xffffffffu, *gave_up)) return false;
     }
 }
 __device__ __forceinline__ uint32_t of_rank(uint32_t addr, uint32_t rank) {  // the same place in another block of the cluster
@@ -115,9 +120,9 @@ __device__ __forceinline__ void tmem_arrived() { asm volatile("tcgen05.wait::ld.
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ int cluster_load(uint32_t addr, uint32_t rank) {
-    int v;
-    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.s32 %0, [a];\n}" : "=r"(v) : "r"(addr), "r"(rank) : "memory");
+__device__ __forceinline__ int4 cluster_load(uint32_t addr, uint32_t rank) {
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(of_rank(addr, rank)) : "memory");
     return v;
 }
 
@@ -141,10 +146,11 @@ template <int TN, int CG> __device__ __forceinline__ Tile tile_of(const TilePara
     const int mt = p.groups ? before[g + 1] - before[g] : (p.M + TN - 1) / TN;
     const int i = t - (p.groups ? before[g] * p.n_tiles : 0);
     const int band = i / (8 * p.n_tiles), first = band * 8, deep = min(8, mt - first), j = i - band * 8 * p.n_tiles;
-    r.group = g;
-    r.row = lo + (first + j % deep) * TN;
-    r.rows = min(TN, hi - r.row);
-    r.chan = (j / deep) * CH * CG + rank * CH;
+    // (the same in all lanes, and by way of the shuffle known to be)
+    r.group = __shfl_sync(0xffffffffu, g, 0);
+    r.row = __shfl_sync(0xffffffffu, lo + (first + j % deep) * TN, 0);
+    r.rows = __shfl_sync(0xffffffffu, min(TN, hi - r.row), 0);
+    r.chan = __shfl_sync(0xffffffffu, (j / deep) * CH * CG + rank * CH, 0);
     return r;
 }
 
@@ -155,7 +161,7 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
     __shared__ int before[HCCL_MAX_EXPERTS + 1];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t base = (smem_addr(dynamic) + 1023) & ~1023u;
     const uint32_t bar0 = smem_addr(bars);
     const auto full = [&](int s) { return bar0 + 8 * s; };
@@ -179,6 +185,7 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
     // Token rows that this block loads: all of the tile's, or, of a pair, a half of them, rounded up to 16.
     const auto half_of = [&](const Tile& t) { return CG == 2 ? ((t.rows + 31) / 32) * 16 : t.rows; };
     const auto full_at = [&](int s) { return CG == 2 ? of_rank(full(s), 0) : full(s); };
+    // The next three by one lane.
     const auto load_w = [&](const Tile& t, int s, int kb) { tma_load<CG>(base + s * S::STAGE, &p.w, kb * KB, t.group * p.N + t.chan, full_at(s)); };
     const auto load_a = [&](const Tile& t, int s, int kb) {
         const int half = half_of(t), boxes = (half + S::BOX - 1) / S::BOX;
@@ -192,19 +199,22 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
     int pre = 0;  // stages of the first tile whose weights are under way
     const auto prefetch = [&](const Tile& t) {
         pre = min(k1 - k0, S::STAGES);
-        for (int i = 0; i < pre; i++) {
-            expect(t, i);
-            load_w(t, i, k0 + i);
-        }
+        if (elected())
+            for (int i = 0; i < pre; i++) {
+                expect(t, i);
+                load_w(t, i, k0 + i);
+            }
+        __syncwarp();
     };
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
-        for (int b = 0; b < 2; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 4 * CG);
+        for (int b = 0; b < 2; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 8 * CG);
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        // The weights do not hang on the kernel before, nor on the other warps: they are asked for at once.
-        if (!p.groups && CG == 1) prefetch(tile_of<TN, CG>(p, before, first, pair_rank, &hint));
     }
+    __syncwarp();
+    // The weights do not hang on the kernel before, nor on the other warps: they are asked for at once.
+    if (warp == 0 && !p.groups && CG == 1) prefetch(tile_of<TN, CG>(p, before, first, pair_rank, &hint));
     if (warp == 2) {
         if constexpr (CG == 2) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::COLS));
@@ -236,20 +246,25 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
     __syncthreads();
     if (CG == 2) cluster_sync();  // both blocks' barriers exist before either uses the other's
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = tmem_at;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
     const int tiles = p.n_tiles * (p.groups ? before[p.groups] : (p.M + TN - 1) / TN);
 
     const auto produce = [&](const Tile& t) {
         if (!pre && !waited) prefetch(t);
         rely();
-        for (int i = 0; i < pre; i++) load_a(t, i, k0 + i);
+        if (elected())
+            for (int i = 0; i < pre; i++) load_a(t, i, k0 + i);
+        __syncwarp();
         it += pre;
         for (int kb = k0 + pre; kb < k1; kb++, it++) {
             const int s = it % S::STAGES;
             if (!mbar_wait(empty(s), ((it / S::STAGES) & 1) ^ 1, &gave_up)) return;
-            expect(t, s);
-            load_w(t, s, kb);
-            load_a(t, s, kb);
+            if (elected()) {
+                expect(t, s);
+                load_w(t, s, kb);
+                load_a(t, s, kb);
+            }
+            __syncwarp();
         }
         pre = 0;
     };
@@ -265,11 +280,14 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
             if (!mbar_wait(full(s), (it / S::STAGES) & 1, &gave_up)) return;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint64_t w = operand(base + s * S::STAGE), a = operand(base + s * S::STAGE + CH * KB);
+            if (elected()) {
 #pragma unroll
-            for (int k = 0; k < KB / 32; k++) mma_i8<CG>(tmem + b * TN, w + 2 * k, a + 2 * k, desc, (kb > k0 || k > 0) ? 1u : 0u);
-            mma_commit<CG>(empty(s));
+                for (int k = 0; k < KB / 32; k++) mma_i8<CG>(tmem + b * TN, w + 2 * k, a + 2 * k, desc, (kb > k0 || k > 0) ? 1u : 0u);
+                mma_commit<CG>(empty(s));
+                if (kb == k1 - 1) mma_commit<CG>(acc_full(b));
+            }
+            __syncwarp();
         }
-        mma_commit<CG>(acc_full(b));
     };
     const auto scaled = [&](int sum, float sa, float sw, float bias) {
         // a sum passes 2^24 from K = 1024 on: its conversion to 32-bit floating point is a rounding, like each scale's product
@@ -281,38 +299,44 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
         const bool in = chan < p.N;
         const long long gc = (long long)t.group * p.N + chan;
         const float sw = in ? p.w_scale[gc] : 0.f, bias = (in && p.bias) ? p.bias[gc] : 0.f;
-        float sa[(TN + 31) / 32];  // scales of the tile's rows, row 32 i + lane in sa[i]: loaded while the products are formed
+        // The tile's columns in blocks of 32, in turn to the two warps of a quarter; the scale of a block's row 32 i + lane is loaded while the
+        // products are formed.
+        constexpr int C = TN < 32 ? TN : 32, U = (TN + 63) / 64;
+        const int half = (warp - 4) >> 2;
+        float sa[U];
 #pragma unroll
-        for (int i = 0; i < (TN + 31) / 32; i++) sa[i] = i * 32 + lane < t.rows ? p.a_scale[t.row + i * 32 + lane] : 0.f;
-        const bool ok = !p.k_blocks || mbar_wait(acc_full(b), (acc >> 1) & 1, &gave_up);
-        if (!__all_sync(0xffffffffu, ok)) return;
+        for (int u = 0; u < U; u++) {
+            const int r = (2 * u + half) * 32 + lane;
+            sa[u] = r < t.rows ? p.a_scale[t.row + r] : 0.f;
+        }
+        if (p.k_blocks && !mbar_wait(acc_full(b), (acc >> 1) & 1, &gave_up)) return;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + b * TN;
 #pragma unroll
-        for (int i = 0; i < (TN + 31) / 32; i++) {
-            if (i * 32 >= t.rows) break;
+        for (int u = 0; u < U; u++) {
+            const int c0 = (2 * u + half) * 32;
+            if (c0 >= t.rows) break;
             int v[32];
             __syncwarp();
             if (p.k_blocks) {
-                tmem_load(at + i * 32, *(int(*)[16])v);
-                if (TN > 16) tmem_load(at + i * 32 + 16, *(int(*)[16])(v + 16));
+                tmem_load(at + c0, *(int(*)[16])v);
+                if (TN > 16) tmem_load(at + c0 + 16, *(int(*)[16])(v + 16));
                 tmem_arrived();
             } else {
 #pragma unroll
                 for (int j = 0; j < 32; j++) v[j] = 0;
             }
-            constexpr int C = TN < 32 ? TN : 32;
             T o[C];  // all of them before the first store: a branch for each would leave its chain of latencies bare
 #pragma unroll
-            for (int j = 0; j < C; j++) o[j] = scaled(v[j], __shfl_sync(0xffffffffu, sa[i], j), sw, bias);
-            T* y = (T*)p.y + (long long)(t.row + i * 32) * p.ldy + chan;
-            if (in && i * 32 + C <= t.rows) {
+            for (int j = 0; j < C; j++) o[j] = scaled(v[j], __shfl_sync(0xffffffffu, sa[u], j), sw, bias);
+            T* y = (T*)p.y + (long long)(t.row + c0) * p.ldy + chan;
+            if (in && c0 + C <= t.rows) {
 #pragma unroll
                 for (int j = 0; j < C; j++, y += p.ldy) *y = o[j];
             } else if (in) {
 #pragma unroll
                 for (int j = 0; j < C; j++, y += p.ldy)
-                    if (i * 32 + j < t.rows) *y = o[j];
+                    if (c0 + j < t.rows) *y = o[j];
             }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -325,10 +349,10 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
     const auto stopped = [&] { return *(volatile int*)&gave_up != 0; };
 
     if (splits == 1) {
-        if (warp == 0 && lane == 0) {
+        if (warp == 0) {
             if (p.k_blocks)
                 for (int t = first; t < tiles && !stopped(); t += step) produce(tile_of<TN, CG>(p, before, t, pair_rank, &hint));
-        } else if (warp == 1 && lane == 0 && pair_rank == 0) {
+        } else if (warp == 1 && pair_rank == 0) {
             if (p.k_blocks)
                 for (int t = first; t < tiles && !stopped(); t += step, acc++) multiply(tile_of<TN, CG>(p, before, t, pair_rank, &hint));
         } else if (warp >= 4) {
@@ -342,14 +366,14 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
         int* part = (int*)(dynamic + (base - smem_addr(dynamic)));
         for (int t = first; t < tiles; t += step, acc++) {
             const Tile tile = tile_of<TN, CG>(p, before, t, 0, &hint);
-            if (warp == 0 && lane == 0) produce(tile);
-            if (warp == 1 && lane == 0) multiply(tile);
+            if (warp == 0) produce(tile);
+            if (warp == 1) multiply(tile);
             if (warp >= 4) {
                 const int b = acc & 1, quarter = warp & 3;
                 const bool ok = mbar_wait(acc_full(b), (acc >> 1) & 1, &gave_up);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (__all_sync(0xffffffffu, ok))
-                    for (int c0 = 0; c0 < tile.rows; c0 += 16) {
+                if (ok)
+                    for (int c0 = ((warp - 4) >> 2) * 16; c0 < tile.rows; c0 += 32) {
                         int v[16];
                         tmem_load(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + c0, v);
                         tmem_arrived();
@@ -363,13 +387,21 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
             rely();
             __syncwarp();
             cluster_sync();
-            const int total = tile.rows * CH, lo = (int)((long long)total * rank / splits), hi = (int)((long long)total * (rank + 1) / splits);
+            const int total = tile.rows * (CH / 4), lo = total * rank / splits, hi = total * (rank + 1) / splits;  // four channels at a time
             for (int i = lo + (int)threadIdx.x; i < hi; i += MM_THREADS) {
-                int sum = 0;
-                for (int r = 0; r < splits; r++) sum += cluster_load(base + 4 * i, r);
-                const int chan = tile.chan + i % CH, row = tile.row + i / CH;
+                int4 part_of[8];
+#pragma unroll
+                for (int r = 0; r < 8; r++) part_of[r] = r < splits ? cluster_load(base + 16 * i, r) : make_int4(0, 0, 0, 0);
+                int sum[4] = {};
+#pragma unroll
+                for (int r = 0; r < 8; r++) sum[0] += part_of[r].x, sum[1] += part_of[r].y, sum[2] += part_of[r].z, sum[3] += part_of[r].w;
+                const int chan = tile.chan + i % (CH / 4) * 4, row = tile.row + i / (CH / 4);
                 const long long gc = (long long)tile.group * p.N + chan;
-                if (chan < p.N) ((T*)p.y)[(long long)row * p.ldy + chan] = scaled(sum, p.a_scale[row], p.w_scale[gc], p.bias ? p.bias[gc] : 0.f);
+                const float sa = p.a_scale[row];
+                T* y = (T*)p.y + (long long)row * p.ldy + chan;
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (chan + j < p.N) y[j] = scaled(sum[j], sa, p.w_scale[gc + j], p.bias ? p.bias[gc + j] : 0.f);
             }
             // what the generic proxy read and wrote here, the next tile's loads will overwrite
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -479,23 +511,55 @@ template <typename T, int TN, int CG> cudaError_t tiles_launch(const MatmulParam
     return cudaLaunchKernelEx(&cfg, hccl_matmul_i8_tiles<T, TN, CG>, p);
 }
 
+// Which tile. Tiles of TN tokens and a cluster of S blocks for each, by an estimate in microseconds fitted to measurements on 15 shapes from 1 x 8192 x 4096 to 2048^3:
+// rounds of the blocks over the tiles, times the stages of one, times a stage's time (0.15 while fetching is the bound, 0.27 for a
+// pair's 2 x 512 cycles of products), and what does not overlap: the last tile's results and the cluster's exchange. One round of a cluster may take 128 blocks at most: more
+// than that do not find their neighbouring SMs free at once (measured: 16 x 8192 x 4096 with S = 4, 256 blocks, 15.2 us against 11.4 with S = 2).
+struct Choice {
+    int tn, splits;
+};
+Choice choose(const MatmulParams& p) {
+    const double k_blocks = (double)((p.K + KB - 1) / KB);
+    if (p.groups) {
+        // Groups are uneven: tiles of twice the mean number of rows hold most groups whole, so that weights are read once
+        // (64 groups, 512 rows, 2048 x 4096: 80 us with 16 to 64, 83 with 256; 4096 rows: 91 with 128, 128 with 32).
+        const long long twice = 2 * ((p.M + p.groups - 1) / p.groups);
+        return {twice <= 16 ? 16 : twice <= 32 ? 32 : twice <= 64 ? 64 : twice <= 128 ? 128 : 256, 1};
+    }
+    static const struct {
+        int tn;
+        double stage, last, exchange;
+    } option[] = {{16, 0.15, 0.0, 1.0}, {32, 0.15, 0.1, 1.5}, {64, 0.16, 0.4, 2.4}, {128, 0.20, 1.2, 0}, {256, 0.27, 3.0, 0}};
+    Choice best = {256, 1};
+    double least = 1e30;
+    for (const auto& o : option) {
+        const bool pair = o.tn == 256;
+        const long long tiles = (p.M + o.tn - 1) / o.tn * ((p.N + (pair ? 2 * CH : CH) - 1) / (pair ? 2 * CH : CH)), at_once = pair ? SMS / 2 : SMS;
+        for (int s = 1; s <= (o.tn <= 64 ? 8 : 1); s *= 2) {
+            if (s > 1 && (tiles * s > (s == 8 ? 64 : 128) || k_blocks < 4 * s)) break;
+            const double t = (double)((tiles + at_once - 1) / at_once) * (k_blocks / s) * o.stage + o.last + (s > 1 ? o.exchange : 0);
+            if (t < least) least = t, best = {o.tn, s};
+        }
+    }
+    return best;
+}
+
 template <typename T> cudaError_t matmul_launch(const MatmulParams& p, cudaStream_t s) {
-    const long long rows = p.groups ? (p.M + p.groups - 1) / p.groups : p.M;  // of a group, if they were even
-    const int k_blocks = (int)((p.K + KB - 1) / KB), n_tiles = (int)((p.N + CH - 1) / CH);
-    int splits = 1;
-    if (rows <= 64)  // few rows: the weights' bytes are the time, and all SMs are to fetch them
-        while (splits < 8 && (long long)n_tiles * splits * 2 * (p.groups ? p.groups : 1) <= SMS && splits * 2 * 4 <= k_blocks) splits *= 2;
-    if (rows <= 16) return tiles_launch<T, 16, 1>(p, splits, s);
-    if (rows <= 32) return tiles_launch<T, 32, 1>(p, splits, s);
-    if (rows <= 64) return tiles_launch<T, 64, 1>(p, splits, s);
-    if (rows <= 128) return tiles_launch<T, 128, 1>(p, 1, s);
-    return tiles_launch<T, 256, 2>(p, 1, s);
+    const Choice c = choose(p);
+    switch (c.tn) {
+        case 16: return tiles_launch<T, 16, 1>(p, c.splits, s);
+        case 32: return tiles_launch<T, 32, 1>(p, c.splits, s);
+        case 64: return tiles_launch<T, 64, 1>(p, c.splits, s);
+        case 128: return tiles_launch<T, 128, 1>(p, 1, s);
+        default: return tiles_launch<T, 256, 2>(p, 1, s);
+    }
 }
 
 }  // namespace
 
 cudaError_t launch_matmul_i8(int dt, const MatmulParams& p, cudaStream_t s) {
     if (p.M == 0 || p.N == 0) return cudaSuccess;
+    if (few_rows(p)) return launch_matmul_i8_few(dt, p, s);
     if (dt == HCCL_FP32) return matmul_launch<float>(p, s);
     if (dt == HCCL_BF16) return matmul_launch<__nv_bfloat16>(p, s);
     return matmul_launch<__half>(p, s);

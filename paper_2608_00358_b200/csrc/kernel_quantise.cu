@@ -3,75 +3,11 @@
 // holds its row in registers between the maximum and the rounding, so every element is read once.
 #include <algorithm>
 
-#include "experts.cuh"
+#include "rows_i8.cuh"
 
 namespace hccl {
 namespace experts {
 namespace {
-
-constexpr float TINY = 1e-30f;  // below it 1 / max could overflow
-
-// 16 bytes of a row as they lie in memory, beyond K zeros.
-template <typename T> struct Sixteen {
-    static constexpr int N = 16 / sizeof(T);
-    unsigned w[4];
-    __device__ __forceinline__ void load(const T* x, int i, int K, bool vec) {
-        if (vec && i + N <= K) {
-            const uint4 v = *(const uint4*)(x + i);
-            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-        } else {
-#pragma unroll
-            for (int u = 0; u < 4; u++) {
-                w[u] = 0;
-#pragma unroll
-                for (int j = 0; j < N / 4; j++) {
-                    const int at = i + u * (N / 4) + j;
-                    if (at < K) w[u] |= (sizeof(T) == 4 ? ((const unsigned*)x)[at] : (unsigned)((const unsigned short*)x)[at]) << (16 * j);
-                }
-            }
-        }
-    }
-    // The largest magnitude, as the bits of a number that is not negative: they are in the numbers' order, with NaN above infinity, so that it sticks.
-    __device__ __forceinline__ unsigned magnitude() const;
-    __device__ __forceinline__ float value(int j) const;
-};
-template <> __device__ __forceinline__ unsigned Sixteen<float>::magnitude() const {
-    return max(max(w[0] & 0x7fffffffu, w[1] & 0x7fffffffu), max(w[2] & 0x7fffffffu, w[3] & 0x7fffffffu));
-}
-template <> __device__ __forceinline__ float Sixteen<float>::value(int j) const { return __uint_as_float(w[j]); }
-template <> __device__ __forceinline__ unsigned Sixteen<__nv_bfloat16>::magnitude() const {
-    __nv_bfloat162 m[4];
-#pragma unroll
-    for (int u = 0; u < 4; u++) {
-        const unsigned a = w[u] & 0x7fff7fffu;
-        m[u] = *(const __nv_bfloat162*)&a;
-    }
-    const __nv_bfloat162 r = __hmax2_nan(__hmax2_nan(m[0], m[1]), __hmax2_nan(m[2], m[3]));
-    return max(__float_as_uint(__low2float(r)), __float_as_uint(__high2float(r))) & 0x7fffffffu;
-}
-template <> __device__ __forceinline__ float Sixteen<__nv_bfloat16>::value(int j) const { return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16); }
-template <> __device__ __forceinline__ unsigned Sixteen<__half>::magnitude() const {
-    __half2 m[4];
-#pragma unroll
-    for (int u = 0; u < 4; u++) {
-        const unsigned a = w[u] & 0x7fff7fffu;
-        m[u] = *(const __half2*)&a;
-    }
-    const __half2 r = __hmax2_nan(__hmax2_nan(m[0], m[1]), __hmax2_nan(m[2], m[3]));
-    return max(__float_as_uint(__low2float(r)) & 0x7fffffffu, __float_as_uint(__high2float(r)) & 0x7fffffffu);
-}
-template <> __device__ __forceinline__ float Sixteen<__half>::value(int j) const {
-    const unsigned short h = (unsigned short)(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu);
-    return __half2float(__ushort_as_half(h));
-}
-
-// Four numbers within [-127.5, 127.5] to bytes. Adding 1.5 * 2^23 leaves the number, rounded half to even, in the low bits.
-__device__ __forceinline__ unsigned four_bytes(float a, float b, float c, float d) {
-    const float big = 12582912.f;
-    const unsigned lo = __byte_perm(__float_as_uint(__fadd_rn(a, big)), __float_as_uint(__fadd_rn(b, big)), 0x0040);
-    const unsigned hi = __byte_perm(__float_as_uint(__fadd_rn(c, big)), __float_as_uint(__fadd_rn(d, big)), 0x0040);
-    return __byte_perm(lo, hi, 0x5410);
-}
 
 // A thread holds P pieces of 16 bytes; rows longer than the block holds are read a second time.
 template <typename T, int P> __global__ void __launch_bounds__(512) hccl_quantise_rows(const __grid_constant__ QuantParams p) {
@@ -96,20 +32,15 @@ template <typename T, int P> __global__ void __launch_bounds__(512) hccl_quantis
             __syncthreads();
             bits = __reduce_max_sync(0xffffffffu, threadIdx.x % 32 < warps ? part[turn][threadIdx.x % 32] : 0u);
         }
-        const float top = __uint_as_float(bits);
-        const bool finite = top < INFINITY, some = finite && top >= TINY;
-        const float inv = some ? __fmul_rn(1.f / top, 127.f) : 0.f;
-        const float scale = !finite ? __int_as_float(0x7fc00000) : some ? top / 127.f : 0.f;
+        float factor, scale;
+        row_scale(bits, &factor, &scale);
         for (int at = 0; at < K; at += span) {
             unsigned o[P][N / 4];
 #pragma unroll
             for (int u = 0; u < P; u++) {
                 if (span < K) v[u].load(x, at + (u * threads + (int)threadIdx.x) * N, K, p.vec);
 #pragma unroll
-                for (int j = 0; j < N / 4; j++)
-                    o[u][j] = some ? four_bytes(__fmul_rn(v[u].value(4 * j), inv), __fmul_rn(v[u].value(4 * j + 1), inv), __fmul_rn(v[u].value(4 * j + 2), inv),
-                                                __fmul_rn(v[u].value(4 * j + 3), inv))
-                                   : 0u;
+                for (int j = 0; j < N / 4; j++) o[u][j] = quantised(v[u], 4 * j, factor);
             }
             for (int c = 0; c < copies; c++) {
                 const long long row = p.slots ? p.slots[m * p.top_k + c] : m;

@@ -1,0 +1,234 @@
+// Products in 8-bit integers for at most 8 rows: the weights are read once and their bytes are the time, so a call's fixed cost is what can
+// be saved. Against the kernel of tiles (tensor memory, tensor maps, a cluster that adds its parts, the quantiser's launch before it) this one
+// starts loading weights with its first instruction and quantises the rows itself where they are short.
+//
+// mma.sync m16n8k32: 16 channels x 8 rows. A warp takes 64 bytes of K of 16 channels at a time, straight from memory to the registers of
+// the instruction: lane 4g + t loads bytes 16t .. 16t + 15 of channels g and g + 8, two instructions' worth. That hands the instruction its
+// columns of K in another order than they have in memory, the same for both operands, and a sum does not mind. Eight such loads are in flight for each warp, across
+// the end of a group of channels. The 8 warps of a block share K and add their sums, exact integers, in shared memory.
+#include <algorithm>
+
+#include "rows_i8.cuh"
+
+namespace hccl {
+namespace experts {
+namespace {
+
+constexpr int FEW_THREADS = 256, FEW_WARPS = FEW_THREADS / 32, DEEP = 8;
+
+struct FewParams {
+    MatmulParams m;
+    const void* x;  // null: m.a and m.a_scale hold the rows in 8 bits
+    long long ldx;
+    int x_dt, x_vec, q_stride;
+};
+
+template <typename X> __device__ __forceinline__ void largest(const FewParams& p, unsigned* top) {
+    constexpr int N = Sixteen<X>::N;
+    const int K = (int)p.m.K, pieces = (K + N - 1) / N;
+    for (int r = 0; r < (int)p.m.M; r++) {
+        unsigned bits = 0;
+        for (int i = threadIdx.x; i < pieces; i += FEW_THREADS) {
+            Sixteen<X> v;
+            v.load((const X*)p.x + r * p.ldx, i * N, K, p.x_vec);
+            bits = max(bits, v.magnitude());
+        }
+        bits = __reduce_max_sync(0xffffffffu, bits);
+        if (threadIdx.x % 32 == 0) atomicMax(&top[r], bits);
+    }
+}
+template <typename X> __device__ __forceinline__ void quantise(const FewParams& p, const unsigned* top, float* scale, char* q) {
+    constexpr int N = Sixteen<X>::N;
+    const int K = (int)p.m.K, pieces = p.q_stride / N;  // zeros beyond K
+    for (int r = 0; r < (int)p.m.M; r++) {
+        float factor, s;
+        row_scale(top[r], &factor, &s);
+        if (threadIdx.x == 0) scale[r] = s;
+        for (int i = threadIdx.x; i < pieces; i += FEW_THREADS) {
+            Sixteen<X> v;
+            v.load((const X*)p.x + r * p.ldx, i * N, K, p.x_vec);
+            unsigned* to = (unsigned*)(q + r * p.q_stride + i * N);
+#pragma unroll
+            for (int j = 0; j < N / 4; j++) to[j] = quantised(v, 4 * j, factor);
+        }
+    }
+}
+
+__device__ __forceinline__ uint4 load_once(const int8_t* at) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at));
+    return v;
+}
+__device__ __forceinline__ void mma(int (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <typename T> __global__ void __launch_bounds__(FEW_THREADS, 2) hccl_matmul_i8_few(const __grid_constant__ FewParams p) {
+    extern __shared__ __align__(16) char q[];  // [M][q_stride] rows in 8 bits
+    __shared__ unsigned top[8];
+    __shared__ float scale[8];
+    __shared__ int part[2][FEW_WARPS][128];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    const int K = (int)p.m.K, M = (int)p.m.M, N = (int)p.m.N;
+    const int groups = (N + 15) / 16, chunks = (K + 63) / 64, per = (chunks + FEW_WARPS - 1) / FEW_WARPS;  // chunks of a warp in a group of channels
+    const int mine = ((int)blockIdx.x < groups) ? (groups - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+    const int items = mine * per;
+
+    // Item i: chunk warp + 8 (i % per) of the block's channel group i / per; what lies beyond K or the items is zero.
+    int next_group = (int)blockIdx.x, next_chunk = 0, asked = 0;
+    const auto piece = [&](const int8_t* row, int k) {
+        if (k + 16 <= K) return load_once(row + k);
+        unsigned w[4] = {0, 0, 0, 0};
+        for (int j = 0; j < 16 && k + j < K; j++) w[j / 4] |= (unsigned)(uint8_t)row[k + j] << (8 * (j & 3));
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    };
+    const auto fetch = [&](uint4& lo, uint4& hi) {
+        lo = hi = make_uint4(0, 0, 0, 0);
+        if (asked < items) {
+            const int k = (warp + FEW_WARPS * next_chunk) * 64 + t * 16;
+            if (k < K) {
+                const int c = next_group * 16 + g;
+                lo = piece(p.m.w + (long long)min(c, N - 1) * p.m.ldw, k);
+                hi = piece(p.m.w + (long long)min(c + 8, N - 1) * p.m.ldw, k);
+            }
+            asked++;
+            if (++next_chunk == per) next_chunk = 0, next_group += (int)gridDim.x;
+        }
+    };
+    uint4 lo[DEEP], hi[DEEP];
+#pragma unroll
+    for (int u = 0; u < DEEP; u++) fetch(lo[u], hi[u]);
+
+    if (threadIdx.x < 8) top[threadIdx.x] = 0;
+    if (p.m.dependent) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (p.x) {
+        __syncthreads();
+        if (p.x_dt == HCCL_FP32) largest<float>(p, top);
+        else if (p.x_dt == HCCL_BF16) largest<__nv_bfloat16>(p, top);
+        else largest<__half>(p, top);
+        __syncthreads();
+        if (p.x_dt == HCCL_FP32) quantise<float>(p, top, scale, q);
+        else if (p.x_dt == HCCL_BF16) quantise<__nv_bfloat16>(p, top, scale, q);
+        else quantise<__half>(p, top, scale, q);
+    } else {
+        const int pieces = p.q_stride / 16;
+        for (int i = threadIdx.x; i < M * pieces; i += FEW_THREADS) {
+            const int r = i / pieces, k = i % pieces * 16;
+            const int8_t* row = p.m.a + r * p.m.lda;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (k + 16 <= K) v = *(const uint4*)(row + k);
+            else if (k < K) {
+                unsigned w[4] = {0, 0, 0, 0};
+                for (int j = 0; j < 16 && k + j < K; j++) w[j / 4] |= (unsigned)(uint8_t)row[k + j] << (8 * (j & 3));
+                v = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            *(uint4*)(q + r * p.q_stride + k) = v;
+        }
+        if (threadIdx.x < M) scale[threadIdx.x] = p.m.a_scale[threadIdx.x];
+    }
+    __syncthreads();
+
+    int acc[4] = {0, 0, 0, 0}, chunk = 0, group = (int)blockIdx.x, turn = 0;
+    const char* row = q + min(g, M - 1) * p.q_stride + t * 16;
+    for (int i0 = 0; i0 < items; i0 += DEEP) {
+#pragma unroll
+        for (int u = 0; u < DEEP; u++) {
+            if (i0 + u >= items) break;
+            const int at = (warp + FEW_WARPS * chunk) * 64;
+            uint4 b = make_uint4(0, 0, 0, 0);
+            if (g < M && at < K) b = *(const uint4*)(row + at);
+            mma(acc, lo[u].x, hi[u].x, lo[u].y, hi[u].y, b.x, b.y);
+            mma(acc, lo[u].z, hi[u].z, lo[u].w, hi[u].w, b.z, b.w);
+            fetch(lo[u], hi[u]);
+            if (++chunk == per) {  // the same for all warps
+                chunk = 0;
+                int* to = part[turn][warp];  // [channel][row]
+                *(int2*)(to + g * 8 + 2 * t) = make_int2(acc[0], acc[1]);
+                *(int2*)(to + (g + 8) * 8 + 2 * t) = make_int2(acc[2], acc[3]);
+                acc[0] = acc[1] = acc[2] = acc[3] = 0;
+                __syncthreads();
+                if (threadIdx.x < 128) {
+                    const int c = threadIdx.x % 16, r = threadIdx.x / 16, chan = group * 16 + c;
+                    if (chan < N && r < M) {
+                        int sum = 0;
+#pragma unroll
+                        for (int w = 0; w < FEW_WARPS; w++) sum += part[turn][w][c * 8 + r];
+                        float v = __fmul_rn(__fmul_rn((float)sum, scale[r]), p.m.w_scale[chan]);
+                        if (p.m.bias) v = __fadd_rn(v, p.m.bias[chan]);
+                        ((T*)p.m.y)[r * p.m.ldy + chan] = from_f32<T>(v);
+                    }
+                }
+                turn ^= 1;  // the next group's sums go elsewhere: they are not written over before the barrier after next
+                group += (int)gridDim.x;
+            }
+        }
+    }
+}
+
+// Shared memory for the rows: a third of an SM's, so that two blocks fit with room to spare.
+constexpr long long FEW_SMEM = 72 * 1024;
+int few_stride(long long K) { return (int)((K + 63) / 64 * 64 + 16); }  // 16: the rows of a quarter warp start on different banks
+
+template <typename T> cudaError_t few_launch(const FewParams& in, cudaStream_t s) {
+    FewParams p = in;
+    p.q_stride = few_stride(p.m.K);
+    const size_t smem = (size_t)p.m.M * p.q_stride;
+    if (smem > 40 * 1024) {
+        static bool ready[64];
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        if (dev >= 64 || !ready[dev]) {
+            e = cudaFuncSetAttribute(hccl_matmul_i8_few<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FEW_SMEM);
+            if (e != cudaSuccess) return e;
+            if (dev < 64) ready[dev] = true;
+        }
+    }
+    const long long groups = (p.m.N + 15) / 16;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<long long>(groups, 2 * SMS));
+    cfg.blockDim = dim3(FEW_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = p.m.dependent ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, hccl_matmul_i8_few<T>, p);
+}
+
+cudaError_t few(int dt, const FewParams& p, cudaStream_t s) {
+    if (dt == HCCL_FP32) return few_launch<float>(p, s);
+    if (dt == HCCL_BF16) return few_launch<__nv_bfloat16>(p, s);
+    return few_launch<__half>(p, s);
+}
+
+}  // namespace
+
+bool few_rows(const MatmulParams& p) { return p.groups == 0 && p.M <= 8 && p.K > 0 && p.M * few_stride(p.K) <= FEW_SMEM; }
+
+// Rows short enough for every block to quantise them again: two passes over them out of the L2 are hidden behind the weights then.
+bool few_rows_quantise(const MatmulParams& p) { return p.M * p.K <= 16384; }
+
+cudaError_t launch_matmul_i8_few(int dt, const MatmulParams& m, cudaStream_t s) {
+    FewParams p = {};
+    p.m = m;
+    return few(dt, p, s);
+}
+
+cudaError_t launch_linear_i8_few(int dt, const MatmulParams& m, const QuantParams& x, int x_dt, cudaStream_t s) {
+    FewParams p = {};
+    p.m = m;
+    p.x = x.x;
+    p.ldx = x.ldx;
+    p.x_dt = x_dt;
+    const int es = x_dt == HCCL_FP32 ? 4 : 2;
+    p.x_vec = (uintptr_t)x.x % 16 == 0 && (x.ldx * es) % 16 == 0;
+    return few(dt, p, s);
+}
+
+}  // namespace experts
+}  // namespace hccl

@@ -601,7 +601,7 @@ hccl_status_t hccl_quantize_rows_i8(const void* x, int64_t ldx, int64_t M, int64
 /* Products in 8-bit integers: y[m,n] = round(float(sum_k a[m,k] * w[g,n,k]) * a_scale[m] * w_scale[g,n] (+ bias[g,n])), the sum
  * exact in 32-bit integers. groups 0: one matrix for all M rows. groups > 0: row m belongs to group g when
  * offsets[g] <= m < offsets[g+1] (device memory, ascending, at most M; rows outside all groups are left alone), and a group without rows costs nothing.
- * a and w must start on 16-byte boundaries with lda and ldw multiples of 16; row n of group g starts at
+ * a and w must start on 16-byte boundaries with lda and ldw multiples of 16 (a row is read, not used, up to the next multiple of 16 from K); row n of group g starts at
  * w + (g * N + n) * ldw. y: any stride, type dt. dev_status: one device int32 or NULL; a failure on the device
  * (a bounded wait that ran out, HCCL_ERR_TIMEOUT) is stored there and y is then undefined; nothing is stored otherwise. */
 typedef struct {

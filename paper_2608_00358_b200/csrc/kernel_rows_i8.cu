@@ -2,10 +2,10 @@
 // be saved. Against the kernel of tiles (tensor memory, tensor maps, a cluster that adds its parts, the quantiser's launch before it) this one
 // starts loading weights with its first instruction and quantises the rows itself where they are short.
 //
-// mma.sync m16n8k32: 16 channels x 8 rows. A warp takes 64 bytes of K of 16 channels at a time, straight from memory to the registers of
-// the instruction: lane 4g + t loads bytes 16t .. 16t + 15 of channels g and g + 8, two instructions' worth. That hands the instruction its
-// columns of K in another order than they have in memory, the same for both operands, and a sum does not mind. Eight such loads are in flight for each warp, across
-// the end of a group of channels. The 8 warps of a block share K and add their sums, exact integers, in shared memory.
+// mma.sync m16n8k32: 16 channels x 8 rows. A warp takes 128 bytes of K of 16 channels at a time, straight from memory to the registers of
+// the instruction: of each half, lane 4g + t loads bytes 16t .. 16t + 15 of channels g and g + 8, two instructions' worth. That hands the instruction its
+// columns of K in another order than they have in memory, the same for both operands, and a sum does not mind. Four such items (8 KB) are in flight for
+// each warp, across the end of a group of channels. The 8 warps of a block share K and add their sums, exact integers, in shared memory.
 #include <algorithm>
 
 #include "rows_i8.cuh"
@@ -14,7 +14,7 @@ namespace hccl {
 namespace experts {
 namespace {
 
-constexpr int FEW_THREADS = 256, FEW_WARPS = FEW_THREADS / 32, DEEP = 8;
+constexpr int FEW_THREADS = 256, FEW_WARPS = FEW_THREADS / 32, DEEP = 4, ITEM = 128 /* bytes of K */;
 
 struct FewParams {
     MatmulParams m;
@@ -39,7 +39,7 @@ template <typename X> __device__ __forceinline__ void largest(const FewParams& p
 }
 template <typename X> __device__ __forceinline__ void quantise(const FewParams& p, const unsigned* top, float* scale, char* q) {
     constexpr int N = Sixteen<X>::N;
-    const int K = (int)p.m.K, pieces = p.q_stride / N;  // zeros beyond K
+    const int K = (int)p.m.K, pieces = (p.q_stride - 16) / N;  // zeros beyond K
     for (int r = 0; r < (int)p.m.M; r++) {
         float factor, s;
         row_scale(top[r], &factor, &s);
@@ -72,34 +72,31 @@ template <typename T> __global__ void __launch_bounds__(FEW_THREADS, 2) hccl_mat
     __shared__ int part[2][FEW_WARPS][128];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     const int K = (int)p.m.K, M = (int)p.m.M, N = (int)p.m.N;
-    const int groups = (N + 15) / 16, chunks = (K + 63) / 64, per = (chunks + FEW_WARPS - 1) / FEW_WARPS;  // chunks of a warp in a group of channels
-    const int mine = ((int)blockIdx.x < groups) ? (groups - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
-    const int items = mine * per;
+    const int groups = (N + 15) / 16, per = (K + ITEM * FEW_WARPS - 1) / (ITEM * FEW_WARPS);  // items of a warp in a group of channels
+    const int mine = (groups - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x, items = mine * per;
+    const int k_first = warp * ITEM + t * 16;
 
-    // Item i: chunk warp + 8 (i % per) of the block's channel group i / per; what lies beyond K or the items is zero.
-    int next_group = (int)blockIdx.x, next_chunk = 0, asked = 0;
-    const auto piece = [&](const int8_t* row, int k) {
-        if (k + 16 <= K) return load_once(row + k);
-        unsigned w[4] = {0, 0, 0, 0};
-        for (int j = 0; j < 16 && k + j < K; j++) w[j / 4] |= (unsigned)(uint8_t)row[k + j] << (8 * (j & 3));
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    };
-    const auto fetch = [&](uint4& lo, uint4& hi) {
-        lo = hi = make_uint4(0, 0, 0, 0);
-        if (asked < items) {
-            const int k = (warp + FEW_WARPS * next_chunk) * 64 + t * 16;
-            if (k < K) {
-                const int c = next_group * 16 + g;
-                lo = piece(p.m.w + (long long)min(c, N - 1) * p.m.ldw, k);
-                hi = piece(p.m.w + (long long)min(c + 8, N - 1) * p.m.ldw, k);
-            }
-            asked++;
-            if (++next_chunk == per) next_chunk = 0, next_group += (int)gridDim.x;
+    // Item i: bytes from (warp + 8 (i % per)) * ITEM on of the block's channel group i / per. Pieces beyond K or beyond the items are zero.
+    int asked = 0, ask_k = k_first, ask_n = 0, ask_group = (int)blockIdx.x;
+    const int8_t *lo_row = p.m.w + (long long)min(ask_group * 16 + g, N - 1) * p.m.ldw, *hi_row = p.m.w + (long long)min(ask_group * 16 + 8 + g, N - 1) * p.m.ldw;
+    const auto fetch = [&](uint4 (&v)[4]) {
+        const bool some = asked < items;
+        v[0] = v[1] = v[2] = v[3] = make_uint4(0, 0, 0, 0);
+        if (some && ask_k < K) v[0] = load_once(lo_row + ask_k), v[1] = load_once(hi_row + ask_k);
+        if (some && ask_k + 64 < K) v[2] = load_once(lo_row + ask_k + 64), v[3] = load_once(hi_row + ask_k + 64);
+        asked++;
+        ask_k += ITEM * FEW_WARPS;
+        if (++ask_n == per) {
+            ask_n = 0;
+            ask_k = k_first;
+            ask_group += (int)gridDim.x;
+            lo_row = p.m.w + (long long)min(ask_group * 16 + g, N - 1) * p.m.ldw;
+            hi_row = p.m.w + (long long)min(ask_group * 16 + 8 + g, N - 1) * p.m.ldw;
         }
     };
-    uint4 lo[DEEP], hi[DEEP];
+    uint4 v[DEEP][4];
 #pragma unroll
-    for (int u = 0; u < DEEP; u++) fetch(lo[u], hi[u]);
+    for (int u = 0; u < DEEP; u++) fetch(v[u]);
 
     if (threadIdx.x < 8) top[threadIdx.x] = 0;
     if (p.m.dependent) asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -113,16 +110,20 @@ template <typename T> __global__ void __launch_bounds__(FEW_THREADS, 2) hccl_mat
         else if (p.x_dt == HCCL_BF16) quantise<__nv_bfloat16>(p, top, scale, q);
         else quantise<__half>(p, top, scale, q);
     } else {
-        const int pieces = p.q_stride / 16;
+        const int pieces = (p.q_stride - 16) / 16;
         for (int i = threadIdx.x; i < M * pieces; i += FEW_THREADS) {
             const int r = i / pieces, k = i % pieces * 16;
             const int8_t* row = p.m.a + r * p.m.lda;
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (k + 16 <= K) v = *(const uint4*)(row + k);
-            else if (k < K) {
-                unsigned w[4] = {0, 0, 0, 0};
-                for (int j = 0; j < 16 && k + j < K; j++) w[j / 4] |= (unsigned)(uint8_t)row[k + j] << (8 * (j & 3));
-                v = make_uint4(w[0], w[1], w[2], w[3]);
+            if (k < K) {
+                v = *(const uint4*)(row + k);
+                if (k + 16 > K) {  // what the row's last 16 bytes hold beyond K
+                    unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int j = 0; j < 16; j++)
+                        if (k + j >= K) w[j / 4] &= ~(0xffu << (8 * (j & 3)));
+                    v = make_uint4(w[0], w[1], w[2], w[3]);
+                }
             }
             *(uint4*)(q + r * p.q_stride + k) = v;
         }
@@ -130,20 +131,23 @@ template <typename T> __global__ void __launch_bounds__(FEW_THREADS, 2) hccl_mat
     }
     __syncthreads();
 
-    int acc[4] = {0, 0, 0, 0}, chunk = 0, group = (int)blockIdx.x, turn = 0;
+    int acc[4] = {0, 0, 0, 0}, n = 0, at = warp * ITEM, group = (int)blockIdx.x, turn = 0;
     const char* row = q + min(g, M - 1) * p.q_stride + t * 16;
     for (int i0 = 0; i0 < items; i0 += DEEP) {
 #pragma unroll
         for (int u = 0; u < DEEP; u++) {
             if (i0 + u >= items) break;
-            const int at = (warp + FEW_WARPS * chunk) * 64;
-            uint4 b = make_uint4(0, 0, 0, 0);
-            if (g < M && at < K) b = *(const uint4*)(row + at);
-            mma(acc, lo[u].x, hi[u].x, lo[u].y, hi[u].y, b.x, b.y);
-            mma(acc, lo[u].z, hi[u].z, lo[u].w, hi[u].w, b.z, b.w);
-            fetch(lo[u], hi[u]);
-            if (++chunk == per) {  // the same for all warps
-                chunk = 0;
+            uint4 b0 = make_uint4(0, 0, 0, 0), b1 = b0;
+            if (g < M && at < p.q_stride - 16) b0 = *(const uint4*)(row + at), b1 = *(const uint4*)(row + at + 64);
+            mma(acc, v[u][0].x, v[u][1].x, v[u][0].y, v[u][1].y, b0.x, b0.y);
+            mma(acc, v[u][0].z, v[u][1].z, v[u][0].w, v[u][1].w, b0.z, b0.w);
+            mma(acc, v[u][2].x, v[u][3].x, v[u][2].y, v[u][3].y, b1.x, b1.y);
+            mma(acc, v[u][2].z, v[u][3].z, v[u][2].w, v[u][3].w, b1.z, b1.w);
+            fetch(v[u]);
+            at += ITEM * FEW_WARPS;
+            if (++n == per) {  // the same for all warps
+                n = 0;
+                at = warp * ITEM;
                 int* to = part[turn][warp];  // [channel][row]
                 *(int2*)(to + g * 8 + 2 * t) = make_int2(acc[0], acc[1]);
                 *(int2*)(to + (g + 8) * 8 + 2 * t) = make_int2(acc[2], acc[3]);
@@ -169,7 +173,7 @@ template <typename T> __global__ void __launch_bounds__(FEW_THREADS, 2) hccl_mat
 
 // Shared memory for the rows: a third of an SM's, so that two blocks fit with room to spare.
 constexpr long long FEW_SMEM = 72 * 1024;
-int few_stride(long long K) { return (int)((K + 63) / 64 * 64 + 16); }  // 16: the rows of a quarter warp start on different banks
+int few_stride(long long K) { return (int)((K + ITEM - 1) / ITEM * ITEM + 16); }  // 16: the rows of a quarter warp start on different banks
 
 template <typename T> cudaError_t few_launch(const FewParams& in, cudaStream_t s) {
     FewParams p = in;
@@ -211,7 +215,7 @@ cudaError_t few(int dt, const FewParams& p, cudaStream_t s) {
 bool few_rows(const MatmulParams& p) { return p.groups == 0 && p.M <= 8 && p.K > 0 && p.M * few_stride(p.K) <= FEW_SMEM; }
 
 // Rows short enough for every block to quantise them again: two passes over them out of the L2 are hidden behind the weights then.
-bool few_rows_quantise(const MatmulParams& p) { return p.M * p.K <= 16384; }
+bool few_rows_quantise(const MatmulParams& p) { return p.M * p.K <= 8192; }
 
 cudaError_t launch_matmul_i8_few(int dt, const MatmulParams& m, cudaStream_t s) {
     FewParams p = {};

@@ -22,6 +22,7 @@ import torch
 from . import binding as hb
 
 _DT = {torch.float32: hb.FP32, torch.bfloat16: hb.BF16, torch.float16: hb.FP16}
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -71,7 +72,7 @@ def _same(a: torch.Tensor, b: torch.Tensor, what: str):
 def _on(device: torch.device, call, *args):
     """call(*args, stream) with `device` current."""
     i = device.index
-    if i == torch.cuda.current_device():
+    if i == _current_device():
         call(*args, _stream(i))
     else:
         with torch.cuda.device(i):
@@ -183,7 +184,7 @@ class Router:
             _refuse(hb.ERR_COUNT_MISMATCH, "route backward: routing of %d tokens on %s" % (routing.tokens, routing.device))
         _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, logits.device)
         if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+            out = logits.new_empty(logits.shape)
         _same(out, logits, "route backward")
         ldd = _matrix(out, "dlogits", cols=self.experts, rows=routing.tokens)
         _on(logits.device, hb.hccl_route_backward, self._ref, logits.data_ptr(), ld, dt, b, m, routing.ref, dweights.data_ptr(), out.data_ptr(), ldd)
@@ -213,7 +214,7 @@ def _rows_in(rows: torch.Tensor, routing: Routing, what: str):
 
 def _new(out, shape, like, what):
     if out is None:
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
+        return like.new_empty(shape)
     _same(out, like, what)
     return out
 
@@ -283,7 +284,7 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, routing: Routing, wei
         _vector(weights, "weights", torch.float32, routing.tokens * routing.top_k, routing.device)
     out = _new(out, (n, H), rows, "combine backward")
     ldd = _matrix(out, "drows", cols=H, rows=n)
-    dw = torch.empty((routing.tokens, routing.top_k), dtype=torch.float32, device=rows.device)
+    dw = routing.weights.new_empty((routing.tokens, routing.top_k))
     _on(rows.device, hb.hccl_combine_backward, dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.ref, weights.data_ptr(), out.data_ptr(), ldd,
         dw.data_ptr())
     return out, dw

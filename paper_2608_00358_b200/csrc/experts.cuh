@@ -30,10 +30,59 @@ template <> struct Piece<8> { using type = uint2; };
 template <> struct Piece<4> { using type = unsigned int; };
 template <> struct Piece<2> { using type = unsigned short; };
 
+template <typename A, typename B> struct Same {
+    static constexpr bool value = false;
+};
+template <typename A> struct Same<A, A> {
+    static constexpr bool value = true;
+};
+
 template <typename T, int N> union Pack {
     typename Piece<N * sizeof(T)>::type raw;
     T v[N];
+    unsigned w[N * sizeof(T) >= 4 ? N * sizeof(T) / 4 : 1];
     __device__ __forceinline__ Pack() {}
+    // Two 16-bit elements of a word at a time, where there are two.
+    __device__ __forceinline__ void get(float (&f)[N]) const {
+        if constexpr (sizeof(T) == 2 && N >= 2) {
+#pragma unroll
+            for (int i = 0; i < N / 2; i++) two(w[i], f[2 * i], f[2 * i + 1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) f[i] = to_f32<T>(v[i]);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&f)[N]) {
+        if constexpr (sizeof(T) == 2 && N >= 2) {
+#pragma unroll
+            for (int i = 0; i < N / 2; i++) w[i] = word(f[2 * i], f[2 * i + 1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) v[i] = from_f32<T>(f[i]);
+        }
+    }
+    static __device__ __forceinline__ void two(unsigned w, float& a, float& b) {
+        if constexpr (sizeof(T) == 2) {
+            if constexpr (BF) {
+                a = __uint_as_float(w << 16);
+                b = __uint_as_float(w & 0xffff0000u);
+            } else {
+                const float2 f = __half22float2(*(const __half2*)&w);
+                a = f.x;
+                b = f.y;
+            }
+        }
+    }
+    static __device__ __forceinline__ unsigned word(float a, float b) {
+        if constexpr (BF) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+            return *(const unsigned*)&h;
+        } else {
+            const __half2 h = __floats2half2_rn(a, b);
+            return *(const unsigned*)&h;
+        }
+    }
+    static constexpr bool BF = Same<T, __nv_bfloat16>::value;
 };
 
 // ---------------------------------------------------------------- routing

@@ -1,7 +1,7 @@
 // Exchange of rows between token order and expert order: dispatch (copy), combine (weighted sum) and the gradient of
 // combine. All three walk tokens, so that a token's row is read (or written) once and each of its top_k rows in
 // expert order is touched once, without atomics: a row belongs to one choice. Memory is the bound of all three; what
-// costs is latency, so every thread asks for the pieces of eight choices before it uses the first.
+// costs is latency, so every thread asks for the pieces of several choices before it uses the first.
 #include <algorithm>
 
 #include "experts.cuh"
@@ -13,14 +13,25 @@ namespace {
 constexpr unsigned FULL = 0xffffffffu;
 constexpr int ROWS_THREADS = 256, BATCH = 8 /* choices at a time */;
 
+// A token belongs to a team of `team` warps (1, 2, 4 or 8) of a block.
+struct Team {
+    int lanes, rank;          // threads of the team, this thread's place in it
+    long long first, step;    // tokens first, first + step, ...
+    __device__ __forceinline__ explicit Team(int warps) : lanes(32 * warps), rank((int)threadIdx.x % lanes) {
+        const int per = (int)blockDim.x / lanes;
+        first = (long long)blockIdx.x * per + (int)threadIdx.x / lanes;
+        step = (long long)gridDim.x * per;
+    }
+};
+
 // A warp's look at a token's choices: lane k holds the row of choice k (-1: none) and its weight.
 struct Choices {
-    long long slot;
+    int slot;
     float w;
     __device__ __forceinline__ Choices(const RowsParams& p, long long t) : slot(-1), w(0.f) {
         const int k = threadIdx.x % 32;
         if (k < p.K) {
-            const long long s = p.slots[t * p.K + k];
+            const int s = p.slots[t * p.K + k];
             if (s >= 0 && s < p.n_rows) {
                 slot = s;
                 w = p.weights ? p.weights[t * p.K + k] : 1.f;
@@ -41,20 +52,21 @@ template <typename T, int N> __device__ __forceinline__ void clear_tail(const Ro
     }
 }
 
-template <typename T, int N> __global__ void __launch_bounds__(ROWS_THREADS) hccl_rows_dispatch(const __grid_constant__ RowsParams p) {
+template <typename T, int N> __global__ void __launch_bounds__(ROWS_THREADS) hccl_rows_dispatch(const __grid_constant__ RowsParams p, int team) {
     using P = typename Piece<N * sizeof(T)>::type;
-    const long long cols = p.H / N;
-    for (long long t = blockIdx.x; t < p.tokens; t += gridDim.x) {
+    const int cols = (int)(p.H / N);
+    const Team m(team);
+    for (long long t = m.first; t < p.tokens; t += m.step) {
         const Choices mine(p, t);
         const P* x = (const P*)((const T*)p.x + t * p.ldx);
         for (int k0 = 0; k0 < p.K; k0 += BATCH) {
             P* to[BATCH];
 #pragma unroll
             for (int j = 0; j < BATCH; j++) {
-                const long long s = k0 + j < p.K ? __shfl_sync(FULL, mine.slot, k0 + j) : -1;
+                const int s = k0 + j < p.K ? __shfl_sync(FULL, mine.slot, k0 + j) : -1;
                 to[j] = s >= 0 ? (P*)((T*)p.rows_out + s * p.ldro) : nullptr;
             }
-            for (long long c = threadIdx.x; c < cols; c += blockDim.x) {
+            for (int c = m.rank; c < cols; c += m.lanes) {
                 const P v = x[c];
 #pragma unroll
                 for (int j = 0; j < BATCH; j++)
@@ -97,7 +109,7 @@ template <int PIECE> __global__ void __launch_bounds__(32 * BULK_WARPS) hccl_row
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // what arrived, before the copy unit reads it
         __syncwarp();
         if (mine.slot >= 0)
-            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"((char*)p.rows_out + mine.slot * row_step + i % pieces * PIECE),
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"((char*)p.rows_out + (long long)mine.slot * row_step + i % pieces * PIECE),
                          "r"((unsigned)__cvta_generic_to_shared(buf[warp][b])), "r"(size_of(i))
                          : "memory");
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
@@ -109,103 +121,119 @@ template <int PIECE> __global__ void __launch_bounds__(32 * BULK_WARPS) hccl_row
         for (long long c = threadIdx.x * 16ll; c < bytes; c += 32 * BULK_WARPS * 16) *(uint4*)((char*)p.rows_out + r * row_step + c) = make_uint4(0, 0, 0, 0);
 }
 
-// Block (x, y): columns [x * span, ...) of tokens y, y + gridDim.y, ...
-template <typename T, int N> __global__ void __launch_bounds__(ROWS_THREADS) hccl_rows_combine(const __grid_constant__ RowsParams p, int span) {
+// KB: choices at a time, the least of 2, 4 and 8 that is not below K, or 8. blockIdx.y: which span of the columns.
+template <typename T, int N, int KB> __global__ void __launch_bounds__(ROWS_THREADS) hccl_rows_combine(const __grid_constant__ RowsParams p, int team, int span) {
     using P = typename Piece<N * sizeof(T)>::type;
-    const long long cols = p.H / N, c0 = (long long)blockIdx.x * span, c1 = min(c0 + span, cols);
-    for (long long t = blockIdx.y; t < p.tokens; t += gridDim.y) {
+    const int cols = (int)(p.H / N), c0 = (int)blockIdx.y * span, c1 = min(c0 + span, cols);
+    const Team m(team);
+    for (long long t = m.first; t < p.tokens; t += m.step) {
         const Choices mine(p, t);
         P* y = (P*)((T*)p.y + t * p.ldy);
-        // (a thread's first column decides how often the warp goes round, so that all lanes take part in the shuffles)
-        for (long long base = c0; base < c1; base += blockDim.x) {
-            const long long c = base + threadIdx.x;
+        const P* from[KB];
+        float w[KB];
+        const auto take = [&](int k0) {
+#pragma unroll
+            for (int j = 0; j < KB; j++) {
+                const int s = k0 + j < p.K ? __shfl_sync(FULL, mine.slot, k0 + j) : -1;
+                w[j] = __shfl_sync(FULL, mine.w, (k0 + j) & 31);
+                from[j] = s >= 0 ? (const P*)((const T*)p.rows + s * p.ldr) : nullptr;
+            }
+        };
+        take(0);
+        // (the team's first column decides how often a warp goes round, so that all lanes take part in the shuffles)
+        for (int base = c0; base < c1; base += m.lanes) {
+            const int c = base + m.rank;
             float acc[N];
 #pragma unroll
             for (int i = 0; i < N; i++) acc[i] = 0.f;
-            for (int k0 = 0; k0 < p.K; k0 += BATCH) {
-                Pack<T, N> v[BATCH];
-                float w[BATCH];
-                bool some[BATCH];
+            for (int k0 = 0; k0 < p.K; k0 += KB) {
+                if (p.K > KB) take(k0);
+                if (c < c1) {
+                    Pack<T, N> v[KB];
 #pragma unroll
-                for (int j = 0; j < BATCH; j++) {
-                    const long long s = k0 + j < p.K ? __shfl_sync(FULL, mine.slot, k0 + j) : -1;
-                    w[j] = __shfl_sync(FULL, mine.w, (k0 + j) & 31);
-                    some[j] = s >= 0 && c < c1;
-                    if (some[j]) v[j].raw = ((const P*)((const T*)p.rows + s * p.ldr))[c];
+                    for (int j = 0; j < KB; j++)
+                        if (from[j]) v[j].raw = from[j][c];
+#pragma unroll
+                    for (int j = 0; j < KB; j++)
+                        if (from[j]) {
+                            float f[N];
+                            v[j].get(f);
+#pragma unroll
+                            for (int i = 0; i < N; i++) acc[i] = fmaf(w[j], f[i], acc[i]);
+                        }
                 }
-#pragma unroll
-                for (int j = 0; j < BATCH; j++)
-                    if (some[j]) {
-#pragma unroll
-                        for (int i = 0; i < N; i++) acc[i] = fmaf(w[j], to_f32<T>(v[j].v[i]), acc[i]);
-                    }
             }
             if (c < c1) {
                 Pack<T, N> o;
-#pragma unroll
-                for (int i = 0; i < N; i++) o.v[i] = from_f32<T>(acc[i]);
+                o.set(acc);
                 y[c] = o.raw;
             }
         }
     }
 }
 
-template <typename T, int N> __global__ void __launch_bounds__(ROWS_THREADS) hccl_rows_combine_grad(const __grid_constant__ RowsParams p) {
+// KB as above, at most 4: the gradient holds more for each choice.
+template <typename T, int N, int KB> __global__ void __launch_bounds__(ROWS_THREADS) hccl_rows_combine_grad(const __grid_constant__ RowsParams p, int team) {
     using P = typename Piece<N * sizeof(T)>::type;
     __shared__ float part[2][ROWS_THREADS / 32][32];
-    const long long cols = p.H / N;
-    const int warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int cols = (int)(p.H / N), warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const Team m(team);
     int turn = 0;
-    for (long long t = blockIdx.x; t < p.tokens; t += gridDim.x, turn ^= 1) {
+    for (long long t = m.first; t < p.tokens; t += m.step, turn ^= 1) {
         const Choices mine(p, t);
         const P* dy = (const P*)((const T*)p.x + t * p.ldx);
         float sums = 0.f;  // lane k: this warp's part of choice k
-        for (int k0 = 0; k0 < p.K; k0 += BATCH) {
-            const P* from[BATCH];
-            P* to[BATCH];
-            float w[BATCH], dot[BATCH];
+        for (int k0 = 0; k0 < p.K; k0 += KB) {
+            const P* from[KB];
+            P* to[KB];
+            float w[KB], dot[KB];
 #pragma unroll
-            for (int j = 0; j < BATCH; j++) {
-                const long long s = k0 + j < p.K ? __shfl_sync(FULL, mine.slot, k0 + j) : -1;
+            for (int j = 0; j < KB; j++) {
+                const int s = k0 + j < p.K ? __shfl_sync(FULL, mine.slot, k0 + j) : -1;
                 w[j] = __shfl_sync(FULL, mine.w, (k0 + j) & 31);
                 from[j] = s >= 0 ? (const P*)((const T*)p.rows + s * p.ldr) : nullptr;
                 to[j] = s >= 0 ? (P*)((T*)p.rows_out + s * p.ldro) : nullptr;
                 dot[j] = 0.f;
             }
-            for (long long c = threadIdx.x; c < cols; c += blockDim.x) {
-                Pack<T, N> g, v[BATCH];
+            for (int c = m.rank; c < cols; c += m.lanes) {
+                Pack<T, N> g, v[KB];
                 g.raw = dy[c];
 #pragma unroll
-                for (int j = 0; j < BATCH; j++)
+                for (int j = 0; j < KB; j++)
                     if (from[j]) v[j].raw = from[j][c];
+                float d[N];
+                g.get(d);
 #pragma unroll
-                for (int j = 0; j < BATCH; j++)
+                for (int j = 0; j < KB; j++)
                     if (from[j]) {
                         Pack<T, N> o;
+                        float f[N];
+                        v[j].get(f);
 #pragma unroll
                         for (int i = 0; i < N; i++) {
-                            dot[j] = fmaf(to_f32<T>(g.v[i]), to_f32<T>(v[j].v[i]), dot[j]);
-                            o.v[i] = from_f32<T>(w[j] * to_f32<T>(g.v[i]));
+                            dot[j] = fmaf(d[i], f[i], dot[j]);
+                            f[i] = w[j] * d[i];
                         }
+                        o.set(f);
                         to[j][c] = o.raw;
                     }
             }
 #pragma unroll
-            for (int j = 0; j < BATCH; j++) {
+            for (int j = 0; j < KB; j++) {
 #pragma unroll
                 for (int o = 16; o; o >>= 1) dot[j] += __shfl_xor_sync(FULL, dot[j], o);
                 if (lane == k0 + j) sums = dot[j];
             }
         }
-        if (warps > 1) {  // two places in turn: a warp may be a token ahead of the one that adds up, not two
+        if (team > 1) {  // two places in turn: a warp may be a token ahead of the one that adds up, not two
             part[turn][warp][lane] = sums;
-            __syncthreads();
-            if (warp == 0) {
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / team), "r"(m.lanes) : "memory");
+            if (m.rank < 32) {
                 sums = 0.f;
-                for (int i = 0; i < warps; i++) sums += part[turn][i][lane];
+                for (int i = 0; i < team; i++) sums += part[turn][warp + i][lane];
             }
         }
-        if (warp == 0 && lane < p.K) p.dweights[t * p.K + lane] = sums;
+        if (m.rank < p.K) p.dweights[t * p.K + m.rank] = sums;
     }
     clear_tail<T, N>(p, blockIdx.x, gridDim.x);
 }
@@ -219,25 +247,36 @@ int piece_bytes(int es, long long H, const void* const* ptr, const long long* ld
 
 enum { DISPATCH, COMBINE, COMBINE_GRAD };
 
+// Warps for each token, by measurement (8192 x 4096 of 8, 4099 x 2056 of 6, 2000 x 1024 of 4, all bf16): the gradient 189, 50 and 12 us with two, 200, 55 and 11
+// with one, 206, 60 and 15 with four; combine 109, 30 and 5 us with one, 112, 37 and 5 with four. With few tokens as many as make 16 warps for each SM.
+int team_of(int what, long long tokens, long long cols) {
+    int w = what == COMBINE_GRAD && cols >= 64 ? 2 : 1;
+    while (w < ROWS_THREADS / 32 && tokens * w < SMS * 16 && cols > 32 * w) w *= 2;
+    return w;
+}
+
 template <typename T, int N> cudaError_t rows_launch(int what, const RowsParams& p, cudaStream_t s) {
     const long long cols = p.H / N;
-    int threads = 32;
+    if (cols > 1 << 30) return cudaErrorInvalidValue;
+    const int team = team_of(what, p.tokens, cols), per = ROWS_THREADS / 32 / team;
+    const long long whole = (p.tokens + per - 1) / per;  // a block for each `per` tokens: the hardware hands out the next one where one has ended
+    const unsigned blocks = (unsigned)std::min<long long>(std::max<long long>(whole, what == COMBINE ? 1 : SMS), 1 << 30);
     if (what == COMBINE) {
-        if (p.tokens == 0) return cudaSuccess;
-        while (threads < ROWS_THREADS && threads < cols) threads *= 2;
-        // a block takes two rounds of columns where tokens fill the SMs, one where they do not
-        const int span = threads * (p.tokens >= SMS * 4 ? 2 : 1);
-        const unsigned across = (unsigned)std::max<long long>(1, (cols + span - 1) / span);
-        hccl_rows_combine<T, N><<<dim3(across, (unsigned)std::min<long long>(p.tokens, 65535)), threads, 0, s>>>(p, span);
+        if (p.tokens == 0 || p.H == 0) return cudaSuccess;
+        // few tokens: a row's columns go to several blocks, one round for each
+        const long long rounds = (cols + 32 * team - 1) / (32 * team);
+        const unsigned across = (unsigned)std::min<long long>(rounds, std::max<long long>(1, SMS * 4 / std::max<long long>(whole, 1)));
+        const int span = (int)((rounds + across - 1) / across) * 32 * team;
+        const dim3 grid(blocks, across);
+        if (p.K <= 2) hccl_rows_combine<T, N, 2><<<grid, ROWS_THREADS, 0, s>>>(p, team, span);
+        else if (p.K <= 4) hccl_rows_combine<T, N, 4><<<grid, ROWS_THREADS, 0, s>>>(p, team, span);
+        else hccl_rows_combine<T, N, 8><<<grid, ROWS_THREADS, 0, s>>>(p, team, span);
         return cudaGetLastError();
     }
-    const long long work = std::max(p.tokens, p.n_rows);
-    if (work == 0) return cudaSuccess;
-    const int a_thread = what == COMBINE_GRAD ? 4 : 2;  // pieces of a thread, about
-    while (threads < ROWS_THREADS && threads * a_thread < cols) threads *= 2;
-    const int blocks = (int)std::min<long long>(work, (long long)SMS * (2048 / threads));
-    if (what == DISPATCH) hccl_rows_dispatch<T, N><<<blocks, threads, 0, s>>>(p);
-    else hccl_rows_combine_grad<T, N><<<blocks, threads, 0, s>>>(p);
+    if (p.tokens == 0 && p.n_rows == 0) return cudaSuccess;
+    if (what == DISPATCH) hccl_rows_dispatch<T, N><<<blocks, ROWS_THREADS, 0, s>>>(p, team);
+    else if (p.K <= 2) hccl_rows_combine_grad<T, N, 2><<<blocks, ROWS_THREADS, 0, s>>>(p, team);
+    else hccl_rows_combine_grad<T, N, 4><<<blocks, ROWS_THREADS, 0, s>>>(p, team);
     return cudaGetLastError();
 }
 
@@ -261,9 +300,14 @@ cudaError_t launch_dispatch(int dt, const RowsParams& p, cudaStream_t s) {
     const void* ptr[] = {p.x, p.rows_out};
     const long long ld[] = {p.ldx, p.ldro};
     const int piece = piece_bytes(es, p.H, ptr, ld, 2);
-    if (piece == 16 && p.tokens && p.H) {
+    // (a copy through shared memory has its own latency: below some 4 MB of rows, plain stores; 50 x 2048 to 8 places 4.8 us by bulk copies)
+    if (piece == 16 && p.tokens * p.K * p.H * es >= 4 << 20) {
         const long long bytes = p.H * es, items = p.tokens * ((bytes + 4095) / 4096);
-        const int blocks = (int)std::min<long long>((items + BULK_WARPS - 1) / BULK_WARPS, SMS * 6);
+        // Warps: 32 KB of buffers on each SM, as many bytes of rows as it takes (8192 x 4096 to 8 places: 102 us with one block on each SM, 108-111
+        // with two to six; 131 with half the bytes), and no more warps than bring every one to the same number of pieces.
+        const long long per_sm = std::min<long long>(8, std::max<long long>(1, 4096 / bytes)), most = std::min<long long>(items, SMS * per_sm * BULK_WARPS);
+        const long long rounds = (items + most - 1) / most, warps = (items + rounds - 1) / rounds;
+        const int blocks = (int)((warps + BULK_WARPS - 1) / BULK_WARPS);
         hccl_rows_dispatch_bulk<4096><<<blocks, 32 * BULK_WARPS, 0, s>>>(p, bytes, p.ldx * es, p.ldro * es);
         return cudaGetLastError();
     }

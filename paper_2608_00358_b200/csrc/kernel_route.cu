@@ -24,20 +24,39 @@ constexpr int NOT_A_NUMBER = 0x7fc00000;
 __host__ __device__ constexpr int round_up(int n, int m) { return (n + m - 1) / m * m; }
 // floats from one token's keys to the next: 8 banks on, so that lanes of four tokens that walk their groups do not collide
 __host__ __device__ __forceinline__ int key_stride(int E) { return round_up(E, 32) + 8; }
+// Lines of threads that add up counts in the layout, at most 32.
+__host__ __device__ __forceinline__ int layout_lines(int E) {
+    const int n = LAYOUT_THREADS / (round_up(E, 16) / 16);
+    return n < 32 ? n : 32;
+}
 __host__ __device__ __forceinline__ int token_floats(const RouteParams& p) { return key_stride(p.E) + (p.groups > 1 ? 2 * round_up(p.groups, 4) : 0) + round_up(p.K, 4); }
 
 template <int L> __device__ __forceinline__ float lanes_max(float v) {
-#pragma unroll
-    for (int o = L / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
-    return v;
-}
-template <int L> __device__ __forceinline__ int lanes_min(int v) {
     if constexpr (L == 32) {
-        return __reduce_min_sync(FULL, v);
+        float r;
+        asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+        return r;
     } else {
 #pragma unroll
-        for (int o = L / 2; o; o >>= 1) v = min(v, __shfl_xor_sync(FULL, v, o));
+        for (int o = L / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
         return v;
+    }
+}
+// The largest value over the lanes, and of the quads that have it the lowest.
+template <int L> __device__ __forceinline__ void lanes_best(float& v, int& quad) {
+    if constexpr (L == 32) {
+        const float m = lanes_max<32>(v);
+        quad = __reduce_min_sync(FULL, v == m ? quad : 0x7fffffff);
+        v = m;
+    } else {
+#pragma unroll
+        for (int o = L / 2; o; o >>= 1) {
+            const float u = __shfl_xor_sync(FULL, v, o);
+            const int q = __shfl_xor_sync(FULL, quad, o);
+            const bool take = (u > v) | ((u == v) & (q < quad));  // no branch: the chain of these is the latency of a round
+            v = take ? u : v;
+            quad = take ? q : quad;
+        }
     }
 }
 template <int L> __device__ __forceinline__ float lanes_sum(float v) {
@@ -50,25 +69,17 @@ template <int L> __device__ __forceinline__ bool lanes_any(bool v) {
     return (b >> (threadIdx.x % 32 / L * L)) & (L == 32 ? FULL : (1u << (L % 32)) - 1);
 }
 
-// Experts 4q .. 4q + 3 of a row; -inf from E on.
-template <typename T> __device__ __forceinline__ void load_quad(const T* row, int q, int E, bool vec, float (&x)[4]) {
-    if (vec && 4 * q + 4 <= E) {
-        Pack<T, 4> v;
-        v.raw = *(const typename Piece<4 * sizeof(T)>::type*)(row + 4 * q);
-#pragma unroll
-        for (int j = 0; j < 4; j++) x[j] = to_f32<T>(v.v[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; j++) x[j] = 4 * q + j < E ? to_f32<T>(row[4 * q + j]) : -INFINITY;
-    }
+__device__ __forceinline__ float quick_sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 
-__device__ __forceinline__ float quick_sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
-
-// One token for each L lanes. keys: this token's shared memory (token_floats). sbias: the bias in shared memory, up to a multiple of 4 experts.
-// Writes ids and weights, counts the chosen in hist.
+// One token for each L lanes. keys: this token's shared memory (token_floats). sbias: the bias in shared memory, up to a multiple of 4 experts; odd: some of
+// it is infinite or NaN. Writes ids and weights (ids to `kept` too, shared, unless null), counts the chosen in hist.
 template <typename T, int Q, int L>
-__device__ __forceinline__ void choose_token(const RouteParams& p, long long t, bool in, float* keys, const float* sbias, int* hist) {
+__device__ __forceinline__ void choose_token(const RouteParams& p, long long t, bool in, float* keys, const float* sbias, bool odd, int* hist, int* kept) {
     const int lane = threadIdx.x % 32, l = lane % L;
     const int stride = key_stride(p.E), gpad = p.groups > 1 ? round_up(p.groups, 4) : 0;
     float* gscore = keys + stride;
@@ -76,94 +87,149 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
     int* chosen = (int*)(keys + stride + 2 * gpad);
     const bool live = in && (!p.mask || p.mask[t]);
     const T* row = (const T*)p.logits + (in ? t : 0) * p.ld;
+    const auto bias_quad = [&](int i, float (&b)[4]) {
+        const float4 b4 = *(const float4*)(sbias + (i * L + l) * 4);
+        b[0] = b4.x, b[1] = b4.y, b[2] = b4.z, b[3] = b4.w;
+    };
 
     float x[Q][4];
+    if (p.vec) {  // whole quads, all asked for before the first is looked at
+        Pack<T, 4> raw[Q];
 #pragma unroll
-    for (int i = 0; i < Q; i++) {
-        if (live) load_quad<T>(row, i * L + l, p.E, p.vec, x[i]);
-        else x[i][0] = x[i][1] = x[i][2] = x[i][3] = -INFINITY;
+        for (int i = 0; i < Q; i++) {
+            raw[i].raw = {};
+            if (live && (i * L + l) * 4 < p.E) raw[i].raw = ((const typename Piece<4 * sizeof(T)>::type*)row)[i * L + l];
+        }
+#pragma unroll
+        for (int i = 0; i < Q; i++) {
+            raw[i].get(x[i]);
+            const float off = live && (i * L + l) * 4 < p.E ? 0.f : -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[i][j] += off;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < Q; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int e = (i * L + l) * 4 + j;
+                x[i][j] = -INFINITY;
+                if (live && e < p.E) x[i][j] = to_f32<T>(row[e]);
+            }
     }
     bool bad = false;
-    float m = -INFINITY;
+    if (odd) {
 #pragma unroll
-    for (int i = 0; i < Q; i++) {
-        if (p.bias && (i * L + l) * 4 < p.E) {
-            const float4 b4 = *(const float4*)(sbias + (i * L + l) * 4);
-            const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+        for (int i = 0; i < Q; i++) {
+            if ((i * L + l) * 4 >= p.E) continue;
+            float b[4];
+            bias_quad(i, b);
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 if (b[j] == -INFINITY) x[i][j] = -INFINITY;  // the expert is off, whatever its logit
                 bad |= x[i][j] != -INFINITY && !(b[j] < INFINITY);
             }
         }
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            bad |= isnan(x[i][j]);
-            m = fmaxf(m, x[i][j]);
-        }
     }
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < Q; i++) m = max_or_nan(m, max_or_nan(max_or_nan(x[i][0], x[i][1]), max_or_nan(x[i][2], x[i][3])));
+    bad |= isnan(m);
     m = lanes_max<L>(m);
     bad |= !p.sigmoid && m == INFINITY;
     bad = lanes_any<L>(bad);
     float total = 1.f;
-    if (p.sigmoid || p.bias || !p.renorm) {
-        const float base = m == -INFINITY ? 0.f : m;
-        float sum = 0.f;
+    if (p.sigmoid) {
 #pragma unroll
         for (int i = 0; i < Q; i++) {
             float b[4] = {0.f, 0.f, 0.f, 0.f};
-            if (p.sigmoid) {
-                if (p.bias && (i * L + l) * 4 < p.E) {
-                    const float4 b4 = *(const float4*)(sbias + (i * L + l) * 4);
-                    b[0] = b4.x, b[1] = b4.y, b[2] = b4.z, b[3] = b4.w;
-                }
+            if (p.bias && (i * L + l) * 4 < p.E) bias_quad(i, b);
 #pragma unroll
-                for (int j = 0; j < 4; j++)
-                    if (x[i][j] != -INFINITY) x[i][j] = quick_sigmoid(x[i][j]) + b[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; j++) sum += __expf(x[i][j] - base);
+            for (int j = 0; j < 4; j++) {
+                const float off = x[i][j] == -INFINITY ? -INFINITY : b[j];  // (not around the sigmoid: that would be a branch for each)
+                x[i][j] = quick_sigmoid(x[i][j]) + off;
             }
         }
-        if (!p.sigmoid) {
-            total = lanes_sum<L>(sum);
-            if (p.bias) {
-                const float r = __fdividef(1.f, total);
+    } else if (p.bias || !p.renorm) {
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < Q; i++)
-                    if ((i * L + l) * 4 < p.E) {
-                        const float4 b4 = *(const float4*)(sbias + (i * L + l) * 4);
-                        const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+        for (int i = 0; i < Q; i++)
 #pragma unroll
-                        for (int j = 0; j < 4; j++)
-                            if (x[i][j] != -INFINITY) x[i][j] = __expf(x[i][j] - base) * r + b[j];
+            for (int j = 0; j < 4; j++) sum += __expf(x[i][j] - base);
+        total = lanes_sum<L>(sum);
+        if (p.bias) {
+            const float r = __fdividef(1.f, total);
+#pragma unroll
+            for (int i = 0; i < Q; i++)
+                if ((i * L + l) * 4 < p.E) {
+                    float b[4];
+                    bias_quad(i, b);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const float off = x[i][j] == -INFINITY ? -INFINITY : b[j];
+                        x[i][j] = __expf(x[i][j] - base) * r + off;
                     }
-            }
+                }
         }
     }
     // x is the key now
 #pragma unroll
     for (int i = 0; i < Q; i++)
         if ((i * L + l) * 4 < p.E) *(float4*)(keys + (i * L + l) * 4) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+    float top[Q];
+#pragma unroll
+    for (int i = 0; i < Q; i++) top[i] = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
     if (p.groups > 1) {
         __syncwarp();
         for (int g = l; g < p.groups; g += L) {
-            float k1 = -INFINITY, k2 = -INFINITY;
-            int at = g % p.per_group;  // lanes start at different places of their groups: different banks
-            const float* k = keys + g * p.per_group;
-            for (int i = 0; i < p.per_group; i++) {
-                const float v = k[at];
+            float k1 = -INFINITY, k2 = -INFINITY, o1 = -INFINITY, o2 = -INFINITY;  // the two largest, of two halves: two chains of latencies side by side
+            const auto seen = [&](float v) {
                 k2 = fmaxf(k2, fminf(k1, v));
                 k1 = fmaxf(k1, v);
-                at = at + 1 == p.per_group ? 0 : at + 1;
+            };
+            const auto seen_too = [&](float v) {
+                o2 = fmaxf(o2, fminf(o1, v));
+                o1 = fmaxf(o1, v);
+            };
+            const float* k = keys + g * p.per_group;
+            // lanes start at different places of their groups: different banks
+            if (p.per4) {
+                const int quads = p.per_group / 4;
+                int at = g % quads;
+                for (int i = 0; i < quads; i += 4) {
+                    float4 v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; u++) {
+                        v[u] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                        if (i + u < quads) v[u] = *(const float4*)(k + 4 * at);
+                        at = at + 1 == quads ? 0 : at + 1;
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; u++) seen(v[u].x), seen_too(v[u].z), seen(v[u].y), seen_too(v[u].w);
+                }
+            } else {
+                int at = g % p.per_group;
+                for (int i = 0; i < p.per_group; i++) {
+                    seen(k[at]);
+                    at = at + 1 == p.per_group ? 0 : at + 1;
+                }
             }
+            seen(o1), seen(o2);
             gscore[g] = (p.group_best == 2 && k2 != -INFINITY) ? k1 + k2 : k1;
         }
+        for (int g = p.groups + l; g < gpad; g += L) gscore[g] = -INFINITY;
         __syncwarp();
         for (int g = l; g < p.groups; g += L) {
             const float mine = gscore[g];
             int above = 0;
-            for (int o = 0; o < p.groups; o++) above += gscore[o] > mine || (gscore[o] == mine && o < g);
+            for (int o = 0; o < gpad; o += 4) {
+                const float4 v = *(const float4*)(gscore + o);
+                above += (v.x > mine) | ((v.x == mine) & (o < g));
+                above += (v.y > mine) | ((v.y == mine) & (o + 1 < g));
+                above += (v.z > mine) | ((v.z == mine) & (o + 2 < g));
+                above += (v.w > mine) | ((v.w == mine) & (o + 3 < g));
+            }
             gkeep[g] = above < p.top_groups;
         }
         __syncwarp();
@@ -172,44 +238,46 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
             const int e = (i * L + l) * 4;
             if (e >= p.E) continue;
             if (p.per4) {
-                if (!gkeep[(e * p.magic) >> 20]) x[i][0] = x[i][1] = x[i][2] = x[i][3] = -INFINITY;
+                if (!gkeep[(e * p.magic) >> 20]) top[i] = -INFINITY;  // its keys are not looked at again
             } else {
-#pragma unroll
-                for (int j = 0; j < 4; j++)
-                    if (e + j < p.E && !gkeep[((e + j) * p.magic) >> 20]) x[i][j] = -INFINITY;
-                *(float4*)(keys + e) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+                float4 v = *(const float4*)(keys + e);
+                if (!gkeep[(e * p.magic) >> 20]) v.x = -INFINITY;
+                if (e + 1 < p.E && !gkeep[((e + 1) * p.magic) >> 20]) v.y = -INFINITY;
+                if (e + 2 < p.E && !gkeep[((e + 2) * p.magic) >> 20]) v.z = -INFINITY;
+                if (e + 3 < p.E && !gkeep[((e + 3) * p.magic) >> 20]) v.w = -INFINITY;
+                *(float4*)(keys + e) = v;
+                top[i] = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
             }
         }
     }
-    float top[Q];
-#pragma unroll
-    for (int i = 0; i < Q; i++) top[i] = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
     __syncwarp();
     for (int k = 0; k < p.K; k++) {
-        float best = top[0];
-        int at = 0;
+        float tree[Q];  // the first of the largest, pair by pair
+        int of[Q];
 #pragma unroll
-        for (int i = 1; i < Q; i++)
-            if (top[i] > best) best = top[i], at = i;
-        const float win = lanes_max<L>(best);
-        const int quad = lanes_min<L>(best == win ? at * L + l : 0x7fffffff);
-        if (win == -INFINITY || bad) {
-            if (l == 0) chosen[k] = -1;
-        } else if (quad == at * L + l && best == win) {
-            float* c = keys + quad * 4;
-            float4 v = *(float4*)c;
-            const int j = v.x == win ? 0 : v.y == win ? 1 : v.z == win ? 2 : 3;
+        for (int i = 0; i < Q; i++) tree[i] = top[i], of[i] = i;
+#pragma unroll
+        for (int step = 1; step < Q; step *= 2)
+#pragma unroll
+            for (int i = 0; i + step < Q; i += 2 * step)
+                if (tree[i + step] > tree[i]) tree[i] = tree[i + step], of[i] = of[i + step];
+        const int at = of[0], mine = at * L + l;
+        // Each lane looks at its own best quad while the lanes find out whose it is.
+        float* c = keys + min(mine * 4, stride - 4);
+        const float4 v = *(const float4*)c;
+        float win = tree[0];
+        const int j = v.x == win ? 0 : v.y == win ? 1 : v.z == win ? 2 : 3;
+        const float next = fmaxf(fmaxf(j == 0 ? -INFINITY : v.x, j == 1 ? -INFINITY : v.y), fmaxf(j == 2 ? -INFINITY : v.z, j == 3 ? -INFINITY : v.w));
+        int quad = mine;
+        lanes_best<L>(win, quad);
+        const bool none = win == -INFINITY || bad, owner = quad == mine && !none;
+        if (owner) {
             chosen[k] = quad * 4 + j;
             c[j] = -INFINITY;
-            if (j == 0) v.x = -INFINITY;
-            if (j == 1) v.y = -INFINITY;
-            if (j == 2) v.z = -INFINITY;
-            if (j == 3) v.w = -INFINITY;
-            const float next = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
-#pragma unroll
-            for (int i = 0; i < Q; i++)
-                if (at == i) top[i] = next;
         }
+        if (none && l == 0) chosen[k] = -1;
+#pragma unroll
+        for (int i = 0; i < Q; i++) top[i] = owner && at == i ? next : top[i];
     }
     __syncwarp();
     constexpr int R = 32 / L;  // at most 32 choices over L lanes
@@ -219,11 +287,10 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
     for (int r = 0; r < R; r++) {
         const int k = r * L + l;
         id[r] = k < p.K ? chosen[k] : -1;
-        s[r] = 0.f;
-        if (id[r] >= 0) {
-            const float v = to_f32<T>(row[id[r]]);
-            s[r] = p.sigmoid ? 1.f / (1.f + expf(-v)) : expf(v - m);  // softmax: the common divisor drops out of renormalised weights
-        }
+        float v = p.sigmoid ? -INFINITY : m;
+        if (id[r] >= 0) v = to_f32<T>(row[id[r]]);
+        s[r] = p.sigmoid ? 1.f / (1.f + expf(-v)) : expf(v - m);  // softmax: the common divisor drops out of renormalised weights
+        s[r] = id[r] >= 0 ? s[r] : 0.f;
         sum += s[r];
         if (r * L + L >= p.K) {
 #pragma unroll
@@ -239,6 +306,7 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
             const int k = r * L + l;
             if (k >= p.K) break;
             p.ids[t * p.K + k] = id[r];
+            if (kept) kept[t * p.K + k] = id[r];
             p.weights[t * p.K + k] = (live && bad) ? __int_as_float(NOT_A_NUMBER) : (id[r] >= 0 && div > 0.f) ? s[r] / div * p.scale : 0.f;
             if (id[r] >= 0) atomicAdd(&hist[id[r]], 1);
         }
@@ -246,23 +314,34 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
     __syncwarp();
 }
 
-// Rows of the choices [first, first + n). base[e] (shared) = first row of expert e for them; rows follow in the order of the choices.
+// Rows of the choices [first, first + n), whose experts are ids[0 .. n). base[e] (shared) = first row of expert e for them; rows follow in the order of the choices.
 // Each warp takes a run of them; a first walk counts by expert, a second hands out the rows with match_any, so that the
 // order does not depend on which warp is faster. cnt: shared, [warps][E].
-__device__ __forceinline__ void layout_choices(const RouteParams& p, long long first, int n, const int* base, int* cnt, int threads) {
+__device__ __forceinline__ void layout_choices(const RouteParams& p, const int* ids, long long first, int n, const int* base, int* cnt, int threads) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = threads / 32;
     const int per = round_up((n + warps - 1) / warps, 32);
     const int lo = min(warp * per, n), hi = min(lo + per, n);
     int* mine = cnt + warp * p.E;
     for (int e = lane; e < p.E; e += 32) mine[e] = 0;
+    constexpr int HELD = 4;  // a run's first 128 choices stay in registers between the walks
+    int id[HELD];
+#pragma unroll
+    for (int u = 0; u < HELD; u++) {
+        const int i = lo + u * 32 + lane;
+        id[u] = i < hi ? ids[i] : -1;
+    }
     __syncwarp();
-    for (int i = lo + lane; i < hi; i += 32) {
-        const int e = p.ids[first + i];
+#pragma unroll
+    for (int u = 0; u < HELD; u++)
+        if (id[u] >= 0) atomicAdd(&mine[id[u]], 1);
+    for (int i = lo + HELD * 32 + lane; i < hi; i += 32) {
+        const int e = ids[i];
         if (e >= 0) atomicAdd(&mine[e], 1);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < p.E; e += threads) {  // counts become first rows
         int at = base[e];
+#pragma unroll 4
         for (int w = 0; w < warps; w++) {
             const int c = cnt[w * p.E + e];
             cnt[w * p.E + e] = at;
@@ -270,9 +349,7 @@ __device__ __forceinline__ void layout_choices(const RouteParams& p, long long f
         }
     }
     __syncthreads();
-    for (int b = lo; b < hi; b += 32) {
-        const int i = b + lane;
-        const int e = i < hi ? p.ids[first + i] : -1;
+    const auto place = [&](int i, int e) {
         const unsigned same = __match_any_sync(FULL, e);
         int row = -1;
         if (e >= 0) row = mine[e] + __popc(same & ((1u << lane) - 1));
@@ -283,71 +360,86 @@ __device__ __forceinline__ void layout_choices(const RouteParams& p, long long f
             p.slots[first + i] = row;
             if (row >= 0) p.source[row] = (int)(first + i);
         }
-    }
+    };
+#pragma unroll
+    for (int u = 0; u < HELD; u++)
+        if (lo + u * 32 < hi) place(lo + u * 32 + lane, id[u]);
+    for (int b = lo + HELD * 32; b < hi; b += 32) place(b + lane, b + lane < hi ? ids[b + lane] : -1);
 }
 
-// Offsets of all experts from their totals tot[E] (shared); each expert's first row is added to base[e]. Returns the number of rows.
-__device__ __forceinline__ int offsets_of(const RouteParams& p, const int* tot, int* base, int* rows, bool write) {
-    if (threadIdx.x < 32) {
-        int run = 0;
-        for (int b = 0; b < p.E; b += 32) {
-            const int e = b + (int)threadIdx.x;
-            const int c = e < p.E ? tot[e] : 0;
-            int inc = c;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(FULL, inc, o);
-                if ((int)threadIdx.x >= o) inc += v;
-            }
-            if (e < p.E) {
-                const int start = run + inc - c;
-                if (write) {
-                    p.offsets[e] = start;
-                    p.counts[e] = c;
-                }
-                base[e] += start;
-            }
-            run += __shfl_sync(FULL, inc, 31);
-        }
-        if (threadIdx.x == 0) {
-            *rows = run;
-            if (write) p.offsets[p.E] = run;
-        }
+// Offsets of all experts from their totals tot[E] (shared); each expert's first row is added to base[e]. Returns the number of rows. A warp scans 32 experts,
+// the warps' sums are added up by each; scratch: shared, 33 ints.
+__device__ __forceinline__ int offsets_of(const RouteParams& p, const int* tot, int* base, int* scratch, bool write, int threads) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = threads / 32, parts = (p.E + 31) / 32;  // at most 32 parts
+    for (int part = warp; part < parts; part += warps) {
+        const int e = part * 32 + lane;
+        const int sum = __reduce_add_sync(FULL, e < p.E ? tot[e] : 0);
+        if (lane == 0) scratch[part] = sum;
     }
     __syncthreads();
-    return *rows;
+    int used = 0;
+    for (int part = warp; part < parts || part == warp; part += warps) {
+        const int sums = lane < parts ? scratch[lane] : 0;
+        used = __reduce_add_sync(FULL, sums);
+        if (part >= parts) break;
+        const int before = __reduce_add_sync(FULL, lane < part ? sums : 0);
+        const int e = part * 32 + lane, c = e < p.E ? tot[e] : 0;
+        int inc = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(FULL, inc, o);
+            if (lane >= o) inc += v;
+        }
+        const int start = before + inc - c;
+        if (e < p.E) {
+            base[e] += start;
+            if (write) {
+                p.offsets[e] = start;
+                p.counts[e] = c;
+            }
+        }
+    }
+    if (write && threadIdx.x == 0) p.offsets[p.E] = used;
+    __syncthreads();
+    return used;
 }
 
-// A block chooses for one chunk of tokens and leaves its counts for the layout; a single block goes on to the layout itself.
-template <typename T, int Q, int L>
-__global__ void __launch_bounds__(32 * ONE_BLOCK_WARPS) hccl_route_choose(const __grid_constant__ RouteParams p) {
-    extern __shared__ __align__(16) int sm[];  // hist[E16] bias[E16], then the tokens' keys; a single block: its layout's base and counts in their place
-    __shared__ int rows;
+// A block chooses for one chunk of tokens and leaves its counts for the layout; a single block (ONE) goes on to the layout itself.
+template <typename T, int Q, int L, bool ONE>
+__global__ void __launch_bounds__(32 * (ONE ? ONE_BLOCK_WARPS : MANY_WARPS), ONE ? 1 : 3) hccl_route_choose(const __grid_constant__ RouteParams p) {
+    extern __shared__ __align__(16) int sm[];  // hist[E16] bias[E16], a single block's ids, then the tokens' keys; a single block: its layout's counts in their place
+    __shared__ int scratch[32];
     const int E16 = round_up(p.E, 16), threads = 32 * p.warps, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     int* hist = sm;
     float* sbias = (float*)(sm + E16);
-    float* keys = sbias + E16;
+    int* kept = ONE ? (int*)(sbias + E16) : nullptr;
+    float* keys = sbias + E16 + (ONE ? round_up((int)p.tokens * p.K, 4) : 0);
     asm volatile("griddepcontrol.launch_dependents;");
+    bool strange = false;
     for (int e = threadIdx.x; e < E16; e += threads) {
         hist[e] = 0;
-        if (p.bias) sbias[e] = e < p.E ? p.bias[e] : 0.f;
+        if (p.bias) {
+            const float b = e < p.E ? p.bias[e] : 0.f;
+            sbias[e] = b;
+            strange |= !(fabsf(b) < INFINITY);
+        }
     }
-    __syncthreads();
+    const bool odd = __syncthreads_or(strange);
     const long long t0 = (long long)blockIdx.x * p.chunk, t1 = min(t0 + p.chunk, p.tokens);
     const int sub = lane / L, per = 32 / L;
     float* mine = keys + (warp * per + sub) * token_floats(p);
-    for (long long t = t0 + warp * per; t < t1; t += p.warps * per) choose_token<T, Q, L>(p, t + sub, t + sub < t1, mine, sbias, hist);
+    for (long long t = t0 + warp * per; t < t1; t += p.warps * per) choose_token<T, Q, L>(p, t + sub, t + sub < t1, mine, sbias, odd, hist, kept);
     __syncthreads();
-    if (p.chunks > 1) {
+    if constexpr (!ONE) {
         for (int e = threadIdx.x; e < E16; e += threads) p.hist[(size_t)blockIdx.x * E16 + e] = (uint8_t)hist[e];
         return;
     }
-    int *base = (int*)sbias, *cnt = base + E16;
+    int *base = (int*)sbias, *cnt = (int*)keys;
     for (int e = threadIdx.x; e < p.E; e += threads) base[e] = 0;
     __syncthreads();
-    const int used = offsets_of(p, hist, base, &rows, true);
+    const int used = offsets_of(p, hist, base, scratch, true, threads);
     const int n = (int)(p.tokens * p.K);
-    layout_choices(p, 0, n, base, cnt, threads);
+    layout_choices(p, kept, 0, n, base, cnt, threads);
     for (int i = used + (int)threadIdx.x; i < n; i += threads) p.source[i] = -1;
 }
 
@@ -360,56 +452,67 @@ __device__ __forceinline__ void add_bytes(uint4 v, unsigned (&sum)[8]) {
         sum[2 * i + 1] += (w[i] >> 8) & 0x00ff00ffu;
     }
 }
-__device__ __forceinline__ void flush_bytes(int* to, int e0, int E, unsigned (&sum)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const int e = e0 + i / 2 * 4 + (i & 1);
-        if (e < E && (sum[i] & 0xffffu)) atomicAdd(&to[e], (int)(sum[i] & 0xffffu));
-        if (e + 2 < E && (sum[i] >> 16)) atomicAdd(&to[e + 2], (int)(sum[i] >> 16));
-        sum[i] = 0;
-    }
-}
-
 // Each block lays out the choices of a run of chunks. How many rows of each expert lie before them, and in all, it adds up itself from the
-// chunks' counts: 8 bits each (a chunk has at most 255 tokens, a token chooses an expert once), read 16 at a time.
+// chunks' counts: 8 bits each (a chunk has at most 255 tokens, a token chooses an expert once), read 16 at a time and summed in 16 bits by a thread, in 32 bits over the threads.
 __global__ void __launch_bounds__(LAYOUT_THREADS) hccl_route_layout(const __grid_constant__ RouteParams p) {
-    extern __shared__ __align__(16) int sm[];  // tot[E16], base[E16], cnt[warps][E]
-    __shared__ int rows;
-    const int E16 = round_up(p.E, 16);
+    extern __shared__ __align__(16) int sm[];  // tot[E16], base[E16], then sums[2][lines][E16 / 2] or, after them, cnt[warps][E]
+    __shared__ int scratch[32];
+    const int E16 = round_up(p.E, 16), columns = E16 / 16, lines = layout_lines(p.E);
     int *tot = sm, *base = sm + E16, *cnt = base + E16;
-    for (int e = threadIdx.x; e < E16; e += LAYOUT_THREADS) tot[e] = base[e] = 0;
-    __syncthreads();
+    unsigned* sums = (unsigned*)cnt;
     const int c0 = (int)((long long)p.chunks * blockIdx.x / gridDim.x), c1 = (int)((long long)p.chunks * (blockIdx.x + 1) / gridDim.x);
+    const int col = (int)threadIdx.x % columns, line = (int)threadIdx.x / columns;
+    for (int e = threadIdx.x; e < 2 * E16; e += LAYOUT_THREADS) tot[e] = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int columns = E16 / 16, lines = LAYOUT_THREADS / columns, col = (int)threadIdx.x % columns, line = (int)threadIdx.x / columns;
-    if (line < lines) {
-        unsigned sum[8] = {};
-        const uint4* h = (const uint4*)p.hist + col;
-        const auto add_up = [&](int from, int to, int* where) {
-            int n = 0;
-            for (int c = from + line; c < to; c += 8 * lines) {
+    const uint4* h = (const uint4*)p.hist + col;
+    const int per_line = (p.chunks + lines - 1) / lines;  // a line adds up every lines-th chunk, 256 of them at a time: 257 bytes of 255 fill 16 bits
+    for (int from = 0; from < per_line; from += 256) {
+        unsigned below[8] = {}, rest[8] = {};
+        if (line < lines)
+            for (int n = from; n < min(from + 256, per_line); n += 8) {
                 uint4 v[8];
 #pragma unroll
-                for (int u = 0; u < 8; u++) v[u] = c + u * lines < to ? h[(size_t)(c + u * lines) * columns] : make_uint4(0, 0, 0, 0);
+                for (int u = 0; u < 8; u++) {
+                    const int c = line + (n + u) * lines;
+                    v[u] = c < p.chunks ? h[(size_t)c * columns] : make_uint4(0, 0, 0, 0);
+                }
 #pragma unroll
-                for (int u = 0; u < 8; u++) add_bytes(v[u], sum);
-                n += 8;
-                if (n + 8 > 256) {  // 257 bytes of 255 fill 16 bits
-                    flush_bytes(where, col * 16, p.E, sum);
-                    n = 0;
+                for (int u = 0; u < 8; u++) {
+                    if (line + (n + u) * lines < c0) add_bytes(v[u], below);
+                    else add_bytes(v[u], rest);
                 }
             }
-            flush_bytes(where, col * 16, p.E, sum);
-        };
-        add_up(0, c0, base);
-        add_up(c0, p.chunks, tot);
+        __syncthreads();
+        if (line < lines) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                sums[line * (E16 / 2) + col * 8 + i] = below[i];
+                sums[(lines + line) * (E16 / 2) + col * 8 + i] = rest[i];
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < E16; i += LAYOUT_THREADS) {  // word i of the sums before, or of the rest: two experts
+            const bool before = i < E16 / 2;
+            const int w = before ? i : i - E16 / 2, e = w / 8 * 16 + (w % 8) / 2 * 4 + (w & 1);
+            const unsigned* from_lines = sums + (before ? 0 : lines * (E16 / 2)) + w;
+            int lo = 0, hi = 0;
+#pragma unroll 8
+            for (int l = 0; l < lines; l++) {
+                const unsigned v = from_lines[l * (E16 / 2)];
+                lo += v & 0xffffu;
+                hi += v >> 16;
+            }
+            int* to = before ? base : tot;
+            to[e] += lo;
+            to[e + 2] += hi;
+        }
+        __syncthreads();
     }
+    for (int e = threadIdx.x; e < E16; e += LAYOUT_THREADS) tot[e] += base[e];
     __syncthreads();
-    for (int e = threadIdx.x; e < p.E; e += LAYOUT_THREADS) tot[e] += base[e];
-    __syncthreads();
-    const int used = offsets_of(p, tot, base, &rows, blockIdx.x == 0);
+    const int used = offsets_of(p, tot, base, scratch, blockIdx.x == 0, LAYOUT_THREADS);
     const long long t0 = (long long)c0 * p.chunk, t1 = min((long long)c1 * p.chunk, p.tokens);
-    if (t0 < t1) layout_choices(p, t0 * p.K, (int)((t1 - t0) * p.K), base, cnt, LAYOUT_THREADS);
+    if (t0 < t1) layout_choices(p, p.ids + t0 * p.K, t0 * p.K, (int)((t1 - t0) * p.K), base, cnt, LAYOUT_THREADS);
     const long long n = p.tokens * p.K;  // rows that belong to no choice
     for (long long i = used + (long long)blockIdx.x * LAYOUT_THREADS + threadIdx.x; i < n; i += (long long)gridDim.x * LAYOUT_THREADS) p.source[i] = -1;
 }
@@ -561,18 +664,25 @@ template <typename K> cudaError_t allow(K* kernel, size_t bytes, bool (&ready)[6
     return e;
 }
 
+template <typename T, int Q, int L, bool ONE> cudaError_t choose_launch(const RouteParams& p, cudaStream_t s) {
+    size_t ints = (size_t)p.warps * (32 / L) * token_floats(p);
+    if (ONE) ints = std::max(ints, (size_t)p.warps * p.E) + round_up((int)p.tokens * p.K, 4);
+    const size_t smem = (2 * round_up(p.E, 16) + ints) * 4;
+    static bool ready[64];
+    const cudaError_t e = allow(hccl_route_choose<T, Q, L, ONE>, smem, ready);
+    if (e != cudaSuccess) return e;
+    hccl_route_choose<T, Q, L, ONE><<<p.chunks, 32 * p.warps, smem, s>>>(p);
+    return cudaGetLastError();
+}
+
 template <typename T, int Q, int L> cudaError_t route_launch(const RouteParams& p, cudaStream_t s) {
     const int E16 = round_up(p.E, 16);
-    size_t smem = (size_t)(2 * E16) * 4 + (size_t)p.warps * (32 / L) * token_floats(p) * 4;
-    if (p.chunks == 1) smem = std::max(smem, (size_t)(2 * E16 + p.warps * p.E) * 4);
-    static bool ready[64];
-    cudaError_t e = allow(hccl_route_choose<T, Q, L>, smem, ready);
+    if (p.chunks == 1) return choose_launch<T, Q, L, true>(p, s);
+    cudaError_t e = choose_launch<T, Q, L, false>(p, s);
     if (e != cudaSuccess) return e;
-    hccl_route_choose<T, Q, L><<<p.chunks, 32 * p.warps, smem, s>>>(p);
-    if (p.chunks == 1) return cudaGetLastError();
     static bool ready2[64];
     cudaLaunchConfig_t cfg = {};
-    cfg.dynamicSmemBytes = (size_t)(2 * E16 + LAYOUT_THREADS / 32 * p.E) * 4;
+    cfg.dynamicSmemBytes = (size_t)(2 * E16 + std::max(LAYOUT_THREADS / 32 * p.E, layout_lines(p.E) * E16)) * 4;
     if ((e = allow(hccl_route_layout, cfg.dynamicSmemBytes, ready2)) != cudaSuccess) return e;
     cfg.gridDim = dim3((unsigned)std::min(p.chunks, SMS));
     cfg.blockDim = dim3(LAYOUT_THREADS);
@@ -627,7 +737,7 @@ cudaError_t launch_route(int dt, const RouteParams& in, cudaStream_t s) {
     p.per4 = p.per_group % 4 == 0;
     p.magic = ((1 << 20) + p.per_group - 1) / p.per_group;
     const int es = dt == HCCL_FP32 ? 4 : 2;
-    p.vec = aligned_rows(p.logits, p.ld, es, 4 * es);
+    p.vec = aligned_rows(p.logits, p.ld, es, 4 * es) && p.E % 4 == 0;
     if (dt == HCCL_FP32) return route_sizes<float>(p, c.lanes, s);
     if (dt == HCCL_BF16) return route_sizes<__nv_bfloat16>(p, c.lanes, s);
     return route_sizes<__half>(p, c.lanes, s);

@@ -249,8 +249,8 @@ enum { DISPATCH, COMBINE, COMBINE_GRAD };
 
 // Warps for each token, by measurement (8192 x 4096 of 8, 4099 x 2056 of 6, 2000 x 1024 of 4, all bf16): the gradient 189, 50 and 12 us with two, 200, 55 and 11
 // with one, 206, 60 and 15 with four; combine 109, 30 and 5 us with one, 112, 37 and 5 with four. With few tokens as many as make 16 warps for each SM.
-int team_of(int what, long long tokens, long long cols) {
-    int w = what == COMBINE_GRAD && cols >= 64 ? 2 : 1;
+int team_of(int what, long long tokens, long long cols, long long row_bytes) {
+    int w = what == COMBINE_GRAD && row_bytes >= 2048 ? 2 : 1;
     while (w < ROWS_THREADS / 32 && tokens * w < SMS * 16 && cols > 32 * w) w *= 2;
     return w;
 }
@@ -258,7 +258,7 @@ int team_of(int what, long long tokens, long long cols) {
 template <typename T, int N> cudaError_t rows_launch(int what, const RowsParams& p, cudaStream_t s) {
     const long long cols = p.H / N;
     if (cols > 1 << 30) return cudaErrorInvalidValue;
-    const int team = team_of(what, p.tokens, cols), per = ROWS_THREADS / 32 / team;
+    const int team = team_of(what, p.tokens, cols, p.H * (long long)sizeof(T)), per = ROWS_THREADS / 32 / team;
     const long long whole = (p.tokens + per - 1) / per;  // a block for each `per` tokens: the hardware hands out the next one where one has ended
     const unsigned blocks = (unsigned)std::min<long long>(std::max<long long>(whole, what == COMBINE ? 1 : SMS), 1 << 30);
     if (what == COMBINE) {

@@ -196,17 +196,19 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
             // lanes start at different places of their groups: different banks
             if (p.per4) {
                 const int quads = p.per_group / 4;
-                int at = g % quads;
+                int at = min(l & 7, quads - 1);
                 for (int i = 0; i < quads; i += 4) {
                     float4 v[4];
 #pragma unroll
                     for (int u = 0; u < 4; u++) {
-                        v[u] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-                        if (i + u < quads) v[u] = *(const float4*)(k + 4 * at);
+                        v[u] = *(const float4*)(k + 4 * at);
                         at = at + 1 == quads ? 0 : at + 1;
                     }
 #pragma unroll
-                    for (int u = 0; u < 4; u++) seen(v[u].x), seen_too(v[u].z), seen(v[u].y), seen_too(v[u].w);
+                    for (int u = 0; u < 4; u++) {
+                        if (i + u >= quads) v[u] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);  // round again: seen already
+                        seen(v[u].x), seen_too(v[u].z), seen(v[u].y), seen_too(v[u].w);
+                    }
                 }
             } else {
                 int at = g % p.per_group;
@@ -316,7 +318,7 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
 
 // Rows of the choices [first, first + n), whose experts are ids[0 .. n). base[e] (shared) = first row of expert e for them; rows follow in the order of the choices.
 // Each warp takes a run of them; a first walk counts by expert, a second hands out the rows with match_any, so that the
-// order does not depend on which warp is faster. cnt: shared, [warps][E].
+// order does not depend on which warp is faster. cnt: shared, [warps][E], of at most 16 warps.
 __device__ __forceinline__ void layout_choices(const RouteParams& p, const int* ids, long long first, int n, const int* base, int* cnt, int threads) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = threads / 32;
     const int per = round_up((n + warps - 1) / warps, 32);
@@ -340,12 +342,13 @@ __device__ __forceinline__ void layout_choices(const RouteParams& p, const int* 
     }
     __syncthreads();
     for (int e = threadIdx.x; e < p.E; e += threads) {  // counts become first rows
-        int at = base[e];
-#pragma unroll 4
-        for (int w = 0; w < warps; w++) {
-            const int c = cnt[w * p.E + e];
-            cnt[w * p.E + e] = at;
-            at += c;
+        int at = base[e], c[16];
+#pragma unroll
+        for (int w = 0; w < 16; w++) c[w] = w < warps ? cnt[w * p.E + e] : 0;
+#pragma unroll
+        for (int w = 0; w < 16; w++) {
+            if (w < warps) cnt[w * p.E + e] = at;
+            at += c[w];
         }
     }
     __syncthreads();
@@ -465,51 +468,60 @@ __global__ void __launch_bounds__(LAYOUT_THREADS) hccl_route_layout(const __grid
     for (int e = threadIdx.x; e < 2 * E16; e += LAYOUT_THREADS) tot[e] = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint4* h = (const uint4*)p.hist + col;
-    const int per_line = (p.chunks + lines - 1) / lines;  // a line adds up every lines-th chunk, 256 of them at a time: 257 bytes of 255 fill 16 bits
+    const int per_line = (p.chunks + lines - 1) / lines;  // a line adds up a run of chunks, 256 of them at a time: 257 bytes of 255 fill 16 bits
     for (int from = 0; from < per_line; from += 256) {
         unsigned below[8] = {}, rest[8] = {};
-        if (line < lines)
-            for (int n = from; n < min(from + 256, per_line); n += 8) {
-                uint4 v[8];
-#pragma unroll
-                for (int u = 0; u < 8; u++) {
-                    const int c = line + (n + u) * lines;
-                    v[u] = c < p.chunks ? h[(size_t)c * columns] : make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int u = 0; u < 8; u++) {
-                    if (line + (n + u) * lines < c0) add_bytes(v[u], below);
-                    else add_bytes(v[u], rest);
-                }
-            }
-        __syncthreads();
         if (line < lines) {
+            const auto add_up = [&](int c, int end, unsigned (&sum)[8]) {
+                for (; c < end; c += 8) {
+                    uint4 v[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                sums[line * (E16 / 2) + col * 8 + i] = below[i];
-                sums[(lines + line) * (E16 / 2) + col * 8 + i] = rest[i];
-            }
+                    for (int u = 0; u < 8; u++) v[u] = c + u < end ? h[(size_t)(c + u) * columns] : make_uint4(0, 0, 0, 0);
+                    if (p.chunk <= 63) {  // four of them still fit 8 bits
+#pragma unroll
+                        for (int u = 0; u < 8; u += 4)
+                            add_bytes(make_uint4(v[u].x + v[u + 1].x + v[u + 2].x + v[u + 3].x, v[u].y + v[u + 1].y + v[u + 2].y + v[u + 3].y,
+                                                 v[u].z + v[u + 1].z + v[u + 2].z + v[u + 3].z, v[u].w + v[u + 1].w + v[u + 2].w + v[u + 3].w), sum);
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 8; u++) add_bytes(v[u], sum);
+                    }
+                }
+            };
+            const int lo = line * per_line + from, hi = min(min(lo + 256, (line + 1) * per_line), p.chunks);
+            add_up(lo, min(hi, c0), below);
+            add_up(max(lo, c0), hi, rest);
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < E16; i += LAYOUT_THREADS) {  // word i of the sums before, or of the rest: two experts
-            const bool before = i < E16 / 2;
-            const int w = before ? i : i - E16 / 2, e = w / 8 * 16 + (w % 8) / 2 * 4 + (w & 1);
+        if (line < lines) {
+            uint4 *a = (uint4*)(sums + line * (E16 / 2) + col * 8), *b = (uint4*)(sums + (lines + line) * (E16 / 2) + col * 8);
+            a[0] = make_uint4(below[0], below[1], below[2], below[3]);
+            a[1] = make_uint4(below[4], below[5], below[6], below[7]);
+            b[0] = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+            b[1] = make_uint4(rest[4], rest[5], rest[6], rest[7]);
+        }
+        __syncthreads();
+        // word w of the sums before, or of the rest: two experts; the lines in `parts` shares
+        const int parts = max(1, LAYOUT_THREADS / E16);
+        for (int i = threadIdx.x; i < E16 * parts; i += LAYOUT_THREADS) {
+            const int part = i / E16, at = i % E16;
+            const bool before = at < E16 / 2;
+            const int w = before ? at : at - E16 / 2, e = w / 8 * 16 + (w % 8) / 2 * 4 + (w & 1);
             const unsigned* from_lines = sums + (before ? 0 : lines * (E16 / 2)) + w;
             int lo = 0, hi = 0;
 #pragma unroll 8
-            for (int l = 0; l < lines; l++) {
+            for (int l = part; l < lines; l += parts) {
                 const unsigned v = from_lines[l * (E16 / 2)];
                 lo += v & 0xffffu;
                 hi += v >> 16;
             }
-            int* to = before ? base : tot;
-            to[e] += lo;
-            to[e + 2] += hi;
+            if (lo) atomicAdd(&tot[e], lo);
+            if (hi) atomicAdd(&tot[e + 2], hi);
+            if (before && lo) atomicAdd(&base[e], lo);
+            if (before && hi) atomicAdd(&base[e + 2], hi);
         }
         __syncthreads();
     }
-    for (int e = threadIdx.x; e < E16; e += LAYOUT_THREADS) tot[e] += base[e];
-    __syncthreads();
     const int used = offsets_of(p, tot, base, scratch, blockIdx.x == 0, LAYOUT_THREADS);
     const long long t0 = (long long)c0 * p.chunk, t1 = min((long long)c1 * p.chunk, p.tokens);
     if (t0 < t1) layout_choices(p, p.ids + t0 * p.K, t0 * p.K, (int)((t1 - t0) * p.K), base, cnt, LAYOUT_THREADS);

@@ -31,13 +31,15 @@ def _refuse(status: int, what: str):
     raise hb.HcclError(status, what)
 
 
-def _matrix(t: torch.Tensor, what: str, cols: Optional[int] = None, rows: Optional[int] = None) -> int:
-    """Checks a 2-d CUDA matrix with adjacent columns; returns the distance between its rows."""
-    if not t.is_cuda:
-        _refuse(hb.ERR_INVALID_ARG, "%s must be on a CUDA device" % what)
-    if t.dim() != 2:
+def _matrix(t: torch.Tensor, what: str, cols: Optional[int] = None, rows: Optional[int] = None, dev: Optional[int] = None) -> int:
+    """Checks a 2-d matrix with adjacent columns on CUDA device number `dev` (None: any); returns the distance between its rows."""
+    try:
+        n, m = t.shape
+    except ValueError:
         _refuse(hb.ERR_INVALID_ARG, "%s must have two dimensions, not %d" % (what, t.dim()))
-    n, m = t.shape
+    at = t.get_device()
+    if at < 0 or (dev is not None and at != dev):
+        _refuse(hb.ERR_INVALID_ARG, "%s must be on %s, not %s" % (what, "a CUDA device" if dev is None else "cuda:%d" % dev, t.device))
     if (cols is not None and m != cols) or (rows is not None and n != rows):
         _refuse(hb.ERR_COUNT_MISMATCH, "%s is [%d, %d], expected [%s, %s]" % (what, n, m, "any" if rows is None else rows, "any" if cols is None else cols))
     ld, step = t.stride()
@@ -53,30 +55,27 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     return d
 
 
-def _vector(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int, device: torch.device):
+def _vector(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int, dev: int):
     if t.dtype != dtype:
         _refuse(hb.ERR_DTYPE, "%s is %s, expected %s" % (what, t.dtype, dtype))
     if t.numel() != numel:
         _refuse(hb.ERR_COUNT_MISMATCH, "%s has %d elements, expected %d" % (what, t.numel(), numel))
-    if t.device != device or not t.is_contiguous():
-        _refuse(hb.ERR_INVALID_ARG, "%s must be contiguous and on %s" % (what, device))
+    if t.get_device() != dev or not t.is_contiguous():
+        _refuse(hb.ERR_INVALID_ARG, "%s must be contiguous and on cuda:%d" % (what, dev))
 
 
-def _same(a: torch.Tensor, b: torch.Tensor, what: str):
+def _same_type(a: torch.Tensor, b: torch.Tensor, what: str):
     if a.dtype != b.dtype:
         _refuse(hb.ERR_DTYPE, "%s: %s and %s" % (what, a.dtype, b.dtype))
-    if a.device != b.device:
-        _refuse(hb.ERR_INVALID_ARG, "%s: %s and %s" % (what, a.device, b.device))
 
 
-def _on(device: torch.device, call, *args):
-    """call(*args, stream) with `device` current."""
-    i = device.index
-    if i == _current_device():
-        call(*args, _stream(i))
+def _on(dev: int, call, *args):
+    """call(*args, stream) with device number `dev` current."""
+    if dev == _current_device():
+        call(*args, _stream(dev))
     else:
-        with torch.cuda.device(i):
-            call(*args, _stream(i))
+        with torch.cuda.device(dev):
+            call(*args, _stream(dev))
 
 
 class _Scratch:
@@ -85,30 +84,32 @@ class _Scratch:
     def __init__(self):
         self._of = {}
 
-    def get(self, device: torch.device, nbytes: int) -> torch.Tensor:
-        key = (device.index, _stream(device.index))
-        t = self._of.get(key)
-        if t is None or t.numel() < nbytes:
-            t = self._of[key] = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        return t
+    def get(self, dev: int, nbytes: int) -> int:
+        """Address of at least nbytes on device number `dev`."""
+        key = (dev, _stream(dev))
+        have = self._of.get(key)
+        if have is None or have[1] < nbytes:
+            t = torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % dev)
+            have = self._of[key] = (t, nbytes, t.data_ptr())
+        return have[2]
 
 
 class Routing:
     """Which token goes to which expert (hccl_routing_t), as tensors: ids, weights, slots [tokens, top_k]; counts [experts];
     offsets [experts + 1]; source [tokens * top_k]. Rows of expert e, in expert order, are offsets[e]:offsets[e + 1]."""
 
-    __slots__ = ("ids", "weights", "counts", "offsets", "slots", "source", "tokens", "top_k", "experts", "device", "record", "ref")
+    __slots__ = ("ids", "weights", "counts", "offsets", "slots", "source", "tokens", "top_k", "experts", "device", "dev", "record", "ref")
 
     def __init__(self, ids, weights, counts, offsets, slots, source):
         if ids.dim() != 2 or not ids.is_cuda:
             _refuse(hb.ERR_INVALID_ARG, "Routing: ids must be a CUDA tensor [tokens, top_k]")
         self.tokens, self.top_k = ids.shape
-        self.experts, self.device = counts.numel(), ids.device
+        self.experts, self.device, self.dev = counts.numel(), ids.device, ids.get_device()
         n = self.tokens * self.top_k
         for t, what, dt, numel in ((ids, "ids", torch.int32, n), (weights, "weights", torch.float32, n), (counts, "counts", torch.int64, self.experts),
                                    (offsets, "offsets", torch.int32, self.experts + 1), (slots, "slots", torch.int32, n),
                                    (source, "source", torch.int32, n)):
-            _vector(t, what, dt, numel, self.device)
+            _vector(t, what, dt, numel, self.dev)
         self.ids, self.weights, self.counts, self.offsets, self.slots, self.source = ids, weights, counts, offsets, slots, source
         self.record = hb.RoutingRecord(self.tokens, self.top_k, self.experts, ids.data_ptr(), weights.data_ptr(), counts.data_ptr(),
                                        offsets.data_ptr(), slots.data_ptr(), source.data_ptr())
@@ -138,28 +139,29 @@ class Router:
                        torch.empty(self.experts, dtype=torch.int64, device=device), torch.empty(self.experts + 1, **i32),
                        torch.empty(n, **i32), torch.empty(tokens * self.top_k, **i32))
 
-    def _inputs(self, logits, bias, token_mask):
-        ld = _matrix(logits, "logits", cols=self.experts)
+    def _inputs(self, logits, bias, token_mask, dev):
+        ld = _matrix(logits, "logits", self.experts, None, dev)
         dt = _dtype(logits, "logits")
+        b = m = None
         if bias is not None:
-            _vector(bias, "bias", torch.float32, self.experts, logits.device)
+            _vector(bias, "bias", torch.float32, self.experts, logits.get_device())
+            b = bias.data_ptr()
         if token_mask is not None:
             if token_mask.dtype == torch.bool:
                 token_mask = token_mask.view(torch.uint8)
-            _vector(token_mask, "token_mask", torch.uint8, logits.shape[0], logits.device)
-        return ld, dt, (bias.data_ptr() if bias is not None else None), (token_mask.data_ptr() if token_mask is not None else None)
+            _vector(token_mask, "token_mask", torch.uint8, logits.shape[0], logits.get_device())
+            m = token_mask.data_ptr()
+        return ld, dt, b, m
 
     def _run(self, logits, bias, token_mask, out):
-        ld, dt, b, m = self._inputs(logits, bias, token_mask)
-        if out.tokens != logits.shape[0] or out.experts != self.experts or out.top_k != self.top_k:
-            _refuse(hb.ERR_COUNT_MISMATCH, "route: out is for %d tokens, %d experts, top %d" % (out.tokens, out.experts, out.top_k))
-        if out.device != logits.device:
-            _refuse(hb.ERR_INVALID_ARG, "route: out is on %s" % out.device)
-        need = self._need.get(out.tokens)
+        dev, tokens = out.dev, out.tokens
+        ld, dt, b, m = self._inputs(logits, bias, token_mask, dev)
+        if tokens != logits.shape[0] or out.experts != self.experts or out.top_k != self.top_k:
+            _refuse(hb.ERR_COUNT_MISMATCH, "route: out is for %d tokens, %d experts, top %d" % (tokens, out.experts, out.top_k))
+        need = self._need.get(tokens)
         if need is None:
-            need = self._need[out.tokens] = max(hb.hccl_route_workspace_bytes(self.config, out.tokens), 16)
-        ws = self._scratch.get(logits.device, need)
-        _on(logits.device, hb.hccl_route, self._ref, logits.data_ptr(), ld, dt, b, m, out.ref, ws.data_ptr(), need)
+            need = self._need[tokens] = hb.hccl_route_workspace_bytes(self.config, tokens)
+        _on(dev, hb.hccl_route, self._ref, logits.data_ptr(), ld, dt, b, m, out.ref, self._scratch.get(dev, need), need)
 
     def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, token_mask: Optional[torch.Tensor] = None,
               out: Optional[Routing] = None) -> Routing:
@@ -179,15 +181,17 @@ class Router:
     def backward(self, logits: torch.Tensor, routing: Routing, dweights: torch.Tensor, bias: Optional[torch.Tensor] = None,
                  token_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Gradient of the logits for a gradient of the weights (fp32 [tokens, top_k])."""
-        ld, dt, b, m = self._inputs(logits, bias, token_mask)
-        if routing.tokens != logits.shape[0] or routing.device != logits.device:
-            _refuse(hb.ERR_COUNT_MISMATCH, "route backward: routing of %d tokens on %s" % (routing.tokens, routing.device))
-        _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, logits.device)
+        dev = routing.dev
+        ld, dt, b, m = self._inputs(logits, bias, token_mask, dev)
+        if routing.tokens != logits.shape[0]:
+            _refuse(hb.ERR_COUNT_MISMATCH, "route backward: routing of %d tokens" % routing.tokens)
+        _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, dev)
         if out is None:
             out = logits.new_empty(logits.shape)
-        _same(out, logits, "route backward")
-        ldd = _matrix(out, "dlogits", cols=self.experts, rows=routing.tokens)
-        _on(logits.device, hb.hccl_route_backward, self._ref, logits.data_ptr(), ld, dt, b, m, routing.ref, dweights.data_ptr(), out.data_ptr(), ldd)
+        else:
+            _same_type(out, logits, "route backward")
+        ldd = _matrix(out, "dlogits", self.experts, routing.tokens, dev)
+        _on(dev, hb.hccl_route_backward, self._ref, logits.data_ptr(), ld, dt, b, m, routing.ref, dweights.data_ptr(), out.data_ptr(), ldd)
         return out
 
 
@@ -205,28 +209,27 @@ class _Route(torch.autograd.Function):
         return ctx.router.backward(logits, ctx.routing, dweights.contiguous(), bias, token_mask), None, None, None, None
 
 
-def _rows_in(rows: torch.Tensor, routing: Routing, what: str):
-    ld = _matrix(rows, what)
-    if rows.device != routing.device:
-        _refuse(hb.ERR_INVALID_ARG, "%s is on %s, the routing on %s" % (what, rows.device, routing.device))
-    return ld, _dtype(rows, what)
-
-
 def _new(out, shape, like, what):
     if out is None:
         return like.new_empty(shape)
-    _same(out, like, what)
+    _same_type(out, like, what)
     return out
 
 
+def _weights(weights, routing) -> int:
+    if weights is None:
+        return routing.weights.data_ptr()
+    _vector(weights, "weights", torch.float32, routing.tokens * routing.top_k, routing.dev)
+    return weights.data_ptr()
+
+
 def _dispatch(x, routing, out, n_rows):
-    ldx, dt = _rows_in(x, routing, "x")
-    if x.shape[0] != routing.tokens:
-        _refuse(hb.ERR_COUNT_MISMATCH, "dispatch: %d tokens, the routing has %d" % (x.shape[0], routing.tokens))
+    dev = routing.dev
+    ldx, dt = _matrix(x, "x", None, routing.tokens, dev), _dtype(x, "x")
     H = x.shape[1]
     out = _new(out, (routing.tokens * routing.top_k if n_rows is None else n_rows, H), x, "dispatch")
-    ldr = _matrix(out, "rows", cols=H)
-    _on(x.device, hb.hccl_dispatch, x.data_ptr(), ldx, H, dt, routing.ref, out.data_ptr(), ldr, out.shape[0])
+    ldr = _matrix(out, "rows", H, n_rows, dev)
+    _on(dev, hb.hccl_dispatch, x.data_ptr(), ldx, H, dt, routing.ref, out.data_ptr(), ldr, out.shape[0])
     return out
 
 
@@ -241,24 +244,23 @@ def dispatch(x: torch.Tensor, routing: Routing, out: Optional[torch.Tensor] = No
 
 def dispatch_backward(drows: torch.Tensor, routing: Routing, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dx[t] = sum over k of drows[slots[t, k]]."""
-    ldr, dt = _rows_in(drows, routing, "drows")
+    dev = routing.dev
+    ldr, dt = _matrix(drows, "drows", None, None, dev), _dtype(drows, "drows")
     n, H = drows.shape
     out = _new(out, (routing.tokens, H), drows, "dispatch backward")
-    ldx = _matrix(out, "dx", cols=H, rows=routing.tokens)
-    _on(drows.device, hb.hccl_dispatch_backward, drows.data_ptr(), ldr, n, H, dt, routing.ref, out.data_ptr(), ldx)
+    ldx = _matrix(out, "dx", H, routing.tokens, dev)
+    _on(dev, hb.hccl_dispatch_backward, drows.data_ptr(), ldr, n, H, dt, routing.ref, out.data_ptr(), ldx)
     return out
 
 
 def _combine(rows, routing, weights, out):
-    ldr, dt = _rows_in(rows, routing, "rows")
-    if weights is None:
-        weights = routing.weights
-    else:
-        _vector(weights, "weights", torch.float32, routing.tokens * routing.top_k, routing.device)
+    dev = routing.dev
+    ldr, dt = _matrix(rows, "rows", None, None, dev), _dtype(rows, "rows")
+    w = _weights(weights, routing)
     n, H = rows.shape
     out = _new(out, (routing.tokens, H), rows, "combine")
-    ldy = _matrix(out, "y", cols=H, rows=routing.tokens)
-    _on(rows.device, hb.hccl_combine, rows.data_ptr(), ldr, n, H, dt, routing.ref, weights.data_ptr(), out.data_ptr(), ldy)
+    ldy = _matrix(out, "y", H, routing.tokens, dev)
+    _on(dev, hb.hccl_combine, rows.data_ptr(), ldr, n, H, dt, routing.ref, w, out.data_ptr(), ldy)
     return out
 
 
@@ -274,19 +276,16 @@ def combine(rows: torch.Tensor, routing: Routing, weights: Optional[torch.Tensor
 def combine_backward(dy: torch.Tensor, rows: torch.Tensor, routing: Routing, weights: Optional[torch.Tensor] = None,
                      out: Optional[torch.Tensor] = None):
     """(drows, dweights) for a gradient dy of combine's result."""
-    ldr, dt = _rows_in(rows, routing, "rows")
+    dev = routing.dev
+    ldr, dt = _matrix(rows, "rows", None, None, dev), _dtype(rows, "rows")
     n, H = rows.shape
-    ldy = _matrix(dy, "dy", cols=H, rows=routing.tokens)
-    _same(dy, rows, "combine backward")
-    if weights is None:
-        weights = routing.weights
-    else:
-        _vector(weights, "weights", torch.float32, routing.tokens * routing.top_k, routing.device)
+    ldy = _matrix(dy, "dy", H, routing.tokens, dev)
+    _same_type(dy, rows, "combine backward")
+    w = _weights(weights, routing)
     out = _new(out, (n, H), rows, "combine backward")
-    ldd = _matrix(out, "drows", cols=H, rows=n)
+    ldd = _matrix(out, "drows", H, n, dev)
     dw = routing.weights.new_empty((routing.tokens, routing.top_k))
-    _on(rows.device, hb.hccl_combine_backward, dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.ref, weights.data_ptr(), out.data_ptr(), ldd,
-        dw.data_ptr())
+    _on(dev, hb.hccl_combine_backward, dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.ref, w, out.data_ptr(), ldd, dw.data_ptr())
     return out, dw
 
 
@@ -327,16 +326,12 @@ def _pad16(n: int) -> int:
 def quantize_rows(x: torch.Tensor, routing: Optional[Routing] = None, n_rows: Optional[int] = None):
     """(q, scale): 8-bit rows and a scale for each, x[m] ~ q[m] * scale[m]. With a routing the rows come in expert order (n_rows: the
     capacity, default tokens * top_k; rows that no choice fills are left alone). q's rows start 16 bytes apart or a multiple of it."""
-    ldx = _matrix(x, "x")
-    dt = _dtype(x, "x")
+    ldx, dt, dev = _matrix(x, "x", dev=None if routing is None else routing.dev), _dtype(x, "x"), x.get_device()
     M, K = x.shape
     n = M if routing is None else (routing.tokens * routing.top_k if n_rows is None else n_rows)
-    if routing is not None and routing.device != x.device:
-        _refuse(hb.ERR_INVALID_ARG, "quantize_rows: the routing is on %s" % routing.device)
     q = torch.empty((n, _pad16(K)), dtype=torch.int8, device=x.device)
     scale = torch.empty(n, dtype=torch.float32, device=x.device)
-    _on(x.device, hb.hccl_quantize_rows_i8, x.data_ptr(), ldx, M, K, dt, routing.ref if routing is not None else None, q.data_ptr(), q.shape[1], n,
-        scale.data_ptr())
+    _on(dev, hb.hccl_quantize_rows_i8, x.data_ptr(), ldx, M, K, dt, routing.ref if routing is not None else None, q.data_ptr(), q.shape[1], n, scale.data_ptr())
     return q[:, :K], scale
 
 
@@ -352,11 +347,11 @@ class Int8Linear:
             _refuse(hb.ERR_INVALID_ARG, "Int8Linear: weight must be a CUDA tensor [N, K] or [experts, N, K]")
         self.experts = weight.shape[0] if weight.dim() == 3 else 0
         self.N, self.K = weight.shape[-2:]
-        self.device = weight.device
+        self.device, self.dev = weight.device, weight.get_device()
         rows = max(self.experts, 1) * self.N
-        _vector(scale, "scale", torch.float32, rows, self.device)
+        _vector(scale, "scale", torch.float32, rows, self.dev)
         if bias is not None:
-            _vector(bias, "bias", torch.float32, rows, self.device)
+            _vector(bias, "bias", torch.float32, rows, self.dev)
         if not weight.is_contiguous() or self.K % 16 or weight.data_ptr() % 16:
             padded = torch.zeros(weight.shape[:-1] + (_pad16(self.K),), dtype=torch.int8, device=self.device)
             padded[..., : self.K] = weight
@@ -365,6 +360,8 @@ class Int8Linear:
         self.ldw = weight.shape[-1]
         self._scratch = _Scratch()
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._fixed = (weight.data_ptr(), self.ldw, scale.data_ptr(), bias.data_ptr() if bias is not None else None)
+        self._status_at = self._status.data_ptr()
 
     @classmethod
     def from_float(cls, weight: torch.Tensor, bias: Optional[torch.Tensor] = None) -> "Int8Linear":
@@ -372,51 +369,46 @@ class Int8Linear:
         q, scale = quantize_rows(weight.reshape(-1, weight.shape[-1]))
         return cls(q.reshape(weight.shape), scale.view(weight.shape[:-1]), bias)
 
-    def _args(self, M, y, ldy, offsets):
+    def _args(self, M, a, lda, a_scale, dt, y, ldy, offsets):
+        w, ldw, w_scale, bias = self._fixed
         if offsets is not None:
-            _vector(offsets, "offsets", torch.int32, self.experts + 1, self.device)
-        return hb.MatmulI8(M, self.N, self.K, self.experts, _DT[y.dtype], None, 0, None, self.weight.data_ptr(), self.ldw, self.scale.data_ptr(),
-                           self.bias.data_ptr() if self.bias is not None else None, offsets.data_ptr() if offsets is not None else None,
-                           y.data_ptr(), ldy, self._status.data_ptr())
+            _vector(offsets, "offsets", torch.int32, self.experts + 1, self.dev)
+            offsets = offsets.data_ptr()
+        return C.byref(hb.MatmulI8(M, self.N, self.K, self.experts, dt, a, lda, a_scale, w, ldw, w_scale, bias, offsets, y, ldy, self._status_at))
 
     def _out(self, out, M, dtype):
+        """The result, its row distance and its type."""
         if out is None:
-            return torch.empty((M, self.N), dtype=dtype, device=self.device), self.N
-        if out.device != self.device:
-            _refuse(hb.ERR_INVALID_ARG, "Int8Linear: out is on %s" % out.device)
-        _dtype(out, "out")
-        return out, _matrix(out, "out", cols=self.N, rows=M)
+            if dtype not in _DT:
+                _refuse(hb.ERR_DTYPE, "Int8Linear: result in %s" % dtype)
+            return torch.empty((M, self.N), dtype=dtype, device=self.device), self.N, _DT[dtype]
+        return out, _matrix(out, "out", self.N, M, self.dev), _dtype(out, "out")
 
     def _which(self, routing, offsets):
         if self.experts and (routing is None) == (offsets is None):
             _refuse(hb.ERR_INVALID_ARG, "Int8Linear over experts takes a routing or offsets")
         if not self.experts and (routing is not None or offsets is not None):
             _refuse(hb.ERR_INVALID_ARG, "Int8Linear with one matrix takes neither a routing nor offsets")
-        if routing is not None and (routing.experts != self.experts or routing.device != self.device):
+        if routing is not None and (routing.experts != self.experts or routing.dev != self.dev):
             _refuse(hb.ERR_COUNT_MISMATCH, "Int8Linear: routing over %d experts on %s" % (routing.experts, routing.device))
 
     def __call__(self, x: torch.Tensor, routing: Optional[Routing] = None, offsets: Optional[torch.Tensor] = None,
                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [M, K]. Over experts: with a routing, x holds tokens and row r of the result belongs to choice source[r]; with offsets (int32
         [experts + 1], on the device) x is in expert order already."""
-        ldx = _matrix(x, "x", cols=self.K)
-        dt = _dtype(x, "x")
-        if x.device != self.device:
-            _refuse(hb.ERR_INVALID_ARG, "Int8Linear: x is on %s" % x.device)
+        dev, K = self.dev, self.K
+        ldx, dt = _matrix(x, "x", K, None, dev), _dtype(x, "x")
         self._which(routing, offsets)
         M, ref = x.shape[0], None
         if routing is not None:
             if M != routing.tokens:
                 _refuse(hb.ERR_COUNT_MISMATCH, "Int8Linear: %d tokens, the routing has %d" % (M, routing.tokens))
             M, ref, offsets = M * routing.top_k, routing.ref, routing.offsets
-        y, ldy = self._out(out, M, x.dtype)
-        a = self._args(M, y, ldy, offsets)
-        lda = _pad16(self.K)
+        y, ldy, y_dt = self._out(out, M, x.dtype)
+        lda = _pad16(K)
         room = M * lda
-        t = self._scratch.get(self.device, room + 4 * M)
-        a.a, a.lda = t.data_ptr(), lda
-        a.a_scale = a.a + room
-        _on(self.device, hb.hccl_linear_i8, C.byref(a), x.data_ptr(), ldx, dt, ref)
+        at = self._scratch.get(dev, room + 4 * M)
+        _on(dev, hb.hccl_linear_i8, self._args(M, at, lda, at + room, y_dt, y.data_ptr(), ldy, offsets), x.data_ptr(), ldx, dt, ref)
         return y
 
     def matmul(self, q: torch.Tensor, q_scale: torch.Tensor, offsets: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -424,15 +416,12 @@ class Int8Linear:
         """The product alone, of rows that are in 8 bits already (quantize_rows; received from an exchange)."""
         if q.dtype != torch.int8:
             _refuse(hb.ERR_DTYPE, "Int8Linear: q is %s" % q.dtype)
-        lda = _matrix(q, "q", cols=self.K)
-        if q.device != self.device:
-            _refuse(hb.ERR_INVALID_ARG, "Int8Linear: q is on %s" % q.device)
-        _vector(q_scale, "q_scale", torch.float32, q.shape[0], self.device)
+        lda = _matrix(q, "q", self.K, None, self.dev)
+        M = q.shape[0]
+        _vector(q_scale, "q_scale", torch.float32, M, self.dev)
         self._which(None, offsets)
-        y, ldy = self._out(out, q.shape[0], dtype)
-        a = self._args(q.shape[0], y, ldy, offsets)
-        a.a, a.lda, a.a_scale = q.data_ptr(), lda if q.shape[0] > 1 else _pad16(lda), q_scale.data_ptr()
-        _on(self.device, hb.hccl_matmul_i8, C.byref(a))
+        y, ldy, y_dt = self._out(out, M, dtype)
+        _on(self.dev, hb.hccl_matmul_i8, self._args(M, q.data_ptr(), lda if M > 1 else _pad16(lda), q_scale.data_ptr(), y_dt, y.data_ptr(), ldy, offsets))
         return y
 
     def check(self):

@@ -40,6 +40,7 @@ struct TileParams {
     void* y;
     int* status;
     int M, N, groups, k_blocks, n_tiles, splits, dependent;
+    int pairs;  // two neighbouring 16-bit results of a row can be written at once
 };
 
 // ---------------------------------------------------------------- instructions
@@ -292,7 +293,7 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
     const auto scaled = [&](int sum, float sa, float sw, float bias) {
         // a sum passes 2^24 from K = 1024 on: its conversion to 32-bit floating point is a rounding, like each scale's product
         const float v = __fmul_rn(__fmul_rn((float)sum, sa), sw);
-        return from_f32<T>(p.bias ? __fadd_rn(v, bias) : v);
+        return p.bias ? __fadd_rn(v, bias) : v;
     };
     const auto results = [&](const Tile& t) {
         const int b = acc & 1, quarter = warp & 3, chan = t.chan + quarter * 32 + lane;
@@ -326,17 +327,24 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
 #pragma unroll
                 for (int j = 0; j < 32; j++) v[j] = 0;
             }
-            T o[C];  // all of them before the first store: a branch for each would leave its chain of latencies bare
+            float o[C];  // all of them before the first store: a branch for each would leave its chain of latencies bare
 #pragma unroll
             for (int j = 0; j < C; j++) o[j] = scaled(v[j], __shfl_sync(0xffffffffu, sa[u], j), sw, bias);
             T* y = (T*)p.y + (long long)(t.row + c0) * p.ldy + chan;
-            if (in && c0 + C <= t.rows) {
+            if (sizeof(T) == 2 && p.pairs && c0 + C <= t.rows && t.chan + quarter * 32 + 32 <= p.N) {
+                // Two neighbouring lanes trade: the even one keeps row j of both channels, the odd one row j + 1, four bytes each, so that a store
+                // instruction writes 64 bytes of two rows.
+                const int odd = lane & 1;
+                y += odd * p.ldy - odd;
 #pragma unroll
-                for (int j = 0; j < C; j++, y += p.ldy) *y = o[j];
+                for (int j = 0; j < C; j += 2, y += 2 * p.ldy) {
+                    const unsigned mine = Pack<T, 2>::word(o[j], o[j + 1]), other = __shfl_xor_sync(0xffffffffu, mine, 1);
+                    *(unsigned*)y = __byte_perm(mine, other, odd ? 0x3276 : 0x5410);
+                }
             } else if (in) {
 #pragma unroll
                 for (int j = 0; j < C; j++, y += p.ldy)
-                    if (c0 + j < t.rows) *y = o[j];
+                    if (c0 + j < t.rows) *y = from_f32<T>(o[j]);
             }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -401,7 +409,7 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
                 T* y = (T*)p.y + (long long)row * p.ldy + chan;
 #pragma unroll
                 for (int j = 0; j < 4; j++)
-                    if (chan + j < p.N) y[j] = scaled(sum[j], sa, p.w_scale[gc + j], p.bias ? p.bias[gc + j] : 0.f);
+                    if (chan + j < p.N) y[j] = from_f32<T>(scaled(sum[j], sa, p.w_scale[gc + j], p.bias ? p.bias[gc + j] : 0.f));
             }
             // what the generic proxy read and wrote here, the next tile's loads will overwrite
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -472,6 +480,7 @@ template <typename T, int TN, int CG> cudaError_t tiles_launch(const MatmulParam
     p.n_tiles = (int)((q.N + CH * CG - 1) / (CH * CG));
     p.splits = splits;
     p.dependent = q.dependent;
+    p.pairs = (uintptr_t)q.y % 4 == 0 && q.ldy % 2 == 0;
     cudaError_t e;
     if (q.K) {
         if ((e = make_map(&p.a, q.a, q.M, q.K, q.lda, S::BOX)) != cudaSuccess) return e;

@@ -77,7 +77,7 @@ template <typename T> cudaError_t quant_launch(const QuantParams& in, cudaStream
     p.vec_q = (uintptr_t)p.q % 8 == 0 && p.ldq % 8 == 0;
     int threads = 32;  // two pieces to a thread, up to 512 threads; then eight
     while (threads < 512 && threads * N * 2 < p.K) threads *= 2;
-    const int blocks = (int)std::min<long long>(p.M, (long long)SMS * (2048 / threads));
+    const int blocks = (int)std::min<long long>(p.M, 1 << 30);  // one for each row: the hardware hands out the next one where one has ended
     if (p.K <= 512 * N * 2) hccl_quantise_rows<T, 2><<<blocks, threads, 0, s>>>(p);
     else hccl_quantise_rows<T, 8><<<blocks, threads, 0, s>>>(p);
     return cudaGetLastError();

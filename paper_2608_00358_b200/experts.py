@@ -186,11 +186,7 @@ class Router:
         if routing.tokens != logits.shape[0]:
             _refuse(hb.ERR_COUNT_MISMATCH, "route backward: routing of %d tokens" % routing.tokens)
         _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, dev)
-        if out is None:
-            out = logits.new_empty(logits.shape)
-        else:
-            _same_type(out, logits, "route backward")
-        ldd = _matrix(out, "dlogits", self.experts, routing.tokens, dev)
+        out, ldd = _new(out, routing.tokens, self.experts, logits, "dlogits", dev)
         _on(dev, hb.hccl_route_backward, self._ref, logits.data_ptr(), ld, dt, b, m, routing.ref, dweights.data_ptr(), out.data_ptr(), ldd)
         return out
 
@@ -209,11 +205,12 @@ class _Route(torch.autograd.Function):
         return ctx.router.backward(logits, ctx.routing, dweights.contiguous(), bias, token_mask), None, None, None, None
 
 
-def _new(out, shape, like, what):
+def _new(out, rows, cols, like, what, dev):
+    """The output and the distance between its rows: memory of `like`'s type, or the caller's after a check."""
     if out is None:
-        return like.new_empty(shape)
+        return like.new_empty((rows, cols)), cols
     _same_type(out, like, what)
-    return out
+    return out, _matrix(out, what, cols, rows, dev)
 
 
 def _weights(weights, routing) -> int:
@@ -227,8 +224,9 @@ def _dispatch(x, routing, out, n_rows):
     dev = routing.dev
     ldx, dt = _matrix(x, "x", None, routing.tokens, dev), _dtype(x, "x")
     H = x.shape[1]
-    out = _new(out, (routing.tokens * routing.top_k if n_rows is None else n_rows, H), x, "dispatch")
-    ldr = _matrix(out, "rows", H, n_rows, dev)
+    if out is None and n_rows is None:
+        n_rows = routing.tokens * routing.top_k
+    out, ldr = _new(out, n_rows, H, x, "rows", dev)
     _on(dev, hb.hccl_dispatch, x.data_ptr(), ldx, H, dt, routing.ref, out.data_ptr(), ldr, out.shape[0])
     return out
 
@@ -247,8 +245,7 @@ def dispatch_backward(drows: torch.Tensor, routing: Routing, out: Optional[torch
     dev = routing.dev
     ldr, dt = _matrix(drows, "drows", None, None, dev), _dtype(drows, "drows")
     n, H = drows.shape
-    out = _new(out, (routing.tokens, H), drows, "dispatch backward")
-    ldx = _matrix(out, "dx", H, routing.tokens, dev)
+    out, ldx = _new(out, routing.tokens, H, drows, "dx", dev)
     _on(dev, hb.hccl_dispatch_backward, drows.data_ptr(), ldr, n, H, dt, routing.ref, out.data_ptr(), ldx)
     return out
 
@@ -258,8 +255,7 @@ def _combine(rows, routing, weights, out):
     ldr, dt = _matrix(rows, "rows", None, None, dev), _dtype(rows, "rows")
     w = _weights(weights, routing)
     n, H = rows.shape
-    out = _new(out, (routing.tokens, H), rows, "combine")
-    ldy = _matrix(out, "y", H, routing.tokens, dev)
+    out, ldy = _new(out, routing.tokens, H, rows, "y", dev)
     _on(dev, hb.hccl_combine, rows.data_ptr(), ldr, n, H, dt, routing.ref, w, out.data_ptr(), ldy)
     return out
 
@@ -282,8 +278,7 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, routing: Routing, wei
     ldy = _matrix(dy, "dy", H, routing.tokens, dev)
     _same_type(dy, rows, "combine backward")
     w = _weights(weights, routing)
-    out = _new(out, (n, H), rows, "combine backward")
-    ldd = _matrix(out, "drows", H, n, dev)
+    out, ldd = _new(out, n, H, rows, "drows", dev)
     dw = routing.weights.new_empty((routing.tokens, routing.top_k))
     _on(dev, hb.hccl_combine_backward, dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.ref, w, out.data_ptr(), ldd, dw.data_ptr())
     return out, dw

@@ -127,6 +127,15 @@ __device__ __forceinline__ int4 cluster_load(uint32_t addr, uint32_t rank) {
     return v;
 }
 
+// The same value as (float)v, one rounding to nearest even, by way of its halves: 2^23 + h is a number whose low bits are the 16-bit h, so both
+// halves become exact floating-point numbers by a byte permutation and a subtraction, and one fused multiply-add joins and rounds them.
+// The conversion instruction runs at an eighth of the rate of these six; results take turns between the two.
+__device__ __forceinline__ float by_halves(int v) {
+    const unsigned up = (unsigned)v ^ 0x80000000u;  // high half + 2^15
+    const float hi = __fadd_rn(__uint_as_float(__byte_perm(up, 0x4b000000u, 0x7632)), -8421376.f), lo = __fadd_rn(__uint_as_float(__byte_perm(up, 0x4b000000u, 0x7610)), -8388608.f);
+    return __fmaf_rn(hi, 65536.f, lo);
+}
+
 // ---------------------------------------------------------------- tiles
 struct Tile {
     int group, row, rows, chan;  // rows [row, row + rows) of the tokens, this block's channels from chan on
@@ -214,8 +223,9 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
+    if (CG == 2) cluster_sync();  // both blocks' barriers exist before either uses the other's
     // The weights do not hang on the kernel before, nor on the other warps: they are asked for at once.
-    if (warp == 0 && !p.groups && CG == 1) prefetch(tile_of<TN, CG>(p, before, first, pair_rank, &hint));
+    if (warp == 0 && !p.groups) prefetch(tile_of<TN, CG>(p, before, first, pair_rank, &hint));
     if (warp == 2) {
         if constexpr (CG == 2) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::COLS));
@@ -245,7 +255,6 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (CG == 2) cluster_sync();  // both blocks' barriers exist before either uses the other's
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
     const int tiles = p.n_tiles * (p.groups ? before[p.groups] : (p.M + TN - 1) / TN);
@@ -290,9 +299,9 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
             __syncwarp();
         }
     };
-    const auto scaled = [&](int sum, float sa, float sw, float bias) {
-        // a sum passes 2^24 from K = 1024 on: its conversion to 32-bit floating point is a rounding, like each scale's product
-        const float v = __fmul_rn(__fmul_rn((float)sum, sa), sw);
+    // A sum passes 2^24 from K = 1024 on: its conversion to 32-bit floating point is a rounding, like each scale's product.
+    const auto scaled = [&](float sum, float sa, float sw, float bias) {
+        const float v = __fmul_rn(__fmul_rn(sum, sa), sw);
         return p.bias ? __fadd_rn(v, bias) : v;
     };
     const auto results = [&](const Tile& t) {
@@ -329,7 +338,7 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
             }
             float o[C];  // all of them before the first store: a branch for each would leave its chain of latencies bare
 #pragma unroll
-            for (int j = 0; j < C; j++) o[j] = scaled(v[j], __shfl_sync(0xffffffffu, sa[u], j), sw, bias);
+            for (int j = 0; j < C; j++) o[j] = scaled(j & 1 ? by_halves(v[j]) : (float)v[j], __shfl_sync(0xffffffffu, sa[u], j), sw, bias);
             T* y = (T*)p.y + (long long)(t.row + c0) * p.ldy + chan;
             if (sizeof(T) == 2 && p.pairs && c0 + C <= t.rows && t.chan + quarter * 32 + 32 <= p.N) {
                 // Two neighbouring lanes trade: the even one keeps row j of both channels, the odd one row j + 1, four bytes each, so that a store
@@ -409,7 +418,7 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
                 T* y = (T*)p.y + (long long)row * p.ldy + chan;
 #pragma unroll
                 for (int j = 0; j < 4; j++)
-                    if (chan + j < p.N) y[j] = from_f32<T>(scaled(sum[j], sa, p.w_scale[gc + j], p.bias ? p.bias[gc + j] : 0.f));
+                    if (chan + j < p.N) y[j] = from_f32<T>(scaled((float)sum[j], sa, p.w_scale[gc + j], p.bias ? p.bias[gc + j] : 0.f));
             }
             // what the generic proxy read and wrote here, the next tile's loads will overwrite
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

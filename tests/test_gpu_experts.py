@@ -585,3 +585,20 @@ def test_refusals_of_the_python_layer():
     refused(ali, lambda: lin.matmul(torch.zeros(4, 40, dtype=torch.int8, device="cuda")[:, :32], torch.ones(4, device="cuda")))
     refused(dty, lambda: ex.Int8Linear(x, torch.ones(4, device="cuda")))
     refused(mism, lambda: ex.Int8Linear(torch.zeros(4, 32, dtype=torch.int8, device="cuda"), torch.ones(5, device="cuda")))
+
+
+@pytest.mark.parametrize("M,K,dt,pad", [(4200, 4096, BF16, 0), (2100, 8192, F16, 8), (1100, 8192, F32, 4), (2100, 8184, BF16, 0), (1030, 16384, BF16, 0)])
+def test_many_long_rows_quantise_alike(M, K, dt, pad):
+    """Sizes that stream through shared memory: against the definition on a sample of rows, against the rows one by one on all."""
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(K)).to(dt)
+    x[5] = 0
+    x[M - 2, K - 1] = float("nan")
+    x[M - 1, K - 1] = 900.0  # the last row's scale hangs on its last element
+    xd = strided(x, pad)
+    q, s = ex.quantize_rows(xd)
+    pick = torch.cat([torch.arange(0, M, 97), torch.tensor([5, M - 2, M - 1])])
+    wq, ws = ref.quantise(x[pick].float().numpy())
+    assert np.array_equal(q[pick.cuda()].cpu().numpy(), wq) and np.array_equal(s[pick.cuda()].cpu().numpy(), ws, equal_nan=True)
+    for a in range(0, M, 500):  # few rows take the other way
+        q1, s1 = ex.quantize_rows(xd[a: a + 500])
+        assert torch.equal(q1, q[a: a + 500]) and torch.equal(s1.view(torch.int32), s[a: a + 500].view(torch.int32))

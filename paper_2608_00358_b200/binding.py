@@ -7,6 +7,7 @@ work, as do raw integers). Importing this module fails loudly if the library can
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional, Sequence
 
 from . import _build
@@ -153,6 +154,8 @@ def _load() -> C.CDLL:
     lib.hccl_last_cuda_error.restype = C.c_char_p
     lib.hccl_version.argtypes = []
     lib.hccl_version.restype = C.c_int
+    lib.hccl_call_packed.argtypes = [C.c_int, C.c_char_p]
+    lib.hccl_call_packed.restype = C.c_int
     lib.hccl_opts_for_overlap.argtypes = [C.POINTER(Opts)]
     lib.hccl_opts_for_overlap.restype = None
     return lib
@@ -370,6 +373,20 @@ hccl_combine_backward = _call("hccl_combine_backward")
 hccl_quantize_rows_i8 = _call("hccl_quantize_rows_i8")
 hccl_matmul_i8 = _call("hccl_matmul_i8")
 hccl_linear_i8 = _call("hccl_linear_i8")
+
+
+def packed(name: str):
+    """The same call for code that makes it often: all arguments integers (structures by address, NULL 0; of the products the fields of
+    hccl_matmul_i8_t one by one), handed over as one array."""
+    which, n = {"hccl_route": (0, 10), "hccl_route_backward": (1, 11), "hccl_dispatch": (2, 9), "hccl_dispatch_backward": (3, 9), "hccl_combine": (4, 10),
+                "hccl_combine_backward": (5, 13), "hccl_quantize_rows_i8": (6, 11), "hccl_matmul_i8": (7, 17), "hccl_linear_i8": (8, 21)}[name]
+    fn, pack = _lib.hccl_call_packed, struct.Struct("%dq" % n).pack
+
+    def call(*args):
+        rc = fn(which, pack(*args))
+        if rc:
+            raise HcclError(rc, name)
+    return call
 
 
 def hccl_route_workspace_bytes(router: RouterConfig, tokens: int) -> int:

@@ -15,7 +15,7 @@ from typing import List
 import torch
 
 from . import binding as hb
-from .experts import Int8Linear, Router, Routing, _pad16, combine
+from .experts import Int8Linear, Router, Routing, _pad16, _quantize, combine
 from .runtime import DeviceCollective
 
 
@@ -59,7 +59,7 @@ class ExpertParallel:
         stream = torch.cuda.current_stream()
         for r in range(self.R):
             self.router.route(logits[r], out=self.routing[r])
-            hb.hccl_quantize_rows_i8(x[r].data_ptr(), x[r].stride(0), self.tokens, self.hidden, _type(x[r]), self.routing[r].ref, self.send[r].data_ptr(), self.row,
+            _quantize(x[r].data_ptr(), x[r].stride(0), self.tokens, self.hidden, _type(x[r]), self.routing[r].at, self.send[r].data_ptr(), self.row,
                                      self.send_rows, self.scale.data_ptr(), stream.cuda_stream)
             self.send[r][:, self.at: self.at + 4] = self.scale[: self.send_rows].view(torch.int8).view(-1, 4)
         self._out.execute(stream)

@@ -21,6 +21,10 @@ import torch
 
 from . import binding as hb
 
+_route, _route_backward = hb.packed("hccl_route"), hb.packed("hccl_route_backward")
+_c_dispatch, _c_dispatch_backward = hb.packed("hccl_dispatch"), hb.packed("hccl_dispatch_backward")
+_c_combine, _c_combine_backward = hb.packed("hccl_combine"), hb.packed("hccl_combine_backward")
+_quantize, _matmul, _linear = hb.packed("hccl_quantize_rows_i8"), hb.packed("hccl_matmul_i8"), hb.packed("hccl_linear_i8")
 _DT = {torch.float32: hb.FP32, torch.bfloat16: hb.BF16, torch.float16: hb.FP16}
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
@@ -98,7 +102,7 @@ class Routing:
     """Which token goes to which expert (hccl_routing_t), as tensors: ids, weights, slots [tokens, top_k]; counts [experts];
     offsets [experts + 1]; source [tokens * top_k]. Rows of expert e, in expert order, are offsets[e]:offsets[e + 1]."""
 
-    __slots__ = ("ids", "weights", "counts", "offsets", "slots", "source", "tokens", "top_k", "experts", "device", "dev", "record", "ref")
+    __slots__ = ("ids", "weights", "counts", "offsets", "slots", "source", "tokens", "top_k", "experts", "device", "dev", "record", "at")
 
     def __init__(self, ids, weights, counts, offsets, slots, source):
         if ids.dim() != 2 or not ids.is_cuda:
@@ -113,7 +117,7 @@ class Routing:
         self.ids, self.weights, self.counts, self.offsets, self.slots, self.source = ids, weights, counts, offsets, slots, source
         self.record = hb.RoutingRecord(self.tokens, self.top_k, self.experts, ids.data_ptr(), weights.data_ptr(), counts.data_ptr(),
                                        offsets.data_ptr(), slots.data_ptr(), source.data_ptr())
-        self.ref = C.byref(self.record)
+        self.at = C.addressof(self.record)
 
 
 class Router:
@@ -128,7 +132,7 @@ class Router:
                                       1 if renormalise else 0, scale)
         hb.hccl_route_workspace_bytes(self.config, 0)  # refuses a configuration that does not hold together
         self.experts, self.top_k = experts, top_k
-        self._ref = C.byref(self.config)
+        self._at = C.addressof(self.config)
         self._scratch = _Scratch()
         self._need = {}  # workspace bytes by number of tokens
 
@@ -142,7 +146,7 @@ class Router:
     def _inputs(self, logits, bias, token_mask, dev):
         ld = _matrix(logits, "logits", self.experts, None, dev)
         dt = _dtype(logits, "logits")
-        b = m = None
+        b = m = 0
         if bias is not None:
             _vector(bias, "bias", torch.float32, self.experts, logits.get_device())
             b = bias.data_ptr()
@@ -161,7 +165,7 @@ class Router:
         need = self._need.get(tokens)
         if need is None:
             need = self._need[tokens] = hb.hccl_route_workspace_bytes(self.config, tokens)
-        _on(dev, hb.hccl_route, self._ref, logits.data_ptr(), ld, dt, b, m, out.ref, self._scratch.get(dev, need), need)
+        _on(dev, _route, self._at, logits.data_ptr(), ld, dt, b, m, out.at, self._scratch.get(dev, need), need)
 
     def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, token_mask: Optional[torch.Tensor] = None,
               out: Optional[Routing] = None) -> Routing:
@@ -187,7 +191,7 @@ class Router:
             _refuse(hb.ERR_COUNT_MISMATCH, "route backward: routing of %d tokens" % routing.tokens)
         _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, dev)
         out, ldd = _new(out, routing.tokens, self.experts, logits, "dlogits", dev)
-        _on(dev, hb.hccl_route_backward, self._ref, logits.data_ptr(), ld, dt, b, m, routing.ref, dweights.data_ptr(), out.data_ptr(), ldd)
+        _on(dev, _route_backward, self._at, logits.data_ptr(), ld, dt, b, m, routing.at, dweights.data_ptr(), out.data_ptr(), ldd)
         return out
 
 
@@ -227,7 +231,7 @@ def _dispatch(x, routing, out, n_rows):
     if out is None and n_rows is None:
         n_rows = routing.tokens * routing.top_k
     out, ldr = _new(out, n_rows, H, x, "rows", dev)
-    _on(dev, hb.hccl_dispatch, x.data_ptr(), ldx, H, dt, routing.ref, out.data_ptr(), ldr, out.shape[0])
+    _on(dev, _c_dispatch, x.data_ptr(), ldx, H, dt, routing.at, out.data_ptr(), ldr, out.shape[0])
     return out
 
 
@@ -246,7 +250,7 @@ def dispatch_backward(drows: torch.Tensor, routing: Routing, out: Optional[torch
     ldr, dt = _matrix(drows, "drows", None, None, dev), _dtype(drows, "drows")
     n, H = drows.shape
     out, ldx = _new(out, routing.tokens, H, drows, "dx", dev)
-    _on(dev, hb.hccl_dispatch_backward, drows.data_ptr(), ldr, n, H, dt, routing.ref, out.data_ptr(), ldx)
+    _on(dev, _c_dispatch_backward, drows.data_ptr(), ldr, n, H, dt, routing.at, out.data_ptr(), ldx)
     return out
 
 
@@ -256,7 +260,7 @@ def _combine(rows, routing, weights, out):
     w = _weights(weights, routing)
     n, H = rows.shape
     out, ldy = _new(out, routing.tokens, H, rows, "y", dev)
-    _on(dev, hb.hccl_combine, rows.data_ptr(), ldr, n, H, dt, routing.ref, w, out.data_ptr(), ldy)
+    _on(dev, _c_combine, rows.data_ptr(), ldr, n, H, dt, routing.at, w, out.data_ptr(), ldy)
     return out
 
 
@@ -280,7 +284,7 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, routing: Routing, wei
     w = _weights(weights, routing)
     out, ldd = _new(out, n, H, rows, "drows", dev)
     dw = routing.weights.new_empty((routing.tokens, routing.top_k))
-    _on(dev, hb.hccl_combine_backward, dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.ref, w, out.data_ptr(), ldd, dw.data_ptr())
+    _on(dev, _c_combine_backward, dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.at, w, out.data_ptr(), ldd, dw.data_ptr())
     return out, dw
 
 
@@ -326,7 +330,7 @@ def quantize_rows(x: torch.Tensor, routing: Optional[Routing] = None, n_rows: Op
     n = M if routing is None else (routing.tokens * routing.top_k if n_rows is None else n_rows)
     q = torch.empty((n, _pad16(K)), dtype=torch.int8, device=x.device)
     scale = torch.empty(n, dtype=torch.float32, device=x.device)
-    _on(dev, hb.hccl_quantize_rows_i8, x.data_ptr(), ldx, M, K, dt, routing.ref if routing is not None else None, q.data_ptr(), q.shape[1], n, scale.data_ptr())
+    _on(dev, _quantize, x.data_ptr(), ldx, M, K, dt, routing.at if routing is not None else 0, q.data_ptr(), q.shape[1], n, scale.data_ptr())
     return q[:, :K], scale
 
 
@@ -355,7 +359,7 @@ class Int8Linear:
         self.ldw = weight.shape[-1]
         self._scratch = _Scratch()
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self._fixed = (weight.data_ptr(), self.ldw, scale.data_ptr(), bias.data_ptr() if bias is not None else None)
+        self._fixed = (weight.data_ptr(), self.ldw, scale.data_ptr(), bias.data_ptr() if bias is not None else 0)
         self._status_at = self._status.data_ptr()
 
     @classmethod
@@ -369,7 +373,7 @@ class Int8Linear:
         if offsets is not None:
             _vector(offsets, "offsets", torch.int32, self.experts + 1, self.dev)
             offsets = offsets.data_ptr()
-        return C.byref(hb.MatmulI8(M, self.N, self.K, self.experts, dt, a, lda, a_scale, w, ldw, w_scale, bias, offsets, y, ldy, self._status_at))
+        return M, self.N, self.K, self.experts, dt, a, lda, a_scale, w, ldw, w_scale, bias, offsets or 0, y, ldy, self._status_at
 
     def _out(self, out, M, dtype):
         """The result, its row distance and its type."""
@@ -394,16 +398,16 @@ class Int8Linear:
         dev, K = self.dev, self.K
         ldx, dt = _matrix(x, "x", K, None, dev), _dtype(x, "x")
         self._which(routing, offsets)
-        M, ref = x.shape[0], None
+        M, record = x.shape[0], 0
         if routing is not None:
             if M != routing.tokens:
                 _refuse(hb.ERR_COUNT_MISMATCH, "Int8Linear: %d tokens, the routing has %d" % (M, routing.tokens))
-            M, ref, offsets = M * routing.top_k, routing.ref, routing.offsets
+            M, record, offsets = M * routing.top_k, routing.at, routing.offsets
         y, ldy, y_dt = self._out(out, M, x.dtype)
         lda = _pad16(K)
         room = M * lda
         at = self._scratch.get(dev, room + 4 * M)
-        _on(dev, hb.hccl_linear_i8, self._args(M, at, lda, at + room, y_dt, y.data_ptr(), ldy, offsets), x.data_ptr(), ldx, dt, ref)
+        _on(dev, _linear, *self._args(M, at, lda, at + room, y_dt, y.data_ptr(), ldy, offsets), x.data_ptr(), ldx, dt, record)
         return y
 
     def matmul(self, q: torch.Tensor, q_scale: torch.Tensor, offsets: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -416,7 +420,7 @@ class Int8Linear:
         _vector(q_scale, "q_scale", torch.float32, M, self.dev)
         self._which(None, offsets)
         y, ldy, y_dt = self._out(out, M, dtype)
-        _on(self.dev, hb.hccl_matmul_i8, self._args(M, q.data_ptr(), lda if M > 1 else _pad16(lda), q_scale.data_ptr(), y_dt, y.data_ptr(), ldy, offsets))
+        _on(self.dev, _matmul, *self._args(M, q.data_ptr(), lda if M > 1 else _pad16(lda), q_scale.data_ptr(), y_dt, y.data_ptr(), ldy, offsets))
         return y
 
     def check(self):

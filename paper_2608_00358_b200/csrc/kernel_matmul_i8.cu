@@ -14,6 +14,8 @@
 // too few tiles for the SMs, a cluster of blocks shares a tile's K and adds its partial sums through distributed shared memory.
 #include <cuda.h>
 
+#include <atomic>
+
 #include "experts.cuh"
 
 namespace hccl {
@@ -495,7 +497,7 @@ template <typename T, int TN, int CG> cudaError_t tiles_launch(const MatmulParam
         if ((e = make_map(&p.a, q.a, q.M, q.K, q.lda, S::BOX)) != cudaSuccess) return e;
         if ((e = make_map(&p.w, q.w, q.N * (q.groups ? q.groups : 1), q.K, q.ldw, CH)) != cudaSuccess) return e;
     }
-    static bool ready[64];  // by device; setting it twice does no harm
+    static std::atomic<bool> ready[64];  // by device; setting it twice does no harm
     int dev = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     if (dev >= 64 || !ready[dev]) {

@@ -2,6 +2,7 @@
 // is written to every place that the token was sent to, so it is read and quantised once. Memory is the bound: a block
 // holds its row in registers between the maximum and the rounding, so every element is read once.
 #include <algorithm>
+#include <atomic>
 
 #include "rows_i8.cuh"
 
@@ -147,7 +148,7 @@ template <typename T> cudaError_t ring_launch(const QuantParams& p, cudaStream_t
     int team = 32;
     while (team * HELD * 16 < bytes) team *= 2;
     const int threads = team == 256 ? 256 : 128, smem = threads * RING * HELD * 16;
-    static bool ready[64];
+    static std::atomic<bool> ready[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;

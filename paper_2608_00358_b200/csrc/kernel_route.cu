@@ -9,6 +9,7 @@
 // Keys are good to a few 2^-24 (__expf and an approximate reciprocal); the weights of the chosen are formed anew with
 // expf and a rounded division.
 #include <algorithm>
+#include <atomic>
 
 #include "experts.cuh"
 
@@ -666,7 +667,7 @@ Cut cut(long long tokens, int E) {
 }
 
 // Opt-in to large shared memory, once for each kernel and device.
-template <typename K> cudaError_t allow(K* kernel, size_t bytes, bool (&ready)[64]) {
+template <typename K> cudaError_t allow(K* kernel, size_t bytes, std::atomic<bool> (&ready)[64]) {
     if (bytes <= 48 * 1024) return cudaSuccess;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -680,7 +681,7 @@ template <typename T, int Q, int L, bool ONE> cudaError_t choose_launch(const Ro
     size_t ints = (size_t)p.warps * (32 / L) * token_floats(p);
     if (ONE) ints = std::max(ints, (size_t)p.warps * p.E) + round_up((int)p.tokens * p.K, 4);
     const size_t smem = (2 * round_up(p.E, 16) + ints) * 4;
-    static bool ready[64];
+    static std::atomic<bool> ready[64];
     const cudaError_t e = allow(hccl_route_choose<T, Q, L, ONE>, smem, ready);
     if (e != cudaSuccess) return e;
     hccl_route_choose<T, Q, L, ONE><<<p.chunks, 32 * p.warps, smem, s>>>(p);
@@ -692,7 +693,7 @@ template <typename T, int Q, int L> cudaError_t route_launch(const RouteParams& 
     if (p.chunks == 1) return choose_launch<T, Q, L, true>(p, s);
     cudaError_t e = choose_launch<T, Q, L, false>(p, s);
     if (e != cudaSuccess) return e;
-    static bool ready2[64];
+    static std::atomic<bool> ready2[64];
     cudaLaunchConfig_t cfg = {};
     cfg.dynamicSmemBytes = (size_t)(2 * E16 + std::max(LAYOUT_THREADS / 32 * p.E, layout_lines(p.E) * E16)) * 4;
     if ((e = allow(hccl_route_layout, cfg.dynamicSmemBytes, ready2)) != cudaSuccess) return e;

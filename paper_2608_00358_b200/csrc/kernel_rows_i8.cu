@@ -7,6 +7,7 @@
 // columns of K in another order than they have in memory, the same for both operands, and a sum does not mind. Four such items (8 KB) are in flight for
 // each warp, across the end of a group of channels. The 8 warps of a block share K and add their sums, exact integers, in shared memory.
 #include <algorithm>
+#include <atomic>
 
 #include "rows_i8.cuh"
 
@@ -180,7 +181,7 @@ template <typename T> cudaError_t few_launch(const FewParams& in, cudaStream_t s
     p.q_stride = few_stride(p.m.K);
     const size_t smem = (size_t)p.m.M * p.q_stride;
     if (smem > 40 * 1024) {
-        static bool ready[64];
+        static std::atomic<bool> ready[64];
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;

@@ -27,6 +27,7 @@ _c_combine, _c_combine_backward = hb.packed("hccl_combine"), hb.packed("hccl_com
 _quantize, _matmul, _linear = hb.packed("hccl_quantize_rows_i8"), hb.packed("hccl_matmul_i8"), hb.packed("hccl_linear_i8")
 _DT = {torch.float32: hb.FP32, torch.bfloat16: hb.BF16, torch.float16: hb.FP16}
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_capturing = torch._C._cuda_isCurrentStreamCapturing if hasattr(torch._C, "_cuda_isCurrentStreamCapturing") else torch.cuda.is_current_stream_capturing
 _stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -83,19 +84,23 @@ def _on(dev: int, call, *args):
 
 
 class _Scratch:
-    """Device memory of one object, one piece for each stream it is used on: calls on different streams do not share it."""
+    """Device memory of one object, one piece for each stream it is used on: calls on different streams do not share it. A call that is captured
+    into a CUDA graph gets memory of the graph's own, since the graph may be replayed on any stream, beside later calls."""
 
     def __init__(self):
         self._of = {}
 
-    def get(self, dev: int, nbytes: int) -> int:
-        """Address of at least nbytes on device number `dev`."""
+    def get(self, dev: int, nbytes: int):
+        """(tensor, address) of at least nbytes on device number `dev`; hold the tensor until the call is made."""
+        if _capturing():
+            t = torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % dev)
+            return t, t.data_ptr()
         key = (dev, _stream(dev))
         have = self._of.get(key)
-        if have is None or have[1] < nbytes:
+        if have is None or have[2] < nbytes:
             t = torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % dev)
-            have = self._of[key] = (t, nbytes, t.data_ptr())
-        return have[2]
+            have = self._of[key] = (t, t.data_ptr(), nbytes)
+        return have[:2]
 
 
 class Routing:
@@ -165,7 +170,8 @@ class Router:
         need = self._need.get(tokens)
         if need is None:
             need = self._need[tokens] = hb.hccl_route_workspace_bytes(self.config, tokens)
-        _on(dev, _route, self._at, logits.data_ptr(), ld, dt, b, m, out.at, self._scratch.get(dev, need), need)
+        hold, ws = self._scratch.get(dev, need)
+        _on(dev, _route, self._at, logits.data_ptr(), ld, dt, b, m, out.at, ws, need)
 
     def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, token_mask: Optional[torch.Tensor] = None,
               out: Optional[Routing] = None) -> Routing:
@@ -406,7 +412,7 @@ class Int8Linear:
         y, ldy, y_dt = self._out(out, M, x.dtype)
         lda = _pad16(K)
         room = M * lda
-        at = self._scratch.get(dev, room + 4 * M)
+        hold, at = self._scratch.get(dev, room + 4 * M)
         _on(dev, _linear, *self._args(M, at, lda, at + room, y_dt, y.data_ptr(), ldy, offsets), x.data_ptr(), ldx, dt, record)
         return y
 

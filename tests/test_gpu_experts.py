@@ -602,3 +602,25 @@ def test_many_long_rows_quantise_alike(M, K, dt, pad):
     for a in range(0, M, 500):  # few rows take the other way
         q1, s1 = ex.quantize_rows(xd[a: a + 500])
         assert torch.equal(q1, q[a: a + 500]) and torch.equal(s1.view(torch.int32), s[a: a + 500].view(torch.int32))
+
+
+def test_calls_captured_on_a_stream_do_not_share_scratch_with_calls_made_on_it():
+    g = torch.Generator(device="cuda").manual_seed(4)
+    lin = ex.Int8Linear.from_float(torch.randn(256, 512, generator=g, device="cuda"))
+    a, b = (torch.randn(64, 512, generator=g, device="cuda") for _ in range(2))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        want_a, want_b = lin(a), lin(b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        ya = lin(a)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    for _ in range(20):  # the graph on one stream, plain calls on the stream it was captured on
+        with torch.cuda.stream(other):
+            graph.replay()
+        with torch.cuda.stream(s):
+            yb = lin(b)
+    torch.cuda.synchronize()
+    assert torch.equal(ya, want_a) and torch.equal(yb, want_b)

@@ -4,7 +4,10 @@
 // The choice. L lanes share a token (8: four tokens to a warp; 32: one). Experts go to lanes in quads: quad q = experts 4q .. 4q + 3 belongs to
 // lane q % L, as its quad q / L. Keys lie in shared memory and the largest key of each quad in a register, so a round of
 // the top k costs a maximum over the lane's quads, one over the lanes, and a second look at one quad. Not eligible: -inf. What bounds it is
-// the number of instructions: a token of 256 experts is 512 bytes of input and some 270 instructions of a warp.
+// the number of instructions and, for few tokens, their chain: a token of 256 experts is 512 bytes of input and some 500 instructions of a warp.
+//
+// Measured (B200): 16384 x 256 bf16, sigmoid, 8 groups, top 8: 16 us choosing and 8 of layout behind it; softmax without groups 10 and 9; 32768 x 128 21 us in all; one token of 256
+// 6 us, 61 x 60 5.4 us, in one launch; the gradient of 32768 x 128 6.3 us = 3.0 TB/s.
 //
 // Keys are good to a few 2^-24 (__expf and an approximate reciprocal); the weights of the chosen are formed anew with
 // expf and a rounded division.
@@ -410,7 +413,7 @@ __device__ __forceinline__ int offsets_of(const RouteParams& p, const int* tot, 
 
 // A block chooses for one chunk of tokens and leaves its counts for the layout; a single block (ONE) goes on to the layout itself.
 template <typename T, int Q, int L, bool ONE>
-__global__ void __launch_bounds__(32 * (ONE ? ONE_BLOCK_WARPS : MANY_WARPS), ONE ? 1 : 3) hccl_route_choose(const __grid_constant__ RouteParams p) {
+__global__ void __launch_bounds__(32 * (ONE ? ONE_BLOCK_WARPS : MANY_WARPS), ONE ? 1 : Q <= 4 ? 4 : 3) hccl_route_choose(const __grid_constant__ RouteParams p) {
     extern __shared__ __align__(16) int sm[];  // hist[E16] bias[E16], a single block's ids, then the tokens' keys; a single block: its layout's counts in their place
     __shared__ int scratch[32];
     const int E16 = round_up(p.E, 16), threads = 32 * p.warps, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -640,8 +643,9 @@ __global__ void __launch_bounds__(256) hccl_route_grad(const __grid_constant__ R
 }
 
 // ---------------------------------------------------------------- host
-// Lanes for a token: 32 while each can have a warp of the one block, or where 8 lanes would hold more than 8 quads each.
-int lanes_for(long long tokens, int E) { return (tokens <= ONE_BLOCK_WARPS || E > 256) ? 32 : 8; }
+// Lanes for a token. 8 do the least work in all (16384 x 256: 25 us against 36 with 32; 32 x 64: 4.5 against 5.8), 32 have the shorter chain of latencies where keys are many for each lane and
+// tokens do not fill the SMs (1024 x 256: 10.0 us against 11.7, 64 x 256: 8.9 against 10.2, one token of 64: 3.7 against 4.2); beyond 256 experts 8 lanes would hold more than 8 quads each.
+int lanes_for(long long tokens, int E) { return (tokens <= ONE_BLOCK_WARPS || E > 256 || (E > 128 && tokens <= 1024)) ? 32 : 8; }
 bool one_block(long long tokens, int lanes) { return tokens <= ONE_BLOCK_WARPS * (32 / lanes) * 2; }
 
 struct Cut {

@@ -6,6 +6,9 @@
 // the instruction: of each half, lane 4g + t loads bytes 16t .. 16t + 15 of channels g and g + 8, two instructions' worth. That hands the instruction its
 // columns of K in another order than they have in memory, the same for both operands, and a sum does not mind. Four such items (8 KB) are in flight for
 // each warp, across the end of a group of channels. The 8 warps of a block share K and add their sums, exact integers, in shared memory.
+//
+// Measured (B200, weights not in the L2): one row, 8192 x 4096 9 us with the quantising = 3.7 TB/s (the tiles: 12.6), 16384 x 8192 25 us = 5.2 TB/s; 8 rows, 8192 x 4096 10.5 us
+// (the tiles: 11.4 for 16).
 #include <algorithm>
 #include <atomic>
 

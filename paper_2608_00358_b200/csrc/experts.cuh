@@ -94,6 +94,7 @@ struct RouteParams {
     int E, K, groups, per_group, top_groups, group_best, sigmoid, renorm;
     float scale;
     int per4, magic;     // quads of experts lie in one group each; e * magic >> 20 = e / per_group
+    int segment;         // quads of a group, if they are 1, 2, 4, .. lanes side by side; 0 otherwise
     int vec;             // rows of logits can be read four elements at once
     int warps;           // per block
     int chunk, chunks;   // tokens counted together; chunks of them (1: a single block does everything)

@@ -7,7 +7,7 @@
 // the number of instructions and, for few tokens, their chain: a token of 256 experts is 512 bytes of input and some 500 instructions of a warp.
 //
 // Measured (B200): 16384 x 256 bf16, sigmoid, 8 groups, top 8: 16 us choosing and 8 of layout behind it; softmax without groups 10 and 9; 32768 x 128 21 us in all; one token of 256
-// 6 us, 61 x 60 5.4 us, in one launch; the gradient of 32768 x 128 6.3 us = 3.0 TB/s.
+// 5.7 us, 61 x 60 5.4 us, in one launch; the gradient of 32768 x 128 6.3 us = 3.0 TB/s.
 //
 // Keys are good to a few 2^-24 (__expf and an approximate reciprocal); the weights of the chosen are formed anew with
 // expf and a rounded division.
@@ -185,44 +185,62 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
 #pragma unroll
     for (int i = 0; i < Q; i++) top[i] = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
     if (p.groups > 1) {
-        __syncwarp();
-        for (int g = l; g < p.groups; g += L) {
-            float k1 = -INFINITY, k2 = -INFINITY, o1 = -INFINITY, o2 = -INFINITY;  // the two largest, of two halves: two chains of latencies side by side
-            const auto seen = [&](float v) {
-                k2 = fmaxf(k2, fminf(k1, v));
-                k1 = fmaxf(k1, v);
-            };
-            const auto seen_too = [&](float v) {
-                o2 = fmaxf(o2, fminf(o1, v));
-                o1 = fmaxf(o1, v);
-            };
-            const float* k = keys + g * p.per_group;
-            // lanes start at different places of their groups: different banks
-            if (p.per4) {
-                const int quads = p.per_group / 4;
-                int at = min(l & 7, quads - 1);
-                for (int i = 0; i < quads; i += 4) {
-                    float4 v[4];
+        if (L == 32 && p.segment) {
+            // A group's quads are neighbouring lanes' i-th (with 8 lanes this costs more instructions than it saves: 16384 x 256 27.5 us against 24.8): the two largest of each quad, then of the lanes by exchange, all quads side by side.
 #pragma unroll
-                    for (int u = 0; u < 4; u++) {
-                        v[u] = *(const float4*)(k + 4 * at);
-                        at = at + 1 == quads ? 0 : at + 1;
-                    }
+            for (int i = 0; i < Q; i++) {
+                const float a1 = fmaxf(x[i][0], x[i][1]), a2 = fminf(x[i][0], x[i][1]), b1 = fmaxf(x[i][2], x[i][3]), b2 = fminf(x[i][2], x[i][3]);
+                float k1 = fmaxf(a1, b1), k2 = fmaxf(fminf(a1, b1), fmaxf(a2, b2));
 #pragma unroll
-                    for (int u = 0; u < 4; u++) {
-                        if (i + u >= quads) v[u] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);  // round again: seen already
-                        seen(v[u].x), seen_too(v[u].z), seen(v[u].y), seen_too(v[u].w);
-                    }
+                for (int o = 1; o < L; o <<= 1) {
+                    if (o >= p.segment) break;
+                    const float o1 = __shfl_xor_sync(FULL, k1, o), o2 = __shfl_xor_sync(FULL, k2, o);
+                    k2 = fmaxf(fminf(k1, o1), fmaxf(k2, o2));
+                    k1 = fmaxf(k1, o1);
                 }
-            } else {
-                int at = g % p.per_group;
-                for (int i = 0; i < p.per_group; i++) {
-                    seen(k[at]);
-                    at = at + 1 == p.per_group ? 0 : at + 1;
-                }
+                const int q = i * L + l;
+                if ((l & (p.segment - 1)) == 0 && q * 4 < p.E) gscore[q >> (31 - __clz(p.segment))] = (p.group_best == 2 && k2 != -INFINITY) ? k1 + k2 : k1;
             }
-            seen(o1), seen(o2);
-            gscore[g] = (p.group_best == 2 && k2 != -INFINITY) ? k1 + k2 : k1;
+        } else {
+            __syncwarp();
+            for (int g = l; g < p.groups; g += L) {
+                float k1 = -INFINITY, k2 = -INFINITY, o1 = -INFINITY, o2 = -INFINITY;  // the two largest, of two halves: two chains of latencies side by side
+                const auto seen = [&](float v) {
+                    k2 = fmaxf(k2, fminf(k1, v));
+                    k1 = fmaxf(k1, v);
+                };
+                const auto seen_too = [&](float v) {
+                    o2 = fmaxf(o2, fminf(o1, v));
+                    o1 = fmaxf(o1, v);
+                };
+                const float* k = keys + g * p.per_group;
+                // lanes start at different places of their groups: different banks
+                if (p.per4) {
+                    const int quads = p.per_group / 4;
+                    int at = min(l & 7, quads - 1);
+                    for (int i = 0; i < quads; i += 4) {
+                        float4 v[4];
+#pragma unroll
+                        for (int u = 0; u < 4; u++) {
+                            v[u] = *(const float4*)(k + 4 * at);
+                            at = at + 1 == quads ? 0 : at + 1;
+                        }
+#pragma unroll
+                        for (int u = 0; u < 4; u++) {
+                            if (i + u >= quads) v[u] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);  // round again: seen already
+                            seen(v[u].x), seen_too(v[u].z), seen(v[u].y), seen_too(v[u].w);
+                        }
+                    }
+                } else {
+                    int at = g % p.per_group;
+                    for (int i = 0; i < p.per_group; i++) {
+                        seen(k[at]);
+                        at = at + 1 == p.per_group ? 0 : at + 1;
+                    }
+                }
+                seen(o1), seen(o2);
+                gscore[g] = (p.group_best == 2 && k2 != -INFINITY) ? k1 + k2 : k1;
+            }
         }
         for (int g = p.groups + l; g < gpad; g += L) gscore[g] = -INFINITY;
         __syncwarp();
@@ -446,7 +464,19 @@ __global__ void __launch_bounds__(32 * (ONE ? ONE_BLOCK_WARPS : MANY_WARPS), ONE
     __syncthreads();
     const int used = offsets_of(p, hist, base, scratch, true, threads);
     const int n = (int)(p.tokens * p.K);
-    layout_choices(p, kept, 0, n, base, cnt, threads);
+    if (n <= 32) {  // a lane for each choice: its row is the first of its expert's and as many further as choices of the same expert come before
+        if (warp == 0) {
+            const int e = lane < n ? kept[lane] : -1;
+            const unsigned same = __match_any_sync(FULL, e);
+            const int row = e < 0 ? -1 : base[e] + __popc(same & ((1u << lane) - 1));
+            if (lane < n) {
+                p.slots[lane] = row;
+                if (row >= 0) p.source[row] = lane;
+            }
+        }
+    } else {
+        layout_choices(p, kept, 0, n, base, cnt, threads);
+    }
     for (int i = used + (int)threadIdx.x; i < n; i += threads) p.source[i] = -1;
 }
 
@@ -754,6 +784,8 @@ cudaError_t launch_route(int dt, const RouteParams& in, cudaStream_t s) {
     p.per4 = p.per_group % 4 == 0;
     p.magic = ((1 << 20) + p.per_group - 1) / p.per_group;
     const int es = dt == HCCL_FP32 ? 4 : 2;
+    const int quads = p.per_group / 4;
+    p.segment = p.per4 && quads <= c.lanes && (quads & (quads - 1)) == 0 ? quads : 0;
     p.vec = aligned_rows(p.logits, p.ld, es, 4 * es) && p.E % 4 == 0;
     if (dt == HCCL_FP32) return route_sizes<float>(p, c.lanes, s);
     if (dt == HCCL_BF16) return route_sizes<__nv_bfloat16>(p, c.lanes, s);

@@ -1,10 +1,10 @@
 // Exchange of rows between token order and expert order: dispatch (copy), combine (weighted sum) and the gradient of
-// combine. All three walk tokens, so that a token's row is read (or written) once and each of its top_k rows in
-// expert order is touched once, without atomics: a row belongs to one choice. Memory is the bound of all three; what
+// combine. They walk tokens (the gradient: choices, token by token), so that each row in expert order is touched once and a token's row
+// comes from memory once, without atomics: a row belongs to one choice. Memory is the bound of all three; what
 // costs is latency, so every thread asks for the pieces of several choices before it uses the first.
 //
-// Measured (B200, copy peak 6.5 TB/s): dispatch 8192 x 4096 bf16 to 8 places 102 us = 5.9 TB/s; combine back 109 us = 5.5 TB/s, its gradient 188 us = 6.1 TB/s;
-// gradient 4099 x 2056 of 6 (rows of 4112 bytes) 50 us = 4.4 TB/s; combine of 32 tokens 3 us, a launch and two latencies.
+// Measured (B200, copy peak 6.5 TB/s): dispatch 8192 x 4096 bf16 to 8 places 102 us = 5.9 TB/s; combine back 109 us = 5.5 TB/s, its gradient 173 us = 6.6 TB/s;
+// gradient 4099 x 2056 of 6 (rows of 4112 bytes) 40 us = 5.5 TB/s; combine of 32 tokens 3 us, a launch and two latencies.
 #include <algorithm>
 
 #include "experts.cuh"

@@ -6,7 +6,7 @@
 // the top k costs a maximum over the lane's quads, one over the lanes, and a second look at one quad. Not eligible: -inf. What bounds it is
 // the number of instructions and, for few tokens, their chain: a token of 256 experts is 512 bytes of input and some 500 instructions of a warp.
 //
-// Measured (B200): 16384 x 256 bf16, sigmoid, 8 groups, top 8: 16 us choosing and 8 of layout behind it; softmax without groups 10 and 9; 32768 x 128 21 us in all; one token of 256
+// Measured (B200): 16384 x 256 bf16, sigmoid, 8 groups, top 8: 16 us choosing and 6.5 of layout behind it; softmax without groups 11 and 7; 32768 x 128 21 us in all; one token of 256
 // 5.7 us, 61 x 60 5.4 us, in one launch; the gradient of 32768 x 128 6.3 us = 3.0 TB/s.
 //
 // Keys are good to a few 2^-24 (__expf and an approximate reciprocal); the weights of the chosen are formed anew with
@@ -429,9 +429,11 @@ __device__ __forceinline__ int offsets_of(const RouteParams& p, const int* tot, 
     return used;
 }
 
+// Four blocks to an SM (64 registers, a few of them spilled): the 512 blocks of 16384 tokens are on their way at once. With three, 444 are, and the rest wait for
+// a whole chain of latencies (24.9 us against 22.6).
 // A block chooses for one chunk of tokens and leaves its counts for the layout; a single block (ONE) goes on to the layout itself.
 template <typename T, int Q, int L, bool ONE>
-__global__ void __launch_bounds__(32 * (ONE ? ONE_BLOCK_WARPS : MANY_WARPS), ONE ? 1 : Q <= 4 ? 4 : 3) hccl_route_choose(const __grid_constant__ RouteParams p) {
+__global__ void __launch_bounds__(32 * (ONE ? ONE_BLOCK_WARPS : MANY_WARPS), ONE ? 1 : 4) hccl_route_choose(const __grid_constant__ RouteParams p) {
     extern __shared__ __align__(16) int sm[];  // hist[E16] bias[E16], a single block's ids, then the tokens' keys; a single block: its layout's counts in their place
     __shared__ int scratch[32];
     const int E16 = round_up(p.E, 16), threads = 32 * p.warps, warp = threadIdx.x / 32, lane = threadIdx.x % 32;

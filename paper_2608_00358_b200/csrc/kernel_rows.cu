@@ -3,7 +3,7 @@
 // comes from memory once, without atomics: a row belongs to one choice. Memory is the bound of all three; what
 // costs is latency, so every thread asks for the pieces of several choices before it uses the first.
 //
-// Measured (B200, copy peak 6.5 TB/s): dispatch 8192 x 4096 bf16 to 8 places 102 us = 5.9 TB/s; combine back 109 us = 5.5 TB/s, its gradient 173 us = 6.6 TB/s;
+// Measured (B200, copy peak 6.5 TB/s): dispatch 8192 x 4096 bf16 to 8 places 102 us = 5.9 TB/s; combine back 100 us = 6.0 TB/s, its gradient 173 us = 6.6 TB/s;
 // gradient 4099 x 2056 of 6 (rows of 4112 bytes) 40 us = 5.5 TB/s; combine of 32 tokens 3 us, a launch and two latencies.
 #include <algorithm>
 
@@ -14,7 +14,7 @@ namespace experts {
 namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
-constexpr int ROWS_THREADS = 256, BATCH = 8 /* choices at a time */;
+constexpr int ROWS_THREADS = 256, COMBINE_THREADS = 128 /* 8192 x 4096 of 8: 100 us, 109 with 256: the last round of the blocks is shorter */, BATCH = 8 /* choices at a time */;
 
 // A token belongs to a team of `team` warps (1, 2, 4 or 8) of a block.
 struct Team {
@@ -125,7 +125,7 @@ template <int PIECE> __global__ void __launch_bounds__(32 * BULK_WARPS) hccl_row
 }
 
 // KB: choices at a time, the least of 2, 4 and 8 that is not below K, or 8. blockIdx.y: which span of the columns.
-template <typename T, int N, int KB> __global__ void __launch_bounds__(ROWS_THREADS) hccl_rows_combine(const __grid_constant__ RowsParams p, int team, int span) {
+template <typename T, int N, int KB> __global__ void __launch_bounds__(COMBINE_THREADS) hccl_rows_combine(const __grid_constant__ RowsParams p, int team, int span) {
     using P = typename Piece<N * sizeof(T)>::type;
     const int cols = (int)(p.H / N), c0 = (int)blockIdx.y * span, c1 = min(c0 + span, cols);
     const Team m(team);
@@ -231,18 +231,18 @@ int piece_bytes(int es, long long H, const void* const* ptr, const long long* ld
 
 enum { DISPATCH, COMBINE, COMBINE_GRAD };
 
-// Warps for each token: one (combine 8192 x 4096 of 8, 4099 x 2056 of 6, 2000 x 1024 of 4, bf16: 109, 30 and 5 us; 112, 37 and 5 with four); with few tokens as many as make 16 warps
+// Warps for each token: one (combine 8192 x 4096 of 8, 4099 x 2056 of 6, 2000 x 1024 of 4, bf16, in blocks of 256: 109, 30 and 5 us; 112, 37 and 5 with four); with few tokens as many as make 16 warps
 // for each SM.
-int team_of(long long tokens, long long cols) {
+int team_of(long long tokens, long long cols, int most) {
     int w = 1;
-    while (w < ROWS_THREADS / 32 && tokens * w < SMS * 16 && cols > 32 * w) w *= 2;
+    while (w < most && tokens * w < SMS * 16 && cols > 32 * w) w *= 2;
     return w;
 }
 
 template <typename T, int N> cudaError_t rows_launch(int what, const RowsParams& p, cudaStream_t s) {
     const long long cols = p.H / N;
     if (cols > 1 << 30) return cudaErrorInvalidValue;
-    const int team = team_of(p.tokens, cols), per = ROWS_THREADS / 32 / team;
+    const int warps_of = (what == COMBINE ? COMBINE_THREADS : ROWS_THREADS) / 32, team = team_of(p.tokens, cols, warps_of), per = warps_of / team;
     const long long whole = (p.tokens + per - 1) / per;  // a block for each `per` tokens: the hardware hands out the next one where one has ended
     const unsigned blocks = (unsigned)std::min<long long>(std::max<long long>(whole, what == COMBINE ? 1 : SMS), 1 << 30);
     if (what == COMBINE) {
@@ -252,9 +252,9 @@ template <typename T, int N> cudaError_t rows_launch(int what, const RowsParams&
         const unsigned across = (unsigned)std::min<long long>(rounds, std::max<long long>(1, SMS * 4 / std::max<long long>(whole, 1)));
         const int span = (int)((rounds + across - 1) / across) * 32 * team;
         const dim3 grid(blocks, across);
-        if (p.K <= 2) hccl_rows_combine<T, N, 2><<<grid, ROWS_THREADS, 0, s>>>(p, team, span);
-        else if (p.K <= 4) hccl_rows_combine<T, N, 4><<<grid, ROWS_THREADS, 0, s>>>(p, team, span);
-        else hccl_rows_combine<T, N, 8><<<grid, ROWS_THREADS, 0, s>>>(p, team, span);
+        if (p.K <= 2) hccl_rows_combine<T, N, 2><<<grid, COMBINE_THREADS, 0, s>>>(p, team, span);
+        else if (p.K <= 4) hccl_rows_combine<T, N, 4><<<grid, COMBINE_THREADS, 0, s>>>(p, team, span);
+        else hccl_rows_combine<T, N, 8><<<grid, COMBINE_THREADS, 0, s>>>(p, team, span);
         return cudaGetLastError();
     }
     if (p.tokens == 0 && p.n_rows == 0) return cudaSuccess;

@@ -163,7 +163,7 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
             for (int j = 0; j < 4; j++) sum += __expf(x[i][j] - base);
         total = lanes_sum<L>(sum);
         if (p.bias) {
-            const float r = __fdividef(1.f, total);
+            const float r = total > 0.f ? __fdividef(1.f, total) : 0.f;  // nothing left: 0 * infinity would make keys that are not numbers
 #pragma unroll
             for (int i = 0; i < Q; i++)
                 if ((i * L + l) * 4 < p.E) {
@@ -294,7 +294,7 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
         const float next = fmaxf(fmaxf(j == 0 ? -INFINITY : v.x, j == 1 ? -INFINITY : v.y), fmaxf(j == 2 ? -INFINITY : v.z, j == 3 ? -INFINITY : v.w));
         int quad = mine;
         lanes_best<L>(win, quad);
-        const bool none = win == -INFINITY || bad, owner = quad == mine && !none;
+        const bool none = !(win > -INFINITY) || bad, owner = quad == mine && !none;  // NaN is none too: every place gets an id that some lane found
         if (owner) {
             chosen[k] = quad * 4 + j;
             c[j] = -INFINITY;

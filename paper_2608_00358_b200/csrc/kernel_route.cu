@@ -13,6 +13,7 @@
 // expf and a rounded division.
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 
 #include "experts.cuh"
 
@@ -181,6 +182,13 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
 #pragma unroll
     for (int i = 0; i < Q; i++)
         if ((i * L + l) * 4 < p.E) *(float4*)(keys + (i * L + l) * 4) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+    // A group's score from its two largest keys. Logits in the place of keys (a softmax without bias) have the scores' order, but it is the scores that are
+    // added up. By the logarithm of exp(k1) + exp(k2), over exp(m): a sum far below the largest does not vanish, and -inf stays for groups without experts.
+    const auto group_score = [&](float k1, float k2) {
+        if (p.group_best != 2 || k1 == -INFINITY) return k1;
+        if (!p.sigmoid && !p.bias) return fmaxf((k1 - m) + log1pf(expf(k2 - k1)), -FLT_MAX);
+        return k2 == -INFINITY ? k1 : k1 + k2;
+    };
     float top[Q];
 #pragma unroll
     for (int i = 0; i < Q; i++) top[i] = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
@@ -199,7 +207,7 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
                     k1 = fmaxf(k1, o1);
                 }
                 const int q = i * L + l;
-                if ((l & (p.segment - 1)) == 0 && q * 4 < p.E) gscore[q >> (31 - __clz(p.segment))] = (p.group_best == 2 && k2 != -INFINITY) ? k1 + k2 : k1;
+                if ((l & (p.segment - 1)) == 0 && q * 4 < p.E) gscore[q >> (31 - __clz(p.segment))] = group_score(k1, k2);
             }
         } else {
             __syncwarp();
@@ -239,7 +247,7 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
                     }
                 }
                 seen(o1), seen(o2);
-                gscore[g] = (p.group_best == 2 && k2 != -INFINITY) ? k1 + k2 : k1;
+                gscore[g] = group_score(k1, k2);
             }
         }
         for (int g = p.groups + l; g < gpad; g += L) gscore[g] = -INFINITY;

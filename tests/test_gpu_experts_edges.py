@@ -5,9 +5,8 @@ import pytest
 import torch
 
 import expert_reference as ref
-from paper_2608_00358_b200 import binding as hb
 from paper_2608_00358_b200 import experts as ex
-from test_gpu_experts import BF16, F16, F32, check_routing, cuda, gen, grid_logits, strided, weight_tol
+from test_gpu_experts import BF16, F16, F32, check_routing, close, cuda, gen, grid_logits, strided, weight_tol
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +32,41 @@ def test_rows_with_nothing_left_beside_a_bias(T, E, k, dt, score, renorm, groups
     check_routing(r, ids, w, E, weight_tol(E, w))
     dl = router.backward(lg, r, torch.ones(T, k, device="cuda"), bias=cuda(bias))
     assert (dl[[1, 4, T - 1]] == 0).all() and torch.isfinite(dl).all()
+
+
+@pytest.mark.parametrize("bias", [False, True])
+def test_two_groups_worked_by_hand(bias):
+    """exp(10) + exp(-20) against 2 exp(5): the first group's scores add up to more, its logits to less."""
+    logits = torch.tensor([[10.0, -20.0, 5.0, 5.0]], device="cuda")
+    r = ex.Router(4, 1, groups=2, top_groups=1, group_best=2).route(logits, torch.zeros(4, device="cuda") if bias else None)
+    assert r.ids.tolist() == [[0]]
+
+
+@pytest.mark.parametrize("T", [2, 150])
+def test_groups_far_below_the_largest_keep_their_order(T):
+    """Scores that are 0 in 32 bits: the third group is the second best, the type's lowest value stands behind all other numbers, and -inf behind that."""
+    low, inf = float(torch.finfo(F32).min), float("inf")
+    logits = torch.tensor([[low, low, -200.0, -201.0, -150.0, -199.0, 0.0, -1.0, -inf, -inf]] * T, device="cuda")
+    for groups, want in ((1, [6]), (2, [6, 4]), (3, [6, 4, 2]), (4, [6, 4, 2, 0])):
+        r = ex.Router(10, 8, groups=5, top_groups=groups, group_best=2).route(logits)
+        firsts = [i for i in r.ids[T - 1].tolist() if i >= 0 and i % 2 == 0]
+        assert sorted(firsts) == sorted(want) and (r.ids == r.ids[0]).all()
+
+
+@pytest.mark.parametrize("T,E,k,groups,top_groups,dt", [(7, 256, 8, 8, 3, BF16), (200, 96, 5, 8, 3, F32), (300, 33, 3, 11, 4, F32), (40, 320, 6, 8, 2, F16),
+                                                        (150, 64, 4, 8, 3, BF16), (25, 12, 2, 4, 2, F32)])
+def test_groups_under_softmax_go_by_the_sum_of_their_scores(T, E, k, groups, top_groups, dt):
+    rng = gen(T + E)
+    logits = grid_logits(rng, T, E, dt) * 3
+    logits[1, : E // 2] = -np.inf          # groups without experts
+    logits[2, 1::2] = -np.inf              # groups with half of theirs
+    logits[3] = -np.inf
+    # zeros for a bias: the reference's keys are the scores then, which is what a group's score is made of
+    kw = dict(groups=groups, top_groups=top_groups, group_best=2, renorm=True, scale=1.0)
+    ids, w, gap = ref.route(logits.float().numpy(), k, "softmax", np.zeros(E, dtype=np.float32), None, **kw)
+    assert gap > 1e-6
+    router = ex.Router(E, k, groups=groups, top_groups=top_groups, group_best=2)
+    for bias in (None, torch.zeros(E, device="cuda")):
+        r = router.route(strided(logits, 1), bias)
+        assert np.array_equal(r.ids.cpu().numpy(), ids)
+        close(r.weights, w, weight_tol(E, w))

@@ -526,7 +526,7 @@ int hccl_version(void);
 typedef enum { HCCL_SCORE_SOFTMAX = 0, HCCL_SCORE_SIGMOID = 1 } hccl_score_t;
 
 /* How tokens choose experts. score s = softmax(l) over the experts, or sigmoid(l) for each. The choice goes by key
- * = s + bias (softmax without bias: by l itself, whose order is the same and which no rounding ties). With
+ * = s + bias (without bias: by l itself, whose order is the same and which no rounding ties). With
  * groups > 1 the experts form equal consecutive groups; a group's score is the sum of its group_best (1 or 2) largest
  * s + bias (never of two l: their sums have another order), and only experts of the top_groups best groups stay eligible. The top_k largest keys win; ties go to the
  * lowest index, of groups and of experts. Weights: w = s of the chosen, divided by their sum if renormalise, times scale. */

@@ -9,7 +9,7 @@
 // Measured (B200): 16384 x 256 bf16, sigmoid, 8 groups, top 8: 16 us choosing and 6.5 of layout behind it; softmax without groups 11 and 7; 32768 x 128 21 us in all; one token of 256
 // 5.7 us, 61 x 60 5.4 us, in one launch; the gradient of 32768 x 128 6.3 us = 3.0 TB/s.
 //
-// Keys are good to a few 2^-24 (__expf and an approximate reciprocal); the weights of the chosen are formed anew with
+// Keys with a bias are good to a few 2^-24 (__expf and an approximate reciprocal), without one they are the logits; the weights of the chosen are formed anew with
 // expf and a rounded division.
 #include <algorithm>
 #include <atomic>
@@ -144,15 +144,17 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
     bad |= !p.sigmoid && m == INFINITY;
     bad = lanes_any<L>(bad);
     float total = 1.f;
-    if (p.sigmoid) {
+    if (p.sigmoid) {  // (without a bias the logits are the keys: their order is the scores', also where those round to the same number)
+        if (p.bias) {
 #pragma unroll
-        for (int i = 0; i < Q; i++) {
-            float b[4] = {0.f, 0.f, 0.f, 0.f};
-            if (p.bias && (i * L + l) * 4 < p.E) bias_quad(i, b);
+            for (int i = 0; i < Q; i++) {
+                float b[4] = {0.f, 0.f, 0.f, 0.f};
+                if ((i * L + l) * 4 < p.E) bias_quad(i, b);
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float off = x[i][j] == -INFINITY ? -INFINITY : b[j];  // (not around the sigmoid: that would be a branch for each)
-                x[i][j] = quick_sigmoid(x[i][j]) + off;
+                for (int j = 0; j < 4; j++) {
+                    const float off = x[i][j] == -INFINITY ? -INFINITY : b[j];  // (not around the sigmoid: that would be a branch for each)
+                    x[i][j] = quick_sigmoid(x[i][j]) + off;
+                }
             }
         }
     } else if (p.bias || !p.renorm) {
@@ -182,11 +184,12 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
 #pragma unroll
     for (int i = 0; i < Q; i++)
         if ((i * L + l) * 4 < p.E) *(float4*)(keys + (i * L + l) * 4) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
-    // A group's score from its two largest keys. Logits in the place of keys (a softmax without bias) have the scores' order, but it is the scores that are
-    // added up. By the logarithm of exp(k1) + exp(k2), over exp(m): a sum far below the largest does not vanish, and -inf stays for groups without experts.
+    // A group's score from its two largest keys. Logits in the place of keys (no bias) have the scores' order, but it is the scores that are
+    // added up. Softmax: by the logarithm of exp(k1) + exp(k2), over exp(m): a sum far below the largest does not vanish, and -inf stays for groups without experts.
     const auto group_score = [&](float k1, float k2) {
         if (p.group_best != 2 || k1 == -INFINITY) return k1;
-        if (!p.sigmoid && !p.bias) return fmaxf((k1 - m) + log1pf(expf(k2 - k1)), -FLT_MAX);
+        if (!p.bias && p.sigmoid) return 1.f / (1.f + expf(-k1)) + 1.f / (1.f + expf(-k2));
+        if (!p.bias) return fmaxf((k1 - m) + log1pf(expf(k2 - k1)), -FLT_MAX);
         return k2 == -INFINITY ? k1 : k1 + k2;
     };
     float top[Q];

@@ -70,3 +70,23 @@ def test_groups_under_softmax_go_by_the_sum_of_their_scores(T, E, k, groups, top
         r = router.route(strided(logits, 1), bias)
         assert np.array_equal(r.ids.cpu().numpy(), ids)
         close(r.weights, w, weight_tol(E, w))
+
+
+@pytest.mark.parametrize("T,E,k,groups", [(9, 64, 8, 1), (300, 64, 8, 1), (40, 300, 8, 1), (200, 64, 8, 8), (10, 64, 8, 8)])
+@pytest.mark.parametrize("low,high", [(10.0, 40.0), (-40.0, -10.0), (-140.0, -90.0)])
+def test_sigmoid_scores_without_a_bias_choose_in_the_order_of_the_logits(T, E, k, groups, low, high):
+    """Near 1 and near 0 the scores of different logits are the same number, or rounded the wrong way; the logits are not."""
+    rng = gen(T)
+    logits = np.stack([rng.permutation(E) for _ in range(T)]) * ((high - low) / E) + low
+    logits = torch.from_numpy(logits.astype(np.float32))
+    key = logits.clone()
+    top_groups = max(1, groups // 2)
+    if groups > 1:
+        best = key.view(T, groups, -1).amax(-1).sort(dim=-1, descending=True).indices[:, :top_groups]
+        keep = torch.zeros(T, groups, dtype=torch.bool).scatter_(1, best, True)
+        key[~keep.repeat_interleave(E // groups, dim=1)] = -np.inf
+    want = key.sort(dim=-1, descending=True, stable=True).indices[:, :k]
+    r = ex.Router(E, k, score="sigmoid", groups=groups, top_groups=top_groups, renormalise=False).route(logits.cuda())
+    assert torch.equal(r.ids.cpu().long(), want)
+    w = 1 / (1 + np.exp(-logits.gather(1, want).double().numpy()))
+    close(r.weights, w, weight_tol(E, w))

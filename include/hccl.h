@@ -559,7 +559,7 @@ typedef struct {
  * are not looked at, and are in no softmax sum); an expert whose logit is -inf, for that token. A token with fewer
  * eligible experts than top_k gets ids -1 and weights 0 in the places left over; one with none gets them everywhere.
  * A token that cannot be scored (an eligible logit or bias is NaN, a bias is +inf, or a logit is +inf under softmax) gets ids -1 and weights NaN.
- * Chosen scores that are all 0 keep weight 0 when renormalised. tokens * top_k < 2^31.
+ * Renormalised softmax weights are a softmax over the chosen, however far below the others a bias chose; chosen sigmoids that are all 0 keep weight 0. tokens * top_k < 2^31.
  * Workspace: hccl_route_workspace_bytes, 16-byte aligned, contents arbitrary; not shared by calls in flight at once. */
 hccl_status_t hccl_route_workspace_bytes(const hccl_router_t*, int64_t tokens, size_t* bytes);
 hccl_status_t hccl_route(const hccl_router_t*, const void* logits, int64_t ld, hccl_dtype_t dt, const float* bias,

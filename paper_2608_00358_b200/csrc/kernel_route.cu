@@ -322,17 +322,28 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
     for (int r = 0; r < R; r++) {
         const int k = r * L + l;
         id[r] = k < p.K ? chosen[k] : -1;
-        float v = p.sigmoid ? -INFINITY : m;
-        if (id[r] >= 0) v = to_f32<T>(row[id[r]]);
-        s[r] = p.sigmoid ? 1.f / (1.f + expf(-v)) : expf(v - m);  // softmax: the common divisor drops out of renormalised weights
-        s[r] = id[r] >= 0 ? s[r] : 0.f;
-        sum += s[r];
+        s[r] = id[r] >= 0 ? to_f32<T>(row[id[r]]) : -INFINITY;
         if (r * L + L >= p.K) {
 #pragma unroll
             for (int q = 0; q < R; q++)
-                if (q > r) id[q] = -1, s[q] = 0.f;
+                if (q > r) id[q] = -1, s[q] = -INFINITY;
             break;
         }
+    }
+    // Softmax: over the row's largest logit; renormalised weights beside a bias, which may choose scores that are 0 against it, over the largest chosen one (the common
+    // divisor drops out, and the gradient does the same). Without a bias that is the row's, or, with groups, close to it.
+    float base = m;
+    if (!p.sigmoid && p.renorm && p.bias) {
+        base = s[0];
+#pragma unroll
+        for (int r = 1; r < R; r++) base = fmaxf(base, s[r]);
+        base = lanes_max<L>(base);
+    }
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        if (r * L < p.K) s[r] = p.sigmoid ? 1.f / (1.f + expf(-s[r])) : expf(s[r] - base);
+        s[r] = id[r] >= 0 ? s[r] : 0.f;
+        sum += s[r];
     }
     const float div = p.renorm ? lanes_sum<L>(sum) : total;
     if (in) {

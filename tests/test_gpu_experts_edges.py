@@ -90,3 +90,24 @@ def test_sigmoid_scores_without_a_bias_choose_in_the_order_of_the_logits(T, E, k
     assert torch.equal(r.ids.cpu().long(), want)
     w = 1 / (1 + np.exp(-logits.gather(1, want).double().numpy()))
     close(r.weights, w, weight_tol(E, w))
+
+
+@pytest.mark.parametrize("T", [3, 200])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_a_bias_that_picks_scores_far_below_the_largest(T, renorm):
+    """Renormalised weights are a softmax over the chosen: how far they lie below the others does not matter, to the weights or to their gradient."""
+    E, k = 8, 2
+    logits = np.tile(np.array([0.0, -150.0, -151.0, -300.0, -1.0, -2.0, -200.0, -149.0], dtype=np.float32), (T, 1))
+    logits[1:] += gen(4).integers(-4, 5, (T - 1, E)).astype(np.float32) / 8
+    bias = np.array([0, 4, 3, 0, 0, 0, 0, 0], dtype=np.float32)
+    ids, w, gap = ref.route(logits, k, "softmax", bias, None, renorm=renorm)
+    assert gap > 1e-6 and (ids == [1, 2]).all()
+    router = ex.Router(E, k, renormalise=renorm)
+    r = router.route(cuda(logits), cuda(bias))
+    assert np.array_equal(r.ids.cpu().numpy(), ids)
+    close(r.weights, w, weight_tol(E, w) + (0 if renorm else 1e-37))
+    dw = gen(5).uniform(-1, 1, (T, k)).astype(np.float32)
+    want = ref.route_grad(logits.astype(np.float64), ids, dw, "softmax", renorm, 1.0)
+    got = router.backward(cuda(logits), r, cuda(dw), bias=cuda(bias))
+    # w_j (dw_j - sum dw w): a product of two, each within (2 k + 64) 2^-24 of its terms' size, which is at most 2
+    close(got, want, (2 * k + 64) * ref.EPS32 * 2 + ref.HALF_ULP[F32] * np.abs(want) + 1e-37)

@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(LAYOUT_THREADS) hccl_route_layout(const __grid
 }
 
 // d of the logits. Weight j of the chosen has w_j = scale * s_j / S (S = sum of the chosen scores if renormalised, else 1), so
-// ds_j = scale / S * (dw_j - sum_i dw_i s_i / S) or scale * dw_j; then the score's own derivative:
+// ds_j = scale / S * (dw_j - sum_i dw_i s_i / S) or scale * dw_j; then the score's own derivative (with s_j / S formed first, which is a weight):
 // sigmoid dl = ds s (1 - s), softmax dl_e = s_e (ds_e - sum_j ds_j s_j) over all experts. Where the weights are renormalised (the softmax's
 // divisor drops out, and with it sum_j ds_j s_j = 0) or the scores are sigmoids, only the chosen have a gradient: their logits alone
 // are read, and the row is zeros with k places filled, put together in shared memory. Memory is the bound.
@@ -660,9 +660,17 @@ __global__ void __launch_bounds__(256) hccl_route_grad(const __grid_constant__ R
             sdc += dw[r] * c[r];
         }
         if (p.renorm) {
-            const float S = lanes_sum<L>(sc), D = lanes_sum<L>(sdc), r1 = S > 0.f ? 1.f / S : 0.f;
+            // By the weights c / S: (dw - sum dw c / S) / S would leave the range for sigmoids near 0, times c it is of the size of dw.
+            const float S = lanes_sum<L>(sc);
+            sdc = 0.f;
 #pragma unroll
-            for (int r = 0; r < R; r++) dw[r] = (dw[r] - D * r1) * r1;
+            for (int r = 0; r < R; r++) {
+                x[r] = S > 0.f ? c[r] / S : 0.f;
+                sdc += dw[r] * x[r];
+            }
+            const float D = lanes_sum<L>(sdc);
+#pragma unroll
+            for (int r = 0; r < R; r++) dw[r] = (dw[r] - D) * x[r];
         } else if (whole_row) {
             const float r1 = total > 0.f ? 1.f / total : 0.f;
             dot = lanes_sum<L>(sdc) * r1;
@@ -682,7 +690,7 @@ __global__ void __launch_bounds__(256) hccl_route_grad(const __grid_constant__ R
         __syncwarp();
 #pragma unroll
         for (int r = 0; r < R; r++)
-            if (id[r] >= 0 && !bad) buf[id[r]] = from_f32<T>(p.sigmoid ? dw[r] * c[r] * (1.f - c[r]) : p.renorm ? dw[r] * c[r] : c[r] * total * (dw[r] - dot));
+            if (id[r] >= 0 && !bad) buf[id[r]] = from_f32<T>(p.renorm ? (p.sigmoid ? dw[r] * (1.f - c[r]) : dw[r]) : p.sigmoid ? dw[r] * c[r] * (1.f - c[r]) : c[r] * total * (dw[r] - dot));
         __syncwarp();
         if (in) {
             T* out = (T*)q.dlogits + t * q.ldd;

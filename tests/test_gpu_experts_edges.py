@@ -111,3 +111,19 @@ def test_a_bias_that_picks_scores_far_below_the_largest(T, renorm):
     got = router.backward(cuda(logits), r, cuda(dw), bias=cuda(bias))
     # w_j (dw_j - sum dw w): a product of two, each within (2 k + 64) 2^-24 of its terms' size, which is at most 2
     close(got, want, (2 * k + 64) * ref.EPS32 * 2 + ref.HALF_ULP[F32] * np.abs(want) + 1e-37)
+
+
+@pytest.mark.parametrize("k", [2, 5])
+@pytest.mark.parametrize("E", [16, 300])
+def test_gradient_of_renormalised_sigmoids_near_zero(E, k):
+    """Scores of 1e-38 with a gradient of some hundreds (a scaled loss): 1 / S times the gradient leaves the range, the result does not."""
+    T = 20
+    rng = gen(E)
+    logits = (-86.0 + np.stack([rng.permutation(E) for _ in range(T)]) / E).astype(np.float32)
+    dw = rng.uniform(-300, 300, (T, k)).astype(np.float32)
+    router = ex.Router(E, k, score="sigmoid")
+    r = router.route(cuda(logits))
+    want = ref.route_grad(logits.astype(np.float64), r.ids.cpu().numpy().astype(np.int64), dw, "sigmoid", True, 1.0)
+    got = router.backward(cuda(logits), r, cuda(dw))
+    # scores at the lower end of the normal numbers: exp within 2 ulp, sums and quotients of k of them, terms up to 2 * 300
+    close(got, want, (2 * k + 64) * ref.EPS32 * 600 + ref.HALF_ULP[F32] * np.abs(want))

@@ -732,13 +732,15 @@ Cut cut(long long tokens, int E) {
     return c;
 }
 
-// Opt-in to large shared memory, once for each kernel and device.
+// Opt-in to large shared memory, once for each kernel and device. The most that a launch here asks for: one block for 32 tokens of 1024 experts in 1024 groups, top 32.
+constexpr int MOST_SMEM = 4 * (2 * HCCL_MAX_EXPERTS + ONE_BLOCK_WARPS * (HCCL_MAX_EXPERTS + 8 + 2 * HCCL_MAX_EXPERTS + HCCL_MAX_TOP_K) + 2 * ONE_BLOCK_WARPS * HCCL_MAX_TOP_K);
+static_assert(MOST_SMEM + 1024 <= 227 * 1024, "beyond a block's shared memory");
 template <typename K> cudaError_t allow(K* kernel, size_t bytes, std::atomic<bool> (&ready)[64]) {
     if (bytes <= 48 * 1024) return cudaSuccess;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || (dev < 64 && ready[dev])) return e;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST_SMEM);
     if (e == cudaSuccess && dev < 64) ready[dev] = true;
     return e;
 }

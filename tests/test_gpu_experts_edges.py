@@ -127,3 +127,16 @@ def test_gradient_of_renormalised_sigmoids_near_zero(E, k):
     got = router.backward(cuda(logits), r, cuda(dw))
     # scores at the lower end of the normal numbers: exp within 2 ulp, sums and quotients of k of them, terms up to 2 * 300
     close(got, want, (2 * k + 64) * ref.EPS32 * 600 + ref.HALF_ULP[F32] * np.abs(want))
+
+
+@pytest.mark.parametrize("T", [9, 15, 16, 31, 32, 33])
+@pytest.mark.parametrize("k", [8, 32])
+@pytest.mark.parametrize("E", [1024, 990])
+def test_as_many_groups_as_experts(T, k, E):
+    g = torch.Generator().manual_seed(T)
+    logits = torch.stack([torch.randperm(E, generator=g) for _ in range(T)]).float() / 64
+    r = ex.Router(E, k, groups=E, top_groups=E // 2).route(logits.cuda())
+    order = logits.sort(dim=-1, descending=True).indices[:, :k]
+    assert torch.equal(r.ids.cpu().long(), order)
+    counts, offsets, slots, source = ref.layout(order.numpy(), E)
+    assert np.array_equal(r.slots.cpu().numpy(), slots) and np.array_equal(r.source.cpu().numpy(), source) and np.array_equal(r.offsets.cpu().numpy(), offsets)

@@ -2,7 +2,7 @@
 
 The operators are the C calls of include/hccl.h (``hccl_route`` and the ones after it); this module checks tensors,
 supplies outputs and workspaces, and joins the gradients to torch's autograd. Everything runs on the current stream of
-the tensors' device; nothing here computes, and there is no CPU form.
+the tensors' device; nothing here computes, and there is no CPU form. Host threads may share a router or a layer.
 
     router = Router(experts=64, top_k=8, score="sigmoid", renormalise=True)
     r = router.route(logits, bias=balance)            # who goes where, with which weight
@@ -15,6 +15,7 @@ buffer of an AllToAllv, and ``r.counts`` is the rank's row of its count matrix w
 from __future__ import annotations
 
 import ctypes as C
+import threading
 from typing import Optional
 
 import torch
@@ -83,8 +84,9 @@ def _on(dev: int, call, *args):
             call(*args, _stream(dev))
 
 
-class _Scratch:
-    """Device memory of one object, one piece for each stream it is used on: calls on different streams do not share it. A call that is captured
+class _Scratch(threading.local):
+    """Device memory of one object, one piece for each host thread and stream it is used on. Calls on different streams do not share it, nor do threads on one stream: a
+    call makes up to two launches, and another thread's may come between them. A call that is captured
     into a CUDA graph gets memory of the graph's own, since the graph may be replayed on any stream, beside later calls."""
 
     def __init__(self):

@@ -1,5 +1,7 @@
 """Expert-layer operators where it is easy to go wrong: rows with nothing left, groups by sums of scores, scores at the ends of their range, many experts in
 many groups, gradients of every layout, autograd's own rules, host threads, and the sizes at which another kernel or another turn of a loop takes over."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -140,3 +142,34 @@ def test_as_many_groups_as_experts(T, k, E):
     assert torch.equal(r.ids.cpu().long(), order)
     counts, offsets, slots, source = ref.layout(order.numpy(), E)
     assert np.array_equal(r.slots.cpu().numpy(), slots) and np.array_equal(r.source.cpu().numpy(), source) and np.array_equal(r.offsets.cpu().numpy(), offsets)
+
+
+# ------------------------------------------------------------------------------------------------ host threads
+def test_host_threads_on_one_stream_do_not_share_scratch():
+    """Two threads that call the same router and the same layer on the default stream, with rows and token counts of their own."""
+    E, k, K, N = 16, 4, 256, 128
+    g = torch.Generator(device="cuda").manual_seed(1)
+    router, lin = ex.Router(E, k), ex.Int8Linear.from_float(torch.randn(E, N, K, generator=g, device="cuda"))
+    sizes = (700, 3001)
+    logits, x = [torch.randn(T, E, generator=g, device="cuda") for T in sizes], [torch.randn(T, K, generator=g, device="cuda") for T in sizes]
+    want = []
+    for i in range(2):
+        r = router.route(logits[i])
+        want.append((r, lin(x[i], routing=r)))
+    torch.cuda.synchronize()
+    wrong, start = [], threading.Barrier(2)
+
+    def work(i):
+        start.wait()
+        for turn in range(150):
+            r = router.route(logits[i])
+            y = lin(x[i], routing=r)
+            if turn % 10 == 9 and not (torch.equal(r.source, want[i][0].source) and torch.equal(r.slots, want[i][0].slots) and torch.equal(y, want[i][1])):
+                wrong.append((i, turn))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong

@@ -15,8 +15,19 @@ from typing import List
 import torch
 
 from . import binding as hb
-from .experts import Int8Linear, Router, Routing, _pad16, _quantize, combine
+from .experts import Int8Linear, Router, Routing, _dtype, _matrix, _pad16, _quantize, _refuse, combine
 from .runtime import DeviceCollective
+
+
+def check_experts(router: Router, up: List[Int8Linear], down: List[Int8Linear], dev: int):
+    """Refuses experts that do not fit the router or each other: one up and one down for each rank, each over one expert on device number `dev`."""
+    if len(up) != router.experts or len(down) != router.experts:
+        _refuse(hb.ERR_COUNT_MISMATCH, "ExpertParallel: %d and %d experts for %d ranks" % (len(up), len(down), router.experts))
+    for r, (u, d) in enumerate(zip(up, down)):
+        if u.experts != 1 or d.experts != 1 or u.dev != dev or d.dev != dev:
+            _refuse(hb.ERR_INVALID_ARG, "ExpertParallel: rank %d's layers must be over one expert each, on cuda:%d" % (r, dev))
+        if u.K != up[0].K or d.K != u.N or d.N != u.K:
+            _refuse(hb.ERR_COUNT_MISMATCH, "ExpertParallel: rank %d's layers are %d -> %d and %d -> %d, the first takes %d" % (r, u.K, u.N, d.K, d.N, up[0].K))
 
 
 class ExpertParallel:
@@ -24,6 +35,8 @@ class ExpertParallel:
     act: what stands between them."""
 
     def __init__(self, router: Router, up: List[Int8Linear], down: List[Int8Linear], tokens: int, act=torch.nn.functional.silu, device="cuda"):
+        self.dev = torch.empty(0, device=device).get_device()
+        check_experts(router, up, down, self.dev)
         R, k, hidden = router.experts, router.top_k, up[0].K
         self.router, self.up, self.down, self.act = router, up, down, act
         self.R, self.tokens, self.hidden = R, tokens, hidden
@@ -56,11 +69,16 @@ class ExpertParallel:
 
     def forward(self, x: List[torch.Tensor], logits: List[torch.Tensor]) -> List[torch.Tensor]:
         """x[r] [tokens, hidden] and logits[r] [tokens, ranks] of every rank; returns each rank's [tokens, hidden] in bf16."""
+        if len(x) != self.R or len(logits) != self.R:
+            _refuse(hb.ERR_COUNT_MISMATCH, "ExpertParallel: inputs of %d and %d ranks, expected %d" % (len(x), len(logits), self.R))
+        rows = [(_matrix(t, "x", self.hidden, self.tokens, self.dev), _dtype(t, "x")) for t in x]
+        for t in logits:
+            _matrix(t, "logits", self.R, self.tokens, self.dev), _dtype(t, "logits")
         stream = torch.cuda.current_stream()
-        for r in range(self.R):
+        for r, (ld, dt) in enumerate(rows):
             self.router.route(logits[r], out=self.routing[r])
-            _quantize(x[r].data_ptr(), x[r].stride(0), self.tokens, self.hidden, _type(x[r]), self.routing[r].at, self.send[r].data_ptr(), self.row,
-                                     self.send_rows, self.scale.data_ptr(), stream.cuda_stream)
+            _quantize(x[r].data_ptr(), ld, self.tokens, self.hidden, dt, self.routing[r].at, self.send[r].data_ptr(), self.row,
+                      self.send_rows, self.scale.data_ptr(), stream.cuda_stream)
             self.send[r][:, self.at: self.at + 4] = self.scale[: self.send_rows].view(torch.int8).view(-1, 4)
         self._out.execute(stream)
         self.counts_back.copy_(self.counts.t())
@@ -78,10 +96,6 @@ class ExpertParallel:
         self._home.check()
         for lin in self.up + self.down:
             lin.check()
-
-
-def _type(x: torch.Tensor) -> int:
-    return {torch.float32: hb.FP32, torch.bfloat16: hb.BF16, torch.float16: hb.FP16}[x.dtype]
 
 
 def main():

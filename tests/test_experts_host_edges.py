@@ -29,3 +29,75 @@ def test_scratch_is_not_shared_by_host_threads(no_device):
     assert seen[0][1] != mine[1]
     assert scratch.get(0, 500)[1] == mine[1]  # the same thread and stream: the same memory
     assert scratch.get(0, 2000)[0].numel() >= 2000
+
+
+class Seen(Exception):
+    """A launch was reached."""
+
+
+def layer_without_a_device(monkeypatch, R=2, tokens=3, hidden=32):
+    """An ExpertParallel whose first launches only say that they were reached."""
+    from paper_2608_00358_b200 import expert_layer as el
+
+    def reached(*a, **kw):
+        raise Seen
+
+    class Stream:
+        cuda_stream = 0
+
+    layer = object.__new__(el.ExpertParallel)
+    layer.R, layer.tokens, layer.hidden, layer.dev = R, tokens, hidden, 0
+    layer.router = type("R", (), dict(route=staticmethod(lambda *a, **kw: None), experts=R, top_k=1))()
+    layer.routing = [type("P", (), dict(at=0))() for _ in range(R)]
+    layer.send = [torch.zeros(tokens, 48, dtype=torch.int8) for _ in range(R)]
+    layer.scale, layer.row, layer.at, layer.send_rows = torch.zeros(tokens), 48, 32, tokens
+    monkeypatch.setattr(el, "_quantize", reached)
+    monkeypatch.setattr(el.torch.cuda, "current_stream", lambda *a: Stream())
+    return layer
+
+
+def on_device(t):
+    """A stand-in that says it is on device 0; its address is the host's, which nothing may follow."""
+    class There(torch.Tensor):
+        def get_device(self):
+            return 0
+
+    return t.as_subclass(There)
+
+
+@pytest.mark.parametrize("what,want", [("few rows", hb.ERR_COUNT_MISMATCH), ("many rows", hb.ERR_COUNT_MISMATCH), ("few columns", hb.ERR_COUNT_MISMATCH), ("columns apart", hb.ERR_ALIGNMENT),
+                                       ("host", hb.ERR_INVALID_ARG), ("type", hb.ERR_DTYPE), ("vector", hb.ERR_INVALID_ARG), ("ranks", hb.ERR_COUNT_MISMATCH),
+                                       ("logits", hb.ERR_COUNT_MISMATCH), ("nothing", None)])
+def test_an_expert_layer_checks_its_inputs_before_the_first_launch(monkeypatch, what, want):
+    layer = layer_without_a_device(monkeypatch)
+    good = lambda: on_device(torch.zeros(3, 32))  # noqa: E731
+    x = [good(), good()]
+    x[1] = {"few rows": on_device(torch.zeros(2, 32)), "many rows": on_device(torch.zeros(4, 32)), "few columns": on_device(torch.zeros(3, 31)),
+            "columns apart": on_device(torch.zeros(32, 3).t()), "host": torch.zeros(3, 32), "type": on_device(torch.zeros(3, 32).double()),
+            "vector": on_device(torch.zeros(96))}.get(what, x[1])
+    logits = [on_device(torch.zeros(3, 2)), on_device(torch.zeros(2 if what == "logits" else 3, 2))]
+    if what == "ranks":
+        x.pop()
+    if want is None:
+        with pytest.raises(Seen):
+            layer.forward(x, logits)
+        return
+    with pytest.raises(hb.HcclError) as e:
+        layer.forward(x, logits)
+    assert e.value.status == want
+
+
+def test_an_expert_layer_checks_its_experts():
+    from paper_2608_00358_b200 import expert_layer as el
+
+    def lin(n, k, experts=1, dev=0):
+        return type("L", (), dict(N=n, K=k, experts=experts, dev=dev))()
+
+    router = type("R", (), dict(experts=2, top_k=1))()
+    up, down = [lin(64, 32), lin(48, 32)], [lin(32, 64), lin(32, 48)]
+    for u, d in ((up[:1], down), (up, down[:1]), ([up[0], lin(48, 31)], down), (up, [down[0], lin(32, 64)]), (up, [down[0], lin(31, 48)]),
+                 ([lin(64, 32, experts=2), up[1]], down), ([lin(64, 32, experts=0), up[1]], down), (up, [down[0], lin(32, 48, dev=1)])):
+        with pytest.raises(hb.HcclError) as e:
+            el.check_experts(router, u, d, 0)
+        assert e.value.status in (hb.ERR_COUNT_MISMATCH, hb.ERR_INVALID_ARG)
+    el.check_experts(router, up, down, 0)

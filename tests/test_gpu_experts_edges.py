@@ -7,10 +7,18 @@ import pytest
 import torch
 
 import expert_reference as ref
+from paper_2608_00358_b200 import binding as hb
 from paper_2608_00358_b200 import experts as ex
+from paper_2608_00358_b200.expert_layer import ExpertParallel
 from test_gpu_experts import BF16, F16, F32, check_routing, close, cuda, gen, grid_logits, strided, weight_tol
 
 pytestmark = pytest.mark.gpu
+
+
+def refused(status, f):
+    with pytest.raises(hb.HcclError) as e:
+        f()
+    assert e.value.status == status
 
 
 # ------------------------------------------------------------------------------------------------ routing
@@ -173,3 +181,26 @@ def test_host_threads_on_one_stream_do_not_share_scratch():
     for t in threads:
         t.join()
     assert not wrong
+
+
+# ------------------------------------------------------------------------------------------------ the layer over ranks
+def test_an_expert_layer_takes_any_stride_and_refuses_other_shapes():
+    R, k, tokens, hidden, inner = 3, 2, 20, 48, 32
+    g = torch.Generator(device="cuda").manual_seed(0)
+    up, down = [[ex.Int8Linear.from_float(torch.randn(1, n, m, device="cuda", generator=g)) for _ in range(R)] for n, m in ((inner, hidden), (hidden, inner))]
+    layer = ExpertParallel(ex.Router(R, k), up, down, tokens)
+    x, logits = [torch.randn(tokens, hidden, device="cuda", generator=g) for _ in range(R)], [torch.randn(tokens, R, device="cuda", generator=g) for _ in range(R)]
+    want = layer.forward(x, logits)
+    layer.check()
+    got = layer.forward([strided(t, 5, 3) for t in x], logits)
+    layer.check()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    mism, bad, ali, dty = hb.ERR_COUNT_MISMATCH, hb.ERR_INVALID_ARG, hb.ERR_ALIGNMENT, hb.ERR_DTYPE
+    for status, t in ((mism, x[0][:-1]), (mism, x[0][:, :-1]), (ali, torch.randn(hidden, tokens, device="cuda").t()), (bad, x[0].cpu()), (dty, x[0].double()), (bad, x[0][0])):
+        refused(status, lambda: layer.forward([x[0], t, x[2]], logits))
+    refused(mism, lambda: layer.forward(x[:2], logits))
+    refused(mism, lambda: layer.forward(x, logits[:2]))
+    refused(mism, lambda: layer.forward(x, [logits[0][:-1], logits[1], logits[2]]))
+    refused(mism, lambda: ExpertParallel(ex.Router(R, k), up[:2], down, tokens))
+    refused(mism, lambda: ExpertParallel(ex.Router(R, k), up, up, tokens))
+    assert all(torch.equal(a, b) for a, b in zip(layer.forward(x, logits), want))

@@ -515,7 +515,7 @@ int hccl_version(void);
  * hccl_plan_alltoallv_dynamic.
  *
  * All calls below are asynchronous on `stream`, keep no state between calls, allocate nothing and may be captured in
- * a CUDA graph. Matrices are row-major with the stated distance between rows (ld*, in elements); any distance
+ * a CUDA graph. Matrices are row-major with the stated distance between rows (ld*, in elements); any distance from a row's length on
  * and any element-aligned base address is legal unless said otherwise. Types: hccl_dtype_t. Sums, statistics and
  * scores are FP32 or 32-bit integers. No call uses atomics on floating-point data: results repeat bit for bit.
  * Zero tokens or rows are legal and launch what little is left to do.

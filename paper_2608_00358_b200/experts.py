@@ -49,7 +49,7 @@ def _matrix(t: torch.Tensor, what: str, cols: Optional[int] = None, rows: Option
     if (cols is not None and m != cols) or (rows is not None and n != rows):
         _refuse(hb.ERR_COUNT_MISMATCH, "%s is [%d, %d], expected [%s, %s]" % (what, n, m, "any" if rows is None else rows, "any" if cols is None else cols))
     ld, step = t.stride()
-    if step != 1 and m > 1:
+    if step != 1 and m > 1 and n:
         _refuse(hb.ERR_ALIGNMENT, "%s must have adjacent columns" % what)
     return ld if n > 1 else max(ld, m)
 
@@ -297,8 +297,9 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, routing: Routing, wei
 
 
 def _cols(t: torch.Tensor) -> torch.Tensor:
-    """Adjacent columns for a gradient that autograd hands over in any layout (an expanded one, say)."""
-    return t if t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
+    """Adjacent columns and rows that do not overlap, for a gradient that autograd hands over in any layout (expanded over tokens, say)."""
+    n, m = t.shape
+    return t if (t.stride(1) == 1 or m <= 1) and (t.stride(0) >= m or n <= 1) else t.contiguous()
 
 
 class _Dispatch(torch.autograd.Function):

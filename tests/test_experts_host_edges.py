@@ -101,3 +101,19 @@ def test_an_expert_layer_checks_its_experts():
             el.check_experts(router, u, d, 0)
         assert e.value.status in (hb.ERR_COUNT_MISMATCH, hb.ERR_INVALID_ARG)
     el.check_experts(router, up, down, 0)
+
+
+@pytest.mark.parametrize("T,H", [(5, 4), (5, 1), (1, 4), (1, 1), (0, 4), (4, 0)])
+def test_a_gradient_of_any_layout_gets_rows_that_the_calls_take(T, H):
+    """What autograd hands over is expanded over rows, over columns, over both, or transposed; the C calls want adjacent columns and rows that do not overlap."""
+    base = torch.arange(T * H, dtype=torch.float32).view(T, H)
+    row, col = torch.arange(H, dtype=torch.float32), torch.arange(T, dtype=torch.float32)[:, None]
+    for g in (base, row.expand(T, H), col.expand(T, H), torch.tensor(3.0).expand(T, H), base.t().contiguous().t(), torch.zeros(T, H + 3)[:, :H],
+              torch.arange(T + H + 1, dtype=torch.float32).as_strided((T, H), (1, 1))):
+        v = ex._cols(g)
+        assert torch.equal(v, g)
+        assert v.stride(1) == 1 or H <= 1 or T == 0
+        assert v.stride(0) >= H or T <= 1
+        assert ex._matrix(on_device(v), "g", H, T, 0) >= H  # (of an empty one the strides do not matter)
+    wide = torch.zeros(T, H + 3)[:, :H]
+    assert ex._cols(wide) is wide  # no copy where none is needed

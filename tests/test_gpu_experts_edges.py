@@ -10,7 +10,7 @@ import expert_reference as ref
 from paper_2608_00358_b200 import binding as hb
 from paper_2608_00358_b200 import experts as ex
 from paper_2608_00358_b200.expert_layer import ExpertParallel
-from test_gpu_experts import BF16, F16, F32, check_routing, close, cuda, gen, grid_logits, strided, weight_tol
+from test_gpu_experts import BF16, F16, F32, check_routing, close, cuda, gen, grid_logits, random_routing, strided, weight_tol
 
 pytestmark = pytest.mark.gpu
 
@@ -204,3 +204,41 @@ def test_an_expert_layer_takes_any_stride_and_refuses_other_shapes():
     refused(mism, lambda: ExpertParallel(ex.Router(R, k), up[:2], down, tokens))
     refused(mism, lambda: ExpertParallel(ex.Router(R, k), up, up, tokens))
     assert all(torch.equal(a, b) for a, b in zip(layer.forward(x, logits), want))
+
+
+# ------------------------------------------------------------------------------------------------ gradients and autograd
+@pytest.mark.parametrize("T", [0, 1, 12])
+@pytest.mark.parametrize("H", [1, 5, 64])
+@pytest.mark.parametrize("how", ["sum", "sum over tokens", "mean over tokens", "sum over columns", "transposed"])
+def test_gradients_arrive_in_any_layout(T, H, how):
+    k, E = 3, 6
+    r = random_routing(T, k, E, 3)[-1]
+    g = torch.Generator(device="cuda").manual_seed(H)
+    c = torch.randn(H, generator=g, device="cuda")
+
+    def loss(y):
+        if how == "sum":
+            return y.sum()
+        if how == "sum over tokens":
+            return (y.sum(0) * c).sum()
+        if how == "mean over tokens":
+            return (y.mean(0) * c).sum()
+        if how == "sum over columns":
+            return (y.sum(1) ** 2).sum()
+        return (y.t().contiguous() * c[:, None]).sum()
+
+    def grad_of(y):
+        z = y.detach().requires_grad_()
+        loss(z).backward()
+        return z.grad.contiguous()
+
+    x = torch.randn(T, H, generator=g, device="cuda").requires_grad_()
+    rows = ex.dispatch(x, r)
+    loss(rows).backward()
+    assert torch.equal(x.grad, ex.dispatch_backward(grad_of(rows), r))
+    v = torch.randn(T * k, H, generator=g, device="cuda").requires_grad_()
+    w = torch.randn(T, k, generator=g, device="cuda").requires_grad_()
+    y = ex.combine(v, r, weights=w)
+    loss(y).backward()
+    want_v, want_w = ex.combine_backward(grad_of(y), v.detach(), r, weights=w.detach())
+    assert torch.equal(v.grad, want_v) and torch.equal(w.grad, want_w)

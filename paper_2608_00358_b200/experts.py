@@ -19,6 +19,7 @@ import threading
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as hb
 
@@ -212,6 +213,7 @@ class _Route(torch.autograd.Function):
         return out.weights
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dweights):
         logits, bias, token_mask, _ = ctx.saved_tensors
         return ctx.router.backward(logits, ctx.routing, dweights.contiguous(), bias, token_mask), None, None, None, None
@@ -309,6 +311,7 @@ class _Dispatch(torch.autograd.Function):
         return _dispatch(x, routing, None, n_rows)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, drows):
         return dispatch_backward(_cols(drows), ctx.routing), None, None
 
@@ -321,6 +324,7 @@ class _Combine(torch.autograd.Function):
         return _combine(rows, routing, weights, None)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         rows, weights = ctx.saved_tensors
         drows, dw = combine_backward(_cols(dy), rows, ctx.routing, weights)

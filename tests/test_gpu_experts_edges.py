@@ -242,3 +242,16 @@ def test_gradients_arrive_in_any_layout(T, H, how):
     loss(y).backward()
     want_v, want_w = ex.combine_backward(grad_of(y), v.detach(), r, weights=w.detach())
     assert torch.equal(v.grad, want_v) and torch.equal(w.grad, want_w)
+
+
+def test_second_derivatives_are_refused():
+    T, E, k, H = 6, 8, 2, 16
+    router = ex.Router(E, k)
+    logits, x = torch.randn(T, E, device="cuda").requires_grad_(), torch.randn(T, H, device="cuda").requires_grad_()
+    r = router.route(logits)
+    plain = router.route(logits.detach())
+    v = torch.randn(T * k, H, device="cuda").requires_grad_()
+    for out, by in (((r.weights ** 2).sum(), logits), ((ex.dispatch(x, plain) ** 2).sum(), x), ((ex.combine(v, plain) ** 2).sum(), v)):
+        d, = torch.autograd.grad(out + (by ** 3).sum(), by, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):  # not a Hessian of the second term alone
+            (d ** 2).sum().backward()

@@ -19,6 +19,7 @@ import threading
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad as _forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import binding as hb
@@ -38,6 +39,12 @@ def _refuse(status: int, what: str):
     raise hb.HcclError(status, what)
 
 
+def _no_tangent(t: torch.Tensor, what: str):
+    """Refuses a dual number of forward-mode differentiation: the kernels would see its value alone and its tangent would be lost."""
+    if _forward_ad.unpack_dual(t).tangent is not None:
+        _refuse(hb.ERR_INVALID_ARG, "%s has a tangent; there is no forward-mode derivative" % what)
+
+
 def _matrix(t: torch.Tensor, what: str, cols: Optional[int] = None, rows: Optional[int] = None, dev: Optional[int] = None) -> int:
     """Checks a 2-d matrix with adjacent columns on CUDA device number `dev` (None: any); returns the distance between its rows."""
     try:
@@ -49,6 +56,8 @@ def _matrix(t: torch.Tensor, what: str, cols: Optional[int] = None, rows: Option
         _refuse(hb.ERR_INVALID_ARG, "%s must be on %s, not %s" % (what, "a CUDA device" if dev is None else "cuda:%d" % dev, t.device))
     if (cols is not None and m != cols) or (rows is not None and n != rows):
         _refuse(hb.ERR_COUNT_MISMATCH, "%s is [%d, %d], expected [%s, %s]" % (what, n, m, "any" if rows is None else rows, "any" if cols is None else cols))
+    if _forward_ad._current_level >= 0:
+        _no_tangent(t, what)
     ld, step = t.stride()
     if step != 1 and m > 1 and n:
         _refuse(hb.ERR_ALIGNMENT, "%s must have adjacent columns" % what)
@@ -69,6 +78,8 @@ def _vector(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int, dev: int
         _refuse(hb.ERR_COUNT_MISMATCH, "%s has %d elements, expected %d" % (what, t.numel(), numel))
     if t.get_device() != dev or not t.is_contiguous():
         _refuse(hb.ERR_INVALID_ARG, "%s must be contiguous and on cuda:%d" % (what, dev))
+    if _forward_ad._current_level >= 0:
+        _no_tangent(t, what)
 
 
 def _same_type(a: torch.Tensor, b: torch.Tensor, what: str):
@@ -76,13 +87,15 @@ def _same_type(a: torch.Tensor, b: torch.Tensor, what: str):
         _refuse(hb.ERR_DTYPE, "%s: %s and %s" % (what, a.dtype, b.dtype))
 
 
-def _on(dev: int, call, *args):
-    """call(*args, stream) with device number `dev` current."""
+def _on(dev: int, call):
+    """The call with device number `dev` current; its last argument is that device's stream."""
     if dev == _current_device():
-        call(*args, _stream(dev))
-    else:
+        return call
+
+    def there(*args):
         with torch.cuda.device(dev):
-            call(*args, _stream(dev))
+            call(*args)
+    return there
 
 
 class _Scratch(threading.local):
@@ -93,12 +106,12 @@ class _Scratch(threading.local):
     def __init__(self):
         self._of = {}
 
-    def get(self, dev: int, nbytes: int):
-        """(tensor, address) of at least nbytes on device number `dev`; hold the tensor until the call is made."""
+    def get(self, dev: int, stream: int, nbytes: int):
+        """(tensor, address) of at least nbytes on device number `dev` for a call on its current stream `stream`; hold the tensor until the call is made."""
         if _capturing():
             t = torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % dev)
             return t, t.data_ptr()
-        key = (dev, _stream(dev))
+        key = (dev, stream)
         have = self._of.get(key)
         if have is None or have[2] < nbytes:
             t = torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % dev)
@@ -173,8 +186,9 @@ class Router:
         need = self._need.get(tokens)
         if need is None:
             need = self._need[tokens] = hb.hccl_route_workspace_bytes(self.config, tokens)
-        hold, ws = self._scratch.get(dev, need)
-        _on(dev, _route, self._at, logits.data_ptr(), ld, dt, b, m, out.at, ws, need)
+        stream = _stream(dev)
+        hold, ws = self._scratch.get(dev, stream, need)
+        _on(dev, _route)(self._at, logits.data_ptr(), ld, dt, b, m, out.at, ws, need, stream)
 
     def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, token_mask: Optional[torch.Tensor] = None,
               out: Optional[Routing] = None) -> Routing:
@@ -200,7 +214,7 @@ class Router:
             _refuse(hb.ERR_COUNT_MISMATCH, "route backward: routing of %d tokens" % routing.tokens)
         _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, dev)
         out, ldd = _new(out, routing.tokens, self.experts, logits, "dlogits", dev)
-        _on(dev, _route_backward, self._at, logits.data_ptr(), ld, dt, b, m, routing.at, dweights.data_ptr(), out.data_ptr(), ldd)
+        _on(dev, _route_backward)(self._at, logits.data_ptr(), ld, dt, b, m, routing.at, dweights.data_ptr(), out.data_ptr(), ldd, _stream(dev))
         return out
 
 
@@ -241,7 +255,7 @@ def _dispatch(x, routing, out, n_rows):
     if out is None and n_rows is None:
         n_rows = routing.tokens * routing.top_k
     out, ldr = _new(out, n_rows, H, x, "rows", dev)
-    _on(dev, _c_dispatch, x.data_ptr(), ldx, H, dt, routing.at, out.data_ptr(), ldr, out.shape[0])
+    _on(dev, _c_dispatch)(x.data_ptr(), ldx, H, dt, routing.at, out.data_ptr(), ldr, out.shape[0], _stream(dev))
     return out
 
 
@@ -260,7 +274,7 @@ def dispatch_backward(drows: torch.Tensor, routing: Routing, out: Optional[torch
     ldr, dt = _matrix(drows, "drows", None, None, dev), _dtype(drows, "drows")
     n, H = drows.shape
     out, ldx = _new(out, routing.tokens, H, drows, "dx", dev)
-    _on(dev, _c_dispatch_backward, drows.data_ptr(), ldr, n, H, dt, routing.at, out.data_ptr(), ldx)
+    _on(dev, _c_dispatch_backward)(drows.data_ptr(), ldr, n, H, dt, routing.at, out.data_ptr(), ldx, _stream(dev))
     return out
 
 
@@ -270,7 +284,7 @@ def _combine(rows, routing, weights, out):
     w = _weights(weights, routing)
     n, H = rows.shape
     out, ldy = _new(out, routing.tokens, H, rows, "y", dev)
-    _on(dev, _c_combine, rows.data_ptr(), ldr, n, H, dt, routing.at, w, out.data_ptr(), ldy)
+    _on(dev, _c_combine)(rows.data_ptr(), ldr, n, H, dt, routing.at, w, out.data_ptr(), ldy, _stream(dev))
     return out
 
 
@@ -294,7 +308,7 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, routing: Routing, wei
     w = _weights(weights, routing)
     out, ldd = _new(out, n, H, rows, "drows", dev)
     dw = routing.weights.new_empty((routing.tokens, routing.top_k))
-    _on(dev, _c_combine_backward, dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.at, w, out.data_ptr(), ldd, dw.data_ptr())
+    _on(dev, _c_combine_backward)(dy.data_ptr(), ldy, rows.data_ptr(), ldr, n, H, dt, routing.at, w, out.data_ptr(), ldd, dw.data_ptr(), _stream(dev))
     return out, dw
 
 
@@ -343,7 +357,7 @@ def quantize_rows(x: torch.Tensor, routing: Optional[Routing] = None, n_rows: Op
     n = M if routing is None else (routing.tokens * routing.top_k if n_rows is None else n_rows)
     q = torch.empty((n, _pad16(K)), dtype=torch.int8, device=x.device)
     scale = torch.empty(n, dtype=torch.float32, device=x.device)
-    _on(dev, _quantize, x.data_ptr(), ldx, M, K, dt, routing.at if routing is not None else 0, q.data_ptr(), q.shape[1], n, scale.data_ptr())
+    _on(dev, _quantize)(x.data_ptr(), ldx, M, K, dt, routing.at if routing is not None else 0, q.data_ptr(), q.shape[1], n, scale.data_ptr(), _stream(dev))
     return q[:, :K], scale
 
 
@@ -419,8 +433,9 @@ class Int8Linear:
         y, ldy, y_dt = self._out(out, M, x.dtype)
         lda = _pad16(K)
         room = M * lda
-        hold, at = self._scratch.get(dev, room + 4 * M)
-        _on(dev, _linear, *self._args(M, at, lda, at + room, y_dt, y.data_ptr(), ldy, offsets), x.data_ptr(), ldx, dt, record)
+        stream = _stream(dev)
+        hold, at = self._scratch.get(dev, stream, room + 4 * M)
+        _on(dev, _linear)(*self._args(M, at, lda, at + room, y_dt, y.data_ptr(), ldy, offsets), x.data_ptr(), ldx, dt, record, stream)
         return y
 
     def matmul(self, q: torch.Tensor, q_scale: torch.Tensor, offsets: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
@@ -433,7 +448,7 @@ class Int8Linear:
         _vector(q_scale, "q_scale", torch.float32, M, self.dev)
         self._which(None, offsets)
         y, ldy, y_dt = self._out(out, M, dtype)
-        _on(self.dev, _matmul, *self._args(M, q.data_ptr(), lda if M > 1 else _pad16(lda), q_scale.data_ptr(), y_dt, y.data_ptr(), ldy, offsets))
+        _on(self.dev, _matmul)(*self._args(M, q.data_ptr(), lda if M > 1 else _pad16(lda), q_scale.data_ptr(), y_dt, y.data_ptr(), ldy, offsets), _stream(self.dev))
         return y
 
     def check(self):

@@ -5,6 +5,7 @@ import threading
 import numpy as np
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import expert_reference as ref
 from paper_2608_00358_b200 import binding as hb
@@ -255,3 +256,26 @@ def test_second_derivatives_are_refused():
         d, = torch.autograd.grad(out + (by ** 3).sum(), by, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):  # not a Hessian of the second term alone
             (d ** 2).sum().backward()
+
+
+def test_forward_mode_is_refused():
+    T, E, k, H = 6, 8, 2, 32
+    router, lin = ex.Router(E, k), ex.Int8Linear.from_float(torch.randn(16, H, device="cuda"))
+    logits, x, v, w = (torch.randn(s, device="cuda") for s in ((T, E), (T, H), (T * k, H), (T, k)))
+    r = router.route(logits)
+    bad = hb.ERR_INVALID_ARG
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))  # noqa: E731
+        refused(bad, lambda: router.route(dual(logits)))
+        refused(bad, lambda: router.route(dual(logits), out=r))
+        refused(bad, lambda: router.backward(dual(logits), r, w))
+        refused(bad, lambda: router.backward(logits, r, dual(w)))
+        refused(bad, lambda: ex.dispatch(dual(x), r))
+        refused(bad, lambda: ex.dispatch_backward(dual(v), r))
+        refused(bad, lambda: ex.combine(dual(v), r))
+        refused(bad, lambda: ex.combine(v, r, weights=dual(w)))
+        refused(bad, lambda: ex.combine_backward(dual(x), v, r))
+        refused(bad, lambda: ex.combine_backward(x, dual(v), r))
+        refused(bad, lambda: lin(dual(x)))
+        refused(bad, lambda: ex.quantize_rows(dual(x)))
+        assert torch.equal(ex.dispatch(x, r), ex.dispatch(x.clone(), r))  # what has no tangent goes through

@@ -15,7 +15,7 @@ from typing import List
 import torch
 
 from . import binding as hb
-from .experts import Int8Linear, Router, Routing, _dtype, _matrix, _pad16, _quantize, _refuse, combine
+from .experts import Int8Linear, Router, Routing, _dtype, _matrix, _no_gradient, _pad16, _quantize, _refuse, combine
 from .runtime import DeviceCollective
 
 
@@ -71,6 +71,8 @@ class ExpertParallel:
         """x[r] [tokens, hidden] and logits[r] [tokens, ranks] of every rank; returns each rank's [tokens, hidden] in bf16."""
         if len(x) != self.R or len(logits) != self.R:
             _refuse(hb.ERR_COUNT_MISMATCH, "ExpertParallel: inputs of %d and %d ranks, expected %d" % (len(x), len(logits), self.R))
+        for t in x:
+            _no_gradient(t, "x")
         rows = [(_matrix(t, "x", self.hidden, self.tokens, self.dev), _dtype(t, "x")) for t in x]
         for t in logits:
             _matrix(t, "logits", self.R, self.tokens, self.dev), _dtype(t, "logits")

@@ -45,6 +45,12 @@ def _no_tangent(t: torch.Tensor, what: str):
         _refuse(hb.ERR_INVALID_ARG, "%s has a tangent; there is no forward-mode derivative" % what)
 
 
+def _no_gradient(t: torch.Tensor, what: str):
+    """Refuses what autograd would follow: rows in 8 bits have no gradient, and a result that only looks differentiable stops training without a word."""
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(hb.ERR_INVALID_ARG, "%s requires a gradient, and 8-bit rows have none: detach it or call under torch.no_grad()" % what)
+
+
 def _matrix(t: torch.Tensor, what: str, cols: Optional[int] = None, rows: Optional[int] = None, dev: Optional[int] = None) -> int:
     """Checks a 2-d matrix with adjacent columns on CUDA device number `dev` (None: any); returns the distance between its rows."""
     try:
@@ -352,6 +358,7 @@ def _pad16(n: int) -> int:
 def quantize_rows(x: torch.Tensor, routing: Optional[Routing] = None, n_rows: Optional[int] = None):
     """(q, scale): 8-bit rows and a scale for each, x[m] ~ q[m] * scale[m]. With a routing the rows come in expert order (n_rows: the
     capacity, default tokens * top_k; rows that no choice fills are left alone). q's rows start 16 bytes apart or a multiple of it."""
+    _no_gradient(x, "x")
     ldx, dt, dev = _matrix(x, "x", dev=None if routing is None else routing.dev), _dtype(x, "x"), x.get_device()
     M, K = x.shape
     n = M if routing is None else (routing.tokens * routing.top_k if n_rows is None else n_rows)
@@ -364,7 +371,7 @@ def quantize_rows(x: torch.Tensor, routing: Optional[Routing] = None, n_rows: Op
 class Int8Linear:
     """y = x W^T (+ bias) with W in 8-bit integers and a scale for each output channel: weight [N, K], or [experts, N, K]; scale and bias
     (fp32) [N] or [experts, N]. The rows of x are quantised within the call, each with a scale of its own. Weights whose rows do not start
-    on 16-byte boundaries are laid out anew once, here. A result's rows beyond the last expert's are left alone. For serving: no gradient."""
+    on 16-byte boundaries are laid out anew once, here. A result's rows beyond the last expert's are left alone. For serving: an input that requires a gradient is refused."""
 
     def __init__(self, weight: torch.Tensor, scale: torch.Tensor, bias: Optional[torch.Tensor] = None):
         if weight.dtype != torch.int8:
@@ -423,6 +430,7 @@ class Int8Linear:
         """x [M, K]. Over experts: with a routing, x holds tokens and row r of the result belongs to choice source[r]; with offsets (int32
         [experts + 1], on the device) x is in expert order already."""
         dev, K = self.dev, self.K
+        _no_gradient(x, "x")
         ldx, dt = _matrix(x, "x", K, None, dev), _dtype(x, "x")
         self._which(routing, offsets)
         M, record = x.shape[0], 0
@@ -443,6 +451,7 @@ class Int8Linear:
         """The product alone, of rows that are in 8 bits already (quantize_rows; received from an exchange)."""
         if q.dtype != torch.int8:
             _refuse(hb.ERR_DTYPE, "Int8Linear: q is %s" % q.dtype)
+        _no_gradient(q_scale, "q_scale")
         lda = _matrix(q, "q", self.K, None, self.dev)
         M = q.shape[0]
         _vector(q_scale, "q_scale", torch.float32, M, self.dev)

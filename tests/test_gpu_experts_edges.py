@@ -200,6 +200,7 @@ def test_an_expert_layer_takes_any_stride_and_refuses_other_shapes():
     for status, t in ((mism, x[0][:-1]), (mism, x[0][:, :-1]), (ali, torch.randn(hidden, tokens, device="cuda").t()), (bad, x[0].cpu()), (dty, x[0].double()), (bad, x[0][0])):
         refused(status, lambda: layer.forward([x[0], t, x[2]], logits))
     refused(mism, lambda: layer.forward(x[:2], logits))
+    refused(bad, lambda: layer.forward([x[0], x[1], x[2].clone().requires_grad_()], logits))
     refused(mism, lambda: layer.forward(x, logits[:2]))
     refused(mism, lambda: layer.forward(x, [logits[0][:-1], logits[1], logits[2]]))
     refused(mism, lambda: ExpertParallel(ex.Router(R, k), up[:2], down, tokens))
@@ -279,3 +280,15 @@ def test_forward_mode_is_refused():
         refused(bad, lambda: lin(dual(x)))
         refused(bad, lambda: ex.quantize_rows(dual(x)))
         assert torch.equal(ex.dispatch(x, r), ex.dispatch(x.clone(), r))  # what has no tangent goes through
+
+
+def test_a_linear_layer_without_a_gradient_says_so():
+    lin = ex.Int8Linear.from_float(torch.randn(16, 32, device="cuda"))
+    x = torch.randn(4, 32, device="cuda").requires_grad_()
+    refused(hb.ERR_INVALID_ARG, lambda: lin(x))
+    refused(hb.ERR_INVALID_ARG, lambda: ex.quantize_rows(x))
+    q, scale = ex.quantize_rows(x.detach())
+    refused(hb.ERR_INVALID_ARG, lambda: lin.matmul(q, scale.clone().requires_grad_()))
+    with torch.no_grad():
+        y = lin(x)
+    assert torch.equal(y, lin(x.detach())) and not y.requires_grad

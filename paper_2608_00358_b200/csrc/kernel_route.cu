@@ -210,7 +210,7 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
                     k1 = fmaxf(k1, o1);
                 }
                 const int q = i * L + l;
-                if ((l & (p.segment - 1)) == 0 && q * 4 < p.E) gscore[q >> (31 - __clz(p.segment))] = group_score(k1, k2);
+                if ((l & (p.segment - 1)) == 0 && q * 4 < p.E) gscore[q >> (31 - __clz(p.segment))] = (p.group_best == 2 && k2 != -INFINITY) ? k1 + k2 : k1;
             }
         } else {
             __syncwarp();
@@ -661,16 +661,9 @@ __global__ void __launch_bounds__(256) hccl_route_grad(const __grid_constant__ R
         }
         if (p.renorm) {
             // By the weights c / S: (dw - sum dw c / S) / S would leave the range for sigmoids near 0, times c it is of the size of dw.
-            const float S = lanes_sum<L>(sc);
-            sdc = 0.f;
+            const float S = lanes_sum<L>(sc), D = lanes_sum<L>(sdc), r1 = S > 0.f ? 1.f / S : 0.f;
 #pragma unroll
-            for (int r = 0; r < R; r++) {
-                x[r] = S > 0.f ? c[r] / S : 0.f;
-                sdc += dw[r] * x[r];
-            }
-            const float D = lanes_sum<L>(sdc);
-#pragma unroll
-            for (int r = 0; r < R; r++) dw[r] = (dw[r] - D) * x[r];
+            for (int r = 0; r < R; r++) dw[r] = (dw[r] - D * r1) * (c[r] * r1);
         } else if (whole_row) {
             const float r1 = total > 0.f ? 1.f / total : 0.f;
             dot = lanes_sum<L>(sdc) * r1;
@@ -819,7 +812,9 @@ cudaError_t launch_route(int dt, const RouteParams& in, cudaStream_t s) {
     p.magic = ((1 << 20) + p.per_group - 1) / p.per_group;
     const int es = dt == HCCL_FP32 ? 4 : 2;
     const int quads = p.per_group / 4;
-    p.segment = p.per4 && quads <= c.lanes && (quads & (quads - 1)) == 0 ? quads : 0;
+    // (Sums of two scores without a bias are formed in the other walk alone: once in the code instead of once for each quad of a lane, which a single token would wait for.)
+    const bool sums_of_scores = p.group_best == 2 && !p.bias;
+    p.segment = p.per4 && quads <= c.lanes && (quads & (quads - 1)) == 0 && !sums_of_scores ? quads : 0;
     p.vec = aligned_rows(p.logits, p.ld, es, 4 * es) && p.E % 4 == 0;
     if (dt == HCCL_FP32) return route_sizes<float>(p, c.lanes, s);
     if (dt == HCCL_BF16) return route_sizes<__nv_bfloat16>(p, c.lanes, s);

@@ -560,7 +560,9 @@ typedef struct {
  * eligible experts than top_k gets ids -1 and weights 0 in the places left over; one with none gets them everywhere.
  * A token that cannot be scored (an eligible logit or bias is NaN, a bias is +inf, or a logit is +inf under softmax) gets ids -1 and weights NaN.
  * Renormalised softmax weights are a softmax over the chosen, however far below the others a bias chose; chosen sigmoids that are all 0 keep weight 0. tokens * top_k < 2^31.
- * Workspace: hccl_route_workspace_bytes, 16-byte aligned, contents arbitrary; not shared by calls in flight at once. */
+ * Workspace: hccl_route_workspace_bytes, 16-byte aligned, contents arbitrary; not shared by calls in flight at once. HCCL_ROUTE_NO_WORKSPACE bytes
+ * are asked for where the call has no use for any (so few tokens that one block does everything): they are not touched, and any number of calls may name the same. */
+#define HCCL_ROUTE_NO_WORKSPACE 16
 hccl_status_t hccl_route_workspace_bytes(const hccl_router_t*, int64_t tokens, size_t* bytes);
 hccl_status_t hccl_route(const hccl_router_t*, const void* logits, int64_t ld, hccl_dtype_t dt, const float* bias,
                          const uint8_t* token_mask, const hccl_routing_t* out, void* workspace, size_t bytes, void* stream);

@@ -30,6 +30,7 @@ NOALLOC_WORKSPACE_BYTES = 8 << 20
 ELEM_BYTES = {FP32: 4, BF16: 2, FP16: 2}
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 MAX_EXPERTS, MAX_TOP_K, MAX_I8_K = 1024, 32, 131071
+ROUTE_NO_WORKSPACE = 16
 
 
 class Opts(C.Structure):

@@ -799,7 +799,7 @@ bool aligned_rows(const void* at, long long ld, int es, int bytes) { return (uin
 
 size_t route_workspace(int E, long long tokens) {
     const Cut c = cut(tokens, E);
-    return c.chunks > 1 ? (size_t)c.chunks * round_up(E, 16) : 16;  // never nothing: one rule for callers
+    return c.chunks > 1 ? (size_t)c.chunks * round_up(E, 16) : HCCL_ROUTE_NO_WORKSPACE;  // (more than one chunk: more than that)
 }
 
 cudaError_t launch_route(int dt, const RouteParams& in, cudaStream_t s) {

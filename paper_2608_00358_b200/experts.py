@@ -31,6 +31,7 @@ _quantize, _matmul, _linear = hb.packed("hccl_quantize_rows_i8"), hb.packed("hcc
 _DT = {torch.float32: hb.FP32, torch.bfloat16: hb.BF16, torch.float16: hb.FP16}
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _capturing = torch._C._cuda_isCurrentStreamCapturing if hasattr(torch._C, "_cuda_isCurrentStreamCapturing") else torch.cuda.is_current_stream_capturing
+_written = torch._C._increment_version if hasattr(torch._C, "_increment_version") else torch.autograd.graph.increment_version  # of a tuple of tensors
 _stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -49,6 +50,13 @@ def _no_gradient(t: torch.Tensor, what: str):
     """Refuses what autograd would follow: rows in 8 bits have no gradient, and a result that only looks differentiable stops training without a word."""
     if t.requires_grad and torch.is_grad_enabled():
         _refuse(hb.ERR_INVALID_ARG, "%s requires a gradient, and 8-bit rows have none: detach it or call under torch.no_grad()" % what)
+
+
+def _given(t: torch.Tensor, what: str):
+    """A caller's output is about to be written: autograd, which may hold it for a gradient, is to know as it does of torch's own writes."""
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(hb.ERR_INVALID_ARG, "%s: an output that requires a gradient" % what)
+    _written((t,))
 
 
 def _matrix(t: torch.Tensor, what: str, cols: Optional[int] = None, rows: Optional[int] = None, dev: Optional[int] = None) -> int:
@@ -162,6 +170,12 @@ class Router:
         self._at = C.addressof(self.config)
         self._scratch = _Scratch()
         self._need = {}  # workspace bytes by number of tokens
+        self._untouched = {}  # by device, what calls get that have no use for a workspace
+
+    def _some(self, dev: int):
+        t = torch.empty(hb.ROUTE_NO_WORKSPACE, dtype=torch.uint8, device="cuda:%d" % dev)
+        have = self._untouched[dev] = (t, t.data_ptr())
+        return have
 
     def outputs(self, tokens: int, device="cuda") -> Routing:
         """Memory for one routing of `tokens` tokens, to be given as out=."""
@@ -170,30 +184,33 @@ class Router:
                        torch.empty(self.experts, dtype=torch.int64, device=device), torch.empty(self.experts + 1, **i32),
                        torch.empty(n, **i32), torch.empty(tokens * self.top_k, **i32))
 
-    def _inputs(self, logits, bias, token_mask, dev):
-        ld = _matrix(logits, "logits", self.experts, None, dev)
+    def _inputs(self, logits, bias, token_mask, tokens, dev):
+        ld = _matrix(logits, "logits", self.experts, tokens, dev)
         dt = _dtype(logits, "logits")
         b = m = 0
         if bias is not None:
-            _vector(bias, "bias", torch.float32, self.experts, logits.get_device())
+            _vector(bias, "bias", torch.float32, self.experts, dev)
             b = bias.data_ptr()
         if token_mask is not None:
             if token_mask.dtype == torch.bool:
                 token_mask = token_mask.view(torch.uint8)
-            _vector(token_mask, "token_mask", torch.uint8, logits.shape[0], logits.get_device())
+            _vector(token_mask, "token_mask", torch.uint8, tokens, dev)
             m = token_mask.data_ptr()
         return ld, dt, b, m
 
     def _run(self, logits, bias, token_mask, out):
         dev, tokens = out.dev, out.tokens
-        ld, dt, b, m = self._inputs(logits, bias, token_mask, dev)
-        if tokens != logits.shape[0] or out.experts != self.experts or out.top_k != self.top_k:
+        ld, dt, b, m = self._inputs(logits, bias, token_mask, tokens, dev)
+        if out.experts != self.experts or out.top_k != self.top_k:
             _refuse(hb.ERR_COUNT_MISMATCH, "route: out is for %d tokens, %d experts, top %d" % (tokens, out.experts, out.top_k))
         need = self._need.get(tokens)
         if need is None:
             need = self._need[tokens] = hb.hccl_route_workspace_bytes(self.config, tokens)
         stream = _stream(dev)
-        hold, ws = self._scratch.get(dev, stream, need)
+        if need <= hb.ROUTE_NO_WORKSPACE:
+            hold, ws = self._untouched.get(dev) or self._some(dev)
+        else:
+            hold, ws = self._scratch.get(dev, stream, need)
         _on(dev, _route)(self._at, logits.data_ptr(), ld, dt, b, m, out.at, ws, need, stream)
 
     def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, token_mask: Optional[torch.Tensor] = None,
@@ -208,16 +225,19 @@ class Router:
             return Routing(out.ids, w, out.counts, out.offsets, out.slots, out.source)
         if out is None:
             out = self.outputs(logits.shape[0], logits.device)
+            self._run(logits, bias, token_mask, out)
+            return out
+        if out.weights.requires_grad and torch.is_grad_enabled():
+            _refuse(hb.ERR_INVALID_ARG, "route: out= has weights that carry a gradient")
         self._run(logits, bias, token_mask, out)
+        _written((out.ids, out.weights, out.counts, out.offsets, out.slots, out.source))
         return out
 
     def backward(self, logits: torch.Tensor, routing: Routing, dweights: torch.Tensor, bias: Optional[torch.Tensor] = None,
                  token_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Gradient of the logits for a gradient of the weights (fp32 [tokens, top_k])."""
         dev = routing.dev
-        ld, dt, b, m = self._inputs(logits, bias, token_mask, dev)
-        if routing.tokens != logits.shape[0]:
-            _refuse(hb.ERR_COUNT_MISMATCH, "route backward: routing of %d tokens" % routing.tokens)
+        ld, dt, b, m = self._inputs(logits, bias, token_mask, routing.tokens, dev)
         _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, dev)
         out, ldd = _new(out, routing.tokens, self.experts, logits, "dlogits", dev)
         _on(dev, _route_backward)(self._at, logits.data_ptr(), ld, dt, b, m, routing.at, dweights.data_ptr(), out.data_ptr(), ldd, _stream(dev))
@@ -244,7 +264,9 @@ def _new(out, rows, cols, like, what, dev):
     if out is None:
         return like.new_empty((rows, cols)), cols
     _same_type(out, like, what)
-    return out, _matrix(out, what, cols, rows, dev)
+    ld = _matrix(out, what, cols, rows, dev)
+    _given(out, what)
+    return out, ld
 
 
 def _weights(weights, routing) -> int:
@@ -327,26 +349,28 @@ def _cols(t: torch.Tensor) -> torch.Tensor:
 class _Dispatch(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, routing, n_rows):
+        ctx.save_for_backward(routing.slots)  # for torch's check alone: a routing that was routed into again has no gradient to give
         ctx.routing = routing
         return _dispatch(x, routing, None, n_rows)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, drows):
+        ctx.saved_tensors
         return dispatch_backward(_cols(drows), ctx.routing), None, None
 
 
 class _Combine(torch.autograd.Function):
     @staticmethod
     def forward(ctx, rows, weights, routing):
-        ctx.save_for_backward(rows, weights)
+        ctx.save_for_backward(rows, weights, routing.slots, routing.offsets)
         ctx.routing = routing
         return _combine(rows, routing, weights, None)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        rows, weights = ctx.saved_tensors
+        rows, weights, _, _ = ctx.saved_tensors
         drows, dw = combine_backward(_cols(dy), rows, ctx.routing, weights)
         return drows, dw.view_as(weights), None
 
@@ -415,7 +439,9 @@ class Int8Linear:
             if dtype not in _DT:
                 _refuse(hb.ERR_DTYPE, "Int8Linear: result in %s" % dtype)
             return torch.empty((M, self.N), dtype=dtype, device=self.device), self.N, _DT[dtype]
-        return out, _matrix(out, "out", self.N, M, self.dev), _dtype(out, "out")
+        ldy, dt = _matrix(out, "out", self.N, M, self.dev), _dtype(out, "out")
+        _given(out, "out")
+        return out, ldy, dt
 
     def _which(self, routing, offsets):
         if self.experts and (routing is None) == (offsets is None):

@@ -292,3 +292,76 @@ def test_a_linear_layer_without_a_gradient_says_so():
     with torch.no_grad():
         y = lin(x)
     assert torch.equal(y, lin(x.detach())) and not y.requires_grad
+
+
+def test_writes_through_out_are_seen_by_autograd():
+    T, E, k, H = 10, 8, 2, 32
+    router, lin = ex.Router(E, k), ex.Int8Linear.from_float(torch.randn(16, H, device="cuda"))
+    logits, x, v, w = (torch.randn(s, device="cuda") for s in ((T, E), (T, H), (T * k, H), (T, k)))
+    r = router.route(logits)
+
+    def bumped(tensors, call):
+        before = [t._version for t in tensors]
+        call()
+        assert all(t._version > b for t, b in zip(tensors, before))
+
+    bumped([r.ids, r.weights, r.counts, r.offsets, r.slots, r.source], lambda: router.route(logits, out=r))
+    dl, y, dx, rows, lo = torch.empty_like(logits), torch.empty_like(x), torch.empty_like(x), torch.empty_like(v), torch.empty(T, 16, device="cuda")
+    q, s = ex.quantize_rows(x)
+    bumped([dl], lambda: router.backward(logits, r, w, out=dl))
+    bumped([rows], lambda: ex.dispatch(x, r, out=rows))
+    bumped([dx], lambda: ex.dispatch_backward(v, r, out=dx))
+    bumped([y], lambda: ex.combine(v, r, out=y))
+    bumped([rows], lambda: ex.combine_backward(x, v, r, out=rows))
+    bumped([lo], lambda: lin(x, out=lo))
+    bumped([lo], lambda: lin.matmul(q, s, out=lo))
+    # a buffer that autograd holds: torch refuses the gradient
+    p = torch.ones(T, 1, device="cuda").requires_grad_()
+    z = y * p
+    ex.combine(v, r, out=y)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        z.sum().backward()
+    with torch.inference_mode():
+        buf = torch.empty(T, H, device="cuda")
+        ex.combine(v, r, out=buf)
+        router.route(logits, out=router.outputs(T))
+    ex.combine(v, r, out=buf)  # has no version to count
+    # an output that is part of a graph itself
+    refused(hb.ERR_INVALID_ARG, lambda: ex.combine(v, r, out=torch.empty(T, H, device="cuda").requires_grad_()))
+    refused(hb.ERR_INVALID_ARG, lambda: router.route(logits, out=router.route(logits.clone().requires_grad_())))
+    with torch.no_grad():
+        ex.combine(v, r, out=torch.empty(T, H, device="cuda").requires_grad_())
+
+
+@pytest.mark.parametrize("T,E", [(1, 8), (32, 1024), (128, 64), (129, 64), (33, 1024), (17, 200)])
+def test_calls_that_need_no_workspace_touch_none(T, E):
+    """Up to some 128 tokens one block does everything; the workspace it is given stays as it was, whichever call that is."""
+    logits = torch.randn(T, E, device="cuda")
+    router = ex.Router(E, 2)
+    out = router.outputs(T)
+    need = hb.hccl_route_workspace_bytes(router.config, T)
+    assert need >= hb.ROUTE_NO_WORKSPACE
+    ws = torch.full((need,), 0xa5, dtype=torch.uint8, device="cuda")
+    ex._route(router._at, logits.data_ptr(), E, hb.FP32, 0, 0, out.at, ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+    assert (need == hb.ROUTE_NO_WORKSPACE) == bool((ws == 0xa5).all())
+    r = router.route(logits)
+    assert torch.equal(r.source, out.source) and torch.equal(r.weights, out.weights)
+
+
+@pytest.mark.parametrize("what", ["dispatch", "combine"])
+def test_a_routing_that_is_routed_into_again_refuses_its_gradient(what):
+    T, E, k, H = 10, 8, 2, 32
+    router = ex.Router(E, k)
+    a, b = torch.randn(T, E, device="cuda"), torch.randn(T, E, device="cuda")
+    r = router.outputs(T)
+    x, v = torch.randn(T, H, device="cuda").requires_grad_(), torch.randn(T * k, H, device="cuda").requires_grad_()
+
+    def forward():
+        return ex.dispatch(x, r) if what == "dispatch" else ex.combine(v, r, weights=torch.ones(T, k, device="cuda"))
+
+    router.route(a, out=r)
+    forward().sum().backward()  # in order: nothing to refuse
+    y = forward()
+    router.route(b, out=r)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()

@@ -236,11 +236,13 @@ class Router:
     def backward(self, logits: torch.Tensor, routing: Routing, dweights: torch.Tensor, bias: Optional[torch.Tensor] = None,
                  token_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Gradient of the logits for a gradient of the weights (fp32 [tokens, top_k])."""
-        dev = routing.dev
-        ld, dt, b, m = self._inputs(logits, bias, token_mask, routing.tokens, dev)
-        _vector(dweights, "dweights", torch.float32, routing.tokens * routing.top_k, dev)
-        out, ldd = _new(out, routing.tokens, self.experts, logits, "dlogits", dev)
-        _on(dev, _route_backward)(self._at, logits.data_ptr(), ld, dt, b, m, routing.at, dweights.data_ptr(), out.data_ptr(), ldd, _stream(dev))
+        return self._gradient(logits, routing.at, routing.tokens, routing.top_k, routing.dev, dweights, bias, token_mask, out)
+
+    def _gradient(self, logits, routing_at, tokens, top_k, dev, dweights, bias, token_mask, out):
+        ld, dt, b, m = self._inputs(logits, bias, token_mask, tokens, dev)
+        _vector(dweights, "dweights", torch.float32, tokens * top_k, dev)
+        out, ldd = _new(out, tokens, self.experts, logits, "dlogits", dev)
+        _on(dev, _route_backward)(self._at, logits.data_ptr(), ld, dt, b, m, routing_at, dweights.data_ptr(), out.data_ptr(), ldd, _stream(dev))
         return out
 
 
@@ -248,15 +250,18 @@ class _Route(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, router, bias, token_mask, out):
         router._run(logits, bias, token_mask, out)
+        # Not `out` itself: its weights are this function's result and would hold on to it, a cycle that only the collector frees.
         ctx.save_for_backward(logits, bias, token_mask, out.ids)
-        ctx.router, ctx.routing = router, out
+        ctx.router = router
         return out.weights
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dweights):
-        logits, bias, token_mask, _ = ctx.saved_tensors
-        return ctx.router.backward(logits, ctx.routing, dweights.contiguous(), bias, token_mask), None, None, None, None
+        logits, bias, token_mask, ids = ctx.saved_tensors
+        tokens, top_k = ids.shape
+        record = hb.RoutingRecord(tokens, top_k, ctx.router.experts, ids.data_ptr())  # the gradient reads the ids alone
+        return ctx.router._gradient(logits, C.addressof(record), tokens, top_k, ids.get_device(), dweights.contiguous(), bias, token_mask, None), None, None, None, None
 
 
 def _new(out, rows, cols, like, what, dev):

@@ -1,6 +1,8 @@
 """Expert-layer operators where it is easy to go wrong: rows with nothing left, groups by sums of scores, scores at the ends of their range, many experts in
 many groups, gradients of every layout, autograd's own rules, host threads, and the sizes at which another kernel or another turn of a loop takes over."""
+import gc
 import threading
+import weakref
 
 import numpy as np
 import pytest
@@ -365,3 +367,19 @@ def test_a_routing_that_is_routed_into_again_refuses_its_gradient(what):
     router.route(b, out=r)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.sum().backward()
+
+
+def test_a_training_step_leaves_nothing_for_the_collector():
+    router, logits = ex.Router(16, 2), torch.randn(40, 16, device="cuda").requires_grad_()
+    gc.collect()
+    gc.disable()
+    try:
+        for step in ("with backward", "without"):
+            r = router.route(logits)
+            held = [weakref.ref(t) for t in (r.ids, r.weights, r.source)]
+            if step == "with backward":
+                (r.weights ** 2).sum().backward()
+            del r
+            assert [h() for h in held] == [None] * 3, step
+    finally:
+        gc.enable()

@@ -113,8 +113,8 @@ def _on(dev: int, call):
 
 
 class _Scratch(threading.local):
-    """Device memory of one object, one piece for each host thread and stream it is used on. Calls on different streams do not share it, nor do threads on one stream: a
-    call makes up to two launches, and another thread's may come between them. A call that is captured
+    """Device memory for the calls' own use, one piece for each host thread and stream. What a call leaves there, the next call on that stream may write over, whichever object makes it. Calls on different
+    streams do not share a piece, nor do threads on one stream: a call makes up to two launches, and another thread's may come between them. A call that is captured
     into a CUDA graph gets memory of the graph's own, since the graph may be replayed on any stream, beside later calls."""
 
     def __init__(self):
@@ -131,6 +131,9 @@ class _Scratch(threading.local):
             t = torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % dev)
             have = self._of[key] = (t, t.data_ptr(), nbytes)
         return have[:2]
+
+
+_scratch = _Scratch()
 
 
 class Routing:
@@ -168,7 +171,6 @@ class Router:
         hb.hccl_route_workspace_bytes(self.config, 0)  # refuses a configuration that does not hold together
         self.experts, self.top_k = experts, top_k
         self._at = C.addressof(self.config)
-        self._scratch = _Scratch()
         self._need = {}  # workspace bytes by number of tokens
         self._untouched = {}  # by device, what calls get that have no use for a workspace
 
@@ -210,7 +212,7 @@ class Router:
         if need <= hb.ROUTE_NO_WORKSPACE:
             hold, ws = self._untouched.get(dev) or self._some(dev)
         else:
-            hold, ws = self._scratch.get(dev, stream, need)
+            hold, ws = _scratch.get(dev, stream, need)
         _on(dev, _route)(self._at, logits.data_ptr(), ld, dt, b, m, out.at, ws, need, stream)
 
     def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, token_mask: Optional[torch.Tensor] = None,
@@ -420,7 +422,6 @@ class Int8Linear:
             weight = padded
         self.weight, self.scale, self.bias = weight, scale, bias
         self.ldw = weight.shape[-1]
-        self._scratch = _Scratch()
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._fixed = (weight.data_ptr(), self.ldw, scale.data_ptr(), bias.data_ptr() if bias is not None else 0)
         self._status_at = self._status.data_ptr()
@@ -473,7 +474,7 @@ class Int8Linear:
         lda = _pad16(K)
         room = M * lda
         stream = _stream(dev)
-        hold, at = self._scratch.get(dev, stream, room + 4 * M)
+        hold, at = _scratch.get(dev, stream, room + 4 * M)
         _on(dev, _linear)(*self._args(M, at, lda, at + room, y_dt, y.data_ptr(), ldy, offsets), x.data_ptr(), ldx, dt, record, stream)
         return y
 

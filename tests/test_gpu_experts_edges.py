@@ -383,3 +383,18 @@ def test_a_training_step_leaves_nothing_for_the_collector():
             assert [h() for h in held] == [None] * 3, step
     finally:
         gc.enable()
+
+
+def test_layers_of_one_thread_share_their_scratch():
+    K, N, M = 2048, 64, 4096
+    lins = [ex.Int8Linear.from_float(torch.randn(N, K, device="cuda")) for _ in range(4)]
+    x, y = torch.randn(M, K, device="cuda"), torch.empty(M, N, device="cuda")
+    want = [lin(x) for lin in lins]
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for lin in lins:
+        lin(x, out=y)
+    more = [ex.Int8Linear(lin.weight, lin.scale) for lin in lins]
+    got = [lin(x) for lin in more]
+    assert torch.cuda.memory_allocated() - before < 4 * (M * N * 4 + 1024)  # the results and the status words, no rows in 8 bits
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -157,6 +157,9 @@ class Routing:
                                        offsets.data_ptr(), slots.data_ptr(), source.data_ptr())
         self.at = C.addressof(self.record)
 
+    def __reduce__(self):  # copies and pickles are made from the tensors: the record holds addresses
+        return Routing, (self.ids, self.weights, self.counts, self.offsets, self.slots, self.source)
+
 
 class Router:
     """How tokens choose experts (hccl_router_t). score "softmax" or "sigmoid"; groups > 1: only the experts of the top_groups best
@@ -170,9 +173,13 @@ class Router:
                                       1 if renormalise else 0, scale)
         hb.hccl_route_workspace_bytes(self.config, 0)  # refuses a configuration that does not hold together
         self.experts, self.top_k = experts, top_k
+        self._made_of = (experts, top_k, score, groups, top_groups, group_best, renormalise, scale)
         self._at = C.addressof(self.config)
         self._need = {}  # workspace bytes by number of tokens
         self._untouched = {}  # by device, what calls get that have no use for a workspace
+
+    def __reduce__(self):  # a copy has a configuration, and its address, of its own
+        return Router, self._made_of
 
     def _some(self, dev: int):
         t = torch.empty(hb.ROUTE_NO_WORKSPACE, dtype=torch.uint8, device="cuda:%d" % dev)
@@ -425,6 +432,9 @@ class Int8Linear:
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._fixed = (weight.data_ptr(), self.ldw, scale.data_ptr(), bias.data_ptr() if bias is not None else 0)
         self._status_at = self._status.data_ptr()
+
+    def __reduce__(self):  # a copy has weights, and their addresses, of its own
+        return Int8Linear, (self.weight[..., : self.K], self.scale, self.bias)
 
     @classmethod
     def from_float(cls, weight: torch.Tensor, bias: Optional[torch.Tensor] = None) -> "Int8Linear":

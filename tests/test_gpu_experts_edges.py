@@ -1,6 +1,8 @@
 """Expert-layer operators where it is easy to go wrong: rows with nothing left, groups by sums of scores, scores at the ends of their range, many experts in
 many groups, gradients of every layout, autograd's own rules, host threads, and the sizes at which another kernel or another turn of a loop takes over."""
+import copy
 import gc
+import pickle
 import threading
 import weakref
 
@@ -398,3 +400,22 @@ def test_layers_of_one_thread_share_their_scratch():
     got = [lin(x) for lin in more]
     assert torch.cuda.memory_allocated() - before < 4 * (M * N * 4 + 1024)  # the results and the status words, no rows in 8 bits
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_copies_have_addresses_of_their_own():
+    logits, x, w = torch.randn(9, 8, device="cuda"), torch.randn(9, 40, device="cuda"), torch.randn(8, 24, 40, device="cuda")
+    router, lin = ex.Router(8, 3, score="sigmoid", groups=4, top_groups=2, group_best=2, renormalise=False, scale=2.5), ex.Int8Linear.from_float(w, torch.randn(8, 24, device="cuda"))
+    r = router.route(logits)
+    y = lin(x, routing=r)
+    used = int(r.offsets[-1])
+    for make in (copy.copy, copy.deepcopy, lambda o: pickle.loads(pickle.dumps(o))):
+        router2, lin2 = make(router), make(lin)
+        assert router2._at != router._at and router2.config is not router.config
+        if make is not copy.copy:
+            assert lin2.weight.data_ptr() != lin.weight.data_ptr() and lin2._fixed[0] == lin2.weight.data_ptr()
+        r2 = router2.route(logits)
+        assert torch.equal(r2.ids, r.ids) and torch.equal(r2.weights, r.weights)
+        assert torch.equal(lin2(x, routing=r2)[:used], y[:used])
+    r3 = copy.deepcopy(r)
+    assert r3.slots.data_ptr() != r.slots.data_ptr() and r3.record.slots == r3.slots.data_ptr()
+    assert torch.equal(lin(x, routing=r3)[:used], y[:used])

@@ -81,6 +81,14 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
     return r;
 }
 
+// Two scores added up from their logits k1 >= k2 (k2 may be -inf), m the token's largest: without a bias logits stand in the place of keys, which have the scores' order, but it is the scores that
+// are added up. Softmax: by the logarithm of exp(k1) + exp(k2), over exp(m), so that a sum far below the largest does not vanish. Not inlined: seldom asked for, and
+// a call for few tokens waits for its instructions (one token of 256 experts 4.72 us against 4.78).
+__device__ __noinline__ float two_scores(float k1, float k2, float m, int sigmoid) {
+    if (sigmoid) return 1.f / (1.f + expf(-k1)) + 1.f / (1.f + expf(-k2));
+    return fmaxf((k1 - m) + log1pf(expf(k2 - k1)), -FLT_MAX);  // -inf is for groups without experts
+}
+
 // One token for each L lanes. keys: this token's shared memory (token_floats). sbias: the bias in shared memory, up to a multiple of 4 experts; odd: some of
 // it is infinite or NaN. Writes ids and weights (ids to `kept` too, shared, unless null), counts the chosen in hist.
 template <typename T, int Q, int L>
@@ -184,12 +192,9 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
 #pragma unroll
     for (int i = 0; i < Q; i++)
         if ((i * L + l) * 4 < p.E) *(float4*)(keys + (i * L + l) * 4) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
-    // A group's score from its two largest keys. Logits in the place of keys (no bias) have the scores' order, but it is the scores that are
-    // added up. Softmax: by the logarithm of exp(k1) + exp(k2), over exp(m): a sum far below the largest does not vanish, and -inf stays for groups without experts.
     const auto group_score = [&](float k1, float k2) {
         if (p.group_best != 2 || k1 == -INFINITY) return k1;
-        if (!p.bias && p.sigmoid) return 1.f / (1.f + expf(-k1)) + 1.f / (1.f + expf(-k2));
-        if (!p.bias) return fmaxf((k1 - m) + log1pf(expf(k2 - k1)), -FLT_MAX);
+        if (!p.bias) return two_scores(k1, k2, m, p.sigmoid);
         return k2 == -INFINITY ? k1 : k1 + k2;
     };
     float top[Q];
@@ -322,28 +327,31 @@ __device__ __forceinline__ void choose_token(const RouteParams& p, long long t, 
     for (int r = 0; r < R; r++) {
         const int k = r * L + l;
         id[r] = k < p.K ? chosen[k] : -1;
-        s[r] = id[r] >= 0 ? to_f32<T>(row[id[r]]) : -INFINITY;
+        float v = p.sigmoid ? -INFINITY : m;
+        if (id[r] >= 0) v = to_f32<T>(row[id[r]]);
+        s[r] = p.sigmoid ? 1.f / (1.f + expf(-v)) : expf(v - m);  // softmax: the common divisor drops out of renormalised weights
+        s[r] = id[r] >= 0 ? s[r] : 0.f;
+        sum += s[r];
         if (r * L + L >= p.K) {
 #pragma unroll
             for (int q = 0; q < R; q++)
-                if (q > r) id[q] = -1, s[q] = -INFINITY;
+                if (q > r) id[q] = -1, s[q] = 0.f;
             break;
         }
     }
-    // Softmax: over the row's largest logit; renormalised weights beside a bias, which may choose scores that are 0 against it, over the largest chosen one (the common
-    // divisor drops out, and the gradient does the same). Without a bias that is the row's, or, with groups, close to it.
-    float base = m;
     if (!p.sigmoid && p.renorm && p.bias) {
-        base = s[0];
+        // A bias may choose scores that are 0 against the row's largest: over the largest chosen one, as the gradient does. (Without a bias that is the row's, or, with groups, close to it.)
+        float base = -INFINITY;
 #pragma unroll
-        for (int r = 1; r < R; r++) base = fmaxf(base, s[r]);
+        for (int r = 0; r < R; r++)
+            if (id[r] >= 0) base = fmaxf(base, to_f32<T>(row[id[r]]));
         base = lanes_max<L>(base);
-    }
+        sum = 0.f;
 #pragma unroll
-    for (int r = 0; r < R; r++) {
-        if (r * L < p.K) s[r] = p.sigmoid ? 1.f / (1.f + expf(-s[r])) : expf(s[r] - base);
-        s[r] = id[r] >= 0 ? s[r] : 0.f;
-        sum += s[r];
+        for (int r = 0; r < R; r++) {
+            s[r] = id[r] >= 0 ? expf(to_f32<T>(row[id[r]]) - base) : 0.f;
+            sum += s[r];
+        }
     }
     const float div = p.renorm ? lanes_sum<L>(sum) : total;
     if (in) {

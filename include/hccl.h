@@ -624,6 +624,15 @@ hccl_status_t hccl_matmul_i8(const hccl_matmul_i8_t*, void* stream);
  * expert e (groups = routing->experts, offsets = routing->offsets, M the rows of y and of the scratch). */
 hccl_status_t hccl_linear_i8(const hccl_matmul_i8_t*, const void* x, int64_t ldx, hccl_dtype_t x_dt, const hccl_routing_t* routing, void* stream);
 
+/* The expert-layer calls with their arguments as one array of 64-bit integers in the same order (pointers as addresses; in the place of an hccl_matmul_i8_t its
+ * fields one by one), for bindings to which each argument costs. The names carry the number of arguments in their second byte. Refusals are the call's own;
+ * any other value of `call` is refused. */
+typedef enum {
+    HCCL_CALL_ROUTE = 0x0a00, HCCL_CALL_ROUTE_BACKWARD = 0x0b01, HCCL_CALL_DISPATCH = 0x0902, HCCL_CALL_DISPATCH_BACKWARD = 0x0903, HCCL_CALL_COMBINE = 0x0a04,
+    HCCL_CALL_COMBINE_BACKWARD = 0x0d05, HCCL_CALL_QUANTIZE_ROWS_I8 = 0x0b06, HCCL_CALL_MATMUL_I8 = 0x1107, HCCL_CALL_LINEAR_I8 = 0x1508
+} hccl_call_t;
+hccl_status_t hccl_call_packed(int32_t call, const int64_t* arguments);
+
 /* ------------------------------------------------------------------------
  * Plan verification on the host (debugging aids for schedules; never part of hccl_execute).
  * ------------------------------------------------------------------------ */

@@ -175,7 +175,7 @@ EXPORTS = ["hccl_plan_allreduce", "hccl_plan_reducescatter", "hccl_plan_allgathe
            "hccl_hostpipe_alltoallv_create", "hccl_hostpipe_windows", "hccl_hostpipe_workspace_bytes", "hccl_hostpipe_bind",
            "hccl_hostpipe_execute", "hccl_hostpipe_status", "hccl_hostpipe_destroy", "hccl_opts_for_overlap",
            "hccl_route_workspace_bytes", "hccl_route", "hccl_route_backward", "hccl_dispatch", "hccl_dispatch_backward", "hccl_combine",
-           "hccl_combine_backward", "hccl_quantize_rows_i8", "hccl_matmul_i8", "hccl_linear_i8"]
+           "hccl_combine_backward", "hccl_quantize_rows_i8", "hccl_matmul_i8", "hccl_linear_i8", "hccl_call_packed"]
 
 
 def status_string(status: int) -> str:
@@ -376,12 +376,16 @@ hccl_matmul_i8 = _call("hccl_matmul_i8")
 hccl_linear_i8 = _call("hccl_linear_i8")
 
 
+# hccl_call_t: which call, and in the second byte how many arguments it has
+CALLS = {"hccl_route": 0x0a00, "hccl_route_backward": 0x0b01, "hccl_dispatch": 0x0902, "hccl_dispatch_backward": 0x0903, "hccl_combine": 0x0a04,
+         "hccl_combine_backward": 0x0d05, "hccl_quantize_rows_i8": 0x0b06, "hccl_matmul_i8": 0x1107, "hccl_linear_i8": 0x1508}
+
+
 def packed(name: str):
     """The same call for code that makes it often: all arguments integers (structures by address, NULL 0; of the products the fields of
     hccl_matmul_i8_t one by one), handed over as one array."""
-    which, n = {"hccl_route": (0, 10), "hccl_route_backward": (1, 11), "hccl_dispatch": (2, 9), "hccl_dispatch_backward": (3, 9), "hccl_combine": (4, 10),
-                "hccl_combine_backward": (5, 13), "hccl_quantize_rows_i8": (6, 11), "hccl_matmul_i8": (7, 17), "hccl_linear_i8": (8, 21)}[name]
-    fn, pack = _lib.hccl_call_packed, struct.Struct("%dq" % n).pack
+    which = CALLS[name]
+    fn, pack = _lib.hccl_call_packed, struct.Struct("%dq" % (which >> 8)).pack
 
     def call(*args):
         rc = fn(which, pack(*args))

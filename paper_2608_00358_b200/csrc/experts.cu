@@ -298,9 +298,9 @@ hccl_status_t hccl_linear_i8(const hccl_matmul_i8_t* in, const void* x, int64_t 
     return done(launch_matmul_i8(m.dtype, mm, (cudaStream_t)stream), "hccl_linear_i8");
 }
 
-// The calls above with their arguments as an array of 64-bit integers in the same order (structures by address, the product's fields one by one). For the
-// Python binding: it packs an array in one step, which takes half the time of handing over ten arguments one by one.
-hccl_status_t hccl_call_packed(int which, const int64_t* a) {
+// For the Python binding: it packs an array in one step, which takes half the time of handing over ten arguments one by one.
+hccl_status_t hccl_call_packed(int32_t call, const int64_t* a) {
+    if (!a) return HCCL_ERR_INVALID_ARG;
     const auto at = [&](int i) { return (void*)(uintptr_t)a[i]; };
     const auto dt = [&](int i) { return (hccl_dtype_t)a[i]; };
     const auto matmul = [&] {
@@ -312,27 +312,27 @@ hccl_status_t hccl_call_packed(int which, const int64_t* a) {
         m.y = at(13), m.ldy = a[14], m.dev_status = (int32_t*)at(15);
         return m;
     };
-    switch (which) {
-        case 0:
+    switch (call) {
+        case HCCL_CALL_ROUTE:
             return hccl_route((const hccl_router_t*)at(0), at(1), a[2], dt(3), (const float*)at(4), (const uint8_t*)at(5), (const hccl_routing_t*)at(6), at(7), (size_t)a[8], at(9));
-        case 1:
+        case HCCL_CALL_ROUTE_BACKWARD:
             return hccl_route_backward((const hccl_router_t*)at(0), at(1), a[2], dt(3), (const float*)at(4), (const uint8_t*)at(5), (const hccl_routing_t*)at(6),
                                        (const float*)at(7), at(8), a[9], at(10));
-        case 2:
+        case HCCL_CALL_DISPATCH:
             return hccl_dispatch(at(0), a[1], a[2], dt(3), (const hccl_routing_t*)at(4), at(5), a[6], a[7], at(8));
-        case 3:
+        case HCCL_CALL_DISPATCH_BACKWARD:
             return hccl_dispatch_backward(at(0), a[1], a[2], a[3], dt(4), (const hccl_routing_t*)at(5), at(6), a[7], at(8));
-        case 4:
+        case HCCL_CALL_COMBINE:
             return hccl_combine(at(0), a[1], a[2], a[3], dt(4), (const hccl_routing_t*)at(5), (const float*)at(6), at(7), a[8], at(9));
-        case 5:
+        case HCCL_CALL_COMBINE_BACKWARD:
             return hccl_combine_backward(at(0), a[1], at(2), a[3], a[4], a[5], dt(6), (const hccl_routing_t*)at(7), (const float*)at(8), at(9), a[10], (float*)at(11), at(12));
-        case 6:
+        case HCCL_CALL_QUANTIZE_ROWS_I8:
             return hccl_quantize_rows_i8(at(0), a[1], a[2], a[3], dt(4), (const hccl_routing_t*)at(5), (int8_t*)at(6), a[7], a[8], (float*)at(9), at(10));
-        case 7: {
+        case HCCL_CALL_MATMUL_I8: {
             const hccl_matmul_i8_t m = matmul();
             return hccl_matmul_i8(&m, at(16));
         }
-        case 8: {
+        case HCCL_CALL_LINEAR_I8: {
             const hccl_matmul_i8_t m = matmul();
             return hccl_linear_i8(&m, at(16), a[17], dt(18), (const hccl_routing_t*)at(19), at(20));
         }

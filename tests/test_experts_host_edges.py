@@ -1,4 +1,8 @@
 """Expert layers, host side: what the Python layer does before a launch, checked on the CPU with stand-ins for the device's calls."""
+import ctypes as C
+import os
+import re
+import struct
 import threading
 
 import pytest
@@ -116,3 +120,80 @@ def test_a_gradient_of_any_layout_gets_rows_that_the_calls_take(T, H):
         assert ex._matrix(on_device(v), "g", H, T, 0) >= H  # (of an empty one the strides do not matter)
     wide = torch.zeros(T, H + 3)[:, :H]
     assert ex._cols(wide) is wide  # no copy where none is needed
+
+
+# ------------------------------------------------------------------------------------------------ the binding's calls with packed arguments
+A = 1 << 20  # an aligned address that nothing reads
+
+
+def packed_calls():
+    """What the records must outlive, and for each call its name, arguments that hold together, and (place, value, status) for every place with a refusal of its own. Only
+    lists with such a change are handed over: none reaches a device."""
+    router = hb.RouterConfig(8, 2, 0, 1, 1, 1, 1, 1.0)
+    routing = hb.RoutingRecord(4, 2, 8, A, A, A, A, A, A)
+    other = hb.RoutingRecord(5, 2, 8, A, A, A, A, A, A)
+    without = hb.RoutingRecord(4, 2, 8, A, A, A, 0, A, A)
+    R, P, O, N = C.addressof(router), C.addressof(routing), C.addressof(other), C.addressof(without)
+    keep = (router, routing, other, without)
+    bad, ali, dty, mism, wsp = hb.ERR_INVALID_ARG, hb.ERR_ALIGNMENT, hb.ERR_DTYPE, hb.ERR_COUNT_MISMATCH, hb.ERR_WORKSPACE
+    mm = [4, 8, 32, 0, hb.BF16, A, 32, A, A, 32, A, 0, 0, A, 8, 0]  # M N K groups dtype a lda a_scale w ldw w_scale bias offsets y ldy dev_status
+    mm_bad = [(0, -1, bad), (1, -1, bad), (2, hb.MAX_I8_K + 1, bad), (3, 2, bad), (4, 9, dty), (5, 0, bad), (5, A + 8, ali), (6, 16, bad), (6, 40, ali), (7, 0, bad), (7, A + 2, ali),
+              (8, 0, bad), (8, A + 1, ali), (9, 16, bad), (9, 40, ali), (10, 0, bad), (10, A + 2, ali), (11, A + 2, ali), (12, A + 2, ali), (13, 0, bad), (13, A + 1, ali), (14, 7, bad), (15, A + 1, ali)]
+    return keep, [
+        ("hccl_route", [R, A, 8, hb.BF16, 0, 0, P, A, 1 << 20, 0],
+         [(0, 0, bad), (1, 0, bad), (1, A + 1, ali), (2, 7, bad), (3, 9, dty), (4, A + 2, ali), (6, 0, bad), (7, 0, bad), (7, A + 4, ali), (8, 0, wsp)]),
+        ("hccl_route_backward", [R, A, 8, hb.FP32, 0, 0, P, A, A, 8, 0],
+         [(0, 0, bad), (1, 0, bad), (2, 7, bad), (3, 9, dty), (4, A + 2, ali), (6, 0, bad), (7, 0, bad), (7, A + 2, ali), (8, 0, bad), (8, A + 2, ali), (9, 3, bad)]),
+        ("hccl_dispatch", [A, 16, 16, hb.BF16, P, A, 16, 8, 0],
+         [(0, 0, bad), (0, A + 1, ali), (1, 15, bad), (2, -1, bad), (3, 9, dty), (4, 0, bad), (5, 0, bad), (5, A + 1, ali), (6, 15, bad), (7, -1, bad)]),
+        ("hccl_dispatch_backward", [A, 16, 8, 16, hb.BF16, P, A, 16, 0],
+         [(0, 0, bad), (0, A + 1, ali), (1, 15, bad), (2, -1, bad), (3, -1, bad), (4, 9, dty), (5, 0, bad), (6, 0, bad), (6, A + 1, ali), (7, 15, bad)]),
+        ("hccl_combine", [A, 16, 8, 16, hb.BF16, P, A, A, 16, 0],
+         [(0, 0, bad), (0, A + 1, ali), (1, 15, bad), (2, -1, bad), (3, -1, bad), (4, 9, dty), (5, 0, bad), (6, 0, bad), (6, A + 2, ali), (7, 0, bad), (7, A + 1, ali), (8, 15, bad)]),
+        ("hccl_combine_backward", [A, 16, A, 16, 8, 16, hb.BF16, P, A, A, 16, A, 0],
+         [(0, 0, bad), (1, 15, bad), (2, 0, bad), (2, A + 1, ali), (3, 15, bad), (4, -1, bad), (5, -1, bad), (6, 9, dty), (7, 0, bad), (8, 0, bad), (8, A + 2, ali), (9, 0, bad), (9, A + 1, ali),
+          (10, 15, bad), (11, 0, bad), (11, A + 2, ali)]),
+        ("hccl_quantize_rows_i8", [A, 32, 4, 32, hb.BF16, P, A, 32, 8, A, 0],
+         [(0, 0, bad), (0, A + 1, ali), (1, 31, bad), (2, 5, mism), (3, hb.MAX_I8_K + 1, bad), (4, 9, dty), (5, O, mism), (6, 0, bad), (7, 31, bad), (8, -1, bad), (9, 0, bad), (9, A + 1, ali)]),
+        ("hccl_matmul_i8", mm + [0], mm_bad),
+        ("hccl_linear_i8", mm + [A, 32, hb.BF16, 0, 0], mm_bad + [(16, 0, bad), (16, A + 1, ali), (17, 31, bad), (18, 9, dty), (19, N, bad)]),
+    ]
+
+
+def plain(name, args):
+    """The same through the call itself."""
+    if name in ("hccl_matmul_i8", "hccl_linear_i8"):
+        m = hb.MatmulI8(*args[:16])
+        rest = list(args[16:])
+        if name == "hccl_linear_i8":
+            rest[3] = C.cast(rest[3], C.POINTER(hb.RoutingRecord)) if rest[3] else None
+        return getattr(hb, name)(C.byref(m), *rest)
+    typed = {"hccl_route": {0: hb.RouterConfig, 6: hb.RoutingRecord}, "hccl_route_backward": {0: hb.RouterConfig, 6: hb.RoutingRecord}, "hccl_dispatch": {4: hb.RoutingRecord},
+             "hccl_dispatch_backward": {5: hb.RoutingRecord}, "hccl_combine": {5: hb.RoutingRecord}, "hccl_combine_backward": {7: hb.RoutingRecord}, "hccl_quantize_rows_i8": {5: hb.RoutingRecord}}[name]
+    return getattr(hb, name)(*[(C.cast(a, C.POINTER(typed[i])) if a else None) if i in typed else a for i, a in enumerate(args)])
+
+
+@pytest.mark.parametrize("at", range(9))
+def test_packed_arguments_reach_the_places_of_the_call(at):
+    """Every place that the call can refuse, one at a time: the packed call gives the call's own answer."""
+    keep, calls = packed_calls()
+    name, good, changes = calls[at]
+    assert len(good) == hb.CALLS[name] >> 8
+    for place, value, want in changes:
+        args = list(good)
+        args[place] = value
+        for call in (lambda: plain(name, args), lambda: hb.packed(name)(*args)):
+            with pytest.raises(hb.HcclError) as e:
+                call()
+            assert e.value.status == want, (name, place, value)
+
+
+def test_packed_calls_are_those_of_the_header():
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "hccl.h")).read()
+    declared = {"hccl_" + n.lower(): int(v, 16) for n, v in re.findall(r"HCCL_CALL_(\w+) = (0x[0-9a-f]+)", text)}
+    assert declared == hb.CALLS
+    for call in (0, 10, 0x0a01, 0x0b00, 0x1509, -1):
+        assert hb._lib.hccl_call_packed(call, b"\0" * 256) == hb.ERR_INVALID_ARG
+    assert hb._lib.hccl_call_packed(hb.CALLS["hccl_route"], None) == hb.ERR_INVALID_ARG
+    with pytest.raises(struct.error):
+        hb.packed("hccl_route")(0, 0)  # too few arguments

@@ -15,7 +15,7 @@ import expert_reference as ref
 from paper_2608_00358_b200 import binding as hb
 from paper_2608_00358_b200 import experts as ex
 from paper_2608_00358_b200.expert_layer import ExpertParallel
-from test_gpu_experts import BF16, F16, F32, check_routing, close, cuda, gen, grid_logits, random_routing, strided, weight_tol
+from test_gpu_experts import BF16, F16, F32, SENT, check_routing, close, cuda, gen, grid_logits, product_tol, random_routing, strided, weight_tol
 
 pytestmark = pytest.mark.gpu
 
@@ -419,3 +419,136 @@ def test_copies_have_addresses_of_their_own():
     r3 = copy.deepcopy(r)
     assert r3.slots.data_ptr() != r.slots.data_ptr() and r3.record.slots == r3.slots.data_ptr()
     assert torch.equal(lin(x, routing=r3)[:used], y[:used])
+
+
+# ------------------------------------------------------------------------------------------------ other kernels, other turns of their loops
+@pytest.mark.parametrize("T,k,E,H,dt,pad,short", [(300, 8, 40, 1032, BF16, 0, 0), (300, 8, 40, 1032, BF16, 8, 37), (130, 32, 60, 2056, F16, 16, 11), (1200, 2, 9, 4100, F32, 4, 0),
+                                                  (5000, 4, 16, 136, F32, 0, 100), (40, 3, 7, 24584, BF16, 0, 0)])
+def test_dispatch_of_many_bytes(T, k, E, H, dt, pad, short):
+    """From 4 MB of rows on, by bulk copies: rows of several pieces with a remainder, distances between rows, places without a row, a capacity that drops some,
+    a tail without choices. Nothing but copies: equal bits, and nothing beside the rows' ranges."""
+    es = torch.empty(0, dtype=dt).element_size()
+    assert T * k * H * es >= 4 << 20 and H * es % 16 == 0 and (H + pad) * es % 16 == 0
+    ids, w, slots, source, used, r = random_routing(T, k, E, T)
+    n = (used - short) if short else T * k
+    assert short or n > used  # either some choices are dropped or a tail is left
+    x = torch.randn(T, H, generator=torch.Generator().manual_seed(k)).to(dt)
+    flat = torch.full((n * (H + pad) + 64,), SENT, dtype=dt, device="cuda")
+    out = flat[32: 32 + n * (H + pad)].view(n, H + pad)
+    ex.dispatch(strided(x, pad), r, out=out[:, :H])
+    want = torch.zeros(n, H, dtype=dt)
+    t, j = np.nonzero((slots >= 0) & (slots < n))
+    want[torch.from_numpy(slots[t, j])] = x[torch.from_numpy(t)]
+    assert torch.equal(out[:, :H].cpu(), want)
+    assert (out[:, H:] == SENT).all() and (flat[:32] == SENT).all() and (flat[-32:] == SENT).all()
+
+
+@pytest.mark.parametrize("M,N,K,dt", [(2000, 2900, 384, BF16), (5000, 1030, 272, F32), (600, 16400, 128, F16), (20000, 512, 1024, BF16)])
+def test_pairs_of_blocks_walk_several_tiles(M, N, K, dt):
+    """More tiles of 256 x 256 than there are pairs of SMs: accumulators and stages in turn, the last tile ragged."""
+    assert -(-M // 256) * -(-N // 256) > 74
+    g = torch.Generator(device="cuda").manual_seed(M)
+    a = torch.randint(-127, 128, (M, K), generator=g, device="cuda").to(torch.int8)
+    w = torch.randint(-127, 128, (N, K), generator=g, device="cuda").to(torch.int8)
+    sa, sw = torch.rand(M, generator=g, device="cuda") * 0.002 + 0.001, torch.rand(N, generator=g, device="cuda") * 0.002 + 0.001
+    lin = ex.Int8Linear(w, sw)
+    y = torch.full((M, N + 1), SENT, dtype=dt, device="cuda")
+    lin.matmul(a, sa, out=y[:, :N])
+    lin.check()
+    want = (a.double() @ w.double().t()) * sa.double()[:, None] * sw.double()  # sums below 2^53: exact
+    want = want.cpu().numpy()
+    close(y[:, :N], want, product_tol(want, np.abs(want), dt))
+    assert (y[:, N:] == SENT).all()
+
+
+@pytest.mark.parametrize("M,N,K,dt", [(2, 300, 8192, BF16), (3, 100, 5000, F32), (8, 512, 4096, BF16), (8, 130, 8200, F16), (5, 64, 13000, F16), (8, 48, 20000, BF16)])
+def test_few_long_rows_are_quantised_ahead(M, N, K, dt):
+    """Few rows that are too long for every block to quantise: the quantiser, and the product of few rows behind it; the last too long for that one too."""
+    assert M * K > 8192
+    g = torch.Generator().manual_seed(K)
+    x, w = torch.randn(M, K, generator=g).to(dt), torch.randn(N, K, generator=g)
+    lin = ex.Int8Linear.from_float(w.cuda())
+    wq, ws = ref.quantise(w.numpy())
+    xq, xs = ref.quantise(x.float().numpy())
+    want, size = ref.matmul(xq, xs, wq[None], ws[None])
+    for _ in range(3):
+        y = lin(x.cuda())
+    lin.check()
+    close(y, want, product_tol(want, size, dt))
+
+
+@pytest.mark.parametrize("T,E,k,score", [(80000, 24, 3, "softmax"), (200000, 8, 2, "sigmoid"), (18900, 1024, 4, "softmax"), (600000, 5, 1, "softmax")])
+def test_layout_of_chunks_that_count_by_other_rules(T, E, k, score):
+    """Chunks of more than 63 tokens (from 75 777 on), and more chunks than a line adds up at once (1024 experts, some 18 900 tokens)."""
+    g = torch.Generator().manual_seed(T)
+    mask = torch.rand(T, generator=g) < 0.9
+    logits = (torch.rand(T, E, generator=g) * 4 - 2 + torch.linspace(1, -1, E)).float()
+    r = ex.Router(E, k, score=score).route(logits.cuda(), token_mask=mask.cuda())
+    order = logits.sort(dim=-1, descending=True, stable=True).indices[:, :k].numpy()
+    order[~mask.numpy()] = -1
+    flat = order.reshape(-1)
+    live = np.nonzero(flat >= 0)[0]
+    source = np.full(flat.size, -1)
+    source[: live.size] = live[np.argsort(flat[live], kind="stable")]
+    slots = np.full(flat.size, -1)
+    slots[source[: live.size]] = np.arange(live.size)
+    counts = np.bincount(flat[live], minlength=E)
+    assert np.array_equal(r.ids.cpu().numpy(), order) and np.array_equal(r.counts.cpu().numpy(), counts)
+    assert np.array_equal(r.offsets.cpu().numpy(), np.concatenate([[0], np.cumsum(counts)]))
+    assert np.array_equal(r.source.cpu().numpy(), source) and np.array_equal(r.slots.cpu().numpy().reshape(-1), slots)
+
+
+def row_scaled_gradient(logits, ids, dw, score, renorm, scale, bias=None):
+    """The gradient in 64 bits by its formula, and the size of the terms of each element."""
+    off = np.isneginf(logits) | (np.zeros(logits.shape, dtype=bool) if bias is None else np.isneginf(bias)[None])
+    with np.errstate(all="ignore"):
+        top = np.where(off, -np.inf, logits).max(-1, keepdims=True)
+        e = np.where(off, 0.0, np.exp(logits - top))
+        s = np.where(off, 0.0, 1 / (1 + np.exp(-logits))) if score == "sigmoid" else e / np.maximum(e.sum(-1, keepdims=True), 1e-300)
+    live = ids >= 0
+    at = np.where(live, ids, 0)
+    c = np.where(live, np.take_along_axis(s, at, 1), 0.0)
+    g = np.where(live, dw * float(scale), 0.0)
+    if renorm:
+        total = c.sum(-1, keepdims=True)
+        p = np.where(total > 0, c / np.where(total > 0, total, 1.0), 0.0)
+        d, size = p * (g - (g * p).sum(-1, keepdims=True)), p * (np.abs(g) + (np.abs(g) * p).sum(-1, keepdims=True))
+        if score == "sigmoid":
+            d = d * (1 - c)
+    elif score == "sigmoid":
+        d, size = g * c * (1 - c), np.abs(g) * c
+    if renorm or score == "sigmoid":
+        D, S = np.zeros(s.shape), np.zeros(s.shape)
+        t, j = np.nonzero(live)
+        D[t, ids[t, j]], S[t, ids[t, j]] = d[t, j], size[t, j]
+        return D, S
+    G = np.zeros(s.shape)
+    t, j = np.nonzero(live)
+    G[t, ids[t, j]] = g[t, j]
+    return s * (G - (G * s).sum(-1, keepdims=True)), s * (np.abs(G) + (np.abs(G) * s).sum(-1, keepdims=True))
+
+
+@pytest.mark.parametrize("T,E,k,score,renorm,dt,with_bias", [
+    (50, 320, 8, "softmax", False, F32, False), (33, 1024, 32, "softmax", False, F32, True), (40, 300, 5, "softmax", True, F32, True), (33, 1024, 32, "softmax", True, F32, False),
+    (25, 1000, 6, "sigmoid", True, F32, True), (25, 1000, 6, "sigmoid", False, BF16, True), (61, 60, 4, "softmax", False, F16, True), (300, 256, 8, "softmax", True, BF16, True),
+    (200, 128, 8, "sigmoid", True, F32, True), (40000, 16, 2, "softmax", True, F32, False), (40000, 12, 2, "softmax", False, BF16, True), (20000, 260, 2, "softmax", False, F32, False)])
+def test_route_gradient_within_the_size_of_its_terms(T, E, k, score, renorm, dt, with_bias):
+    """Scores in 32 bits are within (E + 32) 2^-24 of themselves (the sum over E of them), a dot of k terms within (k + 8) 2^-24 of theirs, then a few roundings: within
+    (2 E + 2 k + 64) 2^-24 of the size of an element's own terms, and the output's rounding."""
+    rng = gen(T + E + k)
+    logits = grid_logits(rng, T, E, dt)
+    logits[2, : E // 2] = -np.inf
+    logits[3] = -np.inf
+    bias = None
+    if with_bias:
+        bias = rng.integers(-1, 2, E).astype(np.float32)
+        bias[[1, E // 3]] = -np.inf
+    router = ex.Router(E, k, score=score, renormalise=renorm, scale=1.5)
+    lg = strided(logits, 3)
+    r = router.route(lg, cuda(bias))
+    ids = r.ids.cpu().numpy().astype(np.int64)
+    assert (ids[3] == -1).all() and (bias is None or not np.isin(ids, [1, E // 3]).any())
+    dw = np.clip(rng.standard_normal((T, k)), -5.9, 5.9).astype(np.float32)
+    want, size = row_scaled_gradient(logits.double().numpy(), ids, dw, score, renorm, 1.5, bias)
+    got = router.backward(lg, r, cuda(dw), bias=cuda(bias))
+    close(got, want, (2 * E + 2 * k + 64) * ref.EPS32 * size + ref.HALF_ULP[dt] * 1.01 * np.abs(want) + ref.SMALLEST[dt] + 1e-37)

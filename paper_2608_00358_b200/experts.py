@@ -438,7 +438,8 @@ class Int8Linear:
 
     @classmethod
     def from_float(cls, weight: torch.Tensor, bias: Optional[torch.Tensor] = None) -> "Int8Linear":
-        """Quantises a weight matrix (or one for each expert), a scale for each output channel."""
+        """Quantises a weight matrix (or one for each expert), a scale for each output channel. Of a parameter, its values."""
+        weight = weight.detach()
         q, scale = quantize_rows(weight.reshape(-1, weight.shape[-1]))
         return cls(q.reshape(weight.shape), scale.view(weight.shape[:-1]), bias)
 

@@ -298,6 +298,13 @@ def test_a_linear_layer_without_a_gradient_says_so():
     assert torch.equal(y, lin(x.detach())) and not y.requires_grad
 
 
+def test_a_layer_is_made_from_parameters():
+    w, b = torch.nn.Parameter(torch.randn(24, 40, device="cuda")), torch.nn.Parameter(torch.randn(24, device="cuda"))
+    x = torch.randn(5, 40, device="cuda")
+    y = ex.Int8Linear.from_float(w, b)(x)
+    assert not y.requires_grad and torch.equal(y, ex.Int8Linear.from_float(w.detach(), b.detach())(x))
+
+
 def test_writes_through_out_are_seen_by_autograd():
     T, E, k, H = 10, 8, 2, 32
     router, lin = ex.Router(E, k), ex.Int8Linear.from_float(torch.randn(16, H, device="cuda"))

@@ -597,11 +597,12 @@ hccl_status_t hccl_combine_backward(const void* dy, int64_t ldy, const void* row
  * left alone. routing NULL: M rows of x to M rows of q. Otherwise M must be routing->tokens and row t is written to
  * every slots[t,k] below n_q (the 8-bit form of hccl_dispatch, for half the bytes in the exchange). */
 #define HCCL_MAX_I8_K 131071 /* 128 * 128 * K stays below 2^31 */
+#define HCCL_MAX_I8_ROWS 2147467263 /* 2^31 - 1 - 2^14: of M, and of groups * N; the kernels count rows and channels in 32 bits, up to the end of the last round of tiles */
 hccl_status_t hccl_quantize_rows_i8(const void* x, int64_t ldx, int64_t M, int64_t K, hccl_dtype_t dt, const hccl_routing_t* routing,
                                     int8_t* q, int64_t ldq, int64_t n_q, float* scale, void* stream);
 
 /* Products in 8-bit integers: y[m,n] = round(float(sum_k a[m,k] * w[g,n,k]) * a_scale[m] * w_scale[g,n] (+ bias[g,n])), the sum
- * exact in 32-bit integers. groups 0: one matrix for all M rows. groups > 0: row m belongs to group g when
+ * exact in 32-bit integers. M and groups * N: at most HCCL_MAX_I8_ROWS. groups 0: one matrix for all M rows. groups > 0: row m belongs to group g when
  * offsets[g] <= m < offsets[g+1] (device memory, ascending, at most M; rows outside all groups are left alone), and a group without rows costs nothing.
  * a and w must start on 16-byte boundaries with lda and ldw multiples of 16 (a row is read, not used, up to the next multiple of 16 from K); row n of group g starts at
  * w + (g * N + n) * ldw. y: any stride, type dt. dev_status: one device int32 or NULL; a failure on the device

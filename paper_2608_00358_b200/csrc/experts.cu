@@ -94,7 +94,7 @@ hccl_status_t check_matmul(const hccl_matmul_i8_t* m) {
     if (!hccl::valid_dtype(m->dtype)) return HCCL_ERR_DTYPE;
     if (m->K > HCCL_MAX_I8_K) return HCCL_ERR_INVALID_ARG;
     const int64_t g = m->groups ? m->groups : 1;
-    if (m->M > INT32_MAX || m->N > INT32_MAX / g) return HCCL_ERR_INVALID_ARG;
+    if (m->M > HCCL_MAX_I8_ROWS || m->N > HCCL_MAX_I8_ROWS / g) return HCCL_ERR_INVALID_ARG;
     if (!sane(m->M, m->lda, m->K) || !sane(m->N * g, m->ldw, m->K)) return HCCL_ERR_INVALID_ARG;
     if (m->groups && !m->offsets) return HCCL_ERR_INVALID_ARG;
     if (m->M && m->N) {

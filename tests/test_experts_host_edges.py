@@ -197,3 +197,16 @@ def test_packed_calls_are_those_of_the_header():
     assert hb._lib.hccl_call_packed(hb.CALLS["hccl_route"], None) == hb.ERR_INVALID_ARG
     with pytest.raises(struct.error):
         hb.packed("hccl_route")(0, 0)  # too few arguments
+
+
+@pytest.mark.parametrize("kw", [dict(M=(1 << 31) - 1), dict(M=(1 << 31) - 200), dict(N=(1 << 31) - 1, ldy=1 << 31), dict(N=(1 << 31) - 100, ldy=1 << 31),
+                                dict(groups=2, offsets=A, N=(1 << 30) - 1, ldy=1 << 30)])
+def test_products_whose_last_tile_would_pass_32_bits_are_refused(kw):
+    """A tile's rows and channels are counted in 32 bits, beyond the matrix up to the tile's end."""
+    c = dict(M=4, N=8, K=16, groups=0, dtype=hb.BF16, a=A, lda=16, a_scale=A, w=A, ldw=16, w_scale=A, bias=0, offsets=0, y=A, ldy=8, dev_status=0)
+    c.update(kw)
+    m = hb.MatmulI8(*c.values())
+    for call in (lambda: hb.hccl_matmul_i8(C.byref(m), 0), lambda: hb.hccl_linear_i8(C.byref(m), A, 16, hb.BF16, None, 0)):
+        with pytest.raises(hb.HcclError) as e:
+            call()
+        assert e.value.status == hb.ERR_INVALID_ARG

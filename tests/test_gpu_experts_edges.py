@@ -559,3 +559,57 @@ def test_route_gradient_within_the_size_of_its_terms(T, E, k, score, renorm, dt,
     want, size = row_scaled_gradient(logits.double().numpy(), ids, dw, score, renorm, 1.5, bias)
     got = router.backward(lg, r, cuda(dw), bias=cuda(bias))
     close(got, want, (2 * E + 2 * k + 64) * ref.EPS32 * size + ref.HALF_ULP[dt] * 1.01 * np.abs(want) + ref.SMALLEST[dt] + 1e-37)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_random_routers(seed):
+    """60 configurations: experts, groups, scores, biases and masks of every kind, rows with -inf, NaN and infinities in them; routing, layout and gradient. A row whose choice hangs
+    on less than 1e-6 is left out of the comparison of choices."""
+    rng = gen(900 + seed)
+    pick = lambda *a: a[rng.integers(len(a))]  # noqa: E731
+    compared = 0
+    for _ in range(60):
+        E = int(pick(rng.integers(1, 65), rng.integers(1, 401), 2 ** rng.integers(3, 11), rng.integers(200, 1025)))
+        groups = int(pick(1, 1, pick(*[d for d in range(1, E + 1) if E % d == 0])))
+        top_groups, best, k = int(rng.integers(1, groups + 1)), int(pick(1, 2)), int(rng.integers(1, min(32, E) + 1))
+        T = min(int(pick(rng.integers(1, 21), rng.integers(1, 301), rng.integers(100, 1501))), max(1, 100000 // E))
+        score, renorm, dt = pick("softmax", "sigmoid"), bool(rng.integers(2)), pick(F32, BF16, F16)
+        logits = (grid_logits(rng, T, E, dt) * int(pick(1, 2))).float().numpy()
+        for t in range(T):
+            u = rng.random()
+            if u < 0.2:
+                logits[t, rng.random(E) < pick(0.5, 0.95, 1.0)] = -np.inf
+            elif u < 0.25:
+                logits[t, rng.integers(E)] = pick(np.nan, np.inf)
+        bias = None
+        if rng.integers(2):
+            bias = rng.integers(-2, 3, E).astype(np.float32)
+            bias[rng.random(E) < pick(0.0, 0.1, 0.5, 0.95)] = -np.inf
+        mask = (rng.random(T) < 0.8) if rng.integers(2) else None
+        # (zeros for a bias where group scores are sums: the reference's keys are the scores then)
+        bias_ref = np.zeros(E, dtype=np.float32) if bias is None and score == "softmax" and groups > 1 and best == 2 else bias
+        ids, w, sure = np.full((T, k), -1, dtype=np.int64), np.zeros((T, k)), np.ones(T, dtype=bool)
+        for t in range(T):
+            i, v, gap = ref.route(logits[t: t + 1], k, score, bias_ref, None if mask is None else mask[t: t + 1], groups=groups, top_groups=top_groups, group_best=best, renorm=renorm, scale=2.5)
+            ids[t], w[t], sure[t] = i[0], v[0], gap > 1e-6
+        compared += int(sure.sum())
+        what = (T, E, k, score, groups, top_groups, best, renorm, dt, bias is not None)
+        router = ex.Router(E, k, score=score, groups=groups, top_groups=top_groups, group_best=best, renormalise=renorm, scale=2.5)
+        lg = strided(torch.from_numpy(logits).to(dt), int(pick(0, 0, 3, 4)), int(pick(0, 1, 4)))
+        r = router.route(lg, cuda(bias), cuda(mask))
+        got, got_w = r.ids.cpu().numpy().astype(np.int64), r.weights.double().cpu().numpy()
+        assert np.array_equal(got[sure], ids[sure]), what
+        close(r.weights[torch.from_numpy(sure).cuda()], w[sure], weight_tol(E, w[sure]))
+        for a, b in zip((r.counts, r.offsets, r.slots, r.source), ref.layout(got, E)):
+            assert np.array_equal(a.cpu().numpy(), b), what
+        dw = np.clip(rng.standard_normal((T, k)), -5.9, 5.9).astype(np.float32)
+        dl = router.backward(lg, r, cuda(dw), bias=cuda(bias), token_mask=cuda(mask))
+        unscored = np.isnan(got_w).any(-1)
+        live = ~unscored & (np.ones(T, dtype=bool) if mask is None else mask)
+        x = np.where(np.isposinf(logits), 800.0, logits).astype(np.float64)  # (a sigmoid of 1)
+        want, size = row_scaled_gradient(x, np.where(live[:, None], got, -1), dw, score, renorm, 2.5, bias)
+        chose = live & (got >= 0).any(-1)
+        want[~chose], size[~chose] = 0, 0
+        want[unscored] = np.nan
+        close(dl, want, (2 * E + 2 * k + 64) * ref.EPS32 * np.nan_to_num(size) + ref.HALF_ULP[dt] * 1.01 * np.abs(np.nan_to_num(want)) + ref.SMALLEST[dt] + 1e-37)
+    assert compared > 1000

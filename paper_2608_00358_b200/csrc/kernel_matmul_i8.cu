@@ -14,8 +14,8 @@
 // too few tiles for the SMs, a cluster of blocks shares a tile's K and adds its partial sums through distributed shared memory.
 //
 // Measured (B200; twice the bf16 library rate is 3.3 POP/s): 8192^3 308-345 us = 3.2-3.6 POP/s, 535 cycles for a stage whose products take 512, at the 1.5 GHz that the power
-// limit leaves (1.9 GHz and 255 us on zeros): the tensor cores are the bound. 64 matrices 2048 x 4096: 512 rows 85 us = 6.3 TB/s of weights, 65536 rows 390 us.
-// 997 x 2064 x 4104, one round of the blocks: 13.8 us, of which 0.8 set-up, 7 products (665 cycles a stage, fed from the L2), 3 results.
+// limit leaves (1.9 GHz and 255 us on zeros): the tensor cores are the bound. 64 matrices 2048 x 4096: 512 rows 85 us = 6.1-6.3 TB/s of weights, 65536 rows 375-390 us. 16 rows, 8192 x 4096: 10.8 us = 3.1 TB/s.
+// 997 x 2064 x 4104, one round of the blocks: 13.7 us, of which 0.8 set-up, 7 products (665 cycles a stage, fed from the L2), 3 results.
 #include <cuda.h>
 
 #include <atomic>
@@ -535,7 +535,9 @@ template <typename T, int TN, int CG> cudaError_t tiles_launch(const MatmulParam
     return cudaLaunchKernelEx(&cfg, hccl_matmul_i8_tiles<T, TN, CG>, p);
 }
 
-// Which tile. Tiles of TN tokens and a cluster of S blocks for each, by an estimate in microseconds fitted to measurements on 15 shapes from 1 x 8192 x 4096 to 2048^3:
+// Which tile. Tiles of TN tokens and a cluster of S blocks for each, by an estimate in microseconds fitted to measurements on shapes from 16 x 8192 x 4096 to 2048^3 (measured against
+// every other choice on 14 of them, TN,S: 16 x 8192 x 4096 takes 10.8 us with its 16,1 and 15.1 with 32,4; 16 x 2048 x 4096 6.7 with 16,4, the best is 6.6 with 32,4, 16,1 takes 9.9; 128 x 2048 x 8192 11.4 with 64,4 and 17.2
+// with 64,1; 512 x 4096 x 4096 12.9 with 128,1 and 16.4 with 256,1; 997 x 4104 x 2064 13.7 with 256,1 and 18.3 with 128,1; nowhere is the choice more than 6 % behind the best):
 // rounds of the blocks over the tiles, times the stages of one, times a stage's time (0.15 while fetching is the bound, 0.27 for a
 // pair's 2 x 512 cycles of products), and what does not overlap: the last tile's results and the cluster's exchange. One round of a cluster may take 128 blocks at most: more
 // than that do not find their neighbouring SMs free at once (measured: 16 x 8192 x 4096 with S = 4, 256 blocks, 15.2 us against 11.4 with S = 2).

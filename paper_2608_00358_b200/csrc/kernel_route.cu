@@ -4,10 +4,10 @@
 // The choice. L lanes share a token (8: four tokens to a warp; 32: one). Experts go to lanes in quads: quad q = experts 4q .. 4q + 3 belongs to
 // lane q % L, as its quad q / L. Keys lie in shared memory and the largest key of each quad in a register, so a round of
 // the top k costs a maximum over the lane's quads, one over the lanes, and a second look at one quad. Not eligible: -inf. What bounds it is
-// the number of instructions and, for few tokens, their chain: a token of 256 experts is 512 bytes of input and some 500 instructions of a warp.
+// the chain of the rounds, each a few dependent exchanges between lanes: 1.6 instructions a cycle of 4 at 37 % of the warps for 16384 x 256, some 500 instructions of a warp for each token.
 //
-// Measured (B200): 16384 x 256 bf16, sigmoid, 8 groups, top 8: 16 us choosing and 6.5 of layout behind it; softmax without groups 11 and 7; 32768 x 128 21 us in all; one token of 256
-// 5.7 us, 61 x 60 5.4 us, in one launch; the gradient of 32768 x 128 6.3 us = 3.0 TB/s.
+// Measured (B200, replayed from a graph): 16384 x 256 bf16, sigmoid, 8 groups, top 8: 21.6 us, some 15 choosing and 6.5 of layout behind it; without groups 17.2, as softmax 17.3; 32768 x 128 20.8; one token of 256
+// 4.7-5.1 us, 61 x 60 5.1-5.7 us, in one launch; the gradient of 32768 x 128 5.9-7.0 us = 2.7-3.2 TB/s, of a softmax that is not renormalised 18.3 us = 1.0 TB/s: a row is read three times there.
 //
 // Keys with a bias are good to a few 2^-24 (__expf and an approximate reciprocal), without one they are the logits; the weights of the chosen are formed anew with
 // expf and a rounded division.
@@ -460,7 +460,7 @@ __device__ __forceinline__ int offsets_of(const RouteParams& p, const int* tot, 
 }
 
 // Four blocks to an SM (64 registers, a few of them spilled): the 512 blocks of 16384 tokens are on their way at once. With three, 444 are, and the rest wait for
-// a whole chain of latencies (24.9 us against 22.6).
+// a whole chain of latencies (24.9 us against 22.6, when that was measured).
 // A block chooses for one chunk of tokens and leaves its counts for the layout; a single block (ONE) goes on to the layout itself.
 template <typename T, int Q, int L, bool ONE>
 __global__ void __launch_bounds__(32 * (ONE ? ONE_BLOCK_WARPS : MANY_WARPS), ONE ? 1 : 4) hccl_route_choose(const __grid_constant__ RouteParams p) {

@@ -185,9 +185,9 @@ def prepare(case, seed):
         if "wide" in s:
             s["wide"] = float(s["wide"])
         if op == "product":
-            s["linear"] = fp4.Fp4Linear(*s["w"], format=case["format"], bias=s["bias"], x_scale=s["wide"])
+            s["linear"] = fp4.Fp4Linear(*s["w"], K=case["K"], format=case["format"], bias=s["bias"], x_scale=s["wide"])
         if op == "layer":
-            up, down = (fp4.Fp4Linear(*s[n], format=case["format"]) for n in ("up", "down"))
+            up, down = (fp4.Fp4Linear(*s[n], K=case[K], format=case["format"]) for n, K in (("up", "H"), ("down", "I")))
             s["layer"] = fp4.FewTokens(up, down, act="silu")
         return s
     if "wide" in s:

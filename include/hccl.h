@@ -625,12 +625,61 @@ hccl_status_t hccl_matmul_i8(const hccl_matmul_i8_t*, void* stream);
  * expert e (groups = routing->experts, offsets = routing->offsets, M the rows of y and of the scratch). */
 hccl_status_t hccl_linear_i8(const hccl_matmul_i8_t*, const void* x, int64_t ldx, hccl_dtype_t x_dt, const hccl_routing_t* routing, void* stream);
 
-/* The expert-layer calls with their arguments as one array of 64-bit integers in the same order (pointers as addresses; in the place of an hccl_matmul_i8_t its
- * fields one by one), for bindings to which each argument costs. The names carry the number of arguments in their second byte. Refusals are the call's own;
+/* ---- Experts in 4-bit floating point -------------------------------------------------------------------------------
+ * Elements are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and negatives), two to a byte, the earlier in the low half. Every block of a row has a step d, and
+ * q = e2m1(x / d): the quotient rounded to FP32, then to the nearest element, ties to even, beyond 6 to 6.
+ * HCCL_NVFP4: 16 elements; the stored byte is s = e4m3(min(max|x| / (6 g), 448)) with the matrix's FP32 scale g, each step rounded to FP32, and d = s g.
+ * HCCL_MXFP4: 32 elements; the byte e stands for d = 2^(e - 127), the least with max|x| <= 6 d (from 2^-126 on); g is not used. Nothing saturates.
+ * A block with an infinity or a NaN has the scale NaN (0x7f, 0xff) and stands for NaN throughout. A block's last elements may lie beyond K. */
+typedef enum { HCCL_NVFP4 = 0, HCCL_MXFP4 = 1 } hccl_fp4_t;
+
+/* Rows by blocks: q [rows, (K + 1) / 2] bytes, scale [rows, ceil(K / 16 or 32)] bytes; an odd K leaves the last half-byte 0. wide: g, from 1e-30 to 1e30.
+ * routing NULL: M rows of x to M rows. Otherwise M must be routing->tokens and row t is written to every slots[t,k] below n_q (the 4-bit form of
+ * hccl_dispatch, for about a quarter of the bytes in the exchange); rows that no choice fills are left alone. K <= HCCL_MAX_FP4_K.
+ * The way back: y[m,k] = round(element * d), dt. */
+#define HCCL_MAX_FP4_K 131072
+hccl_status_t hccl_quantize_rows_fp4(const void* x, int64_t ldx, int64_t M, int64_t K, hccl_dtype_t dt, int32_t format, float wide, const hccl_routing_t* routing,
+                                     uint8_t* q, int64_t ldq, uint8_t* scale, int64_t lds, int64_t n_q, void* stream);
+hccl_status_t hccl_dequantize_rows_fp4(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, int64_t M, int64_t K, int32_t format, float wide,
+                                       void* y, int64_t ldy, hccl_dtype_t dt, void* stream);
+
+/* Weights' scales in the order that the tensor cores take, laid out once: from [groups * N, blocks] (lds bytes apart; groups 0 counts as 1) to
+ * hccl_fp4_weight_scale_bytes bytes, 16-byte aligned. */
+hccl_status_t hccl_fp4_weight_scale_bytes(int64_t N, int64_t K, int32_t groups, int32_t format, size_t* bytes);
+hccl_status_t hccl_fp4_weight_scales(const uint8_t* scale, int64_t lds, int64_t N, int64_t K, int32_t groups, int32_t format, void* out, void* stream);
+
+/* Products: y[m,n] = round((sum over the blocks b of s[m,b] t[g,n,b] sum_k q[m,k] v[g,n,k]) * (x_wide * w_wide[g]) (+ bias[g,n])), sums in FP32.
+ * Groups, offsets, y, dev_status as in hccl_matmul_i8_t. w must start on a 16-byte boundary with ldw (bytes) a multiple of 16;
+ * row n of group g starts at w + (g * N + n) * ldw. w_scale: from hccl_fp4_weight_scales. scratch: hccl_fp4_scratch_bytes, 128-byte aligned, contents
+ * arbitrary, not shared by calls in flight at once.
+ * hccl_matmul_fp4: of rows that are in 4 bits already, q (16-byte aligned, ldq a multiple of 16) and scale by rows. hccl_linear_fp4: of 16- or 32-bit
+ * rows, quantised within the call as by hccl_quantize_rows_fp4 with wide = x_wide; with a routing as in hccl_linear_i8. */
+typedef struct {
+    int64_t M, N, K;
+    int32_t groups;
+    int32_t dtype;  /* of y */
+    int32_t format;
+    float x_wide;   /* 1 for HCCL_MXFP4 */
+    const uint8_t* w; int64_t ldw;
+    const void* w_scale;
+    const float* w_wide;      /* [groups, at least 1] */
+    const float* bias;        /* NULL: none */
+    const int32_t* offsets;   /* [groups + 1], NULL when groups is 0 */
+    void* y; int64_t ldy;
+    void* scratch; int64_t scratch_bytes;
+    int32_t* dev_status;
+} hccl_matmul_fp4_t;
+hccl_status_t hccl_fp4_scratch_bytes(int64_t M, int64_t N, int64_t K, int32_t groups, int32_t format, size_t* bytes);
+hccl_status_t hccl_matmul_fp4(const hccl_matmul_fp4_t*, const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, void* stream);
+hccl_status_t hccl_linear_fp4(const hccl_matmul_fp4_t*, const void* x, int64_t ldx, hccl_dtype_t x_dt, const hccl_routing_t* routing, void* stream);
+
+/* The expert-layer calls with their arguments as one array of 64-bit integers in the same order (pointers as addresses; in the place of an hccl_matmul_i8_t or
+ * hccl_matmul_fp4_t its fields one by one, a 32-bit float by its bits), for bindings to which each argument costs. The names carry the number of arguments in their second byte. Refusals are the call's own;
  * any other value of `call` is refused. */
 typedef enum {
     HCCL_CALL_ROUTE = 0x0a00, HCCL_CALL_ROUTE_BACKWARD = 0x0b01, HCCL_CALL_DISPATCH = 0x0902, HCCL_CALL_DISPATCH_BACKWARD = 0x0903, HCCL_CALL_COMBINE = 0x0a04,
-    HCCL_CALL_COMBINE_BACKWARD = 0x0d05, HCCL_CALL_QUANTIZE_ROWS_I8 = 0x0b06, HCCL_CALL_MATMUL_I8 = 0x1107, HCCL_CALL_LINEAR_I8 = 0x1508
+    HCCL_CALL_COMBINE_BACKWARD = 0x0d05, HCCL_CALL_QUANTIZE_ROWS_I8 = 0x0b06, HCCL_CALL_MATMUL_I8 = 0x1107, HCCL_CALL_LINEAR_I8 = 0x1508,
+    HCCL_CALL_QUANTIZE_ROWS_FP4 = 0x0e09, HCCL_CALL_DEQUANTIZE_ROWS_FP4 = 0x0c0a, HCCL_CALL_MATMUL_FP4 = 0x170b, HCCL_CALL_LINEAR_FP4 = 0x170c
 } hccl_call_t;
 hccl_status_t hccl_call_packed(int32_t call, const int64_t* arguments);
 

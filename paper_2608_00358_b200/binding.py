@@ -29,6 +29,7 @@ MAX_RANKS = 256
 NOALLOC_WORKSPACE_BYTES = 8 << 20
 ELEM_BYTES = {FP32: 4, BF16: 2, FP16: 2}
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+NVFP4, MXFP4 = 0, 1
 MAX_EXPERTS, MAX_TOP_K, MAX_I8_K = 1024, 32, 131071
 ROUTE_NO_WORKSPACE = 16
 
@@ -77,6 +78,13 @@ class MatmulI8(C.Structure):
     _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("groups", C.c_int32), ("dtype", C.c_int32), ("a", C.c_void_p),
                 ("lda", C.c_int64), ("a_scale", C.c_void_p), ("w", C.c_void_p), ("ldw", C.c_int64), ("w_scale", C.c_void_p),
                 ("bias", C.c_void_p), ("offsets", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("dev_status", C.c_void_p)]
+
+
+class MatmulFp4(C.Structure):
+    """hccl_matmul_fp4_t"""
+    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("groups", C.c_int32), ("dtype", C.c_int32), ("format", C.c_int32), ("x_wide", C.c_float),
+                ("w", C.c_void_p), ("ldw", C.c_int64), ("w_scale", C.c_void_p), ("w_wide", C.c_void_p), ("bias", C.c_void_p), ("offsets", C.c_void_p),
+                ("y", C.c_void_p), ("ldy", C.c_int64), ("scratch", C.c_void_p), ("scratch_bytes", C.c_int64), ("dev_status", C.c_void_p)]
 
 
 class HcclError(RuntimeError):
@@ -138,6 +146,13 @@ def _load() -> C.CDLL:
         "hccl_quantize_rows_i8": [P, C.c_int64, C.c_int64, C.c_int64, C.c_int, RG, P, C.c_int64, C.c_int64, P, P],
         "hccl_matmul_i8": [C.POINTER(MatmulI8), P],
         "hccl_linear_i8": [C.POINTER(MatmulI8), P, C.c_int64, C.c_int, RG, P],
+        "hccl_quantize_rows_fp4": [P, C.c_int64, C.c_int64, C.c_int64, C.c_int, C.c_int32, C.c_float, RG, P, C.c_int64, P, C.c_int64, C.c_int64, P],
+        "hccl_dequantize_rows_fp4": [P, C.c_int64, P, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_float, P, C.c_int64, C.c_int, P],
+        "hccl_fp4_weight_scale_bytes": [C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)],
+        "hccl_fp4_weight_scales": [P, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, P, P],
+        "hccl_fp4_scratch_bytes": [C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)],
+        "hccl_matmul_fp4": [C.POINTER(MatmulFp4), P, C.c_int64, P, C.c_int64, P],
+        "hccl_linear_fp4": [C.POINTER(MatmulFp4), P, C.c_int64, C.c_int, RG, P],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -175,7 +190,9 @@ EXPORTS = ["hccl_plan_allreduce", "hccl_plan_reducescatter", "hccl_plan_allgathe
            "hccl_hostpipe_alltoallv_create", "hccl_hostpipe_windows", "hccl_hostpipe_workspace_bytes", "hccl_hostpipe_bind",
            "hccl_hostpipe_execute", "hccl_hostpipe_status", "hccl_hostpipe_destroy", "hccl_opts_for_overlap",
            "hccl_route_workspace_bytes", "hccl_route", "hccl_route_backward", "hccl_dispatch", "hccl_dispatch_backward", "hccl_combine",
-           "hccl_combine_backward", "hccl_quantize_rows_i8", "hccl_matmul_i8", "hccl_linear_i8", "hccl_call_packed"]
+           "hccl_combine_backward", "hccl_quantize_rows_i8", "hccl_matmul_i8", "hccl_linear_i8", "hccl_call_packed",
+           "hccl_quantize_rows_fp4", "hccl_dequantize_rows_fp4", "hccl_fp4_weight_scale_bytes", "hccl_fp4_weight_scales", "hccl_fp4_scratch_bytes",
+           "hccl_matmul_fp4", "hccl_linear_fp4"]
 
 
 def status_string(status: int) -> str:
@@ -374,16 +391,22 @@ hccl_combine_backward = _call("hccl_combine_backward")
 hccl_quantize_rows_i8 = _call("hccl_quantize_rows_i8")
 hccl_matmul_i8 = _call("hccl_matmul_i8")
 hccl_linear_i8 = _call("hccl_linear_i8")
+hccl_quantize_rows_fp4 = _call("hccl_quantize_rows_fp4")
+hccl_dequantize_rows_fp4 = _call("hccl_dequantize_rows_fp4")
+hccl_fp4_weight_scales = _call("hccl_fp4_weight_scales")
+hccl_matmul_fp4 = _call("hccl_matmul_fp4")
+hccl_linear_fp4 = _call("hccl_linear_fp4")
 
 
 # hccl_call_t: which call, and in the second byte how many arguments it has
 CALLS = {"hccl_route": 0x0a00, "hccl_route_backward": 0x0b01, "hccl_dispatch": 0x0902, "hccl_dispatch_backward": 0x0903, "hccl_combine": 0x0a04,
-         "hccl_combine_backward": 0x0d05, "hccl_quantize_rows_i8": 0x0b06, "hccl_matmul_i8": 0x1107, "hccl_linear_i8": 0x1508}
+         "hccl_combine_backward": 0x0d05, "hccl_quantize_rows_i8": 0x0b06, "hccl_matmul_i8": 0x1107, "hccl_linear_i8": 0x1508,
+         "hccl_quantize_rows_fp4": 0x0e09, "hccl_dequantize_rows_fp4": 0x0c0a, "hccl_matmul_fp4": 0x170b, "hccl_linear_fp4": 0x170c}
 
 
 def packed(name: str):
     """The same call for code that makes it often: all arguments integers (structures by address, NULL 0; of the products the fields of
-    hccl_matmul_i8_t one by one), handed over as one array."""
+    hccl_matmul_i8_t or hccl_matmul_fp4_t one by one, a float by its bits), handed over as one array."""
     which = CALLS[name]
     fn, pack = _lib.hccl_call_packed, struct.Struct("%dq" % (which >> 8)).pack
 
@@ -397,6 +420,18 @@ def packed(name: str):
 def hccl_route_workspace_bytes(router: RouterConfig, tokens: int) -> int:
     n = C.c_size_t()
     _chk(_lib.hccl_route_workspace_bytes(C.byref(router), tokens, C.byref(n)), "hccl_route_workspace_bytes")
+    return n.value
+
+
+def hccl_fp4_weight_scale_bytes(N: int, K: int, groups: int, format: int) -> int:
+    n = C.c_size_t()
+    _chk(_lib.hccl_fp4_weight_scale_bytes(N, K, groups, format, C.byref(n)), "hccl_fp4_weight_scale_bytes")
+    return n.value
+
+
+def hccl_fp4_scratch_bytes(M: int, N: int, K: int, groups: int, format: int) -> int:
+    n = C.c_size_t()
+    _chk(_lib.hccl_fp4_scratch_bytes(M, N, K, groups, format, C.byref(n)), "hccl_fp4_scratch_bytes")
     return n.value
 
 

@@ -1,22 +1,12 @@
 // C entry points of the expert-layer operators: argument checks and launches.
-#include <cstdio>
+#include <cstring>
 
-#include "experts.cuh"
-#include "plan.hpp"
+#include "checks.h"
+#include "fp4.cuh"
 
 using namespace hccl::experts;
 
-namespace hccl {
-hccl_status_t note_cuda_error(cudaError_t e, const char* what);  // executor.cu
-}
-
 namespace {
-
-bool aligned(const void* p, int64_t bytes) { return ((uintptr_t)p) % (uintptr_t)bytes == 0; }
-// rows * ld may not wrap: every offset the kernels form stays below 2^62 bytes
-bool sane(int64_t rows, int64_t ld, int64_t width) { return rows >= 0 && width >= 0 && (rows <= 1 || ld >= width) && ld >= 0 && (ld == 0 || rows < (INT64_C(1) << 60) / ld); }
-
-hccl_status_t done(cudaError_t e, const char* what) { return e == cudaSuccess ? HCCL_OK : hccl::note_cuda_error(e, what); }
 
 hccl_status_t check_router(const hccl_router_t* r, int64_t tokens) {
     if (!r || tokens < 0) return HCCL_ERR_INVALID_ARG;
@@ -31,27 +21,6 @@ hccl_status_t check_router(const hccl_router_t* r, int64_t tokens) {
     if (tokens >= (INT64_C(1) << 31) / r->top_k) return HCCL_ERR_INVALID_ARG;
     return HCCL_OK;
 }
-
-// What the rows' movers read of a routing.
-hccl_status_t check_routing(const hccl_routing_t* r) {
-    if (!r || r->tokens < 0 || r->top_k < 1 || r->top_k > HCCL_MAX_TOP_K || r->experts < 1 || r->experts > HCCL_MAX_EXPERTS) return HCCL_ERR_INVALID_ARG;
-    if (r->tokens >= (INT64_C(1) << 31) / r->top_k) return HCCL_ERR_INVALID_ARG;
-    if (!r->offsets || (r->tokens && !r->slots)) return HCCL_ERR_INVALID_ARG;
-    if (!aligned(r->offsets, 4) || !aligned(r->slots, 4)) return HCCL_ERR_ALIGNMENT;
-    return HCCL_OK;
-}
-
-hccl_status_t check_matrix(const void* p, int64_t rows, int64_t ld, int64_t width, int dt) {
-    if (!sane(rows, ld, width)) return HCCL_ERR_INVALID_ARG;
-    if (rows && width && !p) return HCCL_ERR_INVALID_ARG;
-    return aligned(p, hccl::elem_bytes(dt)) ? HCCL_OK : HCCL_ERR_ALIGNMENT;
-}
-
-#define TRY(x)                               \
-    do {                                     \
-        const hccl_status_t st_ = (x);       \
-        if (st_ != HCCL_OK) return st_;      \
-    } while (0)
 
 RouteParams route_params(const hccl_router_t* c, const void* logits, int64_t ld, const float* bias, const uint8_t* mask, const hccl_routing_t* r) {
     RouteParams p = {};
@@ -312,6 +281,21 @@ hccl_status_t hccl_call_packed(int32_t call, const int64_t* a) {
         m.y = at(13), m.ldy = a[14], m.dev_status = (int32_t*)at(15);
         return m;
     };
+    const auto f32 = [&](int i) {
+        const uint32_t bits = (uint32_t)a[i];
+        float f;
+        memcpy(&f, &bits, 4);
+        return f;
+    };
+    const auto matmul_fp4 = [&] {
+        hccl_matmul_fp4_t m = {};
+        m.M = a[0], m.N = a[1], m.K = a[2], m.groups = (int32_t)a[3], m.dtype = (int32_t)a[4], m.format = (int32_t)a[5], m.x_wide = f32(6);
+        m.w = (const uint8_t*)at(7), m.ldw = a[8], m.w_scale = at(9), m.w_wide = (const float*)at(10);
+        m.bias = (const float*)at(11), m.offsets = (const int32_t*)at(12);
+        m.y = at(13), m.ldy = a[14], m.scratch = at(15), m.scratch_bytes = a[16];
+        m.dev_status = (int32_t*)at(17);
+        return m;
+    };
     switch (call) {
         case HCCL_CALL_ROUTE:
             return hccl_route((const hccl_router_t*)at(0), at(1), a[2], dt(3), (const float*)at(4), (const uint8_t*)at(5), (const hccl_routing_t*)at(6), at(7), (size_t)a[8], at(9));
@@ -335,6 +319,18 @@ hccl_status_t hccl_call_packed(int32_t call, const int64_t* a) {
         case HCCL_CALL_LINEAR_I8: {
             const hccl_matmul_i8_t m = matmul();
             return hccl_linear_i8(&m, at(16), a[17], dt(18), (const hccl_routing_t*)at(19), at(20));
+        }
+        case HCCL_CALL_QUANTIZE_ROWS_FP4:
+            return hccl_quantize_rows_fp4(at(0), a[1], a[2], a[3], dt(4), (int32_t)a[5], f32(6), (const hccl_routing_t*)at(7), (uint8_t*)at(8), a[9], (uint8_t*)at(10), a[11], a[12], at(13));
+        case HCCL_CALL_DEQUANTIZE_ROWS_FP4:
+            return hccl_dequantize_rows_fp4((const uint8_t*)at(0), a[1], (const uint8_t*)at(2), a[3], a[4], a[5], (int32_t)a[6], f32(7), at(8), a[9], dt(10), at(11));
+        case HCCL_CALL_MATMUL_FP4: {
+            const hccl_matmul_fp4_t m = matmul_fp4();
+            return hccl_matmul_fp4(&m, (const uint8_t*)at(18), a[19], (const uint8_t*)at(20), a[21], at(22));
+        }
+        case HCCL_CALL_LINEAR_FP4: {
+            const hccl_matmul_fp4_t m = matmul_fp4();
+            return hccl_linear_fp4(&m, at(18), a[19], dt(20), (const hccl_routing_t*)at(21), at(22));
         }
         default:
             return HCCL_ERR_INVALID_ARG;

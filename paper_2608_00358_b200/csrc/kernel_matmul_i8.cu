@@ -16,18 +16,15 @@
 // Measured (B200; twice the bf16 library rate is 3.3 POP/s): 8192^3 308-345 us = 3.2-3.6 POP/s, 535 cycles for a stage whose products take 512, at the 1.5 GHz that the power
 // limit leaves (1.9 GHz and 255 us on zeros): the tensor cores are the bound. 64 matrices 2048 x 4096: 512 rows 85 us = 6.1-6.3 TB/s of weights, 65536 rows 375-390 us. 16 rows, 8192 x 4096: 10.8 us = 3.1 TB/s.
 // 997 x 2064 x 4104, one round of the blocks: 13.7 us, of which 0.8 set-up, 7 products (665 cycles a stage, fed from the L2), 3 results.
-#include <cuda.h>
-
 #include <atomic>
 
-#include "experts.cuh"
+#include "tensor.cuh"
 
 namespace hccl {
 namespace experts {
 namespace {
 
-constexpr int MM_THREADS = 384, CH = 128 /* channels of a tile */, KB = 128 /* bytes of K in a stage */;
-constexpr unsigned long long WAIT_NS = 2000000000ull;  // bound of every wait
+constexpr int MM_THREADS = 384, CH = 128 /* channels of a tile */;
 
 template <int TN, int CG> struct Shape {
     static constexpr int ROWS = TN / CG;               // token rows that a block holds
@@ -50,89 +47,12 @@ struct TileParams {
 };
 
 // ---------------------------------------------------------------- instructions
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok;
-}
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-// One lane of a warp that is whole here. The matrix and copy instructions want their operands in uniform registers: issued behind
-// `lane == 0` the compiler cannot tell that one lane is left and wraps each in a loop over lanes (169 cycles an instruction, measured, against
-// 128 of products at 256 columns); behind this it can, if the operands come from values that are the same in all lanes.
-__device__ __forceinline__ bool elected() {
-    uint32_t e;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(e));
-    return e;
-}
-// Waits for a phase to complete, by a whole warp. After WAIT_NS, or once another wait of this block has given up, it returns false.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
-    const unsigned long long t0 = now_ns();
-    for (;;) {
-        for (int i = 0; i < 64; i++)
-            if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
-        if (now_ns() - t0 > WAIT_NS) *gave_up = 1;
-        if (__any_sync(0xffffffffu, *gave_up)) return false;
-    }
-}
-__device__ __forceinline__ uint32_t of_rank(uint32_t addr, uint32_t rank) {  // the same place in another block of the cluster
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory"); }
-// bar: an address in the cluster's shared memory; with CG = 2 it may lie in the pair's other block.
-template <int CG> __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    if constexpr (CG == 2) {
-        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-        return;
-    }
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-// Shared-memory operand with 128-byte rows of K in the 128-byte swizzle: groups of 8 rows lie 1024 bytes apart.
-__device__ __forceinline__ uint64_t operand(uint32_t addr) {
-    return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
 template <int CG> __device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t accumulate) {
     if constexpr (CG == 2)
         asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(accumulate) : "memory");
     else
         asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(accumulate) : "memory");
 }
-// Arrives at the barrier, in both blocks of a pair, when the instructions issued so far are done.
-template <int CG> __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    if constexpr (CG == 2)
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_load(uint32_t addr, int (&v)[16]) {  // 16 columns of a warp's 32 lanes; tmem_arrived before use
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
-                   "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-                 : "r"(addr));
-}
-__device__ __forceinline__ void tmem_arrived() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ int4 cluster_load(uint32_t addr, uint32_t rank) {
-    int4 v;
-    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(of_rank(addr, rank)) : "memory");
-    return v;
-}
-
 // The same value as (float)v, one rounding to nearest even, by way of its halves: 2^23 + h is a number whose low bits are the 16-bit h, so both
 // halves become exact floating-point numbers by a byte permutation and a subtraction, and one fused multiply-add joins and rounds them.
 // The conversion instruction runs at an eighth of the rate of these six; results take turns between the two.
@@ -452,32 +372,6 @@ template <typename T, int TN, int CG> __global__ void __launch_bounds__(MM_THREA
 }
 
 // ---------------------------------------------------------------- host
-typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn encoder() {
-    static const EncodeFn fn = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) f = nullptr;
-        return (EncodeFn)f;
-    }();
-    return fn;
-}
-
-// Rows of `ld` bytes of which K count; a box is 128 bytes wide. What lies beyond K or beyond the rows reads as zero.
-cudaError_t make_map(CUtensorMap* m, const void* at, long long rows, long long K, long long ld, int box_rows) {
-    const EncodeFn fn = encoder();
-    if (!fn) return cudaErrorNotSupported;
-    const long long least = (K + 15) / 16 * 16;
-    const cuuint64_t dim[2] = {(cuuint64_t)K, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)(ld > least ? ld : least)};
-    const cuuint32_t box[2] = {KB, (cuuint32_t)box_rows}, one[2] = {1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(at), dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
-               ? cudaSuccess
-               : cudaErrorInvalidValue;
-}
-
 template <typename T, int TN, int CG> cudaError_t tiles_launch(const MatmulParams& q, int splits, cudaStream_t s) {
     using S = Shape<TN, CG>;
     TileParams p = {};

@@ -673,13 +673,46 @@ hccl_status_t hccl_fp4_scratch_bytes(int64_t M, int64_t N, int64_t K, int32_t gr
 hccl_status_t hccl_matmul_fp4(const hccl_matmul_fp4_t*, const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, void* stream);
 hccl_status_t hccl_linear_fp4(const hccl_matmul_fp4_t*, const void* x, int64_t ldx, hccl_dtype_t x_dt, const hccl_routing_t* routing, void* stream);
 
-/* The expert-layer calls with their arguments as one array of 64-bit integers in the same order (pointers as addresses; in the place of an hccl_matmul_i8_t or
- * hccl_matmul_fp4_t its fields one by one, a 32-bit float by its bits), for bindings to which each argument costs. The names carry the number of arguments in their second byte. Refusals are the call's own;
+/* A whole expert layer for a few tokens, in two kernels: y[t] = round(sum over k of weights[t,k] (down_e h_e + down_bias_e)), e = ids[t,k], with
+ * u = up_e x[t] + up_bias_e and h = act(u[0..I-1]) * u[I..2I-1] if gated, act(u) otherwise. Weights in 4 bits as in hccl_matmul_fp4_t: up [experts, 2 I or I, H], down
+ * [experts, H, I], their scales from hccl_fp4_weight_scales. Activations are not rounded to 4 bits: they enter the products as sums of eight such numbers, which leaves 6^-8 (HCCL_MXFP4: 4^-8) of a block's largest
+ * element; sums, u and h are FP32. A row with an infinity or a NaN gives NaN. Choices without an expert add nothing; a token without any gets 0.
+ * Reads the routing's weights, offsets, slots and source. tokens <= HCCL_MAX_FEW_TOKENS; H and I from 1 to HCCL_MAX_FP4_K. scratch: hccl_expert_layer_scratch_bytes, 128-byte aligned, contents
+ * arbitrary, not shared by calls in flight at once. dev_status as in hccl_matmul_i8_t. */
+#define HCCL_MAX_FEW_TOKENS 64
+typedef enum { HCCL_ACT_SILU = 0, HCCL_ACT_GELU = 1, HCCL_ACT_RELU = 2 } hccl_act_t; /* x sigmoid(x); x Phi(x), Phi of the normal distribution; max(x, 0) */
+typedef struct {
+    int64_t H, I;
+    int32_t experts, format, act, gated;
+    const uint8_t* up; int64_t ld_up; const void* up_scale; const float* up_wide; const float* up_bias;
+    const uint8_t* down; int64_t ld_down; const void* down_scale; const float* down_wide; const float* down_bias;
+} hccl_experts_fp4_t;
+hccl_status_t hccl_expert_layer_scratch_bytes(const hccl_experts_fp4_t*, int64_t tokens, int32_t top_k, size_t* bytes);
+hccl_status_t hccl_expert_layer_fp4(const hccl_experts_fp4_t*, const void* x, int64_t ldx, hccl_dtype_t dt, const hccl_routing_t* routing, void* y, int64_t ldy,
+                                    void* scratch, size_t bytes, int32_t* dev_status, void* stream);
+
+/* What stands between an expert's two products in training: y[r,i] = act(x[r,i]) * x[r,I+i] * m[r,i] (x [M, 2 I]; not gated: x [M, I], y = act(x) m), and its gradient
+ * dx for a gradient dy [M, I] of y. m is 0 or 1 / (1 - p), from Philox-4x32-10 with the key seed[0] and the counter (n / 4, seed[1]), n = r * I + i: kept
+ * if word n % 4 is at least p 2^32 rounded (p 2^32 at most 2^32 - 1). The mask is not stored; the same seed gives it again. A dropped element and its gradient are 0, whatever x is. seed: two int64 in device
+ * memory, not read if p is 0. groups > 0: rows from offsets[groups] on (device memory) are not read and become 0 in y and dx. One rounding at the end. */
+typedef struct {
+    int32_t act, gated;
+    double p;             /* from 0 to below 1 */
+    const int64_t* seed;
+} hccl_activation_t;
+hccl_status_t hccl_activate(const hccl_activation_t*, const void* x, int64_t ldx, int64_t M, int64_t I, hccl_dtype_t dt, const int32_t* offsets, int32_t groups,
+                            void* y, int64_t ldy, void* stream);
+hccl_status_t hccl_activate_backward(const hccl_activation_t*, const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t M, int64_t I, hccl_dtype_t dt,
+                                     const int32_t* offsets, int32_t groups, void* dx, int64_t lddx, void* stream);
+
+/* The expert-layer calls with their arguments as one array of 64-bit integers in the same order (pointers as addresses; in the place of an hccl_matmul_i8_t,
+ * hccl_matmul_fp4_t or hccl_activation_t its fields one by one, floating-point numbers by their bits), for bindings to which each argument costs. The names carry the number of arguments in their second byte. Refusals are the call's own;
  * any other value of `call` is refused. */
 typedef enum {
     HCCL_CALL_ROUTE = 0x0a00, HCCL_CALL_ROUTE_BACKWARD = 0x0b01, HCCL_CALL_DISPATCH = 0x0902, HCCL_CALL_DISPATCH_BACKWARD = 0x0903, HCCL_CALL_COMBINE = 0x0a04,
     HCCL_CALL_COMBINE_BACKWARD = 0x0d05, HCCL_CALL_QUANTIZE_ROWS_I8 = 0x0b06, HCCL_CALL_MATMUL_I8 = 0x1107, HCCL_CALL_LINEAR_I8 = 0x1508,
-    HCCL_CALL_QUANTIZE_ROWS_FP4 = 0x0e09, HCCL_CALL_DEQUANTIZE_ROWS_FP4 = 0x0c0a, HCCL_CALL_MATMUL_FP4 = 0x170b, HCCL_CALL_LINEAR_FP4 = 0x170c
+    HCCL_CALL_QUANTIZE_ROWS_FP4 = 0x0e09, HCCL_CALL_DEQUANTIZE_ROWS_FP4 = 0x0c0a, HCCL_CALL_MATMUL_FP4 = 0x170b, HCCL_CALL_LINEAR_FP4 = 0x170c,
+    HCCL_CALL_EXPERT_LAYER_FP4 = 0x0b0d, HCCL_CALL_ACTIVATE = 0x0e0e, HCCL_CALL_ACTIVATE_BACKWARD = 0x100f
 } hccl_call_t;
 hccl_status_t hccl_call_packed(int32_t call, const int64_t* arguments);
 

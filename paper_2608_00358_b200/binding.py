@@ -30,6 +30,8 @@ NOALLOC_WORKSPACE_BYTES = 8 << 20
 ELEM_BYTES = {FP32: 4, BF16: 2, FP16: 2}
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 NVFP4, MXFP4 = 0, 1
+ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
+MAX_FEW_TOKENS = 64
 MAX_EXPERTS, MAX_TOP_K, MAX_I8_K = 1024, 32, 131071
 ROUTE_NO_WORKSPACE = 16
 
@@ -85,6 +87,18 @@ class MatmulFp4(C.Structure):
     _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("groups", C.c_int32), ("dtype", C.c_int32), ("format", C.c_int32), ("x_wide", C.c_float),
                 ("w", C.c_void_p), ("ldw", C.c_int64), ("w_scale", C.c_void_p), ("w_wide", C.c_void_p), ("bias", C.c_void_p), ("offsets", C.c_void_p),
                 ("y", C.c_void_p), ("ldy", C.c_int64), ("scratch", C.c_void_p), ("scratch_bytes", C.c_int64), ("dev_status", C.c_void_p)]
+
+
+class ExpertsFp4(C.Structure):
+    """hccl_experts_fp4_t"""
+    _fields_ = [("H", C.c_int64), ("I", C.c_int64), ("experts", C.c_int32), ("format", C.c_int32), ("act", C.c_int32), ("gated", C.c_int32),
+                ("up", C.c_void_p), ("ld_up", C.c_int64), ("up_scale", C.c_void_p), ("up_wide", C.c_void_p), ("up_bias", C.c_void_p),
+                ("down", C.c_void_p), ("ld_down", C.c_int64), ("down_scale", C.c_void_p), ("down_wide", C.c_void_p), ("down_bias", C.c_void_p)]
+
+
+class Activation(C.Structure):
+    """hccl_activation_t"""
+    _fields_ = [("act", C.c_int32), ("gated", C.c_int32), ("p", C.c_double), ("seed", C.c_void_p)]
 
 
 class HcclError(RuntimeError):
@@ -153,6 +167,10 @@ def _load() -> C.CDLL:
         "hccl_fp4_scratch_bytes": [C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)],
         "hccl_matmul_fp4": [C.POINTER(MatmulFp4), P, C.c_int64, P, C.c_int64, P],
         "hccl_linear_fp4": [C.POINTER(MatmulFp4), P, C.c_int64, C.c_int, RG, P],
+        "hccl_expert_layer_scratch_bytes": [C.POINTER(ExpertsFp4), C.c_int64, C.c_int32, C.POINTER(C.c_size_t)],
+        "hccl_expert_layer_fp4": [C.POINTER(ExpertsFp4), P, C.c_int64, C.c_int, RG, P, C.c_int64, P, C.c_size_t, P, P],
+        "hccl_activate": [C.POINTER(Activation), P, C.c_int64, C.c_int64, C.c_int64, C.c_int, P, C.c_int32, P, C.c_int64, P],
+        "hccl_activate_backward": [C.POINTER(Activation), P, C.c_int64, P, C.c_int64, C.c_int64, C.c_int64, C.c_int, P, C.c_int32, P, C.c_int64, P],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -192,7 +210,7 @@ EXPORTS = ["hccl_plan_allreduce", "hccl_plan_reducescatter", "hccl_plan_allgathe
            "hccl_route_workspace_bytes", "hccl_route", "hccl_route_backward", "hccl_dispatch", "hccl_dispatch_backward", "hccl_combine",
            "hccl_combine_backward", "hccl_quantize_rows_i8", "hccl_matmul_i8", "hccl_linear_i8", "hccl_call_packed",
            "hccl_quantize_rows_fp4", "hccl_dequantize_rows_fp4", "hccl_fp4_weight_scale_bytes", "hccl_fp4_weight_scales", "hccl_fp4_scratch_bytes",
-           "hccl_matmul_fp4", "hccl_linear_fp4"]
+           "hccl_matmul_fp4", "hccl_linear_fp4", "hccl_expert_layer_scratch_bytes", "hccl_expert_layer_fp4", "hccl_activate", "hccl_activate_backward"]
 
 
 def status_string(status: int) -> str:
@@ -396,17 +414,21 @@ hccl_dequantize_rows_fp4 = _call("hccl_dequantize_rows_fp4")
 hccl_fp4_weight_scales = _call("hccl_fp4_weight_scales")
 hccl_matmul_fp4 = _call("hccl_matmul_fp4")
 hccl_linear_fp4 = _call("hccl_linear_fp4")
+hccl_expert_layer_fp4 = _call("hccl_expert_layer_fp4")
+hccl_activate = _call("hccl_activate")
+hccl_activate_backward = _call("hccl_activate_backward")
 
 
 # hccl_call_t: which call, and in the second byte how many arguments it has
 CALLS = {"hccl_route": 0x0a00, "hccl_route_backward": 0x0b01, "hccl_dispatch": 0x0902, "hccl_dispatch_backward": 0x0903, "hccl_combine": 0x0a04,
          "hccl_combine_backward": 0x0d05, "hccl_quantize_rows_i8": 0x0b06, "hccl_matmul_i8": 0x1107, "hccl_linear_i8": 0x1508,
-         "hccl_quantize_rows_fp4": 0x0e09, "hccl_dequantize_rows_fp4": 0x0c0a, "hccl_matmul_fp4": 0x170b, "hccl_linear_fp4": 0x170c}
+         "hccl_quantize_rows_fp4": 0x0e09, "hccl_dequantize_rows_fp4": 0x0c0a, "hccl_matmul_fp4": 0x170b, "hccl_linear_fp4": 0x170c,
+         "hccl_expert_layer_fp4": 0x0b0d, "hccl_activate": 0x0e0e, "hccl_activate_backward": 0x100f}
 
 
 def packed(name: str):
     """The same call for code that makes it often: all arguments integers (structures by address, NULL 0; of the products the fields of
-    hccl_matmul_i8_t or hccl_matmul_fp4_t one by one, a float by its bits), handed over as one array."""
+    hccl_matmul_i8_t, hccl_matmul_fp4_t or hccl_activation_t one by one, floating-point numbers by their bits), handed over as one array."""
     which = CALLS[name]
     fn, pack = _lib.hccl_call_packed, struct.Struct("%dq" % (which >> 8)).pack
 
@@ -432,6 +454,12 @@ def hccl_fp4_weight_scale_bytes(N: int, K: int, groups: int, format: int) -> int
 def hccl_fp4_scratch_bytes(M: int, N: int, K: int, groups: int, format: int) -> int:
     n = C.c_size_t()
     _chk(_lib.hccl_fp4_scratch_bytes(M, N, K, groups, format, C.byref(n)), "hccl_fp4_scratch_bytes")
+    return n.value
+
+
+def hccl_expert_layer_scratch_bytes(experts: ExpertsFp4, tokens: int, top_k: int) -> int:
+    n = C.c_size_t()
+    _chk(_lib.hccl_expert_layer_scratch_bytes(C.byref(experts), tokens, top_k, C.byref(n)), "hccl_expert_layer_scratch_bytes")
     return n.value
 
 

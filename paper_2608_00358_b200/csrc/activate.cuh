@@ -1,0 +1,43 @@
+// Activations of expert layers and their slopes, in 32 bits.
+#pragma once
+#include "experts.cuh"
+
+namespace hccl {
+namespace experts {
+
+__device__ __forceinline__ float activation(int act, float g) {
+    if (act == HCCL_ACT_SILU) return g / (1.f + expf(-g));
+    if (act == HCCL_ACT_GELU) return g * normcdff(g);
+    return g > 0.f || g != g ? g : 0.f;
+}
+// And its derivative; of the rectifier at 0: 0.
+__device__ __forceinline__ void activation_slope(int act, float g, float* a, float* slope) {
+    if (act == HCCL_ACT_SILU) {
+        const float s = 1.f / (1.f + expf(-g));
+        *a = g * s;
+        *slope = s * (1.f + g * (1.f - s));
+    } else if (act == HCCL_ACT_GELU) {
+        const float phi = normcdff(g);
+        *a = g * phi;
+        *slope = phi + g * expf(-0.5f * g * g) * 0.39894228f;
+    } else {
+        *a = g > 0.f || g != g ? g : 0.f;
+        *slope = g > 0.f ? 1.f : 0.f;
+    }
+}
+
+struct ActivateParams {
+    const void *x, *dy;  // [M, 2 I] (not gated: [M, I]); the gradient of the result [M, I]
+    void* out;
+    long long ldx, ldy, ldo, M, I;
+    const long long* seed;  // key and call
+    const int* offsets;     // null: all rows
+    int groups, act, gated, drop;
+    unsigned threshold;     // of a 32-bit word
+    float keep;             // 1 / (1 - p)
+};
+cudaError_t launch_activate(int dt, const ActivateParams& p, cudaStream_t s);
+cudaError_t launch_activate_grad(int dt, const ActivateParams& p, cudaStream_t s);
+
+}  // namespace experts
+}  // namespace hccl

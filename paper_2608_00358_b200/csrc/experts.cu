@@ -296,6 +296,13 @@ hccl_status_t hccl_call_packed(int32_t call, const int64_t* a) {
         m.dev_status = (int32_t*)at(17);
         return m;
     };
+    const auto activation = [&] {
+        hccl_activation_t f = {};
+        f.act = (int32_t)a[0], f.gated = (int32_t)a[1];
+        memcpy(&f.p, &a[2], 8);
+        f.seed = (const int64_t*)at(3);
+        return f;
+    };
     switch (call) {
         case HCCL_CALL_ROUTE:
             return hccl_route((const hccl_router_t*)at(0), at(1), a[2], dt(3), (const float*)at(4), (const uint8_t*)at(5), (const hccl_routing_t*)at(6), at(7), (size_t)a[8], at(9));
@@ -331,6 +338,16 @@ hccl_status_t hccl_call_packed(int32_t call, const int64_t* a) {
         case HCCL_CALL_LINEAR_FP4: {
             const hccl_matmul_fp4_t m = matmul_fp4();
             return hccl_linear_fp4(&m, at(18), a[19], dt(20), (const hccl_routing_t*)at(21), at(22));
+        }
+        case HCCL_CALL_EXPERT_LAYER_FP4:
+            return hccl_expert_layer_fp4((const hccl_experts_fp4_t*)at(0), at(1), a[2], dt(3), (const hccl_routing_t*)at(4), at(5), a[6], at(7), (size_t)a[8], (int32_t*)at(9), at(10));
+        case HCCL_CALL_ACTIVATE: {
+            const hccl_activation_t f = activation();
+            return hccl_activate(&f, at(4), a[5], a[6], a[7], dt(8), (const int32_t*)at(9), (int32_t)a[10], at(11), a[12], at(13));
+        }
+        case HCCL_CALL_ACTIVATE_BACKWARD: {
+            const hccl_activation_t f = activation();
+            return hccl_activate_backward(&f, at(4), a[5], at(6), a[7], a[8], a[9], dt(10), (const int32_t*)at(11), (int32_t)a[12], at(13), a[14], at(15));
         }
         default:
             return HCCL_ERR_INVALID_ARG;

@@ -1,4 +1,7 @@
 // C entry points of the operators in 4-bit floating point: argument checks and launches.
+#include <cmath>
+
+#include "activate.cuh"
 #include "checks.h"
 #include "fp4.cuh"
 
@@ -250,6 +253,120 @@ hccl_status_t hccl_linear_fp4(const hccl_matmul_fp4_t* in, const void* x, int64_
         mm.dependent = p.M > 0;
     }
     return done(launch_matmul_fp4(m.dtype, mm, (cudaStream_t)stream), "hccl_linear_fp4");
+}
+
+static hccl_status_t check_experts(const hccl_experts_fp4_t* e, int64_t tokens, int32_t top_k) {
+    if (!e || tokens < 0 || tokens > HCCL_MAX_FEW_TOKENS || top_k < 1 || top_k > HCCL_MAX_TOP_K) return HCCL_ERR_INVALID_ARG;
+    if (e->experts < 1 || e->H < 1 || e->I < 1 || e->I > HCCL_MAX_FP4_K) return HCCL_ERR_INVALID_ARG;
+    if (e->act != HCCL_ACT_SILU && e->act != HCCL_ACT_GELU && e->act != HCCL_ACT_RELU) return HCCL_ERR_INVALID_ARG;
+    TRY(check_weights(e->gated ? 2 * e->I : e->I, e->H, e->experts, e->format));
+    return check_weights(e->H, e->I, e->experts, e->format);
+}
+
+hccl_status_t hccl_expert_layer_scratch_bytes(const hccl_experts_fp4_t* e, int64_t tokens, int32_t top_k, size_t* bytes) {
+    TRY(check_experts(e, tokens, top_k));
+    if (!bytes) return HCCL_ERR_INVALID_ARG;
+    *bytes = few_fp4_scratch(tokens, e->H, e->I, top_k, e->gated != 0);
+    return HCCL_OK;
+}
+
+hccl_status_t hccl_expert_layer_fp4(const hccl_experts_fp4_t* e, const void* x, int64_t ldx, hccl_dtype_t dt, const hccl_routing_t* r, void* y, int64_t ldy, void* scratch,
+                                    size_t bytes, int32_t* dev_status, void* stream) {
+    TRY(check_routing(r));
+    TRY(check_experts(e, r->tokens, r->top_k));
+    if (!hccl::valid_dtype(dt)) return HCCL_ERR_DTYPE;
+    if (r->experts != e->experts) return HCCL_ERR_COUNT_MISMATCH;
+    TRY(check_matrix(x, r->tokens, ldx, e->H, dt));
+    TRY(check_matrix(y, r->tokens, ldy, e->H, dt));
+    const int64_t N = e->gated ? 2 * e->I : e->I;
+    if (!sane(N * e->experts, e->ld_up, (e->H + 1) / 2) || !sane(e->H * e->experts, e->ld_down, (e->I + 1) / 2)) return HCCL_ERR_INVALID_ARG;
+    if (!e->up || !e->up_scale || !e->up_wide || !e->down || !e->down_scale || !e->down_wide) return HCCL_ERR_INVALID_ARG;
+    if (!aligned(e->up, 16) || e->ld_up % 16 || !aligned(e->up_scale, 16) || !aligned(e->down, 16) || e->ld_down % 16 || !aligned(e->down_scale, 16)) return HCCL_ERR_ALIGNMENT;
+    if (!aligned(e->up_wide, 4) || !aligned(e->up_bias, 4) || !aligned(e->down_wide, 4) || !aligned(e->down_bias, 4) || !aligned(dev_status, 4)) return HCCL_ERR_ALIGNMENT;
+    if (r->tokens == 0) return HCCL_OK;
+    if (!r->weights || !r->source) return HCCL_ERR_INVALID_ARG;
+    if (!aligned(r->weights, 4) || !aligned(r->source, 4)) return HCCL_ERR_ALIGNMENT;
+    if (!scratch || bytes < few_fp4_scratch(r->tokens, e->H, e->I, r->top_k, e->gated != 0)) return HCCL_ERR_WORKSPACE;
+    if (!aligned(scratch, 128)) return HCCL_ERR_ALIGNMENT;
+    FewFp4 p = {};
+    p.T = r->tokens;
+    p.H = e->H;
+    p.I = e->I;
+    p.ldx = ldx;
+    p.ldy = ldy;
+    p.top_k = r->top_k;
+    p.experts = e->experts;
+    p.format = e->format;
+    p.act = e->act;
+    p.gated = e->gated != 0;
+    p.x = x;
+    p.y = y;
+    p.offsets = r->offsets;
+    p.source = r->source;
+    p.slots = r->slots;
+    p.weights = r->weights;
+    p.up = e->up;
+    p.up_scale = (const uint8_t*)e->up_scale;
+    p.ld_up = e->ld_up;
+    p.up_wide = e->up_wide;
+    p.up_bias = e->up_bias;
+    p.down = e->down;
+    p.down_scale = (const uint8_t*)e->down_scale;
+    p.ld_down = e->ld_down;
+    p.down_wide = e->down_wide;
+    p.down_bias = e->down_bias;
+    p.scratch = (char*)scratch;
+    p.status = dev_status;
+    return done(launch_few_fp4(dt, p, (cudaStream_t)stream), "hccl_expert_layer_fp4");
+}
+
+static hccl_status_t activate_params(ActivateParams* q, const hccl_activation_t* a, const void* x, int64_t ldx, int64_t M, int64_t I, hccl_dtype_t dt, const int32_t* offsets,
+                                     int32_t groups) {
+    if (!a || M < 0 || I < 0 || I > (INT64_C(1) << 40) || groups < 0) return HCCL_ERR_INVALID_ARG;
+    if (a->act != HCCL_ACT_SILU && a->act != HCCL_ACT_GELU && a->act != HCCL_ACT_RELU) return HCCL_ERR_INVALID_ARG;
+    if (!(a->p >= 0 && a->p < 1)) return HCCL_ERR_INVALID_ARG;
+    if (!hccl::valid_dtype(dt)) return HCCL_ERR_DTYPE;
+    if ((a->p > 0 && M && I && !a->seed) || (groups && !offsets)) return HCCL_ERR_INVALID_ARG;
+    TRY(check_matrix(x, M, ldx, a->gated ? 2 * I : I, dt));
+    if (!aligned(a->seed, 8) || !aligned(offsets, 4)) return HCCL_ERR_ALIGNMENT;
+    *q = {};
+    q->x = x;
+    q->ldx = ldx;
+    q->M = M;
+    q->I = I;
+    q->seed = (const long long*)a->seed;
+    q->offsets = groups ? offsets : nullptr;
+    q->groups = groups;
+    q->act = a->act;
+    q->gated = a->gated != 0;
+    q->drop = a->p > 0;
+    const double at = nearbyint(a->p * 4294967296.0);
+    q->threshold = at > 4294967295.0 ? 4294967295u : (unsigned)at;
+    q->keep = (float)(1.0 / (1.0 - a->p));
+    return HCCL_OK;
+}
+
+hccl_status_t hccl_activate(const hccl_activation_t* a, const void* x, int64_t ldx, int64_t M, int64_t I, hccl_dtype_t dt, const int32_t* offsets, int32_t groups, void* y,
+                            int64_t ldy, void* stream) {
+    ActivateParams p;
+    TRY(activate_params(&p, a, x, ldx, M, I, dt, offsets, groups));
+    TRY(check_matrix(y, M, ldy, I, dt));
+    p.out = y;
+    p.ldo = ldy;
+    return done(launch_activate(dt, p, (cudaStream_t)stream), "hccl_activate");
+}
+
+hccl_status_t hccl_activate_backward(const hccl_activation_t* a, const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t M, int64_t I, hccl_dtype_t dt,
+                                     const int32_t* offsets, int32_t groups, void* dx, int64_t lddx, void* stream) {
+    ActivateParams p;
+    TRY(activate_params(&p, a, x, ldx, M, I, dt, offsets, groups));
+    TRY(check_matrix(dy, M, lddy, I, dt));
+    TRY(check_matrix(dx, M, lddx, a->gated ? 2 * I : I, dt));
+    p.dy = dy;
+    p.ldy = lddy;
+    p.out = dx;
+    p.ldo = lddx;
+    return done(launch_activate_grad(dt, p, (cudaStream_t)stream), "hccl_activate_backward");
 }
 
 }  // extern "C"

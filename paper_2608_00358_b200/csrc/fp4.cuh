@@ -65,6 +65,7 @@ __device__ __forceinline__ unsigned eight_codes(const float* q) {
         : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
     return r;
 }
+// Of a word from memory or from another lane: straight behind eight_codes, in registers, the compiler (12.9) gets the bytes wrong.
 __device__ __forceinline__ void eight_values(unsigned w, float* v) {
     unsigned h[4];
     asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"

@@ -8,19 +8,22 @@ the ones after it); streams, scratch and errors are those of experts.py.
     y = up(x, routing=r)                                                    # rows gathered, quantised, multiplied
     rows = quantize_rows(x, routing=r)                                      # the send buffer of an exchange, in about a quarter of the bytes
     h = up.matmul(rows, offsets=r.offsets)
+    y = FewTokens(up, down, act="silu")(x, r)                               # a decode step: the whole layer in two kernels
 """
 from __future__ import annotations
 
+import ctypes as C
 import struct
 from typing import Optional
 
 import torch
 
 from . import binding as hb
-from .experts import (_DT, _capturing, _dtype, _given, _matrix, _new, _no_gradient, _on, _pad16, _refuse, _scratch, _stream, _vector, Routing)
+from .activation import ACTS
+from .experts import (_DT, _dtype, _given, _matrix, _new, _no_gradient, _on, _pad16, _refuse, _scratch, _stream, _vector, Routing)
 
 _quantize, _dequantize = hb.packed("hccl_quantize_rows_fp4"), hb.packed("hccl_dequantize_rows_fp4")
-_matmul, _linear = hb.packed("hccl_matmul_fp4"), hb.packed("hccl_linear_fp4")
+_matmul, _linear, _layer = hb.packed("hccl_matmul_fp4"), hb.packed("hccl_linear_fp4"), hb.packed("hccl_expert_layer_fp4")
 
 FORMATS = {"nvfp4": hb.NVFP4, "mxfp4": hb.MXFP4}
 BLOCK = {"nvfp4": 16, "mxfp4": 32}
@@ -242,3 +245,60 @@ class Fp4Linear:
         if st != hb.OK:
             self._status.zero_()
             raise hb.HcclError(st, "Fp4Linear")
+
+
+class FewTokens:
+    """A whole expert layer for a few tokens (at most 64) in two kernels: y[t] = sum over k of weights[t, k] down_e(h_e), e = ids[t, k]. gated: up is [experts, 2 I, H] with the
+    gate's rows first, h = act(gate) * other; otherwise up is [experts, I, H] and h = act(up(x)). down is [experts, H, I], of the same format. The weights
+    are in 4 bits, activations are not: where up and down quantise the rows that they are called with, this does not, so that it is nearer to the layer in floating point
+    than down(act(up(x))). For serving: an input that requires a gradient is refused."""
+
+    def __init__(self, up: Fp4Linear, down: Fp4Linear, act: str = "silu", gated: bool = True):
+        if act not in ACTS:
+            _refuse(hb.ERR_INVALID_ARG, "FewTokens: act %r, expected one of %s" % (act, ", ".join(ACTS)))
+        if not up.experts or up.experts != down.experts or up.dev != down.dev:
+            _refuse(hb.ERR_INVALID_ARG, "FewTokens: up and down must be over the same number of experts, on one device")
+        if up.format != down.format:
+            _refuse(hb.ERR_DTYPE, "FewTokens: up in %s, down in %s" % (up.format, down.format))
+        if up.N != (2 if gated else 1) * down.K or down.N != up.K:
+            _refuse(hb.ERR_COUNT_MISMATCH, "FewTokens: layers are %d -> %d and %d -> %d" % (up.K, up.N, down.K, down.N))
+        self.up, self.down, self.act, self.gated = up, down, act, bool(gated)
+        self.H, self.dev, self.device = up.K, up.dev, up.device
+        _, w_up, ld_up, s_up, g_up, b_up = up._fixed
+        _, w_down, ld_down, s_down, g_down, b_down = down._fixed
+        self.record = hb.ExpertsFp4(up.K, down.K, up.experts, up.fmt, ACTS[act], 1 if gated else 0, w_up, ld_up, s_up, g_up, b_up, w_down, ld_down, s_down, g_down, b_down)
+        hb.hccl_expert_layer_scratch_bytes(self.record, 1, 1)  # refuses sizes that the kernels do not take
+        self._at = C.addressof(self.record)
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._status_at = self._status.data_ptr()
+        self._need = {}  # scratch bytes by tokens and top_k
+
+    def __reduce__(self):  # the record holds addresses
+        return FewTokens, (self.up, self.down, self.act, self.gated)
+
+    def __call__(self, x: torch.Tensor, routing: Routing, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x [tokens, H], its routing; returns [tokens, H] in x's type."""
+        dev, T, k = self.dev, routing.tokens, routing.top_k
+        _no_gradient(x, "x")
+        _no_gradient(routing.weights, "the routing's weights")
+        ldx, dt = _matrix(x, "x", self.H, T, dev), _dtype(x, "x")
+        if routing.experts != self.up.experts or routing.dev != dev:
+            _refuse(hb.ERR_COUNT_MISMATCH, "FewTokens: routing over %d experts on %s" % (routing.experts, routing.device))
+        need = self._need.get((T, k))
+        if need is None:
+            if T > hb.MAX_FEW_TOKENS:
+                _refuse(hb.ERR_INVALID_ARG, "FewTokens: %d tokens, at most %d" % (T, hb.MAX_FEW_TOKENS))
+            need = self._need[T, k] = hb.hccl_expert_layer_scratch_bytes(self.record, T, k)
+        out, ldy = _new(out, T, self.H, x, "out", dev)
+        stream = _stream(dev)
+        hold, at = _scratch.get(dev, stream, need)
+        _on(dev, _layer)(self._at, x.data_ptr(), ldx, dt, routing.at, out.data_ptr(), ldy, at, need, self._status_at, stream)
+        return out
+
+    def check(self):
+        """Synchronises and raises if a call failed on the device since the last check (its result is then undefined)."""
+        torch.cuda.synchronize(self.device)
+        st = int(self._status.item())
+        if st != hb.OK:
+            self._status.zero_()
+            raise hb.HcclError(st, "FewTokens")

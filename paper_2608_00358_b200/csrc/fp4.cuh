@@ -54,7 +54,7 @@ template <int FORMAT> __device__ __forceinline__ Step step_of(unsigned top, floa
 template <int FORMAT> __device__ __forceinline__ float quotient(float x, const Step& s) {
     const float y = __fmul_rn(x, s.inv);
     if constexpr (FORMAT == HCCL_MXFP4) return y;
-    return __fmaf_rn(__fmaf_rn(-y, s.d, x), s.inv, y);
+    return __fmaf_rn(-__fmaf_rn(y, s.d, -x), s.inv, y);  // (in these signs a negative zero stays one)
 }
 // Eight quotients to four bytes, the first in the lowest half-byte; |q| > 6 becomes 6.
 __device__ __forceinline__ unsigned eight_codes(const float* q) {

@@ -167,7 +167,7 @@ class Fp4Linear:
         wide = [1.0] * each.shape[0]
         if format == "nvfp4" and weight.numel():
             top = each.abs().amax((1, 2)).float()
-            wide = torch.where(torch.isfinite(top), (top / 2688).clamp(1e-30, 1e30), 1.0).tolist()
+            wide = torch.where(torch.isfinite(top), (top / top.new_tensor(2688.0)).clamp(1e-30, 1e30), 1.0).tolist()
         rows = [quantize_rows(w, format, s) for w, s in zip(each, wide)]
         q, s = (torch.stack([getattr(r, n) for r in rows]).view(weight.shape[:-1] + (-1,)) if rows and weight.numel() else
                 torch.zeros(weight.shape[:-1] + (width,), dtype=torch.uint8, device=weight.device)

@@ -33,7 +33,7 @@ bool few_atoms(int64_t tiles, int64_t K, int format) { return tiles * stages(K) 
 
 hccl_status_t check_weights(int64_t N, int64_t K, int32_t groups, int32_t format) {
     TRY(check_shape(N, K, format));
-    if (groups < 0 || groups > HCCL_MAX_EXPERTS) return HCCL_ERR_INVALID_ARG;
+    if (groups < 0 || groups > 2 * HCCL_MAX_EXPERTS) return HCCL_ERR_INVALID_ARG;
     const int64_t g = groups ? groups : 1;
     if (N > HCCL_MAX_I8_ROWS / g || !few_atoms((N + 127) / 128 * g, K, format)) return HCCL_ERR_INVALID_ARG;
     return HCCL_OK;
@@ -56,7 +56,7 @@ Scratch scratch_of(int64_t M, int64_t K, int32_t groups, int32_t format, int tn)
 }
 hccl_status_t check_product(int64_t M, int64_t N, int64_t K, int32_t groups, int32_t format) {
     TRY(check_weights(N, K, groups, format));
-    if (M < 0 || M > HCCL_MAX_I8_ROWS) return HCCL_ERR_INVALID_ARG;
+    if (M < 0 || M > HCCL_MAX_I8_ROWS || groups > HCCL_MAX_EXPERTS) return HCCL_ERR_INVALID_ARG;
     const int tn = choose_fp4(M, N, K, groups).tn;
     return few_atoms(((M + tn - 1) / tn + (groups ? groups : 1)) * (tn > 128 ? 2 : 1), K, format) ? HCCL_OK : HCCL_ERR_INVALID_ARG;
 }
@@ -257,16 +257,16 @@ hccl_status_t hccl_linear_fp4(const hccl_matmul_fp4_t* in, const void* x, int64_
 
 static hccl_status_t check_experts(const hccl_experts_fp4_t* e, int64_t tokens, int32_t top_k) {
     if (!e || tokens < 0 || tokens > HCCL_MAX_FEW_TOKENS || top_k < 1 || top_k > HCCL_MAX_TOP_K) return HCCL_ERR_INVALID_ARG;
-    if (e->experts < 1 || e->H < 1 || e->I < 1 || e->I > HCCL_MAX_FP4_K) return HCCL_ERR_INVALID_ARG;
+    if (e->experts < 1 || e->experts > HCCL_MAX_EXPERTS || e->H < 1 || e->I < 1 || e->I > HCCL_MAX_FP4_K) return HCCL_ERR_INVALID_ARG;
     if (e->act != HCCL_ACT_SILU && e->act != HCCL_ACT_GELU && e->act != HCCL_ACT_RELU) return HCCL_ERR_INVALID_ARG;
-    TRY(check_weights(e->gated ? 2 * e->I : e->I, e->H, e->experts, e->format));
+    TRY(check_weights(e->I, e->H, e->gated ? 2 * e->experts : e->experts, e->format));
     return check_weights(e->H, e->I, e->experts, e->format);
 }
 
 hccl_status_t hccl_expert_layer_scratch_bytes(const hccl_experts_fp4_t* e, int64_t tokens, int32_t top_k, size_t* bytes) {
     TRY(check_experts(e, tokens, top_k));
     if (!bytes) return HCCL_ERR_INVALID_ARG;
-    *bytes = few_fp4_scratch(tokens, e->H, e->I, top_k, e->gated != 0);
+    *bytes = few_fp4_scratch(tokens, e->H, e->I, top_k, e->gated != 0, e->format);
     return HCCL_OK;
 }
 
@@ -286,7 +286,7 @@ hccl_status_t hccl_expert_layer_fp4(const hccl_experts_fp4_t* e, const void* x, 
     if (r->tokens == 0) return HCCL_OK;
     if (!r->weights || !r->source) return HCCL_ERR_INVALID_ARG;
     if (!aligned(r->weights, 4) || !aligned(r->source, 4)) return HCCL_ERR_ALIGNMENT;
-    if (!scratch || bytes < few_fp4_scratch(r->tokens, e->H, e->I, r->top_k, e->gated != 0)) return HCCL_ERR_WORKSPACE;
+    if (!scratch || bytes < few_fp4_scratch(r->tokens, e->H, e->I, r->top_k, e->gated != 0, e->format)) return HCCL_ERR_WORKSPACE;
     if (!aligned(scratch, 128)) return HCCL_ERR_ALIGNMENT;
     FewFp4 p = {};
     p.T = r->tokens;

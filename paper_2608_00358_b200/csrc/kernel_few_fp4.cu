@@ -4,17 +4,20 @@
 // numbers by 4-bit numbers all the same: an activation goes in as a sum of eight of them. Of a block x of a row, q0 = e2m1(x / s0) is taken, of what is left q1, and so on,
 // each with a scale of its own; a step leaves at most a sixth (powers of two as scales: a quarter) of the block's maximum, so eight leave 6^-8 (4^-8). Eight columns is
 // also the least that an instruction computes: a token's eight pieces are its eight columns, and for one token they cost nothing. The sum over the pieces
-// is taken in 32 bits. With e4m3 scales each row's part of K is first multiplied by a power of two that brings its largest element to 1024 .. 2048, near 448 x 6, the top of their range; what
+// is taken in 32 bits. With e4m3 scales a row is first multiplied by a power of two that brings its largest element to 1024 .. 2048, near 448 x 6, the top of their range; what
 // four pieces leave is less than 2048 x 0.178^4 = 2.1 (a rounded scale leaves up to 17 / 96 of a block's maximum) and is multiplied by 2^10, so that the last four have the whole range
 // again and the scales' smallest step, 2^-9, is 2^-30 of the row's largest element.
 //
-// Work: units of 128 channels x `span` stages of 256 elements of K x a chunk of at most 8 of an expert's rows, in the order [chunk][part of K][channels]; every block takes an equal run of
-// them. Within a chunk and a part of K the pieces are made once and stay in shared memory while the weights stream past them. A unit's sums go to memory as 32-bit partial
-// sums, one for each part of K; the second kernel adds the first's up in their order, applies the activation and splits the result. Who finishes the last
-// unit of 128 output channels adds up all partial sums of these channels in their order: results repeat bit for bit.
+// Rows in expert order are taken in chunks of at most 8 rows of one expert. Both kernels run one block to an SM, and weights never wait for anything but room:
 //
-// Roles of a block (16 warps): warp 0 loads weights, warp 1 copies scales to tensor memory and issues the products, warp 2 owns the tensor memory, warp 3 lists the chunks, warps 4-7 take
-// the sums out, warps 8-15 make the pieces, one part of K ahead.
+//   up    units of 128 channels x `span` stages of 256 elements of K x a chunk, in the order [chunk][1024 columns of the activated rows][part of K][channels]; every block takes an equal run
+//         of them. For each chunk and part of K a block makes the pieces itself, one part ahead; a unit's sums go to memory, one 32-bit partial sum for each part of K. At its end a block counts its
+//         units; whoever counts the last one of 1024 columns adds up their parts in their order, applies the activation and makes the pieces for the second kernel.
+//   down  stages in the order [128 channels][chunk][K], every block an equal run of them. A chunk's sums over 1024 of K stay in tensor memory; weighted, they are added up in
+//         shared memory over the chunks, [token][channel]. Where the channels' run ends within a block its sums are the result; otherwise the blocks that share the channels leave
+//         partial sums, and whoever counts the last stage adds these up in the blocks' order.
+//
+// All sums have a fixed order: results repeat bit for bit.
 #include <algorithm>
 #include <atomic>
 
@@ -26,43 +29,58 @@ namespace hccl {
 namespace experts {
 namespace {
 
-constexpr int THREADS = 512, CH = 128, ROWS = 8 /* of a chunk */, PIECES = 8, SPAN = 4 /* stages of K at most */, COLS = 512;
+constexpr int CH = 128, ROWS = 8 /* of a chunk */, PIECES = 8, SPAN = 4 /* stages of K in a part at most, of the second product in every one */, WIDE = SPAN * 256, GROUP = WIDE / CH /* channel tiles of a half in 1024 columns */, COLS = 512;
 constexpr int TN = ROWS * PIECES;
 constexpr float LATER = 1024.f;  // e4m3 scales: what the last half of the pieces is larger by
 constexpr int ENOUGH = 6;  // units for each block, below which K is cut finer
-constexpr int SPLIT_WARPS = 8, SPLITTERS = 32 * SPLIT_WARPS, EACH = 8 /* elements of a thread */, TASKS = ROWS * SPAN * 256 / EACH / SPLITTERS;
+constexpr int EACH = 8;  // elements of a thread that makes pieces
+static_assert(ROWS * WIDE % EACH == 0, "");
+constexpr int UP_THREADS = 512, SPLIT_WARPS = 8, SPLITTERS = 32 * SPLIT_WARPS, TASKS = ROWS * SPAN * 256 / EACH / SPLITTERS;
+constexpr int DOWN_THREADS = 256;
+constexpr int MAX_CHUNKS = HCCL_MAX_FEW_TOKENS * HCCL_MAX_TOP_K, OWN = (MAX_CHUNKS + SMS - 1) / SMS + 2;  // chunks in all, and in one block's run of the first kernel
 
 template <int FORMAT> struct Shape {
     static constexpr int ATOMS = stage_atoms(FORMAT);
-    static constexpr int STAGE = CH * KB + ATOMS * ATOM;
     static constexpr int STAGES = 6;
-    static constexpr int PIECE_STAGE = TN * KB, PIECE_SCALES = SPAN * PIECE_STAGE;  // of a part of K: its rows by stages, then their scales
+    // up: the ring of weights, two parts' pieces (their rows by stages, then their scales), and elements between their row's maximum and their pieces
+    static constexpr int STAGE = CH * KB + ATOMS * ATOM;
+    static constexpr int PIECE_STAGE = TN * KB, PIECE_SCALES = SPAN * PIECE_STAGE;
     static constexpr int PART = PIECE_SCALES + SPAN * ATOMS * ATOM;
     static constexpr int RING = (STAGES * STAGE + 1023) / 1024 * 1024;
-    static constexpr int SMEM = RING + 2 * PART + 1024;
-    // tensor memory: two accumulators, two parts' scales, the stages' scales
+    static constexpr int HELD = ROWS * WIDE * 4;
+    static constexpr int SMEM_UP = RING + 2 * PART + HELD + 1024;
+    // its tensor memory: two accumulators, two parts' scales, the stages' scales
     static constexpr int X_SCALES = 2 * TN, W_SCALES = X_SCALES + 2 * SPAN * 4 * ATOMS;
     static_assert(W_SCALES + STAGES * 4 * ATOMS <= COLS, "tensor memory");
     static_assert(STAGE % 1024 == 0 && PART % 1024 == 0, "operands start on 1024-byte boundaries");
+    // down: a stage of weights, their scales, pieces, their scales; then [token][channel]
+    static constexpr int D_PIECES = STAGE, D_SCALES = D_PIECES + TN * KB, D_STAGE = D_SCALES + ATOMS * ATOM;
+    static constexpr int D_SUMS = STAGES * D_STAGE;
+    static constexpr int SMEM_DOWN = D_SUMS + HCCL_MAX_FEW_TOKENS * CH * 4 + 1024;
+    static_assert(2 * TN + STAGES * 8 * ATOMS <= COLS, "tensor memory");
+    static_assert(D_STAGE % 1024 == 0, "operands start on 1024-byte boundaries");
 };
 
 struct FewParams {
-    CUtensorMap w, w_scale;
-    const void* x;     // up: [T, K] in T; down: the first kernel's partial sums
-    void* y;           // up: partial sums; down: [T, H]
-    float* part;       // down: its partial sums
-    int* arrived;      // [channel tiles of down]
-    long long ldx, ldy;
-    const int *offsets, *source, *slots;
+    CUtensorMap w, w_scale, x, x_scale;  // the last two: down
+    const void* in;        // up: [T, K] in T
+    void* y;               // down: [T, N]
+    float* sums;           // up: partial sums [part of K][row][width]
+    uint8_t *pieces, *piece_scales;  // [row][8][pitch] and, in atoms, [chunk][stage]
+    float* unscale;        // [row][part of the second product's K]
+    float* part;           // down: two tiles of partial sums for each block, [token][channel]
+    int *chunk_count, *tile_count;
+    long long ldx, ldy, pitch;
+    const int *offsets, *source;
     const float *weights, *wide, *bias;
     int* status;
-    int K, N, I, k_blocks, chan_tiles, x_blocks, x_tiles /* down: of the first kernel */;
-    int experts, top_k, T, rows /* T * top_k */, act, gated, half /* width of a row of the first kernel's sums, of the gate's and of the other half */, wide_y;
-    int down_tiles, vec;
+    int K, N, I, k_blocks, down_blocks /* stages of the second product */, down_parts;
+    int chan_tiles;        // up: of a half; down: of all channels
+    int experts, top_k, T, rows /* T * top_k */, act, gated, half /* I, up to a multiple of 8 */, width /* of a row of sums: half, or both halves */, vec;
 };
 
-// How many stages of K a unit has, so that there are enough units to share out evenly. (Both kernels and the scratch's size go by it.)
-__host__ __device__ __forceinline__ int span_of(int chunks, int tiles, int k_blocks, int blocks) {
+// How many stages of K a unit has at most, so that there are enough units to share out evenly. (The scratch's size goes by it.)
+__device__ __forceinline__ int span_of(int chunks, int tiles, int k_blocks, int blocks) {
     int span = SPAN;
     while (span > 1 && (long long)chunks * tiles * ((k_blocks + span - 1) / span) < (long long)ENOUGH * blocks) span /= 2;
     return span;
@@ -125,23 +143,106 @@ template <int FORMAT> __device__ __forceinline__ Step some_step(unsigned top) {
     return r;
 }
 
+// What pieces of a row with this largest magnitude are larger by, and its inverse: powers of two that are no subnormal numbers, 2^10 <= largest * factor < 2^11.
+__device__ __forceinline__ void row_factor(unsigned top, float* factor, float* back) {
+    const int e = (int)(top >> 23) - 127, up = min(max(10 - e, -126), 126);
+    *factor = __uint_as_float((unsigned)(127 + up) << 23);
+    *back = __uint_as_float((unsigned)(127 - up) << 23);
+}
+// Eight elements of a block that lies with 2 (e4m3 scales) or 4 neighbouring lanes, to eight pieces, one after the other: put(piece, codes, scale byte). Whole warps.
+template <int FORMAT, typename Put> __device__ __forceinline__ void make_pieces(float (&v)[EACH], const Put& put) {
+    // (a loop: code that a warp passes once is fetched instruction by instruction)
+#pragma unroll 1
+    for (int q = 0; q < PIECES; q++) {
+        if (FORMAT == HCCL_NVFP4 && q == PIECES / 2)
+#pragma unroll
+            for (int j = 0; j < EACH; j++) v[j] *= LATER;
+        unsigned top = 0;
+#pragma unroll
+        for (int j = 0; j < EACH; j++) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        if (FORMAT == HCCL_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const Step s = some_step<FORMAT>(top);
+        float quo[EACH], val[EACH];
+#pragma unroll
+        for (int j = 0; j < EACH; j++) quo[j] = v[j] * s.inv;
+        const unsigned code = eight_codes(quo);
+        eight_values(__shfl_sync(0xffffffffu, code, (int)threadIdx.x % 32), val);
+#pragma unroll
+        for (int j = 0; j < EACH; j++) v[j] = fmaf(-val[j], s.d, v[j]);
+        put(q, code, s.byte);
+    }
+}
+// The eight columns of a row's pieces, as the products come out, to one sum: the smallest first.
+template <int FORMAT> __device__ __forceinline__ float sum_of_pieces(const float (&v)[8]) {
+    float s = ((v[7] + v[6]) + v[5]) + v[4];
+    if (FORMAT == HCCL_NVFP4) s *= 1.f / LATER;
+#pragma unroll
+    for (int i = 3; i >= 0; i--) s += v[i];
+    return s;
+}
+// Chunks by expert, by one warp: each(chunk, packed) for every one. Returns how many.
+struct Chunk {
+    int expert, row, rows;  // rows [row, row + rows) in expert order
+};
+static_assert(HCCL_MAX_EXPERTS <= 1 << 11 && HCCL_MAX_FEW_TOKENS * HCCL_MAX_TOP_K <= 1 << 12 && ROWS < 1 << 4, "packed");
+__device__ __forceinline__ int packed(int expert, int row, int rows) { return expert << 16 | row << 4 | rows; }
+__device__ __forceinline__ Chunk unpacked(int c) {
+    c = __shfl_sync(0xffffffffu, c, 0);  // (the same in all lanes, and by way of the shuffle known to be)
+    return {c >> 16, c >> 4 & 0xfff, c & 15};
+}
+template <typename Each> __device__ __forceinline__ int list_chunks(const FewParams& p, int lane, const Each& each) {
+    int run = 0;
+    for (int b = 0; b < p.experts; b += 32) {
+        const int g = b + lane;
+        int lo = 0, hi = 0;
+        if (g < p.experts) lo = max(0, p.offsets[g]), hi = min(p.rows, p.offsets[g + 1]);
+        const int n = max(0, (hi - lo + ROWS - 1) / ROWS);
+        int inc = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += v;
+        }
+        for (int i = 0; i < n; i++) each(run + inc - n + i, packed(g, lo + i * ROWS, min(ROWS, hi - lo - i * ROWS)));
+        run += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    return run;
+}
+__device__ __forceinline__ uint32_t instruction(int rows, int format) {  // e2m1 operands, 128 channels, rows * 8 columns
+    return (1u << 7) | (1u << 10) | ((uint32_t)rows << 17) | (format == HCCL_MXFP4 ? 1u << 23 : 0u) | (1u << 27);
+}
+// After a wait that gave up, loads may still be in flight: wait (with a limit) for the stages that were issued.
+template <typename Full> __device__ __forceinline__ void drain(const Full& full, int stages, int it, int* status) {
+    const unsigned long long t0 = now_ns();
+    for (int i = max(0, it - stages); i < it; i++)
+        while (!mbar_try(full(i % stages), (i / stages) & 1) && now_ns() - t0 < WAIT_NS) {}
+    __nanosleep(1000000);  // and the instructions issued last, which end by themselves
+    if (status) *status = HCCL_ERR_TIMEOUT;
+}
+
+// ---------------------------------------------------------------- first product, activation, pieces
+// Where a block is in its run of units. index: among the `of` units with the same chunk, part and kc.
 struct Unit {
-    int expert, row, rows;  // a chunk: rows [row, row + rows) in expert order
-    int kc, tile;
+    Chunk c;
+    int u, chunk, part /* of the second product's K */, kc, half /* gate or other */, tile /* of the half */, index, of, group;
 };
 
-template <typename T, int FORMAT, bool DOWN> __global__ void __launch_bounds__(THREADS, 1) hccl_few_fp4(const __grid_constant__ FewParams p) {
+// Roles (16 warps): warp 0 loads weights, warp 1 copies scales to tensor memory and issues the products, warp 2 owns the tensor memory, warp 3 lists the chunks, warps 4-7 take
+// the sums out, warps 8-15 make the pieces.
+template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 1) hccl_few_up(const __grid_constant__ FewParams p) {
     using S = Shape<FORMAT>;
     extern __shared__ char dynamic[];
     __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 8];
     __shared__ uint32_t tmem_at;
-    __shared__ int gave_up, last_one;
-    __shared__ int before[HCCL_MAX_EXPERTS + 1];
+    __shared__ int gave_up, completed;
+    __shared__ int chunk_total, table[OWN];
     __shared__ float unscale[2][ROWS];
     __shared__ unsigned top_of[2][ROWS];
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t base = (smem_addr(dynamic) + 1023) & ~1023u;
     char* const parts = dynamic + (base - smem_addr(dynamic)) + S::RING;
+    float4* const held = (float4*)(parts + 2 * S::PART);
     const uint32_t bar0 = smem_addr(bars);
     const auto full = [&](int s) { return bar0 + 8 * s; };
     const auto empty = [&](int s) { return bar0 + 8 * (S::STAGES + s); };
@@ -150,77 +251,93 @@ template <typename T, int FORMAT, bool DOWN> __global__ void __launch_bounds__(T
     const auto part_full = [&](int b) { return bar0 + 8 * (2 * S::STAGES + 4 + b); };
     const auto part_empty = [&](int b) { return bar0 + 8 * (2 * S::STAGES + 6 + b); };
 
-    if (!DOWN) asm volatile("griddepcontrol.launch_dependents;");  // its blocks may start to fetch weights as this one's leave
+    asm volatile("griddepcontrol.launch_dependents;");  // the second kernel's blocks may start to fetch weights as this one's leave
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
         for (int b = 0; b < 2; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 4), mbar_init(part_full(b), SPLIT_WARPS), mbar_init(part_empty(b), 5);
         gave_up = 0;
+        completed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (!DOWN)  // for the second kernel
-        for (int i = (int)(blockIdx.x * THREADS + threadIdx.x); i < p.down_tiles; i += (int)gridDim.x * THREADS) p.arrived[i] = 0;
     if (threadIdx.x < 2 * ROWS) top_of[threadIdx.x / ROWS][threadIdx.x % ROWS] = 0;
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(COLS));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
+    const int blocks = (int)gridDim.x;
     if (warp == 3) {
-        int run = 0;
-        for (int b = 0; b < p.experts; b += 32) {
-            const int g = b + lane;
-            int n = 0;
-            if (g < p.experts) n = max(0, (min(p.rows, p.offsets[g + 1]) - max(0, p.offsets[g]) + ROWS - 1) / ROWS);
-            int inc = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, inc, o);
-                if (lane >= o) inc += v;
-            }
-            if (g < p.experts) before[g] = run + inc - n;
-            run += __shfl_sync(0xffffffffu, inc, 31);
-        }
-        if (lane == 0) before[p.experts] = run;
+        // Chunks of a block's run: every chunk has the same number of units, so the run begins in chunk floor(chunks * block / blocks).
+        const int n = min(p.rows, list_chunks(p, lane, [](int, int) {}));  // (never more than rows, if the offsets ascend)
+        const int own = (int)((long long)n * blockIdx.x / blocks);
+        list_chunks(p, lane, [&](int chunk, int c) {
+            if (chunk >= own && chunk < own + OWN) table[chunk - own] = c;
+        });
+        if (lane == 0) chunk_total = n;
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
-    const int chunks = __shfl_sync(0xffffffffu, before[p.experts], 0), blocks = (int)gridDim.x;
-    const int span = span_of(chunks, p.chan_tiles, p.k_blocks, blocks), parts_of_k = (p.k_blocks + span - 1) / span;
-    const long long units = (long long)chunks * parts_of_k * p.chan_tiles;
+    const int chunks = __shfl_sync(0xffffffffu, chunk_total, 0), own = (int)((long long)chunks * blockIdx.x / blocks);
+    const int halves = p.gated ? 2 : 1, span = span_of(chunks, halves * p.chan_tiles, p.k_blocks, blocks), parts_of_k = (p.k_blocks + span - 1) / span;
+    const int of_chunk = parts_of_k * halves * p.chan_tiles, of_part = parts_of_k * halves * GROUP;  // units; a chunk's last part may have fewer
+    const long long units = (long long)chunks * of_chunk;
     const int u0 = (int)(units * blockIdx.x / blocks), u1 = (int)(units * (blockIdx.x + 1) / blocks);
     const int filled = min(p.rows, max(0, p.offsets[p.experts]));  // rows that have sums: how far apart the parts of K lie
 
-    int hint = 0;
-    const auto unit_of = [&](int u) {
-        Unit r;
-        const int chunk = u / (parts_of_k * p.chan_tiles), rest = u - chunk * parts_of_k * p.chan_tiles;
-        while (chunk >= before[hint + 1]) hint++;
-        const int lo = max(0, p.offsets[hint]), hi = min(p.rows, p.offsets[hint + 1]), row = lo + (chunk - before[hint]) * ROWS;
-        r.expert = __shfl_sync(0xffffffffu, hint, 0);
-        r.row = __shfl_sync(0xffffffffu, row, 0);
-        r.rows = __shfl_sync(0xffffffffu, min(ROWS, hi - row), 0);
-        r.kc = __shfl_sync(0xffffffffu, rest / p.chan_tiles, 0);
-        r.tile = __shfl_sync(0xffffffffu, rest % p.chan_tiles, 0);
-        return r;
+    const auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
+    const auto place = [&](Unit& t) { t.half = t.index >= t.group, t.tile = t.part * GROUP + t.index - t.half * t.group; };
+    const auto in_part = [&](Unit& t) { t.group = min(GROUP, p.chan_tiles - t.part * GROUP), t.of = halves * t.group; };
+    const auto unit_at = [&](int u) {
+        Unit t = {};
+        t.u = u;
+        if (u >= u1) return t;
+        t.chunk = uniform(u / of_chunk);
+        t.c = unpacked(table[t.chunk - own]);
+        int rest = u - t.chunk * of_chunk;
+        t.part = uniform(rest / of_part);
+        in_part(t);
+        rest -= t.part * of_part;
+        t.kc = uniform(rest / t.of);
+        t.index = uniform(rest - t.kc * t.of);
+        place(t);
+        return t;
     };
-    const auto stages_of = [&](int kc) { return min(span, p.k_blocks - kc * span); };
-    const auto ends = [&](int u) { return u == u1 - 1 || (u + 1) % p.chan_tiles == 0; };  // the last unit of its part of K here
+    const auto advance = [&](Unit& t) {
+        t.u++;
+        if (++t.index == t.of) {
+            t.index = 0;
+            if (++t.kc == parts_of_k) {
+                t.kc = 0;
+                if (++t.part == p.down_parts) {
+                    t.part = 0;
+                    t.chunk++;
+                    if (t.u < u1) t.c = unpacked(table[t.chunk - own]);
+                }
+                in_part(t);
+            }
+        }
+        place(t);
+    };
+    // With one part of K a chunk's pieces serve all its units.
+    const auto begins = [&](const Unit& t) { return t.u == u0 || (t.index == 0 && (parts_of_k > 1 || t.part == 0)); };
+    const auto ends = [&](const Unit& t) { return t.u == u1 - 1 || (t.index == t.of - 1 && (parts_of_k > 1 || t.part == p.down_parts - 1)); };
+    const auto stage_of = [&](int kc) { return p.k_blocks * kc / parts_of_k; };  // the first of a part of K; parts differ by one stage at most
+    const auto stages_of = [&](int kc) { return stage_of(kc + 1) - stage_of(kc); };
     int it = 0, acc = 0, turn = 0;  // stages, units and parts of K passed
 
     if (warp == 0) {
-        for (int u = u0; u < u1; u++) {
-            const Unit t = unit_of(u);
-            const int n = stages_of(t.kc);
+        for (Unit t = unit_at(u0); t.u < u1; advance(t)) {
+            const int n = stages_of(t.kc), first = stage_of(t.kc);
             for (int i = 0; i < n; i++, it++) {
-                const int s = it % S::STAGES, kb = t.kc * span + i;
+                const int s = it % S::STAGES, kb = first + i;
                 if (!mbar_wait(empty(s), ((it / S::STAGES) & 1) ^ 1, &gave_up)) break;
                 if (elected()) {
                     const uint32_t at = base + s * S::STAGE;
                     mbar_expect(full(s), S::STAGE);
-                    tma_load<1>(at, &p.w, kb * KB, t.expert * p.N + t.tile * CH, full(s));
-                    tma_load<1>(at + CH * KB, &p.w_scale, 0, ((t.expert * p.chan_tiles + t.tile) * p.k_blocks + kb) * S::ATOMS, full(s));
+                    tma_load<1>(at, &p.w, kb * KB, t.c.expert * p.N + t.half * p.I + t.tile * CH, full(s));
+                    tma_load<1>(at + CH * KB, &p.w_scale, 0, (((t.c.expert * halves + t.half) * p.chan_tiles + t.tile) * p.k_blocks + kb) * S::ATOMS, full(s));
                 }
                 __syncwarp();
             }
@@ -229,12 +346,11 @@ template <typename T, int FORMAT, bool DOWN> __global__ void __launch_bounds__(T
     } else if (warp == 1) {
         const int steps = (p.K + 63) / 64;
         bool ok = true;
-        for (int u = u0; u < u1 && ok; u++, acc++) {
-            const Unit t = unit_of(u);
-            const int n = stages_of(t.kc), b = acc & 1, half = turn & 1;
+        for (Unit t = unit_at(u0); t.u < u1 && ok; advance(t), acc++) {
+            const int n = stages_of(t.kc), first = stage_of(t.kc), b = acc & 1, half = turn & 1;
             const uint32_t x_scales = tmem + S::X_SCALES + half * SPAN * 4 * S::ATOMS, pieces = base + S::RING + half * S::PART;
-            const uint32_t desc = (1u << 7) | (1u << 10) | ((uint32_t)t.rows << 17) | (FORMAT == HCCL_MXFP4 ? 1u << 23 : 0u) | (1u << 27);  // 128 channels, rows * 8 columns
-            if (u == u0 || t.tile == 0) {
+            const uint32_t desc = instruction(t.c.rows, FORMAT);
+            if (begins(t)) {
                 ok = mbar_wait(part_full(half), (turn >> 1) & 1, &gave_up);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -246,7 +362,7 @@ template <typename T, int FORMAT, bool DOWN> __global__ void __launch_bounds__(T
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (int i = 0; i < n; i++, it++) {
-                const int s = it % S::STAGES, left = min(4, steps - 4 * (t.kc * span + i));
+                const int s = it % S::STAGES, left = min(4, steps - 4 * (first + i));
                 ok = mbar_wait(full(s), (it / S::STAGES) & 1, &gave_up);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -265,199 +381,99 @@ template <typename T, int FORMAT, bool DOWN> __global__ void __launch_bounds__(T
                     mma_commit<1>(empty(s));
                     if (i == n - 1) {
                         mma_commit<1>(acc_full(b));
-                        if (ends(u)) mma_commit<1>(part_empty(half));
+                        if (ends(t)) mma_commit<1>(part_empty(half));
                     }
                 }
                 __syncwarp();
             }
-            if (ends(u)) turn++;
+            if (ends(t)) turn++;
         }
     } else if (warp >= 4 && warp < 8) {
         const int quarter = warp & 3;
-        if (DOWN) asm volatile("griddepcontrol.wait;" ::: "memory");
         bool ok = true;
-        // Adds up what the experts of each token have for 128 channels.
-        const auto combine = [&](int tile) {
-            const int chan = tile * CH + quarter * 32 + lane;
-            const bool in = chan < p.N;
-            constexpr int BATCH = 16;
-            float sum = 0.f;
-            for (int q0 = 0; q0 < p.rows; q0 += BATCH) {
-                const int mine = q0 + lane < p.rows && lane < BATCH ? p.slots[q0 + lane] : -1;
-                const float weight = q0 + lane < p.rows && lane < BATCH ? p.weights[q0 + lane] : 0.f;
-                float z[BATCH];
-#pragma unroll
-                for (int i = 0; i < BATCH; i++) z[i] = 0.f;
-                for (int kc = 0; kc < parts_of_k; kc++) {
-#pragma unroll
-                    for (int i = 0; i < BATCH; i++) {
-                        const int slot = __shfl_sync(0xffffffffu, mine, i);
-                        if (in && slot >= 0 && slot < filled) z[i] += __ldcg(p.part + ((long long)kc * filled + slot) * p.wide_y + chan);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < BATCH; i++) {
-                    const int q = q0 + i, slot = __shfl_sync(0xffffffffu, mine, i);
-                    const float f = __shfl_sync(0xffffffffu, weight, i);
-                    if (q < p.rows) {
-                        if (slot >= 0 && slot < filled) sum = fmaf(f, z[i], sum);
-                        if ((q + 1) % p.top_k == 0) {
-                            if (in) ((T*)p.y)[(long long)(q / p.top_k) * p.ldy + chan] = from_f32<T>(sum);
-                            sum = 0.f;
-                        }
-                    }
-                }
-            }
-        };
-        if (DOWN && units == 0)
-            for (int tile = blockIdx.x; tile < p.chan_tiles; tile += blocks) combine(tile);  // nobody has anything: zeros
-        for (int u = u0; u < u1 && ok; u++, acc++) {
-            const Unit t = unit_of(u);
+        for (Unit t = unit_at(u0); t.u < u1 && ok; advance(t), acc++) {
             const int b = acc & 1, half = turn & 1, chan = t.tile * CH + quarter * 32 + lane;
-            const bool in = chan < p.N;
-            const float wide = p.wide[t.expert], bias = (in && p.bias && t.kc == 0) ? p.bias[(long long)t.expert * p.N + chan] : 0.f;
+            const bool in = chan < p.I;
+            const float wide = p.wide[t.c.expert], bias = (in && p.bias && t.kc == 0) ? p.bias[(long long)t.c.expert * p.N + t.half * p.I + chan] : 0.f;
             ok = mbar_wait(part_full(half), (turn >> 1) & 1, &gave_up) && mbar_wait(acc_full(b), (acc >> 1) & 1, &gave_up);
-            if (DOWN) ok = all_of(ok, 1, 128);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             float sums[ROWS];
 #pragma unroll
             for (int r = 0; r < ROWS; r++) {
-                if (r >= t.rows) break;
+                if (r >= t.c.rows) break;
                 float v[8];
                 __syncwarp();
                 tmem_load8(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + r * PIECES, v);
                 tmem_arrived();
-                float s = ((v[7] + v[6]) + v[5]) + v[4];  // the smallest first
-                if (FORMAT == HCCL_NVFP4) s *= 1.f / LATER;
-#pragma unroll
-                for (int i = 3; i >= 0; i--) s += v[i];
-                sums[r] = fmaf(s, unscale[half][r] * wide, bias);
+                sums[r] = fmaf(sum_of_pieces<FORMAT>(v), unscale[half][r] * wide, bias);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(acc_empty(b));
-                if (ends(u)) mbar_arrive(part_empty(half));
+                if (ends(t)) mbar_arrive(part_empty(half));
             }
-            if (ends(u)) turn++;
-            float* out = DOWN ? p.part : (float*)p.y;
-            const int width = DOWN ? p.wide_y : (p.gated ? 2 : 1) * p.half, at = !DOWN && p.gated && chan >= p.I ? p.half + chan - p.I : chan;
-            out += ((long long)t.kc * filled + t.row) * width + at;
+            if (ends(t)) turn++;
+            float* out = p.sums + ((long long)t.kc * filled + t.c.row) * p.width + t.half * p.half + chan;
             if (in)
 #pragma unroll
                 for (int r = 0; r < ROWS; r++)
-                    if (r < t.rows) __stcg(out + (long long)r * width, sums[r]);
-            if (DOWN) {
-                // All four warps' sums are out before the unit is counted; who counts the last one sees the others'.
-                __threadfence();
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-                if (threadIdx.x == 128) {
-                    const int n = chunks * parts_of_k;
-                    last_one = atomicAdd(p.arrived + t.tile, 1) == n - 1;
-                    __threadfence();
-                }
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-                if (last_one) combine(t.tile);
-            }
+                    if (r < t.c.rows) __stcg(out + (long long)r * p.width, sums[r]);
         }
+        __threadfence();  // the sums are out before this block counts its units
     } else if (warp >= 8) {
         const int me = (int)threadIdx.x - 256;
-        if (DOWN) asm volatile("griddepcontrol.wait;" ::: "memory");
-        const int x_span = DOWN ? span_of(chunks, p.x_tiles, p.x_blocks, blocks) : 0, x_parts = DOWN ? (p.x_blocks + x_span - 1) / x_span : 0;
         bool ok = true;
-        for (int u = u0; u < u1 && ok; u = (u / p.chan_tiles + 1) * p.chan_tiles, turn++) {
-            const Unit t = unit_of(u);
-            const int half = turn & 1, k0 = t.kc * span * 256, wide = stages_of(t.kc) * 256 / EACH;  // threads to a row
+        for (int u = u0, next; u < u1 && ok; u = next, turn++) {
+            const Unit t = unit_at(u);
+            next = parts_of_k > 1 ? u + t.of - t.index : (t.chunk + 1) * of_chunk;
+            const int half = turn & 1, k0 = stage_of(t.kc) * 256, wide = stages_of(t.kc) * 256 / EACH;  // threads to a row
             char* const part = parts + half * S::PART;
-            // A thread's elements: those of task i of (row, eight elements), i = me, me + 256, ...
-            float v[TASKS][EACH];
+            // A thread's elements, eight at a time, are those of task i of (row, eight elements), i = me, me + 256, ...
             const auto row_of = [&](int i) { return (me + i * SPLITTERS) / wide; };
             const auto k_of = [&](int i) { return k0 + (me + i * SPLITTERS) % wide * EACH; };
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < TASKS; i++) {
                 const int r = row_of(i), k = k_of(i);
-                if (r >= t.rows) break;
-                if constexpr (!DOWN) {
-                    const int from = p.source[t.row + r];
-                    load8<T>((const T*)p.x + (long long)(from / p.top_k) * p.ldx, k, (unsigned)from < (unsigned)p.rows ? p.K : 0, p.vec, v[i]);
-                } else {
-                    const int width = (p.gated ? 2 : 1) * p.half;
-                    const float* from = (const float*)p.x + (long long)(t.row + r) * width;
-                    float g[EACH] = {}, o[EACH] = {};
-                    if (k < p.K)
-                        for (int c = 0; c < x_parts; c++, from += (long long)filled * width) {
+                if (r >= t.c.rows) break;
+                float v[EACH];
+                const int from = p.source[t.c.row + r];
+                load8<T>((const T*)p.in + (long long)(from / p.top_k) * p.ldx, k, (unsigned)from < (unsigned)p.rows ? p.K : 0, p.vec, v);
+                if (FORMAT == HCCL_NVFP4) {  // the largest magnitude of each row's part of K
+                    unsigned top = 0;
 #pragma unroll
-                            for (int j = 0; j < EACH; j += 4) {
-                                const float4 a = __ldcg((const float4*)(from + k + j));
-                                g[j] += a.x, g[j + 1] += a.y, g[j + 2] += a.z, g[j + 3] += a.w;
-                                if (p.gated) {
-                                    const float4 q = __ldcg((const float4*)(from + p.half + k + j));
-                                    o[j] += q.x, o[j + 1] += q.y, o[j + 2] += q.z, o[j + 3] += q.w;
-                                }
-                            }
-                        }
-#pragma unroll
-                    for (int j = 0; j < EACH; j++) v[i][j] = k + j < p.K ? (p.gated ? activation(p.act, g[j]) * o[j] : activation(p.act, g[j])) : 0.f;
+                    for (int j = 0; j < EACH; j++) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+                    top = __reduce_max_sync(0xffffffffu, top);
+                    if (lane == 0) atomicMax(&top_of[half][r], top);
                 }
+                held[2 * i * SPLITTERS + me] = make_float4(v[0], v[1], v[2], v[3]);
+                held[(2 * i + 1) * SPLITTERS + me] = make_float4(v[4], v[5], v[6], v[7]);
             }
             // (the buffers' last readers)
             ok = mbar_wait(part_empty(half), ((turn >> 1) & 1) ^ 1, &gave_up);
             if (FORMAT == HCCL_NVFP4) ok = all_of(ok, 2, SPLITTERS);
             if (!ok) break;
-            // The largest magnitude of each row's part of K.
-            if (FORMAT == HCCL_NVFP4) {
-#pragma unroll
-                for (int i = 0; i < TASKS; i++) {
-                    const int r = row_of(i);
-                    if (r >= t.rows) break;
-                    unsigned top = 0;
-#pragma unroll
-                    for (int j = 0; j < EACH; j++) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
-                    top = __reduce_max_sync(0xffffffffu, top);
-                    if (top) atomicMax(&top_of[half][r], top);
-                }
-                asm volatile("bar.sync 2, 256;" ::: "memory");
-            }
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < TASKS; i++) {
                 const int r = row_of(i), k = k_of(i);
-                if (r >= t.rows) break;
+                if (r >= t.c.rows) break;
                 float factor = 1.f, back = 1.f;
-                if (FORMAT == HCCL_NVFP4) {
-                    // 2^10 <= largest * factor < 2^11; both factors stay powers of two that are no subnormal numbers
-                    const unsigned top = top_of[half][r];
-                    const int e = (int)(top >> 23) - 127, up = min(max(10 - e, -126), 126);
-                    factor = __uint_as_float((unsigned)(127 + up) << 23), back = __uint_as_float((unsigned)(127 - up) << 23);
-                }
+                if (FORMAT == HCCL_NVFP4) row_factor(top_of[half][r], &factor, &back);
                 if (k == k0) unscale[half][r] = back;
+                const float4 a = held[2 * i * SPLITTERS + me], b = held[(2 * i + 1) * SPLITTERS + me];
+                float v[EACH] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-                for (int j = 0; j < EACH; j++) v[i][j] *= factor;
+                for (int j = 0; j < EACH; j++) v[j] *= factor;
                 const int kk = k - k0, stage = kk / 256, in_stage = kk % 256;
-#pragma unroll
-                for (int q = 0; q < PIECES; q++) {
-                    if (FORMAT == HCCL_NVFP4 && q == PIECES / 2)
-#pragma unroll
-                        for (int j = 0; j < EACH; j++) v[i][j] *= LATER;
-                    unsigned top = 0;
-#pragma unroll
-                    for (int j = 0; j < EACH; j++) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
-                    // a block's elements lie with two neighbouring lanes, or four
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    if (FORMAT == HCCL_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const Step s = some_step<FORMAT>(top);
-                    float quo[EACH], val[EACH];
-#pragma unroll
-                    for (int j = 0; j < EACH; j++) quo[j] = v[i][j] * s.inv;
-                    const unsigned code = eight_codes(quo);
-                    eight_values(__shfl_sync(0xffffffffu, code, lane), val);
-#pragma unroll
-                    for (int j = 0; j < EACH; j++) v[i][j] = fmaf(-val[j], s.d, v[i][j]);
-                    const int n = r * PIECES + q, sixteen = in_stage / 32;
-                    *(unsigned*)(part + stage * S::PIECE_STAGE + n * KB + ((sixteen ^ (n & 7)) * 16) + in_stage % 32 / 2) = code;
-                    constexpr int B = block_of(FORMAT);
-                    if (kk % B == 0) part[S::PIECE_SCALES + kk / (4 * B) * ATOM + atom_row(n) + kk / B % 4] = (char)s.byte;
-                }
+                char* const codes = part + stage * S::PIECE_STAGE + in_stage % 32 / 2;
+                constexpr int B = block_of(FORMAT);
+                char* const scales = part + S::PIECE_SCALES + kk / (4 * B) * ATOM + kk / B % 4;
+                make_pieces<FORMAT>(v, [&](int q, unsigned code, unsigned byte) {
+                    const int n = r * PIECES + q;  // n % 8 = q
+                    *(unsigned*)(codes + n * KB + ((in_stage / 32 ^ q) * 16)) = code;
+                    if (kk % B == 0) scales[atom_row(n)] = (char)byte;
+                });
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -469,75 +485,419 @@ template <typename T, int FORMAT, bool DOWN> __global__ void __launch_bounds__(T
             }
         }
     }
-    // After a wait that gave up, loads may still be in flight: wait (with a limit) for the stages that were issued.
-    if (warp == 0 && lane == 0 && *(volatile int*)&gave_up) {
-        const unsigned long long t0 = now_ns();
-        for (int i = max(0, it - S::STAGES); i < it; i++)
-            while (!mbar_try(full(i % S::STAGES), (i / S::STAGES) & 1) && now_ns() - t0 < WAIT_NS) {}
-        __nanosleep(1000000);  // and the instructions issued last, which end by themselves
-        if (p.status) *p.status = HCCL_ERR_TIMEOUT;
-    }
+    if (warp == 0 && lane == 0 && *(volatile int*)&gave_up) drain(full, S::STAGES, it, p.status);
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(COLS));
+    if (*(volatile int*)&gave_up || u0 >= u1) return;
+
+    // The block counts its units, all at once; parts of chunks that are complete with them are its own to finish.
+    int* const list = (int*)parts;  // (its last readers are done)
+    const auto part_at = [&](int u) { return u / of_chunk * p.down_parts + u % of_chunk / of_part; };
+    for (int i = part_at(u0) + (int)threadIdx.x; i <= part_at(u1 - 1); i += UP_THREADS) {
+        const int lo = i / p.down_parts * of_chunk + i % p.down_parts * of_part, hi = min(lo + of_part, (i / p.down_parts + 1) * of_chunk);
+        const int n = min(u1, hi) - max(u0, lo);
+        if (atomicAdd(p.chunk_count + i, n) + n == hi - lo) list[atomicAdd(&completed, 1)] = i;
+    }
+    __threadfence();
+    __syncthreads();
+    for (int l = 0; l < completed; l++) {
+        const int chunk = list[l] / p.down_parts, part = list[l] % p.down_parts, first = part * WIDE;
+        const Chunk c = unpacked(table[chunk - own]);
+        const int per_row = (min(WIDE, p.I - first) + 63) / 64 * 8;  // eights of a row, up to the end of the last instruction's 64 elements
+        const int tasks = c.rows * per_row;
+        if (threadIdx.x < ROWS) top_of[0][threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int i = (int)threadIdx.x; i < tasks; i += UP_THREADS) {
+            const int r = i / per_row, k = first + i % per_row * EACH;
+            float v[EACH] = {}, o[EACH] = {};
+            if (k < p.half) {
+                const float* from = p.sums + (long long)(c.row + r) * p.width + k;
+                const long long apart = (long long)filled * p.width;
+#pragma unroll 4
+                for (int kc = 0; kc < parts_of_k; kc++) {
+                    const float4* a = (const float4*)(from + kc * apart);
+                    const float4 a0 = __ldcg(a), a1 = __ldcg(a + 1);
+                    v[0] += a0.x, v[1] += a0.y, v[2] += a0.z, v[3] += a0.w, v[4] += a1.x, v[5] += a1.y, v[6] += a1.z, v[7] += a1.w;
+                    if (p.gated) {
+                        const float4 b0 = __ldcg(a + p.half / 4), b1 = __ldcg(a + p.half / 4 + 1);
+                        o[0] += b0.x, o[1] += b0.y, o[2] += b0.z, o[3] += b0.w, o[4] += b1.x, o[5] += b1.y, o[6] += b1.z, o[7] += b1.w;
+                    }
+                }
+            }
+            if (p.act == HCCL_ACT_SILU)
+#pragma unroll
+                for (int j = 0; j < EACH; j++) v[j] = activation(HCCL_ACT_SILU, v[j]);
+            else if (p.act == HCCL_ACT_GELU)
+#pragma unroll
+                for (int j = 0; j < EACH; j++) v[j] = activation(HCCL_ACT_GELU, v[j]);
+            else
+#pragma unroll
+                for (int j = 0; j < EACH; j++) v[j] = activation(HCCL_ACT_RELU, v[j]);
+            unsigned top = 0;
+#pragma unroll
+            for (int j = 0; j < EACH; j++) {
+                v[j] = k + j < p.I ? (p.gated ? v[j] * o[j] : v[j]) : 0.f;
+                top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+            }
+            if (FORMAT == HCCL_NVFP4 && top) atomicMax(&top_of[0][r], top);
+            held[i] = make_float4(v[0], v[1], v[2], v[3]), held[ROWS * WIDE / EACH + i] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int i0 = 0; i0 < tasks; i0 += UP_THREADS) {
+            // (lanes beyond the last task go along, for the shuffles)
+            const int i = i0 + (int)threadIdx.x, r = i / per_row, k = first + i % per_row * EACH;
+            const bool in = i < tasks;
+            float v[EACH] = {}, factor = 1.f, back = 1.f;
+            if (in) {
+                const float4 a = held[i], b = held[ROWS * WIDE / EACH + i];
+                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+                if (FORMAT == HCCL_NVFP4) row_factor(top_of[0][r], &factor, &back);
+                if (k == first) p.unscale[(long long)(c.row + r) * p.down_parts + part] = back;
+            }
+#pragma unroll
+            for (int j = 0; j < EACH; j++) v[j] *= factor;
+            constexpr int B = block_of(FORMAT);
+            uint8_t* const codes = p.pieces + (long long)(c.row + r) * PIECES * p.pitch + k / 2;
+            uint8_t* const scales = p.piece_scales + ((long long)chunk * p.down_blocks * S::ATOMS + k / (4 * B)) * ATOM + k / B % 4;
+            make_pieces<FORMAT>(v, [&](int q, unsigned code, unsigned byte) {
+                if (in) {
+                    *(unsigned*)(codes + q * p.pitch) = code;
+                    if (k % B == 0) scales[atom_row(r * PIECES + q)] = (uint8_t)byte;
+                }
+            });
+        }
+        __syncthreads();
+    }
 }
 
-template <typename T, int FORMAT, bool DOWN> cudaError_t launch(const FewParams& p, cudaStream_t s) {
+// ---------------------------------------------------------------- second product, weighted sums
+// Where a block is in its run of stages: a segment has one chunk and one part of K. g1: where it ends.
+struct Segment {
+    Chunk c;
+    int g, g1, chunk, tile, k0, k1;  // stages of K
+};
+
+// Roles (8 warps): warp 0 loads weights and pieces, warp 1 copies scales to tensor memory and issues the products, warp 2 owns the tensor memory, warp 3 lists the chunks, warps 4-7 take
+// the sums out.
+template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS, 1) hccl_few_down(const __grid_constant__ FewParams p) {
     using S = Shape<FORMAT>;
-    static std::atomic<bool> ready[64];  // by device; setting it twice does no harm
+    extern __shared__ char dynamic[];
+    __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 4];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up, completed, list[2];
+    __shared__ int chunk_total, table[MAX_CHUNKS];
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    const uint32_t base = (smem_addr(dynamic) + 1023) & ~1023u;
+    float* const sums = (float*)(dynamic + (base - smem_addr(dynamic)) + S::D_SUMS);
+    const uint32_t bar0 = smem_addr(bars);
+    const auto full = [&](int s) { return bar0 + 8 * s; };
+    const auto empty = [&](int s) { return bar0 + 8 * (S::STAGES + s); };
+    const auto acc_full = [&](int b) { return bar0 + 8 * (2 * S::STAGES + b); };
+    const auto acc_empty = [&](int b) { return bar0 + 8 * (2 * S::STAGES + 2 + b); };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::STAGES; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
+        for (int b = 0; b < 2; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 4);
+        gave_up = 0;
+        completed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(COLS));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (warp == 3) {
+        const int n = list_chunks(p, lane, [&](int chunk, int c) {
+            if (chunk < p.rows) table[chunk] = c;
+        });
+        if (lane == 0) chunk_total = min(p.rows, n);  // (never more than rows, if the offsets ascend)
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
+    const int chunks = __shfl_sync(0xffffffffu, chunk_total, 0), blocks = (int)gridDim.x;
+    const int of_tile = chunks * p.k_blocks;
+    const long long total = (long long)of_tile * p.chan_tiles;
+    const auto first_of = [&](int block) { return (int)(total * block / blocks); };
+    const int g0 = first_of((int)blockIdx.x), g1 = first_of((int)blockIdx.x + 1);
+
+    const auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
+    const auto bound = [&](Segment& t) {
+        t.k1 = min(min(p.k_blocks, (t.k0 / SPAN + 1) * SPAN), t.k0 + g1 - t.g);
+        t.g1 = t.g + t.k1 - t.k0;
+    };
+    const auto first_segment = [&] {
+        Segment t = {};
+        t.g = g0;
+        if (g0 >= g1) return t;
+        t.tile = uniform(g0 / of_tile);
+        const int rest = g0 - t.tile * of_tile;
+        t.chunk = uniform(rest / p.k_blocks);
+        t.k0 = rest - t.chunk * p.k_blocks;
+        t.c = unpacked(table[t.chunk]);
+        bound(t);
+        return t;
+    };
+    const auto advance = [&](Segment& t) {
+        t.g = t.g1;
+        t.k0 = t.k1;
+        if (t.k0 == p.k_blocks) {
+            t.k0 = 0;
+            if (++t.chunk == chunks) t.chunk = 0, t.tile++;
+            t.c = unpacked(table[t.chunk]);
+        }
+        bound(t);
+    };
+    int it = 0, acc = 0;  // stages and segments passed
+
+    if (warp == 0) {
+        const auto expect = [&](const Segment& t, int s) { mbar_expect(full(s), (uint32_t)(S::STAGE + t.c.rows * PIECES * KB + S::ATOMS * ATOM)); };
+        const auto load_w = [&](const Segment& t, int s, int kb) {
+            const uint32_t at = base + s * S::D_STAGE;
+            tma_load<1>(at, &p.w, kb * KB, t.c.expert * p.N + t.tile * CH, full(s));
+            tma_load<1>(at + CH * KB, &p.w_scale, 0, ((t.c.expert * p.chan_tiles + t.tile) * p.k_blocks + kb) * S::ATOMS, full(s));
+        };
+        const auto load_x = [&](const Segment& t, int s, int kb) {
+            const uint32_t at = base + s * S::D_STAGE;
+            for (int r = 0; r < t.c.rows; r++) tma_load<1>(at + S::D_PIECES + r * PIECES * KB, &p.x, kb * KB, (t.c.row + r) * PIECES, full(s));
+            tma_load<1>(at + S::D_SCALES, &p.x_scale, 0, (t.chunk * p.k_blocks + kb) * S::ATOMS, full(s));
+        };
+        // The first stages' weights do not hang on the first kernel's results.
+        const auto first = [&](const auto& each) {
+            int n = 0;
+            for (Segment t = first_segment(); t.g < g1 && n < S::STAGES; advance(t)) {
+                for (int kb = t.k0; kb < t.k1 && n < S::STAGES; kb++, n++)
+                    if (elected()) each(t, n, kb);
+                __syncwarp();
+            }
+            return n;
+        };
+        const int pre = first([&](const Segment& t, int s, int kb) {
+            expect(t, s);
+            load_w(t, s, kb);
+        });
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        first(load_x);
+        for (Segment t = first_segment(); t.g < g1; advance(t)) {
+            for (int kb = t.k0; kb < t.k1; kb++, it++) {
+                if (it < pre) continue;
+                const int s = it % S::STAGES;
+                if (!mbar_wait(empty(s), ((it / S::STAGES) & 1) ^ 1, &gave_up)) break;
+                if (elected()) {
+                    expect(t, s);
+                    load_w(t, s, kb);
+                    load_x(t, s, kb);
+                }
+                __syncwarp();
+            }
+            if (*(volatile int*)&gave_up) break;
+        }
+    } else if (warp == 1) {
+        const int steps = (p.K + 63) / 64;
+        bool ok = true;
+        for (Segment t = first_segment(); t.g < g1 && ok; advance(t), acc++) {
+            const int b = acc & 1;
+            const uint32_t desc = instruction(t.c.rows, FORMAT);
+            ok = mbar_wait(acc_empty(b), ((acc >> 1) & 1) ^ 1, &gave_up);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int kb = t.k0; kb < t.k1; kb++, it++) {
+                const int s = it % S::STAGES, left = min(4, steps - 4 * kb);
+                ok = mbar_wait(full(s), (it / S::STAGES) & 1, &gave_up);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t at = base + s * S::D_STAGE, w_scales = tmem + 2 * TN + s * 8 * S::ATOMS, x_scales = w_scales + 4 * S::ATOMS;
+                const uint64_t w = operand(at), x = operand(at + S::D_PIECES);
+                if (elected()) {
+#pragma unroll
+                    for (int a = 0; a < S::ATOMS; a++) copy_scales(w_scales + 4 * a, at + CH * KB + a * ATOM), copy_scales(x_scales + 4 * a, at + S::D_SCALES + a * ATOM);
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        if (k >= left) break;
+                        const int a = k * S::ATOMS / 4;
+                        const uint32_t two = FORMAT == HCCL_MXFP4 ? 2u * (k & 1) : 0u;
+                        mma_fp4<FORMAT>(tmem + b * TN, w + 2 * k, x + 2 * k, desc | (two << 4) | (two << 29), w_scales + 4 * a, x_scales + 4 * a, (kb > t.k0 || k > 0) ? 1u : 0u);
+                    }
+                    mma_commit<1>(empty(s));
+                    if (kb == t.k1 - 1) mma_commit<1>(acc_full(b));
+                }
+                __syncwarp();
+            }
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, me = quarter * 32 + lane;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        for (int t = 0; t < p.T; t++) sums[t * CH + me] = 0.f;
+        bool ok = true;
+        // What a segment's sums are multiplied with, asked for one segment ahead: each lane below the number of rows holds one row's choice.
+        struct Row {
+            int token;
+            float weight, back, wide, bias;
+        };
+        const auto row_of = [&](const Segment& t) {
+            Row r = {-1, 0.f, 0.f, p.wide[t.c.expert], 0.f};  // (of no segment: nothing)
+            if (p.bias && t.k0 == 0 && t.tile * CH + me < p.N) r.bias = p.bias[(long long)t.c.expert * p.N + t.tile * CH + me];
+            if (lane < t.c.rows) {
+                const int choice = p.source[t.c.row + lane];
+                if ((unsigned)choice < (unsigned)p.rows) r.token = choice / p.top_k, r.weight = p.weights[choice];
+                r.back = __ldcg(p.unscale + (long long)(t.c.row + lane) * p.down_parts + t.k0 / SPAN);
+            }
+            return r;
+        };
+        Segment next = first_segment();
+        Row row, next_row = row_of(next);
+        while (next.g < g1 && ok) {
+            const Segment t = next;
+            row = next_row;
+            advance(next);
+            if (next.g < g1) next_row = row_of(next);
+            const int b = acc & 1, chan = t.tile * CH + me;
+            const bool in = chan < p.N;
+            ok = mbar_wait(acc_full(b), (acc >> 1) & 1, &gave_up);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int r = 0; r < ROWS; r++) {
+                if (r >= t.c.rows) break;
+                float v[8];
+                __syncwarp();
+                tmem_load8(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + r * PIECES, v);
+                tmem_arrived();
+                const int to = __shfl_sync(0xffffffffu, row.token, r);
+                const float z = fmaf(sum_of_pieces<FORMAT>(v), __shfl_sync(0xffffffffu, row.back, r) * row.wide, row.bias), f = __shfl_sync(0xffffffffu, row.weight, r);
+                if (to >= 0) sums[to * CH + me] = fmaf(f, z, sums[to * CH + me]);
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acc_empty(b));
+            acc++;
+            if (t.g1 == g1 || t.g1 == (t.tile + 1) * of_tile) {  // the last of its channels here
+                if (g0 <= t.tile * of_tile && t.g1 == (t.tile + 1) * of_tile) {
+                    T* y = (T*)p.y + chan;
+                    for (int i = 0; i < p.T; i++, y += p.ldy) {
+                        if (in) *y = from_f32<T>(sums[i * CH + me]);
+                        sums[i * CH + me] = 0.f;
+                    }
+                } else {
+                    float* part = p.part + (long long)(2 * blockIdx.x + (t.tile == g0 / of_tile ? 0 : 1)) * p.T * CH + me;
+                    for (int i = 0; i < p.T; i++, part += CH) {
+                        __stcg(part, sums[i * CH + me]);
+                        sums[i * CH + me] = 0.f;
+                    }
+                }
+            }
+        }
+        __threadfence();  // the sums are out before this block counts its stages
+    }
+    if (warp == 0 && lane == 0 && *(volatile int*)&gave_up) drain(full, S::STAGES, it, p.status);
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(COLS));
+    if (*(volatile int*)&gave_up) return;
+    if (total == 0) {  // no token has an expert
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        for (long long i = (long long)blockIdx.x * DOWN_THREADS + threadIdx.x; i < (long long)p.T * p.N; i += (long long)blocks * DOWN_THREADS)
+            ((T*)p.y)[i / p.N * p.ldy + i % p.N] = from_f32<T>(0.f);
+        return;
+    }
+    if (threadIdx.x < 2 && g0 < g1) {  // the first and the last of this block's runs of channels, if others share them
+        const int tile = threadIdx.x == 0 ? g0 / of_tile : (g1 - 1) / of_tile, lo = max(g0, tile * of_tile), hi = min(g1, (tile + 1) * of_tile), n = hi - lo;
+        if (n < of_tile && (threadIdx.x == 0 || tile != g0 / of_tile)) {
+            if (atomicAdd(p.tile_count + tile, n) + n == of_tile) list[atomicAdd(&completed, 1)] = tile;
+            __threadfence();
+        }
+    }
+    __syncthreads();
+    for (int i = warp; i < completed * p.T; i += DOWN_THREADS / 32) {
+        const int token = i / completed, tile = list[i % completed], chan = tile * CH + 4 * lane;
+        const auto block_of_stage = [&](long long g) { return (int)(((g + 1) * blocks - 1) / total); };
+        const int from = block_of_stage((long long)tile * of_tile), to = block_of_stage((long long)(tile + 1) * of_tile - 1);
+        float sum[4] = {};
+#pragma unroll 8
+        for (int b = from; b <= to; b++) {
+            const int lo = first_of(b), which = tile == lo / of_tile ? 0 : 1;
+            const bool some = first_of(b + 1) > lo;  // (with fewer stages than blocks some have none)
+            const float4 v = __ldcg((const float4*)(p.part + ((long long)(2 * b + which) * p.T + token) * CH) + lane);
+            if (some) sum[0] += v.x, sum[1] += v.y, sum[2] += v.z, sum[3] += v.w;
+        }
+        T* y = (T*)p.y + (long long)token * p.ldy + chan;
+#pragma unroll
+        for (int c = 0; c < 4; c++)
+            if (chan + c < p.N) y[c] = from_f32<T>(sum[c]);
+    }
+}
+
+// ---------------------------------------------------------------- host
+constexpr long long up_to(long long n, long long m) { return (n + m - 1) / m * m; }
+
+// Floats of the first product's partial sums: [parts of K][rows][width]. With all SPAN stages to a unit there are that many parts; where span_of cuts finer, it does so because there
+// are fewer than ENOUGH * SMS units of twice the size, each of 128 channels x at most 8 rows (width is at most 16 more than the channels).
+long long partial_sums(long long rows, long long width, long long k_blocks) {
+    const long long most = rows * k_blocks * width, fine = 2ll * ROWS * ENOUGH * SMS * (CH + 16), coarse = rows * ((k_blocks + SPAN - 1) / SPAN) * width;
+    return std::max(coarse, std::min(most, fine));
+}
+
+struct Places {  // in the scratch, in bytes
+    long long half, width, pitch, parts, counts, count_bytes, sums, unscale, pieces, scales, part, end;
+};
+Places places(long long T, long long rows, long long H, long long I, int gated, int format) {
+    Places a;
+    a.half = up_to(I, 8);
+    a.width = (gated ? 2 : 1) * a.half;
+    a.pitch = up_to(I, 256) / 2;
+    long long at = 0;
+    const auto take = [&](long long bytes) {
+        const long long here = at;
+        at += up_to(bytes, 512);
+        return here;
+    };
+    a.parts = (I + WIDE - 1) / WIDE;
+    a.count_bytes = 4 * (rows * a.parts + (H + CH - 1) / CH);  // of parts of chunks (there are at most as many chunks as rows) and of the second product's tiles
+    a.counts = take(a.count_bytes);
+    a.sums = take(4 * partial_sums(rows, a.width, (H + 255) / 256));
+    a.unscale = take(4 * rows * a.parts);
+    a.pieces = take(rows * PIECES * a.pitch);
+    a.scales = take(rows * ((I + 255) / 256) * stage_atoms(format) * ATOM);
+    a.part = take(4 * 2ll * SMS * T * CH);
+    a.end = at;
+    return a;
+}
+
+template <typename Kernel> cudaError_t launch(Kernel* kernel, std::atomic<bool>* ready, int threads, int smem, bool dependent, const FewParams& p, cudaStream_t s) {
     int dev = 0;
     cudaError_t e;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     if (dev >= 64 || !ready[dev]) {
-        e = cudaFuncSetAttribute(hccl_few_fp4<T, FORMAT, DOWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-        if (e != cudaSuccess) return e;
+        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
         if (dev < 64) ready[dev] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(SMS);
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = S::SMEM;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = DOWN ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, hccl_few_fp4<T, FORMAT, DOWN>, p);
-}
-
-constexpr long long up_to(long long n, long long m) { return (n + m - 1) / m * m; }
-
-// Floats of partial sums: [parts of K][rows][width]. With all SPAN stages to a unit there are that many parts; where span_of cuts finer, it does so because there are fewer than
-// ENOUGH * SMS units of twice the size, each of 128 channels x at most 8 rows (width is at most 16 more than the channels).
-long long partial_sums(long long rows, long long width, long long k_blocks) {
-    const long long most = rows * k_blocks * width, fine = 2ll * ROWS * ENOUGH * SMS * (CH + 16), coarse = rows * ((k_blocks + SPAN - 1) / SPAN) * width;
-    return up_to(std::max(coarse, std::min(most, fine)), 64);
-}
-
-struct Places {
-    long long half, wide_up, wide_y, sums_up, sums_down, tiles;
-};
-Places places(long long rows, long long H, long long I, int gated) {
-    Places a;
-    a.half = up_to(I, 8);
-    a.wide_up = (gated ? 2 : 1) * a.half;
-    a.wide_y = H;
-    a.sums_up = partial_sums(rows, a.wide_up, (H + 255) / 256);
-    a.sums_down = partial_sums(rows, a.wide_y, (I + 255) / 256);
-    a.tiles = (H + CH - 1) / CH;
-    return a;
+    cfg.numAttrs = dependent ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 template <typename T, int FORMAT> cudaError_t few(const FewFp4& q, cudaStream_t s) {
     using S = Shape<FORMAT>;
-    const long long rows = q.T * q.top_k, N = (q.gated ? 2 : 1) * q.I;
-    const Places at = places(rows, q.H, q.I, q.gated);
+    const long long rows = q.T * q.top_k;
+    const Places at = places(q.T, rows, q.H, q.I, q.gated, FORMAT);
     FewParams p = {};
     p.offsets = q.offsets;
     p.source = q.source;
-    p.slots = q.slots;
     p.weights = q.weights;
     p.status = q.status;
     p.experts = q.experts;
@@ -546,47 +906,50 @@ template <typename T, int FORMAT> cudaError_t few(const FewFp4& q, cudaStream_t 
     p.rows = (int)rows;
     p.act = q.act;
     p.gated = q.gated;
-    p.half = (int)at.half;
     p.I = (int)q.I;
-    p.wide_y = (int)at.wide_y;
-    p.down_tiles = (int)at.tiles;
-    float* const sums = (float*)q.scratch;
-    p.arrived = (int*)(sums + at.sums_up + at.sums_down);
-    p.part = sums + at.sums_up;
+    p.half = (int)at.half;
+    p.width = (int)at.width;
+    p.pitch = at.pitch;
+    p.down_blocks = (int)((q.I + 255) / 256);
+    p.down_parts = (int)at.parts;
+    p.chunk_count = (int*)(q.scratch + at.counts);
+    p.tile_count = p.chunk_count + rows * at.parts;
+    p.sums = (float*)(q.scratch + at.sums);
+    p.unscale = (float*)(q.scratch + at.unscale);
+    p.pieces = (uint8_t*)(q.scratch + at.pieces);
+    p.piece_scales = (uint8_t*)(q.scratch + at.scales);
+    p.part = (float*)(q.scratch + at.part);
     cudaError_t e;
-    const auto maps = [&](const uint8_t* w, const uint8_t* scale, long long ld, long long n, long long k) {
-        p.N = (int)n;
+    const auto maps = [&](const uint8_t* w, const uint8_t* scale, long long ld, long long n, long long k, int halves) {
+        p.N = (int)(n * halves);
         p.K = (int)k;
         p.k_blocks = (int)((k + 255) / 256);
         p.chan_tiles = (int)((n + CH - 1) / CH);
-        if ((e = make_map(&p.w, w, n * q.experts, (k + 1) / 2, ld, CH)) != cudaSuccess) return e;
-        return make_atom_map(&p.w_scale, scale, (long long)q.experts * p.chan_tiles * p.k_blocks * S::ATOMS, S::ATOMS);
+        if ((e = make_map(&p.w, w, n * halves * q.experts, (k + 1) / 2, ld, CH)) != cudaSuccess) return e;
+        return make_atom_map(&p.w_scale, scale, (long long)q.experts * halves * p.chan_tiles * p.k_blocks * S::ATOMS, S::ATOMS);
     };
-    if ((e = maps(q.up, q.up_scale, q.ld_up, N, q.H)) != cudaSuccess) return e;
-    p.x = q.x;
+    if ((e = cudaMemsetAsync(p.chunk_count, 0, at.count_bytes, s)) != cudaSuccess) return e;
+    if ((e = maps(q.up, q.up_scale, q.ld_up, q.I, q.H, q.gated ? 2 : 1)) != cudaSuccess) return e;
+    p.in = q.x;
     p.ldx = q.ldx;
     p.vec = (uintptr_t)q.x % 16 == 0 && (q.T <= 1 || q.ldx * sizeof(T) % 16 == 0);
-    p.y = sums;
     p.wide = q.up_wide;
     p.bias = q.up_bias;
-    if ((e = launch<T, FORMAT, false>(p, s)) != cudaSuccess) return e;
-    p.x_blocks = p.k_blocks;
-    p.x_tiles = p.chan_tiles;
-    if ((e = maps(q.down, q.down_scale, q.ld_down, q.H, q.I)) != cudaSuccess) return e;
-    p.x = sums;
+    static std::atomic<bool> up_ready[64], down_ready[64];  // by device; setting it twice does no harm
+    if ((e = launch(hccl_few_up<T, FORMAT>, up_ready, UP_THREADS, S::SMEM_UP, false, p, s)) != cudaSuccess) return e;
+    if ((e = maps(q.down, q.down_scale, q.ld_down, q.H, q.I, 1)) != cudaSuccess) return e;
+    if ((e = make_map(&p.x, p.pieces, rows * PIECES, at.pitch, at.pitch, PIECES)) != cudaSuccess) return e;
+    if ((e = make_atom_map(&p.x_scale, p.piece_scales, rows * p.k_blocks * S::ATOMS, S::ATOMS)) != cudaSuccess) return e;
     p.y = q.y;
     p.ldy = q.ldy;
     p.wide = q.down_wide;
     p.bias = q.down_bias;
-    return launch<T, FORMAT, true>(p, s);
+    return launch(hccl_few_down<T, FORMAT>, down_ready, DOWN_THREADS, S::SMEM_DOWN, true, p, s);
 }
 
 }  // namespace
 
-size_t few_fp4_scratch(long long T, long long H, long long I, int top_k, int gated) {
-    const Places at = places(T * top_k, H, I, gated);
-    return (size_t)((at.sums_up + at.sums_down) * 4 + up_to(at.tiles * 4, 128));
-}
+size_t few_fp4_scratch(long long T, long long H, long long I, int top_k, int gated, int format) { return (size_t)places(T, T * top_k, H, I, gated, format).end; }
 
 cudaError_t launch_few_fp4(int dt, const FewFp4& p, cudaStream_t s) {
     if (p.T == 0) return cudaSuccess;

@@ -143,15 +143,20 @@ class Fp4Linear:
             weight = padded
         self.weight, self.tensor_scale, self.bias = weight, tensor_scale, bias
         self.ldw = weight.shape[-1]
-        self._rows_scale = scale  # kept for copies
-        with torch.cuda.device(self.dev):
-            self.scale = torch.empty(max(hb.hccl_fp4_weight_scale_bytes(self.N, self.K, self.experts, self.fmt), 16), dtype=torch.uint8, device=self.device)
-            hb.hccl_fp4_weight_scales(scale.contiguous().data_ptr(), blocks, self.N, self.K, self.experts, self.fmt, self.scale.data_ptr(), _stream(self.dev))
+        self._rows_scale = scale.contiguous()  # kept for copies
+        self.scale = self._laid_out(self.N, self.experts)
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._fixed = (self.fmt, weight.data_ptr(), self.ldw, self.scale.data_ptr(), tensor_scale.data_ptr(), bias.data_ptr() if bias is not None else 0)
         self._status_at = self._status.data_ptr()
         self._x_bits = _bits(self.x_scale)
         self._need = {}  # scratch bytes by number of rows
+
+    def _laid_out(self, N: int, groups: int) -> torch.Tensor:
+        """The scales as the tensor cores take them, in groups of N rows."""
+        out = torch.empty(max(hb.hccl_fp4_weight_scale_bytes(N, self.K, groups, self.fmt), 16), dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.dev):
+            hb.hccl_fp4_weight_scales(self._rows_scale.data_ptr(), self._rows_scale.shape[-1], N, self.K, groups, self.fmt, out.data_ptr(), _stream(self.dev))
+        return out
 
     def __reduce__(self):  # a copy has weights, and their addresses, of its own
         return Fp4Linear, (self.weight[..., : (self.K + 1) // 2], self._rows_scale, self.tensor_scale, self.bias, self.format, self.x_scale, self.K)
@@ -266,6 +271,9 @@ class FewTokens:
         self.H, self.dev, self.device = up.K, up.dev, up.device
         _, w_up, ld_up, s_up, g_up, b_up = up._fixed
         _, w_down, ld_down, s_down, g_down, b_down = down._fixed
+        if gated and down.K % 128:  # the halves' scales begin on tiles of their own
+            self._up_scale = up._laid_out(down.K, 2 * up.experts)
+            s_up = self._up_scale.data_ptr()
         self.record = hb.ExpertsFp4(up.K, down.K, up.experts, up.fmt, ACTS[act], 1 if gated else 0, w_up, ld_up, s_up, g_up, b_up, w_down, ld_down, s_down, g_down, b_down)
         hb.hccl_expert_layer_scratch_bytes(self.record, 1, 1)  # refuses sizes that the kernels do not take
         self._at = C.addressof(self.record)

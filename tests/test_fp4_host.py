@@ -45,7 +45,7 @@ def test_sizes_of_laid_out_scales():
     assert hb.hccl_fp4_weight_scale_bytes(129, 257, 3, hb.NVFP4) == 3 * 2 * 2 * 2048
     assert hb.hccl_fp4_weight_scale_bytes(1, 1, 1, hb.MXFP4) == 1024
     assert hb.hccl_fp4_weight_scale_bytes(0, 64, 0, hb.MXFP4) == 0 and hb.hccl_fp4_weight_scale_bytes(64, 0, 0, hb.MXFP4) == 0
-    for bad in ((-1, 64, 0, 0), (64, -1, 0, 0), (64, 64, -1, 0), (64, 64, 1025, 0), (64, (1 << 17) + 1, 0, 0), (1 << 31, 64, 0, 0), (1 << 28, 1 << 17, 0, 0)):
+    for bad in ((-1, 64, 0, 0), (64, -1, 0, 0), (64, 64, -1, 0), (64, 64, 2049, 0), (64, (1 << 17) + 1, 0, 0), (1 << 31, 64, 0, 0), (1 << 28, 1 << 17, 0, 0)):
         with pytest.raises(hb.HcclError) as e:
             hb.hccl_fp4_weight_scale_bytes(*bad)
         assert e.value.status == hb.ERR_INVALID_ARG
@@ -59,7 +59,7 @@ def test_weight_scale_refusals():
         return status(hb.hccl_fp4_weight_scales, s, lds, N, K, groups, fmt, out, 0)
 
     assert go(s=0) == hb.ERR_INVALID_ARG and go(out=0) == hb.ERR_INVALID_ARG and go(out=A + 8) == hb.ERR_ALIGNMENT
-    assert go(lds=3) == hb.ERR_INVALID_ARG and go(fmt=9) == hb.ERR_DTYPE and go(groups=1025) == hb.ERR_INVALID_ARG
+    assert go(lds=3) == hb.ERR_INVALID_ARG and go(fmt=9) == hb.ERR_DTYPE and go(groups=2049) == hb.ERR_INVALID_ARG
     assert go(N=0) == hb.OK and go(K=0) == hb.OK
 
 
@@ -130,26 +130,24 @@ def test_layer_refusals():
         hb.hccl_expert_layer_scratch_bytes(experts(), 4, 33)
 
 
-@pytest.mark.parametrize("rows,H,I,gated", [(1, 64, 32, 1), (8, 4096, 2048, 1), (512, 4096, 2048, 1), (2048, 131072, 1000, 0), (3, 131072, 131072, 1), (100, 257, 129, 0)])
-def test_layer_scratch_holds_every_cut_of_k(rows, H, I, gated):
-    """The kernels cut K by the number of units; whatever number of chunks the rows make, the partial sums fit."""
-    blocks, up_width = 148, (2 if gated else 1) * (-(-I // 8) * 8)
-
-    def floats(width, tiles, k_blocks):
-        most = 0
-        for filled in {1, 2, rows // 8 + 1, rows // 2 + 1, rows}:
-            if filled > rows:
-                continue
-            for chunks in {-(-filled // 8), min(filled, 1024), filled}:  # from full chunks to a row in each
-                span = 4
-                while span > 1 and chunks * tiles * -(-k_blocks // span) < 6 * blocks:
-                    span //= 2
-                most = max(most, -(-k_blocks // span) * filled * width)
-        return most
-
-    need = floats(up_width, -(-(2 if gated else 1) * I // 128), -(-H // 256)) + floats(H, -(-H // 128), -(-I // 256))
-    T, k = (rows, 1) if rows <= 64 else (64, rows // 64)
-    assert 4 * need + 4 * -(-H // 128) <= hb.hccl_expert_layer_scratch_bytes(experts(H=H, I=I, gated=gated, ld_up=1 << 17, ld_down=1 << 17), T, max(k, 1) if T * k >= rows else k + 1)
+@pytest.mark.parametrize("T,k,H,I,gated", [(1, 1, 64, 32, 1), (1, 8, 4096, 2048, 1), (64, 8, 4096, 2048, 1), (64, 32, 131072, 1000, 0), (3, 1, 131072, 131072, 1), (50, 2, 257, 129, 0), (64, 1, 1, 1, 1)])
+@pytest.mark.parametrize("fmt", [hb.NVFP4, hb.MXFP4])
+def test_layer_scratch_holds_every_cut_of_k(T, k, H, I, gated, fmt):
+    """The first kernel cuts K by the number of units; whatever number of chunks the rows make, the partial sums fit, and beside them the pieces with their scales
+    and two tiles of partial results for each block."""
+    blocks, rows, halves, k_blocks = 148, T * k, 2 if gated else 1, -(-H // 256)
+    width, tiles, most = halves * (-(-I // 8) * 8), halves * -(-I // 128), 0
+    for filled in {1, 2, rows // 8 + 1, rows // 2 + 1, rows}:
+        if filled > rows:
+            continue
+        for chunks in {-(-filled // 8), filled}:  # from full chunks to a row in each
+            span = 4
+            while span > 1 and chunks * tiles * -(-k_blocks // span) < 6 * blocks:
+                span //= 2
+            most = max(most, -(-k_blocks // span) * filled * width)
+    stages, atoms = -(-I // 256), 4 if fmt == hb.NVFP4 else 2
+    need = 4 * most + rows * 8 * stages * 128 + rows * stages * atoms * 512 + 2 * blocks * T * 128 * 4 + 4 * rows * -(-I // 1024) * 2 + 4 * -(-H // 128)
+    assert need <= hb.hccl_expert_layer_scratch_bytes(experts(H=H, I=I, gated=gated, format=fmt, ld_up=1 << 17, ld_down=1 << 17), T, k)
 
 
 def test_activation_refusals():

@@ -676,8 +676,8 @@ hccl_status_t hccl_linear_fp4(const hccl_matmul_fp4_t*, const void* x, int64_t l
 /* A whole expert layer for a few tokens, in two kernels: y[t] = round(sum over k of weights[t,k] (down_e h_e + down_bias_e)), e = ids[t,k], with
  * u = up_e x[t] + up_bias_e and h = act(u[0..I-1]) * u[I..2I-1] if gated, act(u) otherwise. Weights in 4 bits as in hccl_matmul_fp4_t: up [experts, 2 I or I, H], down
  * [experts, H, I], their scales from hccl_fp4_weight_scales (up's, if gated, laid
- * out as 2 * experts groups of I rows, which for I a multiple of 128 is the same). Activations are not rounded to 4 bits: they enter the products as sums of eight such numbers, which leaves 6^-8 (HCCL_MXFP4: 4^-8) of a block's largest
- * element; sums, u and h are FP32. A row with an infinity or a NaN gives NaN. Choices without an expert add nothing; a token without any gets 0.
+ * out as 2 * experts groups of I rows, which for I a multiple of 128 is the same). Activations are not rounded to 4 bits: they enter the products as sums of eight such numbers, which leaves 2^-22 of the largest
+ * of up to 1024 neighbours; sums, u and h are FP32. A row with an infinity or a NaN gives NaN. Choices without an expert add nothing; a token without any gets 0.
  * Reads the routing's weights, offsets and source. tokens <= HCCL_MAX_FEW_TOKENS; H and I from 1 to HCCL_MAX_FP4_K. scratch: hccl_expert_layer_scratch_bytes, 128-byte aligned, contents
  * arbitrary, not shared by calls in flight at once. dev_status as in hccl_matmul_i8_t. */
 #define HCCL_MAX_FEW_TOKENS 64

@@ -5,15 +5,21 @@
 namespace hccl {
 namespace experts {
 
+// 1 / x within 1 ulp, subnormal results too.
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ float activation(int act, float g) {
-    if (act == HCCL_ACT_SILU) return g / (1.f + expf(-g));
+    if (act == HCCL_ACT_SILU) return g * reciprocal(1.f + expf(-g));
     if (act == HCCL_ACT_GELU) return g * normcdff(g);
     return g > 0.f || g != g ? g : 0.f;
 }
 // And its derivative; of the rectifier at 0: 0.
 __device__ __forceinline__ void activation_slope(int act, float g, float* a, float* slope) {
     if (act == HCCL_ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-g));
+        const float s = reciprocal(1.f + expf(-g));
         *a = g * s;
         *slope = s * (1.f + g * (1.f - s));
     } else if (act == HCCL_ACT_GELU) {

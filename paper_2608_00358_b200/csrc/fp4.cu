@@ -266,7 +266,7 @@ static hccl_status_t check_experts(const hccl_experts_fp4_t* e, int64_t tokens, 
 hccl_status_t hccl_expert_layer_scratch_bytes(const hccl_experts_fp4_t* e, int64_t tokens, int32_t top_k, size_t* bytes) {
     TRY(check_experts(e, tokens, top_k));
     if (!bytes) return HCCL_ERR_INVALID_ARG;
-    *bytes = few_fp4_scratch(tokens, e->H, e->I, top_k, e->gated != 0, e->format);
+    *bytes = few_fp4_scratch(tokens, e->H, e->I, top_k, e->gated != 0);
     return HCCL_OK;
 }
 
@@ -286,7 +286,7 @@ hccl_status_t hccl_expert_layer_fp4(const hccl_experts_fp4_t* e, const void* x, 
     if (r->tokens == 0) return HCCL_OK;
     if (!r->weights || !r->source) return HCCL_ERR_INVALID_ARG;
     if (!aligned(r->weights, 4) || !aligned(r->source, 4)) return HCCL_ERR_ALIGNMENT;
-    if (!scratch || bytes < few_fp4_scratch(r->tokens, e->H, e->I, r->top_k, e->gated != 0, e->format)) return HCCL_ERR_WORKSPACE;
+    if (!scratch || bytes < few_fp4_scratch(r->tokens, e->H, e->I, r->top_k, e->gated != 0)) return HCCL_ERR_WORKSPACE;
     if (!aligned(scratch, 128)) return HCCL_ERR_ALIGNMENT;
     FewFp4 p = {};
     p.T = r->tokens;

@@ -153,7 +153,7 @@ struct FewFp4 {        // a whole expert layer for few tokens
     char* scratch;
     int* status;
 };
-size_t few_fp4_scratch(long long T, long long H, long long I, int top_k, int gated, int format);
+size_t few_fp4_scratch(long long T, long long H, long long I, int top_k, int gated);
 cudaError_t launch_few_fp4(int dt, const FewFp4& p, cudaStream_t s);
 
 }  // namespace experts

@@ -1,12 +1,10 @@
 // A whole expert layer for a few tokens in two kernels: y[t] = sum over j of w[t, j] down_e(act(up_e(x[t]))), weights in 4-bit floating point, activations not rounded.
 //
 // With few tokens the chosen experts' weights are read once and that is the time, so 4-bit activations would save nothing and cost accuracy. The tensor cores multiply 4-bit
-// numbers by 4-bit numbers all the same: an activation goes in as a sum of eight of them. Of a block x of a row, q0 = e2m1(x / s0) is taken, of what is left q1, and so on,
-// each with a scale of its own; a step leaves at most a sixth (powers of two as scales: a quarter) of the block's maximum, so eight leave 6^-8 (4^-8). Eight columns is
-// also the least that an instruction computes: a token's eight pieces are its eight columns, and for one token they cost nothing. The sum over the pieces
-// is taken in 32 bits. With e4m3 scales a row is first multiplied by a power of two that brings its largest element to 1024 .. 2048, near 448 x 6, the top of their range; what
-// four pieces leave is less than 2048 x 0.178^4 = 2.1 (a rounded scale leaves up to 17 / 96 of a block's maximum) and is multiplied by 2^10, so that the last four have the whole range
-// again and the scales' smallest step, 2^-9, is 2^-30 of the row's largest element.
+// numbers by 4-bit numbers all the same: an activation goes in as the sum of eight of them. 1024 elements of a row (or what there is) are brought to whole numbers below 2^22 by a power of
+// two, which leaves less than 2^-22 of their largest, and written with eight digits from -4 to 3 in base 8; half a digit is an e2m1 number, and its scale, a power of 8, the same for all blocks.
+// Four digits span what one byte's scale can: the last four columns have the scales of the first four again, and their sum 8^-4 of the weight. Eight columns is also the least that an
+// instruction computes: a token's eight digits are its eight columns, and for one token they cost nothing. The sum over them is taken in 32 bits.
 //
 // Rows in expert order are taken in chunks of at most 8 rows of one expert. Both kernels run one block to an SM, and weights never wait for anything but room:
 //
@@ -31,7 +29,7 @@ namespace {
 
 constexpr int CH = 128, ROWS = 8 /* of a chunk */, PIECES = 8, SPAN = 4 /* stages of K in a part at most, of the second product in every one */, WIDE = SPAN * 256, GROUP = WIDE / CH /* channel tiles of a half in 1024 columns */, COLS = 512;
 constexpr int TN = ROWS * PIECES;
-constexpr float LATER = 1024.f;  // e4m3 scales: what the last half of the pieces is larger by
+constexpr float LATER = 4096.f;  // what the last half of the pieces is larger by
 constexpr int ENOUGH = 6;  // units for each block, below which K is cut finer
 constexpr int EACH = 8;  // elements of a thread that makes pieces
 static_assert(ROWS * WIDE % EACH == 0, "");
@@ -42,31 +40,27 @@ constexpr int MAX_CHUNKS = HCCL_MAX_FEW_TOKENS * HCCL_MAX_TOP_K, OWN = (MAX_CHUN
 template <int FORMAT> struct Shape {
     static constexpr int ATOMS = stage_atoms(FORMAT);
     static constexpr int STAGES = 6;
-    // up: the ring of weights, two parts' pieces (their rows by stages, then their scales), and elements between their row's maximum and their pieces
+    // up: the ring of weights, two parts' pieces, and elements between their row's maximum and their pieces
     static constexpr int STAGE = CH * KB + ATOMS * ATOM;
-    static constexpr int PIECE_STAGE = TN * KB, PIECE_SCALES = SPAN * PIECE_STAGE;
-    static constexpr int PART = PIECE_SCALES + SPAN * ATOMS * ATOM;
-    static constexpr int RING = (STAGES * STAGE + 1023) / 1024 * 1024;
+    static constexpr int PIECE_STAGE = TN * KB, PART = SPAN * PIECE_STAGE;
+    static constexpr int RING = STAGES * STAGE;
     static constexpr int HELD = ROWS * WIDE * 4;
     static constexpr int SMEM_UP = RING + 2 * PART + HELD + 1024;
-    // its tensor memory: two accumulators, two parts' scales, the stages' scales
-    static constexpr int X_SCALES = 2 * TN, W_SCALES = X_SCALES + 2 * SPAN * 4 * ATOMS;
-    static_assert(W_SCALES + STAGES * 4 * ATOMS <= COLS, "tensor memory");
     static_assert(STAGE % 1024 == 0 && PART % 1024 == 0, "operands start on 1024-byte boundaries");
-    // down: a stage of weights, their scales, pieces, their scales; then [token][channel]
-    static constexpr int D_PIECES = STAGE, D_SCALES = D_PIECES + TN * KB, D_STAGE = D_SCALES + ATOMS * ATOM;
-    static constexpr int D_SUMS = STAGES * D_STAGE;
+    // down: a stage of weights, their scales, pieces; then [token][channel]
+    static constexpr int D_STAGE = STAGE + PIECE_STAGE, D_SUMS = STAGES * D_STAGE;
     static constexpr int SMEM_DOWN = D_SUMS + HCCL_MAX_FEW_TOKENS * CH * 4 + 1024;
-    static_assert(2 * TN + STAGES * 8 * ATOMS <= COLS, "tensor memory");
-    static_assert(D_STAGE % 1024 == 0, "operands start on 1024-byte boundaries");
+    // tensor memory: two accumulators, the pieces' scales, the stages' scales
+    static constexpr int X_SCALES = 2 * TN, W_SCALES = X_SCALES + 4;
+    static_assert(W_SCALES + STAGES * 4 * ATOMS <= COLS, "tensor memory");
 };
 
 struct FewParams {
-    CUtensorMap w, w_scale, x, x_scale;  // the last two: down
+    CUtensorMap w, w_scale, x;  // the last: down
     const void* in;        // up: [T, K] in T
     void* y;               // down: [T, N]
     float* sums;           // up: partial sums [part of K][row][width]
-    uint8_t *pieces, *piece_scales;  // [row][8][pitch] and, in atoms, [chunk][stage]
+    uint8_t* pieces;       // [row][8][pitch]
     float* unscale;        // [row][part of the second product's K]
     float* part;           // down: two tiles of partial sums for each block, [token][channel]
     int *chunk_count, *tile_count;
@@ -129,54 +123,51 @@ __device__ __forceinline__ bool all_of(bool ok, int barrier, int count) {
     return r != 0;
 }
 
-// A step that serves for a piece: whatever it is, what it leaves is exact and goes to the next piece, so that divisions need not be rounded to nearest.
-template <int FORMAT> __device__ __forceinline__ Step some_step(unsigned top) {
-    if constexpr (FORMAT == HCCL_MXFP4) return step_of<FORMAT>(top, 1.f, 6.f);
-    Step r;
-    unsigned short two;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(__uint_as_float(top) * (1.f / 6.f)));
-    unsigned halves;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(halves) : "h"(two));
-    r.byte = top >= 0x7f800000u ? 0x7fu : two & 0xffu;
-    r.d = __low2float(*(const __half2*)&halves);
-    r.inv = r.byte ? __fdividef(1.f, r.d) : 0.f;
-    return r;
-}
-
-// What pieces of a row with this largest magnitude are larger by, and its inverse: powers of two that are no subnormal numbers, 2^10 <= largest * factor < 2^11.
+// What 1024 elements with this largest magnitude are multiplied with, a power of two, to become whole numbers below 2^22; and what half a digit of the first columns' scales stands for.
 __device__ __forceinline__ void row_factor(unsigned top, float* factor, float* back) {
-    const int e = (int)(top >> 23) - 127, up = min(max(10 - e, -126), 126);
+    const int e = (int)(top >> 23) - 127, up = min(21 - e, 126);  // (numbers near the smallest are cut at 2^-127)
     *factor = __uint_as_float((unsigned)(127 + up) << 23);
-    *back = __uint_as_float((unsigned)(127 - up) << 23);
+    *back = top >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : __uint_as_float((unsigned)(127 + 16 - up) << 23);  // 2 * 8^5 / factor
 }
-// Eight elements of a block that lies with 2 (e4m3 scales) or 4 neighbouring lanes, to eight pieces, one after the other: put(piece, codes, scale byte). Whole warps.
-template <int FORMAT, typename Put> __device__ __forceinline__ void make_pieces(float (&v)[EACH], const Put& put) {
-    // (a loop: code that a warp passes once is fetched instruction by instruction)
-#pragma unroll 1
-    for (int q = 0; q < PIECES; q++) {
-        if (FORMAT == HCCL_NVFP4 && q == PIECES / 2)
+// The scale of piece q, as stored, four times: 64, 8, 1, 1/8, and again.
+template <int FORMAT> __device__ __forceinline__ unsigned piece_scale(int q) {
+    const unsigned e = 6 - 3 * (q & 3), byte = FORMAT == HCCL_NVFP4 ? (e + 7) << 3 : e + 127;
+    return byte * 0x01010101u;
+}
+// Eight neighbouring elements to eight pieces of them; piece q's codes go to codes + q * pitch, there to the sixteen bytes number (sixteen ^ (q & swizzle)).
+// One function for all places, since code that a warp passes for the first time is fetched line by line.
+__device__ __noinline__ void make_pieces(float4 lo, float4 hi, float factor, char* codes, long long pitch, int sixteen, int swizzle) {
+    const float v[EACH] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    unsigned a[EACH];
 #pragma unroll
-            for (int j = 0; j < EACH; j++) v[j] *= LATER;
-        unsigned top = 0;
+    for (int j = 0; j < EACH; j++) {
+        // 1.5 * 2^23 + n has the whole number n in its low bits; with 44444444 in base 8 added, digit + 4 in every three of them.
+        unsigned x = __float_as_uint(__fmaf_rn(v[j], factor, 12582912.f)) - 0x4b400000u + 044444444u;
+        x = (x & 0xfffu) | (x << 4 & 0x0fff0000u);  // three bits to four
+        x = (x & 0x003f003fu) | (x << 2 & 0x3f003f00u);
+        x = (x & 0x07070707u) | (x << 1 & 0x70707070u);
+        const unsigned n = ~x >> 2 & 0x11111111u;     // 1 where the digit is negative
+        a[j] = ((x & 0x33333333u) ^ (n * 3)) + n * 9;  // half the digit: 0 .. 3 stay, -1 .. -4 become 9 .. 12
+    }
+    // Eight words of an element's eight digits to eight words of eight elements' digit.
+    unsigned b[EACH];
 #pragma unroll
-        for (int j = 0; j < EACH; j++) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        if (FORMAT == HCCL_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const Step s = some_step<FORMAT>(top);
-        float quo[EACH], val[EACH];
+    for (int j = 0; j < 4; j++) b[j] = __byte_perm(a[j], a[j + 4], 0x5410), b[j + 4] = __byte_perm(a[j], a[j + 4], 0x7632);
 #pragma unroll
-        for (int j = 0; j < EACH; j++) quo[j] = v[j] * s.inv;
-        const unsigned code = eight_codes(quo);
-        eight_values(__shfl_sync(0xffffffffu, code, (int)threadIdx.x % 32), val);
+    for (int h = 0; h < 2; h++)
 #pragma unroll
-        for (int j = 0; j < EACH; j++) v[j] = fmaf(-val[j], s.d, v[j]);
-        put(q, code, s.byte);
+        for (int j = 0; j < 2; j++) a[4 * h + j] = __byte_perm(b[4 * h + j], b[4 * h + j + 2], 0x6240), a[4 * h + j + 2] = __byte_perm(b[4 * h + j], b[4 * h + j + 2], 0x7351);
+#pragma unroll
+    for (int h = 0; h < 4; h++) {  // a[2 h]: digits 2 h and 2 h + 1 of the even elements, a[2 h + 1]: of the odd ones
+        const unsigned even = a[2 * h], odd = a[2 * h + 1];
+        const int q = PIECES - 1 - 2 * h;  // the first piece is the highest digit
+        *(unsigned*)(codes + q * pitch + (sixteen ^ (q & swizzle)) * 16) = (even & 0x0f0f0f0fu) | (odd << 4 & 0xf0f0f0f0u);
+        *(unsigned*)(codes + (q - 1) * pitch + (sixteen ^ ((q - 1) & swizzle)) * 16) = (even >> 4 & 0x0f0f0f0fu) | (odd & 0xf0f0f0f0u);
     }
 }
 // The eight columns of a row's pieces, as the products come out, to one sum: the smallest first.
-template <int FORMAT> __device__ __forceinline__ float sum_of_pieces(const float (&v)[8]) {
-    float s = ((v[7] + v[6]) + v[5]) + v[4];
-    if (FORMAT == HCCL_NVFP4) s *= 1.f / LATER;
+__device__ __forceinline__ float sum_of_pieces(const float (&v)[8]) {
+    float s = (((v[7] + v[6]) + v[5]) + v[4]) * (1.f / LATER);
 #pragma unroll
     for (int i = 3; i >= 0; i--) s += v[i];
     return s;
@@ -234,6 +225,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     using S = Shape<FORMAT>;
     extern __shared__ char dynamic[];
     __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 8];
+    __shared__ __align__(16) unsigned scale_atom[ATOM / 4];  // of the pieces: the same for all blocks
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up, completed;
     __shared__ int chunk_total, table[OWN];
@@ -260,11 +252,15 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x < 2 * ROWS) top_of[threadIdx.x / ROWS][threadIdx.x % ROWS] = 0;
+    if (threadIdx.x < 128) {
+        scale_atom[atom_row((int)threadIdx.x) / 4] = piece_scale<FORMAT>((int)threadIdx.x % PIECES);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(COLS));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
-    const int blocks = (int)gridDim.x;
+    constexpr int blocks = SMS;
     if (warp == 3) {
         // Chunks of a block's run: every chunk has the same number of units, so the run begins in chunk floor(chunks * block / blocks).
         const int n = min(p.rows, list_chunks(p, lane, [](int, int) {}));  // (never more than rows, if the offsets ascend)
@@ -346,17 +342,16 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     } else if (warp == 1) {
         const int steps = (p.K + 63) / 64;
         bool ok = true;
+        if (elected()) copy_scales(tmem + S::X_SCALES, smem_addr(scale_atom));
+        __syncwarp();
         for (Unit t = unit_at(u0); t.u < u1 && ok; advance(t), acc++) {
             const int n = stages_of(t.kc), first = stage_of(t.kc), b = acc & 1, half = turn & 1;
-            const uint32_t x_scales = tmem + S::X_SCALES + half * SPAN * 4 * S::ATOMS, pieces = base + S::RING + half * S::PART;
+            const uint32_t pieces = base + S::RING + half * S::PART;
             const uint32_t desc = instruction(t.c.rows, FORMAT);
             if (begins(t)) {
                 ok = mbar_wait(part_full(half), (turn >> 1) & 1, &gave_up);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (elected())
-                    for (int i = 0; i < n * S::ATOMS; i++) copy_scales(x_scales + 4 * i, pieces + S::PIECE_SCALES + i * ATOM);
-                __syncwarp();
             }
             ok = mbar_wait(acc_empty(b), ((acc >> 1) & 1) ^ 1, &gave_up);
             if (!ok) break;
@@ -376,7 +371,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
                         if (k >= left) break;
                         const int a = k * S::ATOMS / 4;
                         const uint32_t two = FORMAT == HCCL_MXFP4 ? 2u * (k & 1) : 0u;
-                        mma_fp4<FORMAT>(tmem + b * TN, w + 2 * k, x + 2 * k, desc | (two << 4) | (two << 29), scales + 4 * a, x_scales + 4 * (i * S::ATOMS + a), (i > 0 || k > 0) ? 1u : 0u);
+                        mma_fp4<FORMAT>(tmem + b * TN, w + 2 * k, x + 2 * k, desc | (two << 4) | (two << 29), scales + 4 * a, tmem + S::X_SCALES, (i > 0 || k > 0) ? 1u : 0u);
                     }
                     mma_commit<1>(empty(s));
                     if (i == n - 1) {
@@ -406,7 +401,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
                 __syncwarp();
                 tmem_load8(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + r * PIECES, v);
                 tmem_arrived();
-                sums[r] = fmaf(sum_of_pieces<FORMAT>(v), unscale[half][r] * wide, bias);
+                sums[r] = fmaf(sum_of_pieces(v), unscale[half][r] * wide, bias);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -440,49 +435,34 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
                 float v[EACH];
                 const int from = p.source[t.c.row + r];
                 load8<T>((const T*)p.in + (long long)(from / p.top_k) * p.ldx, k, (unsigned)from < (unsigned)p.rows ? p.K : 0, p.vec, v);
-                if (FORMAT == HCCL_NVFP4) {  // the largest magnitude of each row's part of K
-                    unsigned top = 0;
+                unsigned top = 0;  // the largest magnitude of each row's part of K
 #pragma unroll
-                    for (int j = 0; j < EACH; j++) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-                    top = __reduce_max_sync(0xffffffffu, top);
-                    if (lane == 0) atomicMax(&top_of[half][r], top);
-                }
+                for (int j = 0; j < EACH; j++) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+                top = __reduce_max_sync(0xffffffffu, top);
+                if (lane == 0) atomicMax(&top_of[half][r], top);
                 held[2 * i * SPLITTERS + me] = make_float4(v[0], v[1], v[2], v[3]);
                 held[(2 * i + 1) * SPLITTERS + me] = make_float4(v[4], v[5], v[6], v[7]);
             }
             // (the buffers' last readers)
             ok = mbar_wait(part_empty(half), ((turn >> 1) & 1) ^ 1, &gave_up);
-            if (FORMAT == HCCL_NVFP4) ok = all_of(ok, 2, SPLITTERS);
+            ok = all_of(ok, 2, SPLITTERS);
             if (!ok) break;
 #pragma unroll 1
             for (int i = 0; i < TASKS; i++) {
                 const int r = row_of(i), k = k_of(i);
                 if (r >= t.c.rows) break;
-                float factor = 1.f, back = 1.f;
-                if (FORMAT == HCCL_NVFP4) row_factor(top_of[half][r], &factor, &back);
+                float factor, back;
+                row_factor(top_of[half][r], &factor, &back);
                 if (k == k0) unscale[half][r] = back;
-                const float4 a = held[2 * i * SPLITTERS + me], b = held[(2 * i + 1) * SPLITTERS + me];
-                float v[EACH] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                for (int j = 0; j < EACH; j++) v[j] *= factor;
-                const int kk = k - k0, stage = kk / 256, in_stage = kk % 256;
-                char* const codes = part + stage * S::PIECE_STAGE + in_stage % 32 / 2;
-                constexpr int B = block_of(FORMAT);
-                char* const scales = part + S::PIECE_SCALES + kk / (4 * B) * ATOM + kk / B % 4;
-                make_pieces<FORMAT>(v, [&](int q, unsigned code, unsigned byte) {
-                    const int n = r * PIECES + q;  // n % 8 = q
-                    *(unsigned*)(codes + n * KB + ((in_stage / 32 ^ q) * 16)) = code;
-                    if (kk % B == 0) scales[atom_row(n)] = (char)byte;
-                });
+                const int kk = k - k0, in_stage = kk % 256;
+                make_pieces(held[2 * i * SPLITTERS + me], held[(2 * i + 1) * SPLITTERS + me], factor, part + kk / 256 * S::PIECE_STAGE + r * PIECES * KB + in_stage % 32 / 2, KB, in_stage / 32, 7);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(part_full(half));
-            if (FORMAT == HCCL_NVFP4) {
-                // everyone has read the maxima: they start at zero when this half's turn comes again
-                asm volatile("bar.sync 2, 256;" ::: "memory");
-                if (me < ROWS) top_of[half][me] = 0;
-            }
+            // everyone has read the maxima: they start at zero when this half's turn comes again
+            asm volatile("bar.sync 2, 256;" ::: "memory");
+            if (me < ROWS) top_of[half][me] = 0;
         }
     }
     if (warp == 0 && lane == 0 && *(volatile int*)&gave_up) drain(full, S::STAGES, it, p.status);
@@ -507,68 +487,53 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
         const Chunk c = unpacked(table[chunk - own]);
         const int per_row = (min(WIDE, p.I - first) + 63) / 64 * 8;  // eights of a row, up to the end of the last instruction's 64 elements
         const int tasks = c.rows * per_row;
+        float4* const h = held;  // [task][two fours]
         if (threadIdx.x < ROWS) top_of[0][threadIdx.x] = 0;
         __syncthreads();
 #pragma unroll 1
-        for (int i = (int)threadIdx.x; i < tasks; i += UP_THREADS) {
-            const int r = i / per_row, k = first + i % per_row * EACH;
-            float v[EACH] = {}, o[EACH] = {};
+        for (int i = (int)threadIdx.x; i < 2 * tasks; i += UP_THREADS) {
+            const int r = i / (2 * per_row), k = first + (i - r * 2 * per_row) * 4;
+            float4 g = make_float4(0.f, 0.f, 0.f, 0.f), o = make_float4(1.f, 1.f, 1.f, 1.f);
             if (k < p.half) {
-                const float* from = p.sums + (long long)(c.row + r) * p.width + k;
-                const long long apart = (long long)filled * p.width;
-#pragma unroll 4
-                for (int kc = 0; kc < parts_of_k; kc++) {
-                    const float4* a = (const float4*)(from + kc * apart);
-                    const float4 a0 = __ldcg(a), a1 = __ldcg(a + 1);
-                    v[0] += a0.x, v[1] += a0.y, v[2] += a0.z, v[3] += a0.w, v[4] += a1.x, v[5] += a1.y, v[6] += a1.z, v[7] += a1.w;
-                    if (p.gated) {
-                        const float4 b0 = __ldcg(a + p.half / 4), b1 = __ldcg(a + p.half / 4 + 1);
-                        o[0] += b0.x, o[1] += b0.y, o[2] += b0.z, o[3] += b0.w, o[4] += b1.x, o[5] += b1.y, o[6] += b1.z, o[7] += b1.w;
-                    }
+                const float4* from = (const float4*)(p.sums + (long long)(c.row + r) * p.width + k);
+                const long long apart = (long long)filled * p.width / 4, other = p.gated ? p.half / 4 : 0;
+                g = __ldcg(from), o = __ldcg(from + other);
+#pragma unroll 2
+                for (int kc = 1; kc < parts_of_k; kc++) {
+                    const float4 x = __ldcg(from + kc * apart), y = __ldcg(from + kc * apart + other);
+                    g.x += x.x, g.y += x.y, g.z += x.z, g.w += x.w;
+                    o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
                 }
+                if (!p.gated) o = make_float4(1.f, 1.f, 1.f, 1.f);
             }
+            float v[4] = {g.x, g.y, g.z, g.w};
             if (p.act == HCCL_ACT_SILU)
 #pragma unroll
-                for (int j = 0; j < EACH; j++) v[j] = activation(HCCL_ACT_SILU, v[j]);
+                for (int j = 0; j < 4; j++) v[j] = activation(HCCL_ACT_SILU, v[j]);
             else if (p.act == HCCL_ACT_GELU)
 #pragma unroll
-                for (int j = 0; j < EACH; j++) v[j] = activation(HCCL_ACT_GELU, v[j]);
+                for (int j = 0; j < 4; j++) v[j] = activation(HCCL_ACT_GELU, v[j]);
             else
 #pragma unroll
-                for (int j = 0; j < EACH; j++) v[j] = activation(HCCL_ACT_RELU, v[j]);
+                for (int j = 0; j < 4; j++) v[j] = activation(HCCL_ACT_RELU, v[j]);
+            v[0] *= o.x, v[1] *= o.y, v[2] *= o.z, v[3] *= o.w;
             unsigned top = 0;
 #pragma unroll
-            for (int j = 0; j < EACH; j++) {
-                v[j] = k + j < p.I ? (p.gated ? v[j] * o[j] : v[j]) : 0.f;
+            for (int j = 0; j < 4; j++) {
+                if (k + j >= p.I) v[j] = 0.f;
                 top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
             }
-            if (FORMAT == HCCL_NVFP4 && top) atomicMax(&top_of[0][r], top);
-            held[i] = make_float4(v[0], v[1], v[2], v[3]), held[ROWS * WIDE / EACH + i] = make_float4(v[4], v[5], v[6], v[7]);
+            if (top) atomicMax(&top_of[0][r], top);
+            h[i] = make_float4(v[0], v[1], v[2], v[3]);
         }
         __syncthreads();
 #pragma unroll 1
-        for (int i0 = 0; i0 < tasks; i0 += UP_THREADS) {
-            // (lanes beyond the last task go along, for the shuffles)
-            const int i = i0 + (int)threadIdx.x, r = i / per_row, k = first + i % per_row * EACH;
-            const bool in = i < tasks;
-            float v[EACH] = {}, factor = 1.f, back = 1.f;
-            if (in) {
-                const float4 a = held[i], b = held[ROWS * WIDE / EACH + i];
-                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-                if (FORMAT == HCCL_NVFP4) row_factor(top_of[0][r], &factor, &back);
-                if (k == first) p.unscale[(long long)(c.row + r) * p.down_parts + part] = back;
-            }
-#pragma unroll
-            for (int j = 0; j < EACH; j++) v[j] *= factor;
-            constexpr int B = block_of(FORMAT);
-            uint8_t* const codes = p.pieces + (long long)(c.row + r) * PIECES * p.pitch + k / 2;
-            uint8_t* const scales = p.piece_scales + ((long long)chunk * p.down_blocks * S::ATOMS + k / (4 * B)) * ATOM + k / B % 4;
-            make_pieces<FORMAT>(v, [&](int q, unsigned code, unsigned byte) {
-                if (in) {
-                    *(unsigned*)(codes + q * p.pitch) = code;
-                    if (k % B == 0) scales[atom_row(r * PIECES + q)] = (uint8_t)byte;
-                }
-            });
+        for (int i = (int)threadIdx.x; i < tasks; i += UP_THREADS) {
+            const int r = i / per_row, k = first + (i - r * per_row) * EACH;
+            float factor, back;
+            row_factor(top_of[0][r], &factor, &back);
+            if (k == first) p.unscale[(long long)(c.row + r) * p.down_parts + part] = back;
+            make_pieces(h[2 * i], h[2 * i + 1], factor, (char*)p.pieces + (long long)(c.row + r) * PIECES * p.pitch + k / 2, p.pitch, 0, 0);
         }
         __syncthreads();
     }
@@ -587,6 +552,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
     using S = Shape<FORMAT>;
     extern __shared__ char dynamic[];
     __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 4];
+    __shared__ __align__(16) unsigned scale_atom[ATOM / 4];  // of the pieces: the same for all blocks
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up, completed, list[2];
     __shared__ int chunk_total, table[MAX_CHUNKS];
@@ -606,6 +572,10 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
         completed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (threadIdx.x < 128) {
+        scale_atom[atom_row((int)threadIdx.x) / 4] = piece_scale<FORMAT>((int)threadIdx.x % PIECES);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(COLS));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -621,7 +591,8 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
-    const int chunks = __shfl_sync(0xffffffffu, chunk_total, 0), blocks = (int)gridDim.x;
+    const int chunks = __shfl_sync(0xffffffffu, chunk_total, 0);
+    constexpr int blocks = SMS;
     const int of_tile = chunks * p.k_blocks;
     const long long total = (long long)of_tile * p.chan_tiles;
     const auto first_of = [&](int block) { return (int)(total * block / blocks); };
@@ -657,7 +628,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
     int it = 0, acc = 0;  // stages and segments passed
 
     if (warp == 0) {
-        const auto expect = [&](const Segment& t, int s) { mbar_expect(full(s), (uint32_t)(S::STAGE + t.c.rows * PIECES * KB + S::ATOMS * ATOM)); };
+        const auto expect = [&](const Segment& t, int s) { mbar_expect(full(s), (uint32_t)(S::STAGE + t.c.rows * PIECES * KB)); };
         const auto load_w = [&](const Segment& t, int s, int kb) {
             const uint32_t at = base + s * S::D_STAGE;
             tma_load<1>(at, &p.w, kb * KB, t.c.expert * p.N + t.tile * CH, full(s));
@@ -665,8 +636,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
         };
         const auto load_x = [&](const Segment& t, int s, int kb) {
             const uint32_t at = base + s * S::D_STAGE;
-            for (int r = 0; r < t.c.rows; r++) tma_load<1>(at + S::D_PIECES + r * PIECES * KB, &p.x, kb * KB, (t.c.row + r) * PIECES, full(s));
-            tma_load<1>(at + S::D_SCALES, &p.x_scale, 0, (t.chunk * p.k_blocks + kb) * S::ATOMS, full(s));
+            for (int r = 0; r < t.c.rows; r++) tma_load<1>(at + S::STAGE + r * PIECES * KB, &p.x, kb * KB, (t.c.row + r) * PIECES, full(s));
         };
         // The first stages' weights do not hang on the first kernel's results.
         const auto first = [&](const auto& each) {
@@ -701,6 +671,8 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
     } else if (warp == 1) {
         const int steps = (p.K + 63) / 64;
         bool ok = true;
+        if (elected()) copy_scales(tmem + S::X_SCALES, smem_addr(scale_atom));
+        __syncwarp();
         for (Segment t = first_segment(); t.g < g1 && ok; advance(t), acc++) {
             const int b = acc & 1;
             const uint32_t desc = instruction(t.c.rows, FORMAT);
@@ -712,17 +684,17 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
                 ok = mbar_wait(full(s), (it / S::STAGES) & 1, &gave_up);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t at = base + s * S::D_STAGE, w_scales = tmem + 2 * TN + s * 8 * S::ATOMS, x_scales = w_scales + 4 * S::ATOMS;
-                const uint64_t w = operand(at), x = operand(at + S::D_PIECES);
+                const uint32_t at = base + s * S::D_STAGE, scales = tmem + S::W_SCALES + s * 4 * S::ATOMS;
+                const uint64_t w = operand(at), x = operand(at + S::STAGE);
                 if (elected()) {
 #pragma unroll
-                    for (int a = 0; a < S::ATOMS; a++) copy_scales(w_scales + 4 * a, at + CH * KB + a * ATOM), copy_scales(x_scales + 4 * a, at + S::D_SCALES + a * ATOM);
+                    for (int a = 0; a < S::ATOMS; a++) copy_scales(scales + 4 * a, at + CH * KB + a * ATOM);
 #pragma unroll
                     for (int k = 0; k < 4; k++) {
                         if (k >= left) break;
                         const int a = k * S::ATOMS / 4;
                         const uint32_t two = FORMAT == HCCL_MXFP4 ? 2u * (k & 1) : 0u;
-                        mma_fp4<FORMAT>(tmem + b * TN, w + 2 * k, x + 2 * k, desc | (two << 4) | (two << 29), w_scales + 4 * a, x_scales + 4 * a, (kb > t.k0 || k > 0) ? 1u : 0u);
+                        mma_fp4<FORMAT>(tmem + b * TN, w + 2 * k, x + 2 * k, desc | (two << 4) | (two << 29), scales + 4 * a, tmem + S::X_SCALES, (kb > t.k0 || k > 0) ? 1u : 0u);
                     }
                     mma_commit<1>(empty(s));
                     if (kb == t.k1 - 1) mma_commit<1>(acc_full(b));
@@ -770,7 +742,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
                 tmem_load8(tmem + ((uint32_t)(quarter * 32) << 16) + b * TN + r * PIECES, v);
                 tmem_arrived();
                 const int to = __shfl_sync(0xffffffffu, row.token, r);
-                const float z = fmaf(sum_of_pieces<FORMAT>(v), __shfl_sync(0xffffffffu, row.back, r) * row.wide, row.bias), f = __shfl_sync(0xffffffffu, row.weight, r);
+                const float z = fmaf(sum_of_pieces(v), __shfl_sync(0xffffffffu, row.back, r) * row.wide, row.bias), f = __shfl_sync(0xffffffffu, row.weight, r);
                 if (to >= 0) sums[to * CH + me] = fmaf(f, z, sums[to * CH + me]);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -820,9 +792,9 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
         const auto block_of_stage = [&](long long g) { return (int)(((g + 1) * blocks - 1) / total); };
         const int from = block_of_stage((long long)tile * of_tile), to = block_of_stage((long long)(tile + 1) * of_tile - 1);
         float sum[4] = {};
-#pragma unroll 8
+#pragma unroll 4
         for (int b = from; b <= to; b++) {
-            const int lo = first_of(b), which = tile == lo / of_tile ? 0 : 1;
+            const int lo = first_of(b), which = lo >= tile * of_tile ? 0 : 1;
             const bool some = first_of(b + 1) > lo;  // (with fewer stages than blocks some have none)
             const float4 v = __ldcg((const float4*)(p.part + ((long long)(2 * b + which) * p.T + token) * CH) + lane);
             if (some) sum[0] += v.x, sum[1] += v.y, sum[2] += v.z, sum[3] += v.w;
@@ -845,9 +817,9 @@ long long partial_sums(long long rows, long long width, long long k_blocks) {
 }
 
 struct Places {  // in the scratch, in bytes
-    long long half, width, pitch, parts, counts, count_bytes, sums, unscale, pieces, scales, part, end;
+    long long half, width, pitch, parts, counts, count_bytes, sums, unscale, pieces, part, end;
 };
-Places places(long long T, long long rows, long long H, long long I, int gated, int format) {
+Places places(long long T, long long rows, long long H, long long I, int gated) {
     Places a;
     a.half = up_to(I, 8);
     a.width = (gated ? 2 : 1) * a.half;
@@ -864,7 +836,6 @@ Places places(long long T, long long rows, long long H, long long I, int gated, 
     a.sums = take(4 * partial_sums(rows, a.width, (H + 255) / 256));
     a.unscale = take(4 * rows * a.parts);
     a.pieces = take(rows * PIECES * a.pitch);
-    a.scales = take(rows * ((I + 255) / 256) * stage_atoms(format) * ATOM);
     a.part = take(4 * 2ll * SMS * T * CH);
     a.end = at;
     return a;
@@ -894,7 +865,7 @@ template <typename Kernel> cudaError_t launch(Kernel* kernel, std::atomic<bool>*
 template <typename T, int FORMAT> cudaError_t few(const FewFp4& q, cudaStream_t s) {
     using S = Shape<FORMAT>;
     const long long rows = q.T * q.top_k;
-    const Places at = places(q.T, rows, q.H, q.I, q.gated, FORMAT);
+    const Places at = places(q.T, rows, q.H, q.I, q.gated);
     FewParams p = {};
     p.offsets = q.offsets;
     p.source = q.source;
@@ -917,7 +888,6 @@ template <typename T, int FORMAT> cudaError_t few(const FewFp4& q, cudaStream_t 
     p.sums = (float*)(q.scratch + at.sums);
     p.unscale = (float*)(q.scratch + at.unscale);
     p.pieces = (uint8_t*)(q.scratch + at.pieces);
-    p.piece_scales = (uint8_t*)(q.scratch + at.scales);
     p.part = (float*)(q.scratch + at.part);
     cudaError_t e;
     const auto maps = [&](const uint8_t* w, const uint8_t* scale, long long ld, long long n, long long k, int halves) {
@@ -939,7 +909,6 @@ template <typename T, int FORMAT> cudaError_t few(const FewFp4& q, cudaStream_t 
     if ((e = launch(hccl_few_up<T, FORMAT>, up_ready, UP_THREADS, S::SMEM_UP, false, p, s)) != cudaSuccess) return e;
     if ((e = maps(q.down, q.down_scale, q.ld_down, q.H, q.I, 1)) != cudaSuccess) return e;
     if ((e = make_map(&p.x, p.pieces, rows * PIECES, at.pitch, at.pitch, PIECES)) != cudaSuccess) return e;
-    if ((e = make_atom_map(&p.x_scale, p.piece_scales, rows * p.k_blocks * S::ATOMS, S::ATOMS)) != cudaSuccess) return e;
     p.y = q.y;
     p.ldy = q.ldy;
     p.wide = q.down_wide;
@@ -949,7 +918,7 @@ template <typename T, int FORMAT> cudaError_t few(const FewFp4& q, cudaStream_t 
 
 }  // namespace
 
-size_t few_fp4_scratch(long long T, long long H, long long I, int top_k, int gated, int format) { return (size_t)places(T, T * top_k, H, I, gated, format).end; }
+size_t few_fp4_scratch(long long T, long long H, long long I, int top_k, int gated) { return (size_t)places(T, T * top_k, H, I, gated).end; }
 
 cudaError_t launch_few_fp4(int dt, const FewFp4& p, cudaStream_t s) {
     if (p.T == 0) return cudaSuccess;

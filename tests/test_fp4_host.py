@@ -133,7 +133,7 @@ def test_layer_refusals():
 @pytest.mark.parametrize("T,k,H,I,gated", [(1, 1, 64, 32, 1), (1, 8, 4096, 2048, 1), (64, 8, 4096, 2048, 1), (64, 32, 131072, 1000, 0), (3, 1, 131072, 131072, 1), (50, 2, 257, 129, 0), (64, 1, 1, 1, 1)])
 @pytest.mark.parametrize("fmt", [hb.NVFP4, hb.MXFP4])
 def test_layer_scratch_holds_every_cut_of_k(T, k, H, I, gated, fmt):
-    """The first kernel cuts K by the number of units; whatever number of chunks the rows make, the partial sums fit, and beside them the pieces with their scales
+    """The first kernel cuts K by the number of units; whatever number of chunks the rows make, the partial sums fit, and beside them the pieces
     and two tiles of partial results for each block."""
     blocks, rows, halves, k_blocks = 148, T * k, 2 if gated else 1, -(-H // 256)
     width, tiles, most = halves * (-(-I // 8) * 8), halves * -(-I // 128), 0
@@ -145,8 +145,7 @@ def test_layer_scratch_holds_every_cut_of_k(T, k, H, I, gated, fmt):
             while span > 1 and chunks * tiles * -(-k_blocks // span) < 6 * blocks:
                 span //= 2
             most = max(most, -(-k_blocks // span) * filled * width)
-    stages, atoms = -(-I // 256), 4 if fmt == hb.NVFP4 else 2
-    need = 4 * most + rows * 8 * stages * 128 + rows * stages * atoms * 512 + 2 * blocks * T * 128 * 4 + 4 * rows * -(-I // 1024) * 2 + 4 * -(-H // 128)
+    need = 4 * most + rows * 8 * -(-I // 256) * 128 + 2 * blocks * T * 128 * 4 + 4 * rows * -(-I // 1024) * 2 + 4 * -(-H // 128)
     assert need <= hb.hccl_expert_layer_scratch_bytes(experts(H=H, I=I, gated=gated, format=fmt, ld_up=1 << 17, ld_down=1 << 17), T, k)
 
 

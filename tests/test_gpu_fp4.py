@@ -312,11 +312,11 @@ def test_copies_have_addresses_of_their_own(how):
 
 # ------------------------------------------------------------------------------------------------ the layer for few tokens
 def layer_reference(x, ids, weights, up, down, act, gated, fmt, dt):
-    """y in 64 bits and a bound of the error: of the pieces (0.178^8 or 4^-8 of a row's largest element, for each weight), of the sums (2^-23 for each term), of the
+    """y in 64 bits and a bound of the error: of the pieces (2^-22 of a row's largest element, for each weight), of the sums (2^-23 for each term), of the
     activation (its slope; a few steps of its own), and the type's rounding."""
     wu, gu, bu = up
     wd, gd, bd = down
-    left = 0.178 ** 8 if fmt == "nvfp4" else 4.0 ** -8
+    left = 2.0 ** -22
     T, H = x.shape
     I = wd.shape[-1]
 

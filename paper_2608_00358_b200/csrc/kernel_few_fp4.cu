@@ -34,12 +34,12 @@ constexpr int ENOUGH = 6;  // units for each block, below which K is cut finer
 constexpr int EACH = 8;  // elements of a thread that makes pieces
 static_assert(ROWS * WIDE % EACH == 0, "");
 constexpr int UP_THREADS = 512, SPLIT_WARPS = 8, SPLITTERS = 32 * SPLIT_WARPS, TASKS = ROWS * SPAN * 256 / EACH / SPLITTERS;
-constexpr int DOWN_THREADS = 256;
+constexpr int DOWN_THREADS = 512;  // 8 warps at work, all of them in the last sums
 constexpr int MAX_CHUNKS = HCCL_MAX_FEW_TOKENS * HCCL_MAX_TOP_K, OWN = (MAX_CHUNKS + SMS - 1) / SMS + 2;  // chunks in all, and in one block's run of the first kernel
 
 template <int FORMAT> struct Shape {
     static constexpr int ATOMS = stage_atoms(FORMAT);
-    static constexpr int STAGES = 6;
+    static constexpr int STAGES = 7;
     // up: the ring of weights, two parts' pieces, and elements between their row's maximum and their pieces
     static constexpr int STAGE = CH * KB + ATOMS * ATOM;
     static constexpr int PIECE_STAGE = TN * KB, PART = SPAN * PIECE_STAGE;
@@ -165,6 +165,8 @@ __device__ __noinline__ void make_pieces(float4 lo, float4 hi, float factor, cha
         *(unsigned*)(codes + (q - 1) * pitch + (sixteen ^ ((q - 1) & swizzle)) * 16) = (even >> 4 & 0x0f0f0f0fu) | (odd & 0xf0f0f0f0u);
     }
 }
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m)); }
 // The eight columns of a row's pieces, as the products come out, to one sum: the smallest first.
 __device__ __forceinline__ float sum_of_pieces(const float (&v)[8]) {
     float s = (((v[7] + v[6]) + v[5]) + v[4]) * (1.f / LATER);
@@ -176,6 +178,7 @@ __device__ __forceinline__ float sum_of_pieces(const float (&v)[8]) {
 struct Chunk {
     int expert, row, rows;  // rows [row, row + rows) in expert order
 };
+static_assert(OWN <= 32, "a lane each");
 static_assert(HCCL_MAX_EXPERTS <= 1 << 11 && HCCL_MAX_FEW_TOKENS * HCCL_MAX_TOP_K <= 1 << 12 && ROWS < 1 << 4, "packed");
 __device__ __forceinline__ int packed(int expert, int row, int rows) { return expert << 16 | row << 4 | rows; }
 __device__ __forceinline__ Chunk unpacked(int c) {
@@ -212,6 +215,32 @@ template <typename Full> __device__ __forceinline__ void drain(const Full& full,
     if (status) *status = HCCL_ERR_TIMEOUT;
 }
 
+// Four elements of act(gate) * other from partial sums, `apart` fours apart; other: how far the other half is, 0: no gate. A function, so that a warp with nothing else
+// to do can fetch its code ahead of time: on the few blocks that finish others' sums that was half of what it took.
+__device__ __noinline__ float4 activated(const float4* from, long long apart, int other, int parts, int act) {
+    float4 g = make_float4(0.f, 0.f, 0.f, 0.f), o = g;
+    if (from)
+#pragma unroll 1
+        for (int kc = 0; kc < parts; kc += 4) {
+            float4 x[4], y[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                x[i] = y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (kc + i < parts) x[i] = __ldcg(from + (kc + i) * apart), y[i] = __ldcg(from + (kc + i) * apart + other);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                g.x += x[i].x, g.y += x[i].y, g.z += x[i].z, g.w += x[i].w;
+                o.x += y[i].x, o.y += y[i].y, o.z += y[i].z, o.w += y[i].w;
+            }
+        }
+    if (!other) o = make_float4(1.f, 1.f, 1.f, 1.f);
+    if (act == HCCL_ACT_SILU) g.x = activation(HCCL_ACT_SILU, g.x), g.y = activation(HCCL_ACT_SILU, g.y), g.z = activation(HCCL_ACT_SILU, g.z), g.w = activation(HCCL_ACT_SILU, g.w);
+    else if (act == HCCL_ACT_GELU) g.x = activation(HCCL_ACT_GELU, g.x), g.y = activation(HCCL_ACT_GELU, g.y), g.z = activation(HCCL_ACT_GELU, g.z), g.w = activation(HCCL_ACT_GELU, g.w);
+    else g.x = activation(HCCL_ACT_RELU, g.x), g.y = activation(HCCL_ACT_RELU, g.y), g.z = activation(HCCL_ACT_RELU, g.z), g.w = activation(HCCL_ACT_RELU, g.w);
+    return make_float4(g.x * o.x, g.y * o.y, g.z * o.z, g.w * o.w);
+}
+
 // ---------------------------------------------------------------- first product, activation, pieces
 // Where a block is in its run of units. index: among the `of` units with the same chunk, part and kc.
 struct Unit {
@@ -231,6 +260,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     __shared__ int chunk_total, table[OWN];
     __shared__ float unscale[2][ROWS];
     __shared__ unsigned top_of[2][ROWS];
+    __shared__ int job_row[ROWS], job_part[ROWS];
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t base = (smem_addr(dynamic) + 1023) & ~1023u;
     char* const parts = dynamic + (base - smem_addr(dynamic)) + S::RING;
@@ -243,6 +273,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     const auto part_full = [&](int b) { return bar0 + 8 * (2 * S::STAGES + 4 + b); };
     const auto part_empty = [&](int b) { return bar0 + 8 * (2 * S::STAGES + 6 + b); };
 
+    if (threadIdx.x == 32) prefetch_map(&p.w), prefetch_map(&p.w_scale);
     asm volatile("griddepcontrol.launch_dependents;");  // the second kernel's blocks may start to fetch weights as this one's leave
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
@@ -261,13 +292,25 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     constexpr int blocks = SMS;
+    if (warp >= 8) {
+        // While the chunks are listed: what comes first from memory is asked for, a share by each block, and the code that makes pieces is fetched by running it.
+        const long long row = (long long)p.K * sizeof(T), bytes = row * p.T;
+        for (long long i = ((long long)blockIdx.x * SPLITTERS + threadIdx.x - 256) * 128; i < bytes; i += (long long)blocks * SPLITTERS * 128) {
+            const long long t = i / row;
+            prefetch((const char*)p.in + t * p.ldx * sizeof(T) + (i - t * row));
+        }
+        if (blockIdx.x * SPLITTERS + threadIdx.x - 256 < p.rows) prefetch(p.source + (blockIdx.x * SPLITTERS + threadIdx.x - 256));
+        make_pieces(make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f), 0.f, (char*)(held + threadIdx.x - 256), SPLITTERS * 16, 0, 0);
+    }
     if (warp == 3) {
         // Chunks of a block's run: every chunk has the same number of units, so the run begins in chunk floor(chunks * block / blocks).
-        const int n = min(p.rows, list_chunks(p, lane, [](int, int) {}));  // (never more than rows, if the offsets ascend)
+        int* const all = (int*)parts;  // (free until the first pieces)
+        const int n = min(p.rows, list_chunks(p, lane, [&](int chunk, int c) {
+            if (chunk < p.rows) all[chunk] = c;  // (never more than rows, if the offsets ascend)
+        }));
+        __syncwarp();
         const int own = (int)((long long)n * blockIdx.x / blocks);
-        list_chunks(p, lane, [&](int chunk, int c) {
-            if (chunk >= own && chunk < own + OWN) table[chunk - own] = c;
-        });
+        if (lane < OWN && own + lane < n) table[lane] = all[own + lane];
         if (lane == 0) chunk_total = n;
     }
     __syncwarp();
@@ -465,6 +508,10 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
             if (me < ROWS) top_of[half][me] = 0;
         }
     }
+    else if (warp == 3) {
+        const float4 x = activated((const float4*)p.sums, 0, 1, 1, p.act);  // (whatever lies there)
+        if (__float_as_int(x.x) == 0x7fc12345) held[lane] = x;               // (so that it is run: no sum has these bits)
+    }
     if (warp == 0 && lane == 0 && *(volatile int*)&gave_up) drain(full, S::STAGES, it, p.status);
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -482,58 +529,49 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     }
     __threadfence();
     __syncthreads();
-    for (int l = 0; l < completed; l++) {
-        const int chunk = list[l] / p.down_parts, part = list[l] % p.down_parts, first = part * WIDE;
-        const Chunk c = unpacked(table[chunk - own]);
-        const int per_row = (min(WIDE, p.I - first) + 63) / 64 * 8;  // eights of a row, up to the end of the last instruction's 64 elements
-        const int tasks = c.rows * per_row;
-        float4* const h = held;  // [task][two fours]
-        if (threadIdx.x < ROWS) top_of[0][threadIdx.x] = 0;
+    // As many of them at once as have ROWS rows together: a row's 1024 columns are a job for 128 threads' eights.
+    float4* const h = held;  // [job][four columns]
+    for (int l = 0; l < completed;) {
+        int jobs = 0;
+        for (; l < completed; l++) {  // (all threads the same; one of them writes it down)
+            const int chunk = list[l] / p.down_parts, part = list[l] - chunk * p.down_parts;
+            const Chunk c = unpacked(table[chunk - own]);
+            if (jobs + c.rows > ROWS) break;
+            for (int r = 0; r < c.rows; r++, jobs++)
+                if (threadIdx.x == 0) job_row[jobs] = c.row + r, job_part[jobs] = part, top_of[0][jobs] = 0;
+        }
         __syncthreads();
+        const auto columns = [&](int job, int* first) {  // up to the end of the last instruction's 64 elements
+            *first = job_part[job] * WIDE;
+            return (min(WIDE, p.I - *first) + 63) & ~63;
+        };
 #pragma unroll 1
-        for (int i = (int)threadIdx.x; i < 2 * tasks; i += UP_THREADS) {
-            const int r = i / (2 * per_row), k = first + (i - r * 2 * per_row) * 4;
-            float4 g = make_float4(0.f, 0.f, 0.f, 0.f), o = make_float4(1.f, 1.f, 1.f, 1.f);
-            if (k < p.half) {
-                const float4* from = (const float4*)(p.sums + (long long)(c.row + r) * p.width + k);
-                const long long apart = (long long)filled * p.width / 4, other = p.gated ? p.half / 4 : 0;
-                g = __ldcg(from), o = __ldcg(from + other);
-#pragma unroll 2
-                for (int kc = 1; kc < parts_of_k; kc++) {
-                    const float4 x = __ldcg(from + kc * apart), y = __ldcg(from + kc * apart + other);
-                    g.x += x.x, g.y += x.y, g.z += x.z, g.w += x.w;
-                    o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
-                }
-                if (!p.gated) o = make_float4(1.f, 1.f, 1.f, 1.f);
-            }
-            float v[4] = {g.x, g.y, g.z, g.w};
-            if (p.act == HCCL_ACT_SILU)
-#pragma unroll
-                for (int j = 0; j < 4; j++) v[j] = activation(HCCL_ACT_SILU, v[j]);
-            else if (p.act == HCCL_ACT_GELU)
-#pragma unroll
-                for (int j = 0; j < 4; j++) v[j] = activation(HCCL_ACT_GELU, v[j]);
-            else
-#pragma unroll
-                for (int j = 0; j < 4; j++) v[j] = activation(HCCL_ACT_RELU, v[j]);
-            v[0] *= o.x, v[1] *= o.y, v[2] *= o.z, v[3] *= o.w;
+        for (int i = (int)threadIdx.x; i < jobs * (WIDE / 4); i += UP_THREADS) {
+            int first;
+            const int job = i / (WIDE / 4), col = i % (WIDE / 4) * 4;
+            if (col >= columns(job, &first)) continue;
+            const int k = first + col;
+            const float4 x = activated(k < p.half ? (const float4*)(p.sums + (long long)job_row[job] * p.width + k) : nullptr, (long long)filled * p.width / 4, p.gated ? p.half / 4 : 0, parts_of_k, p.act);
+            float v[4] = {x.x, x.y, x.z, x.w};
             unsigned top = 0;
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 if (k + j >= p.I) v[j] = 0.f;
                 top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
             }
-            if (top) atomicMax(&top_of[0][r], top);
+            if (top) atomicMax(&top_of[0][job], top);
             h[i] = make_float4(v[0], v[1], v[2], v[3]);
         }
         __syncthreads();
 #pragma unroll 1
-        for (int i = (int)threadIdx.x; i < tasks; i += UP_THREADS) {
-            const int r = i / per_row, k = first + (i - r * per_row) * EACH;
+        for (int i = (int)threadIdx.x; i < jobs * (WIDE / EACH); i += UP_THREADS) {
+            int first;
+            const int job = i / (WIDE / EACH), col = i % (WIDE / EACH) * EACH;
+            if (col >= columns(job, &first)) continue;
             float factor, back;
-            row_factor(top_of[0][r], &factor, &back);
-            if (k == first) p.unscale[(long long)(c.row + r) * p.down_parts + part] = back;
-            make_pieces(h[2 * i], h[2 * i + 1], factor, (char*)p.pieces + (long long)(c.row + r) * PIECES * p.pitch + k / 2, p.pitch, 0, 0);
+            row_factor(top_of[0][job], &factor, &back);
+            if (col == 0) p.unscale[(long long)job_row[job] * p.down_parts + job_part[job]] = back;
+            make_pieces(h[2 * i], h[2 * i + 1], factor, (char*)p.pieces + (long long)job_row[job] * PIECES * p.pitch + (first + col) / 2, p.pitch, 0, 0);
         }
         __syncthreads();
     }
@@ -546,7 +584,7 @@ struct Segment {
     int g, g1, chunk, tile, k0, k1;  // stages of K
 };
 
-// Roles (8 warps): warp 0 loads weights and pieces, warp 1 copies scales to tensor memory and issues the products, warp 2 owns the tensor memory, warp 3 lists the chunks, warps 4-7 take
+// Roles (the first 8 of 16 warps): warp 0 loads weights and pieces, warp 1 copies scales to tensor memory and issues the products, warp 2 owns the tensor memory, warp 3 lists the chunks, warps 4-7 take
 // the sums out.
 template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS, 1) hccl_few_down(const __grid_constant__ FewParams p) {
     using S = Shape<FORMAT>;
@@ -565,6 +603,9 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
     const auto acc_full = [&](int b) { return bar0 + 8 * (2 * S::STAGES + b); };
     const auto acc_empty = [&](int b) { return bar0 + 8 * (2 * S::STAGES + 2 + b); };
 
+    if (threadIdx.x == 32) prefetch_map(&p.w), prefetch_map(&p.w_scale), prefetch_map(&p.x);
+    if (threadIdx.x >= 128 && threadIdx.x < 256)  // what the sums are weighted with, a share by each block
+        for (int i = (int)(blockIdx.x * 128 + threadIdx.x - 128); i < p.rows; i += SMS * 128) prefetch(p.source + i), prefetch(p.weights + i);
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
         for (int b = 0; b < 2; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 4);
@@ -702,7 +743,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
                 __syncwarp();
             }
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && warp < 8) {
         const int quarter = warp & 3, me = quarter * 32 + lane;
         asm volatile("griddepcontrol.wait;" ::: "memory");
         for (int t = 0; t < p.T; t++) sums[t * CH + me] = 0.f;
@@ -792,7 +833,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
         const auto block_of_stage = [&](long long g) { return (int)(((g + 1) * blocks - 1) / total); };
         const int from = block_of_stage((long long)tile * of_tile), to = block_of_stage((long long)(tile + 1) * of_tile - 1);
         float sum[4] = {};
-#pragma unroll 4
+#pragma unroll 8
         for (int b = from; b <= to; b++) {
             const int lo = first_of(b), which = lo >= tile * of_tile ? 0 : 1;
             const bool some = first_of(b + 1) > lo;  // (with fewer stages than blocks some have none)

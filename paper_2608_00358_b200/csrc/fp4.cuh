@@ -65,16 +65,22 @@ __device__ __forceinline__ unsigned eight_codes(const float* q) {
         : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
     return r;
 }
-// Of a word from memory or from another lane: straight behind eight_codes, in registers, the compiler (12.9) gets the bytes wrong.
+// Eight codes to their values. A byte permutation looks four of them up: the upper byte of a magnitude as a 16-bit number is all that it has; its sign comes from a
+// permutation of negative bytes, which a selector's fourth bit turns to ones. (The conversion instruction, given bytes of a register, was compiled wrongly in some places.)
 __device__ __forceinline__ void eight_values(unsigned w, float* v) {
-    unsigned h[4];
-    asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"
-        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
-        : "r"(w));
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const float2 f = __half22float2(*(const __half2*)&h[i]);
-        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    for (int h = 0; h < 2; h++) {
+        const unsigned x = h ? w >> 16 : w;
+        const unsigned four = __byte_perm(0x3e3c3800u, 0x46444240u, x & 0x7777u);  // 0, 0.5, 1, 1.5, 2, 3, 4, 6
+        unsigned sign;
+        asm("prmt.b32 %0, %1, %1, %2;" : "=r"(sign) : "r"(0x80808080u), "r"(x));  // 0xff where the code is negative, 0x80 elsewhere
+        const unsigned signed_four = four | (sign << 1 & 0x80808080u);
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const unsigned two = __byte_perm(signed_four, 0u, i ? 0x3424 : 0x1404);
+            const float2 f = __half22float2(*(const __half2*)&two);
+            v[4 * h + 2 * i] = f.x, v[4 * h + 2 * i + 1] = f.y;
+        }
     }
 }
 // The step that a stored byte stands for.
@@ -97,7 +103,7 @@ struct Fp4Rows {       // quantiser
     long long lds;
     int tn, atoms;     // tokens of a tile; atoms of a row of tiles' blocks, up to whole stages
     float wide, six;
-    int vec, vec_q;
+    int vec_q;
     const int* slots;  // null: row m of x to row m of q
     int top_k;
     const int* offsets;  // of the groups, where the scales go to tiles; null: one group
@@ -110,7 +116,6 @@ struct Fp4Values {     // the way back
     long long ldq, lds, M, K, ldy;
     void* y;
     float wide;
-    int vec;
 };
 cudaError_t launch_dequantise_fp4(int dt, int format, const Fp4Values& p, cudaStream_t s);
 

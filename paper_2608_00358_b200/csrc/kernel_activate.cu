@@ -16,68 +16,112 @@ constexpr int THREADS = 256;
 struct Words {
     unsigned w[4];
 };
-__device__ __forceinline__ Words philox(unsigned long long counter, unsigned long long call, unsigned long long key) {
-    unsigned c0 = (unsigned)counter, c1 = (unsigned)(counter >> 32), c2 = (unsigned)call, c3 = (unsigned)(call >> 32), k0 = (unsigned)key, k1 = (unsigned)(key >> 32);
+// A call's generator. The keys of the ten rounds, and of the first two rounds what hangs on the call and on the counter's upper half alone, are formed once.
+struct Generator {
+    unsigned k[10][2], upper, c0, c1;
+    unsigned long long a, call;
+    __device__ __forceinline__ Generator(unsigned long long key, unsigned long long call) : call(call) {
 #pragma unroll
-    for (int r = 0; r < 10; r++) {
-        const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
-        c0 = (unsigned)(b >> 32) ^ c1 ^ k0;
-        c1 = (unsigned)b;
-        c2 = (unsigned)(a >> 32) ^ c3 ^ k1;
-        c3 = (unsigned)a;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
+        for (int r = 0; r < 10; r++) k[r][0] = (unsigned)key + r * 0x9E3779B9u, k[r][1] = (unsigned)(key >> 32) + r * 0xBB67AE85u;
+        set(0);
     }
-    return {{c0, c1, c2, c3}};
-}
+    __device__ __forceinline__ void set(unsigned u) {
+        const unsigned long long b = (unsigned long long)(unsigned)call * 0xCD9E8D57u;
+        upper = u;
+        c0 = (unsigned)(b >> 32) ^ upper ^ k[0][0];
+        c1 = (unsigned)b;
+        a = (unsigned long long)c0 * 0xD2511F53u;
+    }
+    __device__ __forceinline__ Words at(unsigned long long counter) {
+        if ((unsigned)(counter >> 32) != upper) set((unsigned)(counter >> 32));
+        const unsigned long long first = (unsigned long long)(unsigned)counter * 0xD2511F53u;
+        const unsigned d2 = (unsigned)(first >> 32) ^ (unsigned)(call >> 32) ^ k[0][1], d3 = (unsigned)first;
+        const unsigned long long second = (unsigned long long)d2 * 0xCD9E8D57u;
+        unsigned x0 = (unsigned)(second >> 32) ^ c1 ^ k[1][0], x1 = (unsigned)second, x2 = (unsigned)(a >> 32) ^ d3 ^ k[1][1], x3 = (unsigned)a;
+#pragma unroll
+        for (int r = 2; r < 10; r++) {
+            const unsigned long long m = (unsigned long long)x0 * 0xD2511F53u, q = (unsigned long long)x2 * 0xCD9E8D57u;
+            x0 = (unsigned)(q >> 32) ^ x1 ^ k[r][0];
+            x1 = (unsigned)q;
+            x2 = (unsigned)(m >> 32) ^ x3 ^ k[r][1];
+            x3 = (unsigned)m;
+        }
+        return {{x0, x1, x2, x3}};
+    }
+};
 
-// The factors that dropout multiplies N neighbouring elements with, N a multiple of 4, the first being element `at` of the result. A counter's words begin within the
-// elements where I is odd.
-template <int N> __device__ __forceinline__ void factors(const ActivateParams& p, unsigned long long key, unsigned long long call, unsigned long long at, float (&f)[N]) {
+// The random words of N neighbouring elements, N a multiple of 4, the first being element `at` of the result. A counter's words begin within the
+// elements where I is no multiple of 4.
+template <int N> __device__ __forceinline__ void words(Generator& gen, unsigned long long at, unsigned (&f)[N]) {
     const unsigned o = (unsigned)at & 3u;
     if (o == 0) {
 #pragma unroll
         for (int j = 0; j < N; j += 4) {
-            const Words w = philox(at / 4 + j / 4, call, key);
+            const Words w = gen.at(at / 4 + j / 4);
 #pragma unroll
-            for (int i = 0; i < 4; i++) f[j + i] = w.w[i] >= p.threshold ? p.keep : 0.f;
+            for (int i = 0; i < 4; i++) f[j + i] = w.w[i];
         }
     } else {
-        Words w = philox(at / 4, call, key);
+        Words w = gen.at(at / 4);
 #pragma unroll
         for (int j = 0; j < N; j += 4) {
-            const Words next = philox(at / 4 + j / 4 + 1, call, key);
+            const Words next = gen.at(at / 4 + j / 4 + 1);
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const unsigned v = i + o == 1 ? w.w[1] : i + o == 2 ? w.w[2] : i + o == 3 ? w.w[3] : i + o == 4 ? next.w[0] : i + o == 5 ? next.w[1] : next.w[2];
-                f[j + i] = v >= p.threshold ? p.keep : 0.f;
-            }
+            for (int i = 0; i < 4; i++) f[j + i] = i + o == 1 ? w.w[1] : i + o == 2 ? w.w[2] : i + o == 3 ? w.w[3] : i + o == 4 ? next.w[0] : i + o == 5 ? next.w[1] : next.w[2];
             w = next;
         }
     }
 }
 
-// N elements, V at a time; from `left` on nothing is read (0) or written.
-template <typename T, int N, int V> __device__ __forceinline__ void load(const T* x, int left, float (&v)[N]) {
-#pragma unroll
-    for (int u = 0; u < N / V; u++) {
-        float part[V];
-        if (V == N || u * V < left) {
-            if constexpr (V == 1) {
-                part[0] = to_f32<T>(x[u]);
-            } else {
-                Pack<T, V> q;
-                q.raw = *(const typename Piece<V * sizeof(T)>::type*)(x + u * V);
-                q.get(part);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; j++) part[j] = 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < V; j++) v[u * V + j] = part[j];
-    }
+// Two numbers at a time: one instruction multiplies both.
+struct Two {
+    unsigned long long v;
+    __device__ __forceinline__ Two() {}
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
+    __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
 }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+// 4 / (1 + exp(-x)) for results of 16 bits, as logistic<true>.
+__device__ __forceinline__ Two four_logistic(Two x) {
+    float a, b;
+    (x * Two(-1.44269504f)).get(a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    fma2(Two(a, b), Two(0.25f), Two(0.25f)).get(a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return Two(a, b);
+}
+
+// N elements as they lie in memory, V to an access; from `left` on nothing is read.
+template <typename T, int N, int V> struct Raw {
+    Pack<T, V> q[N / V];
+    __device__ __forceinline__ void load(const T* x, int left) {
+#pragma unroll
+        for (int u = 0; u < N / V; u++)
+            if (V == N || u * V < left) q[u].raw = *(const typename Piece<V * sizeof(T)>::type*)(x + u * V);
+    }
+    __device__ __forceinline__ void get(float (&v)[N]) const {
+#pragma unroll
+        for (int u = 0; u < N / V; u++) {
+            float part[V];
+            q[u].get(part);
+#pragma unroll
+            for (int j = 0; j < V; j++) v[u * V + j] = part[j];
+        }
+    }
+};
+// The first `left` of them to memory.
 template <typename T, int N, int V> __device__ __forceinline__ void store(T* y, int left, const float (&v)[N]) {
 #pragma unroll
     for (int u = 0; u < N / V; u++) {
@@ -97,57 +141,115 @@ template <typename T, int N, int V> __device__ __forceinline__ void store(T* y, 
 }
 
 // A thread holds N elements of a row, V of them to an access (V < N: rows that do not start on 16 bytes or hold no whole pieces). `team` threads side by side walk a row.
+// Where a piece is one access, RING pieces of each thread are on their way into shared memory, where it alone reads them: what the generator keeps busy cannot also keep enough loads in flight.
 // Rows from the last expert's end on are set to zero, and not read.
+constexpr int RING = 4;
 template <typename T, int N, int V, bool GRAD, int ACT> __global__ void __launch_bounds__(THREADS) hccl_activate_rows(const __grid_constant__ ActivateParams p, int team) {
+    constexpr bool SHORT = sizeof(T) == 2, RINGED = V == N;
+    constexpr int INPUTS = GRAD ? 3 : 2;
+    extern __shared__ __align__(16) uint4 ring[];  // [RING][INPUTS][threads]
     const int teams = THREADS / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team;
     const long long rows = p.offsets ? min((long long)p.offsets[p.groups], p.M) : p.M;
-    unsigned long long key = 0, call = 0;
-    if (p.drop) key = (unsigned long long)p.seed[0], call = (unsigned long long)p.seed[1];
-    for (long long r = (long long)blockIdx.x * teams + mine; r < p.M; r += (long long)gridDim.x * teams) {
-        const T* x = (const T*)p.x + r * p.ldx;
-        const T* dy = (const T*)p.dy + r * p.ldy;
-        T* out = (T*)p.out + r * p.ldo;
+    // A thread has `n` pieces of each of its rows.
+    const long long step = (long long)gridDim.x * teams, across = (long long)team * N, c0 = (long long)rank * N;
+    if (c0 >= p.I) return;
+    Generator generator(p.drop ? (unsigned long long)p.seed[0] : 0, p.drop ? (unsigned long long)p.seed[1] : 0);
+    const int n = (int)((p.I - c0 + across - 1) / across);
+    const auto left_of = [&](long long c) { return RINGED ? N : (int)min((long long)N, p.I - c); };
+    Raw<T, N, V> raw[INPUTS] = {};  // gate, other half, gradient
+
+    // Where the loads are (ringed: ahead of the work).
+    long long fr = (long long)blockIdx.x * teams + mine;
+    int fk = 0, turn = 0;
+    const auto fetch = [&](int slot) {
+        if (fr < rows) {
+            const long long c = c0 + fk * across;
+            const T* const at[3] = {(const T*)p.x + fr * p.ldx + c, (const T*)p.x + fr * p.ldx + p.I + c, (const T*)p.dy + fr * p.ldy + c};
+#pragma unroll
+            for (int i = 0; i < INPUTS; i++) {
+                if (i == 1 && !p.gated) continue;
+                if constexpr (RINGED)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(ring + (slot * INPUTS + i) * THREADS + threadIdx.x)), "l"(at[i]) : "memory");
+                else
+                    raw[i].load(at[i], left_of(c));
+            }
+        }
+        if (RINGED) asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++fk == n) fk = 0, fr += step;
+    };
+    if (RINGED)
+#pragma unroll
+        for (int i = 0; i < RING - 1; i++) fetch(i);
+    for (long long r = (long long)blockIdx.x * teams + mine; r < p.M; r += step) {
+        T* const out = (T*)p.out + r * p.ldo;
         const unsigned long long at = (unsigned long long)r * (unsigned long long)p.I;
-        for (long long c = (long long)rank * N; c < p.I; c += (long long)team * N) {
-            const int left = (int)min((long long)N, p.I - c);
-            float f[N], g[N], u[N], d[N];
+        for (int k = 0; k < n; k++) {
+            const long long c = c0 + k * across;
+            const int left = left_of(c);
+            fetch(turn == 0 ? RING - 1 : turn - 1);
+            if constexpr (RINGED) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
+#pragma unroll
+                for (int i = 0; i < INPUTS; i++) {
+                    const uint4 v = ring[(turn * INPUTS + i) * THREADS + threadIdx.x];
+                    raw[i].q[0].raw = v;
+                }
+                turn = turn == RING - 1 ? 0 : turn + 1;
+            }
+            float g[N], u[N], d[N];
+            unsigned word[N];
             if (r >= rows) {
 #pragma unroll
-                for (int j = 0; j < N; j++) f[j] = 0.f;
-                store<T, N, V>(out + c, left, f);
-                if (GRAD && p.gated) store<T, N, V>(out + p.I + c, left, f);
+                for (int j = 0; j < N; j++) g[j] = 0.f;
+                store<T, N, V>(out + c, left, g);
+                if (GRAD && p.gated) store<T, N, V>(out + p.I + c, left, g);
                 continue;
             }
-            load<T, N, V>(x + c, left, g);
-            if (p.gated) load<T, N, V>(x + p.I + c, left, u);
-            if (GRAD) load<T, N, V>(dy + c, left, d);
-            if (!p.gated)
-#pragma unroll
-                for (int j = 0; j < N; j++) u[j] = 1.f;
-            if (p.drop) factors<N>(p, key, call, at + (unsigned long long)c, f);
+            if (p.drop) words<N>(generator, at + (unsigned long long)c, word);
             else
 #pragma unroll
-                for (int j = 0; j < N; j++) f[j] = 1.f;
-            if constexpr (!GRAD) {
+                for (int j = 0; j < N; j++) word[j] = 0xffffffffu;
+            raw[0].get(g);
+            if (p.gated) raw[1].get(u);
+            else
 #pragma unroll
-                for (int j = 0; j < N; j++) {
-                    const float v = activation(ACT, g[j]) * u[j] * f[j];
-                    g[j] = f[j] == 0.f ? 0.f : v;  // (dropped is 0, whatever it was)
+                for (int j = 0; j < N; j++) u[j] = 1.f;
+            if constexpr (GRAD) raw[INPUTS - 1].get(d);
+            // (what is dropped is 0, whatever it was)
+            if constexpr (SHORT && ACT == HCCL_ACT_SILU) {
+#pragma unroll
+                for (int j = 0; j < N; j += 2) {
+                    const Two x(g[j], g[j + 1]), o(u[j], u[j + 1]), s = four_logistic(x);
+                    if constexpr (!GRAD) {
+                        (x * (o * Two(0.25f * p.keep)) * s).get(g[j], g[j + 1]);
+                    } else {
+                        const Two sig = s * Two(0.25f), act = x * sig, dd = Two(d[j], d[j + 1]) * Two(p.keep);
+                        const Two slope = fma2(act, fma2(sig, Two(-1.f), Two(1.f)), sig);
+                        (dd * o * slope).get(g[j], g[j + 1]);
+                        (dd * act).get(u[j], u[j + 1]);
+                    }
                 }
-                store<T, N, V>(out + c, left, g);
             } else {
 #pragma unroll
                 for (int j = 0; j < N; j++) {
-                    float a, slope;
-                    activation_slope(ACT, g[j], &a, &slope);
-                    const float dd = d[j] * f[j];
-                    const bool off = f[j] == 0.f;
-                    g[j] = off ? 0.f : dd * u[j] * slope;
-                    u[j] = off ? 0.f : dd * a;
+                    if constexpr (!GRAD) {
+                        g[j] = activation<SHORT>(ACT, g[j]) * (u[j] * p.keep);
+                    } else {
+                        float a, slope;
+                        activation_slope<SHORT>(ACT, g[j], &a, &slope);
+                        const float dd = d[j] * p.keep;
+                        g[j] = dd * u[j] * slope;
+                        u[j] = dd * a;
+                    }
                 }
-                store<T, N, V>(out + c, left, g);
-                if (p.gated) store<T, N, V>(out + p.I + c, left, u);
             }
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                g[j] = word[j] >= p.threshold ? g[j] : 0.f;
+                if (GRAD) u[j] = word[j] >= p.threshold ? u[j] : 0.f;
+            }
+            store<T, N, V>(out + c, left, g);
+            if (GRAD && p.gated) store<T, N, V>(out + p.I + c, left, u);
         }
     }
 }
@@ -156,8 +258,9 @@ template <typename T, int N, int V, bool GRAD, int ACT> cudaError_t launch(const
     const long long pieces = (p.I + N - 1) / N;
     int team = 32;
     while (team < THREADS && team < pieces) team *= 2;
+    // Two rounds of blocks where each forms keys first, eight without (32768 x 2048 bf16 without dropout: 64 us, with two 71; with dropout 105, with eight 109).
     const long long blocks = (p.M + THREADS / team - 1) / (THREADS / team);
-    hccl_activate_rows<T, N, V, GRAD, ACT><<<(unsigned)std::max(1ll, std::min(blocks, (long long)SMS * 8)), THREADS, 0, s>>>(p, team);
+    hccl_activate_rows<T, N, V, GRAD, ACT><<<(unsigned)std::max(1ll, std::min(blocks, (long long)SMS * (p.drop ? 8 : 32))), THREADS, V == N ? RING * (GRAD ? 3 : 2) * THREADS * 16 : 0, s>>>(p, team);
     return cudaGetLastError();
 }
 

@@ -25,113 +25,191 @@ __device__ __forceinline__ int group_of(const int* offsets, int groups, long lon
     return lo;
 }
 
-// `lanes` neighbouring lanes (8, 16 or 32) share a row; longer rows are walked in pieces of 512 elements by one warp each.
-template <typename T, int FORMAT> __global__ void __launch_bounds__(THREADS) hccl_quantise_fp4(const __grid_constant__ Fp4Rows p, int lanes, int pieces) {
-    constexpr int N = Sixteen<T>::N, PARTS = EACH / N;
+// Where a row goes: its codes, and its scales, by rows or in tiles. row < 0: nowhere.
+struct Place {
+    long long row, scale;
+};
+__device__ __forceinline__ Place place_of(const Fp4Rows& p, long long row) {
+    Place at = {row, -1};
+    if (row < 0 || row >= p.n_q) {
+        at.row = -1;
+    } else if (!p.tn) {
+        at.scale = row * p.lds;
+    } else {
+        const int g = group_of(p.offsets, p.groups, row);
+        if (g >= 0) {
+            const unsigned first = p.offsets ? (unsigned)max(0, p.offsets[g]) : 0u, r = (unsigned)row - first, tn = (unsigned)p.tn, in_tile = r & (tn - 1);  // (rows are counted in 32 bits there, tn is a power of two)
+            const long long tile = first / tn + g + r / tn;
+            at.scale = (tile * (tn > 128 ? tn / 128 : 1) + in_tile / 128) * p.atoms * ATOM + atom_row(in_tile % 128);
+        }
+    }
+    return at;
+}
+
+// A thread has 16 elements of a row at a time, `team` threads side by side (8 to 256) a row. WHOLE: rows start on 16 bytes. Otherwise a warp fetches its 512 elements one by one, lanes
+// side by side, and hands them round through shared memory (16 loads of a thread's own elements touch 32 lines each: 1999 x 2057 fp32 13 us in the place of NNN).
+template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_quantise_fp4(const __grid_constant__ Fp4Rows p, int team) {
+    constexpr int N = Sixteen<T>::N, PARTS = EACH / N, SHARE = FORMAT == HCCL_NVFP4 ? 1 : 2 /* threads to a block */;
+    extern __shared__ __align__(16) Place placed[];  // [2][teams * copies]
+    __shared__ float handed[WHOLE ? 1 : THREADS / 32][WHOLE ? 1 : 32 * 17];
     asm volatile("griddepcontrol.launch_dependents;");  // the product may start to fetch its weights
-    const int lane = threadIdx.x % 32, K = (int)p.K, per_warp = 32 / lanes, copies = p.slots ? p.top_k : 1;
-    const long long tasks = (p.M + per_warp - 1) / per_warp * pieces, step = (long long)gridDim.x * (THREADS / 32);
-    for (long long task = (long long)blockIdx.x * (THREADS / 32) + threadIdx.x / 32; task < tasks; task += step) {
-        const long long m = task / pieces * per_warp + lane / lanes;
-        const int k = ((int)(task % pieces) * lanes + lane % lanes) * EACH;
+    const int teams = THREADS / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team, lane = threadIdx.x % 32, K = (int)p.K, across = team * EACH;
+    const int copies = p.slots ? p.top_k : 1, blocks = (K + SHARE * EACH - 1) / (SHARE * EACH), end = (K + 63) & ~63;
+    const long long step = (long long)gridDim.x * teams;
+    // The places of a round's rows, one round ahead, where the rows have a routing.
+    const auto look_up = [&](long long first, int half) {
+        for (int i = (int)threadIdx.x; i < teams * copies; i += THREADS) {
+            const long long m = first + i / copies;
+            if (m < p.M) placed[half * teams * copies + i] = place_of(p, p.slots[m * p.top_k + i % copies]);
+        }
+    };
+    const auto fetch = [&](long long m, int k, Sixteen<T> (&v)[PARTS]) {
+        const T* x = (const T*)p.x + m * p.ldx;
+#pragma unroll
+        for (int u = 0; u < PARTS; u++) {
+            if (WHOLE && m < p.M) v[u].load(x, k + u * N, K, true);
+            else v[u].w[0] = v[u].w[1] = v[u].w[2] = v[u].w[3] = 0;
+        }
+    };
+    long long first = (long long)blockIdx.x * teams;
+    int half = 0;
+    if (p.slots) look_up(first, 0);
+    Sixteen<T> v[PARTS], next[PARTS];
+    fetch(first + mine, rank * EACH, next);
+    for (; first < p.M; first += step, half ^= 1) {
+        const long long m = first + mine;
         const bool in = m < p.M;
-        Sixteen<T> v[PARTS];
-        unsigned top = 0;
-        if (in) {
-            const T* x = (const T*)p.x + m * p.ldx;
-#pragma unroll
-            for (int u = 0; u < PARTS; u++) v[u].load(x, k + u * N, K, p.vec);
-#pragma unroll
-            for (int u = 0; u < PARTS; u++) top = max(top, v[u].magnitude());
+        Place at = {-1, -1};
+        if (p.slots) {
+            __syncthreads();  // this round's places are there, and the last round's are read
+            if (first + step < p.M) look_up(first + step, half ^ 1);
+        } else if (in) {
+            at = place_of(p, m);
         }
-        if (FORMAT == HCCL_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        const Step s = step_of<FORMAT>(top, p.wide, p.six);
-        unsigned code[2] = {0, 0};
-        if (in && s.inv != 0.f) {
-            // A saturated scale leaves quotients as large as the input: kept finite, so that the remainder is a number.
-            const bool far = FORMAT == HCCL_NVFP4 && s.byte == 0x7eu;
+        for (int base = 0; base < K; base += across) {
+            const int k = base + rank * EACH;
+            float f[EACH];
+            unsigned top = 0;
+            if constexpr (WHOLE) {
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                float q[8];
+                for (int u = 0; u < PARTS; u++) v[u] = next[u];
+                // the next elements are asked for before these are worked on
+                if (base + across < K) fetch(m, k + across, next);
+                else fetch(m + step, rank * EACH, next);
 #pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    float x = v[(8 * h + j) / N].value((8 * h + j) % N);
-                    if (far) x = fminf(fmaxf(x, -8.f * s.d), 8.f * s.d);
-                    q[j] = quotient<FORMAT>(x, s);
-                }
-                code[h] = eight_codes(q);
-            }
-        }
-        // A scale for each 16 or 32 elements; the first of four lanes (eight) has four to write.
-        constexpr int SHARE = FORMAT == HCCL_NVFP4 ? 1 : 2;
-        unsigned four = s.byte;
-        four |= __shfl_down_sync(0xffffffffu, four, SHARE) << 8;
-        four |= __shfl_down_sync(0xffffffffu, four, 2 * SHARE) << 16;
-        const int block = k / (SHARE * EACH), blocks = (K + SHARE * EACH - 1) / (SHARE * EACH);
-        if (!in || k >= ((K + 63) & ~63)) continue;
-        for (int c = 0; c < copies; c++) {
-            const long long row = p.slots ? p.slots[m * p.top_k + c] : m;
-            if (row < 0 || row >= p.n_q) continue;
-            uint8_t* q = p.q + row * p.ldq + k / 2;
-            if (p.vec_q && k + EACH <= K) {
-                *(uint2*)q = make_uint2(code[0], code[1]);
+                for (int u = 0; u < PARTS; u++) top = max(top, v[u].magnitude());
             } else {
+                // 32 lanes have one row's 512 elements, or, of shorter teams, several rows' 16 * team.
+                float* const h = handed[threadIdx.x / 32];
+                const int warp_first = (int)threadIdx.x / 32 * 32;
+                __syncwarp();
 #pragma unroll
-                for (int j = 0; j < 8; j++)
-                    if (k + 2 * j < K) q[j] = (uint8_t)(code[j / 4] >> (8 * (j & 3)));
+                for (int i = 0; i < EACH; i++) {
+                    const int j = i * 32 + lane, owner = j / EACH;  // element j of the warp is owner's
+                    const long long row = first + (warp_first + owner) / team;
+                    const int col = base + (warp_first + owner) % team * EACH + j % EACH;
+                    h[j + owner] = row < p.M && col < K ? to_f32<T>(((const T*)p.x)[row * p.ldx + col]) : 0.f;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < EACH; j++) f[j] = h[lane * 17 + j], top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
             }
-            if (!p.tn) {
-                if (lane % SHARE == 0 && block < blocks) p.scale[row * p.lds + block] = (uint8_t)s.byte;
-            } else if (block % 4 == 0 && lane % SHARE == 0) {
-                const int g = group_of(p.offsets, p.groups, row);
-                if (g < 0) continue;
-                const long long first = p.offsets ? max(0, p.offsets[g]) : 0, r = row - first;
-                const long long tile = tile_base(first, p.tn, g) + r / p.tn;
-                const int in_tile = (int)(r % p.tn), wide = p.tn > 128 ? p.tn / 128 : 1;
-                *(unsigned*)(p.scale + ((tile * wide + in_tile / 128) * p.atoms + block / 4) * ATOM + atom_row(in_tile % 128)) = four;
+            if (FORMAT == HCCL_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            const Step s = step_of<FORMAT>(top, p.wide, p.six);
+            unsigned code[2] = {0, 0};
+            if (s.inv != 0.f) {
+                if constexpr (WHOLE)
+#pragma unroll
+                    for (int j = 0; j < EACH; j++) f[j] = v[j / N].value(j % N);
+                // A saturated scale leaves quotients as large as the input: kept finite, so that the remainder is a number.
+                if (FORMAT == HCCL_NVFP4 && s.byte == 0x7eu)
+#pragma unroll
+                    for (int j = 0; j < EACH; j++) f[j] = fminf(fmaxf(f[j], -8.f * s.d), 8.f * s.d);
+#pragma unroll
+                for (int j = 0; j < EACH; j++) f[j] = quotient<FORMAT>(f[j], s);
+                code[0] = eight_codes(f), code[1] = eight_codes(f + 8);
             }
+            // A scale for each 16 or 32 elements; the first of four lanes (eight) has four to write.
+            unsigned four = s.byte;
+            four |= __shfl_down_sync(0xffffffffu, four, SHARE) << 8;
+            four |= __shfl_down_sync(0xffffffffu, four, 2 * SHARE) << 16;
+            const int block = k / (SHARE * EACH);
+            if (in && k < end)
+                for (int c = 0; c < copies; c++) {
+                    if (p.slots) at = placed[(half * teams + mine) * copies + c];
+                    if (at.row < 0) continue;
+                    uint8_t* q = p.q + at.row * p.ldq + k / 2;
+                    if (p.vec_q && k + EACH <= K) {
+                        *(uint2*)q = make_uint2(code[0], code[1]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; j++)
+                            if (k + 2 * j < K) q[j] = (uint8_t)(code[j / 4] >> (8 * (j & 3)));
+                    }
+                    if (lane % SHARE || at.scale < 0) continue;
+                    if (!p.tn) {
+                        if (block < blocks) p.scale[at.scale + block] = (uint8_t)s.byte;
+                    } else if (block % 4 == 0) {
+                        *(unsigned*)(p.scale + at.scale + (long long)(block / 4) * ATOM) = four;
+                    }
+                }
         }
     }
 }
 
-template <typename T, int FORMAT> __global__ void __launch_bounds__(THREADS) hccl_dequantise_fp4(const __grid_constant__ Fp4Values p, int pieces) {
-    const long long total = p.M * pieces, step = (long long)gridDim.x * THREADS;
-    const int K = (int)p.K;
-    for (long long i = (long long)blockIdx.x * THREADS + threadIdx.x; i < total; i += step) {
-        const long long m = i / pieces;
-        const int k = (int)(i % pieces) * EACH;
-        const uint8_t* q = p.q + m * p.ldq + k / 2;
-        unsigned w[2] = {0, 0};
-        if (p.vec && k + EACH <= K) {
-            const uint2 both = *(const uint2*)q;
-            w[0] = both.x, w[1] = both.y;
-        } else {
+// A thread has V elements at a time, 16 bytes of the result where rows start on them (WHOLE); `team` threads side by side a row, four pieces of each on their way at once. Otherwise an
+// element, so that a warp's stores are side by side.
+template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_dequantise_fp4(const __grid_constant__ Fp4Values p, int team) {
+    constexpr int V = WHOLE ? 16 / sizeof(T) : 1, U = 4;
+    const int teams = THREADS / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team, K = (int)p.K;
+    for (long long m = (long long)blockIdx.x * teams + mine; m < p.M; m += (long long)gridDim.x * teams) {
+        const uint8_t* const q = p.q + m * p.ldq;
+        const uint8_t* const scale = p.scale + m * p.lds;
+        T* const y = (T*)p.y + m * p.ldy;
+        for (int base = 0; base < K; base += U * team * V) {
+            unsigned w[U], byte[U];
 #pragma unroll
-            for (int j = 0; j < 8; j++)
-                if (k + 2 * j < K) w[j / 4] |= (unsigned)q[j] << (8 * (j & 3));
-        }
-        const float d = step_value<FORMAT>(p.scale[m * p.lds + k / block_of(FORMAT)], p.wide);
-        float v[EACH];
-        eight_values(w[0], v);
-        eight_values(w[1], v + 8);
+            for (int u = 0; u < U; u++) {
+                const int k = base + (u * team + rank) * V;
+                w[u] = byte[u] = 0;
+                if (k < K) {
+                    if (!WHOLE || k + V > K) {
 #pragma unroll
-        for (int j = 0; j < EACH; j++) v[j] = __fmul_rn(v[j], d);
-        T* y = (T*)p.y + m * p.ldy + k;
-        constexpr int N = 16 / sizeof(T);
-        if (p.vec && k + EACH <= K) {
-#pragma unroll
-            for (int u = 0; u < EACH / N; u++) {
-                Pack<T, N> o;
-                float part[N];
-#pragma unroll
-                for (int j = 0; j < N; j++) part[j] = v[u * N + j];
-                o.set(part);
-                ((uint4*)y)[u] = o.raw;
+                        for (int j = 0; j < (V + 1) / 2; j++)
+                            if (k + 2 * j < K) w[u] |= (unsigned)q[k / 2 + j] << (8 * j);
+                        if (V == 1 && k % 2) w[u] >>= 4;
+                    } else if constexpr (V == 8) {
+                        w[u] = *(const unsigned*)(q + k / 2);
+                    } else {
+                        w[u] = *(const unsigned short*)(q + k / 2);
+                    }
+                    byte[u] = scale[k / block_of(FORMAT)];
+                }
             }
-        } else {
 #pragma unroll
-            for (int j = 0; j < EACH; j++)
-                if (k + j < K) y[j] = from_f32<T>(v[j]);
+            for (int u = 0; u < U; u++) {
+                const int k = base + (u * team + rank) * V;
+                if (k >= K) break;
+                const float d = step_value<FORMAT>(byte[u], p.wide);
+                float v[8];
+                eight_values(w[u], v);
+#pragma unroll
+                for (int j = 0; j < V; j++) v[j] = __fmul_rn(v[j], d);
+                if (WHOLE && k + V <= K) {
+                    if constexpr (WHOLE) {
+                        Pack<T, V> o;
+                        float part[V];
+#pragma unroll
+                        for (int j = 0; j < V; j++) part[j] = v[j];
+                        o.set(part);
+                        *(uint4*)(y + k) = o.raw;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; j++)
+                        if (k + j < K) y[k + j] = from_f32<T>(v[j]);
+                }
+            }
         }
     }
 }
@@ -166,24 +244,29 @@ __global__ void __launch_bounds__(THREADS) hccl_tile_scales_fp4(const __grid_con
 
 unsigned grid_for(long long blocks) { return (unsigned)std::max(1ll, std::min(blocks, (long long)SMS * 8)); }
 
+int team_for(long long pieces, int least) {
+    int team = least;
+    while (team < THREADS && team < pieces) team *= 2;
+    return team;
+}
+
 template <typename T, int FORMAT> cudaError_t quantise_launch(const Fp4Rows& q, cudaStream_t s) {
     Fp4Rows p = q;
-    p.vec = (uintptr_t)p.x % 16 == 0 && (p.ldx * sizeof(T) % 16 == 0 || p.M <= 1);
     p.vec_q = (uintptr_t)p.q % 8 == 0 && p.ldq % 8 == 0;
-    const long long sixteens = (p.K + EACH - 1) / EACH;
-    int lanes = 8;
-    while (lanes < 32 && lanes < sixteens) lanes *= 2;
-    const int pieces = (int)((sixteens + lanes - 1) / lanes);
-    const long long warps = (p.M + 32 / lanes - 1) / (32 / lanes) * pieces;
-    hccl_quantise_fp4<T, FORMAT><<<grid_for((warps + THREADS / 32 - 1) / (THREADS / 32)), THREADS, 0, s>>>(p, lanes, pieces);
+    const bool whole = (uintptr_t)p.x % 16 == 0 && (p.ldx * sizeof(T) % 16 == 0 || p.M <= 1);
+    const int team = team_for((p.K + EACH - 1) / EACH, p.slots && p.top_k > 24 ? 16 : 8), shared = p.slots ? 2 * (THREADS / team) * p.top_k * (int)sizeof(Place) : 0;  // at most 24 KB
+    const unsigned grid = grid_for((p.M + THREADS / team - 1) / (THREADS / team));
+    if (whole) hccl_quantise_fp4<T, FORMAT, true><<<grid, THREADS, shared, s>>>(p, team);
+    else hccl_quantise_fp4<T, FORMAT, false><<<grid, THREADS, shared, s>>>(p, team);
     return cudaGetLastError();
 }
 
-template <typename T, int FORMAT> cudaError_t dequantise_launch(const Fp4Values& q, cudaStream_t s) {
-    Fp4Values p = q;
-    p.vec = (uintptr_t)p.q % 8 == 0 && p.ldq % 8 == 0 && (uintptr_t)p.y % 16 == 0 && p.ldy * sizeof(T) % 16 == 0;
-    const int pieces = (int)((p.K + EACH - 1) / EACH);
-    hccl_dequantise_fp4<T, FORMAT><<<grid_for((p.M * pieces + THREADS - 1) / THREADS), THREADS, 0, s>>>(p, pieces);
+template <typename T, int FORMAT> cudaError_t dequantise_launch(const Fp4Values& p, cudaStream_t s) {
+    const bool whole = (uintptr_t)p.q % 4 == 0 && p.ldq % 4 == 0 && (uintptr_t)p.y % 16 == 0 && (p.ldy * sizeof(T) % 16 == 0 || p.M <= 1);
+    const int V = whole ? 16 / (int)sizeof(T) : 1, team = team_for((p.K + 4 * V - 1) / (4 * V), 32);
+    const unsigned grid = grid_for((p.M + THREADS / team - 1) / (THREADS / team));
+    if (whole) hccl_dequantise_fp4<T, FORMAT, true><<<grid, THREADS, 0, s>>>(p, team);
+    else hccl_dequantise_fp4<T, FORMAT, false><<<grid, THREADS, 0, s>>>(p, team);
     return cudaGetLastError();
 }
 

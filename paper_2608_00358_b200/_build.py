@@ -11,7 +11,7 @@ LIB = os.path.join(_HERE, "libhccl_b200.so")
 SOURCES = ["graph.cpp", "collectives.cpp", "verify.cpp", "executor.cu", "kernel_lsu.cu", "kernel_lsu_light.cu", "kernel_bulk.cu",
            "kernel_resident.cu", "kernel_chain.cu", "experts.cu", "kernel_route.cu", "kernel_rows.cu", "kernel_quantise.cu", "kernel_matmul_i8.cu", "kernel_rows_i8.cu",
            "fp4.cu", "kernel_rows_fp4.cu", "kernel_matmul_fp4.cu", "kernel_few_fp4.cu", "kernel_activate.cu"]
-HEADERS = ["plan.hpp", "tables.h", "device.cuh", "bulk.cuh", "bulk_layout.h", "kernels.cuh", "experts.cuh", "rows_i8.cuh", "checks.h", "tensor.cuh", "fp4.cuh", "activate.cuh", os.path.join("..", "..", "include", "hccl.h")]
+HEADERS = ["plan.hpp", "tables.h", "device.cuh", "bulk.cuh", "bulk_layout.h", "kernels.cuh", "experts.cuh", "rows_i8.cuh", "checks.h", "tensor.cuh", "fp4.cuh", "activate.cuh", "two.cuh", os.path.join("..", "..", "include", "hccl.h")]
 # a kernel's unit does not use every helper of the shared headers: no "declared but never referenced" remarks for them
 QUIET = ["-diag-suppress", "177"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

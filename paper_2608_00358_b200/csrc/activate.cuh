@@ -1,6 +1,6 @@
 // Activations of expert layers and their slopes, in 32 bits.
 #pragma once
-#include "experts.cuh"
+#include "two.cuh"
 
 namespace hccl {
 namespace experts {

@@ -8,7 +8,7 @@
 // Scales lie in two ways. By rows: [rows][blocks], for exchange and storage. In tiles, as the tensor cores take them: an atom of 512 bytes holds 128 rows x 4 blocks, the
 // four bytes of row r at (r % 32) * 16 + (r / 32) * 4; atoms of a tile's successive blocks follow one another, up to whole stages of 256 elements.
 #pragma once
-#include "experts.cuh"
+#include "two.cuh"
 
 namespace hccl {
 namespace experts {
@@ -50,11 +50,12 @@ template <int FORMAT> __device__ __forceinline__ Step step_of(unsigned top, floa
     }
     return r;
 }
-// x / d rounded to nearest (Markstein 1990: from the rounded reciprocal, by the quotient's exact remainder); for MXFP4 a product with a power of two.
-template <int FORMAT> __device__ __forceinline__ float quotient(float x, const Step& s) {
-    const float y = __fmul_rn(x, s.inv);
+// x / d rounded to nearest, of -x (Markstein 1990: from the rounded reciprocal, by the quotient's exact remainder; in these signs a negative zero stays one); for MXFP4 a product with a
+// power of two.
+template <int FORMAT> __device__ __forceinline__ Two quotients(Two minus_x, const Step& s) {
+    const Two inv(-s.inv), y = minus_x * inv;
     if constexpr (FORMAT == HCCL_MXFP4) return y;
-    return __fmaf_rn(-__fmaf_rn(y, s.d, -x), s.inv, y);  // (in these signs a negative zero stays one)
+    return fma2(fma2(y, Two(s.d), minus_x), inv, y);
 }
 // Eight quotients to four bytes, the first in the lowest half-byte; |q| > 6 becomes 6.
 __device__ __forceinline__ unsigned eight_codes(const float* q) {

@@ -73,24 +73,6 @@ template <int N> __device__ __forceinline__ void words(Generator& gen, unsigned 
     }
 }
 
-// Two numbers at a time: one instruction multiplies both.
-struct Two {
-    unsigned long long v;
-    __device__ __forceinline__ Two() {}
-    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-    __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
-    __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-};
-__device__ __forceinline__ Two operator*(Two a, Two b) {
-    Two r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-    Two r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
 // 4 / (1 + exp(-x)) for results of 16 bits, as logistic<true>.
 __device__ __forceinline__ Two four_logistic(Two x) {
     float a, b;

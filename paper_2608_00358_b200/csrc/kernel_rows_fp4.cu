@@ -46,36 +46,52 @@ __device__ __forceinline__ Place place_of(const Fp4Rows& p, long long row) {
     return at;
 }
 
-// A thread has 16 elements of a row at a time, `team` threads side by side (8 to 256) a row. WHOLE: rows start on 16 bytes. Otherwise a warp fetches its 512 elements one by one, lanes
-// side by side, and hands them round through shared memory (16 loads of a thread's own elements touch 32 lines each: 1999 x 2057 fp32 13 us in the place of NNN).
+// A thread has 16 elements of a row at a time, `team` threads side by side (8 to 256) a row, and its next ones on their way into shared memory, where it alone reads them (WHOLE: rows start
+// on 16 bytes; in registers, with half the loads in flight, 8192 x 8192 bf16 take 54 us in the place of NNN). Otherwise a warp fetches its 512 elements one by one, lanes side by side, and
+// hands them round through shared memory.
+constexpr int RING = 3;
 template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_quantise_fp4(const __grid_constant__ Fp4Rows p, int team) {
     constexpr int N = Sixteen<T>::N, PARTS = EACH / N, SHARE = FORMAT == HCCL_NVFP4 ? 1 : 2 /* threads to a block */;
-    extern __shared__ __align__(16) Place placed[];  // [2][teams * copies]
-    __shared__ float handed[WHOLE ? 1 : THREADS / 32][WHOLE ? 1 : 32 * 17];
+    extern __shared__ __align__(16) uint4 shared[];
+    uint4* const ring = shared;                                                        // [RING][PARTS][threads]
+    float* const handed = (float*)shared + threadIdx.x / 32 * (32 * 17);               // [warp][lane][17]
+    Place* const placed = (Place*)(shared + (WHOLE ? RING * PARTS * blockDim.x : (blockDim.x / 32 * 32 * 17 + 3) / 4));  // [2][teams * copies]
     asm volatile("griddepcontrol.launch_dependents;");  // the product may start to fetch its weights
-    const int teams = THREADS / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team, lane = threadIdx.x % 32, K = (int)p.K, across = team * EACH;
+    const int threads = blockDim.x, teams = threads / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team, lane = threadIdx.x % 32, K = (int)p.K, across = team * EACH;
     const int copies = p.slots ? p.top_k : 1, blocks = (K + SHARE * EACH - 1) / (SHARE * EACH), end = (K + 63) & ~63;
     const long long step = (long long)gridDim.x * teams;
     // The places of a round's rows, one round ahead, where the rows have a routing.
     const auto look_up = [&](long long first, int half) {
-        for (int i = (int)threadIdx.x; i < teams * copies; i += THREADS) {
+        for (int i = (int)threadIdx.x; i < teams * copies; i += threads) {
             const long long m = first + i / copies;
             if (m < p.M) placed[half * teams * copies + i] = place_of(p, p.slots[m * p.top_k + i % copies]);
         }
     };
-    const auto fetch = [&](long long m, int k, Sixteen<T> (&v)[PARTS]) {
-        const T* x = (const T*)p.x + m * p.ldx;
+    long long first = (long long)blockIdx.x * teams;
+    // Where the loads are, ahead of the work.
+    long long fetch_row = first + mine;
+    int fetch_base = 0, slot = 0;
+    const auto fetch = [&](int turn) {
+        if constexpr (WHOLE) {
+            const int k = fetch_base + rank * EACH;
+            if (fetch_row < p.M) {
+                const T* x = (const T*)p.x + fetch_row * p.ldx + k;
 #pragma unroll
-        for (int u = 0; u < PARTS; u++) {
-            if (WHOLE && m < p.M) v[u].load(x, k + u * N, K, true);
-            else v[u].w[0] = v[u].w[1] = v[u].w[2] = v[u].w[3] = 0;
+                for (int u = 0; u < PARTS; u++) {
+                    const int bytes = min(16, (K - k - u * N) * (int)sizeof(T));  // (the rest of the sixteen becomes zeros)
+                    if (bytes > 0)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((unsigned)__cvta_generic_to_shared(ring + (turn * PARTS + u) * threads + threadIdx.x)), "l"(x + u * N), "r"(bytes) : "memory");
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            fetch_base += across;
+            if (fetch_base >= K) fetch_base = 0, fetch_row += step;
         }
     };
-    long long first = (long long)blockIdx.x * teams;
+#pragma unroll
+    for (int i = 0; i < RING - 1; i++) fetch(i);
     int half = 0;
     if (p.slots) look_up(first, 0);
-    Sixteen<T> v[PARTS], next[PARTS];
-    fetch(first + mine, rank * EACH, next);
     for (; first < p.M; first += step, half ^= 1) {
         const long long m = first + mine;
         const bool in = m < p.M;
@@ -88,45 +104,47 @@ template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(
         }
         for (int base = 0; base < K; base += across) {
             const int k = base + rank * EACH;
-            float f[EACH];
+            float f[EACH];  // negated
             unsigned top = 0;
             if constexpr (WHOLE) {
+                fetch(slot == 0 ? RING - 1 : slot - 1);
+                asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
+                Sixteen<T> v[PARTS];
 #pragma unroll
-                for (int u = 0; u < PARTS; u++) v[u] = next[u];
-                // the next elements are asked for before these are worked on
-                if (base + across < K) fetch(m, k + across, next);
-                else fetch(m + step, rank * EACH, next);
-#pragma unroll
-                for (int u = 0; u < PARTS; u++) top = max(top, v[u].magnitude());
-            } else {
-                // 32 lanes have one row's 512 elements, or, of shorter teams, several rows' 16 * team.
-                float* const h = handed[threadIdx.x / 32];
-                const int warp_first = (int)threadIdx.x / 32 * 32;
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < EACH; i++) {
-                    const int j = i * 32 + lane, owner = j / EACH;  // element j of the warp is owner's
-                    const long long row = first + (warp_first + owner) / team;
-                    const int col = base + (warp_first + owner) % team * EACH + j % EACH;
-                    h[j + owner] = row < p.M && col < K ? to_f32<T>(((const T*)p.x)[row * p.ldx + col]) : 0.f;
+                for (int u = 0; u < PARTS; u++) {
+                    uint4 w = make_uint4(0, 0, 0, 0);
+                    if (in && k + u * N < K) w = ring[(slot * PARTS + u) * threads + threadIdx.x];
+                    v[u].w[0] = w.x, v[u].w[1] = w.y, v[u].w[2] = w.z, v[u].w[3] = w.w;
                 }
+                slot = slot == RING - 1 ? 0 : slot + 1;
+#pragma unroll
+                for (int u = 0; u < PARTS; u++) {
+                    top = max(top, v[u].magnitude());
+#pragma unroll
+                    for (int i = 0; i < 4; i++) v[u].w[i] ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+                }
+#pragma unroll
+                for (int j = 0; j < EACH; j++) f[j] = v[j / N].value(j % N);
+            } else {
+                const int col = base + rank / 32 * 512 + lane;  // (a warp has one row here)
+                const T* x = (const T*)p.x + m * p.ldx;
                 __syncwarp();
 #pragma unroll
-                for (int j = 0; j < EACH; j++) f[j] = h[lane * 17 + j], top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
+                for (int i = 0; i < EACH; i++) handed[i * 32 + lane + 2 * i + lane / EACH] = in && col + i * 32 < K ? to_f32<T>(x[col + i * 32]) : 0.f;
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < EACH; j++) f[j] = -handed[lane * 17 + j], top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
             }
             if (FORMAT == HCCL_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             const Step s = step_of<FORMAT>(top, p.wide, p.six);
             unsigned code[2] = {0, 0};
             if (s.inv != 0.f) {
-                if constexpr (WHOLE)
-#pragma unroll
-                    for (int j = 0; j < EACH; j++) f[j] = v[j / N].value(j % N);
                 // A saturated scale leaves quotients as large as the input: kept finite, so that the remainder is a number.
                 if (FORMAT == HCCL_NVFP4 && s.byte == 0x7eu)
 #pragma unroll
                     for (int j = 0; j < EACH; j++) f[j] = fminf(fmaxf(f[j], -8.f * s.d), 8.f * s.d);
 #pragma unroll
-                for (int j = 0; j < EACH; j++) f[j] = quotient<FORMAT>(f[j], s);
+                for (int j = 0; j < EACH; j += 2) quotients<FORMAT>(Two(f[j], f[j + 1]), s).get(f[j], f[j + 1]);
                 code[0] = eight_codes(f), code[1] = eight_codes(f + 8);
             }
             // A scale for each 16 or 32 elements; the first of four lanes (eight) has four to write.
@@ -161,7 +179,7 @@ template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(
 // element, so that a warp's stores are side by side.
 template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_dequantise_fp4(const __grid_constant__ Fp4Values p, int team) {
     constexpr int V = WHOLE ? 16 / sizeof(T) : 1, U = 4;
-    const int teams = THREADS / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team, K = (int)p.K;
+    const int teams = blockDim.x / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team, K = (int)p.K;
     for (long long m = (long long)blockIdx.x * teams + mine; m < p.M; m += (long long)gridDim.x * teams) {
         const uint8_t* const q = p.q + m * p.ldq;
         const uint8_t* const scale = p.scale + m * p.lds;
@@ -244,29 +262,36 @@ __global__ void __launch_bounds__(THREADS) hccl_tile_scales_fp4(const __grid_con
 
 unsigned grid_for(long long blocks) { return (unsigned)std::max(1ll, std::min(blocks, (long long)SMS * 8)); }
 
+// Threads to a row: a power of two up to a warp, then whole warps.
 int team_for(long long pieces, int least) {
     int team = least;
-    while (team < THREADS && team < pieces) team *= 2;
-    return team;
+    while (team < 32 && team < pieces) team *= 2;
+    return team < pieces ? (int)std::min((long long)THREADS, (pieces + 31) / 32 * 32) : team;
 }
 
 template <typename T, int FORMAT> cudaError_t quantise_launch(const Fp4Rows& q, cudaStream_t s) {
     Fp4Rows p = q;
     p.vec_q = (uintptr_t)p.q % 8 == 0 && p.ldq % 8 == 0;
     const bool whole = (uintptr_t)p.x % 16 == 0 && (p.ldx * sizeof(T) % 16 == 0 || p.M <= 1);
-    const int team = team_for((p.K + EACH - 1) / EACH, p.slots && p.top_k > 24 ? 16 : 8), shared = p.slots ? 2 * (THREADS / team) * p.top_k * (int)sizeof(Place) : 0;  // at most 24 KB
-    const unsigned grid = grid_for((p.M + THREADS / team - 1) / (THREADS / team));
-    if (whole) hccl_quantise_fp4<T, FORMAT, true><<<grid, THREADS, shared, s>>>(p, team);
-    else hccl_quantise_fp4<T, FORMAT, false><<<grid, THREADS, shared, s>>>(p, team);
+    const int team = team_for((p.K + EACH - 1) / EACH, whole ? p.slots && p.top_k > 16 ? 16 : 8 : 32), teams = THREADS / team, threads = teams * team;
+    const int held = whole ? RING * (EACH / Sixteen<T>::N) * threads * 16 : (threads * 17 + 3) / 4 * 16;
+    const int shared = held + (p.slots ? 2 * teams * p.top_k * (int)sizeof(Place) : 0);  // at most 48 KB (32-bit rows) and 16 KB
+    const unsigned grid = grid_for((p.M + teams - 1) / teams);
+    const auto kernel = whole ? hccl_quantise_fp4<T, FORMAT, true> : hccl_quantise_fp4<T, FORMAT, false>;
+    if (shared > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<grid, threads, shared, s>>>(p, team);
     return cudaGetLastError();
 }
 
 template <typename T, int FORMAT> cudaError_t dequantise_launch(const Fp4Values& p, cudaStream_t s) {
     const bool whole = (uintptr_t)p.q % 4 == 0 && p.ldq % 4 == 0 && (uintptr_t)p.y % 16 == 0 && (p.ldy * sizeof(T) % 16 == 0 || p.M <= 1);
-    const int V = whole ? 16 / (int)sizeof(T) : 1, team = team_for((p.K + 4 * V - 1) / (4 * V), 32);
-    const unsigned grid = grid_for((p.M + THREADS / team - 1) / (THREADS / team));
-    if (whole) hccl_dequantise_fp4<T, FORMAT, true><<<grid, THREADS, 0, s>>>(p, team);
-    else hccl_dequantise_fp4<T, FORMAT, false><<<grid, THREADS, 0, s>>>(p, team);
+    const int V = whole ? 16 / (int)sizeof(T) : 1, team = team_for((p.K + 4 * V - 1) / (4 * V), 32), teams = THREADS / team;
+    const unsigned grid = grid_for((p.M + teams - 1) / teams);
+    if (whole) hccl_dequantise_fp4<T, FORMAT, true><<<grid, teams * team, 0, s>>>(p, team);
+    else hccl_dequantise_fp4<T, FORMAT, false><<<grid, teams * team, 0, s>>>(p, team);
     return cudaGetLastError();
 }
 

@@ -121,6 +121,7 @@ hccl_status_t quant_params(Fp4Rows* p, const void* x, int64_t ldx, int64_t M, in
     p->K = K;
     p->wide = wide;
     p->six = 6.f * wide;
+    p->sixth = 1.f / p->six;
     p->q = q;
     p->ldq = ldq;
     p->n_q = n_q;
@@ -245,6 +246,7 @@ hccl_status_t hccl_linear_fp4(const hccl_matmul_fp4_t* in, const void* x, int64_
         mm.q = p.q;
         mm.q_scale = p.scale = p.q + s.scales;
         p.tn = mm.tn;
+        while (1 << p.shift < p.tn) p.shift++;
         p.atoms = (int)(stages(m.K) * stage_atoms(m.format));
         p.offsets = m.groups ? m.offsets : nullptr;
         p.groups = m.groups;

@@ -28,18 +28,21 @@ struct Step {
     float d, inv;    // 1 / d, to nearest; 0: the block's elements are zeros
     unsigned byte;   // as stored
 };
-// top: the largest magnitude's bits; NaN is above infinity.
-template <int FORMAT> __device__ __forceinline__ Step step_of(unsigned top, float wide, float six) {
+// top: the largest magnitude's bits; NaN is above infinity. six: 6 wide, and sixth its reciprocal, both to nearest.
+template <int FORMAT> __device__ __forceinline__ Step step_of(unsigned top, float wide, float six, float sixth) {
     Step r;
     if constexpr (FORMAT == HCCL_NVFP4) {
-        const float t = fminf(__fdiv_rn(__uint_as_float(top), six), 448.f);
+        const float x = __uint_as_float(top), y = __fmul_rn(x, sixth);
+        const float t = fminf(__fmaf_rn(-__fmaf_rn(y, six, -x), sixth, y), 448.f);  // x / six, as the quotients below; what is too large for that is NaN there and 448 here
         unsigned short two;
         asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(t));
         r.byte = two & 0xffu;
         unsigned halves;
         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(halves) : "h"(two));
         r.d = __fmul_rn(__low2float(*(const __half2*)&halves), wide);
-        r.inv = r.byte ? __frcp_rn(r.d) : 0.f;
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(r.d));
+        r.inv = r.byte ? __fmaf_rn(inv, __fmaf_rn(-r.d, inv, 1.f), inv) : 0.f;  // one step of Newton's: to nearest but for a few in a million, which the quotients' remainder makes up for
         if (top >= 0x7f800000u) r.byte = 0x7fu, r.inv = 0.f, r.d = __uint_as_float(0x7fffffffu);
     } else {
         const int code = max((int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u), 1);
@@ -102,8 +105,8 @@ struct Fp4Rows {       // quantiser
     uint8_t* q;
     uint8_t* scale;    // by rows (lds) or in tiles (tn > 0)
     long long lds;
-    int tn, atoms;     // tokens of a tile; atoms of a row of tiles' blocks, up to whole stages
-    float wide, six;
+    int tn, shift, atoms;  // tokens of a tile, 1 << shift; atoms of a row of tiles' blocks, up to whole stages
+    float wide, six, sixth;
     int vec_q;
     const int* slots;  // null: row m of x to row m of q
     int top_k;

@@ -39,140 +39,104 @@ __device__ __forceinline__ Place place_of(const Fp4Rows& p, long long row) {
         const int g = group_of(p.offsets, p.groups, row);
         if (g >= 0) {
             const unsigned first = p.offsets ? (unsigned)max(0, p.offsets[g]) : 0u, r = (unsigned)row - first, tn = (unsigned)p.tn, in_tile = r & (tn - 1);  // (rows are counted in 32 bits there, tn is a power of two)
-            const long long tile = first / tn + g + r / tn;
-            at.scale = (tile * (tn > 128 ? tn / 128 : 1) + in_tile / 128) * p.atoms * ATOM + atom_row(in_tile % 128);
+            const unsigned tile = (first >> p.shift) + g + (r >> p.shift), atom = tn > 128 ? tile * (tn >> 7) + in_tile / 128 : tile;
+            at.scale = (long long)atom * (p.atoms * ATOM) + atom_row(in_tile % 128);
         }
     }
     return at;
 }
 
-// A thread has 16 elements of a row at a time, `team` threads side by side (8 to 256) a row, and its next ones on their way into shared memory, where it alone reads them (WHOLE: rows start
-// on 16 bytes; in registers, with half the loads in flight, 8192 x 8192 bf16 take 54 us in the place of NNN). Otherwise a warp fetches its 512 elements one by one, lanes side by side, and
-// hands them round through shared memory.
-constexpr int RING = 3;
+// A thread has 16 elements of a row, `team` threads side by side (8 to 256) a row, or, of long rows, a part of it; blocks come and go, which costs less than walking rows does in
+// instructions, and those are the bound (8192 x 8192 bf16: 45 us; walked, with loads two pieces ahead, 55). WHOLE: rows start on 16 bytes. Otherwise a warp fetches its 512 elements
+// one by one, lanes side by side, and hands them round through shared memory.
 template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_quantise_fp4(const __grid_constant__ Fp4Rows p, int team) {
     constexpr int N = Sixteen<T>::N, PARTS = EACH / N, SHARE = FORMAT == HCCL_NVFP4 ? 1 : 2 /* threads to a block */;
     extern __shared__ __align__(16) uint4 shared[];
-    uint4* const ring = shared;                                                        // [RING][PARTS][threads]
-    float* const handed = (float*)shared + threadIdx.x / 32 * (32 * 17);               // [warp][lane][17]
-    Place* const placed = (Place*)(shared + (WHOLE ? RING * PARTS * blockDim.x : (blockDim.x / 32 * 32 * 17 + 3) / 4));  // [2][teams * copies]
+    float* const handed = (float*)shared + threadIdx.x / 32 * (32 * 17);                              // [warp][lane][17], unless WHOLE
+    Place* const places = (Place*)(shared + (WHOLE ? 0 : blockDim.x / 32 * (32 * 17 / 4)));  // [teams * copies], where rows have a routing
     asm volatile("griddepcontrol.launch_dependents;");  // the product may start to fetch its weights
-    const int threads = blockDim.x, teams = threads / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team, lane = threadIdx.x % 32, K = (int)p.K, across = team * EACH;
-    const int copies = p.slots ? p.top_k : 1, blocks = (K + SHARE * EACH - 1) / (SHARE * EACH), end = (K + 63) & ~63;
-    const long long step = (long long)gridDim.x * teams;
-    // The places of a round's rows, one round ahead, where the rows have a routing.
-    const auto look_up = [&](long long first, int half) {
-        for (int i = (int)threadIdx.x; i < teams * copies; i += threads) {
-            const long long m = first + i / copies;
-            if (m < p.M) placed[half * teams * copies + i] = place_of(p, p.slots[m * p.top_k + i % copies]);
-        }
-    };
-    long long first = (long long)blockIdx.x * teams;
-    // Where the loads are, ahead of the work.
-    long long fetch_row = first + mine;
-    int fetch_base = 0, slot = 0;
-    const auto fetch = [&](int turn) {
-        if constexpr (WHOLE) {
-            const int k = fetch_base + rank * EACH;
-            if (fetch_row < p.M) {
-                const T* x = (const T*)p.x + fetch_row * p.ldx + k;
+    const int mine = (int)threadIdx.x / team, rank = (int)threadIdx.x - mine * team, teams = blockDim.x / team, lane = threadIdx.x % 32, K = (int)p.K;
+    const long long first = (long long)blockIdx.x * teams, m = first + mine;
+    const int k = ((int)blockIdx.y * team + rank) * EACH, copies = p.slots ? p.top_k : 1;
+    const bool in = m < p.M && k < ((K + 63) & ~63);
+    Sixteen<T> v[PARTS];
+    float f[EACH];  // negated
+    unsigned top = 0;
+    if constexpr (WHOLE) {
+        const T* x = (const T*)p.x + m * p.ldx + k;
+        if (in && k + EACH <= K) {
 #pragma unroll
-                for (int u = 0; u < PARTS; u++) {
-                    const int bytes = min(16, (K - k - u * N) * (int)sizeof(T));  // (the rest of the sixteen becomes zeros)
-                    if (bytes > 0)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((unsigned)__cvta_generic_to_shared(ring + (turn * PARTS + u) * threads + threadIdx.x)), "l"(x + u * N), "r"(bytes) : "memory");
-                }
+            for (int u = 0; u < PARTS; u++) {
+                const uint4 w = ((const uint4*)x)[u];
+                v[u].w[0] = w.x, v[u].w[1] = w.y, v[u].w[2] = w.z, v[u].w[3] = w.w;
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            fetch_base += across;
-            if (fetch_base >= K) fetch_base = 0, fetch_row += step;
-        }
-    };
+        } else {
 #pragma unroll
-    for (int i = 0; i < RING - 1; i++) fetch(i);
-    int half = 0;
-    if (p.slots) look_up(first, 0);
-    for (; first < p.M; first += step, half ^= 1) {
-        const long long m = first + mine;
-        const bool in = m < p.M;
-        Place at = {-1, -1};
-        if (p.slots) {
-            __syncthreads();  // this round's places are there, and the last round's are read
-            if (first + step < p.M) look_up(first + step, half ^ 1);
-        } else if (in) {
-            at = place_of(p, m);
-        }
-        for (int base = 0; base < K; base += across) {
-            const int k = base + rank * EACH;
-            float f[EACH];  // negated
-            unsigned top = 0;
-            if constexpr (WHOLE) {
-                fetch(slot == 0 ? RING - 1 : slot - 1);
-                asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
-                Sixteen<T> v[PARTS];
-#pragma unroll
-                for (int u = 0; u < PARTS; u++) {
-                    uint4 w = make_uint4(0, 0, 0, 0);
-                    if (in && k + u * N < K) w = ring[(slot * PARTS + u) * threads + threadIdx.x];
-                    v[u].w[0] = w.x, v[u].w[1] = w.y, v[u].w[2] = w.z, v[u].w[3] = w.w;
-                }
-                slot = slot == RING - 1 ? 0 : slot + 1;
-#pragma unroll
-                for (int u = 0; u < PARTS; u++) {
-                    top = max(top, v[u].magnitude());
-#pragma unroll
-                    for (int i = 0; i < 4; i++) v[u].w[i] ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
-                }
-#pragma unroll
-                for (int j = 0; j < EACH; j++) f[j] = v[j / N].value(j % N);
-            } else {
-                const int col = base + rank / 32 * 512 + lane;  // (a warp has one row here)
-                const T* x = (const T*)p.x + m * p.ldx;
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < EACH; i++) handed[i * 32 + lane + 2 * i + lane / EACH] = in && col + i * 32 < K ? to_f32<T>(x[col + i * 32]) : 0.f;
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < EACH; j++) f[j] = -handed[lane * 17 + j], top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
-            }
-            if (FORMAT == HCCL_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            const Step s = step_of<FORMAT>(top, p.wide, p.six);
-            unsigned code[2] = {0, 0};
-            if (s.inv != 0.f) {
-                // A saturated scale leaves quotients as large as the input: kept finite, so that the remainder is a number.
-                if (FORMAT == HCCL_NVFP4 && s.byte == 0x7eu)
-#pragma unroll
-                    for (int j = 0; j < EACH; j++) f[j] = fminf(fmaxf(f[j], -8.f * s.d), 8.f * s.d);
-#pragma unroll
-                for (int j = 0; j < EACH; j += 2) quotients<FORMAT>(Two(f[j], f[j + 1]), s).get(f[j], f[j + 1]);
-                code[0] = eight_codes(f), code[1] = eight_codes(f + 8);
-            }
-            // A scale for each 16 or 32 elements; the first of four lanes (eight) has four to write.
-            unsigned four = s.byte;
-            four |= __shfl_down_sync(0xffffffffu, four, SHARE) << 8;
-            four |= __shfl_down_sync(0xffffffffu, four, 2 * SHARE) << 16;
-            const int block = k / (SHARE * EACH);
-            if (in && k < end)
-                for (int c = 0; c < copies; c++) {
-                    if (p.slots) at = placed[(half * teams + mine) * copies + c];
-                    if (at.row < 0) continue;
-                    uint8_t* q = p.q + at.row * p.ldq + k / 2;
-                    if (p.vec_q && k + EACH <= K) {
-                        *(uint2*)q = make_uint2(code[0], code[1]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; j++)
-                            if (k + 2 * j < K) q[j] = (uint8_t)(code[j / 4] >> (8 * (j & 3)));
-                    }
-                    if (lane % SHARE || at.scale < 0) continue;
-                    if (!p.tn) {
-                        if (block < blocks) p.scale[at.scale + block] = (uint8_t)s.byte;
-                    } else if (block % 4 == 0) {
-                        *(unsigned*)(p.scale + at.scale + (long long)(block / 4) * ATOM) = four;
-                    }
-                }
+            for (int u = 0; u < PARTS; u++) v[u].load(x, u * N, in ? K - k : 0, true);
         }
     }
+    if (p.slots) {
+        for (int i = (int)threadIdx.x; i < teams * copies; i += blockDim.x)
+            if (first + i / copies < p.M) places[i] = place_of(p, p.slots[(first + i / copies) * p.top_k + i % copies]);
+        __syncthreads();
+    }
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int u = 0; u < PARTS; u++) {
+            top = max(top, v[u].magnitude());
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[u].w[i] ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+        }
+#pragma unroll
+        for (int j = 0; j < EACH; j++) f[j] = v[j / N].value(j % N);
+    } else {
+        const int col = ((int)blockIdx.y * team + rank / 32 * 32) * EACH + lane;  // (a warp has one row here)
+        const T* x = (const T*)p.x + m * p.ldx;
+#pragma unroll
+        for (int i = 0; i < EACH; i++) handed[i * 32 + lane + 2 * i + lane / EACH] = m < p.M && col + i * 32 < K ? to_f32<T>(x[col + i * 32]) : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < EACH; j++) f[j] = -handed[lane * 17 + j], top = max(top, __float_as_uint(f[j]) & 0x7fffffffu);
+    }
+    if (FORMAT == HCCL_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const Step s = step_of<FORMAT>(top, p.wide, p.six, p.sixth);
+    unsigned code[2] = {0, 0};
+    if (s.inv != 0.f) {
+        // A saturated scale leaves quotients as large as the input: kept finite, so that the remainder is a number.
+        if (FORMAT == HCCL_NVFP4 && s.byte == 0x7eu)
+#pragma unroll
+            for (int j = 0; j < EACH; j++) f[j] = fminf(fmaxf(f[j], -8.f * s.d), 8.f * s.d);
+#pragma unroll
+        for (int j = 0; j < EACH; j += 2) quotients<FORMAT>(Two(f[j], f[j + 1]), s).get(f[j], f[j + 1]);
+        code[0] = eight_codes(f), code[1] = eight_codes(f + 8);
+    }
+    // A scale for each 16 or 32 elements; the first of four lanes (eight) has four to write.
+    unsigned four = s.byte;
+    four |= __shfl_down_sync(0xffffffffu, four, SHARE) << 8;
+    four |= __shfl_down_sync(0xffffffffu, four, 2 * SHARE) << 16;
+    if (!in) return;
+    const int block = k / (SHARE * EACH), blocks = (K + SHARE * EACH - 1) / (SHARE * EACH);
+    const auto put = [&](const Place& at) {
+        if (at.row < 0) return;
+        uint8_t* q = p.q + at.row * p.ldq + k / 2;
+        if (p.vec_q && k + EACH <= K) {
+            *(uint2*)q = make_uint2(code[0], code[1]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (k + 2 * j < K) q[j] = (uint8_t)(code[j / 4] >> (8 * (j & 3)));
+        }
+        if (lane % SHARE || at.scale < 0) return;
+        if (!p.tn) {
+            if (block < blocks) p.scale[at.scale + block] = (uint8_t)s.byte;
+        } else if (block % 4 == 0) {
+            *(unsigned*)(p.scale + at.scale + block / 4 * ATOM) = four;
+        }
+    };
+    if (p.slots)
+        for (int c = 0; c < copies; c++) put(places[mine * copies + c]);
+    else
+        put(place_of(p, m));
 }
 
 // A thread has V elements at a time, 16 bytes of the result where rows start on them (WHOLE); `team` threads side by side a row, four pieces of each on their way at once. Otherwise an
@@ -273,16 +237,11 @@ template <typename T, int FORMAT> cudaError_t quantise_launch(const Fp4Rows& q, 
     Fp4Rows p = q;
     p.vec_q = (uintptr_t)p.q % 8 == 0 && p.ldq % 8 == 0;
     const bool whole = (uintptr_t)p.x % 16 == 0 && (p.ldx * sizeof(T) % 16 == 0 || p.M <= 1);
-    const int team = team_for((p.K + EACH - 1) / EACH, whole ? p.slots && p.top_k > 16 ? 16 : 8 : 32), teams = THREADS / team, threads = teams * team;
-    const int held = whole ? RING * (EACH / Sixteen<T>::N) * threads * 16 : (threads * 17 + 3) / 4 * 16;
-    const int shared = held + (p.slots ? 2 * teams * p.top_k * (int)sizeof(Place) : 0);  // at most 48 KB (32-bit rows) and 16 KB
-    const unsigned grid = grid_for((p.M + teams - 1) / teams);
-    const auto kernel = whole ? hccl_quantise_fp4<T, FORMAT, true> : hccl_quantise_fp4<T, FORMAT, false>;
-    if (shared > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
-        if (e != cudaSuccess) return e;
-    }
-    kernel<<<grid, threads, shared, s>>>(p, team);
+    const int team = team_for((p.K + EACH - 1) / EACH, whole ? 8 : 32), teams = THREADS / team, threads = teams * team;
+    const int shared = (whole ? 0 : threads * 17 * 4) + (p.slots ? teams * p.top_k * (int)sizeof(Place) : 0);  // at most 17 and 16 KB
+    const dim3 grid((unsigned)((p.M + teams - 1) / teams), (unsigned)((p.K + team * EACH - 1) / (team * EACH)));
+    if (whole) hccl_quantise_fp4<T, FORMAT, true><<<grid, threads, shared, s>>>(p, team);
+    else hccl_quantise_fp4<T, FORMAT, false><<<grid, threads, shared, s>>>(p, team);
     return cudaGetLastError();
 }
 

@@ -37,6 +37,8 @@ def _format(name: str) -> int:
 
 
 def _bits(x: float) -> int:
+    if x == 1.0:
+        return 0x3F800000
     try:
         return struct.unpack("<I", struct.pack("<f", x))[0]
     except (struct.error, OverflowError, TypeError):
@@ -75,17 +77,26 @@ class Fp4Rows:
     def __reduce__(self):
         return Fp4Rows, (self.q, self.scale, self.K, self.format, self.wide)
 
+    @classmethod
+    def _made(cls, q, scale, K, format, wide):
+        """Of tensors that hold together, because they were made here."""
+        self = cls.__new__(cls)
+        self.q, self.scale, self.K, self.format, self.wide = q, scale, K, format, wide
+        return self
+
     def dequantize(self, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The values that the rows stand for, rounded to dtype."""
-        M, dev = self.q.shape[0], self.q.get_device()
+        q, scale, K = self.q, self.scale, self.K
+        M, dev = q.shape[0], q.get_device()
         if out is None:
-            if dtype not in _DT:
+            dt, ldy = _DT.get(dtype), K
+            if dt is None:
                 _refuse(hb.ERR_DTYPE, "dequantize: result in %s" % dtype)
-            out, ldy, dt = torch.empty((M, self.K), dtype=dtype, device=self.q.device), self.K, _DT[dtype]
+            out = q.new_empty((M, K), dtype=dtype)
         else:
-            ldy, dt = _matrix(out, "out", self.K, M, dev), _dtype(out, "out")
+            ldy, dt = _matrix(out, "out", K, M, dev), _dtype(out, "out")
             _given(out, "out")
-        _on(dev, _dequantize)(self.q.data_ptr(), _matrix(self.q, "q"), self.scale.data_ptr(), _matrix(self.scale, "scale"), M, self.K, FORMATS[self.format],
+        _on(dev, _dequantize)(q.data_ptr(), max(q.stride(0), q.shape[1]), scale.data_ptr(), max(scale.stride(0), scale.shape[1]), M, K, FORMATS[self.format],
                               _bits(self.wide), out.data_ptr(), ldy, dt, _stream(dev))
         return out
 
@@ -100,11 +111,11 @@ def quantize_rows(x: torch.Tensor, format: str = "nvfp4", scale: float = 1.0, ro
     M, K = x.shape
     n = M if routing is None else (routing.tokens * routing.top_k if n_rows is None else n_rows)
     blocks = (K + BLOCK[format] - 1) // BLOCK[format]
-    q = torch.empty((n, _pad16((K + 1) // 2)), dtype=torch.uint8, device=x.device)
-    s = torch.empty((n, blocks), dtype=torch.uint8, device=x.device)
-    _on(dev, _quantize)(x.data_ptr(), ldx, M, K, dt, fmt, _bits(wide), routing.at if routing is not None else 0, q.data_ptr(), q.shape[1], s.data_ptr(), blocks, n,
-                        _stream(dev))
-    return Fp4Rows(q[:, : (K + 1) // 2], s, K, format, wide)
+    width = (K + 1) // 2
+    pitch = _pad16(width)
+    q, s = x.new_empty((n, pitch), dtype=torch.uint8), x.new_empty((n, blocks), dtype=torch.uint8)
+    _on(dev, _quantize)(x.data_ptr(), ldx, M, K, dt, fmt, _bits(wide), routing.at if routing is not None else 0, q.data_ptr(), pitch, s.data_ptr(), blocks, n, _stream(dev))
+    return Fp4Rows._made(q if pitch == width else q[:, :width], s, K, format, wide)
 
 
 class Fp4Linear:
@@ -184,7 +195,7 @@ class Fp4Linear:
         if out is None:
             if dtype not in _DT:
                 _refuse(hb.ERR_DTYPE, "Fp4Linear: result in %s" % dtype)
-            return torch.empty((M, self.N), dtype=dtype, device=self.device), self.N, _DT[dtype]
+            return self.weight.new_empty((M, self.N), dtype=dtype), self.N, _DT[dtype]
         ldy, dt = _matrix(out, "out", self.N, M, self.dev), _dtype(out, "out")
         _given(out, "out")
         return out, ldy, dt

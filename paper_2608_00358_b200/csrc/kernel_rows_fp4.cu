@@ -36,12 +36,16 @@ __device__ __forceinline__ Place place_of(const Fp4Rows& p, long long row) {
     } else if (!p.tn) {
         at.scale = row * p.lds;
     } else {
-        const int g = group_of(p.offsets, p.groups, row);
-        if (g >= 0) {
-            const unsigned first = p.offsets ? (unsigned)max(0, p.offsets[g]) : 0u, r = (unsigned)row - first, tn = (unsigned)p.tn, in_tile = r & (tn - 1);  // (rows are counted in 32 bits there, tn is a power of two)
-            const unsigned tile = (first >> p.shift) + g + (r >> p.shift), atom = tn > 128 ? tile * (tn >> 7) + in_tile / 128 : tile;
-            at.scale = (long long)atom * (p.atoms * ATOM) + atom_row(in_tile % 128);
+        // (rows are counted in 32 bits there, tn is a power of two)
+        unsigned first = 0, g = 0;
+        if (p.offsets) {
+            const int of = group_of(p.offsets, p.groups, row);
+            if (of < 0) return at;
+            g = of, first = (unsigned)max(0, p.offsets[of]);
         }
+        const unsigned r = (unsigned)row - first, in_tile = r & ((1u << p.shift) - 1), tile = (first >> p.shift) + g + (r >> p.shift);
+        const unsigned atom = p.shift > 7 ? (tile << (p.shift - 7)) + (in_tile >> 7) : tile;
+        at.scale = (long long)atom * (p.atoms * ATOM) + atom_row(in_tile & 127);
     }
     return at;
 }
@@ -49,13 +53,15 @@ __device__ __forceinline__ Place place_of(const Fp4Rows& p, long long row) {
 // A thread has 16 elements of a row, `team` threads side by side (8 to 256) a row, or, of long rows, a part of it; blocks come and go, which costs less than walking rows does in
 // instructions, and those are the bound (8192 x 8192 bf16: 45 us; walked, with loads two pieces ahead, 55). WHOLE: rows start on 16 bytes. Otherwise a warp fetches its 512 elements
 // one by one, lanes side by side, and hands them round through shared memory.
-template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_quantise_fp4(const __grid_constant__ Fp4Rows p, int team) {
+template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_quantise_fp4(const __grid_constant__ Fp4Rows p, int team, int teams) {
     constexpr int N = Sixteen<T>::N, PARTS = EACH / N, SHARE = FORMAT == HCCL_NVFP4 ? 1 : 2 /* threads to a block */;
     extern __shared__ __align__(16) uint4 shared[];
     float* const handed = (float*)shared + threadIdx.x / 32 * (32 * 17);                              // [warp][lane][17], unless WHOLE
     Place* const places = (Place*)(shared + (WHOLE ? 0 : blockDim.x / 32 * (32 * 17 / 4)));  // [teams * copies], where rows have a routing
     asm volatile("griddepcontrol.launch_dependents;");  // the product may start to fetch its weights
-    const int mine = (int)threadIdx.x / team, rank = (int)threadIdx.x - mine * team, teams = blockDim.x / team, lane = threadIdx.x % 32, K = (int)p.K;
+    int mine = 0, rank = (int)threadIdx.x;
+    if (teams > 1) mine = rank / team, rank -= mine * team;
+    const int lane = threadIdx.x % 32, K = (int)p.K;
     const long long first = (long long)blockIdx.x * teams, m = first + mine;
     const int k = ((int)blockIdx.y * team + rank) * EACH, copies = p.slots ? p.top_k : 1;
     const bool in = m < p.M && k < ((K + 63) & ~63);
@@ -136,14 +142,16 @@ template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(
     if (p.slots)
         for (int c = 0; c < copies; c++) put(places[mine * copies + c]);
     else
-        put(place_of(p, m));
+        put(place_of(p, m));  // (n_q is at least M)
 }
 
 // A thread has V elements at a time, 16 bytes of the result where rows start on them (WHOLE); `team` threads side by side a row, four pieces of each on their way at once. Otherwise an
 // element, so that a warp's stores are side by side.
-template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_dequantise_fp4(const __grid_constant__ Fp4Values p, int team) {
+template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(THREADS) hccl_dequantise_fp4(const __grid_constant__ Fp4Values p, int team, int teams) {
     constexpr int V = WHOLE ? 16 / sizeof(T) : 1, U = 4;
-    const int teams = blockDim.x / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team, K = (int)p.K;
+    int mine = 0, rank = (int)threadIdx.x;
+    if (teams > 1) mine = rank / team, rank -= mine * team;
+    const int K = (int)p.K;
     for (long long m = (long long)blockIdx.x * teams + mine; m < p.M; m += (long long)gridDim.x * teams) {
         const uint8_t* const q = p.q + m * p.ldq;
         const uint8_t* const scale = p.scale + m * p.lds;
@@ -240,17 +248,17 @@ template <typename T, int FORMAT> cudaError_t quantise_launch(const Fp4Rows& q, 
     const int team = team_for((p.K + EACH - 1) / EACH, whole ? 8 : 32), teams = THREADS / team, threads = teams * team;
     const int shared = (whole ? 0 : threads * 17 * 4) + (p.slots ? teams * p.top_k * (int)sizeof(Place) : 0);  // at most 17 and 16 KB
     const dim3 grid((unsigned)((p.M + teams - 1) / teams), (unsigned)((p.K + team * EACH - 1) / (team * EACH)));
-    if (whole) hccl_quantise_fp4<T, FORMAT, true><<<grid, threads, shared, s>>>(p, team);
-    else hccl_quantise_fp4<T, FORMAT, false><<<grid, threads, shared, s>>>(p, team);
+    if (whole) hccl_quantise_fp4<T, FORMAT, true><<<grid, threads, shared, s>>>(p, team, teams);
+    else hccl_quantise_fp4<T, FORMAT, false><<<grid, threads, shared, s>>>(p, team, teams);
     return cudaGetLastError();
 }
 
 template <typename T, int FORMAT> cudaError_t dequantise_launch(const Fp4Values& p, cudaStream_t s) {
     const bool whole = (uintptr_t)p.q % 4 == 0 && p.ldq % 4 == 0 && (uintptr_t)p.y % 16 == 0 && (p.ldy * sizeof(T) % 16 == 0 || p.M <= 1);
     const int V = whole ? 16 / (int)sizeof(T) : 1, team = team_for((p.K + 4 * V - 1) / (4 * V), 32), teams = THREADS / team;
-    const unsigned grid = grid_for((p.M + teams - 1) / teams);
-    if (whole) hccl_dequantise_fp4<T, FORMAT, true><<<grid, teams * team, 0, s>>>(p, team);
-    else hccl_dequantise_fp4<T, FORMAT, false><<<grid, teams * team, 0, s>>>(p, team);
+    const unsigned grid = (unsigned)std::min((p.M + teams - 1) / teams, 1ll << 30);
+    if (whole) hccl_dequantise_fp4<T, FORMAT, true><<<grid, teams * team, 0, s>>>(p, team, teams);
+    else hccl_dequantise_fp4<T, FORMAT, false><<<grid, teams * team, 0, s>>>(p, team, teams);
     return cudaGetLastError();
 }
 

@@ -635,7 +635,8 @@ typedef enum { HCCL_NVFP4 = 0, HCCL_MXFP4 = 1 } hccl_fp4_t;
 
 /* Rows by blocks: q [rows, (K + 1) / 2] bytes, scale [rows, ceil(K / 16 or 32)] bytes; an odd K leaves the last half-byte 0. wide: g, from 1e-30 to 1e30.
  * routing NULL: M rows of x to M rows. Otherwise M must be routing->tokens and row t is written to every slots[t,k] below n_q (the 4-bit form of
- * hccl_dispatch, for about a quarter of the bytes in the exchange); rows that no choice fills are left alone. K <= HCCL_MAX_FP4_K.
+ * hccl_dispatch, for about a quarter of the bytes in the exchange); rows that no choice fills are left alone. K <= HCCL_MAX_FP4_K; rows, of either
+ * side, at most HCCL_MAX_I8_ROWS.
  * The way back: y[m,k] = round(element * d), dt. */
 #define HCCL_MAX_FP4_K 131072
 hccl_status_t hccl_quantize_rows_fp4(const void* x, int64_t ldx, int64_t M, int64_t K, hccl_dtype_t dt, int32_t format, float wide, const hccl_routing_t* routing,

@@ -19,7 +19,7 @@ bool valid_wide(float g) { return g >= 1e-30f && g <= 1e30f; }  // (NaN fails)
 
 hccl_status_t check_shape(int64_t rows, int64_t K, int32_t format) {
     if (!valid_format(format)) return HCCL_ERR_DTYPE;
-    return K < 0 || K > HCCL_MAX_FP4_K || rows < 0 ? HCCL_ERR_INVALID_ARG : HCCL_OK;
+    return K < 0 || K > HCCL_MAX_FP4_K || rows < 0 || rows > HCCL_MAX_I8_ROWS ? HCCL_ERR_INVALID_ARG : HCCL_OK;
 }
 
 // Rows of codes and of scales.
@@ -106,7 +106,7 @@ hccl_status_t quant_params(Fp4Rows* p, const void* x, int64_t ldx, int64_t M, in
                            int64_t ldq, int64_t n_q) {
     TRY(check_shape(M, K, format));
     if (!hccl::valid_dtype(dt)) return HCCL_ERR_DTYPE;
-    if (n_q < 0 || (format == HCCL_NVFP4 && !valid_wide(wide))) return HCCL_ERR_INVALID_ARG;
+    if (n_q < 0 || n_q > HCCL_MAX_I8_ROWS || (format == HCCL_NVFP4 && !valid_wide(wide))) return HCCL_ERR_INVALID_ARG;
     TRY(check_matrix(x, M, ldx, K, dt));
     if (r) {
         TRY(check_routing(r));

@@ -505,7 +505,10 @@ template <typename T, int FORMAT> cudaError_t matmul_launch(const MatmulFp4& p, 
 
 }  // namespace
 
-// Which tile, as for the products in 8-bit integers: tiles of TN tokens and a cluster of S blocks for each, by an estimate in microseconds.
+// Which tile, as for the products in 8-bit integers: tiles of TN tokens and a cluster of S blocks for each, by an estimate in microseconds: rounds of the blocks over the tiles, times stages, times a
+// stage's time, and what does not overlap. Measured with the quantiser against every other choice on 18 shapes, TN,S (1 x 8192 x 4096 takes 10.4 us with 16,1 to 32,2; 1 x 2048 x 4096 8.3 with
+// 16,4 and 10.3 with 32,2; 128 x 2048 x 8192 12.4 with 64,4 and 16.1 with 32,1; 512 x 4096 x 4096 13.3 with 128,1 and 17.3 with 64,1; 997 x 4104 x 2064 14.4 with 256,1 and 16.5 with 128,1); nowhere is
+// the choice more than 8 % behind the best. Groups are uneven: tiles of twice the mean number of rows hold most groups whole, so that weights are read once.
 TileChoice choose_fp4(long long M, long long N, long long K, int groups) {
     if (groups) {
         const long long twice = 2 * ((M + groups - 1) / groups);
@@ -515,7 +518,7 @@ TileChoice choose_fp4(long long M, long long N, long long K, int groups) {
     static const struct {
         int tn;
         double stage, last, exchange;
-    } option[] = {{16, 0.17, 0.0, 1.0}, {32, 0.17, 0.1, 1.5}, {64, 0.18, 0.4, 2.4}, {128, 0.22, 1.2, 0}, {256, 0.30, 3.0, 0}};
+    } option[] = {{16, 0.17, 0.0, 1.4}, {32, 0.17, 0.1, 1.5}, {64, 0.18, 0.4, 2.4}, {128, 0.22, 1.2, 0}, {256, 0.30, 2.3, 0}};
     TileChoice best = {256, 1};
     double least = 1e30;
     for (const auto& o : option) {

@@ -96,8 +96,8 @@ class Fp4Rows:
         else:
             ldy, dt = _matrix(out, "out", K, M, dev), _dtype(out, "out")
             _given(out, "out")
-        _on(dev, _dequantize)(q.data_ptr(), max(q.stride(0), q.shape[1]), scale.data_ptr(), max(scale.stride(0), scale.shape[1]), M, K, FORMATS[self.format],
-                              _bits(self.wide), out.data_ptr(), ldy, dt, _stream(dev))
+        ldq, lds = (q.stride(0), scale.stride(0)) if M > 1 else (q.shape[1], scale.shape[1])
+        _on(dev, _dequantize)(q.data_ptr(), ldq, scale.data_ptr(), lds, M, K, FORMATS[self.format], _bits(self.wide), out.data_ptr(), ldy, dt, _stream(dev))
         return out
 
 

@@ -27,6 +27,7 @@ def test_quantise_refusals():
     assert go(r=routing(tokens=5), n=10) == hb.ERR_COUNT_MISMATCH
     assert go(r=routing(slots=0), n=10) == hb.ERR_INVALID_ARG
     assert go(ldx=1 << 61) == hb.ERR_INVALID_ARG
+    assert go(M=1 << 31, n=1 << 31) == hb.ERR_INVALID_ARG and go(n=1 << 31) == hb.ERR_INVALID_ARG
 
 
 def test_dequantise_refusals():

@@ -139,6 +139,16 @@ def test_rows_beyond_32_bits_of_offset():
     assert torch.equal(got[-3:], want.dequantize(BF16)) and not got[-4].any()
 
 
+def test_rows_that_overlap_are_refused():
+    one = fp4.quantize_rows(torch.ones(1, 64, device="cuda"))
+    rows = fp4.Fp4Rows(one.q.expand(5, -1), one.scale.expand(5, -1), 64)
+    refused(hb.ERR_INVALID_ARG, rows.dequantize)
+    wide = torch.zeros(5, 48, dtype=torch.uint8, device="cuda")
+    wide[:, :32], scales = one.q, one.scale.repeat(5, 3)
+    got = fp4.Fp4Rows(wide[:, :32], scales[:, :4], 64).dequantize()  # rows further apart than they are long
+    assert torch.equal(got, one.dequantize().expand(5, -1))
+
+
 # ------------------------------------------------------------------------------------------------ products
 # Sums in 32 bits: an instruction adds 64 products (exact) to the accumulator, each aligned to the largest of them and cut at its last bit: within K * 2^-23 of the
 # sum of the terms' sizes; then the factor, the bias (2^-24 each) and the type's rounding.
@@ -348,6 +358,8 @@ LAYERS = [
     (2, 257, 129, 3, 3, "gelu", True, True, 0, F16), (3, 300, 70, 5, 2, "relu", False, True, 0.3, F32), (9, 512, 300, 2, 2, "silu", True, False, 0, F32),
     (17, 136, 65, 4, 3, "gelu", False, False, 0.2, BF16), (33, 640, 104, 8, 4, "silu", True, True, 0.1, F32), (64, 260, 130, 6, 5, "silu", True, False, 0, F32),
     (64, 96, 48, 1, 1, "silu", True, False, 0, F16), (5, 2050, 1030, 7, 2, "silu", True, True, 0, F32), (4, 64, 64, 1024, 4, "silu", True, False, 0, F32),
+    (64, 40, 24, 32, 32, "silu", True, False, 0, F32), (64, 33, 17, 1024, 32, "relu", False, True, 0, F32),  # as many rows as there can be, in few chunks and in many
+    (7, 48, 2100, 5, 2, "silu", True, False, 0, F32), (2, 4100, 40, 6, 6, "gelu", True, False, 0, BF16),  # many parts on one side, one on the other
 ]
 
 
@@ -415,6 +427,21 @@ def test_layer_of_small_and_large_inputs(size):
     r = routing_of(some_ids(rng, 3, 2, 2), 2)
     scale = float(2.0 ** np.round(np.log2(size)))
     assert torch.equal(few(x * scale, r) / scale, few(x, r))
+
+
+def test_layer_in_place_with_an_expert_twice_and_rows_that_begin_later():
+    few = small_layer()
+    x = torch.randn(3, 192, device="cuda")
+    once, twice = few(x, routing_of(np.array([[2], [0], [1]]), 4)), few(x, routing_of(np.array([[2, 2], [0, 0], [1, 1]]), 4))
+    assert torch.equal(once + once, twice)
+    # offsets may begin after 0: rows in front of them belong to nobody
+    r = routing_of(np.array([[2], [0], [1]]), 4)
+    late = ex.Routing(r.ids, r.weights, r.counts, r.offsets + 0, r.slots, r.source)
+    late.offsets[0] = 1  # the row of expert 0, token 1's
+    y = few(x, late)
+    assert torch.equal(y[[0, 2]], once[[0, 2]]) and not y[1].any()
+    z = x.clone()
+    assert few(z, routing_of(np.array([[2], [0], [1]]), 4), out=z) is z and torch.equal(z, once)
 
 
 def test_layer_refusals():

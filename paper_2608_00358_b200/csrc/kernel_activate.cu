@@ -2,8 +2,7 @@
 // counter-based generator, and is formed anew wherever it is needed: nothing of it is stored. Without a gate y = act(x) m.
 //
 // The generator is Philox-4x32-10 (Salmon, Moraes, Dror, Shaw 2011): four 32-bit words from a 128-bit counter and a 64-bit key in ten rounds of two 32 x 32 bit
-// products. Element i of the result (row * I + column) takes word i % 4 of the counter (i / 4, call); it is kept if the word is at least p 2^32.
-#include <algorithm>
+// products. Element i of the result (row * I + column) takes word i % 4 of the counter (i / 4, call); it is XX <algorithm>
 
 #include "activate.cuh"
 

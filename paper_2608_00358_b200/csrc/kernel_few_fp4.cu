@@ -79,9 +79,17 @@ struct FewParams {
 
 // How many stages of K a unit has at most, so that there are enough units to share out evenly. (The scratch's size goes by it.)
 __device__ __forceinline__ int span_of(int chunks, int tiles, int k_blocks, int blocks) {
-    int span = SPAN;
-    while (span > 1 && (long long)chunks * tiles * ((k_blocks + span - 1) / span) < (long long)ENOUGH * blocks) span /= 2;
-    return span;
+    int shift = 2;
+    static_assert(SPAN == 1 << 2, "a shift");
+    while (shift && (long long)chunks * tiles * ((k_blocks + (1 << shift) - 1) >> shift) < (long long)ENOUGH * blocks) shift--;
+    return 1 << shift;
+}
+// a / b for numbers that are not negative and a quotient below 2^20: from an approximate one, off by one at most. Where a block's run begins hangs on ten divisions in a
+// row, and a division in whole numbers takes 40 instructions, of 64 bits 150.
+template <typename A> __device__ __forceinline__ int divide(A a, A b) {
+    const int q = (int)__fdividef((float)a, (float)b);
+    const A left = a - (A)q * b;
+    return left < 0 ? q - 1 : left >= b ? q + 1 : q;
 }
 
 template <int FORMAT> __device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
@@ -298,10 +306,10 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     constexpr int blocks = SMS;
     if (warp >= 8) {
         // While the chunks are listed: what comes first from memory is asked for, a share by each block, and the code that makes pieces is fetched by running it.
-        const long long row = (long long)p.K * sizeof(T), bytes = row * p.T;
-        for (long long i = ((long long)blockIdx.x * SPLITTERS + threadIdx.x - 256) * 128; i < bytes; i += (long long)blocks * SPLITTERS * 128) {
-            const long long t = i / row;
-            prefetch((const char*)p.in + t * p.ldx * sizeof(T) + (i - t * row));
+        const int lines = (p.K * (int)sizeof(T) + 127) / 128;  // of a row (one that begins between two reaches into one more: that is fetched when it is needed)
+        for (int i = (int)(blockIdx.x * SPLITTERS + threadIdx.x) - 256; i < lines * p.T; i += blocks * SPLITTERS) {
+            const int t = divide(i, lines);
+            prefetch((const char*)p.in + t * p.ldx * (long long)sizeof(T) + (i - t * lines) * 128);
         }
         if (blockIdx.x * SPLITTERS + threadIdx.x - 256 < p.rows) prefetch(p.source + (blockIdx.x * SPLITTERS + threadIdx.x - 256));
         make_pieces(make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f), 0.f, (char*)(held + threadIdx.x - 256), SPLITTERS * 16, 0, 0);
@@ -313,7 +321,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
             if (chunk < p.rows) all[chunk] = c;  // (never more than rows, if the offsets ascend)
         }));
         __syncwarp();
-        const int own = (int)((long long)n * blockIdx.x / blocks);
+        const int own = n * (int)blockIdx.x / blocks;
         if (lane < OWN && own + lane < n) table[lane] = all[own + lane];
         if (lane == 0) chunk_total = n;
     }
@@ -322,8 +330,8 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_at, 0);
-    const int chunks = __shfl_sync(0xffffffffu, chunk_total, 0), own = (int)((long long)chunks * blockIdx.x / blocks);
-    const int halves = p.gated ? 2 : 1, span = span_of(chunks, halves * p.chan_tiles, p.k_blocks, blocks), parts_of_k = (p.k_blocks + span - 1) / span;
+    const int chunks = __shfl_sync(0xffffffffu, chunk_total, 0), own = chunks * (int)blockIdx.x / blocks;
+    const int halves = p.gated ? 2 : 1, span = span_of(chunks, halves * p.chan_tiles, p.k_blocks, blocks), parts_of_k = divide(p.k_blocks + span - 1, span);
     const int of_chunk = parts_of_k * halves * p.chan_tiles, of_part = parts_of_k * halves * GROUP;  // units; a chunk's last part may have fewer
     const long long units = (long long)chunks * of_chunk;
     const int u0 = (int)(units * blockIdx.x / blocks), u1 = (int)(units * (blockIdx.x + 1) / blocks);
@@ -336,13 +344,13 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
         Unit t = {};
         t.u = u;
         if (u >= u1) return t;
-        t.chunk = uniform(u / of_chunk);
+        t.chunk = uniform(divide(u, of_chunk));
         t.c = unpacked(table[t.chunk - own]);
         int rest = u - t.chunk * of_chunk;
-        t.part = uniform(rest / of_part);
+        t.part = uniform(divide(rest, of_part));
         in_part(t);
         rest -= t.part * of_part;
-        t.kc = uniform(rest / t.of);
+        t.kc = uniform(divide(rest, t.of));
         t.index = uniform(rest - t.kc * t.of);
         place(t);
         return t;
@@ -366,7 +374,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     // With one part of K a chunk's pieces serve all its units.
     const auto begins = [&](const Unit& t) { return t.u == u0 || (t.index == 0 && (parts_of_k > 1 || t.part == 0)); };
     const auto ends = [&](const Unit& t) { return t.u == u1 - 1 || (t.index == t.of - 1 && (parts_of_k > 1 || t.part == p.down_parts - 1)); };
-    const auto stage_of = [&](int kc) { return p.k_blocks * kc / parts_of_k; };  // the first of a part of K; parts differ by one stage at most
+    const auto stage_of = [&](int kc) { return divide(p.k_blocks * kc, parts_of_k); };  // the first of a part of K; parts differ by one stage at most
     const auto stages_of = [&](int kc) { return stage_of(kc + 1) - stage_of(kc); };
     int it = 0, acc = 0, turn = 0;  // stages, units and parts of K passed
 
@@ -473,15 +481,15 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
             const int half = turn & 1, k0 = stage_of(t.kc) * 256, wide = stages_of(t.kc) * 256 / EACH;  // threads to a row
             char* const part = parts + half * S::PART;
             // A thread's elements, eight at a time, are those of task i of (row, eight elements), i = me, me + 256, ...
-            const auto row_of = [&](int i) { return (me + i * SPLITTERS) / wide; };
-            const auto k_of = [&](int i) { return k0 + (me + i * SPLITTERS) % wide * EACH; };
+            const auto row_of = [&](int i) { return divide(me + i * SPLITTERS, wide); };
+            const auto k_of = [&](int i, int r) { return k0 + (me + i * SPLITTERS - r * wide) * EACH; };
 #pragma unroll 1
             for (int i = 0; i < TASKS; i++) {
-                const int r = row_of(i), k = k_of(i);
+                const int r = row_of(i), k = k_of(i, r);
                 if (r >= t.c.rows) break;
                 float v[EACH];
                 const int from = p.source[t.c.row + r];
-                load8<T>((const T*)p.in + (long long)(from / p.top_k) * p.ldx, k, (unsigned)from < (unsigned)p.rows ? p.K : 0, p.vec, v);
+                load8<T>((const T*)p.in + (long long)divide(max(from, 0), p.top_k) * p.ldx, k, (unsigned)from < (unsigned)p.rows ? p.K : 0, p.vec, v);
                 unsigned top = 0;  // the largest magnitude of each row's part of K
 #pragma unroll
                 for (int j = 0; j < EACH; j++) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
@@ -496,7 +504,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
             if (!ok) break;
 #pragma unroll 1
             for (int i = 0; i < TASKS; i++) {
-                const int r = row_of(i), k = k_of(i);
+                const int r = row_of(i), k = k_of(i, r);
                 if (r >= t.c.rows) break;
                 float factor, back;
                 row_factor(top_of[half][r], &factor, &back);
@@ -525,9 +533,12 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
 
     // The block counts its units, all at once; parts of chunks that are complete with them are its own to finish.
     int* const list = (int*)parts;  // (its last readers are done)
-    const auto part_at = [&](int u) { return u / of_chunk * p.down_parts + u % of_chunk / of_part; };
+    const auto part_at = [&](int u) {
+        const int chunk = divide(u, of_chunk);
+        return chunk * p.down_parts + divide(u - chunk * of_chunk, of_part);
+    };
     for (int i = part_at(u0) + (int)threadIdx.x; i <= part_at(u1 - 1); i += UP_THREADS) {
-        const int lo = i / p.down_parts * of_chunk + i % p.down_parts * of_part, hi = min(lo + of_part, (i / p.down_parts + 1) * of_chunk);
+        const int chunk = divide(i, p.down_parts), lo = chunk * of_chunk + (i - chunk * p.down_parts) * of_part, hi = min(lo + of_part, (chunk + 1) * of_chunk);
         const int n = min(u1, hi) - max(u0, lo);
         if (atomicAdd(p.chunk_count + i, n) + n == hi - lo) list[atomicAdd(&completed, 1)] = i;
     }
@@ -538,7 +549,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     for (int l = 0; l < completed;) {
         int jobs = 0;
         for (; l < completed; l++) {  // (all threads the same; one of them writes it down)
-            const int chunk = list[l] / p.down_parts, part = list[l] - chunk * p.down_parts;
+            const int chunk = divide(list[l], p.down_parts), part = list[l] - chunk * p.down_parts;
             const Chunk c = unpacked(table[chunk - own]);
             if (jobs + c.rows > ROWS) break;
             for (int r = 0; r < c.rows; r++, jobs++)
@@ -641,7 +652,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
     const int of_tile = chunks * p.k_blocks;
     const long long total = (long long)of_tile * p.chan_tiles;
     const auto first_of = [&](int block) { return (int)(total * block / blocks); };
-    const int g0 = first_of((int)blockIdx.x), g1 = first_of((int)blockIdx.x + 1);
+    const int g0 = first_of((int)blockIdx.x), g1 = first_of((int)blockIdx.x + 1), first_tile = of_tile ? divide(g0, of_tile) : 0;
 
     const auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
     const auto bound = [&](Segment& t) {
@@ -652,9 +663,9 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
         Segment t = {};
         t.g = g0;
         if (g0 >= g1) return t;
-        t.tile = uniform(g0 / of_tile);
+        t.tile = uniform(first_tile);
         const int rest = g0 - t.tile * of_tile;
-        t.chunk = uniform(rest / p.k_blocks);
+        t.chunk = uniform(divide(rest, p.k_blocks));
         t.k0 = rest - t.chunk * p.k_blocks;
         t.c = unpacked(table[t.chunk]);
         bound(t);
@@ -762,7 +773,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
             if (p.bias && t.k0 == 0 && t.tile * CH + me < p.N) r.bias = p.bias[(long long)t.c.expert * p.N + t.tile * CH + me];
             if (lane < t.c.rows) {
                 const int choice = p.source[t.c.row + lane];
-                if ((unsigned)choice < (unsigned)p.rows) r.token = choice / p.top_k, r.weight = p.weights[choice];
+                if ((unsigned)choice < (unsigned)p.rows) r.token = divide(choice, p.top_k), r.weight = p.weights[choice];
                 r.back = __ldcg(p.unscale + (long long)(t.c.row + lane) * p.down_parts + t.k0 / SPAN);
             }
             return r;
@@ -802,7 +813,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
                         sums[i * CH + me] = 0.f;
                     }
                 } else {
-                    float* part = p.part + (long long)(2 * blockIdx.x + (t.tile == g0 / of_tile ? 0 : 1)) * p.T * CH + me;
+                    float* part = p.part + (long long)(2 * blockIdx.x + (t.tile == first_tile ? 0 : 1)) * p.T * CH + me;
                     for (int i = 0; i < p.T; i++, part += CH) {
                         __stcg(part, sums[i * CH + me]);
                         sums[i * CH + me] = 0.f;
@@ -825,16 +836,16 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(DOWN_THREADS
         return;
     }
     if (threadIdx.x < 2 && g0 < g1) {  // the first and the last of this block's runs of channels, if others share them
-        const int tile = threadIdx.x == 0 ? g0 / of_tile : (g1 - 1) / of_tile, lo = max(g0, tile * of_tile), hi = min(g1, (tile + 1) * of_tile), n = hi - lo;
-        if (n < of_tile && (threadIdx.x == 0 || tile != g0 / of_tile)) {
+        const int tile = threadIdx.x == 0 ? first_tile : divide(g1 - 1, of_tile), lo = max(g0, tile * of_tile), hi = min(g1, (tile + 1) * of_tile), n = hi - lo;
+        if (n < of_tile && (threadIdx.x == 0 || tile != first_tile)) {
             if (atomicAdd(p.tile_count + tile, n) + n == of_tile) list[atomicAdd(&completed, 1)] = tile;
             __threadfence();
         }
     }
     __syncthreads();
     for (int i = warp; i < completed * p.T; i += DOWN_THREADS / 32) {
-        const int token = i / completed, tile = list[i % completed], chan = tile * CH + 4 * lane;
-        const auto block_of_stage = [&](long long g) { return (int)(((g + 1) * blocks - 1) / total); };
+        const int token = divide(i, completed), tile = list[i - token * completed], chan = tile * CH + 4 * lane;
+        const auto block_of_stage = [&](long long g) { return divide((g + 1) * blocks - 1, total); };
         const int from = block_of_stage((long long)tile * of_tile), to = block_of_stage((long long)(tile + 1) * of_tile - 1);
         float sum[4] = {};
 #pragma unroll 8

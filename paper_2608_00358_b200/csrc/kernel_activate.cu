@@ -4,8 +4,8 @@
 // The generator is Philox-4x32-10 (Salmon, Moraes, Dror, Shaw 2011): four 32-bit words from a 128-bit counter and a 64-bit key in ten rounds of two 32 x 32 bit
 // products. Element i of the result (row * I + column) takes word i % 4 of the counter (i / 4, call); it is kept if the word is at least p 2^32.
 //
-// Measured (B200, copy peak 6.5 TB/s): 32768 x 2048 bf16 without dropout 64 us = 6.3 TB/s, gradient 103 = 6.5; with dropout 105 and 125: the generator's 18 wide products for four elements
-// and what joins them are 10 of 34 instructions an element, and those are the bound.
+// Measured (B200, copy peak 6.5 TB/s): 32768 x 2048 bf16 without dropout 64 us = 6.3 TB/s, gradient 103 = 6.5; with dropout 105 and 125: 40 instructions
+// an element issue in 70 % of the cycles, about 10 of them the generator's (18 wide products for four elements, and what joins them).
 #include <algorithm>
 
 #include "activate.cuh"

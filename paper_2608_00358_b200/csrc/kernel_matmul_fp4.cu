@@ -4,14 +4,14 @@
 // 8-bit integers the weights are the instruction's 128-row operand and the tokens its columns. With CG = 2 two blocks on neighbouring SMs form a
 // tile of 256 channels x 256 tokens; each has all 256 tokens' scales in its own tensor memory.
 //
-// Roles of a block (12 or 20 warps): warp 0 issues the TMA loads, warp 1 copies a stage's scales to tensor memory and issues the matrix instructions, warp 2 owns
-// the tensor memory, the warps from 4 on turn accumulators into results. A stage is 256 elements of K: 128 bytes of each row, and the scales' atoms. Every stage has
+// Roles of a block (12 warps): warp 0 issues the TMA loads, warp 1 copies a stage's scales to tensor memory and issues the matrix instructions, warp 2 owns
+// the tensor memory, warps 4-11 turn accumulators into results. A stage is 256 elements of K: 128 bytes of each row, and the scales' atoms. Every stage has
 // columns of tensor memory of its own for its scales, so that they are not written again before the instructions that read them are done.
 // A tile of 256 tokens leaves room for one accumulator: 16-bit results are taken out whole, into registers, and stored while the next tile is formed.
 //
-// Measured (B200; four times the bf16 library rate is 6.7 PFLOP/s): 8192^3 176 us = 6.3 PFLOP/s at the power limit; a stage's products take 512 cycles and its bytes 594 of shared memory's (2 x 38 KB
-// written and read at 128 a cycle), so shared memory is the next bound. 64 matrices 2048 x 4096: 65536 rows 241 us, 512 rows 53 us = 5.7 TB/s of weights. 997 x 4104 x 2064 12 us; 16 rows,
-// 8192 x 4096, 8 to 12 us warm and cold, most of it set-up and the first stages' way.
+// Measured (B200; four times the bf16 library rate is 6.7 PFLOP/s): 8192^3 176-197 us on different machines = 5.6-6.3 PFLOP/s at the power limit, tensor cores active in 75 % of the cycles; a
+// stage's products take 512 cycles and its bytes 594 of shared memory's (2 x 38 KB written and read at 128 a cycle), so shared memory is the next bound. 64 matrices 2048 x 4096: 65536 rows
+// 241-265 us, 512 rows 53 us = 5.7 TB/s of weights. 997 x 4104 x 2064 12 us; 16 rows, 8192 x 4096, 10 us with cold weights, most of it set-up and the first stages' way.
 #include <atomic>
 
 #include "fp4.cuh"
@@ -21,7 +21,7 @@ namespace hccl {
 namespace experts {
 namespace {
 
-constexpr int CH = 128 /* channels of a tile */;
+constexpr int MM_THREADS = 384, CH = 128 /* channels of a tile */;
 
 template <int TN, int CG, int FORMAT> struct Shape {
     static constexpr int ROWS = TN / CG;                   // token rows that a block holds
@@ -34,8 +34,6 @@ template <int TN, int CG, int FORMAT> struct Shape {
     static constexpr int BY_SMEM = (200 * 1024) / STAGE, BY_TMEM = (512 - ACCS * TN) / SCALE_COLS;
     static constexpr int STAGES = BY_SMEM < BY_TMEM ? BY_SMEM : BY_TMEM;
     static constexpr int SMEM = STAGES * STAGE + 1024;
-    // Warps that take results out; with one accumulator the products wait for them (8192^3: 176 us with 16, 194 with 8).
-    static constexpr int OUT = ACCS == 1 ? 16 : 8, SUBS = OUT / 4, THREADS = 128 + 32 * OUT;
     static_assert(STAGE % 1024 == 0, "operands start on 1024-byte boundaries");
 };
 constexpr int COLS = 512;  // of tensor memory: all of it, one block to an SM
@@ -102,7 +100,7 @@ template <int TN, int CG> __device__ __forceinline__ Tile tile_of(const TilePara
     return r;
 }
 
-template <typename T, int TN, int CG, int FORMAT> __global__ void __launch_bounds__(Shape<TN, CG, FORMAT>::THREADS, 1) hccl_matmul_fp4_tiles(const __grid_constant__ TileParams p) {
+template <typename T, int TN, int CG, int FORMAT> __global__ void __launch_bounds__(MM_THREADS, 1) hccl_matmul_fp4_tiles(const __grid_constant__ TileParams p) {
     using S = Shape<TN, CG, FORMAT>;
     constexpr int ACCS = S::ACCS;
     extern __shared__ char dynamic[];
@@ -165,7 +163,7 @@ template <typename T, int TN, int CG, int FORMAT> __global__ void __launch_bound
     };
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
-        for (int b = 0; b < ACCS; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), S::OUT * CG);
+        for (int b = 0; b < ACCS; b++) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 8 * CG);
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -277,10 +275,10 @@ template <typename T, int TN, int CG, int FORMAT> __global__ void __launch_bound
         const int b = acc % ACCS, quarter = warp & 3, chan = t.chan + quarter * 32 + lane;
         const bool in = chan < p.N;
         const float factor = factor_of(t.group), bias = (in && p.bias) ? p.bias[(long long)t.group * p.N + chan] : 0.f;
-        // The tile's columns in blocks of 32, in turn to the warps of a quarter.
-        constexpr int C = TN < 32 ? TN : 32, U = (TN + 32 * S::SUBS - 1) / (32 * S::SUBS);
+        // The tile's columns in blocks of 32, in turn to the two warps of a quarter (four warps instead: no difference at 256 tokens).
+        constexpr int C = TN < 32 ? TN : 32, U = (TN + 63) / 64;
         constexpr bool WHOLE = ACCS == 1 && sizeof(T) == 2;  // everything out of tensor memory first
-        const int sub = (warp - 4) >> 2;
+        const int half = (warp - 4) >> 2;
         if (p.k_blocks && !mbar_wait(acc_full(b), (acc / ACCS) & 1, &gave_up)) return;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + b * TN;
@@ -321,7 +319,7 @@ template <typename T, int TN, int CG, int FORMAT> __global__ void __launch_bound
             unsigned w[U][C / 2];
 #pragma unroll
             for (int u = 0; u < U; u++) {
-                const int c0 = (S::SUBS * u + sub) * 32;
+                const int c0 = (2 * u + half) * 32;
                 if (c0 < t.rows) {
                     float o[C];
                     fetch(c0, o);
@@ -332,11 +330,11 @@ template <typename T, int TN, int CG, int FORMAT> __global__ void __launch_bound
             free_acc(b);
 #pragma unroll
             for (int u = 0; u < U; u++)
-                if ((S::SUBS * u + sub) * 32 < t.rows) store_words((S::SUBS * u + sub) * 32, w[u]);
+                if ((2 * u + half) * 32 < t.rows) store_words((2 * u + half) * 32, w[u]);
         } else {
 #pragma unroll
             for (int u = 0; u < U; u++) {
-                const int c0 = (S::SUBS * u + sub) * 32;
+                const int c0 = (2 * u + half) * 32;
                 if (c0 >= t.rows) break;
                 float o[C];
                 fetch(c0, o);
@@ -398,7 +396,7 @@ template <typename T, int TN, int CG, int FORMAT> __global__ void __launch_bound
             cluster_sync();
             const float factor = factor_of(tile.group);
             const int total = tile.rows * (CH / 4), lo = total * rank / splits, hi = total * (rank + 1) / splits;  // four channels at a time
-            for (int i = lo + (int)threadIdx.x; i < hi; i += S::THREADS) {
+            for (int i = lo + (int)threadIdx.x; i < hi; i += MM_THREADS) {
                 float sum[4] = {};
                 for (int r = 0; r < splits; r++) {
                     const int4 v = cluster_load(base + 16 * i, r);
@@ -478,7 +476,7 @@ template <typename T, int TN, int CG, int FORMAT> cudaError_t tiles_launch(const
     const long long teams = SMS / team;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((tiles < teams ? tiles : teams) * team));
-    cfg.blockDim = dim3(S::THREADS);
+    cfg.blockDim = dim3(MM_THREADS);
     cfg.dynamicSmemBytes = S::SMEM;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];

@@ -2,7 +2,7 @@
 // Memory and instructions bound it at about the same time: an element is read once and everything that hangs on it stays in one thread's registers, 16 elements of a row, so that a block
 // is one thread's (NVFP4) or two neighbours' (MXFP4). With a routing a token's row is quantised once and written to every place it was sent to.
 //
-// Measured (B200, copy peak 6.5 TB/s): 8192 x 8192 bf16 40 us = 4.4 TB/s (18 instructions an element issue in 82 % of the cycles); 8192 x 4096 to 8 places 51 us = 4.3 TB/s, to 4 places 30; the way
+// Measured (B200, copy peak 6.5 TB/s): 8192 x 8192 bf16 40 us = 4.4 TB/s (16 instructions an element issue in 79 % of the cycles); 8192 x 4096 to 8 places 51 us = 4.3 TB/s, to 4 places 30; the way
 // back, 32768 x 4096 to bf16, 62 us = 5.5 TB/s; 1999 x 2057 fp32, rows on 4 bytes, 8 us there and 15 back.
 #include <algorithm>
 

@@ -679,7 +679,7 @@ hccl_status_t hccl_linear_fp4(const hccl_matmul_fp4_t*, const void* x, int64_t l
  * [experts, H, I], their scales from hccl_fp4_weight_scales (up's, if gated, laid
  * out as 2 * experts groups of I rows, which for I a multiple of 128 is the same). Activations are not rounded to 4 bits: they enter the products as sums of eight such numbers, which leaves 2^-22 of the largest
  * of up to 1024 neighbours; sums, u and h are FP32. A row with an infinity or a NaN gives NaN. Choices without an expert add nothing; a token without any gets 0.
- * Reads the routing's weights, offsets and source. tokens <= HCCL_MAX_FEW_TOKENS; H and I from 1 to HCCL_MAX_FP4_K. scratch: hccl_expert_layer_scratch_bytes, 128-byte aligned, contents
+ * Reads the routing's weights, offsets and source; offsets may begin after 0 (some of the experts of a larger routing: the rows of the others add nothing). tokens <= HCCL_MAX_FEW_TOKENS; H and I from 1 to HCCL_MAX_FP4_K. scratch: hccl_expert_layer_scratch_bytes, 128-byte aligned, contents
  * arbitrary, not shared by calls in flight at once. dev_status as in hccl_matmul_i8_t. */
 #define HCCL_MAX_FEW_TOKENS 64
 typedef enum { HCCL_ACT_SILU = 0, HCCL_ACT_GELU = 1, HCCL_ACT_RELU = 2 } hccl_act_t; /* x sigmoid(x); x Phi(x), Phi of the normal distribution; max(x, 0) */

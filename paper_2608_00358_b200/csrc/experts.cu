@@ -2,7 +2,6 @@
 #include <cstring>
 
 #include "checks.h"
-#include "fp4.cuh"
 
 using namespace hccl::experts;
 

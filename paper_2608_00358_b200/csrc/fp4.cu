@@ -305,7 +305,6 @@ hccl_status_t hccl_expert_layer_fp4(const hccl_experts_fp4_t* e, const void* x, 
     p.y = y;
     p.offsets = r->offsets;
     p.source = r->source;
-    p.slots = r->slots;
     p.weights = r->weights;
     p.up = e->up;
     p.up_scale = (const uint8_t*)e->up_scale;

@@ -154,7 +154,7 @@ struct FewFp4 {        // a whole expert layer for few tokens
     int top_k, experts, format, act, gated;
     const void* x;
     void* y;
-    const int *ids, *offsets, *source, *slots;
+    const int *offsets, *source;
     const float* weights;
     const uint8_t *up, *up_scale, *down, *down_scale;
     const float *up_wide, *down_wide, *up_bias, *down_bias;

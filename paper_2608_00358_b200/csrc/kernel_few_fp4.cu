@@ -197,12 +197,16 @@ __device__ __forceinline__ Chunk unpacked(int c) {
     c = __shfl_sync(0xffffffffu, c, 0);  // (the same in all lanes, and by way of the shuffle known to be)
     return {c >> 16, c >> 4 & 0xfff, c & 15};
 }
+// Rows in expert order that have an expert. They may begin later than row 0 (an expert's share of a larger routing).
+__device__ __forceinline__ int first_row(const FewParams& p) { return min(p.rows, max(0, p.offsets[0])); }
+__device__ __forceinline__ int end_row(const FewParams& p) { return min(p.rows, max(0, p.offsets[p.experts])); }
 template <typename Each> __device__ __forceinline__ int list_chunks(const FewParams& p, int lane, const Each& each) {
     int run = 0;
+    const int first = first_row(p), end = end_row(p);
     for (int b = 0; b < p.experts; b += 32) {
         const int g = b + lane;
         int lo = 0, hi = 0;
-        if (g < p.experts) lo = max(0, p.offsets[g]), hi = min(p.rows, p.offsets[g + 1]);
+        if (g < p.experts) lo = max(first, p.offsets[g]), hi = min(end, p.offsets[g + 1]);
         const int n = max(0, (hi - lo + ROWS - 1) / ROWS);
         int inc = n;
 #pragma unroll
@@ -335,7 +339,8 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     const int of_chunk = parts_of_k * halves * p.chan_tiles, of_part = parts_of_k * halves * GROUP;  // units; a chunk's last part may have fewer
     const long long units = (long long)chunks * of_chunk;
     const int u0 = (int)(units * blockIdx.x / blocks), u1 = (int)(units * (blockIdx.x + 1) / blocks);
-    const int filled = min(p.rows, max(0, p.offsets[p.experts]));  // rows that have sums: how far apart the parts of K lie
+    // Rows that have sums: how far apart the parts of K lie. Chunks of 8 hold them all, whatever the offsets are (they telescope), which is what the scratch's size goes by.
+    const int first = first_row(p), filled = max(0, end_row(p) - first);
 
     const auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
     const auto place = [&](Unit& t) { t.half = t.index >= t.group, t.tile = t.part * GROUP + t.index - t.half * t.group; };
@@ -380,9 +385,9 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
 
     if (warp == 0) {
         for (Unit t = unit_at(u0); t.u < u1; advance(t)) {
-            const int n = stages_of(t.kc), first = stage_of(t.kc);
+            const int n = stages_of(t.kc), kb0 = stage_of(t.kc);
             for (int i = 0; i < n; i++, it++) {
-                const int s = it % S::STAGES, kb = first + i;
+                const int s = it % S::STAGES, kb = kb0 + i;
                 if (!mbar_wait(empty(s), ((it / S::STAGES) & 1) ^ 1, &gave_up)) break;
                 if (elected()) {
                     const uint32_t at = base + s * S::STAGE;
@@ -400,7 +405,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
         if (elected()) copy_scales(tmem + S::X_SCALES, smem_addr(scale_atom));
         __syncwarp();
         for (Unit t = unit_at(u0); t.u < u1 && ok; advance(t), acc++) {
-            const int n = stages_of(t.kc), first = stage_of(t.kc), b = acc & 1, half = turn & 1;
+            const int n = stages_of(t.kc), kb0 = stage_of(t.kc), b = acc & 1, half = turn & 1;
             const uint32_t pieces = base + S::RING + half * S::PART;
             const uint32_t desc = instruction(t.c.rows, FORMAT);
             if (begins(t)) {
@@ -412,7 +417,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (int i = 0; i < n; i++, it++) {
-                const int s = it % S::STAGES, left = min(4, steps - 4 * (first + i));
+                const int s = it % S::STAGES, left = min(4, steps - 4 * (kb0 + i));
                 ok = mbar_wait(full(s), (it / S::STAGES) & 1, &gave_up);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -465,7 +470,7 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
                 if (ends(t)) mbar_arrive(part_empty(half));
             }
             if (ends(t)) turn++;
-            float* out = p.sums + ((long long)t.kc * filled + t.c.row) * p.width + t.half * p.half + chan;
+            float* out = p.sums + ((long long)t.kc * filled + t.c.row - first) * p.width + t.half * p.half + chan;
             if (in)
 #pragma unroll
                 for (int r = 0; r < ROWS; r++)
@@ -556,17 +561,17 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
                 if (threadIdx.x == 0) job_row[jobs] = c.row + r, job_part[jobs] = part, top_of[0][jobs] = 0;
         }
         __syncthreads();
-        const auto columns = [&](int job, int* first) {  // up to the end of the last instruction's 64 elements
-            *first = job_part[job] * WIDE;
-            return (min(WIDE, p.I - *first) + 63) & ~63;
+        const auto columns = [&](int job, int* from) {  // up to the end of the last instruction's 64 elements
+            *from = job_part[job] * WIDE;
+            return (min(WIDE, p.I - *from) + 63) & ~63;
         };
 #pragma unroll 1
         for (int i = (int)threadIdx.x; i < jobs * (WIDE / 4); i += UP_THREADS) {
-            int first;
+            int from;
             const int job = i / (WIDE / 4), col = i % (WIDE / 4) * 4;
-            if (col >= columns(job, &first)) continue;
-            const int k = first + col;
-            const float4 x = activated(k < p.half ? (const float4*)(p.sums + (long long)job_row[job] * p.width + k) : nullptr, (long long)filled * p.width / 4, p.gated ? p.half / 4 : 0, parts_of_k, p.act);
+            if (col >= columns(job, &from)) continue;
+            const int k = from + col;
+            const float4 x = activated(k < p.half ? (const float4*)(p.sums + (long long)(job_row[job] - first) * p.width + k) : nullptr, (long long)filled * p.width / 4, p.gated ? p.half / 4 : 0, parts_of_k, p.act);
             float v[4] = {x.x, x.y, x.z, x.w};
             unsigned top = 0;
 #pragma unroll
@@ -580,13 +585,13 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
         __syncthreads();
 #pragma unroll 1
         for (int i = (int)threadIdx.x; i < jobs * (WIDE / EACH); i += UP_THREADS) {
-            int first;
+            int from;
             const int job = i / (WIDE / EACH), col = i % (WIDE / EACH) * EACH;
-            if (col >= columns(job, &first)) continue;
+            if (col >= columns(job, &from)) continue;
             float factor, back;
             row_factor(top_of[0][job], &factor, &back);
             if (col == 0) p.unscale[(long long)job_row[job] * p.down_parts + job_part[job]] = back;
-            make_pieces(h[2 * i], h[2 * i + 1], factor, (char*)p.pieces + (long long)job_row[job] * PIECES * p.pitch + (first + col) / 2, p.pitch, 0, 0);
+            make_pieces(h[2 * i], h[2 * i + 1], factor, (char*)p.pieces + (long long)job_row[job] * PIECES * p.pitch + (from + col) / 2, p.pitch, 0, 0);
         }
         __syncthreads();
     }

@@ -444,6 +444,27 @@ def test_layer_in_place_with_an_expert_twice_and_rows_that_begin_later():
     assert few(z, routing_of(np.array([[2], [0], [1]]), 4), out=z) is z and torch.equal(z, once)
 
 
+@pytest.mark.parametrize("lo,hi", [(63, 64), (20, 23), (0, 2)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_layer_of_a_share_of_a_larger_routing(fmt, lo, hi):
+    """Some of the experts, with the offsets of all choices' rows: the same bits as those choices alone, the others being none. Many parts of K, and far more rows than the share has."""
+    rng = gen(14)
+    T, k, E, H, I = 64, 32, 64, 4100, 40
+    ids = some_ids(rng, T, k, E)
+    w = rng.standard_normal((T, k)).astype(np.float32)
+    up, _, _, _ = make_linear(rng, (hi - lo, 2 * I, H), fmt, False)
+    down, _, _, _ = make_linear(rng, (hi - lo, H, I), fmt, False)
+    up.tensor_scale.mul_(2.0 ** -10)
+    few = fp4.FewTokens(up, down)
+    x = torch.from_numpy(rng.standard_normal((T, H)).astype(np.float32)).cuda()
+    r = routing_of(ids, E, w)
+    share = ex.Routing(r.ids, r.weights, r.counts[lo:hi].clone(), r.offsets[lo:hi + 1].clone(), r.slots, r.source)
+    alone = routing_of(np.where((ids >= lo) & (ids < hi), ids - lo, -1), hi - lo, w)
+    y = few(x, share)
+    assert y.any() and torch.equal(y, few(x, alone))
+    few.check()
+
+
 def test_layer_refusals():
     few = small_layer()
     rng = gen(9)

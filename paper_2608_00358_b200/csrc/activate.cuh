@@ -11,28 +11,16 @@ __device__ __forceinline__ float reciprocal(float x) {
     asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// 1 / (1 + exp(-x)). SHORT: for results of 16 bits; the exponential's argument is rounded once, which costs |x| 2^-24
-// of the result, where expf takes four instructions to save that.
-template <bool SHORT> __device__ __forceinline__ float logistic(float x) {
-    if constexpr (SHORT) {
-        float e, r;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.44269504f));
-        // the quarter keeps the quotient of the largest exponentials a normal number
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaf(e, 0.25f, 0.25f)));
-        return r * 0.25f;
-    } else {
-        return reciprocal(1.f + expf(-x));
-    }
-}
-template <bool SHORT = false> __device__ __forceinline__ float activation(int act, float g) {
-    if (act == HCCL_ACT_SILU) return g * logistic<SHORT>(g);
+__device__ __forceinline__ float logistic(float x) { return reciprocal(1.f + expf(-x)); }  // 1 / (1 + exp(-x))
+__device__ __forceinline__ float activation(int act, float g) {
+    if (act == HCCL_ACT_SILU) return g * logistic(g);
     if (act == HCCL_ACT_GELU) return g * normcdff(g);
     return g > 0.f || g != g ? g : 0.f;
 }
 // And its derivative; of the rectifier at 0: 0.
-template <bool SHORT> __device__ __forceinline__ void activation_slope(int act, float g, float* a, float* slope) {
+__device__ __forceinline__ void activation_slope(int act, float g, float* a, float* slope) {
     if (act == HCCL_ACT_SILU) {
-        const float s = logistic<SHORT>(g);
+        const float s = logistic(g);
         *a = g * s;
         *slope = fmaf(*a, 1.f - s, s);
     } else if (act == HCCL_ACT_GELU) {

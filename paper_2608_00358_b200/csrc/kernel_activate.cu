@@ -4,8 +4,8 @@
 // The generator is Philox-4x32-10 (Salmon, Moraes, Dror, Shaw 2011): four 32-bit words from a 128-bit counter and a 64-bit key in ten rounds of two 32 x 32 bit
 // products. Element i of the result (row * I + column) takes word i % 4 of the counter (i / 4, call); it is kept if the word is at least p 2^32.
 //
-// Measured (B200, copy peak 6.5 TB/s): 32768 x 2048 bf16 without dropout 64 us = 6.3 TB/s, gradient 103 = 6.5; with dropout 105 and 125: 40 instructions
-// an element issue in 70 % of the cycles, about 10 of them the generator's (18 wide products for four elements, and what joins them).
+// Measured (B200, copy peak 6.5 TB/s): SiLU, 32768 x 2048 bf16 without dropout 63 us = 6.4 TB/s, gradient 97 = 6.9; with dropout 94 and 110 (GELU 117 and 131): 33 instructions
+// an element issue in 65 % of the cycles, about 10 of them the generator's (18 wide products for four elements, and what joins them).
 #include <algorithm>
 
 #include "activate.cuh"
@@ -37,7 +37,11 @@ struct Generator {
     }
     __device__ __forceinline__ Words at(unsigned long long counter) {
         if ((unsigned)(counter >> 32) != upper) set((unsigned)(counter >> 32));
-        const unsigned long long first = (unsigned long long)(unsigned)counter * 0xD2511F53u;
+        return beside((unsigned)counter);
+    }
+    // Of a counter whose upper half is that of the last one.
+    __device__ __forceinline__ Words beside(unsigned counter) const {
+        const unsigned long long first = (unsigned long long)counter * 0xD2511F53u;
         const unsigned d2 = (unsigned)(first >> 32) ^ (unsigned)(call >> 32) ^ k[0][1], d3 = (unsigned)first;
         const unsigned long long second = (unsigned long long)d2 * 0xCD9E8D57u;
         unsigned x0 = (unsigned)(second >> 32) ^ c1 ^ k[1][0], x1 = (unsigned)second, x2 = (unsigned)(a >> 32) ^ d3 ^ k[1][1], x3 = (unsigned)a;
@@ -53,14 +57,14 @@ struct Generator {
     }
 };
 
-// The random words of N neighbouring elements, N a multiple of 4, the first being element `at` of the result. A counter's words begin within the
-// elements where I is no multiple of 4.
-template <int N> __device__ __forceinline__ void words(Generator& gen, unsigned long long at, unsigned (&f)[N]) {
-    const unsigned o = (unsigned)at & 3u;
+// The random words of N neighbouring elements, N a multiple of 4, the first being element `at` of the result. WHOLE: `at` is a multiple of N; otherwise a counter's words may
+// begin within the elements.
+template <int N, bool WHOLE> __device__ __forceinline__ void words(Generator& gen, unsigned long long at, unsigned (&f)[N]) {
+    const unsigned o = WHOLE ? 0u : (unsigned)at & 3u;
     if (o == 0) {
 #pragma unroll
         for (int j = 0; j < N; j += 4) {
-            const Words w = gen.at(at / 4 + j / 4);
+            const Words w = WHOLE && j ? gen.beside((unsigned)(at / 4) + j / 4) : gen.at(at / 4 + j / 4);
 #pragma unroll
             for (int i = 0; i < 4; i++) f[j + i] = w.w[i];
         }
@@ -76,16 +80,43 @@ template <int N> __device__ __forceinline__ void words(Generator& gen, unsigned 
     }
 }
 
-// 4 / (1 + exp(-x)) for results of 16 bits, as logistic<true>.
-__device__ __forceinline__ Two four_logistic(Two x) {
+// For results of 16 bits. The exponentials' arguments are rounded once, which costs |x| 2^-24 of the result, where expf takes four instructions to save that.
+__device__ __forceinline__ Two exponentials(Two x) {  // 2^x
     float a, b;
-    (x * Two(-1.44269504f)).get(a, b);
+    x.get(a, b);
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
-    fma2(Two(a, b), Two(0.25f), Two(0.25f)).get(a, b);
+    return Two(a, b);
+}
+__device__ __forceinline__ Two reciprocals(Two x) {
+    float a, b;
+    x.get(a, b);
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
     return Two(a, b);
+}
+// 4 / (1 + exp(-x)): the quarter keeps the quotient of the largest exponentials a normal number.
+__device__ __forceinline__ Two four_logistic(Two x) { return reciprocals(fma2(exponentials(x * Two(-1.44269504f)), Two(0.25f), Two(0.25f))); }
+// The normal distribution, and exp(-x^2 / 2). Below 0 the distribution is exp(-x^2 / 2) R(|x|); R, which falls from 1/2 as slowly as 1 / |x|, is a polynomial of degree 7 in 1 / (1 + 0.35 |x|), by
+// least squares on Chebyshev's points, weighted anew until the relative error was even: 2^-21.5 up to 14.6, where the exponential leaves the normal numbers. (normcdff with expf
+// takes four times the instructions, 32768 x 2048 bf16 with dropout 221 us, gradient 263.)
+__device__ __forceinline__ Two normal(Two x, Two* bell) {
+    float a, b;
+    x.get(a, b);
+    const Two t = reciprocals(fma2(Two(fabsf(a), fabsf(b)), Two(0.35f), Two(1.f)));
+    Two r = fma2(Two(4.88590253e-02f), t, Two(-2.01797222e-01f));
+    r = fma2(r, t, Two(2.40131299e-01f));
+    r = fma2(r, t, Two(-1.65972006e-02f));
+    r = fma2(r, t, Two(1.55758767e-01f));
+    r = fma2(r, t, Two(1.33409697e-01f));
+    r = fma2(r, t, Two(1.40262654e-01f));
+    r = fma2(r, t, Two(-2.68791464e-05f));
+    *bell = exponentials(x * x * Two(-0.72134752f));
+    const Two below = *bell * r;
+    float u, v, c, d;
+    below.get(u, v);
+    fma2(below, Two(-1.f), Two(1.f)).get(c, d);
+    return Two(a < 0.f ? u : c, b < 0.f ? v : d);
 }
 
 // N elements as they lie in memory, V to an access; from `left` on nothing is read.
@@ -135,115 +166,129 @@ template <typename T, int N, int V, bool GRAD, int ACT> __global__ void __launch
     extern __shared__ __align__(16) uint4 ring[];  // [RING][INPUTS][threads]
     const int teams = THREADS / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team;
     const long long rows = p.offsets ? min((long long)p.offsets[p.groups], p.M) : p.M;
-    // A thread has `n` pieces of each of its rows.
-    const long long step = (long long)gridDim.x * teams, across = (long long)team * N, c0 = (long long)rank * N;
+    // A thread has `n` pieces of each of its rows, the last with `end` elements.
+    const long long step = (long long)gridDim.x * teams, across = (long long)team * N, c0 = (long long)rank * N, r0 = (long long)blockIdx.x * teams + mine;
     if (c0 >= p.I) return;
     Generator generator(p.drop ? (unsigned long long)p.seed[0] : 0, p.drop ? (unsigned long long)p.seed[1] : 0);
-    const int n = (int)((p.I - c0 + across - 1) / across);
-    const auto left_of = [&](long long c) { return RINGED ? N : (int)min((long long)N, p.I - c); };
+    const int n = (int)((p.I - c0 + across - 1) / across), end = (int)min((long long)N, p.I - c0 - (n - 1) * across);
+    const long long mine_read = rows > r0 ? (rows - r0 + step - 1) / step : 0;
+    const int pieces = (int)(mine_read * n);
     Raw<T, N, V> raw[INPUTS] = {};  // gate, other half, gradient
 
-    // Where the loads are (ringed: ahead of the work).
-    long long fr = (long long)blockIdx.x * teams + mine;
-    int fk = 0, turn = 0;
+    // Where the loads are (ringed: ahead of the work), and where the work is. From piece to piece it is `across` on, at a row's end a jump: indices formed anew for
+    // each piece took a sixth of the instructions.
+    const long long back = (n - 1) * across;
+    const T *fx = (const T*)p.x + r0 * p.ldx + c0, *fd = (const T*)p.dy + r0 * p.ldy + c0;
+    const long long x_jump = step * p.ldx - back, d_jump = step * p.ldy - back, o_jump = step * p.ldo - back, a_jump = step * p.I - back;
+    T* out = (T*)p.out + r0 * p.ldo + c0;
+    unsigned long long at = (unsigned long long)(r0 * p.I + c0);
+    int fk = 0, ahead = 0, turn = 0, k = 0;
     const auto fetch = [&](int slot) {
-        if (fr < rows) {
-            const long long c = c0 + fk * across;
-            const T* const at[3] = {(const T*)p.x + fr * p.ldx + c, (const T*)p.x + fr * p.ldx + p.I + c, (const T*)p.dy + fr * p.ldy + c};
+        if (ahead++ < pieces) {
+            const T* const from[3] = {fx, fx + p.I, fd};
 #pragma unroll
             for (int i = 0; i < INPUTS; i++) {
                 if (i == 1 && !p.gated) continue;
                 if constexpr (RINGED)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(ring + (slot * INPUTS + i) * THREADS + threadIdx.x)), "l"(at[i]) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(ring + (slot * INPUTS + i) * THREADS + threadIdx.x)), "l"(from[i]) : "memory");
                 else
-                    raw[i].load(at[i], left_of(c));
+                    raw[i].load(from[i], fk == n - 1 ? end : N);
             }
         }
         if (RINGED) asm volatile("cp.async.commit_group;" ::: "memory");
-        if (++fk == n) fk = 0, fr += step;
+        const bool over = ++fk == n;
+        if (over) fk = 0;
+        fx += over ? x_jump : across;
+        if (GRAD) fd += over ? d_jump : across;
     };
     if (RINGED)
 #pragma unroll
         for (int i = 0; i < RING - 1; i++) fetch(i);
-    for (long long r = (long long)blockIdx.x * teams + mine; r < p.M; r += step) {
-        T* const out = (T*)p.out + r * p.ldo;
-        const unsigned long long at = (unsigned long long)r * (unsigned long long)p.I;
-        for (int k = 0; k < n; k++) {
-            const long long c = c0 + k * across;
-            const int left = left_of(c);
-            fetch(turn == 0 ? RING - 1 : turn - 1);
-            if constexpr (RINGED) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
+    for (int i = 0; i < pieces; i++) {
+        fetch(turn == 0 ? RING - 1 : turn - 1);
+        if constexpr (RINGED) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
 #pragma unroll
-                for (int i = 0; i < INPUTS; i++) {
-                    const uint4 v = ring[(turn * INPUTS + i) * THREADS + threadIdx.x];
-                    raw[i].q[0].raw = v;
-                }
-                turn = turn == RING - 1 ? 0 : turn + 1;
-            }
-            float g[N], u[N], d[N];
-            unsigned word[N];
-            if (r >= rows) {
+            for (int j = 0; j < INPUTS; j++) raw[j].q[0].raw = ring[(turn * INPUTS + j) * THREADS + threadIdx.x];
+            turn = turn == RING - 1 ? 0 : turn + 1;
+        }
+        const int left = RINGED || k != n - 1 ? N : end;
+        float g[N], u[N], d[N];
+        unsigned word[N];
+        if (p.drop) words<N, RINGED>(generator, at, word);
+        else
 #pragma unroll
-                for (int j = 0; j < N; j++) g[j] = 0.f;
-                store<T, N, V>(out + c, left, g);
-                if (GRAD && p.gated) store<T, N, V>(out + p.I + c, left, g);
-                continue;
-            }
-            if (p.drop) words<N>(generator, at + (unsigned long long)c, word);
-            else
+            for (int j = 0; j < N; j++) word[j] = 0xffffffffu;
+        raw[0].get(g);
+        if (p.gated) raw[1].get(u);
+        else
 #pragma unroll
-                for (int j = 0; j < N; j++) word[j] = 0xffffffffu;
-            raw[0].get(g);
-            if (p.gated) raw[1].get(u);
-            else
+            for (int j = 0; j < N; j++) u[j] = 1.f;
+        if constexpr (GRAD) raw[INPUTS - 1].get(d);
+        // (What is dropped is 0, whatever it was. Large numbers meet the small factor first: -1e30 of a gate and 1e30 of the other half are 0, not infinity times 0.)
+        if constexpr (SHORT && ACT != HCCL_ACT_RELU) {
 #pragma unroll
-                for (int j = 0; j < N; j++) u[j] = 1.f;
-            if constexpr (GRAD) raw[INPUTS - 1].get(d);
-            // (what is dropped is 0, whatever it was)
-            if constexpr (SHORT && ACT == HCCL_ACT_SILU) {
-#pragma unroll
-                for (int j = 0; j < N; j += 2) {
-                    const Two x(g[j], g[j + 1]), o(u[j], u[j + 1]), s = four_logistic(x);
-                    if constexpr (!GRAD) {
-                        (x * (o * Two(0.25f * p.keep)) * s).get(g[j], g[j + 1]);
-                    } else {
-                        const Two sig = s * Two(0.25f), act = x * sig, dd = Two(d[j], d[j + 1]) * Two(p.keep);
-                        const Two slope = fma2(act, fma2(sig, Two(-1.f), Two(1.f)), sig);
-                        (dd * o * slope).get(g[j], g[j + 1]);
-                        (dd * act).get(u[j], u[j + 1]);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; j++) {
-                    if constexpr (!GRAD) {
-                        g[j] = activation<SHORT>(ACT, g[j]) * (u[j] * p.keep);
-                    } else {
-                        float a, slope;
-                        activation_slope<SHORT>(ACT, g[j], &a, &slope);
-                        const float dd = d[j] * p.keep;
-                        g[j] = dd * u[j] * slope;
-                        u[j] = dd * a;
-                    }
+            for (int j = 0; j < N; j += 2) {
+                const Two x(g[j], g[j + 1]), o(u[j], u[j + 1]);
+                Two f, bell;  // act(x) = x f
+                if constexpr (ACT == HCCL_ACT_SILU) f = four_logistic(x);
+                else f = normal(x, &bell);
+                if constexpr (!GRAD) {
+                    (x * (f * Two(ACT == HCCL_ACT_SILU ? 0.25f * p.keep : p.keep)) * o).get(g[j], g[j + 1]);
+                } else {
+                    if constexpr (ACT == HCCL_ACT_SILU) f = f * Two(0.25f);
+                    const Two act = x * f, dd = Two(d[j], d[j + 1]) * Two(p.keep);
+                    Two slope;
+                    if constexpr (ACT == HCCL_ACT_SILU) slope = fma2(act, fma2(f, Two(-1.f), Two(1.f)), f);
+                    else slope = fma2(x * Two(0.39894228f), bell, f);
+                    (dd * slope * o).get(g[j], g[j + 1]);
+                    (dd * act).get(u[j], u[j + 1]);
                 }
             }
+        } else {
 #pragma unroll
             for (int j = 0; j < N; j++) {
-                g[j] = word[j] >= p.threshold ? g[j] : 0.f;
-                if (GRAD) u[j] = word[j] >= p.threshold ? u[j] : 0.f;
+                if constexpr (!GRAD) {
+                    g[j] = activation(ACT, g[j]) * (u[j] * p.keep);
+                } else {
+                    float a, slope;
+                    activation_slope(ACT, g[j], &a, &slope);
+                    const float dd = d[j] * p.keep;
+                    g[j] = dd * slope * u[j];
+                    u[j] = dd * a;
+                }
             }
-            store<T, N, V>(out + c, left, g);
-            if (GRAD && p.gated) store<T, N, V>(out + p.I + c, left, u);
         }
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            g[j] = word[j] >= p.threshold ? g[j] : 0.f;
+            if (GRAD) u[j] = word[j] >= p.threshold ? u[j] : 0.f;
+        }
+        store<T, N, V>(out, left, g);
+        if (GRAD && p.gated) store<T, N, V>(out + p.I, left, u);
+        const bool over = ++k == n;
+        if (over) k = 0;
+        out += over ? o_jump : across;
+        at += over ? a_jump : across;
     }
+    // (out is where the rows that are not read begin)
+    float none[N];
+#pragma unroll
+    for (int j = 0; j < N; j++) none[j] = 0.f;
+    for (long long r = r0 + mine_read * step; r < p.M; r += step)
+        for (k = 0; k < n; k++) {
+            const int left = k == n - 1 ? end : N;
+            store<T, N, V>(out, left, none);
+            if (GRAD && p.gated) store<T, N, V>(out + p.I, left, none);
+            out += k == n - 1 ? o_jump : across;
+        }
 }
 
 template <typename T, int N, int V, bool GRAD, int ACT> cudaError_t launch(const ActivateParams& p, cudaStream_t s) {
     const long long pieces = (p.I + N - 1) / N;
     int team = 32;
     while (team < THREADS && team < pieces) team *= 2;
-    // Two rounds of blocks where each forms keys first, eight without (32768 x 2048 bf16 without dropout: 64 us, with two 71; with dropout 105, with eight 109).
+    // Two rounds of blocks where each forms keys first, eight without (32768 x 2048 bf16 without dropout: 64 us, with two 71).
     const long long blocks = (p.M + THREADS / team - 1) / (THREADS / team);
     hccl_activate_rows<T, N, V, GRAD, ACT><<<(unsigned)std::max(1ll, std::min(blocks, (long long)SMS * (p.drop ? 8 : 32))), THREADS, V == N ? RING * (GRAD ? 3 : 2) * THREADS * 16 : 0, s>>>(p, team);
     return cudaGetLastError();

@@ -103,6 +103,41 @@ def test_dropped_elements_are_zero_whatever_they_were():
     assert (np.isnan(dx) == np.concatenate([keep, keep], 1)).all()
 
 
+@pytest.mark.parametrize("p", [0.0, 0.3])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("dt", [BF16, F16])
+def test_every_16_bit_number(dt, act, p):
+    """Gates of all finite 16-bit numbers: values, and both gradients, against 64 bits. In 32 bits exp(-x) is infinite below -88.73 and the activation then 0 in the place of at most 88.73 *
+    2^-128 = 2.6e-37, which is what its slope leaves out too."""
+    g = torch.arange(-(2 ** 15), 2 ** 15, dtype=torch.int32).to(torch.int16).view(dt)
+    g = g[torch.isfinite(g.float())].reshape(-1, 64)
+    if dt == BF16:
+        g = g.clamp(-1e37, 1e37)  # (so that 1 / (1 - p) leaves the result in the range)
+    else:
+        g = g.clamp(-2e4, 2e4)
+    M, I = g.shape
+    x = torch.cat((g, torch.ones_like(g)), 1)
+    key = (77, 78)
+    f = np.full((M, I), 1 / (1 - p)) * (ref.keep(M, I, p, key) if p else 1)
+    seed = seed_of(*key) if p else None
+    dy = torch.ones((M, I), dtype=dt)
+    x64 = x.double().numpy()
+    with np.errstate(over="ignore"):  # (exp of a large negative gate: the quotient is then 0)
+        y, tol = forward(x64, act, True, f, dt)
+        dx, dtol = backward(dy.double().numpy(), x64, act, True, f, dt)
+    within(activate(x.cuda(), act, True, p, seed), y, tol + 2.7e-37 * f)
+    within(activate_backward(dy.cuda(), x.cuda(), act, True, p, seed), dx, dtol + 2.7e-37 * np.concatenate([f, f], 1))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_a_closed_gate_stays_closed_before_large_numbers(act, dt):
+    g = torch.full((4, 64), -1e30, device="cuda", dtype=dt)
+    x = torch.cat((g, -g), 1)
+    assert not activate(x, act).any()
+    assert not activate_backward(torch.full_like(g, 1e30), x, act).any()
+
+
 def test_ends_of_the_range():
     for act in ("silu", "gelu", "relu"):
         g = torch.tensor([[-1e38, -200.0, -30.0, -9.0, 0.0, -0.0, 9.0, 30.0, 200.0, 1e30]], device="cuda")

@@ -4,8 +4,8 @@
 // The generator is Philox-4x32-10 (Salmon, Moraes, Dror, Shaw 2011): four 32-bit words from a 128-bit counter and a 64-bit key in ten rounds of two 32 x 32 bit
 // products. Element i of the result (row * I + column) takes word i % 4 of the counter (i / 4, call); it is kept if the word is at least p 2^32.
 //
-// Measured (B200, copy peak 6.5 TB/s): SiLU, 32768 x 2048 bf16 without dropout 63 us = 6.4 TB/s, gradient 97 = 6.9; with dropout 94 and 110 (GELU 117 and 131): 33 instructions
-// an element issue in 65 % of the cycles, about 10 of them the generator's (18 wide products for four elements, and what joins them).
+// Measured (B200, copy peak 6.5 TB/s): SiLU, 32768 x 2048 bf16 without dropout 62 us, gradient 101; with dropout 92 and 105 (GELU 112 and 128): 32 instructions
+// an element issue in two thirds of the cycles, about 10 of them the generator's (18 wide products for four elements, and what joins them).
 #include <algorithm>
 
 #include "activate.cuh"
@@ -14,7 +14,7 @@ namespace hccl {
 namespace experts {
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 128;
 
 struct Words {
     unsigned w[4];
@@ -168,8 +168,10 @@ template <typename T, int N, int V, bool GRAD, int ACT> __global__ void __launch
     const long long rows = p.offsets ? min((long long)p.offsets[p.groups], p.M) : p.M;
     // A thread has `n` pieces of each of its rows, the last with `end` elements.
     const long long step = (long long)gridDim.x * teams, across = (long long)team * N, c0 = (long long)rank * N, r0 = (long long)blockIdx.x * teams + mine;
+    // (the same in all lanes, and by way of the shuffle known to be: the rounds' keys then take none of a thread's registers; 94 -> 91 us)
+    const auto same = [](unsigned long long v) { return (unsigned long long)__shfl_sync(0xffffffffu, (unsigned)(v >> 32), 0) << 32 | __shfl_sync(0xffffffffu, (unsigned)v, 0); };
+    Generator generator(same(p.drop ? (unsigned long long)p.seed[0] : 0), same(p.drop ? (unsigned long long)p.seed[1] : 0));
     if (c0 >= p.I) return;
-    Generator generator(p.drop ? (unsigned long long)p.seed[0] : 0, p.drop ? (unsigned long long)p.seed[1] : 0);
     const int n = (int)((p.I - c0 + across - 1) / across), end = (int)min((long long)N, p.I - c0 - (n - 1) * across);
     const long long mine_read = rows > r0 ? (rows - r0 + step - 1) / step : 0;
     const int pieces = (int)(mine_read * n);
@@ -288,9 +290,9 @@ template <typename T, int N, int V, bool GRAD, int ACT> cudaError_t launch(const
     const long long pieces = (p.I + N - 1) / N;
     int team = 32;
     while (team < THREADS && team < pieces) team *= 2;
-    // Two rounds of blocks where each forms keys first, eight without (32768 x 2048 bf16 without dropout: 64 us, with two 71).
+    // Fewer rounds of blocks where each forms keys first. (Blocks of 128 threads against 256: 1003 x 1410 fp32 10.4 and 12.4 us, 32768 x 2048 bf16 92 and 91, its gradient 105 and 109.)
     const long long blocks = (p.M + THREADS / team - 1) / (THREADS / team);
-    hccl_activate_rows<T, N, V, GRAD, ACT><<<(unsigned)std::max(1ll, std::min(blocks, (long long)SMS * (p.drop ? 8 : 32))), THREADS, V == N ? RING * (GRAD ? 3 : 2) * THREADS * 16 : 0, s>>>(p, team);
+    hccl_activate_rows<T, N, V, GRAD, ACT><<<(unsigned)std::max(1ll, std::min(blocks, (long long)SMS * (p.drop ? 12 : 64))), THREADS, V == N ? RING * (GRAD ? 3 : 2) * THREADS * 16 : 0, s>>>(p, team);
     return cudaGetLastError();
 }
 

@@ -17,8 +17,8 @@
 //
 // All sums have a fixed order: results repeat bit for bit.
 //
-// Measured (B200, copy peak 6.5 TB/s): one token through 8 of 64 experts of 4096 x 2048 35 us in replays of a graph, 45 after a flush of the caches; 8 experts of 8192 x 8192, one token 103 + 53 us
-// = 5.9 TB/s of weights and 8 tokens 136 + 55; 19 tokens through 4 of 60 experts of 2056 x 1416 67 us. Of the 35 us the weights take 17 at the copy rate. The rest are latencies in a row: 5 until the first pieces are
+// Measured (B200, copy peak 6.5 TB/s): one token through 8 of 64 experts of 4096 x 2048 36 us in replays of a graph, 47 after a flush of the caches; 8 experts of 8192 x 8192, one token 103 + 53 us
+// = 5.9 TB/s of weights and 8 tokens 136 + 55; 19 tokens through 4 of 60 experts of 2056 x 1416 67 us. Of the 36 us the weights take 17 at the copy rate. The rest are latencies in a row: 5 until the first pieces are
 // there, 1.5 to count, 5 for a block to finish others' sums, 3 to the second kernel's first product, 4 for its last sums, and a memory set and two launches.
 #include <algorithm>
 #include <atomic>

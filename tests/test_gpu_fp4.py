@@ -227,6 +227,30 @@ def test_product_over_experts(T, E, k, N, K, dt, fmt):
     lin.check()
 
 
+@pytest.mark.parametrize("lo,hi", [(5, 6), (2, 4), (0, 1)])
+@pytest.mark.parametrize("T,K", [(9, 136), (700, 264)])
+def test_product_of_a_share_of_a_larger_routing(T, K, lo, hi):
+    """Some of the experts, with the offsets of all choices' rows: the share's rows against 64 bits, the others left alone."""
+    rng = gen(15)
+    E, k, N = 6, 2, 72
+    some, w, wide, _ = make_linear(rng, (hi - lo, N, K), "nvfp4", False)
+    x = torch.from_numpy(rng.standard_normal((T, K)).astype(np.float32)).to(BF16).cuda()
+    r = routing_of(some_ids(rng, T, k, E), E)
+    share = ex.Routing(r.ids, r.weights, r.counts[lo:hi].clone(), r.offsets[lo:hi + 1].clone(), r.slots, r.source)
+    values, offsets, source = ref.rounded(x.float().cpu().numpy(), "nvfp4"), r.offsets.cpu().numpy(), r.source.cpu().numpy()
+    want, tol = np.full((T * k, N), SENT), np.zeros((T * k, N))
+    for e in range(lo, hi):
+        a, b = offsets[e], offsets[e + 1]
+        want[a:b], tol[a:b] = product(values[source[a:b] // k], w[e - lo], wide[e - lo], None, F32)
+    rows = fp4.quantize_rows(x, routing=r)
+    for f in (lambda out: some(x, routing=share, out=out), lambda out: some.matmul(rows, offsets=share.offsets, out=out),
+              lambda out: some(ex.dispatch(x, r), offsets=share.offsets, out=out)):
+        out = torch.full((T * k, N), SENT, dtype=F32, device="cuda")
+        f(out)
+        within(out, want, tol)
+    some.check()
+
+
 def test_product_with_nothing_to_do():
     lin, _, _, _ = make_linear(gen(0), (64, 128), "nvfp4", True)
     assert lin(torch.zeros(0, 128, device="cuda", dtype=BF16)).shape == (0, 64)

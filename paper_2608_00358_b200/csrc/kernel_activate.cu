@@ -4,7 +4,7 @@
 // The generator is Philox-4x32-10 (Salmon, Moraes, Dror, Shaw 2011): four 32-bit words from a 128-bit counter and a 64-bit key in ten rounds of two 32 x 32 bit
 // products. Element i of the result (row * I + column) takes word i % 4 of the counter (i / 4, call); it is kept if the word is at least p 2^32.
 //
-// Measured (B200, copy peak 6.5 TB/s): SiLU, 32768 x 2048 bf16 without dropout 62 us, gradient 101; with dropout 92 and 105 (GELU 112 and 128): 32 instructions
+// Measured (B200, copy peak 6.5 TB/s): SiLU, 32768 x 2048 bf16 without dropout 62 us, gradient 101; with dropout 92 and 107 (GELU 111 and 127): 32 instructions
 // an element issue in two thirds of the cycles, about 10 of them the generator's (18 wide products for four elements, and what joins them).
 #include <algorithm>
 
@@ -97,25 +97,25 @@ __device__ __forceinline__ Two reciprocals(Two x) {
 }
 // 4 / (1 + exp(-x)): the quarter keeps the quotient of the largest exponentials a normal number.
 __device__ __forceinline__ Two four_logistic(Two x) { return reciprocals(fma2(exponentials(x * Two(-1.44269504f)), Two(0.25f), Two(0.25f))); }
-// The normal distribution, and exp(-x^2 / 2). Below 0 the distribution is exp(-x^2 / 2) R(|x|); R, which falls from 1/2 as slowly as 1 / |x|, is a polynomial of degree 7 in 1 / (1 + 0.35 |x|), by
+// The normal distribution times `part` (a power of two), and exp(-x^2 / 2). Below 0 the distribution is exp(-x^2 / 2) R(|x|); R, which falls from 1/2 as slowly as 1 / |x|, is a polynomial of degree 7 in 1 / (1 + 0.35 |x|), by
 // least squares on Chebyshev's points, weighted anew until the relative error was even: 2^-21.5 up to 14.6, where the exponential leaves the normal numbers. (normcdff with expf
 // takes four times the instructions, 32768 x 2048 bf16 with dropout 221 us, gradient 263.)
-__device__ __forceinline__ Two normal(Two x, Two* bell) {
+__device__ __forceinline__ Two normal(Two x, float part, Two* bell) {
     float a, b;
     x.get(a, b);
     const Two t = reciprocals(fma2(Two(fabsf(a), fabsf(b)), Two(0.35f), Two(1.f)));
-    Two r = fma2(Two(4.88590253e-02f), t, Two(-2.01797222e-01f));
-    r = fma2(r, t, Two(2.40131299e-01f));
-    r = fma2(r, t, Two(-1.65972006e-02f));
-    r = fma2(r, t, Two(1.55758767e-01f));
-    r = fma2(r, t, Two(1.33409697e-01f));
-    r = fma2(r, t, Two(1.40262654e-01f));
-    r = fma2(r, t, Two(-2.68791464e-05f));
+    Two r = fma2(Two(4.88590253e-02f * part), t, Two(-2.01797222e-01f * part));
+    r = fma2(r, t, Two(2.40131299e-01f * part));
+    r = fma2(r, t, Two(-1.65972006e-02f * part));
+    r = fma2(r, t, Two(1.55758767e-01f * part));
+    r = fma2(r, t, Two(1.33409697e-01f * part));
+    r = fma2(r, t, Two(1.40262654e-01f * part));
+    r = fma2(r, t, Two(-2.68791464e-05f * part));
     *bell = exponentials(x * x * Two(-0.72134752f));
     const Two below = *bell * r;
     float u, v, c, d;
     below.get(u, v);
-    fma2(below, Two(-1.f), Two(1.f)).get(c, d);
+    fma2(below, Two(-1.f), Two(part)).get(c, d);
     return Two(a < 0.f ? u : c, b < 0.f ? v : d);
 }
 
@@ -163,6 +163,7 @@ constexpr int RING = 4;
 template <typename T, int N, int V, bool GRAD, int ACT> __global__ void __launch_bounds__(THREADS) hccl_activate_rows(const __grid_constant__ ActivateParams p, int team) {
     constexpr bool SHORT = sizeof(T) == 2, RINGED = V == N;
     constexpr int INPUTS = GRAD ? 3 : 2;
+    constexpr float PART = GRAD ? 0.5f : 1.f;
     extern __shared__ __align__(16) uint4 ring[];  // [RING][INPUTS][threads]
     const int teams = THREADS / team, mine = (int)threadIdx.x / team, rank = (int)threadIdx.x % team;
     const long long rows = p.offsets ? min((long long)p.offsets[p.groups], p.M) : p.M;
@@ -227,37 +228,38 @@ template <typename T, int N, int V, bool GRAD, int ACT> __global__ void __launch
 #pragma unroll
             for (int j = 0; j < N; j++) u[j] = 1.f;
         if constexpr (GRAD) raw[INPUTS - 1].get(d);
-        // (What is dropped is 0, whatever it was. Large numbers meet the small factor first: -1e30 of a gate and 1e30 of the other half are 0, not infinity times 0.)
+        // What is dropped is 0, whatever it was. Of finite numbers no product on the way is infinite unless the result is: large numbers meet the activation first (-1e30 of a gate and
+        // 1e30 of the other half are 0), 1 / (1 - p), which only makes larger, comes last, and a slope, up to 1.13, meets the gradient by its half (PART). (A product below 2^-126 is rounded
+        // to 2^-149 before it grows.)
         if constexpr (SHORT && ACT != HCCL_ACT_RELU) {
 #pragma unroll
             for (int j = 0; j < N; j += 2) {
-                const Two x(g[j], g[j + 1]), o(u[j], u[j + 1]);
-                Two f, bell;  // act(x) = x f
-                if constexpr (ACT == HCCL_ACT_SILU) f = four_logistic(x);
-                else f = normal(x, &bell);
+                const Two x(g[j], g[j + 1]), o(u[j], u[j + 1]), grown(p.keep / PART);
+                Two f, bell;  // act(x) = x f / PART
+                if constexpr (ACT == HCCL_ACT_SILU) f = four_logistic(x) * Two(0.25f * PART);
+                else f = normal(x, PART, &bell);
+                const Two act = x * f;
                 if constexpr (!GRAD) {
-                    (x * (f * Two(ACT == HCCL_ACT_SILU ? 0.25f * p.keep : p.keep)) * o).get(g[j], g[j + 1]);
+                    (act * o * grown).get(g[j], g[j + 1]);
                 } else {
-                    if constexpr (ACT == HCCL_ACT_SILU) f = f * Two(0.25f);
-                    const Two act = x * f, dd = Two(d[j], d[j + 1]) * Two(p.keep);
+                    const Two dd(d[j], d[j + 1]);
                     Two slope;
-                    if constexpr (ACT == HCCL_ACT_SILU) slope = fma2(act, fma2(f, Two(-1.f), Two(1.f)), f);
-                    else slope = fma2(x * Two(0.39894228f), bell, f);
-                    (dd * slope * o).get(g[j], g[j + 1]);
-                    (dd * act).get(u[j], u[j + 1]);
+                    if constexpr (ACT == HCCL_ACT_SILU) slope = fma2(act, fma2(f, Two(-1.f / PART), Two(1.f)), f);
+                    else slope = fma2(x * Two(0.39894228f * PART), bell, f);
+                    (dd * slope * o * grown).get(g[j], g[j + 1]);
+                    (dd * act * grown).get(u[j], u[j + 1]);
                 }
             }
         } else {
 #pragma unroll
             for (int j = 0; j < N; j++) {
                 if constexpr (!GRAD) {
-                    g[j] = activation(ACT, g[j]) * (u[j] * p.keep);
+                    g[j] = activation(ACT, g[j]) * u[j] * p.keep;
                 } else {
                     float a, slope;
                     activation_slope(ACT, g[j], &a, &slope);
-                    const float dd = d[j] * p.keep;
-                    g[j] = dd * slope * u[j];
-                    u[j] = dd * a;
+                    g[j] = d[j] * (PART * slope) * u[j] * (p.keep / PART);
+                    u[j] = d[j] * a * p.keep;
                 }
             }
         }

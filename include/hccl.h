@@ -696,7 +696,8 @@ hccl_status_t hccl_expert_layer_fp4(const hccl_experts_fp4_t*, const void* x, in
 /* What stands between an expert's two products in training: y[r,i] = act(x[r,i]) * x[r,I+i] * m[r,i] (x [M, 2 I]; not gated: x [M, I], y = act(x) m), and its gradient
  * dx for a gradient dy [M, I] of y. m is 0 or 1 / (1 - p), from Philox-4x32-10 with the key seed[0] and the counter (n / 4, seed[1]), n = r * I + i: kept
  * if word n % 4 is at least p 2^32 rounded (p 2^32 at most 2^32 - 1). The mask is not stored; the same seed gives it again. A dropped element and its gradient are 0, whatever x is. seed: two int64 in device
- * memory, not read if p is 0. groups > 0: rows from offsets[groups] on (device memory) are not read and become 0 in y and dx. One rounding at the end. */
+ * memory, not read if p is 0. groups > 0: rows from offsets[groups] on (device memory) are not read and become 0 in y and dx. Everything in FP32 (act and its slope, of 16-bit x, with what is
+ * below 2^-123 as 0), one rounding at the end; of finite x and dy a result is infinite or NaN only where the formula's is beyond the type. */
 typedef struct {
     int32_t act, gated;
     double p;             /* from 0 to below 1 */

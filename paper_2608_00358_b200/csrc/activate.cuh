@@ -5,13 +5,17 @@
 namespace hccl {
 namespace experts {
 
-// 1 / x within 1 ulp, subnormal results too.
+// 1 / x within 1 ulp.
 __device__ __forceinline__ float reciprocal(float x) {
     float r;
     asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float logistic(float x) { return reciprocal(1.f + expf(-x)); }  // 1 / (1 + exp(-x))
+// 1 / (1 + exp(-x)), by an exponential that is never infinite.
+__device__ __forceinline__ float logistic(float x) {
+    const float e = expf(-fabsf(x)), r = reciprocal(1.f + e);
+    return x >= 0.f ? r : e * r;
+}
 __device__ __forceinline__ float activation(int act, float g) {
     if (act == HCCL_ACT_SILU) return g * logistic(g);
     if (act == HCCL_ACT_GELU) return g * normcdff(g);

@@ -62,3 +62,33 @@ def test_numbers_up_to_the_types_largest(gated, p, act, dt):
     if gated:
         do = d64 * a * f
         near(dx[:, I:], do, rounding(do), dt)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_silu_where_the_exponential_leaves_the_range(p, dt):
+    """Gates from -91 to -86, where exp(-g) passes 2^128 and the activation is still above 2^-126: times another half or a gradient of 1e37 that is a number of order 1."""
+    g = torch.linspace(-91, -86, 64).to(dt).repeat(6, 1)
+    o = torch.tensor([1.0, -1.0, 1e20, 1e37, -1e37, 0.0]).to(dt)[:, None].expand(6, 64)
+    d = torch.tensor([1.0, 1e30, -1.0, 1.0, 1.0, 1e37]).to(dt)[:, None].expand(6, 64)
+    key = (9, 9)
+    f = np.full((6, 64), 1 / (1 - p)) * (ref.keep(6, 64, p, key) if p else 1)
+    seed = seed_of(*key) if p else None
+    x = torch.cat((g, o), 1).cuda()
+    g64, o64, d64 = (v.double().numpy() for v in (g, o, d))
+    a, s, _ = ref.act("silu", g64)
+    # In 32 bits exp(g) is a subnormal number: 2 units of 2^-149 off, times |g| up to 91 and another half for each of the products. Of 16-bit gates the exponential's argument, up to
+    # 131, is off by 2^-17 and by what its constant's rounding leaves, and the exponential by as much.
+    each = 2.0 ** -20 if dt == F32 else 2.0 ** -16
+    da, ds = each * np.abs(a) + 250 * 2.0 ** -149, each * np.abs(s) + 250 * 2.0 ** -149
+
+    def check(got, want, tol):
+        tol = tol + eref.HALF_ULP[dt] * np.abs(want) * 1.01 + 2 * eref.SMALLEST[dt]
+        got = got.double().cpu().numpy()
+        assert (np.abs(got - want) <= tol).all(), (got[np.abs(got - want) > tol][:4], want[np.abs(got - want) > tol][:4])
+
+    check(activate(x, "silu", True, p, seed), a * o64 * f, da * np.abs(o64) * f)
+    dx = activate_backward(d.contiguous().cuda(), x, "silu", True, p, seed)
+    check(dx[:, :64], d64 * s * o64 * f, ds * np.abs(d64 * o64) * f)
+    check(dx[:, 64:], d64 * a * f, da * np.abs(d64) * f)
+    assert (np.abs(a * 1e37) > 0.1).all()

@@ -120,7 +120,7 @@ def quantize_rows(x: torch.Tensor, format: str = "nvfp4", scale: float = 1.0, ro
 
 class Fp4Linear:
     """y = x W^T (+ bias) with W in 4-bit floating point: weight uint8 [N, (K + 1) // 2] or [experts, N, (K + 1) // 2], scale (bytes of e4m3 or powers of
-    two) [.., N, blocks], tensor_scale fp32 [1] or [experts] ("nvfp4"; default ones), bias fp32 [N] or [experts, N]. The rows of x are quantised to the same
+    two) [.., N, blocks], tensor_scale fp32 [1] or [experts], by which each matrix is multiplied (default ones), bias fp32 [N] or [experts, N]. The rows of x are quantised to the same
     format within the call, "nvfp4" with the 32-bit scale x_scale. K: the width, where it is odd. Scales, and weights whose rows do not start on 16-byte
     boundaries, are laid out anew once, here. A result's rows beyond the last expert's are left alone. For serving: an input that requires a gradient is refused."""
 
@@ -142,7 +142,7 @@ class Fp4Linear:
             _refuse(hb.ERR_COUNT_MISMATCH, "Fp4Linear: scale is %s, expected %s" % (tuple(scale.shape), tuple(weight.shape[:-1] + (blocks,))))
         if scale.get_device() != self.dev:
             _refuse(hb.ERR_INVALID_ARG, "Fp4Linear: scale must be on cuda:%d" % self.dev)
-        if tensor_scale is None or format == "mxfp4":
+        if tensor_scale is None:
             tensor_scale = torch.ones(G, dtype=torch.float32, device=self.device)
         _vector(tensor_scale, "tensor_scale", torch.float32, G, self.dev)
         if bias is not None:

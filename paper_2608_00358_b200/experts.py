@@ -46,10 +46,10 @@ def _no_tangent(t: torch.Tensor, what: str):
         _refuse(hb.ERR_INVALID_ARG, "%s has a tangent; there is no forward-mode derivative" % what)
 
 
-def _no_gradient(t: torch.Tensor, what: str):
-    """Refuses what autograd would follow: rows in 8 bits have no gradient, and a result that only looks differentiable stops training without a word."""
+def _no_gradient(t: torch.Tensor, what: str, of: str = "8-bit rows have"):
+    """Refuses what autograd would follow: rows in 8 or 4 bits have no gradient, and a result that only looks differentiable stops training without a word."""
     if t.requires_grad and torch.is_grad_enabled():
-        _refuse(hb.ERR_INVALID_ARG, "%s requires a gradient, and 8-bit rows have none: detach it or call under torch.no_grad()" % what)
+        _refuse(hb.ERR_INVALID_ARG, "%s requires a gradient, and %s none: detach it or call under torch.no_grad()" % (what, of))
 
 
 def _given(t: torch.Tensor, what: str):

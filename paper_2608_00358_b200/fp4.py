@@ -106,7 +106,7 @@ def quantize_rows(x: torch.Tensor, format: str = "nvfp4", scale: float = 1.0, ro
     routing the rows come in expert order (n_rows: the capacity, default tokens * top_k; rows that no choice fills are left alone). Rows start 16 bytes
     apart or a multiple of it."""
     fmt, wide = _format(format), _wide(scale, format)
-    _no_gradient(x, "x")
+    _no_gradient(x, "x", "4-bit rows have")
     ldx, dt, dev = _matrix(x, "x", dev=None if routing is None else routing.dev), _dtype(x, "x"), x.get_device()
     M, K = x.shape
     n = M if routing is None else (routing.tokens * routing.top_k if n_rows is None else n_rows)
@@ -225,7 +225,7 @@ class Fp4Linear:
         """x [M, K]. Over experts: with a routing, x holds tokens and row r of the result belongs to choice source[r]; with offsets (int32
         [experts + 1], on the device) x is in expert order already."""
         dev = self.dev
-        _no_gradient(x, "x")
+        _no_gradient(x, "x", "4-bit rows have")
         ldx, dt = _matrix(x, "x", self.K, None, dev), _dtype(x, "x")
         self._which(routing, offsets)
         M, record = x.shape[0], 0
@@ -298,8 +298,8 @@ class FewTokens:
     def __call__(self, x: torch.Tensor, routing: Routing, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [tokens, H], its routing; returns [tokens, H] in x's type."""
         dev, T, k = self.dev, routing.tokens, routing.top_k
-        _no_gradient(x, "x")
-        _no_gradient(routing.weights, "the routing's weights")
+        _no_gradient(x, "x", "FewTokens has")
+        _no_gradient(routing.weights, "the routing's weights", "FewTokens has")
         ldx, dt = _matrix(x, "x", self.H, T, dev), _dtype(x, "x")
         if routing.experts != self.up.experts or routing.dev != dev:
             _refuse(hb.ERR_COUNT_MISMATCH, "FewTokens: routing over %d experts on %s" % (routing.experts, routing.device))

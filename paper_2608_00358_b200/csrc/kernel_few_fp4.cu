@@ -231,9 +231,8 @@ template <typename Full> __device__ __forceinline__ void drain(const Full& full,
     if (status) *status = HCCL_ERR_TIMEOUT;
 }
 
-// Four elements of act(gate) * other from partial sums, `apart` fours apart; other: how far the other half is, 0: no gate. A function, so that a warp with nothing else
-// to do can fetch its code ahead of time: on the few blocks that finish others' sums that was half of what it took.
-__device__ __noinline__ float4 activated(const float4* from, long long apart, int other, int parts, int act) {
+// Four elements of act(gate) * other from partial sums, `apart` fours apart; other: how far the other half is, 0: no gate.
+__device__ __forceinline__ float4 activated(const float4* from, long long apart, int other, int parts, int act) {
     float4 g = make_float4(0.f, 0.f, 0.f, 0.f), o = g;
     if (from)
 #pragma unroll 1
@@ -309,7 +308,8 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
     }
     constexpr int blocks = SMS;
     if (warp >= 8) {
-        // While the chunks are listed: what comes first from memory is asked for, a share by each block, and the code that makes pieces is fetched by running it.
+        // While the chunks are listed: what comes first from memory is asked for, a share by each block, and the code that makes pieces is fetched by running it (one token through 8 of 64
+        // experts of 4096 x 2048 35.6 us, without 36.9).
         const int lines = (p.K * (int)sizeof(T) + 127) / 128;  // of a row (one that begins between two reaches into one more: that is fetched when it is needed)
         for (int i = (int)(blockIdx.x * SPLITTERS + threadIdx.x) - 256; i < lines * p.T; i += blocks * SPLITTERS) {
             const int t = divide(i, lines);
@@ -524,10 +524,6 @@ template <typename T, int FORMAT> __global__ void __launch_bounds__(UP_THREADS, 
             asm volatile("bar.sync 2, 256;" ::: "memory");
             if (me < ROWS) top_of[half][me] = 0;
         }
-    }
-    else if (warp == 3) {
-        const float4 x = activated((const float4*)p.sums, 0, 1, 1, p.act);  // (whatever lies there)
-        if (__float_as_int(x.x) == 0x7fc12345) held[lane] = x;               // (so that it is run: no sum has these bits)
     }
     if (warp == 0 && lane == 0 && *(volatile int*)&gave_up) drain(full, S::STAGES, it, p.status);
     __syncwarp();

@@ -34,3 +34,38 @@ def test_a_matrixs_own_scale_counts_in_both_formats(experts, fmt):
     for f in (lambda v: v, copy.copy, copy.deepcopy, lambda v: pickle.loads(pickle.dumps(v))):
         assert torch.equal(f(lin)(cuda(x), offsets=off) * 2, y)
     refused(hb.ERR_COUNT_MISMATCH, lambda: fp4.Fp4Linear(cuda(flat), cuda(scale), torch.ones(G + 1, device="cuda"), format=fmt))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T,H,I,E,k", [(1, 512, 256, 8, 8), (40, 264, 136, 3, 2), (64, 4100, 40, 32, 4), (3, 96, 2100, 2, 2)])
+def test_scratch_may_hold_anything(monkeypatch, T, H, I, E, k, fmt):
+    """The layer and the products give the same bits whatever earlier calls left in their scratch."""
+    rng = gen(T)
+    up, _, _, _ = make_linear(rng, (E, 2 * I, H), fmt, False)
+    down, _, _, _ = make_linear(rng, (E, H, I), fmt, False)
+    for lin in (up, down):
+        lin.tensor_scale.mul_(2.0 ** -10)
+    few = fp4.FewTokens(up, down)
+    x = cuda(rng.standard_normal((T, H)).astype(np.float32))
+    r = routing_of(some_ids(rng, T, k, E, 0.1), E)
+    seen = []
+
+    class Filled:
+        def __init__(self, byte):
+            self.byte = byte
+
+        def get(self, dev, stream, nbytes):
+            t = torch.full((nbytes,), self.byte, dtype=torch.uint8, device="cuda")
+            seen.append(nbytes)
+            return t, t.data_ptr()
+
+    results = []
+    for byte in (0, 0xFF, 0x7F, 0x3A):
+        monkeypatch.setattr(fp4, "_scratch", Filled(byte))
+        n = int(r.offsets[-1])
+        results.append((few(x, r), up(x, routing=r)[:n], up.matmul(fp4.quantize_rows(x, fmt, routing=r), offsets=r.offsets)[:n]))
+    assert len(seen) == 12 and results[0][0].any() and torch.isfinite(results[0][0]).all()
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+    few.check()
+    up.check()

@@ -1,4 +1,4 @@
-"""Gated activations on the GPU where the range ends."""
+"""Gated activations on the GPU where the range ends, and where a thread has many rows."""
 import numpy as np
 import pytest
 import torch
@@ -7,7 +7,7 @@ import expert_reference as eref
 import fp4_reference as ref
 from paper_2608_00358_b200.activation import activate, activate_backward
 from test_gpu_activation import seed_of
-from test_gpu_experts import BF16, F16, F32
+from test_gpu_experts import BF16, F16, F32, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +92,74 @@ def test_silu_where_the_exponential_leaves_the_range(p, dt):
     check(dx[:, :64], d64 * s * o64 * f, ds * np.abs(d64 * o64) * f)
     check(dx[:, 64:], d64 * a * f, da * np.abs(d64) * f)
     assert (np.abs(a * 1e37) > 0.1).all()
+
+
+# ------------------------------------------------------------------------------------------------ threads that walk from row to row
+def words(n, key):
+    """The first n words of the generator, on the device."""
+    M32 = 0xFFFFFFFF
+
+    def product(a, m):  # high and low half, a below 2^32
+        lo = a * (m & 0xFFFF)
+        mid = a * (m >> 16) + (lo >> 16)
+        return mid >> 16, ((mid & 0xFFFF) << 16) | (lo & 0xFFFF)
+
+    at = torch.arange(-(-n // 4), device="cuda")
+    c = [at & M32, at >> 32, torch.full_like(at, key[1] & M32), torch.full_like(at, (key[1] >> 32) & M32)]
+    k = [key[0] & M32, (key[0] >> 32) & M32]
+    for _ in range(10):
+        (h0, l0), (h1, l1) = product(c[0], 0xD2511F53), product(c[2], 0xCD9E8D57)
+        c = [h1 ^ c[1] ^ k[0], l1, h0 ^ c[3] ^ k[1], l0]
+        k = [(k[0] + 0x9E3779B9) & M32, (k[1] + 0xBB67AE85) & M32]
+    return torch.stack(c, -1).flatten()[:n]
+
+
+def test_the_words_on_the_device_are_those_of_the_reference():
+    key = (-(2 ** 61) - 99, 2 ** 45 + 7)
+    assert (words(1002, key).cpu().numpy() >= 2 ** 31).tolist() == ref.keep(1, 1002, 0.5, key)[0].tolist()
+
+
+@pytest.mark.parametrize("M,I,p,gated,act,dt", [
+    # 148 * 12 blocks at most with dropout, 148 * 64 without, of 4 rows (up to 32 pieces of 16 bytes in a row) to 1: each thread has three rows or more, or some two
+    (16000, 40, 0.1, True, "silu", BF16), (80000, 24, 0.0, True, "gelu", F16), (12001, 33, 0.3, True, "relu", F32), (90000, 9, 0.0, False, "silu", F32),
+    (5000, 1504, 0.25, True, "gelu", BF16), (20000, 1100, 0.0, False, "silu", BF16), (21000, 1280, 0.0, True, "silu", F16), (4000, 999, 0.1, True, "silu", F32),  # two pieces of a row
+    (4000, 3000, 0.1, True, "gelu", F32), (3000, 6200, 0.5, False, "gelu", F16), (3600, 5000, 0.2, True, "relu", BF16),  # more pieces than are on their way at once
+])
+def test_rows_one_after_the_other(M, I, p, gated, act, dt):
+    """Every element of value and gradient against 64 bits where a thread goes on from row to row, with rows that are read no further than the last expert's, and at other alignments."""
+    g = torch.Generator(device="cuda").manual_seed(M + I)
+    W = 2 * I if gated else I
+    x, dy = (2 * torch.randn((M, W), device="cuda", generator=g)).to(dt), torch.randn((M, I), device="cuda", generator=g).to(dt)
+    key, last = (M * 2 ** 33 + 5, -I), M - M // 3 - 1
+    f = torch.full((M, I), 1 / (1 - p), dtype=torch.float64, device="cuda")
+    if p:
+        f *= (words(M * I, key) >= round(p * 2.0 ** 32)).view(M, I)
+    seed = seed_of(*key) if p else None
+    g64, o64, d64 = x[:, :I].double(), x[:, I:].double() if gated else 1.0, dy.double()
+    if act == "silu":
+        s = torch.sigmoid(g64)
+        a, slope = g64 * s, s * (1 + g64 * (1 - s))
+    elif act == "gelu":
+        phi = 0.5 * torch.special.erfc(-g64 * 0.5 ** 0.5)
+        a, slope = g64 * phi, phi + g64 * torch.exp(-0.5 * g64 * g64) * (0.5 / np.pi) ** 0.5
+    else:
+        a, slope = g64.clamp(min=0), (g64 > 0).double()
+    off = torch.tensor([0, last // 3, last], dtype=torch.int32, device="cuda")
+    for shift, pad, offsets in ((0, 0, None), (0, 0, off), (8, 8, off), (1, 3, off)):
+        if offsets is not None:
+            f[last:] = 0
+            x[last:] = float("nan")
+        half, least = eref.HALF_ULP[dt] * 1.01, eref.SMALLEST[dt]
+
+        def check(got, want, tol):
+            want, tol = (torch.where(f == 0, 0.0, v) for v in (want, tol))  # (what is dropped, and rows that are not read: 0)
+            assert ((got.double() - want).abs() <= tol + half * want.abs() + least).all(), (shift, pad)
+
+        y = a * o64 * f
+        xs, ds = strided(x, pad, shift), strided(dy, pad, shift)
+        check(activate(xs, act, gated, p, seed, offsets), y, 2.0 ** -20 * y.abs())
+        dx = activate_backward(ds, xs, act, gated, p, seed, offsets)
+        check(dx[:, :I], d64 * slope * o64 * f, 2.0 ** -20 * (d64 * o64 * f).abs() * (1 + g64.abs()))
+        if gated:
+            do = d64 * a * f
+            check(dx[:, I:], do, 2.0 ** -20 * do.abs())

@@ -72,7 +72,7 @@ struct FewParams {
     const int *offsets, *source;
     const float *weights, *wide, *bias;
     int* status;
-    int K, N, I, k_blocks, down_blocks /* stages of the second product */, down_parts;
+    int K, N, I, k_blocks, down_parts /* parts of the second product's K */;
     int chan_tiles;        // up: of a half; down: of all channels
     int experts, top_k, T, rows /* T * top_k */, act, gated, half /* I, up to a multiple of 8 */, width /* of a row of sums: half, or both halves */, vec;
 };
@@ -938,7 +938,6 @@ template <typename T, int FORMAT> cudaError_t few(const FewFp4& q, cudaStream_t 
     p.half = (int)at.half;
     p.width = (int)at.width;
     p.pitch = at.pitch;
-    p.down_blocks = (int)((q.I + 255) / 256);
     p.down_parts = (int)at.parts;
     p.chunk_count = (int*)(q.scratch + at.counts);
     p.tile_count = p.chunk_count + rows * at.parts;

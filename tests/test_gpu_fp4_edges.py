@@ -235,3 +235,40 @@ def test_rows_cross_an_exchange_in_4_bits(R, k, tokens, hidden, inner, fmt):
     for s, r in enumerate(routings):
         want = ex.combine(down(activate(up(x[s], routing=r), offsets=r.offsets), offsets=r.offsets), r)
         assert want.any() and torch.equal(ex.combine(back[s][:, :hidden], r), want), s
+
+
+# ------------------------------------------------------------------------------------------------ the longest rows
+LONGEST = 131072
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,N,K,dt", [(5, 40, LONGEST, BF16), (300, 130, LONGEST - 1, F32), (70, 129, LONGEST, F16)])
+def test_product_of_the_longest_rows(M, N, K, dt, fmt):
+    rng = gen(M)
+    lin, w, wide, _ = make_linear(rng, (N, K), fmt, False)
+    lin.tensor_scale.mul_(2.0 ** -12), wide.__imul__(2.0 ** -12)
+    x = torch.from_numpy(rng.standard_normal((M, K)).astype(np.float32)).to(dt)
+    codes, scale = ref.quantise(x.float().numpy(), fmt)
+    rows = fp4.quantize_rows(x.cuda(), fmt)
+    assert np.array_equal(rows.q.cpu().numpy(), ref.pack(codes)) and np.array_equal(rows.scale.cpu().numpy(), scale)
+    want = torch.from_numpy(ref.values(codes, scale, fmt).astype(np.float32))
+    assert torch.equal(rows.dequantize().cpu(), want)
+    inside(lin(x.cuda()), *product_on_the_device(want.double().cuda(), cuda(w[0]), float(wide[0]), None, dt))
+    refused(hb.ERR_INVALID_ARG, lambda: fp4.quantize_rows(torch.zeros(1, LONGEST + 1, device="cuda"), fmt))
+    lin.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T,H,I,E,k", [(2, LONGEST, 24, 2, 2), (3, 40, LONGEST, 2, 1)])
+def test_layer_of_the_longest_rows(T, H, I, E, k, fmt):
+    rng = gen(H)
+    up, wu, _, _ = make_linear(rng, (E, 2 * I, H), fmt, False)
+    down, wd, _, _ = make_linear(rng, (E, H, I), fmt, False)
+    for lin, n in ((up, H), (down, I)):
+        lin.tensor_scale.mul_(1 / (np.sqrt(n) * 150 if fmt == "nvfp4" else np.sqrt(n) / 4))
+    gu, gd = up.tensor_scale.double().cpu().numpy(), down.tensor_scale.double().cpu().numpy()
+    x, ids, weights = rng.standard_normal((T, H)).astype(np.float32), some_ids(rng, T, k, E), rng.random((T, k)).astype(np.float32)
+    want, tol = layer_reference(x.astype(np.float64), ids, weights.astype(np.float64), (wu, gu, None), (wd, gd, None), "silu", True, fmt, F32)
+    few = fp4.FewTokens(up, down)
+    within(few(cuda(x), routing_of(ids, E, weights)), want, tol)
+    few.check()

@@ -629,7 +629,8 @@ hccl_status_t hccl_linear_i8(const hccl_matmul_i8_t*, const void* x, int64_t ldx
  * Elements are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and negatives), two to a byte, the earlier in the low half. Every block of a row has a step d, and
  * q = e2m1(x / d): the quotient rounded to FP32, then to the nearest element, ties to even, beyond 6 to 6.
  * HCCL_NVFP4: 16 elements; the stored byte is s = e4m3(min(max|x| / (6 g), 448)) with the matrix's FP32 scale g, each step rounded to FP32, and d = s g.
- * HCCL_MXFP4: 32 elements; the byte e stands for d = 2^(e - 127), the least with max|x| <= 6 d (from 2^-126 on); g is not used. Nothing saturates.
+ * HCCL_MXFP4: 32 elements; the byte e stands for d = 2^(e - 127), the least with max|x| <= 6 d (from 2^-126 on); g is not used. Nothing saturates. (The conversion of OCP's microscaling
+ * specification takes e - 127 = floor(log2 max|x|) - 2 and saturates: where the largest magnitude is more than 1.5 times a power of two, half this step. Rows converted so are read the same.)
  * A block with an infinity or a NaN has the scale NaN (0x7f, 0xff) and stands for NaN throughout. A block's last elements may lie beyond K. */
 typedef enum { HCCL_NVFP4 = 0, HCCL_MXFP4 = 1 } hccl_fp4_t;
 
@@ -678,7 +679,7 @@ hccl_status_t hccl_linear_fp4(const hccl_matmul_fp4_t*, const void* x, int64_t l
  * u = up_e x[t] + up_bias_e and h = act(u[0..I-1]) * u[I..2I-1] if gated, act(u) otherwise. Weights in 4 bits as in hccl_matmul_fp4_t: up [experts, 2 I or I, H], down
  * [experts, H, I], their scales from hccl_fp4_weight_scales (up's, if gated, laid
  * out as 2 * experts groups of I rows, which for I a multiple of 128 is the same). Activations are not rounded to 4 bits: they enter the products as sums of eight such numbers, which leaves 2^-22 of the largest
- * of up to 1024 neighbours; sums, u and h are FP32. A row with an infinity or a NaN gives NaN. Choices without an expert add nothing; a token without any gets 0.
+ * of up to 1024 neighbours (and at least 2^-127); sums, u and h are FP32. A row with an infinity or a NaN gives NaN. Choices without an expert add nothing; a token without any gets 0.
  * Reads the routing's weights, offsets and source; offsets may begin after 0 (some of the experts of a larger routing: the rows of the others add nothing). tokens <= HCCL_MAX_FEW_TOKENS; H and I from 1 to HCCL_MAX_FP4_K. scratch: hccl_expert_layer_scratch_bytes, 128-byte aligned, contents
  * arbitrary, not shared by calls in flight at once. dev_status as in hccl_matmul_i8_t. */
 #define HCCL_MAX_FEW_TOKENS 64

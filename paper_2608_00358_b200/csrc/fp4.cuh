@@ -2,8 +2,8 @@
 //
 // An element is e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two to a byte, the earlier in the low half. A block has a step d that
 // all its elements are multiples of. NVFP4: 16 elements, a byte s = e4m3(max|x| / (6 g)) and d = s g with a 32-bit g for the whole matrix. MXFP4: 32
-// elements, a byte e, d = 2^(e - 127), the least e with max|x| <= 6 d. q = e2m1(x / d), the quotient rounded to 32 bits, ties to even. A
-// block with an infinity or a NaN has the scale NaN (0x7f, 0xff).
+// elements, a byte e, d = 2^(e - 127), the least e with max|x| <= 6 d (not OCP's floor(log2 max|x|) - 2,
+// which cuts up to a quarter off a block's largest elements: nothing saturates here). q = e2m1(x / d), the quotient rounded to 32 bits, ties to even. A block with an infinity or a NaN has the scale NaN (0x7f, 0xff).
 //
 // Scales lie in two ways. By rows: [rows][blocks], for exchange and storage. In tiles, as the tensor cores take them: an atom of 512 bytes holds 128 rows x 4 blocks, the
 // four bytes of row r at (r % 32) * 16 + (r / 32) * 4; atoms of a tile's successive blocks follow one another, up to whole stages of 256 elements.

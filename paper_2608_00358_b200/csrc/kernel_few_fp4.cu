@@ -1,9 +1,10 @@
-// A whole expert layer for a few tokens in two kernels: y[t] = sum over j of w[t, j] down_e(act(up_e(x[t]))), weights in 4-bit floating point, activations not rounded.
+// A whole expert layer for a few tokens in two kernels: y[t] = sum over j of w[t, j] down_e(act(up_e(x[t]))), weights in 4-bit floating point, activations as numbers of 22 bits.
 //
 // With few tokens the chosen experts' weights are read once and that is the time, so 4-bit activations would save nothing and cost accuracy. The tensor cores multiply 4-bit
 // numbers by 4-bit numbers all the same: an activation goes in as the sum of eight of them. 1024 elements of a row (or what there is) are brought to whole numbers below 2^22 by a power of
 // two, which leaves less than 2^-22 of their largest, and written with eight digits from -4 to 3 in base 8; half a digit is an e2m1 number, and its scale, a power of 8, the same for all blocks.
-// Four digits span what one byte's scale can: the last four columns have the scales of the first four again, and their sum 8^-4 of the weight. Eight columns is also the least that an
+// Fewer bits than a 32-bit number's own, by choice: beside a row's largest element the others lose what a 32-bit sum with its product loses four times over (2^-22 of it against 2^-24), and more digits would
+// be more columns. Four digits span what one byte's scale can: the last four columns have the scales of the first four again, and their sum 8^-4 of the weight. Eight columns is also the least that an
 // instruction computes: a token's eight digits are its eight columns, and for one token they cost nothing. The sum over them is taken in 32 bits.
 //
 // Rows in expert order are taken in chunks of at most 8 rows of one expert. Both kernels run one block to an SM, and weights never wait for anything but room:
@@ -17,8 +18,9 @@
 //
 // All sums have a fixed order: results repeat bit for bit.
 //
-// Measured (B200, copy peak 6.5 TB/s): one token through 8 of 64 experts of 4096 x 2048 36 us in replays of a graph, 47 after a flush of the caches; 8 experts of 8192 x 8192, one token 103 + 53 us
-// = 5.9 TB/s of weights and 8 tokens 136 + 55; 19 tokens through 4 of 60 experts of 2056 x 1416 67 us. Of the 36 us the weights take 17 at the copy rate. The rest are latencies in a row: 5 until the first pieces are
+// Measured (B200, copy peak 6.5 TB/s): one token through 8 of 64 experts of 4096 x 2048 35 us in replays of a graph, 45 to 47 after a flush of the caches; 8 experts of 8192 x 8192, one token 103 + 53 us
+// = 5.9 TB/s of weights and 8 tokens 133 + 55; 19 tokens through 4 of 60 experts of 2056 x 1416 68 us. With many tokens and few channels the second kernel's last sums are the time: 50 tokens through 2 of
+// 8 experts of 128 x 192 17 + 90 us. Of the 35 us the weights take 17 at the copy rate. The rest are latencies in a row: 5 until the first pieces are
 // there, 1.5 to count, 5 for a block to finish others' sums, 3 to the second kernel's first product, 4 for its last sums, and a memory set and two launches.
 #include <algorithm>
 #include <atomic>

@@ -11,7 +11,8 @@
 //
 // Measured (B200; four times the bf16 library rate is 6.7 PFLOP/s): 8192^3 176-197 us on different machines = 5.6-6.3 PFLOP/s at the power limit, tensor cores active in 75 % of the cycles; a
 // stage's products take 512 cycles and its bytes 594 of shared memory's (2 x 38 KB written and read at 128 a cycle), so shared memory is the next bound. 64 matrices 2048 x 4096: 65536 rows
-// 241-265 us, 512 rows 53 us = 5.7 TB/s of weights. 997 x 4104 x 2064 12 us; 16 rows, 8192 x 4096, 10 us with cold weights, most of it set-up and the first stages' way.
+// 241-265 us, 512 rows 52 us = 5.8 TB/s of weights. 997 x 4104 x 2064 12 us; 1 to 16 rows, 8192 x 4096, 10 to 11 us with cold weights (with the quantiser 10.3 us in replays of a graph, 14.4 after a flush
+// of the caches), most of it set-up and the first stages' way.
 #include <atomic>
 
 #include "fp4.cuh"

